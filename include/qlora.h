@@ -198,6 +198,93 @@ int qlora_unpack(int bits, int K, int N, const int32_t* Q, uint8_t* codes, void*
 int qlora_lrec_loss(int T, int V, const void* student_logits, const void* teacher_logits, const int32_t* labels, float lambda_kl,
                     float lambda_ce, float grad_scale, float* loss_tokens, void* dlogits, void* cuda_stream);
 
+/* Element types of the tensors that the calls below take in more than one. */
+enum { QLORA_BF16 = 0, QLORA_FP16 = 1, QLORA_FP32 = 2, QLORA_E4M3 = 3 };
+
+/* Log probabilities of given tokens, with the entropy of each row and its most likely alternatives: what an evaluation
+ * (perplexity: Section 4, Table 2), a generation loop or a cache of teacher targets (Appendix C) takes from the logits.
+ * Per row z of V logits, with c = inv_temperature and p = softmax(c z):
+ *     logprobs[t]        = log p[tokens[t]]                          (0 where tokens[t] is outside [0, V))
+ *     entropy[t]         = - sum_j p_j log p_j
+ *     top_ids[t, i], top_logprobs[t, i] = the i-th largest logit's place and its log p, i < k; equal logits (-0 and 0
+ *                          among them) in the order of their places
+ *     stats[t, 0 .. 2]   = max_j z_j,  log sum_j exp(c (z_j - max z)),  entropy    (what the backward call reads)
+ * logits: dtype QLORA_BF16, QLORA_FP16 or QLORA_FP32, [T, V] with rows row_stride >= V elements apart; unlike the other
+ * tensors they may begin at any element (a vocabulary of an odd size, a batch without its first token).  tokens: int32
+ * [T], or NULL when logprobs is NULL.  logprobs, entropy: fp32 [T]; top_ids int32 [T, k], top_logprobs fp32 [T, k]; stats
+ * fp32 [T, 3]; each of them may be NULL, not all.  0 <= k <= QLORA_MAX_TOP and k <= V (k = 0: no alternatives; both
+ * arrays NULL); inv_temperature > 0 and finite; V <= 2^24.
+ * Masked logits (-inf, or the type's lowest value) have probability 0 and add nothing to the sums; a row with nothing
+ * above -inf has log p = -inf everywhere and entropy 0; a row that holds a NaN or +inf has no distribution: its numbers
+ * are NaN, its places are ordered all the same (a NaN counts as larger than anything).
+ * fp32 arithmetic, fixed-order sums (bitwise reproducible).  The logits are read once. */
+#define QLORA_MAX_TOP 64
+int qlora_token_logprobs(int T, int V, long long row_stride, int dtype, const void* logits, const int32_t* tokens,
+                         float inv_temperature, int k, float* logprobs, float* entropy, int32_t* top_ids,
+                         float* top_logprobs, float* stats, void* cuda_stream);
+
+/* Gradient of qlora_token_logprobs with respect to the logits, for upstream gradients of the log probabilities and of the
+ * entropies (the alternatives carry none):
+ *     dlogits[t, j] = c * ( d_logprobs[t] ([j == tokens[t]] - p_j) - d_entropy[t] p_j (log p_j + entropy[t]) )
+ * stats: the forward call's, for the same logits and inv_temperature.  d_logprobs, d_entropy: fp32 [T]; one of them may be
+ * NULL (tokens too, where d_logprobs is).  A row whose token is outside [0, V) takes no d_logprobs.  A row without a
+ * gradient (both zero) gets zeros, whatever its logits and stats hold.  dlogits: the type of logits, [T, V] with rows
+ * grad_stride >= V elements apart (what lies between the rows is left as it was); may be the logits themselves
+ * (same address and stride), must not overlap them otherwise. */
+int qlora_token_logprobs_bwd(int T, int V, long long row_stride, int dtype, const void* logits, const int32_t* tokens,
+                             float inv_temperature, const float* stats, const float* d_logprobs, const float* d_entropy,
+                             long long grad_stride, void* dlogits, void* cuda_stream);
+
+/* The tensors of one optimizer step: every LoRA pair of a model at once (Section 3.2, Eq. 3: only theta_l is optimised).
+ * Host memory; the tensors they point to are the caller's, 16-byte aligned, none overlapping another (not checked here;
+ * the Python binding's adamw_desc checks it once). */
+typedef struct {
+    void* param;       /* [n], updated */
+    float* master;     /* fp32 [n] weights of which param is the rounded copy, updated; or NULL: param itself is the weight */
+    const void* grad;  /* [n] */
+    void* m;           /* [n] first moment, updated: fp32, or e4m3 with m_scale */
+    void* v;           /* [n] second moment, updated: fp32, or the e4m3 root of it with v_scale */
+    float* m_scale;    /* fp32 [ceil(n / 256)]; NULL with 32-bit states */
+    float* v_scale;    /* fp32 [ceil(n / 256)]; NULL with 32-bit states */
+    long long n;       /* elements; 0 is allowed */
+} qlora_adamw_tensor;
+
+typedef struct {
+    int n_tensors;
+    const qlora_adamw_tensor* tensors; /* host array */
+    int param_type;                    /* QLORA_BF16, QLORA_FP16 or QLORA_FP32 (then master must be NULL) */
+    int grad_type;                     /* QLORA_FP32 (what qlora_bwd_lora writes), QLORA_BF16 or QLORA_FP16 */
+    int state_type;                    /* QLORA_FP32 or QLORA_E4M3 */
+    double beta1, beta2;               /* in [0, 1) */
+    double eps;                        /* > 0 */
+    double weight_decay;               /* >= 0 */
+} qlora_adamw_desc;
+
+/* Global norm of all gradients and the factor that the step gives them, without a round trip to the host:
+ *     out[0] = sqrt( sum over every element of (prescale * g)^2 )         (summed in 64 bits, in a fixed order)
+ *     out[1] = prescale * min(1, max_norm / out[0])       (max_norm <= 0: prescale; NaN where the norm is not finite)
+ * prescale undoes a loss scale or turns the ranks' sum into a mean.  out: fp32 [2].  workspace:
+ * QLORA_GRAD_NORM_WORKSPACE_BYTES of device memory, contents undefined between calls. */
+#define QLORA_GRAD_NORM_WORKSPACE_BYTES 8192u
+int qlora_grad_norm(const qlora_adamw_desc* desc, float prescale, float max_norm, float* out, void* workspace,
+                    size_t workspace_bytes, void* cuda_stream);
+
+/* One AdamW step over every tensor of `desc`, element by element in fp32:
+ *     g = f * grad;   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2
+ *     w = w (1 - lr weight_decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ * f = norm[1] of qlora_grad_norm, or 1 where norm is NULL.  An f that is not finite skips the step: nothing is written.
+ * w is master where there is one (param then receives its nearest value), else param.
+ * lr and step (>= 1) are taken from lr_dev (fp32) and step_dev (int32) in device memory where those are given (a captured
+ * step, whose rate and number change between replays), else from the arguments.
+ * 8-bit states: every 256 consecutive elements share a scale, top / 448 with `top` the block's largest magnitude; the first
+ * moment is m = m_scale * code, the second v = (v_scale * code)^2, codes e4m3 (a block whose top is not above 2^-100 is held
+ * as zeros).  A code is one of the two e4m3 neighbours of value / scale, the upper one (in size) with a chance that is the
+ * value's share of the step, decided by a hash of the element's place in its tensor and the number of the step: nearest
+ * rounding would hold v still, as it changes by a thousandth a step where codes lie a sixteenth apart.  A root above zero
+ * stays above zero.  The weights are updated with the moments before they are rounded. */
+int qlora_adamw(const qlora_adamw_desc* desc, double lr, int step, const float* lr_dev, const int32_t* step_dev,
+                const float* norm, void* cuda_stream);
+
 /* Column gather  out[m, j] = in[m, perm[j]]  for 2-byte (bf16) or 4-byte (fp32) elements; perm: int32 [cols] device
  * pointer holding a permutation of 0 .. cols-1 (not checked); in and out must not overlap.
  * This is the per-call step of the activation-order format (Appendix A, "activation order": the group of input feature k

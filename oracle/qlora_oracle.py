@@ -322,6 +322,124 @@ def lrec_loss(student_logits, teacher_logits, labels, lambda_kl: float, lambda_c
     return loss, grad
 
 
+# ----------------------------------------------------------------------------------------------
+# Log probabilities of given tokens, entropies and the most likely alternatives, and their gradient.
+# ----------------------------------------------------------------------------------------------
+def token_logprobs(logits, tokens, c: float, k: int = 0) -> dict:
+    """Row by row, float64: p = softmax(c z).  Returns logprobs [T] (0 for a token outside [0, V)), entropy [T], stats [T, 3] (max z,
+    log sum exp(c (z - max)), entropy), top_ids and top_logprobs [T, k] (larger logits first, NaN before all, equal ones by place)."""
+    z = np.asarray(logits, dtype=np.float64)
+    T, V = z.shape
+    out = dict(logprobs=np.zeros(T), entropy=np.zeros(T), stats=np.zeros((T, 3)), top_ids=np.zeros((T, k), np.int64), top_logprobs=np.zeros((T, k)))
+    for t in range(T):
+        row = z[t]
+        if np.isnan(row).any() or np.isposinf(row).any():
+            logp, m, logs, H = np.full(V, np.nan), np.nan, np.nan, np.nan
+        elif np.isneginf(row).all():
+            logp, m, logs, H = np.full(V, -np.inf), -np.inf, -np.inf, 0.0
+        else:
+            m = row.max()
+            d = (row - m) * c
+            logs = np.log(np.exp(d).sum())
+            logp = d - logs
+            p = np.exp(logp)
+            H = -(p[p > 0] * logp[p > 0]).sum()
+        out["stats"][t] = m, logs, H
+        out["entropy"][t] = H
+        if tokens is not None and 0 <= int(tokens[t]) < V:
+            out["logprobs"][t] = logp[int(tokens[t])]
+        if k:
+            order = np.lexsort((np.arange(V), -np.where(np.isnan(row), np.inf, row), ~np.isnan(row)))[:k]
+            out["top_ids"][t], out["top_logprobs"][t] = order, logp[order]
+    return out
+
+
+def token_logprobs_backward(logits, tokens, c: float, d_logprobs, d_entropy):
+    """Gradient of sum_t d_logprobs[t] logprobs[t] + d_entropy[t] entropy[t] with respect to the logits, float64.  A row without a
+    gradient is zero, and so is a row with nothing above -inf; a row without a distribution (NaN, +inf) is NaN."""
+    z = np.asarray(logits, dtype=np.float64)
+    T, V = z.shape
+    grad = np.zeros((T, V))
+    for t in range(T):
+        known = tokens is not None and 0 <= int(tokens[t]) < V
+        gl = float(d_logprobs[t]) if d_logprobs is not None and known else 0.0
+        gh = float(d_entropy[t]) if d_entropy is not None else 0.0
+        if gl == 0.0 and gh == 0.0 or np.isneginf(z[t]).all():
+            continue
+        if np.isnan(z[t]).any() or np.isposinf(z[t]).any():
+            grad[t] = np.nan
+            continue
+        d = (z[t] - z[t].max()) * c
+        logp = d - np.log(np.exp(d).sum())
+        p = np.exp(logp)
+        plogp = np.where(p > 0, p * np.where(p > 0, logp, 0.0), 0.0)
+        grad[t] = -gl * p - gh * (plogp - p * plogp.sum())
+        if known:
+            grad[t, int(tokens[t])] += gl
+        grad[t] *= c
+    return grad
+
+
+# ----------------------------------------------------------------------------------------------
+# The optimizer step of the trainable pairs (Section 3.2, Eq. 3; the paper does not name the optimizer): AdamW, and the factor that
+# clips the gradients' global norm.
+# ----------------------------------------------------------------------------------------------
+def grad_norm(grads, prescale: float, max_norm: float):
+    """(norm of prescale times all gradients, the factor for each gradient)."""
+    norm = float(np.sqrt(sum(float(np.square(prescale * np.asarray(g, np.float64)).sum()) for g in grads)))
+    if not np.isfinite(norm):
+        return norm, float("nan")
+    return norm, prescale * (max_norm / norm if max_norm > 0 and norm > max_norm else 1.0)
+
+
+def adamw_step(w, g, m, v, step: int, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float, factor: float = 1.0):
+    """(w, m, v) after one step, float64; v is the second moment itself."""
+    w, g, m, v = (np.asarray(x, dtype=np.float64) for x in (w, g, m, v))
+    g = factor * g
+    m = beta1 * m + (1.0 - beta1) * g
+    v = beta2 * v + (1.0 - beta2) * g * g
+    w = w * (1.0 - lr * weight_decay) - lr * (m / (1.0 - beta1 ** step)) / (np.sqrt(v / (1.0 - beta2 ** step)) + eps)
+    return w, m, v
+
+
+def dither(place, step: int):
+    """Two numbers in [0, 2^20) for each element, from its place in its tensor and the number of the step (32-bit arithmetic)."""
+    x = (np.asarray(place, dtype=np.uint64) * np.uint64(0x9E3779B1) + np.uint64((step * 0x7F4A7C15) & 0xFFFFFFFF)) & np.uint64(0xFFFFFFFF)
+    x = ((x ^ (x >> np.uint64(15))) * np.uint64(0x2C1B3C6D)) & np.uint64(0xFFFFFFFF)
+    x = ((x ^ (x >> np.uint64(13))) * np.uint64(0x297A2D39)) & np.uint64(0xFFFFFFFF)
+    x = x ^ (x >> np.uint64(16))
+    y = (x * np.uint64(0x9E3779B1)) & np.uint64(0xFFFFFFFF)
+    return (x >> np.uint64(12)).astype(np.int64), (y >> np.uint64(12)).astype(np.int64)
+
+
+def e4m3_step(a):
+    """The distance of the e4m3 values around |a| (448 at most): 2^-9 below 2^-6, an eighth of the binade above."""
+    a = np.abs(np.asarray(a, dtype=np.float64))
+    return np.exp2(np.floor(np.log2(np.maximum(a, 2.0 ** -6))) - 3)
+
+
+def dithered_e4m3(x, r):
+    """x rounded to an e4m3 value beside it: up (in size) where x's share of the step and r / 2^20 together reach 1."""
+    x = np.asarray(x, dtype=np.float64)
+    ulp = e4m3_step(x)
+    return np.copysign(np.minimum(np.floor(np.abs(x) / ulp + np.asarray(r) / 2.0 ** 20) * ulp, 448.0), x)
+
+
+def held_in_8_bits(x, r, root: bool = False):
+    """Blocks of 256 values as (e4m3 codes, scale of each block); `root`: what is above zero stays above zero.  The last block may be
+    shorter."""
+    x = np.asarray(x, dtype=np.float64)
+    codes, scales = np.zeros_like(x), np.zeros(-(-x.size // 256))
+    for b in range(scales.size):
+        part = x[256 * b:256 * b + 256]
+        top = np.abs(part).max()
+        if top > 2.0 ** -100:
+            scales[b] = top / 448.0
+            c = dithered_e4m3(part / scales[b], r[256 * b:256 * b + 256])
+            codes[256 * b:256 * b + 256] = np.where(part > 0, np.maximum(c, 2.0 ** -9), c) if root else c
+    return codes, scales
+
+
 def layer_reference(inputs: dict, rows=None) -> dict:
     """Convenience wrapper for the tests: takes the dict produced by the synthetic-input module
     (bf16 bit patterns for X, dY, A, B; uint8 codes; fp16 scales / zeros) and returns the oracle's

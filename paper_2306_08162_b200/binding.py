@@ -23,6 +23,16 @@ class _Desc(ctypes.Structure):
                 ("r", ctypes.c_int), ("alpha", ctypes.c_float)]
 
 
+class _AdamwTensor(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("param", "master", "grad", "m", "v", "m_scale", "v_scale")] + [("n", ctypes.c_longlong)]
+
+
+class _AdamwDesc(ctypes.Structure):
+    _fields_ = [("n_tensors", ctypes.c_int), ("tensors", ctypes.POINTER(_AdamwTensor)), ("param_type", ctypes.c_int), ("grad_type", ctypes.c_int),
+                ("state_type", ctypes.c_int), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double)]
+
+
 def desc(bits: int, group_size: int, K: int, N: int, r: int, alpha: float) -> _Desc:
     """Layer descriptor (qlora_desc)."""
     return _Desc(int(bits), int(group_size), int(K), int(N), int(r), float(alpha))
@@ -63,11 +73,17 @@ def library() -> ctypes.CDLL:
     lib.qlora_quantize_rtn.argtypes = [dp, vp, vp, vp, vp, vp]
     lib.qlora_gather_columns.argtypes = [i32, i32, i32, vp, vp, vp, vp]
     lib.qlora_lrec_loss.argtypes = [i32, i32, vp, vp, vp, ctypes.c_float, ctypes.c_float, ctypes.c_float, vp, vp, vp]
+    i64, f64, ap = ctypes.c_longlong, ctypes.c_double, ctypes.POINTER(_AdamwDesc)
+    lib.qlora_token_logprobs.argtypes = [i32, i32, i64, i32, vp, vp, f32, i32, vp, vp, vp, vp, vp, vp]
+    lib.qlora_token_logprobs_bwd.argtypes = [i32, i32, i64, i32, vp, vp, f32, vp, vp, vp, i64, vp, vp]
+    lib.qlora_grad_norm.argtypes = [ap, f32, f32, vp, vp, sz, vp]
+    lib.qlora_adamw.argtypes = [ap, f64, i32, vp, vp, vp, vp]
     lib.qlora_device_status.argtypes = [ctypes.POINTER(ctypes.c_uint), i32]
     lib.qlora_selftest_bounded_wait.argtypes = [i32, vp]
     for name in ("qlora_workspace_bytes", "qlora_fwd", "qlora_bwd_input", "qlora_bwd_input_db", "qlora_bwd_lora", "qlora_bwd_lora_static", "qlora_fwd_dropout", "qlora_bwd_input_dropout",
                  "qlora_bwd_lora_dropout", "qlora_pack",
-                 "qlora_unpack", "qlora_dequant", "qlora_quantize_rtn", "qlora_gather_columns", "qlora_lrec_loss", "qlora_device_status", "qlora_selftest_bounded_wait"):
+                 "qlora_unpack", "qlora_dequant", "qlora_quantize_rtn", "qlora_gather_columns", "qlora_lrec_loss", "qlora_device_status", "qlora_selftest_bounded_wait",
+                 "qlora_token_logprobs", "qlora_token_logprobs_bwd", "qlora_grad_norm", "qlora_adamw"):
         getattr(lib, name).restype = i32
     _lib = lib
     return lib
@@ -79,7 +95,7 @@ def _native():
     if _calls is None:
         library()
         from . import _pycall
-        _pycall.set_desc_type(_Desc)
+        _pycall.set_desc_types((_Desc, _AdamwDesc))
         _calls = _pycall
     return _calls
 
@@ -195,6 +211,189 @@ def qlora_lrec_loss(student_logits, teacher_logits, labels, lambda_kl, lambda_ce
     rc = _native().qlora_lrec_loss(T, V, student_logits, teacher_logits, labels, lambda_kl, lambda_ce, grad_scale, loss_tokens, dlogits, stream)
     if rc != 0:
         raise QloraError(rc, "qlora_lrec_loss")
+
+
+_TYPES = None                    # torch dtype -> QLORA_BF16, QLORA_FP16, QLORA_FP32, QLORA_E4M3
+
+
+def _type_of(t, where: str, allowed) -> int:
+    global _TYPES
+    if _TYPES is None:
+        import torch
+        _TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2, torch.float8_e4m3fn: 3}
+    code = _TYPES.get(t.dtype, -1)
+    if code not in allowed:
+        raise ValueError(f"{where}: {t.dtype} is not supported here")
+    return code
+
+
+_LOGIT_TYPES = (0, 1, 2)
+_FP32 = (2,)
+
+
+def _rows(t, where: str):
+    """Shape and row stride of a 2-D tensor whose rows are dense (they may lie apart and begin anywhere)."""
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{where}: a 2-D tensor with dense rows is needed")
+    T, V = t.shape
+    return T, V, t.stride(0) if T > 1 else V
+
+
+def _vector(t, shape, dtype_name: str, where: str):
+    """An operand of a call over T rows: dense, of the type and the size that the library will assume."""
+    if t is not None and (str(t.dtype) != dtype_name or tuple(t.shape) != shape):
+        raise ValueError(f"{where}: {dtype_name} {list(shape)} is needed, got {t.dtype} {list(t.shape)}")
+
+
+def _on_current_device(where: str, *tensors):
+    """A tensor of another device (or of the host) in a kernel's hands would be a fault: the library works on the current device."""
+    import torch
+    here = torch.cuda.current_device() if torch.cuda.is_initialized() or torch.cuda.is_available() else None
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != here):
+            raise ValueError(f"{where}: tensors must be on the current CUDA device, got {t.device}")
+
+
+def qlora_token_logprobs(logits, tokens, inv_temperature, logprobs, entropy=None, top_ids=None, top_logprobs=None, stats=None, stream=None):
+    """Log probabilities of `tokens` (int32 [T], or None) under logits [T, V] (bf16, fp16 or fp32; rows may lie apart), the entropy of each
+    row and its k most likely places (k = top_ids.shape[1]); stats fp32 [T, 3] is what the backward call reads.  Outputs may be None."""
+    where = "qlora_token_logprobs"
+    T, V, stride = _rows(logits, where)
+    dtype = _type_of(logits, where, _LOGIT_TYPES)
+    top = top_ids if top_ids is not None else top_logprobs
+    if top is not None and top.dim() != 2:
+        raise ValueError(f"{where}: the alternatives are [T, k]")
+    k = top.shape[1] if top is not None else 0
+    _vector(tokens, (T,), "torch.int32", where)
+    _vector(logprobs, (T,), "torch.float32", where)
+    _vector(entropy, (T,), "torch.float32", where)
+    _vector(top_ids, (T, k), "torch.int32", where)
+    _vector(top_logprobs, (T, k), "torch.float32", where)
+    _vector(stats, (T, 3), "torch.float32", where)
+    _on_current_device(where, logits, tokens, logprobs, entropy, top_ids, top_logprobs, stats)
+    rc = _native().qlora_token_logprobs(T, V, stride, dtype, logits.data_ptr(), tokens, inv_temperature, k, logprobs, entropy, top_ids, top_logprobs,
+                                        stats, stream)
+    if rc != 0:
+        raise QloraError(rc, where)
+
+
+def qlora_token_logprobs_bwd(logits, tokens, inv_temperature, stats, d_logprobs, d_entropy, dlogits, stream=None):
+    """Gradient of qlora_token_logprobs with respect to the logits, into dlogits [T, V] (the logits' type; rows may lie apart; may be the
+    logits themselves)."""
+    where = "qlora_token_logprobs_bwd"
+    T, V, stride = _rows(logits, where)
+    dtype = _type_of(logits, where, _LOGIT_TYPES)
+    Tg, Vg, grad_stride = _rows(dlogits, where)
+    if (Tg, Vg) != (T, V) or dlogits.dtype != logits.dtype:
+        raise ValueError(f"{where}: dlogits has the shape and the type of logits")
+    _vector(tokens, (T,), "torch.int32", where)
+    _vector(stats, (T, 3), "torch.float32", where)
+    _vector(d_logprobs, (T,), "torch.float32", where)
+    _vector(d_entropy, (T,), "torch.float32", where)
+    _on_current_device(where, logits, tokens, stats, d_logprobs, d_entropy, dlogits)
+    rc = _native().qlora_token_logprobs_bwd(T, V, stride, dtype, logits.data_ptr(), tokens, inv_temperature, stats, d_logprobs, d_entropy, grad_stride,
+                                            dlogits.data_ptr(), stream)
+    if rc != 0:
+        raise QloraError(rc, where)
+
+
+GRAD_NORM_WORKSPACE_BYTES = 8192   # QLORA_GRAD_NORM_WORKSPACE_BYTES
+
+
+def adamw_desc(params, grads, m, v, master=None, m_scale=None, v_scale=None, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0) -> _AdamwDesc:
+    """Descriptor (qlora_adamw_desc) of the optimizer step over a list of parameters: made once, used every step.  All lists have one tensor
+    per parameter.  m and v are fp32, or float8_e4m3fn with m_scale and v_scale (fp32, one for every 256 elements, rounded up); master
+    (fp32) or None.  The descriptor holds the tensors' addresses and keeps the tensors alive: a gradient that is allocated anew needs a
+    new descriptor."""
+    import bisect
+    where = "adamw_desc"
+    lists = dict(param=list(params), master=list(master) if master is not None else None, grad=list(grads), m=list(m), v=list(v),
+                 m_scale=list(m_scale) if m_scale is not None else None, v_scale=list(v_scale) if v_scale is not None else None)
+    n = len(lists["param"])
+    for name, ts in lists.items():
+        if ts is not None and len(ts) != n:
+            raise ValueError(f"{where}: {len(ts)} tensors in {name}, {n} parameters")
+    d = _AdamwDesc(n_tensors=n, param_type=2, grad_type=2, state_type=2, beta1=beta1, beta2=beta2, eps=eps, weight_decay=weight_decay)
+    eight = n > 0 and _type_of(lists["m"][0], where, (2, 3)) == 3
+    if n:
+        d.param_type, d.grad_type, d.state_type = _type_of(lists["param"][0], where, _LOGIT_TYPES), _type_of(lists["grad"][0], where, _LOGIT_TYPES), 3 if eight else 2
+    if n and (lists["m_scale"] is not None, lists["v_scale"] is not None) != (eight, eight):
+        raise ValueError(f"{where}: m_scale and v_scale go with states in 8 bits, and only with those")
+    if lists["master"] is not None and n and d.param_type == 2:
+        raise ValueError(f"{where}: fp32 parameters have no master weights")
+    want = dict(param=d.param_type, master=2, grad=d.grad_type, m=d.state_type, v=d.state_type, m_scale=2, v_scale=2)
+    array = (_AdamwTensor * max(n, 1))()
+    ranges = []
+    for name, ts in lists.items():
+        for j, t in enumerate(ts or ()):
+            size = lists["param"][j].numel()
+            _type_of(t, f"{where}: {name}[{j}]", (want[name],))
+            if t.numel() != (-(-size // 256) if name.endswith("_scale") else size):
+                raise ValueError(f"{where}: {name}[{j}] has {t.numel()} elements for a parameter of {size}")
+            if not t.is_contiguous():
+                raise ValueError(f"{where}: tensors must be contiguous (dense)")
+            setattr(array[j], name, t.data_ptr())
+            if size:
+                ranges.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), name != "grad"))
+    for j, t in enumerate(lists["param"]):
+        array[j].n = t.numel()
+    written = sorted(r for r in ranges if r[2])
+    for a, b in zip(written, written[1:]):
+        if b[0] < a[1]:
+            raise ValueError(f"{where}: two of the tensors that the step writes overlap (the same one twice?)")
+    starts = [r[0] for r in written]
+    for lo, hi, w in ranges:
+        if not w:
+            at = bisect.bisect_left(starts, hi)                       # the last written range that begins before this one ends
+            if at > 0 and written[at - 1][1] > lo:
+                raise ValueError(f"{where}: a gradient overlaps a tensor that the step writes")
+    flat = [t for ts in lists.values() for t in ts or ()]
+    if flat and (not flat[0].is_cuda or any(t.device != flat[0].device for t in flat)):
+        raise ValueError(f"{where}: tensors must be on one CUDA device")
+    d.tensors = array
+    d.keep = (array, lists)
+    d.device = flat[0].get_device() if flat else None
+    return d
+
+
+def _check_desc_device(d, where: str):
+    import torch
+    if d.device is not None and d.device != torch.cuda.current_device():
+        raise ValueError(f"{where}: the descriptor's tensors are on device {d.device}, the current one is {torch.cuda.current_device()}")
+
+
+def qlora_grad_norm(d, prescale, max_norm, out, workspace, stream=None, workspace_bytes=None):
+    """out fp32 [2]: the norm of prescale times all gradients of the descriptor, and the factor for qlora_adamw that clips it to max_norm."""
+    where = "qlora_grad_norm"
+    if isinstance(d, _AdamwDesc):
+        _check_desc_device(d, where)
+        if not isinstance(out, int):
+            _vector(out, (2,), "torch.float32", where)
+            _on_current_device(where, out, workspace)
+    rc = _native().qlora_grad_norm(d, prescale, max_norm, out, workspace, workspace_bytes, stream)
+    if rc != 0:
+        raise QloraError(rc, where)
+
+
+def qlora_adamw(d, lr, step, norm=None, stream=None):
+    """One AdamW step over the descriptor's tensors.  lr: a number or an fp32 tensor [1]; step: an int from 1 or an int32 tensor [1] (device
+    memory that a captured step reads at replay); norm: fp32 [2] from qlora_grad_norm or None."""
+    where = "qlora_adamw"
+    lr_dev = lr if hasattr(lr, "data_ptr") else None
+    step_dev = step if hasattr(step, "data_ptr") else None
+    if isinstance(d, _AdamwDesc):
+        _check_desc_device(d, where)
+    if lr_dev is not None:
+        _vector(lr_dev, (1,), "torch.float32", where)
+    if step_dev is not None:
+        _vector(step_dev, (1,), "torch.int32", where)
+    if norm is not None and not isinstance(norm, int):
+        _vector(norm, (2,), "torch.float32", where)
+    if lr_dev is not None or step_dev is not None or (norm is not None and not isinstance(norm, int)):
+        _on_current_device(where, lr_dev, step_dev, None if isinstance(norm, int) else norm)
+    rc = _native().qlora_adamw(d, 0.0 if lr_dev is not None else lr, 0 if step_dev is not None else step, lr_dev, step_dev, norm, stream)
+    if rc != 0:
+        raise QloraError(rc, where)
 
 
 def qlora_gather_columns(inp, perm, out, stream=None):

@@ -1,5 +1,8 @@
 // The C ABI declared in qlora.h: argument validation, workspace carving and kernel dispatch.  No kernel lives here.
 #include <cuda_runtime.h>
+#include <math.h>
+
+#include <initializer_list>
 
 #include "launch.h"
 #include "qlora.h"
@@ -30,6 +33,44 @@ int check_desc(const qlora_desc* d, bool need_lora) {
         if (d->r < 0) return QLORA_ERR_INVALID_ARG;
         if (d->r % 8 != 0 || d->r > 64) return QLORA_ERR_UNSUPPORTED;
         if (!(d->alpha == d->alpha)) return QLORA_ERR_INVALID_ARG;   // NaN
+    }
+    return QLORA_OK;
+}
+
+size_t element_bytes(int dtype) { return dtype == QLORA_FP32 ? 4 : dtype == QLORA_E4M3 ? 1 : 2; }
+bool element_aligned(const void* p, int dtype) { return reinterpret_cast<uintptr_t>(p) % element_bytes(dtype) == 0; }
+
+int check_logits(int T, int V, long long row_stride, int dtype, float inv_temperature) {
+    if (T < 0 || V < 0 || (T > 1 && row_stride < V)) return QLORA_ERR_INVALID_ARG;
+    if (!(inv_temperature > 0.0f) || !(inv_temperature < INFINITY)) return QLORA_ERR_INVALID_ARG;
+    if (dtype != QLORA_BF16 && dtype != QLORA_FP16 && dtype != QLORA_FP32) return QLORA_ERR_UNSUPPORTED;
+    if (V == 0 || V > (1 << 24)) return QLORA_ERR_UNSUPPORTED;
+    return QLORA_OK;
+}
+
+// `step`: the whole step (else only the gradients are used).
+int check_adamw(const qlora_adamw_desc* d, bool step) {
+    if (d == nullptr || d->n_tensors < 0 || (d->n_tensors > 0 && d->tensors == nullptr)) return QLORA_ERR_INVALID_ARG;
+    if (!(d->beta1 >= 0.0 && d->beta1 < 1.0 && d->beta2 >= 0.0 && d->beta2 < 1.0)) return QLORA_ERR_INVALID_ARG;
+    if (!(d->eps > 0.0 && d->eps < 1e30) || !((float)d->eps > 0.0f) || !(d->weight_decay >= 0.0 && d->weight_decay < 1e30)) return QLORA_ERR_INVALID_ARG;
+    if (d->grad_type != QLORA_FP32 && d->grad_type != QLORA_BF16 && d->grad_type != QLORA_FP16) return QLORA_ERR_UNSUPPORTED;
+    if (d->param_type != QLORA_FP32 && d->param_type != QLORA_BF16 && d->param_type != QLORA_FP16) return QLORA_ERR_UNSUPPORTED;
+    if (d->state_type != QLORA_FP32 && d->state_type != QLORA_E4M3) return QLORA_ERR_UNSUPPORTED;
+    const bool eight = d->state_type == QLORA_E4M3;
+    for (int i = 0; i < d->n_tensors; ++i) {
+        const qlora_adamw_tensor& t = d->tensors[i];
+        if (t.n < 0) return QLORA_ERR_INVALID_ARG;
+        if (t.n == 0) continue;
+        if (t.n > (1ll << 40)) return QLORA_ERR_UNSUPPORTED;
+        if (!t.grad) return QLORA_ERR_INVALID_ARG;
+        uintptr_t all = reinterpret_cast<uintptr_t>(t.grad);
+        if (step) {
+            if (!t.param || !t.m || !t.v || (t.m_scale != nullptr) != eight || (t.v_scale != nullptr) != eight) return QLORA_ERR_INVALID_ARG;
+            if (t.master && d->param_type == QLORA_FP32) return QLORA_ERR_INVALID_ARG;
+            for (const void* p : {(const void*)t.param, (const void*)t.master, (const void*)t.m, (const void*)t.v, (const void*)t.m_scale, (const void*)t.v_scale})
+                all |= reinterpret_cast<uintptr_t>(p);
+        }
+        if (all & 15u) return QLORA_ERR_ALIGNMENT;
     }
     return QLORA_OK;
 }
@@ -128,6 +169,58 @@ int qlora_lrec_loss(int T, int V, const void* student_logits, const void* teache
         return QLORA_ERR_ALIGNMENT;
     return launch_lrec_loss(T, V, student_logits, teacher_logits, labels, lambda_kl, lambda_ce, grad_scale, loss_tokens, dlogits,
                             (cudaStream_t)cuda_stream);
+}
+
+int qlora_token_logprobs(int T, int V, long long row_stride, int dtype, const void* logits, const int32_t* tokens,
+                         float inv_temperature, int k, float* logprobs, float* entropy, int32_t* top_ids,
+                         float* top_logprobs, float* stats, void* cuda_stream) {
+    const int rc = check_logits(T, V, row_stride, dtype, inv_temperature);
+    if (rc != QLORA_OK) return rc;
+    if (k < 0) return QLORA_ERR_INVALID_ARG;
+    if (k > QLORA_MAX_TOP || k > V) return QLORA_ERR_UNSUPPORTED;
+    if (T == 0) return QLORA_OK;
+    if (!logits || (!logprobs && !entropy && !top_ids && !top_logprobs && !stats)) return QLORA_ERR_INVALID_ARG;
+    if ((logprobs && !tokens) || ((top_ids || top_logprobs) != (k > 0))) return QLORA_ERR_INVALID_ARG;
+    if (!element_aligned(logits, dtype) || !aligned16(tokens) || !aligned16(logprobs) || !aligned16(entropy) || !aligned16(top_ids) ||
+        !aligned16(top_logprobs) || !aligned16(stats))
+        return QLORA_ERR_ALIGNMENT;
+    return launch_token_logprobs(T, V, row_stride, dtype, logits, tokens, inv_temperature, k, logprobs, entropy, top_ids, top_logprobs, stats,
+                                 (cudaStream_t)cuda_stream);
+}
+
+int qlora_token_logprobs_bwd(int T, int V, long long row_stride, int dtype, const void* logits, const int32_t* tokens,
+                             float inv_temperature, const float* stats, const float* d_logprobs, const float* d_entropy,
+                             long long grad_stride, void* dlogits, void* cuda_stream) {
+    const int rc = check_logits(T, V, row_stride, dtype, inv_temperature);
+    if (rc != QLORA_OK) return rc;
+    if (T > 1 && grad_stride < V) return QLORA_ERR_INVALID_ARG;
+    if (T == 0) return QLORA_OK;
+    if (!logits || !stats || !dlogits || (!d_logprobs && !d_entropy) || (d_logprobs && !tokens)) return QLORA_ERR_INVALID_ARG;
+    if (logits == dlogits && T > 1 && row_stride != grad_stride) return QLORA_ERR_INVALID_ARG;
+    if (!element_aligned(logits, dtype) || !element_aligned(dlogits, dtype) || !aligned16(tokens) || !aligned16(stats) ||
+        !aligned16(d_logprobs) || !aligned16(d_entropy))
+        return QLORA_ERR_ALIGNMENT;
+    return launch_token_logprobs_bwd(T, V, row_stride, dtype, logits, tokens, inv_temperature, stats, d_logprobs, d_entropy, grad_stride, dlogits,
+                                     (cudaStream_t)cuda_stream);
+}
+
+int qlora_grad_norm(const qlora_adamw_desc* desc, float prescale, float max_norm, float* out, void* workspace,
+                    size_t workspace_bytes, void* cuda_stream) {
+    const int rc = check_adamw(desc, false);
+    if (rc != QLORA_OK) return rc;
+    if (!(prescale == prescale) || !(max_norm == max_norm) || !out) return QLORA_ERR_INVALID_ARG;
+    if (!aligned16(out) || !aligned16(workspace)) return QLORA_ERR_ALIGNMENT;
+    if (workspace == nullptr || workspace_bytes < QLORA_GRAD_NORM_WORKSPACE_BYTES) return QLORA_ERR_WORKSPACE;
+    return launch_grad_norm(*desc, prescale, max_norm, out, workspace, (cudaStream_t)cuda_stream);
+}
+
+int qlora_adamw(const qlora_adamw_desc* desc, double lr, int step, const float* lr_dev, const int32_t* step_dev,
+                const float* norm, void* cuda_stream) {
+    const int rc = check_adamw(desc, true);
+    if (rc != QLORA_OK) return rc;
+    if ((!lr_dev && !(lr - lr == 0.0)) || (!step_dev && step < 1)) return QLORA_ERR_INVALID_ARG;      // a finite rate, steps from 1
+    if (!aligned16(lr_dev) || !aligned16(step_dev) || !aligned16(norm)) return QLORA_ERR_ALIGNMENT;
+    return launch_adamw(*desc, lr, step, lr_dev, step_dev, norm, (cudaStream_t)cuda_stream);
 }
 
 int qlora_gather_columns(int elem_bytes, int rows, int cols, const void* in, const int32_t* perm, void* out, void* cuda_stream) {

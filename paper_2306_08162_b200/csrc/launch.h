@@ -20,6 +20,16 @@ int launch_quantize_rtn(const qlora_desc& d, const float* W, int32_t* Q, void* s
 int launch_lrec_loss(int T, int V, const void* Z, const void* Tt, const int32_t* labels, float lambda_kl, float lambda_ce,
                      float grad_scale, float* loss_tokens, void* dZ, cudaStream_t st);
 
+// logprob_kernels.cu -- log probabilities of given tokens, entropy and top alternatives over [T, V] logits, and their gradient
+int launch_token_logprobs(int T, int V, long long row_stride, int dtype, const void* logits, const int32_t* tokens, float c, int k, float* logprobs,
+                          float* entropy, int32_t* top_ids, float* top_logprobs, float* stats, cudaStream_t st);
+int launch_token_logprobs_bwd(int T, int V, long long row_stride, int dtype, const void* logits, const int32_t* tokens, float c, const float* stats,
+                              const float* d_logprobs, const float* d_entropy, long long grad_stride, void* dlogits, cudaStream_t st);
+
+// optim_kernels.cu -- the gradients' global norm and the AdamW step over a list of tensors
+int launch_grad_norm(const qlora_adamw_desc& d, float prescale, float max_norm, float* out, void* workspace, cudaStream_t st);
+int launch_adamw(const qlora_adamw_desc& d, double lr, int step, const float* lr_dev, const int32_t* step_dev, const float* norm, cudaStream_t st);
+
 // simt_kernels.cu -- CUDA-core kernels, correct for every supported shape
 // In [M, T] bf16 times the dequantised weight, plus s * P L.  transposed = false: forward (T = K, C = N);
 // true: backward-input (T = N, C = K).  P fp32 [M, r] (H or G) may be NULL when r == 0.

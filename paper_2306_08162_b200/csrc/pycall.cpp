@@ -16,6 +16,7 @@
 namespace {
 
 PyObject* g_desc_type = nullptr;                     // the ctypes structure of qlora_desc
+PyObject* g_adamw_type = nullptr;                    // ... and of qlora_adamw_desc
 PyObject *s_is_contiguous, *s_data_ptr, *s_cuda_stream, *s_numel, *s_element_size, *s_current_stream;
 PyObject *g_torch_cuda = nullptr, *g_get_device = nullptr, *g_raw_stream = nullptr;
 bool g_cuda_ready = false;                           // torch has initialised CUDA in this process
@@ -84,29 +85,37 @@ bool to_stream(PyObject* s, void** out) {
     return true;
 }
 
+// A descriptor: the memory of the ctypes structure itself.
+template <typename T>
+bool to_desc(PyObject* a, PyObject* type, const char* otherwise, T* out) {
+    const int is = PyObject_IsInstance(a, type);
+    if (is < 0) return false;
+    Py_buffer view;
+    if (!is) { PyErr_SetString(PyExc_TypeError, otherwise); return false; }
+    if (PyObject_GetBuffer(a, &view, PyBUF_SIMPLE) != 0) return false;
+    *out = static_cast<T>(view.buf);                              // (the caller holds the object for the whole call)
+    PyBuffer_Release(&view);
+    return true;
+}
+
 // One argument of the C function from the Python argument at the same place.  The last pointer is the stream; a size is that of the
 // tensor before it unless it is given.
 template <typename T>
 bool to_arg(PyObject* const* args, size_t i, size_t n, T* out) {
     PyObject* a = args[i];
     if constexpr (std::is_same_v<T, const qlora_desc*>) {
-        const int is = PyObject_IsInstance(a, g_desc_type);
-        if (is < 0) return false;
-        Py_buffer view;
-        if (!is) { PyErr_SetString(PyExc_TypeError, "the layer descriptor must come from desc()"); return false; }
-        if (PyObject_GetBuffer(a, &view, PyBUF_SIMPLE) != 0) return false;
-        *out = static_cast<const qlora_desc*>(view.buf);          // (the caller holds the object for the whole call)
-        PyBuffer_Release(&view);
-        return true;
+        return to_desc(a, g_desc_type, "the layer descriptor must come from desc()", out);
+    } else if constexpr (std::is_same_v<T, const qlora_adamw_desc*>) {
+        return to_desc(a, g_adamw_type, "the optimizer descriptor must come from adamw_desc()", out);
     } else if constexpr (std::is_pointer_v<T>) {
         void* p = nullptr;
         if (!(i + 1 == n ? to_stream(a, &p) : to_pointer(a, &p))) return false;
         *out = static_cast<T>(p);
         return true;
-    } else if constexpr (std::is_same_v<T, float>) {
+    } else if constexpr (std::is_floating_point_v<T>) {
         PyObject* f = PyNumber_Float(a);                              // (what float() takes, as the binding always did)
         if (f == nullptr) return false;
-        *out = (float)PyFloat_AS_DOUBLE(f);
+        *out = (T)PyFloat_AS_DOUBLE(f);
         Py_DECREF(f);
         return true;
     } else if constexpr (std::is_same_v<T, size_t>) {
@@ -121,7 +130,7 @@ bool to_arg(PyObject* const* args, size_t i, size_t n, T* out) {
         *out = (size_t)v;
         return true;
     } else {
-        static_assert(std::is_same_v<T, int>);
+        static_assert(std::is_same_v<T, int> || std::is_same_v<T, long long>);
         unsigned long long v = 0;
         if (PyLong_CheckExact(a)) {
             v = PyLong_AsUnsignedLongLongMask(a);
@@ -129,7 +138,7 @@ bool to_arg(PyObject* const* args, size_t i, size_t n, T* out) {
         } else if (!call_long(PyNumber_Long(a), &v)) {
             return false;
         }
-        *out = (int)v;
+        *out = (T)v;
         return true;
     }
 }
@@ -157,9 +166,13 @@ PyObject* checked_call(int (*fn)(A...), PyObject* const* args, Py_ssize_t n) {
 template <auto Fn>
 PyObject* py_call(PyObject*, PyObject* const* args, Py_ssize_t n) { return checked_call(Fn, args, n); }
 
-PyObject* py_set_desc_type(PyObject*, PyObject* type) {
-    Py_INCREF(type);
-    Py_XSETREF(g_desc_type, type);
+PyObject* py_set_desc_types(PyObject*, PyObject* types) {
+    PyObject *layer, *adamw;
+    if (!PyArg_ParseTuple(types, "OO", &layer, &adamw)) return nullptr;
+    Py_INCREF(layer);
+    Py_XSETREF(g_desc_type, layer);
+    Py_INCREF(adamw);
+    Py_XSETREF(g_adamw_type, adamw);
     Py_RETURN_NONE;
 }
 
@@ -168,7 +181,8 @@ PyMethodDef methods[] = {
     QLORA_PY(qlora_fwd), QLORA_PY(qlora_bwd_input), QLORA_PY(qlora_bwd_input_db), QLORA_PY(qlora_bwd_lora),
     QLORA_PY(qlora_fwd_dropout), QLORA_PY(qlora_bwd_input_dropout), QLORA_PY(qlora_bwd_lora_dropout),
     QLORA_PY(qlora_gather_columns), QLORA_PY(qlora_lrec_loss), QLORA_PY(qlora_quantize_rtn),
-    {"set_desc_type", py_set_desc_type, METH_O, nullptr},
+    QLORA_PY(qlora_token_logprobs), QLORA_PY(qlora_token_logprobs_bwd), QLORA_PY(qlora_grad_norm), QLORA_PY(qlora_adamw),
+    {"set_desc_types", py_set_desc_types, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
