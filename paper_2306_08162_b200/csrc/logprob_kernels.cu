@@ -9,8 +9,12 @@
 
 namespace qlora {
 
-constexpr int LP_THREADS = 512;
+constexpr int LP_BWD_THREADS = 512;
 constexpr int LP_UNROLL = 4;             // 16-byte vectors that a thread has on their way at a time
+constexpr int LP_CLUSTER = 8;            // most blocks that share a row
+constexpr int LP_GROUPS = 128;           // most groups of threads whose maxima bound the alternatives
+constexpr int LP_CANDIDATES = 512;       // entries that are put in order together
+static_assert(LP_CANDIDATES >= LP_CLUSTER * QLORA_MAX_TOP, "the lists of a cluster are merged in the same place");
 constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ float lp_f(float x) { return x; }
@@ -73,11 +77,12 @@ template <> struct Vec<__half> {
 template <typename T>
 struct RowParts {
     const T* z;
-    int head, vectors, tail;             // tail: where the rest begins
+    int head, vectors, tail, rest;       // tail: where the last `rest` elements begin
     __device__ __forceinline__ RowParts(const T* row, int V) : z(row) {
         head = min(V, (int)((0u - (uint32_t)reinterpret_cast<uintptr_t>(row)) & 15u) / (int)sizeof(T));
         vectors = (V - head) / Vec<T>::N;
         tail = head + vectors * Vec<T>::N;
+        rest = V - tail;
     }
     __device__ __forceinline__ const uint4* body() const { return reinterpret_cast<const uint4*>(z + head); }
 };
@@ -94,7 +99,12 @@ __device__ __forceinline__ uint32_t order_key(float z) {
     const uint32_t b = __float_as_uint(z + 0.f);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-__device__ __forceinline__ uint64_t entry_key(float z, int j) { return (uint64_t)order_key(z) << 32 | (uint32_t)~j; }
+__device__ __forceinline__ uint64_t entry_key(uint32_t key, int j) { return (uint64_t)key << 32 | (uint32_t)~j; }
+__device__ __forceinline__ int entry_place(uint64_t e) { return (int)~(uint32_t)e; }
+__device__ __forceinline__ float entry_logit(uint64_t e) {
+    const uint32_t key = (uint32_t)(e >> 32);
+    return key == 0xFFFFFFFFu ? __int_as_float(0x7FC00000) : __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
+}
 
 // A maximum and sums relative to it: s = sum exp(c (z - m)), a = sum exp(c (z - m)) (z - m).  kd = c log2(e).
 struct RowSums {
@@ -133,27 +143,27 @@ __device__ __forceinline__ RowSums warp_merge(RowSums x, float kd) {
 }
 
 // The sums of this thread's part of the row.
-template <typename T>
-__device__ __forceinline__ RowSums thread_sums(const RowParts<T>& row, int V, float kd) {
+template <typename T, int THREADS>
+__device__ __forceinline__ RowSums thread_sums(const RowParts<T>& row, float kd) {
     RowSums x{-INFINITY, 0.f, 0.f};
     const f2 kd2 = make_f2(kd, kd);
     const uint4* body = row.body();
-    for (int c0 = threadIdx.x; c0 < row.vectors; c0 += LP_UNROLL * LP_THREADS) {
+    for (int c0 = threadIdx.x; c0 < row.vectors; c0 += LP_UNROLL * THREADS) {
         uint4 v[LP_UNROLL];
         typename Vec<T>::Max top = Vec<T>::lowest();
 #pragma unroll
         for (int u = 0; u < LP_UNROLL; ++u)
-            if (c0 + u * LP_THREADS < row.vectors) v[u] = load_stream(body + c0 + u * LP_THREADS);
+            if (c0 + u * THREADS < row.vectors) v[u] = load_stream(body + c0 + u * THREADS);
 #pragma unroll
         for (int u = 0; u < LP_UNROLL; ++u)
-            if (c0 + u * LP_THREADS < row.vectors) top = Vec<T>::fold(top, v[u]);
+            if (c0 + u * THREADS < row.vectors) top = Vec<T>::fold(top, v[u]);
         const float m = max_nan(x.m, Vec<T>::value(top));
         if (m != x.m) rebase(x, m, kd);
         const f2 minus_m = make_f2(-m, -m);
         f2 s2 = make_f2(x.s, 0.f), a2 = make_f2(x.a, 0.f);
 #pragma unroll
         for (int u = 0; u < LP_UNROLL; ++u)
-            if (c0 + u * LP_THREADS < row.vectors) {
+            if (c0 + u * THREADS < row.vectors) {
 #pragma unroll
                 for (int i = 0; i < Vec<T>::N / 2; ++i) add_pair(s2, a2, Vec<T>::pair(v[u], i), minus_m, kd2);
             }
@@ -161,67 +171,251 @@ __device__ __forceinline__ RowSums thread_sums(const RowParts<T>& row, int V, fl
         x.a = lo_of(a2) + hi_of(a2);
     }
     if ((int)threadIdx.x < row.head) add_one(x, lp_f(row.z[threadIdx.x]), kd);
-    if (row.tail + (int)threadIdx.x < V) add_one(x, lp_f(row.z[row.tail + threadIdx.x]), kd);
+    if ((int)threadIdx.x < row.rest) add_one(x, lp_f(row.z[row.tail + threadIdx.x]), kd);
     return x;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(int V, long long stride, const T* __restrict__ logits, const int32_t* __restrict__ tokens, float c, int k,
-                                                              float* __restrict__ logprobs, float* __restrict__ entropy, int32_t* __restrict__ top_ids,
-                                                              float* __restrict__ top_logprobs, float* __restrict__ stats) {
-    __shared__ RowSums sums[LP_THREADS / 32];
-    __shared__ uint64_t best[LP_THREADS / 32];
-    pdl_launch_dependents();
-    pdl_wait();
-    const int row = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const float kd = c * kLog2e;
-    const T* z = logits + row * stride;
-    const RowParts<T> parts(z, V);
-    RowSums x = warp_merge(thread_sums(parts, V, kd), kd);
-    if (lane == 0) sums[warp] = x;
-    __syncthreads();
-    x = warp_merge(lane < LP_THREADS / 32 ? sums[lane] : RowSums{-INFINITY, 0.f, 0.f}, kd);
-    const bool none = x.m == -INFINITY, bad = !(x.m < INFINITY);
-    float logs = logf(x.s), H = fmaxf(logs - c * (x.a / x.s), 0.f);
-    if (none) { logs = -INFINITY; H = 0.f; }
-    if (bad) x.m = logs = H = __int_as_float(0x7FC00000);
-    auto logp = [&](float zj) { return none ? -INFINITY : (zj - x.m) * c - logs; };
-    if (threadIdx.x == 0) {
-        if (stats != nullptr) { stats[3ll * row] = x.m; stats[3ll * row + 1] = logs; stats[3ll * row + 2] = H; }
-        if (entropy != nullptr) entropy[row] = H;
-        if (logprobs != nullptr) {
-            const int t = tokens[row];
-            logprobs[row] = t >= 0 && t < V ? logp(lp_f(z[t])) : 0.f;
+// Calls f(key, place) for this thread's logits of the part of the row (the same ones as in thread_sums) whose key is at least `least`.
+template <typename T, int THREADS, typename F>
+__device__ __forceinline__ void each_from(const RowParts<T>& row, uint32_t least, F f) {
+    const uint4* body = row.body();
+    for (int c0 = threadIdx.x; c0 < row.vectors; c0 += LP_UNROLL * THREADS) {
+        uint4 v[LP_UNROLL];
+#pragma unroll
+        for (int u = 0; u < LP_UNROLL; ++u)
+            if (c0 + u * THREADS < row.vectors) v[u] = body[c0 + u * THREADS];
+#pragma unroll
+        for (int u = 0; u < LP_UNROLL; ++u) {
+            if (c0 + u * THREADS >= row.vectors || order_key(Vec<T>::value(Vec<T>::fold(Vec<T>::lowest(), v[u]))) < least) continue;
+#pragma unroll
+            for (int i = 0; i < Vec<T>::N; ++i) {
+                const f2 pr = Vec<T>::pair(v[u], i / 2);
+                const uint32_t key = order_key(i & 1 ? hi_of(pr) : lo_of(pr));
+                if (key >= least) f(key, row.head + (c0 + u * THREADS) * Vec<T>::N + i);
+            }
         }
     }
-    uint64_t last = ~0ull;
-    for (int i = 0; i < k; ++i) {                                  // the largest entry below the one before
-        uint64_t b = 0;
-        for (int j = threadIdx.x; j < V; j += LP_THREADS) {
-            const uint64_t e = entry_key(lp_f(z[j]), j);
-            if ((e < last || i == 0) && e > b) b = e;
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            const uint64_t other = __shfl_xor_sync(0xFFFFFFFFu, b, o);
-            if (other > b) b = other;
-        }
-        __syncthreads();
-        if (lane == 0) best[warp] = b;
-        __syncthreads();
-        for (int w = 0; w < LP_THREADS / 32; ++w)
-            if (best[w] > b) b = best[w];
-        last = b;
-        if (threadIdx.x == 0) {
-            const int j = (int)~(uint32_t)last;
-            if (top_ids != nullptr) top_ids[(long long)row * k + i] = j;
-            if (top_logprobs != nullptr) top_logprobs[(long long)row * k + i] = logp(lp_f(z[j]));
-        }
+    if ((int)threadIdx.x < row.head) {
+        const uint32_t key = order_key(lp_f(row.z[threadIdx.x]));
+        if (key >= least) f(key, (int)threadIdx.x);
+    }
+    if ((int)threadIdx.x < row.rest) {
+        const uint32_t key = order_key(lp_f(row.z[row.tail + threadIdx.x]));
+        if (key >= least) f(key, row.tail + (int)threadIdx.x);
     }
 }
 
+struct TopShared {
+    uint64_t cand[LP_CANDIDATES];        // entries that may be among the largest; in the first block of a cluster, then everybody's lists
+    uint64_t list[QLORA_MAX_TOP];        // the block's largest entries in order
+    uint32_t group[LP_GROUPS];
+    uint32_t bound;
+    int count, in_warp[32];
+};
+
+// How many logits of the part have a key of at least `least` (the same in every thread).
+template <typename T, int THREADS>
+__device__ __noinline__ int count_from(const RowParts<T>& row, uint32_t least, TopShared& sh) {
+    int n = 0;
+    each_from<T, THREADS>(row, least, [&](uint32_t, int) { ++n; });
+    __syncthreads();                     // (sh.count has been read by everybody)
+    if (threadIdx.x == 0) sh.count = 0;
+    __syncthreads();
+    n = __reduce_add_sync(0xFFFFFFFFu, n);
+    if ((threadIdx.x & 31) == 0 && n > 0) atomicAdd(&sh.count, n);
+    __syncthreads();
+    return sh.count;
+}
+
+// More candidates than there is room for (many equal logits, or large ones in a cluster): the kk-th largest key itself, found bit by bit
+// with a pass over the row each, then everything above it and, in the order of their places, as many equals as are wanted.
+template <typename T, int THREADS>
+__device__ __noinline__ int crowded(const RowParts<T>& row, int first, int n, int kk, uint32_t bound, TopShared& sh) {
+    uint32_t lo = bound, hi = 0xFFFFFFFFu;                          // at least kk keys are >= lo
+    while (lo < hi) {                                               // (first whether it is the bound itself: the usual case)
+        const uint32_t mid = lo == bound ? bound + 1 : lo + (hi - lo) / 2 + ((hi - lo) & 1);
+        if (count_from<T, THREADS>(row, mid, sh) >= kk) lo = mid;
+        else hi = mid - 1;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) sh.count = 0;
+    __syncthreads();
+    if (lo != 0xFFFFFFFFu) each_from<T, THREADS>(row, lo + 1, [&](uint32_t key, int j) { sh.cand[atomicAdd(&sh.count, 1)] = entry_key(key, first + j); });
+    __syncthreads();
+    int have = sh.count;                                            // fewer than kk
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int j0 = 0; j0 < n && have < kk; j0 += THREADS) {
+        const int j = j0 + threadIdx.x;
+        const bool is = j < n && order_key(lp_f(row.z[j])) == lo;
+        const uint32_t who = __ballot_sync(0xFFFFFFFFu, is);
+        if (lane == 0) sh.in_warp[warp] = __popc(who);
+        __syncthreads();
+        int at = have, all = have;
+        for (int w = 0; w < THREADS / 32; ++w) {
+            at += w < warp ? sh.in_warp[w] : 0;
+            all += sh.in_warp[w];
+        }
+        at += __popc(who & ((1u << lane) - 1u));
+        if (is && at < kk) sh.cand[at] = entry_key(lo, first + j);
+        have = all;
+        __syncthreads();
+    }
+    return kk;
+}
+
+// The kk largest entries of the block's part of the row into sh.list, in order.  `top`: the maximum of this thread's logits.
+// The threads fall into groups; at least kk logits are as large as the kk-th largest of the groups' maxima, and few more are (64 groups and kk = 20:
+// 24 in the mean).  So only threads with a maximum from there on look at their logits again, which by now are in L2.
+template <typename T, int THREADS>
+__device__ __forceinline__ void top_of_part(const RowParts<T>& row, int first, int n, int kk, float top, TopShared& sh) {
+    const uint32_t key = order_key(top);
+    const int groups = kk <= LP_GROUPS / 4 ? LP_GROUPS / 2 : LP_GROUPS, width = THREADS / groups;
+    uint32_t g = key;
+    for (int o = 1; o < width; o <<= 1) g = max(g, __shfl_xor_sync(0xFFFFFFFFu, g, o));
+    if (threadIdx.x % width == 0) sh.group[threadIdx.x / width] = g;
+    if (threadIdx.x == 0) { sh.bound = 0xFFFFFFFFu; sh.count = 0; }
+    __syncthreads();
+    if ((int)threadIdx.x < groups) {
+        const uint32_t mine = sh.group[threadIdx.x];
+        int above = 0;
+        for (int q = 0; q < groups; q += 4) {
+            const uint4 o = *reinterpret_cast<const uint4*>(&sh.group[q]);
+            above += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
+        }
+        const uint32_t least = __reduce_min_sync(0xFFFFFFFFu, above < kk ? mine : 0xFFFFFFFFu);
+        if ((threadIdx.x & 31) == 0) atomicMin(&sh.bound, least);
+    }
+    __syncthreads();
+    const uint32_t bound = sh.bound;
+    if (key >= bound)
+        each_from<T, THREADS>(row, bound, [&](uint32_t k, int j) {
+            const int at = atomicAdd(&sh.count, 1);
+            if (at < LP_CANDIDATES) sh.cand[at] = entry_key(k, first + j);
+        });
+    __syncthreads();
+    int count = sh.count;
+    if (count > LP_CANDIDATES) {
+        count = crowded<T, THREADS>(row, first, n, kk, bound, sh);
+        __syncthreads();
+    }
+    for (int i = threadIdx.x; i < count; i += THREADS) {             // an entry's place is the number of larger ones
+        const uint64_t mine = sh.cand[i];
+        int above = 0;
+        for (int q = 0; q < count; ++q) above += sh.cand[q] > mine;
+        if (above < kk) sh.list[above] = mine;
+    }
+    __syncthreads();
+}
+
+// Shared memory of another block of the cluster.
+__device__ __forceinline__ uint32_t remote(const void* p, int rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float remote_float(const void* p, int rank) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote(p, rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint64_t remote_u64(const void* p, int rank) {
+    uint64_t v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(remote(p, rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive;\n\tbarrier.cluster.wait;" ::: "memory");
+}
+
+// A row to a cluster of `blocks` blocks (1: no cluster), each with a part of it.
+template <typename T, int THREADS, bool TOP>
+__global__ void __launch_bounds__(THREADS) logprobs_kernel(int V, long long stride, const T* __restrict__ logits, const int32_t* __restrict__ tokens, float c, int k, int blocks,
+                                                           float* __restrict__ logprobs, float* __restrict__ entropy, int32_t* __restrict__ top_ids,
+                                                           float* __restrict__ top_logprobs, float* __restrict__ stats) {
+    __shared__ RowSums sums[THREADS / 32], mine;
+    __shared__ float result[3];
+    __shared__ __align__(16) unsigned char top_raw[TOP ? sizeof(TopShared) : 16];
+    TopShared& sh = *reinterpret_cast<TopShared*>(top_raw);
+    pdl_launch_dependents();
+    pdl_wait();
+    const int row = blockIdx.x / blocks, rank = blockIdx.x % blocks, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const float kd = c * kLog2e;
+    const T* z = logits + row * stride;
+    int token = -1;
+    float token_logit = 0.f;
+    if (threadIdx.x == 0 && rank == 0 && logprobs != nullptr) {
+        token = tokens[row];
+        if (token >= 0 && token < V) token_logit = lp_f(z[token]);
+        else token = -1;
+    }
+    // the part: whole vectors, but for the row's own ends
+    const RowParts<T> whole(z, V);
+    auto begin_of = [&](int r) { return r == 0 ? 0 : r == blocks ? V : whole.head + (int)((long long)whole.vectors * r / blocks) * Vec<T>::N; };
+    const int first = begin_of(rank), n = begin_of(rank + 1) - first;
+    const RowParts<T> part(z + first, n);
+    RowSums x = thread_sums<T, THREADS>(part, kd);
+    const float top = x.m;
+    x = warp_merge(x, kd);
+    if (lane == 0) sums[warp] = x;
+    if (TOP) top_of_part<T, THREADS>(part, first, n, min(k, n), top, sh);   // (waits for the block)
+    else __syncthreads();
+    if (warp == 0) {
+        x = warp_merge(lane < THREADS / 32 ? sums[lane] : RowSums{-INFINITY, 0.f, 0.f}, kd);
+        if (lane == 0) mine = x;
+    }
+    if (blocks > 1) {
+        cluster_sync();
+        if (rank == 0 && warp == 0) {
+            x = RowSums{-INFINITY, 0.f, 0.f};
+            if (lane < blocks) x = RowSums{remote_float(&mine.m, lane), remote_float(&mine.s, lane), remote_float(&mine.a, lane)};
+            x = warp_merge(x, kd);
+        }
+    }
+    if (rank == 0 && threadIdx.x == 0) {
+        const bool none = x.m == -INFINITY, bad = !(x.m < INFINITY);
+        float logs = logf(x.s), H = fmaxf(logs - c * (x.a / x.s), 0.f);
+        if (none) { logs = -INFINITY; H = 0.f; }
+        if (bad) x.m = logs = H = __int_as_float(0x7FC00000);
+        if (stats != nullptr) { stats[3ll * row] = x.m; stats[3ll * row + 1] = logs; stats[3ll * row + 2] = H; }
+        if (entropy != nullptr) entropy[row] = H;
+        if (logprobs != nullptr) logprobs[row] = token < 0 ? 0.f : none ? -INFINITY : (token_logit - x.m) * c - logs;
+        if (TOP) { result[0] = x.m; result[1] = logs; result[2] = none ? 1.f : 0.f; }
+    }
+    if (TOP && rank == 0) {
+        __syncthreads();
+        auto put = [&](int at, uint64_t e) {
+            if (top_ids != nullptr) top_ids[(long long)row * k + at] = entry_place(e);
+            if (top_logprobs != nullptr) top_logprobs[(long long)row * k + at] = result[2] != 0.f ? -INFINITY : (entry_logit(e) - result[0]) * c - result[1];
+        };
+        if (blocks == 1) {
+            if ((int)threadIdx.x < k) put(threadIdx.x, sh.list[threadIdx.x]);
+        } else {
+            // an entry's place in the whole: its own list's plus, list by list, the number of larger ones
+            auto length = [&](int r) { return min(k, begin_of(r + 1) - begin_of(r)); };
+            for (int e = threadIdx.x; e < blocks * k; e += THREADS) sh.cand[e] = e % k < length(e / k) ? remote_u64(&sh.list[e % k], e / k) : 0;
+            __syncthreads();
+            for (int e = threadIdx.x; e < blocks * k; e += THREADS) {
+                const uint64_t it = sh.cand[e];
+                if (e % k >= length(e / k)) continue;
+                int at = e % k;
+                for (int r = 0; r < blocks; ++r) {
+                    if (r == e / k) continue;
+                    int lo = 0, hi = length(r);                      // entries before lo are larger, those from hi on are not
+                    while (lo < hi) {
+                        const int mid = (lo + hi) >> 1;
+                        if (sh.cand[r * k + mid] > it) lo = mid + 1; else hi = mid;
+                    }
+                    at += lo;
+                }
+                if (at < k) put(at, it);
+            }
+        }
+    }
+    if (blocks > 1) cluster_sync();                                  // (nobody leaves while the first block reads)
+}
+
 template <typename T>
-__global__ void __launch_bounds__(LP_THREADS) logprobs_bwd_kernel(int V, long long stride, const T* logits, const int32_t* __restrict__ tokens, float c,
+__global__ void __launch_bounds__(LP_BWD_THREADS) logprobs_bwd_kernel(int V, long long stride, const T* logits, const int32_t* __restrict__ tokens, float c,
                                                                   const float* __restrict__ stats, const float* __restrict__ d_logprobs,
                                                                   const float* __restrict__ d_entropy, long long grad_stride, T* dlogits) {
     pdl_launch_dependents();
@@ -233,7 +427,7 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_bwd_kernel(int V, long lo
     const float gl = t >= 0 && t < V ? c * d_logprobs[row] : 0.f, gh = d_entropy != nullptr ? c * d_entropy[row] : 0.f;
     const float m = stats[3ll * row], logs = stats[3ll * row + 1], H = stats[3ll * row + 2];
     const bool zero = (gl == 0.f && gh == 0.f) || m == -INFINITY;
-    for (int j = threadIdx.x; j < V; j += LP_THREADS) {
+    for (int j = threadIdx.x; j < V; j += LP_BWD_THREADS) {
         float g = 0.f;
         if (!zero) {
             const float lp = (lp_f(z[j]) - m) * c - logs, p = expf(lp);
@@ -244,15 +438,30 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_bwd_kernel(int V, long lo
     }
 }
 
+// Blocks that share a row: as many as still fit the SMs all at once, while each has 4 KB of it at least.
+static int row_blocks(int T, long long row_bytes, int sms) {
+    int blocks = 1;
+    while (blocks < LP_CLUSTER && (long long)T * blocks * 2 <= 2 * sms && row_bytes / (blocks * 2) >= 4096) blocks *= 2;
+    return blocks;
+}
+
 int launch_token_logprobs(int T, int V, long long row_stride, int dtype, const void* logits, const int32_t* tokens, float c, int k, float* logprobs,
                           float* entropy, int32_t* top_ids, float* top_logprobs, float* stats, cudaStream_t st) {
+    const bool top = k > 0;
+    const long long row_bytes = (long long)V * (dtype == QLORA_FP32 ? 4 : 2);
+    const int blocks = row_blocks(T, row_bytes, sm_count());
+    const bool narrow = row_bytes / blocks <= 8192;
     cudaError_t err;
-#define QLORA_LP(TYPE)                                                                                                                              \
-    err = launch_pdl(logprobs_kernel<TYPE>, dim3((unsigned)T), dim3(LP_THREADS), 0, st, 1, V, row_stride, (const TYPE*)logits, tokens, c, k, logprobs, \
-                     entropy, top_ids, top_logprobs, stats)
-    if (dtype == QLORA_BF16) QLORA_LP(__nv_bfloat16);
-    else if (dtype == QLORA_FP16) QLORA_LP(__half);
-    else QLORA_LP(float);
+#define QLORA_LP(TYPE, THREADS, TOP)                                                                                                               \
+    err = launch_pdl(logprobs_kernel<TYPE, THREADS, TOP>, dim3((unsigned)T * (unsigned)blocks), dim3(THREADS), 0, st, (unsigned)blocks, V, row_stride, \
+                     (const TYPE*)logits, tokens, c, k, blocks, logprobs, entropy, top_ids, top_logprobs, stats)
+#define QLORA_LP_TYPE(TYPE)                                                                                                                        \
+    if (narrow) { if (top) QLORA_LP(TYPE, 128, true); else QLORA_LP(TYPE, 128, false); }                                                            \
+    else { if (top) QLORA_LP(TYPE, 512, true); else QLORA_LP(TYPE, 512, false); }
+    if (dtype == QLORA_BF16) { QLORA_LP_TYPE(__nv_bfloat16) }
+    else if (dtype == QLORA_FP16) { QLORA_LP_TYPE(__half) }
+    else { QLORA_LP_TYPE(float) }
+#undef QLORA_LP_TYPE
 #undef QLORA_LP
     return err == cudaSuccess ? QLORA_OK : QLORA_ERR_CUDA;
 }
@@ -261,7 +470,7 @@ int launch_token_logprobs_bwd(int T, int V, long long row_stride, int dtype, con
                               const float* d_logprobs, const float* d_entropy, long long grad_stride, void* dlogits, cudaStream_t st) {
     cudaError_t err;
 #define QLORA_LP(TYPE)                                                                                                                              \
-    err = launch_pdl(logprobs_bwd_kernel<TYPE>, dim3((unsigned)T), dim3(LP_THREADS), 0, st, 1, V, row_stride, (const TYPE*)logits, tokens, c, stats,  \
+    err = launch_pdl(logprobs_bwd_kernel<TYPE>, dim3((unsigned)T), dim3(LP_BWD_THREADS), 0, st, 1, V, row_stride, (const TYPE*)logits, tokens, c, stats,  \
                      d_logprobs, d_entropy, grad_stride, (TYPE*)dlogits)
     if (dtype == QLORA_BF16) QLORA_LP(__nv_bfloat16);
     else if (dtype == QLORA_FP16) QLORA_LP(__half);
