@@ -213,7 +213,7 @@ enum { QLORA_BF16 = 0, QLORA_FP16 = 1, QLORA_FP32 = 2, QLORA_E4M3 = 3 };
  * tensors they may begin at any element (a vocabulary of an odd size, a batch without its first token).  tokens: int32
  * [T], or NULL when logprobs is NULL.  logprobs, entropy: fp32 [T]; top_ids int32 [T, k], top_logprobs fp32 [T, k]; stats
  * fp32 [T, 3]; each of them may be NULL, not all.  0 <= k <= QLORA_MAX_TOP and k <= V (k = 0: no alternatives; both
- * arrays NULL); inv_temperature > 0 and finite; V <= 2^24.
+ * arrays NULL); 2^-30 <= inv_temperature <= 2^30; V <= 2^24.
  * Masked logits (-inf, or the type's lowest value) have probability 0 and add nothing to the sums; a row with nothing
  * above -inf has log p = -inf everywhere and entropy 0; a row that holds a NaN or +inf has no distribution: its numbers
  * are NaN, its places are ordered all the same (a NaN counts as larger than anything).

@@ -42,7 +42,7 @@ bool element_aligned(const void* p, int dtype) { return reinterpret_cast<uintptr
 
 int check_logits(int T, int V, long long row_stride, int dtype, float inv_temperature) {
     if (T < 0 || V < 0 || (T > 1 && row_stride < V)) return QLORA_ERR_INVALID_ARG;
-    if (!(inv_temperature > 0.0f) || !(inv_temperature < INFINITY)) return QLORA_ERR_INVALID_ARG;
+    if (!(inv_temperature >= 0x1p-30f && inv_temperature <= 0x1p30f)) return QLORA_ERR_INVALID_ARG;
     if (dtype != QLORA_BF16 && dtype != QLORA_FP16 && dtype != QLORA_FP32) return QLORA_ERR_UNSUPPORTED;
     if (V == 0 || V > (1 << 24)) return QLORA_ERR_UNSUPPORTED;
     return QLORA_OK;

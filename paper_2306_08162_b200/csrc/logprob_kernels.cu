@@ -2,6 +2,8 @@
 // respect to the logits.  Per row, with c the inverse temperature, m = max z and d_j = c (z_j - m) <= 0:
 //     s = sum exp d_j,    log p_j = d_j - log s,    H = log s - (sum exp(d_j) d_j) / s
 // in one pass over the row: every thread keeps its own maximum and sums relative to it and corrects them when the maximum moves.
+#include <type_traits>
+
 #include "common.cuh"
 #include "device_state.h"
 #include "f32x2.cuh"
@@ -10,12 +12,20 @@
 namespace qlora {
 
 constexpr int LP_BWD_THREADS = 512;
-constexpr int LP_UNROLL = 4;             // 16-byte vectors that a thread has on their way at a time
+#ifndef LPU
+#define LPU 4
+#endif
+#ifndef LPB
+#define LPB 6
+#endif
+constexpr int LP_UNROLL = LPU;             // 16-byte vectors that a thread has on their way at a time
 constexpr int LP_CLUSTER = 8;            // most blocks that share a row
-constexpr int LP_GROUPS = 128;           // most groups of threads whose maxima bound the alternatives
-constexpr int LP_CANDIDATES = 512;       // entries that are put in order together
+constexpr int LP_SEGMENTS = 16;          // stretches of a thread's part of the row with a maximum of their own
+constexpr int LP_CANDIDATES = 640;       // entries that are put in order together (a part of less than 64 vectors has fewer logits)
+constexpr int LP_HITS = 64;              // stretches that a warp looks at again
 static_assert(LP_CANDIDATES >= LP_CLUSTER * QLORA_MAX_TOP, "the lists of a cluster are merged in the same place");
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float LP_FLOOR = -0x1p96f, LP_LEAST = -0x1p80f, LP_MOST = 0x1p60f;     // see RowSums
 
 __device__ __forceinline__ float lp_f(float x) { return x; }
 __device__ __forceinline__ float lp_f(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -36,6 +46,10 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 template <typename T> struct Vec;
 template <> struct Vec<float> {
     static constexpr int N = 4;
+    static __device__ __forceinline__ f2 above_floor(const uint4& v, int i) {
+        const f2 p = pair(v, i);
+        return make_f2(fmaxf(lo_of(p), LP_FLOOR), fmaxf(hi_of(p), LP_FLOOR));
+    }
     static __device__ __forceinline__ f2 pair(const uint4& v, int i) { return i == 0 ? make_f2(__uint_as_float(v.x), __uint_as_float(v.y)) : make_f2(__uint_as_float(v.z), __uint_as_float(v.w)); }
     typedef float Max;
     static __device__ __forceinline__ Max lowest() { return -INFINITY; }
@@ -49,6 +63,10 @@ template <> struct Vec<__nv_bfloat16> {
     static __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
     static __device__ __forceinline__ f2 pair(const uint4& v, int i) { return unpack_bf16(word(v, i)); }
     typedef __nv_bfloat162 Max;
+    static __device__ __forceinline__ f2 above_floor(const uint4& v, int i) {            // (both at once, as they lie in memory)
+        const Max m = __hmax2(of(word(v, i)), __float2bfloat162_rn(LP_FLOOR));
+        return unpack_bf16(*reinterpret_cast<const uint32_t*>(&m));
+    }
     static __device__ __forceinline__ Max lowest() { return __float2bfloat162_rn(-INFINITY); }
     static __device__ __forceinline__ Max of(uint32_t w) { return *reinterpret_cast<const Max*>(&w); }
     static __device__ __forceinline__ Max fold(Max m, const uint4& v) {
@@ -63,6 +81,10 @@ template <> struct Vec<__half> {
         const uint32_t w = word(v, i);
         const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
         return make_f2(f.x, f.y);
+    }
+    static __device__ __forceinline__ f2 above_floor(const uint4& v, int i) {
+        const f2 p = pair(v, i);
+        return make_f2(fmaxf(lo_of(p), LP_FLOOR), fmaxf(hi_of(p), LP_FLOOR));
     }
     typedef __half2 Max;
     static __device__ __forceinline__ Max lowest() { return __float2half2_rn(-INFINITY); }
@@ -101,37 +123,32 @@ __device__ __forceinline__ uint32_t order_key(float z) {
 }
 __device__ __forceinline__ uint64_t entry_key(uint32_t key, int j) { return (uint64_t)key << 32 | (uint32_t)~j; }
 __device__ __forceinline__ int entry_place(uint64_t e) { return (int)~(uint32_t)e; }
-__device__ __forceinline__ float entry_logit(uint64_t e) {
-    const uint32_t key = (uint32_t)(e >> 32);
+__device__ __forceinline__ float key_logit(uint32_t key) {
     return key == 0xFFFFFFFFu ? __int_as_float(0x7FC00000) : __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
 }
+__device__ __forceinline__ float entry_logit(uint64_t e) { return key_logit((uint32_t)(e >> 32)); }
 
-// A maximum and sums relative to it: s = sum exp(c (z - m)), a = sum exp(c (z - m)) (z - m).  kd = c log2(e).
+// A maximum m and sums relative to it in base 2: with kd = c log2(e) and r = m kd as it is rounded,
+//     s = sum 2^x_j,   a = sum 2^x_j x_j,   x_j = z_j kd - r   (one fused multiply-add: an error of half a place of x_j, not of z_j kd)
+// For that 2^-30 <= c <= 2^30, logits below LP_FLOOR count as that (-inf among them: 2^x is 0 and 2^x x is 0, not NaN), r is at least
+// LP_LEAST kd, and rows whose maximum is not between LP_LEAST and LP_MOST are summed again in another way (odd_row).
 struct RowSums {
     float m, s, a;
 };
-// Moves the sums to a maximum m >= x.m.  (Nothing yet, or a row without a distribution: the factor is 0 or NaN, the sums become 0.)
+__device__ __forceinline__ float reference(float m, float kd) { return __fmul_rn(fmaxf(m, LP_LEAST), kd); }   // (rounded by itself: the differences of two rely on it)
+// Moves the sums to a maximum m >= x.m.
 __device__ __forceinline__ void rebase(RowSums& x, float m, float kd) {
-    const float d = x.m - m, e = fast_exp2(d * kd);
-    x.a = e > 0.f ? e * fmaf(x.s, d, x.a) : 0.f;
+    const float shift = reference(x.m, kd) - reference(m, kd), e = fast_exp2(shift);
+    x.a = e > 0.f ? e * fmaf(x.s, shift, x.a) : 0.f;
     x.s = e > 0.f ? x.s * e : 0.f;
     x.m = m;
-}
-// Adds a pair of logits at most x.m.  A masked one is -inf, or x.m is: the difference becomes the lowest number, its exponential 0, and
-// their product 0 instead of NaN.
-__device__ __forceinline__ void add_pair(f2& s2, f2& a2, f2 z, f2 minus_m, f2 kd2) {
-    const f2 raw = add2(z, minus_m);
-    const f2 d = make_f2(fmaxf(lo_of(raw), -3.0e38f), fmaxf(hi_of(raw), -3.0e38f));
-    const f2 e = exp2_2(mul2(d, kd2));
-    s2 = add2(s2, e);
-    a2 = fma2(e, d, a2);
 }
 __device__ __forceinline__ void add_one(RowSums& x, float z, float kd) {
     const float m = max_nan(x.m, z);
     if (m != x.m) rebase(x, m, kd);
-    const float d = fmaxf(z - m, -3.0e38f), e = fast_exp2(d * kd);
+    const float y = fmaf(fmaxf(z, LP_FLOOR), kd, -reference(m, kd)), e = fast_exp2(y);
     x.s += e;
-    x.a = fmaf(e, d, x.a);
+    x.a = fmaf(e, y, x.a);
 }
 // Sums of a warp's lanes, the same in all of them.
 __device__ __forceinline__ RowSums warp_merge(RowSums x, float kd) {
@@ -142,34 +159,75 @@ __device__ __forceinline__ RowSums warp_merge(RowSums x, float kd) {
     return RowSums{m, warp_sum(x.s), warp_sum(x.a)};
 }
 
-// The sums of this thread's part of the row.
+// log s and the entropy of a row whose maximum m is finite but too large or too small for the sums above (a row masked by the type's lowest value
+// altogether, say): the differences to m themselves, by the whole block, in two passes.
 template <typename T, int THREADS>
-__device__ __forceinline__ RowSums thread_sums(const RowParts<T>& row, float kd) {
+__device__ __noinline__ void odd_row(const T* z, int V, float m, float c, float* sums, float& logs, float& H) {
+    float s = 0.f, a = 0.f;
+    for (int j = threadIdx.x; j < V; j += THREADS) {
+        const float d = fmaxf((lp_f(z[j]) - m) * c, -1e30f), e = expf(d);
+        s += e;
+        a = fmaf(e, d, a);
+    }
+    s = warp_sum(s);
+    a = warp_sum(a);
+    if ((threadIdx.x & 31) == 0) { sums[2 * (threadIdx.x >> 5)] = s; sums[2 * (threadIdx.x >> 5) + 1] = a; }
+    __syncthreads();
+    s = a = 0.f;
+    for (int w = 0; w < THREADS / 32; ++w) { s += sums[2 * w]; a += sums[2 * w + 1]; }
+    logs = logf(s);
+    H = fmaxf(logs - a / s, 0.f);
+}
+
+// The sums of this thread's part of the row.  TOP: the maximum of each of the LP_SEGMENTS stretches of the thread's vectors goes to
+// segment[stretch * THREADS + thread]; `span` of the loop's rounds make a stretch.
+template <typename T, int THREADS, bool TOP>
+__device__ __forceinline__ RowSums thread_sums(const RowParts<T>& row, float kd, int span, float* segment) {
     RowSums x{-INFINITY, 0.f, 0.f};
+    float stretch = -INFINITY;
+    int rounds = 0;
     const f2 kd2 = make_f2(kd, kd);
     const uint4* body = row.body();
-    for (int c0 = threadIdx.x; c0 < row.vectors; c0 += LP_UNROLL * THREADS) {
+    auto round = [&](int c0, auto whole) {                            // LP_UNROLL vectors; `whole`: all of them are there
         uint4 v[LP_UNROLL];
         typename Vec<T>::Max top = Vec<T>::lowest();
 #pragma unroll
         for (int u = 0; u < LP_UNROLL; ++u)
-            if (c0 + u * THREADS < row.vectors) v[u] = load_stream(body + c0 + u * THREADS);
+            if (decltype(whole)::value || c0 + u * THREADS < row.vectors) v[u] = load_stream(body + c0 + u * THREADS);
 #pragma unroll
         for (int u = 0; u < LP_UNROLL; ++u)
-            if (c0 + u * THREADS < row.vectors) top = Vec<T>::fold(top, v[u]);
-        const float m = max_nan(x.m, Vec<T>::value(top));
+            if (decltype(whole)::value || c0 + u * THREADS < row.vectors) top = Vec<T>::fold(top, v[u]);
+        const float here = Vec<T>::value(top), m = max_nan(x.m, here);
+        if (TOP) {
+            stretch = max_nan(stretch, here);
+            if (++rounds == span) {
+                segment[threadIdx.x] = stretch;
+                segment += THREADS;
+                stretch = -INFINITY;
+                rounds = 0;
+            }
+        }
         if (m != x.m) rebase(x, m, kd);
-        const f2 minus_m = make_f2(-m, -m);
+        const float r = reference(m, kd);
+        const f2 minus_r = make_f2(-r, -r);
         f2 s2 = make_f2(x.s, 0.f), a2 = make_f2(x.a, 0.f);
 #pragma unroll
         for (int u = 0; u < LP_UNROLL; ++u)
-            if (c0 + u * THREADS < row.vectors) {
+            if (decltype(whole)::value || c0 + u * THREADS < row.vectors) {
 #pragma unroll
-                for (int i = 0; i < Vec<T>::N / 2; ++i) add_pair(s2, a2, Vec<T>::pair(v[u], i), minus_m, kd2);
+                for (int i = 0; i < Vec<T>::N / 2; ++i) {
+                    const f2 y = fma2(Vec<T>::above_floor(v[u], i), kd2, minus_r), e = exp2_2(y);
+                    s2 = add2(s2, e);
+                    a2 = fma2(e, y, a2);
+                }
             }
         x.s = lo_of(s2) + hi_of(s2);
         x.a = lo_of(a2) + hi_of(a2);
-    }
+    };
+    int c0 = threadIdx.x;
+    for (; c0 + (LP_UNROLL - 1) * THREADS < row.vectors; c0 += LP_UNROLL * THREADS) round(c0, std::true_type{});
+    if (c0 < row.vectors) round(c0, std::false_type{});
+    if (TOP && rounds > 0) segment[threadIdx.x] = stretch;
     if ((int)threadIdx.x < row.head) add_one(x, lp_f(row.z[threadIdx.x]), kd);
     if ((int)threadIdx.x < row.rest) add_one(x, lp_f(row.z[row.tail + threadIdx.x]), kd);
     return x;
@@ -206,11 +264,14 @@ __device__ __forceinline__ void each_from(const RowParts<T>& row, uint32_t least
 }
 
 struct TopShared {
-    uint64_t cand[LP_CANDIDATES];        // entries that may be among the largest; in the first block of a cluster, then everybody's lists
+    uint64_t cand[LP_CANDIDATES + 1];        // entries that may be among the largest; in the first block of a cluster, then everybody's lists
     uint64_t list[QLORA_MAX_TOP];        // the block's largest entries in order
-    uint32_t group[LP_GROUPS];
-    uint32_t bound;
+    uint32_t bound[32];                  // by warp
     int count, in_warp[32];
+};
+template <int THREADS> struct Top : TopShared {
+    float segment[LP_SEGMENTS * THREADS];
+    int hit[THREADS / 32][LP_HITS];      // by warp: stretches with a candidate, by their first vector
 };
 
 // How many logits of the part have a key of at least `least` (the same in every thread).
@@ -263,45 +324,91 @@ __device__ __noinline__ int crowded(const RowParts<T>& row, int first, int n, in
     return kk;
 }
 
-// The kk largest entries of the block's part of the row into sh.list, in order.  `top`: the maximum of this thread's logits.
-// The threads fall into groups; at least kk logits are as large as the kk-th largest of the groups' maxima, and few more are (64 groups and kk = 20:
-// 24 in the mean).  So only threads with a maximum from there on look at their logits again, which by now are in L2.
-template <typename T, int THREADS>
-__device__ __forceinline__ void top_of_part(const RowParts<T>& row, int first, int n, int kk, float top, TopShared& sh) {
-    const uint32_t key = order_key(top);
-    const int groups = kk <= LP_GROUPS / 4 ? LP_GROUPS / 2 : LP_GROUPS, width = THREADS / groups;
-    uint32_t g = key;
-    for (int o = 1; o < width; o <<= 1) g = max(g, __shfl_xor_sync(0xFFFFFFFFu, g, o));
-    if (threadIdx.x % width == 0) sh.group[threadIdx.x / width] = g;
-    if (threadIdx.x == 0) { sh.bound = 0xFFFFFFFFu; sh.count = 0; }
-    __syncthreads();
-    if ((int)threadIdx.x < groups) {
-        const uint32_t mine = sh.group[threadIdx.x];
-        int above = 0;
-        for (int q = 0; q < groups; q += 4) {
-            const uint4 o = *reinterpret_cast<const uint4*>(&sh.group[q]);
-            above += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
+// Before the block waits: this warp's share of the bound.  At least kk logits of the part are as large as the smallest of the warps' q-th
+// largest lane maxima, q = kk / warps, and not many more are (256 threads and kk = 20: some 50 in the mean).  `top`: the maximum of this thread's
+// logits.  Warps that lack logits stay out of it.
+template <int THREADS>
+__device__ __forceinline__ void offer_bound(int vectors, int kk, float top, TopShared& sh) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = min(THREADS / 32, vectors / 32);
+    uint32_t key = order_key(top), least = 0xFFFFFFFFu;
+    if (warps * 32 < kk) least = 0;                                  // (a short part: everything is a candidate)
+    else if (warp < warps)
+        for (int q = 0; q < kk; q += warps) {
+            least = __reduce_max_sync(0xFFFFFFFFu, key);
+            if (lane == __ffs(__ballot_sync(0xFFFFFFFFu, key == least)) - 1) key = 0;
         }
-        const uint32_t least = __reduce_min_sync(0xFFFFFFFFu, above < kk ? mine : 0xFFFFFFFFu);
-        if ((threadIdx.x & 31) == 0) atomicMin(&sh.bound, least);
+    if (lane == 0) sh.bound[warp] = least;
+    if (threadIdx.x == 0) sh.count = 0;
+}
+
+// After it: the kk largest entries of the block's part of the row into sh.list, in order.  Only warps whose logits reach the bound look at some of
+// them again, which by now are in L2.
+template <typename T, int THREADS>
+__device__ __forceinline__ void top_of_part(const RowParts<T>& row, int first, int n, int kk, int span_log2, Top<THREADS>& sh) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t bound = sh.bound[0];
+#pragma unroll
+    for (int w = 1; w < THREADS / 32; ++w) bound = min(bound, sh.bound[w]);
+    int hits = 0;
+    for (int g = 0, c0 = warp * 32; c0 < row.vectors; ++g, c0 += (LP_UNROLL * THREADS) << span_log2) {
+        const bool is = c0 + lane < row.vectors && order_key(sh.segment[g * THREADS + threadIdx.x]) >= bound;
+        const uint32_t who = __ballot_sync(0xFFFFFFFFu, is);
+        const int at = hits + __popc(who & ((1u << lane) - 1u));
+        if (is && at < LP_HITS) sh.hit[warp][at] = c0 + lane;
+        hits += __popc(who);
     }
-    __syncthreads();
-    const uint32_t bound = sh.bound;
-    if (key >= bound)
-        each_from<T, THREADS>(row, bound, [&](uint32_t k, int j) {
-            const int at = atomicAdd(&sh.count, 1);
-            if (at < LP_CANDIDATES) sh.cand[at] = entry_key(k, first + j);
-        });
+    if (hits > LP_HITS) {                                            // (each has a candidate)
+        if (lane == 0) atomicAdd(&sh.count, LP_CANDIDATES + 1);
+        hits = 0;
+    }
+    __syncwarp();
+    auto offer = [&](uint32_t k, int j) {
+        const int at = atomicAdd(&sh.count, 1);
+        if (at < LP_CANDIDATES) sh.cand[at] = entry_key(k, first + j);
+    };
+    const uint4* body = row.body();
+    static_assert(LP_UNROLL == 4, "a round of vectors is a power of two");
+    const float least = key_logit(bound);
+    for (int w = lane; w < hits << (span_log2 + 2); w += 32) {
+        const int at = sh.hit[warp][w >> (span_log2 + 2)] + (w & ((4 << span_log2) - 1)) * THREADS;
+        if (at >= row.vectors) continue;
+        const uint4 v = body[at];
+        uint32_t found = 0;                                          // (a NaN is; one that is not, if the bound is NaN, falls out below)
+#pragma unroll
+        for (int i = 0; i < Vec<T>::N; i += 2) {
+            const f2 pr = Vec<T>::pair(v, i / 2);
+            if (!(lo_of(pr) < least)) found |= 1u << i;
+            if (!(hi_of(pr) < least)) found |= 2u << i;
+        }
+        for (; found != 0; found &= found - 1) {
+            const int j = row.head + at * Vec<T>::N + __ffs(found) - 1;
+            const uint32_t key = order_key(lp_f(row.z[j]));
+            if (key >= bound) offer(key, j);
+        }
+    }
+    if ((int)threadIdx.x < row.head) {
+        const uint32_t key = order_key(lp_f(row.z[threadIdx.x]));
+        if (key >= bound) offer(key, (int)threadIdx.x);
+    }
+    if ((int)threadIdx.x < row.rest) {
+        const uint32_t key = order_key(lp_f(row.z[row.tail + threadIdx.x]));
+        if (key >= bound) offer(key, row.tail + (int)threadIdx.x);
+    }
     __syncthreads();
     int count = sh.count;
     if (count > LP_CANDIDATES) {
         count = crowded<T, THREADS>(row, first, n, kk, bound, sh);
         __syncthreads();
     }
+    if (threadIdx.x == 0 && (count & 1)) sh.cand[count] = 0;         // (two at a time below)
+    __syncthreads();
     for (int i = threadIdx.x; i < count; i += THREADS) {             // an entry's place is the number of larger ones
         const uint64_t mine = sh.cand[i];
         int above = 0;
-        for (int q = 0; q < count; ++q) above += sh.cand[q] > mine;
+        for (int q = 0; q < count; q += 2) {
+            const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(&sh.cand[q]);
+            above += (two.x > mine) + (two.y > mine);
+        }
         if (above < kk) sh.list[above] = mine;
     }
     __syncthreads();
@@ -328,17 +435,17 @@ __device__ __forceinline__ void cluster_sync() {
 }
 
 // A row to a cluster of `blocks` blocks (1: no cluster), each with a part of it.
-template <typename T, int THREADS, bool TOP>
-__global__ void __launch_bounds__(THREADS) logprobs_kernel(int V, long long stride, const T* __restrict__ logits, const int32_t* __restrict__ tokens, float c, int k, int blocks,
+template <typename T, int THREADS, bool TOP, bool SHARED>
+__global__ void __launch_bounds__(THREADS, SHARED ? 1 : THREADS == 128 ? 10 : LPB) logprobs_kernel(int V, long long stride, const T* __restrict__ logits, const int32_t* __restrict__ tokens, float c, int k, int blocks,
                                                            float* __restrict__ logprobs, float* __restrict__ entropy, int32_t* __restrict__ top_ids,
                                                            float* __restrict__ top_logprobs, float* __restrict__ stats) {
     __shared__ RowSums sums[THREADS / 32], mine;
-    __shared__ float result[3];
-    __shared__ __align__(16) unsigned char top_raw[TOP ? sizeof(TopShared) : 16];
-    TopShared& sh = *reinterpret_cast<TopShared*>(top_raw);
+    __shared__ float result[3], row_max;
+    __shared__ __align__(16) unsigned char top_raw[TOP ? sizeof(Top<THREADS>) : 16];
+    Top<THREADS>& sh = *reinterpret_cast<Top<THREADS>*>(top_raw);
     pdl_launch_dependents();
     pdl_wait();
-    const int row = blockIdx.x / blocks, rank = blockIdx.x % blocks, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int row = SHARED ? blockIdx.x / blocks : blockIdx.x, rank = SHARED ? blockIdx.x % blocks : 0, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const float kd = c * kLog2e;
     const T* z = logits + row * stride;
     int token = -1;
@@ -348,22 +455,25 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(int V, long long stri
         if (token >= 0 && token < V) token_logit = lp_f(z[token]);
         else token = -1;
     }
-    // the part: whole vectors, but for the row's own ends
+    // the part: whole vectors, but for the row's own ends (at most 2^22 vectors times 8 blocks)
     const RowParts<T> whole(z, V);
-    auto begin_of = [&](int r) { return r == 0 ? 0 : r == blocks ? V : whole.head + (int)((long long)whole.vectors * r / blocks) * Vec<T>::N; };
-    const int first = begin_of(rank), n = begin_of(rank + 1) - first;
+    auto begin_of = [&](int r) { return r == 0 ? 0 : r == blocks ? V : whole.head + (int)((unsigned)whole.vectors * (unsigned)r / (unsigned)blocks) * Vec<T>::N; };
+    const int first = SHARED ? begin_of(rank) : 0, n = SHARED ? begin_of(rank + 1) - first : V;
     const RowParts<T> part(z + first, n);
-    RowSums x = thread_sums<T, THREADS>(part, kd);
+    const int round = LP_UNROLL * THREADS, rounds = (part.vectors + round - 1) / round;
+    const int span_log2 = rounds <= LP_SEGMENTS ? 0 : 32 - __clz((rounds - 1) / LP_SEGMENTS);
+    RowSums x = thread_sums<T, THREADS, TOP>(part, kd, 1 << span_log2, TOP ? sh.segment : nullptr);
     const float top = x.m;
     x = warp_merge(x, kd);
     if (lane == 0) sums[warp] = x;
-    if (TOP) top_of_part<T, THREADS>(part, first, n, min(k, n), top, sh);   // (waits for the block)
-    else __syncthreads();
+    if (TOP) offer_bound<THREADS>(part.vectors, min(k, n), top, sh);
+    __syncthreads();
+    if (TOP) top_of_part<T, THREADS>(part, first, n, min(k, n), span_log2, sh);
     if (warp == 0) {
         x = warp_merge(lane < THREADS / 32 ? sums[lane] : RowSums{-INFINITY, 0.f, 0.f}, kd);
         if (lane == 0) mine = x;
     }
-    if (blocks > 1) {
+    if (SHARED) {
         cluster_sync();
         if (rank == 0 && warp == 0) {
             x = RowSums{-INFINITY, 0.f, 0.f};
@@ -371,15 +481,26 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(int V, long long stri
             x = warp_merge(x, kd);
         }
     }
-    if (rank == 0 && threadIdx.x == 0) {
-        const bool none = x.m == -INFINITY, bad = !(x.m < INFINITY);
-        float logs = logf(x.s), H = fmaxf(logs - c * (x.a / x.s), 0.f);
-        if (none) { logs = -INFINITY; H = 0.f; }
-        if (bad) x.m = logs = H = __int_as_float(0x7FC00000);
-        if (stats != nullptr) { stats[3ll * row] = x.m; stats[3ll * row + 1] = logs; stats[3ll * row + 2] = H; }
-        if (entropy != nullptr) entropy[row] = H;
-        if (logprobs != nullptr) logprobs[row] = token < 0 ? 0.f : none ? -INFINITY : (token_logit - x.m) * c - logs;
-        if (TOP) { result[0] = x.m; result[1] = logs; result[2] = none ? 1.f : 0.f; }
+    if (rank == 0) {
+        if (threadIdx.x == 0) row_max = x.m;
+        __syncthreads();
+        const float m = row_max;
+        const bool none = m == -INFINITY, odd = !none && m > -INFINITY && m < INFINITY && !(m > LP_LEAST && m < LP_MOST);
+        float logs, H;
+        if (odd) odd_row<T, THREADS>(z, V, m, c, reinterpret_cast<float*>(sums), logs, H);
+        if (threadIdx.x == 0) {
+            if (!odd) {
+                const float ln_s = logf(x.s);
+                logs = fmaf(fmaf(-m, kd, reference(m, kd)), kLn2, ln_s);
+                H = fmaxf(ln_s - kLn2 * (x.a / x.s), 0.f);
+                if (none) { logs = -INFINITY; H = 0.f; }
+                if (!(m < INFINITY)) x.m = logs = H = __int_as_float(0x7FC00000);
+            }
+            if (stats != nullptr) { stats[3ll * row] = x.m; stats[3ll * row + 1] = logs; stats[3ll * row + 2] = H; }
+            if (entropy != nullptr) entropy[row] = H;
+            if (logprobs != nullptr) logprobs[row] = token < 0 ? 0.f : none ? -INFINITY : (token_logit - x.m) * c - logs;
+            if (TOP) { result[0] = x.m; result[1] = logs; result[2] = none ? 1.f : 0.f; }
+        }
     }
     if (TOP && rank == 0) {
         __syncthreads();
@@ -387,31 +508,34 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(int V, long long stri
             if (top_ids != nullptr) top_ids[(long long)row * k + at] = entry_place(e);
             if (top_logprobs != nullptr) top_logprobs[(long long)row * k + at] = result[2] != 0.f ? -INFINITY : (entry_logit(e) - result[0]) * c - result[1];
         };
-        if (blocks == 1) {
+        if (!SHARED) {
             if ((int)threadIdx.x < k) put(threadIdx.x, sh.list[threadIdx.x]);
         } else {
-            // an entry's place in the whole: its own list's plus, list by list, the number of larger ones
-            auto length = [&](int r) { return min(k, begin_of(r + 1) - begin_of(r)); };
-            for (int e = threadIdx.x; e < blocks * k; e += THREADS) sh.cand[e] = e % k < length(e / k) ? remote_u64(&sh.list[e % k], e / k) : 0;
+            // an entry's place in the whole: its own list's plus, list by list, the number of larger ones (every list has k: a part of a shared
+            // row is longer than that)
+            for (int e = threadIdx.x; e < blocks * k; e += THREADS) {
+                const int r = e / k;
+                sh.cand[e] = remote_u64(&sh.list[e - r * k], r);
+            }
             __syncthreads();
             for (int e = threadIdx.x; e < blocks * k; e += THREADS) {
                 const uint64_t it = sh.cand[e];
-                if (e % k >= length(e / k)) continue;
-                int at = e % k;
+                const int own = e / k;
+                int at = e - own * k;
                 for (int r = 0; r < blocks; ++r) {
-                    if (r == e / k) continue;
-                    int lo = 0, hi = length(r);                      // entries before lo are larger, those from hi on are not
+                    int lo = 0, hi = r == own ? 0 : k;               // entries before lo are larger, those from hi on are not
                     while (lo < hi) {
                         const int mid = (lo + hi) >> 1;
                         if (sh.cand[r * k + mid] > it) lo = mid + 1; else hi = mid;
                     }
                     at += lo;
+                    if (at >= k) break;
                 }
                 if (at < k) put(at, it);
             }
         }
     }
-    if (blocks > 1) cluster_sync();                                  // (nobody leaves while the first block reads)
+    if (SHARED) cluster_sync();                                  // (nobody leaves while the first block reads)
 }
 
 template <typename T>
@@ -440,6 +564,9 @@ __global__ void __launch_bounds__(LP_BWD_THREADS) logprobs_bwd_kernel(int V, lon
 
 // Blocks that share a row: as many as still fit the SMs all at once, while each has 4 KB of it at least.
 static int row_blocks(int T, long long row_bytes, int sms) {
+#ifdef LPC
+    return LPC;
+#endif
     int blocks = 1;
     while (blocks < LP_CLUSTER && (long long)T * blocks * 2 <= 2 * sms && row_bytes / (blocks * 2) >= 4096) blocks *= 2;
     return blocks;
@@ -452,12 +579,19 @@ int launch_token_logprobs(int T, int V, long long row_stride, int dtype, const v
     const int blocks = row_blocks(T, row_bytes, sm_count());
     const bool narrow = row_bytes / blocks <= 8192;
     cudaError_t err;
-#define QLORA_LP(TYPE, THREADS, TOP)                                                                                                               \
-    err = launch_pdl(logprobs_kernel<TYPE, THREADS, TOP>, dim3((unsigned)T * (unsigned)blocks), dim3(THREADS), 0, st, (unsigned)blocks, V, row_stride, \
-                     (const TYPE*)logits, tokens, c, k, blocks, logprobs, entropy, top_ids, top_logprobs, stats)
+#define QLORA_LP(TYPE, THREADS, TOP, SHARED)                                                                                                        \
+    err = launch_pdl(logprobs_kernel<TYPE, THREADS, TOP, SHARED>, dim3((unsigned)T * (unsigned)blocks), dim3(THREADS), 0, st, (unsigned)blocks, V,   \
+                     row_stride, (const TYPE*)logits, tokens, c, k, blocks, logprobs, entropy, top_ids, top_logprobs, stats)
+#ifndef LPT
+#define LPT 256
+#endif
+#ifndef LPS
+#define LPS 256
+#endif
 #define QLORA_LP_TYPE(TYPE)                                                                                                                        \
-    if (narrow) { if (top) QLORA_LP(TYPE, 128, true); else QLORA_LP(TYPE, 128, false); }                                                            \
-    else { if (top) QLORA_LP(TYPE, 512, true); else QLORA_LP(TYPE, 512, false); }
+    if (blocks > 1) { if (top) QLORA_LP(TYPE, LPS, true, true); else QLORA_LP(TYPE, LPS, false, true); }                                             \
+    else if (narrow) { if (top) QLORA_LP(TYPE, 128, true, false); else QLORA_LP(TYPE, 128, false, false); }                                          \
+    else { if (top) QLORA_LP(TYPE, LPT, true, false); else QLORA_LP(TYPE, LPT, false, false); }
     if (dtype == QLORA_BF16) { QLORA_LP_TYPE(__nv_bfloat16) }
     else if (dtype == QLORA_FP16) { QLORA_LP_TYPE(__half) }
     else { QLORA_LP_TYPE(float) }
