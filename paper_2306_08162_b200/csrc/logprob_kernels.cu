@@ -2,8 +2,6 @@
 // respect to the logits.  Per row, with c the inverse temperature, m = max z and d_j = c (z_j - m) <= 0:
 //     s = sum exp d_j,    log p_j = d_j - log s,    H = log s - (sum exp(d_j) d_j) / s
 // in one pass over the row: every thread keeps its own maximum and sums relative to it and corrects them when the maximum moves.
-#include <type_traits>
-
 #include "common.cuh"
 #include "device_state.h"
 #include "f32x2.cuh"
@@ -12,13 +10,7 @@
 namespace qlora {
 
 constexpr int LP_BWD_THREADS = 512;
-#ifndef LPU
-#define LPU 4
-#endif
-#ifndef LPB
-#define LPB 6
-#endif
-constexpr int LP_UNROLL = LPU;             // 16-byte vectors that a thread has on their way at a time
+constexpr int LP_UNROLL = 4;             // 16-byte vectors that a thread has on their way at a time
 constexpr int LP_CLUSTER = 8;            // most blocks that share a row
 constexpr int LP_SEGMENTS = 16;          // stretches of a thread's part of the row with a maximum of their own
 constexpr int LP_CANDIDATES = 640;       // entries that are put in order together (a part of less than 64 vectors has fewer logits)
@@ -179,41 +171,39 @@ __device__ __noinline__ void odd_row(const T* z, int V, float m, float c, float*
     H = fmaxf(logs - a / s, 0.f);
 }
 
-// The sums of this thread's part of the row.  TOP: the maximum of each of the LP_SEGMENTS stretches of the thread's vectors goes to
-// segment[stretch * THREADS + thread]; `span` of the loop's rounds make a stretch.
+// This thread's part of a row, LP_UNROLL vectors (a round) at a time.  TOP: the maximum of each stretch of 2^span_log2 rounds goes to
+// segment[stretch * THREADS + thread].
 template <typename T, int THREADS, bool TOP>
-__device__ __forceinline__ RowSums thread_sums(const RowParts<T>& row, float kd, int span, float* segment) {
-    RowSums x{-INFINITY, 0.f, 0.f};
-    float stretch = -INFINITY;
-    int rounds = 0;
-    const f2 kd2 = make_f2(kd, kd);
-    const uint4* body = row.body();
-    auto round = [&](int c0, auto whole) {                            // LP_UNROLL vectors; `whole`: all of them are there
-        uint4 v[LP_UNROLL];
+struct ThreadRow {
+    RowSums x;
+    float stretch;
+    float* segment;
+    int left, span;
+    __device__ __forceinline__ ThreadRow(float* segments, int span_log2) : x{-INFINITY, 0.f, 0.f}, stretch(-INFINITY), segment(segments), left(1 << span_log2), span(1 << span_log2) {}
+    // Vector u of the round is there where c0 + u * THREADS < vectors.
+    template <bool WHOLE>
+    __device__ __forceinline__ void round(const uint4 (&v)[LP_UNROLL], int c0, int vectors, float kd) {
         typename Vec<T>::Max top = Vec<T>::lowest();
 #pragma unroll
         for (int u = 0; u < LP_UNROLL; ++u)
-            if (decltype(whole)::value || c0 + u * THREADS < row.vectors) v[u] = load_stream(body + c0 + u * THREADS);
-#pragma unroll
-        for (int u = 0; u < LP_UNROLL; ++u)
-            if (decltype(whole)::value || c0 + u * THREADS < row.vectors) top = Vec<T>::fold(top, v[u]);
+            if (WHOLE || c0 + u * THREADS < vectors) top = Vec<T>::fold(top, v[u]);
         const float here = Vec<T>::value(top), m = max_nan(x.m, here);
         if (TOP) {
             stretch = max_nan(stretch, here);
-            if (++rounds == span) {
+            if (--left == 0) {
                 segment[threadIdx.x] = stretch;
                 segment += THREADS;
                 stretch = -INFINITY;
-                rounds = 0;
+                left = span;
             }
         }
         if (m != x.m) rebase(x, m, kd);
         const float r = reference(m, kd);
-        const f2 minus_r = make_f2(-r, -r);
+        const f2 minus_r = make_f2(-r, -r), kd2 = make_f2(kd, kd);
         f2 s2 = make_f2(x.s, 0.f), a2 = make_f2(x.a, 0.f);
 #pragma unroll
         for (int u = 0; u < LP_UNROLL; ++u)
-            if (decltype(whole)::value || c0 + u * THREADS < row.vectors) {
+            if (WHOLE || c0 + u * THREADS < vectors) {
 #pragma unroll
                 for (int i = 0; i < Vec<T>::N / 2; ++i) {
                     const f2 y = fma2(Vec<T>::above_floor(v[u], i), kd2, minus_r), e = exp2_2(y);
@@ -223,15 +213,11 @@ __device__ __forceinline__ RowSums thread_sums(const RowParts<T>& row, float kd,
             }
         x.s = lo_of(s2) + hi_of(s2);
         x.a = lo_of(a2) + hi_of(a2);
-    };
-    int c0 = threadIdx.x;
-    for (; c0 + (LP_UNROLL - 1) * THREADS < row.vectors; c0 += LP_UNROLL * THREADS) round(c0, std::true_type{});
-    if (c0 < row.vectors) round(c0, std::false_type{});
-    if (TOP && rounds > 0) segment[threadIdx.x] = stretch;
-    if ((int)threadIdx.x < row.head) add_one(x, lp_f(row.z[threadIdx.x]), kd);
-    if ((int)threadIdx.x < row.rest) add_one(x, lp_f(row.z[row.tail + threadIdx.x]), kd);
-    return x;
-}
+    }
+    __device__ __forceinline__ void finish() {
+        if (TOP && left != span) segment[threadIdx.x] = stretch;
+    }
+};
 
 // Calls f(key, place) for this thread's logits of the part of the row (the same ones as in thread_sums) whose key is at least `least`.
 template <typename T, int THREADS, typename F>
@@ -263,15 +249,15 @@ __device__ __forceinline__ void each_from(const RowParts<T>& row, uint32_t least
     }
 }
 
-struct TopShared {
-    uint64_t cand[LP_CANDIDATES + 1];        // entries that may be among the largest; in the first block of a cluster, then everybody's lists
+struct alignas(16) TopShared {              // (the candidates are read two at a time)
+    uint64_t cand[LP_CANDIDATES];        // entries that may be among the largest; in the first block of a cluster, then everybody's lists
     uint64_t list[QLORA_MAX_TOP];        // the block's largest entries in order
     uint32_t bound[32];                  // by warp
     int count, in_warp[32];
 };
-template <int THREADS> struct Top : TopShared {
-    float segment[LP_SEGMENTS * THREADS];
-    int hit[THREADS / 32][LP_HITS];      // by warp: stretches with a candidate, by their first vector
+template <int THREADS> struct TopWarps {
+    float segment[LP_SEGMENTS * THREADS];   // maxima of the threads' stretches
+    int hit[THREADS / 32][LP_HITS];         // stretches with a candidate, by their first vector
 };
 
 // How many logits of the part have a key of at least `least` (the same in every thread).
@@ -341,20 +327,18 @@ __device__ __forceinline__ void offer_bound(int vectors, int kk, float top, TopS
     if (threadIdx.x == 0) sh.count = 0;
 }
 
-// After it: the kk largest entries of the block's part of the row into sh.list, in order.  Only warps whose logits reach the bound look at some of
-// them again, which by now are in L2.
+// After it: the entries of the block's part of the row from the bound on.  Only warps whose logits reach it look at some of them again, which by now are in L2.
+// `segment`: the maxima of this warp's stretches; `hit`: LP_HITS places of this warp's own; `ends`: the logits at this thread's places of
+// the head and of the rest.
 template <typename T, int THREADS>
-__device__ __forceinline__ void top_of_part(const RowParts<T>& row, int first, int n, int kk, int span_log2, Top<THREADS>& sh) {
+__device__ __forceinline__ void gather(const RowParts<T>& row, int first, uint32_t bound, int span_log2, const float* segment, int* hit, float head, float rest, TopShared& sh) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    uint32_t bound = sh.bound[0];
-#pragma unroll
-    for (int w = 1; w < THREADS / 32; ++w) bound = min(bound, sh.bound[w]);
     int hits = 0;
     for (int g = 0, c0 = warp * 32; c0 < row.vectors; ++g, c0 += (LP_UNROLL * THREADS) << span_log2) {
-        const bool is = c0 + lane < row.vectors && order_key(sh.segment[g * THREADS + threadIdx.x]) >= bound;
+        const bool is = c0 + lane < row.vectors && order_key(segment[g * THREADS + threadIdx.x]) >= bound;
         const uint32_t who = __ballot_sync(0xFFFFFFFFu, is);
         const int at = hits + __popc(who & ((1u << lane) - 1u));
-        if (is && at < LP_HITS) sh.hit[warp][at] = c0 + lane;
+        if (is && at < LP_HITS) hit[at] = c0 + lane;
         hits += __popc(who);
     }
     if (hits > LP_HITS) {                                            // (each has a candidate)
@@ -370,7 +354,7 @@ __device__ __forceinline__ void top_of_part(const RowParts<T>& row, int first, i
     static_assert(LP_UNROLL == 4, "a round of vectors is a power of two");
     const float least = key_logit(bound);
     for (int w = lane; w < hits << (span_log2 + 2); w += 32) {
-        const int at = sh.hit[warp][w >> (span_log2 + 2)] + (w & ((4 << span_log2) - 1)) * THREADS;
+        const int at = hit[w >> (span_log2 + 2)] + (w & ((4 << span_log2) - 1)) * THREADS;
         if (at >= row.vectors) continue;
         const uint4 v = body[at];
         uint32_t found = 0;                                          // (a NaN is; one that is not, if the bound is NaN, falls out below)
@@ -386,32 +370,31 @@ __device__ __forceinline__ void top_of_part(const RowParts<T>& row, int first, i
             if (key >= bound) offer(key, j);
         }
     }
-    if ((int)threadIdx.x < row.head) {
-        const uint32_t key = order_key(lp_f(row.z[threadIdx.x]));
-        if (key >= bound) offer(key, (int)threadIdx.x);
-    }
-    if ((int)threadIdx.x < row.rest) {
-        const uint32_t key = order_key(lp_f(row.z[row.tail + threadIdx.x]));
-        if (key >= bound) offer(key, row.tail + (int)threadIdx.x);
-    }
-    __syncthreads();
+    if ((int)threadIdx.x < row.head && order_key(head) >= bound) offer(order_key(head), (int)threadIdx.x);
+    if ((int)threadIdx.x < row.rest && order_key(rest) >= bound) offer(order_key(rest), row.tail + (int)threadIdx.x);
+}
+
+// With the candidates there (behind a barrier): calls put(place, entry) for the kk largest.
+template <typename T, int THREADS, typename F>
+__device__ __forceinline__ void select(const RowParts<T>& row, int first, int n, int kk, uint32_t bound, TopShared& sh, F put) {
     int count = sh.count;
     if (count > LP_CANDIDATES) {
         count = crowded<T, THREADS>(row, first, n, kk, bound, sh);
         __syncthreads();
     }
-    if (threadIdx.x == 0 && (count & 1)) sh.cand[count] = 0;         // (two at a time below)
-    __syncthreads();
     for (int i = threadIdx.x; i < count; i += THREADS) {             // an entry's place is the number of larger ones
         const uint64_t mine = sh.cand[i];
         int above = 0;
-        for (int q = 0; q < count; q += 2) {
+        for (int q = 0; q + 1 < count; q += 2) {
             const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(&sh.cand[q]);
             above += (two.x > mine) + (two.y > mine);
         }
-        if (above < kk) sh.list[above] = mine;
+        if (count & 1) above += sh.cand[count - 1] > mine;
+        if (above < kk) put(above, mine);
     }
-    __syncthreads();
+}
+__device__ __forceinline__ uint32_t common_bound(const TopShared& sh, int warps) {
+    return __reduce_min_sync(0xFFFFFFFFu, sh.bound[min((int)(threadIdx.x & 31), warps - 1)]);
 }
 
 // Shared memory of another block of the cluster.
@@ -434,46 +417,101 @@ __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive;\n\tbarrier.cluster.wait;" ::: "memory");
 }
 
-// A row to a cluster of `blocks` blocks (1: no cluster), each with a part of it.
-template <typename T, int THREADS, bool TOP, bool SHARED>
-__global__ void __launch_bounds__(THREADS, SHARED ? 1 : THREADS == 128 ? 10 : LPB) logprobs_kernel(int V, long long stride, const T* __restrict__ logits, const int32_t* __restrict__ tokens, float c, int k, int blocks,
-                                                           float* __restrict__ logprobs, float* __restrict__ entropy, int32_t* __restrict__ top_ids,
-                                                           float* __restrict__ top_logprobs, float* __restrict__ stats) {
+struct LogprobArgs {
+    int T, V, k, blocks;
+    long long stride;
+    const void* logits;
+    const int32_t* tokens;
+    float c;
+    float *logprobs, *entropy, *stats, *top_logprobs;
+    int32_t* top_ids;
+};
+
+// What is told about a row, by one thread that has its sums; `found` receives what the alternatives need.
+struct RowResult {
+    float m, logs;
+    int none;
+};
+__device__ __forceinline__ RowResult tell_row(const LogprobArgs& p, int row, RowSums x, float kd, bool odd, float logs, float H, int token, float token_logit) {
+    const bool none = x.m == -INFINITY;
+    if (!odd) {
+        const float ln_s = logf(x.s);
+        logs = fmaf(fmaf(-x.m, kd, reference(x.m, kd)), kLn2, ln_s);
+        H = fmaxf(ln_s - kLn2 * (x.a / x.s), 0.f);
+        if (none) { logs = -INFINITY; H = 0.f; }
+        if (!(x.m < INFINITY)) x.m = logs = H = __int_as_float(0x7FC00000);
+    }
+    if (p.stats != nullptr) { p.stats[3ll * row] = x.m; p.stats[3ll * row + 1] = logs; p.stats[3ll * row + 2] = H; }
+    if (p.entropy != nullptr) p.entropy[row] = H;
+    if (p.logprobs != nullptr) p.logprobs[row] = token < 0 ? 0.f : none ? -INFINITY : (token_logit - x.m) * p.c - logs;
+    return RowResult{x.m, logs, none};
+}
+__device__ __forceinline__ void tell_top(const LogprobArgs& p, int row, int at, uint64_t e, const RowResult& r) {
+    if (p.top_ids != nullptr) p.top_ids[(long long)row * p.k + at] = entry_place(e);
+    if (p.top_logprobs != nullptr) p.top_logprobs[(long long)row * p.k + at] = r.none ? -INFINITY : (entry_logit(e) - r.m) * p.c - r.logs;
+}
+__device__ __forceinline__ bool is_odd(float m) { return fabsf(m) < INFINITY && !(m > LP_LEAST && m < LP_MOST); }
+template <int THREADS>
+__device__ __forceinline__ int span_of(int vectors) {                    // log2 of the rounds that make a stretch
+    const int round = LP_UNROLL * THREADS, rounds = (vectors + round - 1) / round;
+    return rounds <= LP_SEGMENTS ? 0 : 32 - __clz((rounds - 1) / LP_SEGMENTS);
+}
+
+// Few rows: one to a cluster of `blocks` blocks (1: no cluster), each with a part of it.
+template <typename T, int THREADS, bool TOP>
+__global__ void __launch_bounds__(THREADS) logprobs_shared_kernel(const LogprobArgs p) {
     __shared__ RowSums sums[THREADS / 32], mine;
-    __shared__ float result[3], row_max;
-    __shared__ __align__(16) unsigned char top_raw[TOP ? sizeof(Top<THREADS>) : 16];
-    Top<THREADS>& sh = *reinterpret_cast<Top<THREADS>*>(top_raw);
+    __shared__ float row_max;
+    __shared__ RowResult result;
+    __shared__ __align__(16) unsigned char top_raw[TOP ? sizeof(TopShared) : 16], warps_raw[TOP ? sizeof(TopWarps<THREADS>) : 16];
+    TopShared& sh = *reinterpret_cast<TopShared*>(top_raw);
+    TopWarps<THREADS>& own = *reinterpret_cast<TopWarps<THREADS>*>(warps_raw);
     pdl_launch_dependents();
     pdl_wait();
-    const int row = SHARED ? blockIdx.x / blocks : blockIdx.x, rank = SHARED ? blockIdx.x % blocks : 0, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const float kd = c * kLog2e;
-    const T* z = logits + row * stride;
+    const int blocks = p.blocks, V = p.V, k = p.k, row = blockIdx.x / blocks, rank = blockIdx.x % blocks, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const float kd = p.c * kLog2e;
+    const T* z = static_cast<const T*>(p.logits) + row * p.stride;
     int token = -1;
     float token_logit = 0.f;
-    if (threadIdx.x == 0 && rank == 0 && logprobs != nullptr) {
-        token = tokens[row];
+    if (threadIdx.x == 0 && rank == 0 && p.logprobs != nullptr) {
+        token = p.tokens[row];
         if (token >= 0 && token < V) token_logit = lp_f(z[token]);
         else token = -1;
     }
     // the part: whole vectors, but for the row's own ends (at most 2^22 vectors times 8 blocks)
     const RowParts<T> whole(z, V);
     auto begin_of = [&](int r) { return r == 0 ? 0 : r == blocks ? V : whole.head + (int)((unsigned)whole.vectors * (unsigned)r / (unsigned)blocks) * Vec<T>::N; };
-    const int first = SHARED ? begin_of(rank) : 0, n = SHARED ? begin_of(rank + 1) - first : V;
+    const int first = begin_of(rank), n = begin_of(rank + 1) - first, kk = min(k, n);
     const RowParts<T> part(z + first, n);
-    const int round = LP_UNROLL * THREADS, rounds = (part.vectors + round - 1) / round;
-    const int span_log2 = rounds <= LP_SEGMENTS ? 0 : 32 - __clz((rounds - 1) / LP_SEGMENTS);
-    RowSums x = thread_sums<T, THREADS, TOP>(part, kd, 1 << span_log2, TOP ? sh.segment : nullptr);
-    const float top = x.m;
-    x = warp_merge(x, kd);
+    const float head = (int)threadIdx.x < part.head ? lp_f(part.z[threadIdx.x]) : -INFINITY;
+    const float rest = (int)threadIdx.x < part.rest ? lp_f(part.z[part.tail + threadIdx.x]) : -INFINITY;
+    const int span_log2 = span_of<THREADS>(part.vectors);
+    ThreadRow<T, THREADS, TOP> mine_of(own.segment, span_log2);
+    for (int c0 = threadIdx.x; c0 < part.vectors; c0 += LP_UNROLL * THREADS) {
+        uint4 v[LP_UNROLL];
+#pragma unroll
+        for (int u = 0; u < LP_UNROLL; ++u)
+            if (c0 + u * THREADS < part.vectors) v[u] = load_stream(part.body() + c0 + u * THREADS);
+        mine_of.template round<false>(v, c0, part.vectors, kd);
+    }
+    mine_of.finish();
+    if ((int)threadIdx.x < part.head) add_one(mine_of.x, head, kd);
+    if ((int)threadIdx.x < part.rest) add_one(mine_of.x, rest, kd);
+    if (TOP) offer_bound<THREADS>(part.vectors, kk, mine_of.x.m, sh);
+    RowSums x = warp_merge(mine_of.x, kd);
     if (lane == 0) sums[warp] = x;
-    if (TOP) offer_bound<THREADS>(part.vectors, min(k, n), top, sh);
     __syncthreads();
-    if (TOP) top_of_part<T, THREADS>(part, first, n, min(k, n), span_log2, sh);
     if (warp == 0) {
         x = warp_merge(lane < THREADS / 32 ? sums[lane] : RowSums{-INFINITY, 0.f, 0.f}, kd);
         if (lane == 0) mine = x;
     }
-    if (SHARED) {
+    if (TOP) {
+        const uint32_t bound = common_bound(sh, THREADS / 32);
+        gather<T, THREADS>(part, first, bound, span_log2, own.segment, own.hit[warp], head, rest, sh);
+        __syncthreads();
+        select<T, THREADS>(part, first, n, kk, bound, sh, [&](int at, uint64_t e) { sh.list[at] = e; });
+    }
+    if (blocks > 1) {
         cluster_sync();
         if (rank == 0 && warp == 0) {
             x = RowSums{-INFINITY, 0.f, 0.f};
@@ -484,58 +522,103 @@ __global__ void __launch_bounds__(THREADS, SHARED ? 1 : THREADS == 128 ? 10 : LP
     if (rank == 0) {
         if (threadIdx.x == 0) row_max = x.m;
         __syncthreads();
-        const float m = row_max;
-        const bool none = m == -INFINITY, odd = !none && m > -INFINITY && m < INFINITY && !(m > LP_LEAST && m < LP_MOST);
-        float logs, H;
-        if (odd) odd_row<T, THREADS>(z, V, m, c, reinterpret_cast<float*>(sums), logs, H);
-        if (threadIdx.x == 0) {
-            if (!odd) {
-                const float ln_s = logf(x.s);
-                logs = fmaf(fmaf(-m, kd, reference(m, kd)), kLn2, ln_s);
-                H = fmaxf(ln_s - kLn2 * (x.a / x.s), 0.f);
-                if (none) { logs = -INFINITY; H = 0.f; }
-                if (!(m < INFINITY)) x.m = logs = H = __int_as_float(0x7FC00000);
-            }
-            if (stats != nullptr) { stats[3ll * row] = x.m; stats[3ll * row + 1] = logs; stats[3ll * row + 2] = H; }
-            if (entropy != nullptr) entropy[row] = H;
-            if (logprobs != nullptr) logprobs[row] = token < 0 ? 0.f : none ? -INFINITY : (token_logit - x.m) * c - logs;
-            if (TOP) { result[0] = x.m; result[1] = logs; result[2] = none ? 1.f : 0.f; }
-        }
+        const bool odd = is_odd(row_max);
+        float logs = 0.f, H = 0.f;
+        if (odd) odd_row<T, THREADS>(z, V, row_max, p.c, reinterpret_cast<float*>(sums), logs, H);
+        if (threadIdx.x == 0) result = tell_row(p, row, x, kd, odd, logs, H, token, token_logit);
     }
     if (TOP && rank == 0) {
+        // an entry's place in the whole: its own list's plus, list by list, the number of larger ones (every list has k: a part of a shared
+        // row is longer than that)
+        for (int e = threadIdx.x; blocks > 1 && e < blocks * k; e += THREADS) {
+            const int r = e / k;
+            sh.cand[e] = remote_u64(&sh.list[e - r * k], r);
+        }
         __syncthreads();
-        auto put = [&](int at, uint64_t e) {
-            if (top_ids != nullptr) top_ids[(long long)row * k + at] = entry_place(e);
-            if (top_logprobs != nullptr) top_logprobs[(long long)row * k + at] = result[2] != 0.f ? -INFINITY : (entry_logit(e) - result[0]) * c - result[1];
-        };
-        if (!SHARED) {
-            if ((int)threadIdx.x < k) put(threadIdx.x, sh.list[threadIdx.x]);
-        } else {
-            // an entry's place in the whole: its own list's plus, list by list, the number of larger ones (every list has k: a part of a shared
-            // row is longer than that)
-            for (int e = threadIdx.x; e < blocks * k; e += THREADS) {
-                const int r = e / k;
-                sh.cand[e] = remote_u64(&sh.list[e - r * k], r);
-            }
-            __syncthreads();
-            for (int e = threadIdx.x; e < blocks * k; e += THREADS) {
-                const uint64_t it = sh.cand[e];
-                const int own = e / k;
-                int at = e - own * k;
-                for (int r = 0; r < blocks; ++r) {
-                    int lo = 0, hi = r == own ? 0 : k;               // entries before lo are larger, those from hi on are not
-                    while (lo < hi) {
-                        const int mid = (lo + hi) >> 1;
-                        if (sh.cand[r * k + mid] > it) lo = mid + 1; else hi = mid;
-                    }
-                    at += lo;
-                    if (at >= k) break;
+        for (int e = threadIdx.x; e < blocks * k; e += THREADS) {
+            const uint64_t it = blocks > 1 ? sh.cand[e] : sh.list[e];
+            const int of = e / k;
+            int at = e - of * k;
+            for (int r = 0; r < blocks; ++r) {
+                int lo = 0, hi = r == of ? 0 : k;                    // entries before lo are larger, those from hi on are not
+                while (lo < hi) {
+                    const int mid = (lo + hi) >> 1;
+                    if (sh.cand[r * k + mid] > it) lo = mid + 1; else hi = mid;
                 }
-                if (at < k) put(at, it);
+                at += lo;
+                if (at >= k) break;
             }
+            if (at < k) tell_top(p, row, at, it, result);
         }
     }
-    if (SHARED) cluster_sync();                                  // (nobody leaves while the first block reads)
+    if (blocks > 1) cluster_sync();                                  // (nobody leaves while the first block reads)
+}
+
+#ifndef RB
+#define RB 6
+#define RBT 6
+#define NB 10
+#define NBT 10
+#endif
+// Many rows: one to a block.
+template <typename T, int THREADS, bool TOP>
+__global__ void __launch_bounds__(THREADS, THREADS == 128 ? (TOP ? NBT : NB) : (TOP ? RBT : RB)) logprobs_rows_kernel(const __grid_constant__ LogprobArgs p) {
+    __shared__ RowSums sums[THREADS / 32];
+    __shared__ RowResult result;
+    __shared__ float odd_sums[2 * (THREADS / 32)];
+    __shared__ __align__(16) unsigned char top_raw[TOP ? sizeof(TopShared) : 16], warps_raw[TOP ? sizeof(TopWarps<THREADS>) : 16];
+    TopShared& sh = *reinterpret_cast<TopShared*>(top_raw);
+    TopWarps<THREADS>& own = *reinterpret_cast<TopWarps<THREADS>*>(warps_raw);
+    pdl_launch_dependents();
+    pdl_wait();
+    const int row = blockIdx.x, V = p.V, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const float kd = p.c * kLog2e;
+    const T* z = static_cast<const T*>(p.logits) + row * p.stride;
+    const RowParts<T> part(z, V);
+    const int token = threadIdx.x == 0 && p.logprobs != nullptr ? p.tokens[row] : -1;
+    const float head = (int)threadIdx.x < part.head ? lp_f(part.z[threadIdx.x]) : -INFINITY;
+    const float rest = (int)threadIdx.x < part.rest ? lp_f(part.z[part.tail + threadIdx.x]) : -INFINITY;
+    const int span_log2 = span_of<THREADS>(part.vectors);
+    ThreadRow<T, THREADS, TOP> mine(own.segment, span_log2);
+    int c0 = threadIdx.x;
+    for (; c0 + (LP_UNROLL - 1) * THREADS < part.vectors; c0 += LP_UNROLL * THREADS) {
+        uint4 v[LP_UNROLL];
+#pragma unroll
+        for (int u = 0; u < LP_UNROLL; ++u) v[u] = load_stream(part.body() + c0 + u * THREADS);
+        mine.template round<true>(v, c0, part.vectors, kd);
+    }
+    if (c0 < part.vectors) {
+        uint4 v[LP_UNROLL];
+#pragma unroll
+        for (int u = 0; u < LP_UNROLL; ++u)
+            if (c0 + u * THREADS < part.vectors) v[u] = load_stream(part.body() + c0 + u * THREADS);
+        mine.template round<false>(v, c0, part.vectors, kd);
+    }
+    mine.finish();
+    const float token_logit = token >= 0 && token < V ? lp_f(z[token]) : 0.f;
+    if ((int)threadIdx.x < part.head) add_one(mine.x, head, kd);
+    if ((int)threadIdx.x < part.rest) add_one(mine.x, rest, kd);
+    if (TOP) offer_bound<THREADS>(part.vectors, p.k, mine.x.m, sh);
+    RowSums x = warp_merge(mine.x, kd);
+    if (lane == 0) sums[warp] = x;
+    __syncthreads();
+    x = sums[lane & (THREADS / 32 - 1)];
+    float m = x.m;
+#pragma unroll
+    for (int o = THREADS / 64; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    const bool odd = is_odd(m);
+    float logs = 0.f, H = 0.f;
+    if (odd) odd_row<T, THREADS>(z, V, m, p.c, odd_sums, logs, H);
+    if (warp == 0) {
+        x = warp_merge(lane < THREADS / 32 ? x : RowSums{-INFINITY, 0.f, 0.f}, kd);
+        if (lane == 0) result = tell_row(p, row, x, kd, odd, logs, H, token >= 0 && token < V ? token : -1, token_logit);
+    }
+    if (TOP) {
+        const uint32_t bound = common_bound(sh, THREADS / 32);
+        gather<T, THREADS>(part, 0, bound, span_log2, own.segment, own.hit[warp], head, rest, sh);
+        __syncthreads();
+        select<T, THREADS>(part, 0, V, p.k, bound, sh, [&](int at, uint64_t e) { tell_top(p, row, at, e, result); });
+    }
 }
 
 template <typename T>
@@ -564,39 +647,33 @@ __global__ void __launch_bounds__(LP_BWD_THREADS) logprobs_bwd_kernel(int V, lon
 
 // Blocks that share a row: as many as still fit the SMs all at once, while each has 4 KB of it at least.
 static int row_blocks(int T, long long row_bytes, int sms) {
-#ifdef LPC
-    return LPC;
-#endif
     int blocks = 1;
     while (blocks < LP_CLUSTER && (long long)T * blocks * 2 <= 2 * sms && row_bytes / (blocks * 2) >= 4096) blocks *= 2;
     return blocks;
 }
 
+template <typename T, bool TOP>
+static cudaError_t launch_logprobs_shared(const LogprobArgs& p, cudaStream_t st) {
+    return launch_pdl(logprobs_shared_kernel<T, 256, TOP>, dim3((unsigned)p.T * (unsigned)p.blocks), dim3(256), 0, st, (unsigned)p.blocks, p);
+}
+template <typename T, int THREADS, bool TOP>
+static cudaError_t launch_logprobs_rows(const LogprobArgs& p, cudaStream_t st) {
+    return launch_pdl(logprobs_rows_kernel<T, THREADS, TOP>, dim3((unsigned)p.T), dim3(THREADS), 0, st, 1, p);
+}
+template <typename T>
+static cudaError_t launch_logprobs(const LogprobArgs& p, cudaStream_t st) {
+    const bool top = p.k > 0;
+    if (p.blocks > 1) return top ? launch_logprobs_shared<T, true>(p, st) : launch_logprobs_shared<T, false>(p, st);
+    const bool narrow = (long long)p.V * (int)sizeof(T) <= 8192;
+    if (narrow) return top ? launch_logprobs_rows<T, 128, true>(p, st) : launch_logprobs_rows<T, 128, false>(p, st);
+    return top ? launch_logprobs_rows<T, 256, true>(p, st) : launch_logprobs_rows<T, 256, false>(p, st);
+}
+
 int launch_token_logprobs(int T, int V, long long row_stride, int dtype, const void* logits, const int32_t* tokens, float c, int k, float* logprobs,
                           float* entropy, int32_t* top_ids, float* top_logprobs, float* stats, cudaStream_t st) {
-    const bool top = k > 0;
-    const long long row_bytes = (long long)V * (dtype == QLORA_FP32 ? 4 : 2);
-    const int blocks = row_blocks(T, row_bytes, sm_count());
-    const bool narrow = row_bytes / blocks <= 8192;
-    cudaError_t err;
-#define QLORA_LP(TYPE, THREADS, TOP, SHARED)                                                                                                        \
-    err = launch_pdl(logprobs_kernel<TYPE, THREADS, TOP, SHARED>, dim3((unsigned)T * (unsigned)blocks), dim3(THREADS), 0, st, (unsigned)blocks, V,   \
-                     row_stride, (const TYPE*)logits, tokens, c, k, blocks, logprobs, entropy, top_ids, top_logprobs, stats)
-#ifndef LPT
-#define LPT 256
-#endif
-#ifndef LPS
-#define LPS 256
-#endif
-#define QLORA_LP_TYPE(TYPE)                                                                                                                        \
-    if (blocks > 1) { if (top) QLORA_LP(TYPE, LPS, true, true); else QLORA_LP(TYPE, LPS, false, true); }                                             \
-    else if (narrow) { if (top) QLORA_LP(TYPE, 128, true, false); else QLORA_LP(TYPE, 128, false, false); }                                          \
-    else { if (top) QLORA_LP(TYPE, LPT, true, false); else QLORA_LP(TYPE, LPT, false, false); }
-    if (dtype == QLORA_BF16) { QLORA_LP_TYPE(__nv_bfloat16) }
-    else if (dtype == QLORA_FP16) { QLORA_LP_TYPE(__half) }
-    else { QLORA_LP_TYPE(float) }
-#undef QLORA_LP_TYPE
-#undef QLORA_LP
+    LogprobArgs p{T, V, k, 1, row_stride, logits, tokens, c, logprobs, entropy, stats, top_logprobs, top_ids};
+    p.blocks = row_blocks(T, (long long)V * (dtype == QLORA_FP32 ? 4 : 2), sm_count());
+    const cudaError_t err = dtype == QLORA_BF16 ? launch_logprobs<__nv_bfloat16>(p, st) : dtype == QLORA_FP16 ? launch_logprobs<__half>(p, st) : launch_logprobs<float>(p, st);
     return err == cudaSuccess ? QLORA_OK : QLORA_ERR_CUDA;
 }
 
