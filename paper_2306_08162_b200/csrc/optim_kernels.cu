@@ -10,48 +10,38 @@
 
 namespace qlora {
 
-constexpr int OP_BLOCK = 256;            // elements that share one scale of the 8-bit states
+constexpr int OP_BLOCK = 256;            // elements that share one scale of the 8-bit states, and that a warp handles at a time
 constexpr int OP_THREADS = 256;
-constexpr int OP_TABLE = 448;            // tensors per launch: their table travels in the kernel's parameters (32764 bytes at most)
+constexpr int OP_TABLE = 448, OP_SMALL_TABLE = 16;   // tensors per launch: their table travels in the kernel's parameters (32764 bytes at most)
 constexpr int OP_PARTIALS = QLORA_GRAD_NORM_WORKSPACE_BYTES / sizeof(double);
 
 // The tensors of one launch, cut into chunks of `chunk` elements (the last one of a tensor may be shorter): chunk c belongs to the tensor
 // j with first[j] <= c < first[j + 1].
+template <int CAP>
 struct OptTable {
-    qlora_adamw_tensor t[OP_TABLE];
-    uint32_t first[OP_TABLE + 1];
+    qlora_adamw_tensor t[CAP];
+    uint32_t first[CAP + 1];
     int n, chunk;
 };
 
 struct AdamScalars {
     float beta1, one_minus_beta1, beta2, one_minus_beta2, eps, weight_decay;
     float log_beta1, log_beta2;          // for a step number that is in device memory
-    float lr, corr1, corr2;              // the rate, 1 - beta1^step, 1 - beta2^step
+    float lr, inv_corr1, inv_corr2;      // the rate, 1 / (1 - beta1^step), 1 / (1 - beta2^step)
     int step;
     const float* lr_dev;
     const int32_t* step_dev;
     const float* norm;
 };
 
-__device__ __forceinline__ int tensor_of_chunk(const OptTable& tab, uint32_t c) {
+template <int CAP>
+__device__ __forceinline__ int tensor_of_chunk(const OptTable<CAP>& tab, uint32_t c) {
     int lo = 0, hi = tab.n;              // first[lo] <= c < first[hi]
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (tab.first[mid] <= c) lo = mid; else hi = mid;
     }
     return lo;
-}
-
-__device__ __forceinline__ float to_f(float x) { return x; }
-__device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
-template <typename T> __device__ __forceinline__ T from_f(float x);
-template <> __device__ __forceinline__ float from_f<float>(float x) { return x; }
-template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
-template <> __device__ __forceinline__ __half from_f<__half>(float x) { return __float2half_rn(x); }
-
-__device__ __forceinline__ float e4m3_to_f(uint8_t code) {
-    return __half2float(__half(__nv_cvt_fp8_to_halfraw(code, __NV_E4M3)));
 }
 
 // Two numbers in [0, 2^20) from an element's place in its tensor and the number of the step.
@@ -71,82 +61,175 @@ __device__ __forceinline__ float dithered_e4m3(float x, uint32_t dither) {
     return copysignf(fminf(y, 448.f), x);
 }
 
-// One warp per 256 elements (8 per lane).
-template <typename P, typename G, bool EIGHT>
-__global__ void __launch_bounds__(OP_THREADS) adamw_kernel(const __grid_constant__ OptTable tab, const __grid_constant__ AdamScalars sc) {
-    pdl_launch_dependents();
-    pdl_wait();
+// Four consecutive elements (of 16-byte aligned tensors, at a multiple of 4).
+__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    return make_float4(bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y));
+}
+__device__ __forceinline__ float4 load4(const __half* p) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&v.x)), b = __half22float2(*reinterpret_cast<const __half2*>(&v.y));
+    return make_float4(a.x, a.y, b.x, b.y);
+}
+__device__ __forceinline__ float4 load4(const uint8_t* p) {             // e4m3
+    const uint32_t v = *reinterpret_cast<const uint32_t*>(p);
+    const __half2 a = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(v & 0xFFFFu), __NV_E4M3));
+    const __half2 b = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(v >> 16), __NV_E4M3));
+    const float2 x = __half22float2(a), y = __half22float2(b);
+    return make_float4(x.x, x.y, y.x, y.y);
+}
+__device__ __forceinline__ void store4(float* p, const float* v) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, const float* v) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
+    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+__device__ __forceinline__ void store4(__half* p, const float* v) {
+    const __half2 a = __floats2half2_rn(v[0], v[1]), b = __floats2half2_rn(v[2], v[3]);
+    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+__device__ __forceinline__ void store4(uint8_t* p, const float* v) {     // values that e4m3 holds
+    const uint32_t a = __nv_cvt_float2_to_fp8x2(make_float2(v[0], v[1]), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t b = __nv_cvt_float2_to_fp8x2(make_float2(v[2], v[3]), __NV_SATFINITE, __NV_E4M3);
+    *reinterpret_cast<uint32_t*>(p) = a | b << 16;
+}
+__device__ __forceinline__ float one(const float* p) { return *p; }
+__device__ __forceinline__ float one(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ float one(const __half* p) { return __half2float(*p); }
+__device__ __forceinline__ float one(const uint8_t* p) { return __half2float(__half(__nv_cvt_fp8_to_halfraw(*p, __NV_E4M3))); }
+__device__ __forceinline__ void put_one(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put_one(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+__device__ __forceinline__ void put_one(__half* p, float v) { *p = __float2half_rn(v); }
+__device__ __forceinline__ void put_one(uint8_t* p, float v) { *p = __nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3); }
+
+// This lane's 8 of a block of 256 elements: 4 at 4 lane and 4 at 128 + 4 lane, so that every access of a warp is contiguous.  `left`: elements of
+// the block that are there (256 but for the last block of a tensor).
+template <typename E>
+__device__ __forceinline__ void load8(const E* p, int lane, int left, float (&v)[8]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int at = 128 * h + 4 * lane;
+        if (at + 4 <= left) {
+            const float4 x = load4(p + at);
+            v[4 * h] = x.x; v[4 * h + 1] = x.y; v[4 * h + 2] = x.z; v[4 * h + 3] = x.w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[4 * h + i] = at + i < left ? one(p + at + i) : 0.f;
+        }
+    }
+}
+template <typename E>
+__device__ __forceinline__ void store8(E* p, int lane, int left, const float (&v)[8]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int at = 128 * h + 4 * lane;
+        if (at + 4 <= left) store4(p + at, v + 4 * h);
+        else
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (at + i < left) put_one(p + at + i, v[4 * h + i]);
+    }
+}
+
+__device__ __forceinline__ float fast_sqrt(float x) {                     // (of the root's and the quotient's errors, 2^-22, nothing is left after the weight's rounding)
+    float r;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// 8-bit form of a block's values: the scale (for one lane to store) and the codes' values.
+template <bool ROOT>
+__device__ __forceinline__ float to_codes(float (&x)[8], const uint32_t (&dither)[8]) {
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(fabsf(x[i])));
+    top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top)));   // (from 0 on the bits are in order; a NaN is above all and makes the scale one)
+    const bool held = !(top <= 0x1p-100f);
+    const float inv = held ? 448.f / top : 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float y = x[i] * inv, c = dithered_e4m3(y, dither[i]);
+        x[i] = ROOT && y > 0.f ? fmaxf(c, 0x1p-9f) : c;
+    }
+    return held ? top * (1.f / 448.f) : 0.f;
+}
+
+// One warp per block of 256 elements (8 per lane).
+template <typename P, typename G, bool EIGHT, int CAP>
+__global__ void __launch_bounds__(OP_THREADS) adamw_kernel(const __grid_constant__ OptTable<CAP> tab, const __grid_constant__ AdamScalars sc) {
+    __shared__ float corr[2];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    pdl_launch_dependents();
     const int j = tensor_of_chunk(tab, blockIdx.x);
     const qlora_adamw_tensor& t = tab.t[j];
     const long long begin = (long long)(blockIdx.x - tab.first[j]) * tab.chunk;
     const long long end = begin + tab.chunk < t.n ? begin + tab.chunk : t.n;
+    pdl_wait();
     const float f = sc.norm != nullptr ? sc.norm[1] : 1.f;
-    if (!(fabsf(f) <= 3.402823466e38f)) return;
     const float lr = sc.lr_dev != nullptr ? *sc.lr_dev : sc.lr;
-    int step = sc.step;
-    float corr1 = sc.corr1, corr2 = sc.corr2;
+    const int step = sc.step_dev != nullptr ? *sc.step_dev : sc.step;
+    float inv1 = sc.inv_corr1, inv2 = sc.inv_corr2;
     if (sc.step_dev != nullptr) {
-        step = *sc.step_dev;
-        corr1 = -expm1f((float)step * sc.log_beta1);
-        corr2 = -expm1f((float)step * sc.log_beta2);
+        if (threadIdx.x == 0) {
+            corr[0] = 1.f / -expm1f((float)step * sc.log_beta1);
+            corr[1] = 1.f / -expm1f((float)step * sc.log_beta2);
+        }
+        __syncthreads();
+        inv1 = corr[0];
+        inv2 = corr[1];
     }
+    if (!(fabsf(f) < INFINITY)) return;
+    const float keep = 1.f - lr * sc.weight_decay, rate = lr * inv1;
     for (long long base = begin + warp * OP_BLOCK; base < end; base += OP_THREADS / 32 * OP_BLOCK) {
-        float m[8], v[8];
-        float ms = 0.f, us = 0.f;
-        if (EIGHT) { ms = t.m_scale[base / OP_BLOCK]; us = t.v_scale[base / OP_BLOCK]; }
-        float top_m = 0.f, top_u = 0.f;
+        const int left = (int)(end - base < OP_BLOCK ? end - base : OP_BLOCK);
+        float g[8], w[8], m[8], v[8];
+        load8(static_cast<const G*>(t.grad) + base, lane, left, g);
+        if (t.master != nullptr) load8(t.master + base, lane, left, w);
+        else load8(static_cast<const P*>(t.param) + base, lane, left, w);
+        float ms = 1.f, us = 1.f;
+        if constexpr (EIGHT) {
+            load8(static_cast<const uint8_t*>(t.m) + base, lane, left, m);
+            load8(static_cast<const uint8_t*>(t.v) + base, lane, left, v);
+            ms = t.m_scale[base / OP_BLOCK];
+            us = t.v_scale[base / OP_BLOCK];
+        } else {
+            load8(static_cast<const float*>(t.m) + base, lane, left, m);
+            load8(static_cast<const float*>(t.v) + base, lane, left, v);
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const long long e = base + i * 32 + lane;
-            m[i] = v[i] = 0.f;
-            if (e >= end) continue;
-            const float g = f * to_f(static_cast<const G*>(t.grad)[e]);
-            if (EIGHT) {
-                m[i] = ms * e4m3_to_f(static_cast<const uint8_t*>(t.m)[e]);
-                const float u = us * e4m3_to_f(static_cast<const uint8_t*>(t.v)[e]);
-                v[i] = u * u;
-            } else {
-                m[i] = static_cast<const float*>(t.m)[e];
-                v[i] = static_cast<const float*>(t.v)[e];
+            const float gi = f * g[i];
+            if constexpr (EIGHT) {
+                m[i] *= ms;
+                v[i] *= us;
+                v[i] *= v[i];
             }
-            m[i] = sc.beta1 * m[i] + sc.one_minus_beta1 * g;
-            v[i] = sc.beta2 * v[i] + sc.one_minus_beta2 * (g * g);
-            float w = t.master != nullptr ? t.master[e] : to_f(static_cast<const P*>(t.param)[e]);
-            w = w * (1.f - lr * sc.weight_decay) - lr * ((m[i] / corr1) / (sqrtf(v[i] / corr2) + sc.eps));
-            if (t.master != nullptr) t.master[e] = w;
-            static_cast<P*>(t.param)[e] = from_f<P>(w);
-            if (EIGHT) {
-                v[i] = sqrtf(v[i]);
-                top_m = fmaxf(top_m, fabsf(m[i]));
-                top_u = fmaxf(top_u, v[i]);
-            } else {
-                static_cast<float*>(t.m)[e] = m[i];
-                static_cast<float*>(t.v)[e] = v[i];
-            }
+            m[i] = fmaf(sc.beta1, m[i], sc.one_minus_beta1 * gi);
+            v[i] = fmaf(sc.beta2, v[i], sc.one_minus_beta2 * (gi * gi));
+            w[i] = fmaf(w[i], keep, -__fdividef(rate * m[i], fast_sqrt(v[i] * inv2) + sc.eps));
         }
-        if (EIGHT) {
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                top_m = fmaxf(top_m, __shfl_xor_sync(0xFFFFFFFFu, top_m, o));
-                top_u = fmaxf(top_u, __shfl_xor_sync(0xFFFFFFFFu, top_u, o));
-            }
-            const float im = top_m > 0x1p-100f ? 448.f / top_m : 0.f, iu = top_u > 0x1p-100f ? 448.f / top_u : 0.f;
-            if (lane == 0) {
-                t.m_scale[base / OP_BLOCK] = top_m > 0x1p-100f ? top_m * (1.f / 448.f) : 0.f;
-                t.v_scale[base / OP_BLOCK] = top_u > 0x1p-100f ? top_u * (1.f / 448.f) : 0.f;
-            }
+        if (t.master != nullptr) store8(t.master + base, lane, left, w);
+        store8(static_cast<P*>(t.param) + base, lane, left, w);
+        if constexpr (EIGHT) {
+            uint32_t dm[8], du[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const long long e = base + i * 32 + lane;
-                if (e >= end) continue;
-                const uint2 r = dither_of((uint32_t)e, (uint32_t)step);
-                const float cm = dithered_e4m3(m[i] * im, r.x), xu = v[i] * iu;
-                float cu = dithered_e4m3(xu, r.y);
-                if (xu > 0.f) cu = fmaxf(cu, 0x1p-9f);
-                static_cast<uint8_t*>(t.m)[e] = __nv_cvt_float_to_fp8(cm, __NV_SATFINITE, __NV_E4M3);
-                static_cast<uint8_t*>(t.v)[e] = __nv_cvt_float_to_fp8(cu, __NV_SATFINITE, __NV_E4M3);
+                const uint2 r = dither_of((uint32_t)(base + 128 * (i / 4) + 4 * lane + i % 4), (uint32_t)step);
+                dm[i] = r.x;
+                du[i] = r.y;
+                v[i] = fast_sqrt(v[i]);
             }
+            ms = to_codes<false>(m, dm);                             // (elements that are not there are zeros: gradient, moments, codes)
+            us = to_codes<true>(v, du);
+            store8(static_cast<uint8_t*>(t.m) + base, lane, left, m);
+            store8(static_cast<uint8_t*>(t.v) + base, lane, left, v);
+            if (lane == 0) {
+                t.m_scale[base / OP_BLOCK] = ms;
+                t.v_scale[base / OP_BLOCK] = us;
+            }
+        } else {
+            store8(static_cast<float*>(t.m) + base, lane, left, m);
+            store8(static_cast<float*>(t.v) + base, lane, left, v);
         }
     }
 }
@@ -164,24 +247,35 @@ __device__ __forceinline__ double block_sum(double v) {           // the sum in 
     return v;
 }
 
-// Sums of squares, one per block of the launch; `add`: on top of the previous launch's (more tensors than one table holds).
-template <typename G>
-__global__ void __launch_bounds__(OP_THREADS) grad_square_kernel(const __grid_constant__ OptTable tab, float prescale, int add, double* __restrict__ partial) {
+// Sums of squares in 64 bits (a square can leave fp32's range, and HBM leaves the time), one per block of the launch; `add`: on top of the previous launch's
+// (more tensors than one table holds).
+template <typename G, int CAP>
+__global__ void __launch_bounds__(OP_THREADS) grad_square_kernel(const __grid_constant__ OptTable<CAP> tab, float prescale, int add, double* __restrict__ partial) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_launch_dependents();
-    pdl_wait();
     double acc = 0.0;
+    bool waited = false;
     for (uint32_t c = blockIdx.x; c < tab.first[tab.n]; c += gridDim.x) {
         const int j = tensor_of_chunk(tab, c);
         const qlora_adamw_tensor& t = tab.t[j];
         const long long begin = (long long)(c - tab.first[j]) * tab.chunk;
         const long long end = begin + tab.chunk < t.n ? begin + tab.chunk : t.n;
-        const G* g = static_cast<const G*>(t.grad);
-        for (long long e = begin + threadIdx.x; e < end; e += OP_THREADS) {
-            const double x = (double)to_f(g[e]) * (double)prescale;
-            acc = fma(x, x, acc);
+        if (!waited) { pdl_wait(); waited = true; }
+        for (long long base = begin + warp * OP_BLOCK; base < end; base += 2 * (OP_THREADS / 32 * OP_BLOCK)) {
+            float g[2][8];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const long long at = base + u * (OP_THREADS / 32 * OP_BLOCK), left = end - at;
+                load8(static_cast<const G*>(t.grad) + at, lane, (int)(left < 0 ? 0 : left < OP_BLOCK ? left : OP_BLOCK), g[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc = fma((double)g[u][i], (double)g[u][i], acc);
         }
     }
-    acc = block_sum(acc);
+    if (!waited) pdl_wait();
+    acc = block_sum(acc) * (double)prescale * (double)prescale;
     if (threadIdx.x == 0) partial[blockIdx.x] = add ? partial[blockIdx.x] + acc : acc;
 }
 
@@ -196,17 +290,18 @@ __global__ void __launch_bounds__(OP_THREADS) grad_norm_kernel(int n, const doub
         out[0] = norm;
         float f = prescale;
         if (max_norm > 0.f && norm > max_norm) f = prescale * (max_norm / norm);
-        if (!(norm <= 3.402823466e38f)) f = __int_as_float(0x7FC00000);
+        if (!(norm < INFINITY)) f = __int_as_float(0x7FC00000);
         out[1] = f;
     }
 }
 
 // Fills the table with tensors from *at on; returns the number of chunks (0: nothing left).
-static uint32_t fill_table(const qlora_adamw_desc& d, int* at, int chunk, OptTable& tab) {
+template <int CAP>
+static uint32_t fill_table(const qlora_adamw_desc& d, int* at, int chunk, OptTable<CAP>& tab) {
     uint32_t chunks = 0;
     tab.n = 0;
     tab.chunk = chunk;
-    while (*at < d.n_tensors && tab.n < OP_TABLE) {
+    while (*at < d.n_tensors && tab.n < CAP) {
         const qlora_adamw_tensor& t = d.tensors[*at];
         const uint32_t c = (uint32_t)((t.n + chunk - 1) / chunk);
         if (chunks > 0 && chunks + c > 0x7FFFFFFFu) break;
@@ -221,63 +316,75 @@ static uint32_t fill_table(const qlora_adamw_desc& d, int* at, int chunk, OptTab
     return chunks;
 }
 
-static int chunk_of(const qlora_adamw_desc& d) {
-    (void)d;
-    return 2048;
-}
+#ifndef AC
+#define AC 2048
+#define NC 8192
+#define NB 4
+#endif
+static int adamw_chunk(const qlora_adamw_desc& d) { return AC; }
+static int norm_chunk(const qlora_adamw_desc& d) { return NC; }
 
-int launch_grad_norm(const qlora_adamw_desc& d, float prescale, float max_norm, float* out, void* workspace, cudaStream_t st) {
-    static thread_local OptTable tab;
+template <int CAP>
+static int launch_grad_norm_with(const qlora_adamw_desc& d, float prescale, float max_norm, float* out, void* workspace, cudaStream_t st) {
+    static thread_local OptTable<CAP> tab;
     double* partial = static_cast<double*>(workspace);
+    const int chunk = norm_chunk(d), most = NB * sm_count() < OP_PARTIALS ? NB * sm_count() : OP_PARTIALS;
     int at = 0, used = 0;
     for (int launch = 0;; ++launch) {
-        const uint32_t chunks = fill_table(d, &at, chunk_of(d), tab);
+        const uint32_t chunks = fill_table(d, &at, chunk, tab);
         if (chunks == 0) break;
         // (every launch on the grid of the first, whose partial sums the later ones add to)
-        if (launch == 0) used = (int)(chunks < (uint32_t)OP_PARTIALS ? chunks : (uint32_t)OP_PARTIALS);
+        if (launch == 0) used = (int)(chunks < (uint32_t)most ? chunks : (uint32_t)most);
         cudaError_t err;
-        if (d.grad_type == QLORA_FP32) err = launch_pdl(grad_square_kernel<float>, dim3(used), dim3(OP_THREADS), 0, st, 1, tab, prescale, launch, partial);
-        else if (d.grad_type == QLORA_BF16) err = launch_pdl(grad_square_kernel<__nv_bfloat16>, dim3(used), dim3(OP_THREADS), 0, st, 1, tab, prescale, launch, partial);
-        else err = launch_pdl(grad_square_kernel<__half>, dim3(used), dim3(OP_THREADS), 0, st, 1, tab, prescale, launch, partial);
+        if (d.grad_type == QLORA_FP32) err = launch_pdl(grad_square_kernel<float, CAP>, dim3(used), dim3(OP_THREADS), 0, st, 1, tab, prescale, launch, partial);
+        else if (d.grad_type == QLORA_BF16) err = launch_pdl(grad_square_kernel<__nv_bfloat16, CAP>, dim3(used), dim3(OP_THREADS), 0, st, 1, tab, prescale, launch, partial);
+        else err = launch_pdl(grad_square_kernel<__half, CAP>, dim3(used), dim3(OP_THREADS), 0, st, 1, tab, prescale, launch, partial);
         if (err != cudaSuccess) return QLORA_ERR_CUDA;
     }
     return launch_pdl(grad_norm_kernel, dim3(1), dim3(OP_THREADS), 0, st, 1, used, partial, prescale, max_norm, out) == cudaSuccess ? QLORA_OK : QLORA_ERR_CUDA;
 }
 
-template <typename P, typename G>
-static cudaError_t launch_adamw_as(bool eight, uint32_t chunks, const OptTable& tab, const AdamScalars& sc, cudaStream_t st) {
-    if (eight) return launch_pdl(adamw_kernel<P, G, true>, dim3(chunks), dim3(OP_THREADS), 0, st, 1, tab, sc);
-    return launch_pdl(adamw_kernel<P, G, false>, dim3(chunks), dim3(OP_THREADS), 0, st, 1, tab, sc);
+int launch_grad_norm(const qlora_adamw_desc& d, float prescale, float max_norm, float* out, void* workspace, cudaStream_t st) {
+    return d.n_tensors <= OP_SMALL_TABLE ? launch_grad_norm_with<OP_SMALL_TABLE>(d, prescale, max_norm, out, workspace, st)
+                                         : launch_grad_norm_with<OP_TABLE>(d, prescale, max_norm, out, workspace, st);
 }
 
-template <typename P>
-static cudaError_t launch_adamw_param(int grad_type, bool eight, uint32_t chunks, const OptTable& tab, const AdamScalars& sc, cudaStream_t st) {
+template <typename P, typename G, int CAP>
+static cudaError_t launch_adamw_as(bool eight, uint32_t chunks, const OptTable<CAP>& tab, const AdamScalars& sc, cudaStream_t st) {
+    if (eight) return launch_pdl(adamw_kernel<P, G, true, CAP>, dim3(chunks), dim3(OP_THREADS), 0, st, 1, tab, sc);
+    return launch_pdl(adamw_kernel<P, G, false, CAP>, dim3(chunks), dim3(OP_THREADS), 0, st, 1, tab, sc);
+}
+template <typename P, int CAP>
+static cudaError_t launch_adamw_param(int grad_type, bool eight, uint32_t chunks, const OptTable<CAP>& tab, const AdamScalars& sc, cudaStream_t st) {
     if (grad_type == QLORA_FP32) return launch_adamw_as<P, float>(eight, chunks, tab, sc, st);
     if (grad_type == QLORA_BF16) return launch_adamw_as<P, __nv_bfloat16>(eight, chunks, tab, sc, st);
     return launch_adamw_as<P, __half>(eight, chunks, tab, sc, st);
 }
+template <int CAP>
+static int launch_adamw_with(const qlora_adamw_desc& d, const AdamScalars& sc, cudaStream_t st) {
+    static thread_local OptTable<CAP> tab;
+    int at = 0;
+    for (;;) {
+        const uint32_t chunks = fill_table(d, &at, adamw_chunk(d), tab);
+        if (chunks == 0) return QLORA_OK;
+        const bool eight = d.state_type == QLORA_E4M3;
+        const cudaError_t err = d.param_type == QLORA_BF16 ? launch_adamw_param<__nv_bfloat16>(d.grad_type, eight, chunks, tab, sc, st)
+                                : d.param_type == QLORA_FP16 ? launch_adamw_param<__half>(d.grad_type, eight, chunks, tab, sc, st)
+                                                             : launch_adamw_param<float>(d.grad_type, eight, chunks, tab, sc, st);
+        if (err != cudaSuccess) return QLORA_ERR_CUDA;
+    }
+}
 
 int launch_adamw(const qlora_adamw_desc& d, double lr, int step, const float* lr_dev, const int32_t* step_dev, const float* norm, cudaStream_t st) {
-    static thread_local OptTable tab;
     AdamScalars sc;
     sc.beta1 = (float)d.beta1; sc.one_minus_beta1 = (float)(1.0 - d.beta1);
     sc.beta2 = (float)d.beta2; sc.one_minus_beta2 = (float)(1.0 - d.beta2);
     sc.eps = (float)d.eps; sc.weight_decay = (float)d.weight_decay;
     sc.log_beta1 = (float)log(d.beta1); sc.log_beta2 = (float)log(d.beta2);
     sc.lr = (float)lr;
-    sc.corr1 = (float)-expm1(step * log(d.beta1)); sc.corr2 = (float)-expm1(step * log(d.beta2));
+    sc.inv_corr1 = (float)(-1.0 / expm1(step * log(d.beta1))); sc.inv_corr2 = (float)(-1.0 / expm1(step * log(d.beta2)));
     sc.step = step; sc.lr_dev = lr_dev; sc.step_dev = step_dev; sc.norm = norm;
-    int at = 0;
-    for (;;) {
-        const uint32_t chunks = fill_table(d, &at, chunk_of(d), tab);
-        if (chunks == 0) return QLORA_OK;
-        cudaError_t err;
-        const bool eight = d.state_type == QLORA_E4M3;
-        if (d.param_type == QLORA_BF16) err = launch_adamw_param<__nv_bfloat16>(d.grad_type, eight, chunks, tab, sc, st);
-        else if (d.param_type == QLORA_FP16) err = launch_adamw_param<__half>(d.grad_type, eight, chunks, tab, sc, st);
-        else err = launch_adamw_param<float>(d.grad_type, eight, chunks, tab, sc, st);
-        if (err != cudaSuccess) return QLORA_ERR_CUDA;
-    }
+    return d.n_tensors <= OP_SMALL_TABLE ? launch_adamw_with<OP_SMALL_TABLE>(d, sc, st) : launch_adamw_with<OP_TABLE>(d, sc, st);
 }
 
 }  // namespace qlora
