@@ -256,7 +256,7 @@ typedef struct {
     int grad_type;                     /* QLORA_FP32 (what qlora_bwd_lora writes), QLORA_BF16 or QLORA_FP16 */
     int state_type;                    /* QLORA_FP32 or QLORA_E4M3 */
     double beta1, beta2;               /* in [0, 1) */
-    double eps;                        /* > 0 */
+    double eps;                        /* >= 1e-30 */
     double weight_decay;               /* >= 0 */
 } qlora_adamw_desc;
 

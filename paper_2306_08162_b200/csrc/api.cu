@@ -52,7 +52,7 @@ int check_logits(int T, int V, long long row_stride, int dtype, float inv_temper
 int check_adamw(const qlora_adamw_desc* d, bool step) {
     if (d == nullptr || d->n_tensors < 0 || (d->n_tensors > 0 && d->tensors == nullptr)) return QLORA_ERR_INVALID_ARG;
     if (!(d->beta1 >= 0.0 && d->beta1 < 1.0 && d->beta2 >= 0.0 && d->beta2 < 1.0)) return QLORA_ERR_INVALID_ARG;
-    if (!(d->eps > 0.0 && d->eps < 1e30) || !((float)d->eps > 0.0f) || !(d->weight_decay >= 0.0 && d->weight_decay < 1e30)) return QLORA_ERR_INVALID_ARG;
+    if (!(d->eps >= 1e-30 && d->eps < 1e30) || !(d->weight_decay >= 0.0 && d->weight_decay < 1e30)) return QLORA_ERR_INVALID_ARG;
     if (d->grad_type != QLORA_FP32 && d->grad_type != QLORA_BF16 && d->grad_type != QLORA_FP16) return QLORA_ERR_UNSUPPORTED;
     if (d->param_type != QLORA_FP32 && d->param_type != QLORA_BF16 && d->param_type != QLORA_FP16) return QLORA_ERR_UNSUPPORTED;
     if (d->state_type != QLORA_FP32 && d->state_type != QLORA_E4M3) return QLORA_ERR_UNSUPPORTED;

@@ -6,6 +6,7 @@
 
 #include "common.cuh"
 #include "device_state.h"
+#include "f32x2.cuh"
 #include "launch.h"
 
 namespace qlora {
@@ -45,20 +46,20 @@ __device__ __forceinline__ int tensor_of_chunk(const OptTable<CAP>& tab, uint32_
 }
 
 // Two numbers in [0, 2^20) from an element's place in its tensor and the number of the step.
-__device__ __forceinline__ uint2 dither_of(uint32_t place, uint32_t step) {
-    uint32_t x = place * 0x9E3779B1u + step * 0x7F4A7C15u;
+// (x: place * 0x9E3779B1 + step * 0x7F4A7C15)
+__device__ __forceinline__ uint2 dither_of(uint32_t x) {
     x = (x ^ (x >> 15)) * 0x2C1B3C6Du;
     x = (x ^ (x >> 13)) * 0x297A2D39u;
     x ^= x >> 16;
     return make_uint2(x >> 12, (x * 0x9E3779B1u) >> 12);
 }
 
-// x (at most 448 in size) to an e4m3 value beside it: adding the dither below the third fraction bit and cutting there goes up with a
-// chance of the cut part's share of a step.  Below 2^-6 the steps stay 2^-9, those of the binade that x + 2^-6 lies in.
-__device__ __forceinline__ float dithered_e4m3(float x, uint32_t dither) {
-    const float a = fabsf(x), off = a < 0x1p-6f ? 0x1p-6f : 0.f;
-    const float y = __uint_as_float((__float_as_uint(a + off) + dither) & 0xFFF00000u) - off;
-    return copysignf(fminf(y, 448.f), x);
+// x (at most 448 in size, but for a rounding that the conversion to e4m3 cuts) to an e4m3 value beside it: adding the dither below the third
+// fraction bit and cutting there goes up with a chance of the cut part's share of a step.  Below 2^-6 the steps stay 2^-9, those of the binade that
+// x + 2^-6 lies in.
+__device__ __forceinline__ float dithered_size(float a, uint32_t dither) {            // a = |x|
+    const float off = a < 0x1p-6f ? 0x1p-6f : 0.f;
+    return __uint_as_float((__float_as_uint(a + off) + dither) & 0xFFF00000u) - off;
 }
 
 // Four consecutive elements (of 16-byte aligned tensors, at a multiple of 4).
@@ -103,13 +104,13 @@ __device__ __forceinline__ void put_one(__half* p, float v) { *p = __float2half_
 __device__ __forceinline__ void put_one(uint8_t* p, float v) { *p = __nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3); }
 
 // This lane's 8 of a block of 256 elements: 4 at 4 lane and 4 at 128 + 4 lane, so that every access of a warp is contiguous.  `left`: elements of
-// the block that are there (256 but for the last block of a tensor).
-template <typename E>
+// the block that are there; FULL: all 256 (all but the last block of a tensor).
+template <bool FULL, typename E>
 __device__ __forceinline__ void load8(const E* p, int lane, int left, float (&v)[8]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int at = 128 * h + 4 * lane;
-        if (at + 4 <= left) {
+        if (FULL || at + 4 <= left) {
             const float4 x = load4(p + at);
             v[4 * h] = x.x; v[4 * h + 1] = x.y; v[4 * h + 2] = x.z; v[4 * h + 3] = x.w;
         } else {
@@ -118,12 +119,12 @@ __device__ __forceinline__ void load8(const E* p, int lane, int left, float (&v)
         }
     }
 }
-template <typename E>
+template <bool FULL, typename E>
 __device__ __forceinline__ void store8(E* p, int lane, int left, const float (&v)[8]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int at = 128 * h + 4 * lane;
-        if (at + 4 <= left) store4(p + at, v + 4 * h);
+        if (FULL || at + 4 <= left) store4(p + at, v + 4 * h);
         else
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -137,21 +138,104 @@ __device__ __forceinline__ float fast_sqrt(float x) {                     // (of
     return r;
 }
 
-// 8-bit form of a block's values: the scale (for one lane to store) and the codes' values.
-template <bool ROOT>
-__device__ __forceinline__ float to_codes(float (&x)[8], const uint32_t (&dither)[8]) {
-    float top = 0.f;
+// The largest of a warp's values from 0 on (their bits are in order; a NaN is above all).
+__device__ __forceinline__ float warp_top(float lane_top) { return __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(lane_top))); }
+__device__ __forceinline__ void fold_top(float& top, f2 x) {
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(fabsf(lo_of(x))));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(fabsf(hi_of(x))));
+}
+__device__ __forceinline__ f2 both(float x) { return make_f2(x, x); }
+__device__ __forceinline__ float root_ftz(float x) {
+    float r;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float inverse_ftz(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// The step of a block with 8-bit states.  What 12 bytes an element leave at the copy rate is some 65 instructions an element on the SM, of which this takes about 45, so
+// arithmetic goes by pairs, one square root serves the update and the state, and nothing is done twice.
+struct AdamBlock {                                                   // what holds for the whole call
+    float f, keep, rate, root_inv2;
+    uint32_t step_term;
+};
+template <typename P, typename G, bool FULL>
+__device__ __forceinline__ void adamw8_block(const qlora_adamw_tensor& t, const AdamScalars& sc, const AdamBlock& k, long long base, int left, int lane) {
+    float g[8], w[8], mc[8], uc[8];
+    load8<FULL>(static_cast<const G*>(t.grad) + base, lane, left, g);
+    load8<FULL>(static_cast<const uint8_t*>(t.m) + base, lane, left, mc);
+    load8<FULL>(static_cast<const uint8_t*>(t.v) + base, lane, left, uc);
+    if (t.master != nullptr) load8<FULL>(t.master + base, lane, left, w);
+    else load8<FULL>(static_cast<const P*>(t.param) + base, lane, left, w);
+    const float ms = t.m_scale[base / OP_BLOCK], us = t.v_scale[base / OP_BLOCK];
+    const f2 m_by = both(sc.beta1 * ms), one_minus1 = both(sc.one_minus_beta1), u_by = both(us), beta2 = both(sc.beta2), one_minus2 = both(sc.one_minus_beta2);
+    f2 m[4], u[4];
+    float top_m = 0.f, top_u = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(fabsf(x[i])));
-    top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top)));   // (from 0 on the bits are in order; a NaN is above all and makes the scale one)
-    const bool held = !(top <= 0x1p-100f);
-    const float inv = held ? 448.f / top : 0.f;
+    for (int i = 0; i < 4; ++i) {
+        const f2 gi = mul2(make_f2(g[2 * i], g[2 * i + 1]), both(k.f));
+        m[i] = fma2(make_f2(mc[2 * i], mc[2 * i + 1]), m_by, mul2(gi, one_minus1));
+        const f2 old = mul2(make_f2(uc[2 * i], uc[2 * i + 1]), u_by);
+        const f2 v = fma2(mul2(old, old), beta2, mul2(mul2(gi, gi), one_minus2));
+        u[i] = make_f2(root_ftz(lo_of(v)), root_ftz(hi_of(v)));
+        const f2 den = fma2(u[i], both(k.root_inv2), both(sc.eps));
+        const f2 q = mul2(mul2(m[i], both(-k.rate)), make_f2(inverse_ftz(lo_of(den)), inverse_ftz(hi_of(den))));
+        const f2 wi = fma2(make_f2(w[2 * i], w[2 * i + 1]), both(k.keep), q);
+        w[2 * i] = lo_of(wi);
+        w[2 * i + 1] = hi_of(wi);
+        fold_top(top_m, m[i]);
+        fold_top(top_u, u[i]);
+    }
+    if (t.master != nullptr) store8<FULL>(t.master + base, lane, left, w);
+    store8<FULL>(static_cast<P*>(t.param) + base, lane, left, w);
+    top_m = warp_top(top_m);
+    top_u = warp_top(top_u);
+    const bool held_m = !(top_m <= 0x1p-100f), held_u = !(top_u <= 0x1p-100f);
+    const f2 inv_m = both(held_m ? 448.f / top_m : 0.f), inv_u = both(held_u ? 448.f / top_u : 0.f);
+    const uint32_t place = (uint32_t)base + 4u * lane;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const f2 y = mul2(m[i], inv_m), r = mul2(u[i], inv_u);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int e = 2 * i + h;
+            const uint2 d = dither_of((place + 128u * (e / 4) + e % 4) * 0x9E3779B1u + k.step_term);
+            const float ym = h ? hi_of(y) : lo_of(y), yu = h ? hi_of(r) : lo_of(r);
+            mc[e] = copysignf(dithered_size(fabsf(ym), d.x), ym);
+            const float cu = dithered_size(yu, d.y);
+            uc[e] = yu > 0.f ? fmaxf(cu, 0x1p-9f) : cu;
+        }
+    }
+    store8<FULL>(static_cast<uint8_t*>(t.m) + base, lane, left, mc);       // (elements that are not there are zeros: gradient, moments, codes)
+    store8<FULL>(static_cast<uint8_t*>(t.v) + base, lane, left, uc);
+    if (lane == 0) {
+        t.m_scale[base / OP_BLOCK] = held_m ? top_m * (1.f / 448.f) : 0.f;
+        t.v_scale[base / OP_BLOCK] = held_u ? top_u * (1.f / 448.f) : 0.f;
+    }
+}
+
+template <typename P, typename G, bool FULL>
+__device__ __forceinline__ void adamw32_block(const qlora_adamw_tensor& t, const AdamScalars& sc, const AdamBlock& k, long long base, int left, int lane) {
+    float g[8], w[8], m[8], v[8];
+    load8<FULL>(static_cast<const G*>(t.grad) + base, lane, left, g);
+    if (t.master != nullptr) load8<FULL>(t.master + base, lane, left, w);
+    else load8<FULL>(static_cast<const P*>(t.param) + base, lane, left, w);
+    load8<FULL>(static_cast<const float*>(t.m) + base, lane, left, m);
+    load8<FULL>(static_cast<const float*>(t.v) + base, lane, left, v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float y = x[i] * inv, c = dithered_e4m3(y, dither[i]);
-        x[i] = ROOT && y > 0.f ? fmaxf(c, 0x1p-9f) : c;
+        const float gi = k.f * g[i];
+        m[i] = fmaf(sc.beta1, m[i], sc.one_minus_beta1 * gi);
+        v[i] = fmaf(sc.beta2, v[i], sc.one_minus_beta2 * (gi * gi));
+        w[i] = fmaf(w[i], k.keep, -__fdividef(k.rate * m[i], fmaf(fast_sqrt(v[i]), k.root_inv2, sc.eps)));
     }
-    return held ? top * (1.f / 448.f) : 0.f;
+    if (t.master != nullptr) store8<FULL>(t.master + base, lane, left, w);
+    store8<FULL>(static_cast<P*>(t.param) + base, lane, left, w);
+    store8<FULL>(static_cast<float*>(t.m) + base, lane, left, m);
+    store8<FULL>(static_cast<float*>(t.v) + base, lane, left, v);
 }
 
 // One warp per block of 256 elements (8 per lane).
@@ -180,56 +264,15 @@ __global__ void __launch_bounds__(OP_THREADS) adamw_kernel(const __grid_constant
     }
     if (!(fabsf(f) < INFINITY)) return;
     const float keep = 1.f - lr * sc.weight_decay, rate = lr * inv1;
+    const AdamBlock k{f, keep, rate, sqrtf(inv2), (uint32_t)step * 0x7F4A7C15u};
     for (long long base = begin + warp * OP_BLOCK; base < end; base += OP_THREADS / 32 * OP_BLOCK) {
         const int left = (int)(end - base < OP_BLOCK ? end - base : OP_BLOCK);
-        float g[8], w[8], m[8], v[8];
-        load8(static_cast<const G*>(t.grad) + base, lane, left, g);
-        if (t.master != nullptr) load8(t.master + base, lane, left, w);
-        else load8(static_cast<const P*>(t.param) + base, lane, left, w);
-        float ms = 1.f, us = 1.f;
         if constexpr (EIGHT) {
-            load8(static_cast<const uint8_t*>(t.m) + base, lane, left, m);
-            load8(static_cast<const uint8_t*>(t.v) + base, lane, left, v);
-            ms = t.m_scale[base / OP_BLOCK];
-            us = t.v_scale[base / OP_BLOCK];
+            if (left == OP_BLOCK) adamw8_block<P, G, true>(t, sc, k, base, left, lane);
+            else adamw8_block<P, G, false>(t, sc, k, base, left, lane);
         } else {
-            load8(static_cast<const float*>(t.m) + base, lane, left, m);
-            load8(static_cast<const float*>(t.v) + base, lane, left, v);
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float gi = f * g[i];
-            if constexpr (EIGHT) {
-                m[i] *= ms;
-                v[i] *= us;
-                v[i] *= v[i];
-            }
-            m[i] = fmaf(sc.beta1, m[i], sc.one_minus_beta1 * gi);
-            v[i] = fmaf(sc.beta2, v[i], sc.one_minus_beta2 * (gi * gi));
-            w[i] = fmaf(w[i], keep, -__fdividef(rate * m[i], fast_sqrt(v[i] * inv2) + sc.eps));
-        }
-        if (t.master != nullptr) store8(t.master + base, lane, left, w);
-        store8(static_cast<P*>(t.param) + base, lane, left, w);
-        if constexpr (EIGHT) {
-            uint32_t dm[8], du[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint2 r = dither_of((uint32_t)(base + 128 * (i / 4) + 4 * lane + i % 4), (uint32_t)step);
-                dm[i] = r.x;
-                du[i] = r.y;
-                v[i] = fast_sqrt(v[i]);
-            }
-            ms = to_codes<false>(m, dm);                             // (elements that are not there are zeros: gradient, moments, codes)
-            us = to_codes<true>(v, du);
-            store8(static_cast<uint8_t*>(t.m) + base, lane, left, m);
-            store8(static_cast<uint8_t*>(t.v) + base, lane, left, v);
-            if (lane == 0) {
-                t.m_scale[base / OP_BLOCK] = ms;
-                t.v_scale[base / OP_BLOCK] = us;
-            }
-        } else {
-            store8(static_cast<float*>(t.m) + base, lane, left, m);
-            store8(static_cast<float*>(t.v) + base, lane, left, v);
+            if (left == OP_BLOCK) adamw32_block<P, G, true>(t, sc, k, base, left, lane);
+            else adamw32_block<P, G, false>(t, sc, k, base, left, lane);
         }
     }
 }
@@ -261,17 +304,22 @@ __global__ void __launch_bounds__(OP_THREADS) grad_square_kernel(const __grid_co
         const long long begin = (long long)(c - tab.first[j]) * tab.chunk;
         const long long end = begin + tab.chunk < t.n ? begin + tab.chunk : t.n;
         if (!waited) { pdl_wait(); waited = true; }
-        for (long long base = begin + warp * OP_BLOCK; base < end; base += 2 * (OP_THREADS / 32 * OP_BLOCK)) {
+        const G* grad = static_cast<const G*>(t.grad);
+        long long base = begin + warp * OP_BLOCK;
+        for (; base + (OP_THREADS / 32 + 1) * OP_BLOCK <= end; base += 2 * (OP_THREADS / 32 * OP_BLOCK)) {
             float g[2][8];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const long long at = base + u * (OP_THREADS / 32 * OP_BLOCK), left = end - at;
-                load8(static_cast<const G*>(t.grad) + at, lane, (int)(left < 0 ? 0 : left < OP_BLOCK ? left : OP_BLOCK), g[u]);
-            }
+            load8<true>(grad + base, lane, OP_BLOCK, g[0]);
+            load8<true>(grad + base + OP_THREADS / 32 * OP_BLOCK, lane, OP_BLOCK, g[1]);
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) acc = fma((double)g[u][i], (double)g[u][i], acc);
+        }
+        for (; base < end; base += OP_THREADS / 32 * OP_BLOCK) {
+            float g[8];
+            load8<false>(grad + base, lane, (int)(end - base < OP_BLOCK ? end - base : OP_BLOCK), g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc = fma((double)g[i], (double)g[i], acc);
         }
     }
     if (!waited) pdl_wait();
