@@ -17,18 +17,20 @@ constexpr int OP_TABLE = 448, OP_SMALL_TABLE = 16;   // tensors per launch: thei
 constexpr int OP_PARTIALS = QLORA_GRAD_NORM_WORKSPACE_BYTES / sizeof(double);
 
 // The tensors of one launch, cut into chunks of `chunk` elements (the last one of a tensor may be shorter): chunk c belongs to the tensor
-// j with first[j] <= c < first[j + 1].
+// j with first[j] <= c < first[j + 1], which is near[c >> near_log2] or one of the next.
 template <int CAP>
 struct OptTable {
     qlora_adamw_tensor t[CAP];
     uint32_t first[CAP + 1];
-    int n, chunk;
+    int n, chunk, near_log2;
+    uint16_t near[CAP];
 };
+static_assert(sizeof(OptTable<OP_TABLE>) <= 32000, "a kernel's parameters");
 
 struct AdamScalars {
     float beta1, one_minus_beta1, beta2, one_minus_beta2, eps, weight_decay;
     float log_beta1, log_beta2;          // for a step number that is in device memory
-    float lr, inv_corr1, inv_corr2;      // the rate, 1 / (1 - beta1^step), 1 / (1 - beta2^step)
+    float lr, inv_corr1, root_inv_corr2; // the rate, 1 / (1 - beta1^step), 1 / sqrt(1 - beta2^step)
     int step;
     const float* lr_dev;
     const int32_t* step_dev;
@@ -37,30 +39,31 @@ struct AdamScalars {
 
 template <int CAP>
 __device__ __forceinline__ int tensor_of_chunk(const OptTable<CAP>& tab, uint32_t c) {
-    int lo = 0, hi = tab.n;              // first[lo] <= c < first[hi]
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (tab.first[mid] <= c) lo = mid; else hi = mid;
-    }
-    return lo;
+    int j = tab.near[c >> tab.near_log2];
+    while (tab.first[j + 1] <= c) ++j;                               // (c is below first[n])
+    return j;
 }
 
-// Two numbers in [0, 2^20) from an element's place in its tensor and the number of the step.
-// (x: place * 0x9E3779B1 + step * 0x7F4A7C15)
+// Two numbers below 2^32 from an element's place in its tensor and the number of the step (x: place * 0x9E3779B1 + step * 0x7F4A7C15); the
+// dither of a code is the upper 20 bits.
 __device__ __forceinline__ uint2 dither_of(uint32_t x) {
     x = (x ^ (x >> 15)) * 0x2C1B3C6Du;
     x = (x ^ (x >> 13)) * 0x297A2D39u;
     x ^= x >> 16;
-    return make_uint2(x >> 12, (x * 0x9E3779B1u) >> 12);
+    return make_uint2(x, x * 0x9E3779B1u);
 }
 
-// x (at most 448 in size, but for a rounding that the conversion to e4m3 cuts) to an e4m3 value beside it: adding the dither below the third
-// fraction bit and cutting there goes up with a chance of the cut part's share of a step.  Below 2^-6 the steps stay 2^-9, those of the binade that
-// x + 2^-6 lies in.
-__device__ __forceinline__ float dithered_size(float a, uint32_t dither) {            // a = |x|
-    const float off = a < 0x1p-6f ? 0x1p-6f : 0.f;
-    return __uint_as_float((__float_as_uint(a + off) + dither) & 0xFFF00000u) - off;
+// The e4m3 code beside y 2^120, y >= 0, in the top byte of the result: times 2^-120 the values that e4m3 holds, its smallest ones with fewer than three
+// fraction bits among them, are fp32's own with the same exponents and fractions, 20 bits further up.  Adding the dither below the code and cutting
+// there goes up with a chance of the cut part's share of a step.  (y's sign and the dither's lower bits fall out at the ends.)
+__device__ __forceinline__ uint32_t dithered_code(uint32_t y, uint32_t dither) { return y * 16u + (dither >> 8); }
+// Bytes 3 of four words.
+__device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
 }
+
+// Four codes without a sign: 0x7F to 0x7E, the code of 448 (the rounding of 448 / top can put the top one just above).
+__device__ __forceinline__ uint32_t at_most_448(uint32_t codes) { return codes - (((codes + 0x01010101u) >> 7) & 0x01010101u); }
 
 // Four consecutive elements (of 16-byte aligned tensors, at a multiple of 4).
 __device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
@@ -89,11 +92,6 @@ __device__ __forceinline__ void store4(__half* p, const float* v) {
     const __half2 a = __floats2half2_rn(v[0], v[1]), b = __floats2half2_rn(v[2], v[3]);
     *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
-__device__ __forceinline__ void store4(uint8_t* p, const float* v) {     // values that e4m3 holds
-    const uint32_t a = __nv_cvt_float2_to_fp8x2(make_float2(v[0], v[1]), __NV_SATFINITE, __NV_E4M3);
-    const uint32_t b = __nv_cvt_float2_to_fp8x2(make_float2(v[2], v[3]), __NV_SATFINITE, __NV_E4M3);
-    *reinterpret_cast<uint32_t*>(p) = a | b << 16;
-}
 __device__ __forceinline__ float one(const float* p) { return *p; }
 __device__ __forceinline__ float one(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ float one(const __half* p) { return __half2float(*p); }
@@ -101,7 +99,6 @@ __device__ __forceinline__ float one(const uint8_t* p) { return __half2float(__h
 __device__ __forceinline__ void put_one(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put_one(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void put_one(__half* p, float v) { *p = __float2half_rn(v); }
-__device__ __forceinline__ void put_one(uint8_t* p, float v) { *p = __nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3); }
 
 // This lane's 8 of a block of 256 elements: 4 at 4 lane and 4 at 128 + 4 lane, so that every access of a warp is contiguous.  `left`: elements of
 // the block that are there; FULL: all 256 (all but the last block of a tensor).
@@ -194,23 +191,37 @@ __device__ __forceinline__ void adamw8_block(const qlora_adamw_tensor& t, const 
     top_m = warp_top(top_m);
     top_u = warp_top(top_u);
     const bool held_m = !(top_m <= 0x1p-100f), held_u = !(top_u <= 0x1p-100f);
-    const f2 inv_m = both(held_m ? 448.f / top_m : 0.f), inv_u = both(held_u ? 448.f / top_u : 0.f);
-    const uint32_t place = (uint32_t)base + 4u * lane;
+    const f2 inv_m = both(held_m ? 448.f * inverse_ftz(top_m) : 0.f), inv_u = both(held_u ? 448.f * inverse_ftz(top_u) : 0.f), down = both(0x1p-120f);
+    const uint32_t place = ((uint32_t)base + 4u * lane) * 0x9E3779B1u + k.step_term;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const f2 y = mul2(m[i], inv_m), r = mul2(u[i], inv_u);
+    for (int q = 0; q < 2; ++q) {                                    // four consecutive elements
+        uint32_t cm[4], cu[4], sign[4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int e = 2 * i + h;
-            const uint2 d = dither_of((place + 128u * (e / 4) + e % 4) * 0x9E3779B1u + k.step_term);
-            const float ym = h ? hi_of(y) : lo_of(y), yu = h ? hi_of(r) : lo_of(r);
-            mc[e] = copysignf(dithered_size(fabsf(ym), d.x), ym);
-            const float cu = dithered_size(yu, d.y);
-            uc[e] = yu > 0.f ? fmaxf(cu, 0x1p-9f) : cu;
+        for (int e = 0; e < 4; ++e) {
+            const int i = 2 * q + e / 2;
+            const f2 y = mul2(mul2(m[i], inv_m), down), r = mul2(mul2(u[i], inv_u), down);
+            const uint2 d = dither_of(place + (128u * q + e) * 0x9E3779B1u);
+            sign[e] = __float_as_uint(e & 1 ? hi_of(y) : lo_of(y));
+            cm[e] = dithered_code(sign[e], d.x);
+            // (a root above zero has a code above zero: its bits are far above 2^20, those of zero are not)
+            const uint32_t least = min(__float_as_uint(e & 1 ? hi_of(u[i]) : lo_of(u[i])), 1u << 24);
+            cu[e] = max(dithered_code(__float_as_uint(e & 1 ? hi_of(r) : lo_of(r)), d.y), least);
+        }
+        const uint32_t codes_m = at_most_448(top_bytes(cm[0], cm[1], cm[2], cm[3]) & 0x7F7F7F7Fu) | (top_bytes(sign[0], sign[1], sign[2], sign[3]) & 0x80808080u);
+        const uint32_t codes_u = at_most_448(top_bytes(cu[0], cu[1], cu[2], cu[3]));
+        const int at = 128 * q + 4 * lane;
+        uint8_t *pm = static_cast<uint8_t*>(t.m) + base + at, *pu = static_cast<uint8_t*>(t.v) + base + at;
+        if (FULL || at + 4 <= left) {
+            *reinterpret_cast<uint32_t*>(pm) = codes_m;
+            *reinterpret_cast<uint32_t*>(pu) = codes_u;
+        } else {
+            for (int e = 0; e < 4; ++e)
+                if (at + e < left) {
+                    pm[e] = (uint8_t)(codes_m >> (8 * e));
+                    pu[e] = (uint8_t)(codes_u >> (8 * e));
+                }
         }
     }
-    store8<FULL>(static_cast<uint8_t*>(t.m) + base, lane, left, mc);       // (elements that are not there are zeros: gradient, moments, codes)
-    store8<FULL>(static_cast<uint8_t*>(t.v) + base, lane, left, uc);
     if (lane == 0) {
         t.m_scale[base / OP_BLOCK] = held_m ? top_m * (1.f / 448.f) : 0.f;
         t.v_scale[base / OP_BLOCK] = held_u ? top_u * (1.f / 448.f) : 0.f;
@@ -252,19 +263,19 @@ __global__ void __launch_bounds__(OP_THREADS) adamw_kernel(const __grid_constant
     const float f = sc.norm != nullptr ? sc.norm[1] : 1.f;
     const float lr = sc.lr_dev != nullptr ? *sc.lr_dev : sc.lr;
     const int step = sc.step_dev != nullptr ? *sc.step_dev : sc.step;
-    float inv1 = sc.inv_corr1, inv2 = sc.inv_corr2;
+    float inv1 = sc.inv_corr1, root_inv2 = sc.root_inv_corr2;
     if (sc.step_dev != nullptr) {
         if (threadIdx.x == 0) {
             corr[0] = 1.f / -expm1f((float)step * sc.log_beta1);
-            corr[1] = 1.f / -expm1f((float)step * sc.log_beta2);
+            corr[1] = rsqrtf(-expm1f((float)step * sc.log_beta2));
         }
         __syncthreads();
         inv1 = corr[0];
-        inv2 = corr[1];
+        root_inv2 = corr[1];
     }
     if (!(fabsf(f) < INFINITY)) return;
     const float keep = 1.f - lr * sc.weight_decay, rate = lr * inv1;
-    const AdamBlock k{f, keep, rate, sqrtf(inv2), (uint32_t)step * 0x7F4A7C15u};
+    const AdamBlock k{f, keep, rate, root_inv2, (uint32_t)step * 0x7F4A7C15u};
     for (long long base = begin + warp * OP_BLOCK; base < end; base += OP_THREADS / 32 * OP_BLOCK) {
         const int left = (int)(end - base < OP_BLOCK ? end - base : OP_BLOCK);
         if constexpr (EIGHT) {
@@ -361,6 +372,13 @@ static uint32_t fill_table(const qlora_adamw_desc& d, int* at, int chunk, OptTab
         ++*at;
     }
     tab.first[tab.n] = chunks;
+    tab.near_log2 = 0;
+    while (chunks > 0 && ((chunks - 1) >> tab.near_log2) >= (uint32_t)CAP) ++tab.near_log2;
+    int j = 0;
+    for (uint32_t i = 0; chunks > 0 && i <= (chunks - 1) >> tab.near_log2; ++i) {
+        while (tab.first[j + 1] <= i << tab.near_log2) ++j;
+        tab.near[i] = (uint16_t)j;
+    }
     return chunks;
 }
 
@@ -430,7 +448,7 @@ int launch_adamw(const qlora_adamw_desc& d, double lr, int step, const float* lr
     sc.eps = (float)d.eps; sc.weight_decay = (float)d.weight_decay;
     sc.log_beta1 = (float)log(d.beta1); sc.log_beta2 = (float)log(d.beta2);
     sc.lr = (float)lr;
-    sc.inv_corr1 = (float)(-1.0 / expm1(step * log(d.beta1))); sc.inv_corr2 = (float)(-1.0 / expm1(step * log(d.beta2)));
+    sc.inv_corr1 = (float)(-1.0 / expm1(step * log(d.beta1))); sc.root_inv_corr2 = (float)(1.0 / sqrt(-expm1(step * log(d.beta2))));
     sc.step = step; sc.lr_dev = lr_dev; sc.step_dev = step_dev; sc.norm = norm;
     return d.n_tensors <= OP_SMALL_TABLE ? launch_adamw_with<OP_SMALL_TABLE>(d, sc, st) : launch_adamw_with<OP_TABLE>(d, sc, st);
 }
