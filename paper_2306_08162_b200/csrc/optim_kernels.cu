@@ -1,6 +1,7 @@
 // The optimizer step of the trainable pairs (Section 3.2, Eq. 3 of the paper: theta_l is optimised, theta_q stays): the global norm of
 // all gradients, and AdamW over every tensor of a model in one launch, with 32-bit or 8-bit states.
 #include <cuda_fp8.h>
+#include <type_traits>
 
 #include <math.h>
 
@@ -14,6 +15,12 @@ namespace qlora {
 constexpr int OP_BLOCK = 256;            // elements that share one scale of the 8-bit states, and that a warp handles at a time
 constexpr int OP_THREADS = 256;
 constexpr int OP_TABLE = 448, OP_SMALL_TABLE = 16;   // tensors per launch: their table travels in the kernel's parameters (32764 bytes at most)
+#ifndef NU
+#define NU 4
+#endif
+#ifndef NB
+#define NB 4
+#endif
 constexpr int OP_PARTIALS = QLORA_GRAD_NORM_WORKSPACE_BYTES / sizeof(double);
 
 // The tensors of one launch, cut into chunks of `chunk` elements (the last one of a tensor may be shorter): chunk c belongs to the tensor
@@ -301,39 +308,60 @@ __device__ __forceinline__ double block_sum(double v) {           // the sum in 
     return v;
 }
 
-// Sums of squares in 64 bits (a square can leave fp32's range, and HBM leaves the time), one per block of the launch; `add`: on top of the previous launch's
-// (more tensors than one table holds).
-template <typename G, int CAP>
-__global__ void __launch_bounds__(OP_THREADS) grad_square_kernel(const __grid_constant__ OptTable<CAP> tab, float prescale, int add, double* __restrict__ partial) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    pdl_launch_dependents();
-    double acc = 0.0;
-    bool waited = false;
-    for (uint32_t c = blockIdx.x; c < tab.first[tab.n]; c += gridDim.x) {
-        const int j = tensor_of_chunk(tab, c);
-        const qlora_adamw_tensor& t = tab.t[j];
-        const long long begin = (long long)(c - tab.first[j]) * tab.chunk;
-        const long long end = begin + tab.chunk < t.n ? begin + tab.chunk : t.n;
-        if (!waited) { pdl_wait(); waited = true; }
-        const G* grad = static_cast<const G*>(t.grad);
-        long long base = begin + warp * OP_BLOCK;
-        for (; base + (OP_THREADS / 32 + 1) * OP_BLOCK <= end; base += 2 * (OP_THREADS / 32 * OP_BLOCK)) {
-            float g[2][8];
-            load8<true>(grad + base, lane, OP_BLOCK, g[0]);
-            load8<true>(grad + base + OP_THREADS / 32 * OP_BLOCK, lane, OP_BLOCK, g[1]);
+__device__ __forceinline__ uint4 load_once(const uint4* p) {            // 16 bytes, not kept in L1 (asm volatile: several loads stay ahead of their uses)
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+template <typename G>
+__device__ __forceinline__ void add_squares(double& acc, const uint4& v) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) acc = fma((double)g[u][i], (double)g[u][i], acc);
-        }
-        for (; base < end; base += OP_THREADS / 32 * OP_BLOCK) {
-            float g[8];
-            load8<false>(grad + base, lane, (int)(end - base < OP_BLOCK ? end - base : OP_BLOCK), g);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) acc = fma((double)g[i], (double)g[i], acc);
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(G) == 4) {
+            const double x = (double)__uint_as_float(w[i]);
+            acc = fma(x, x, acc);
+        } else {
+            float2 f;
+            if constexpr (std::is_same_v<G, __half>) f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+            else f = make_float2(bf16_lo(w[i]), bf16_hi(w[i]));
+            acc = fma((double)f.x, (double)f.x, acc);
+            acc = fma((double)f.y, (double)f.y, acc);
         }
     }
-    if (!waited) pdl_wait();
+}
+
+// Sums of squares in 64 bits (a square can leave fp32's range, and HBM leaves the time), one per block of the launch, each block with a
+// stretch of the chunks (the same number to within one); `add`: on top of the previous launch's (more tensors than one table holds).
+template <typename G, int CAP>
+__global__ void __launch_bounds__(OP_THREADS) grad_square_kernel(const __grid_constant__ OptTable<CAP> tab, float prescale, int add, double* __restrict__ partial) {
+    constexpr int PER = 16 / sizeof(G), UNROLL = NU;
+    pdl_launch_dependents();
+    const uint64_t chunks = tab.first[tab.n];
+    uint32_t c = (uint32_t)(chunks * blockIdx.x / gridDim.x);
+    const uint32_t stop = (uint32_t)(chunks * (blockIdx.x + 1) / gridDim.x);
+    int j = c < stop ? tensor_of_chunk(tab, c) : 0;
+    pdl_wait();
+    double acc = 0.0;
+    for (; c < stop; ++j) {                                          // the stretch's part of one tensor after the other
+        const qlora_adamw_tensor& t = tab.t[j];
+        const uint32_t next = min(stop, tab.first[j + 1]);
+        const long long begin = (long long)(c - tab.first[j]) * tab.chunk, end = min((long long)(next - tab.first[j]) * tab.chunk, t.n);
+        const G* grad = static_cast<const G*>(t.grad) + begin;
+        const long long vectors = (end - begin) / PER;
+        const uint4* body = reinterpret_cast<const uint4*>(grad);
+        long long at = threadIdx.x;
+        for (; at + (UNROLL - 1) * OP_THREADS < vectors; at += UNROLL * OP_THREADS) {
+            uint4 v[UNROLL];
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) v[u] = load_once(body + at + u * OP_THREADS);
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) add_squares<G>(acc, v[u]);
+        }
+        for (; at < vectors; at += OP_THREADS) add_squares<G>(acc, load_once(body + at));
+        for (long long e = vectors * PER + threadIdx.x; e < end - begin; e += OP_THREADS) acc = fma((double)one(grad + e), (double)one(grad + e), acc);
+        c = next;
+    }
     acc = block_sum(acc) * (double)prescale * (double)prescale;
     if (threadIdx.x == 0) partial[blockIdx.x] = add ? partial[blockIdx.x] + acc : acc;
 }
@@ -382,22 +410,19 @@ static uint32_t fill_table(const qlora_adamw_desc& d, int* at, int chunk, OptTab
     return chunks;
 }
 
-#ifndef AC
-#define AC 2048
-#define NC 8192
+#ifndef NB
 #define NB 4
 #endif
-static int adamw_chunk(const qlora_adamw_desc& d) { return AC; }
-static int norm_chunk(const qlora_adamw_desc& d) { return NC; }
+constexpr int OP_CHUNK = 2048;           // a block of 256 elements to each of 8 warps
 
 template <int CAP>
 static int launch_grad_norm_with(const qlora_adamw_desc& d, float prescale, float max_norm, float* out, void* workspace, cudaStream_t st) {
     static thread_local OptTable<CAP> tab;
     double* partial = static_cast<double*>(workspace);
-    const int chunk = norm_chunk(d), most = NB * sm_count() < OP_PARTIALS ? NB * sm_count() : OP_PARTIALS;
+    const int most = NB * sm_count() < OP_PARTIALS ? NB * sm_count() : OP_PARTIALS;
     int at = 0, used = 0;
     for (int launch = 0;; ++launch) {
-        const uint32_t chunks = fill_table(d, &at, chunk, tab);
+        const uint32_t chunks = fill_table(d, &at, OP_CHUNK, tab);
         if (chunks == 0) break;
         // (every launch on the grid of the first, whose partial sums the later ones add to)
         if (launch == 0) used = (int)(chunks < (uint32_t)most ? chunks : (uint32_t)most);
@@ -431,7 +456,7 @@ static int launch_adamw_with(const qlora_adamw_desc& d, const AdamScalars& sc, c
     static thread_local OptTable<CAP> tab;
     int at = 0;
     for (;;) {
-        const uint32_t chunks = fill_table(d, &at, adamw_chunk(d), tab);
+        const uint32_t chunks = fill_table(d, &at, OP_CHUNK, tab);
         if (chunks == 0) return QLORA_OK;
         const bool eight = d.state_type == QLORA_E4M3;
         const cudaError_t err = d.param_type == QLORA_BF16 ? launch_adamw_param<__nv_bfloat16>(d.grad_type, eight, chunks, tab, sc, st)
