@@ -14,6 +14,7 @@ namespace qlora {
 
 constexpr int OP_BLOCK = 256;            // elements that share one scale of the 8-bit states, and that a warp handles at a time
 constexpr int OP_THREADS = 256;
+constexpr int OP_CHUNK = 2048;           // elements of a chunk: a block of 256 to each of 8 warps
 constexpr int OP_TABLE = 448, OP_SMALL_TABLE = 16;   // tensors per launch: their table travels in the kernel's parameters (32764 bytes at most)
 #ifndef NU
 #define NU 4
@@ -23,13 +24,13 @@ constexpr int OP_TABLE = 448, OP_SMALL_TABLE = 16;   // tensors per launch: thei
 #endif
 constexpr int OP_PARTIALS = QLORA_GRAD_NORM_WORKSPACE_BYTES / sizeof(double);
 
-// The tensors of one launch, cut into chunks of `chunk` elements (the last one of a tensor may be shorter): chunk c belongs to the tensor
+// The tensors of one launch, cut into chunks of OP_CHUNK elements (the last one of a tensor may be shorter): chunk c belongs to the tensor
 // j with first[j] <= c < first[j + 1], which is near[c >> near_log2] or one of the next.
 template <int CAP>
 struct OptTable {
     qlora_adamw_tensor t[CAP];
     uint32_t first[CAP + 1];
-    int n, chunk, near_log2;
+    int n, near_log2;
     uint16_t near[CAP];
 };
 static_assert(sizeof(OptTable<OP_TABLE>) <= 32000, "a kernel's parameters");
@@ -110,29 +111,29 @@ __device__ __forceinline__ void put_one(__half* p, float v) { *p = __float2half_
 // This lane's 8 of a block of 256 elements: 4 at 4 lane and 4 at 128 + 4 lane, so that every access of a warp is contiguous.  `left`: elements of
 // the block that are there; FULL: all 256 (all but the last block of a tensor).
 template <bool FULL, typename E>
-__device__ __forceinline__ void load8(const E* p, int lane, int left, float (&v)[8]) {
+__device__ __forceinline__ void load8(const E* p, uint32_t base, uint32_t lane, int left, float (&v)[8]) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int at = 128 * h + 4 * lane;
-        if (FULL || at + 4 <= left) {
+    for (uint32_t h = 0; h < 2; ++h) {
+        const uint32_t in = 128 * h + 4 * lane, at = base + in;
+        if (FULL || (int)in + 4 <= left) {
             const float4 x = load4(p + at);
             v[4 * h] = x.x; v[4 * h + 1] = x.y; v[4 * h + 2] = x.z; v[4 * h + 3] = x.w;
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[4 * h + i] = at + i < left ? one(p + at + i) : 0.f;
+            for (int i = 0; i < 4; ++i) v[4 * h + i] = (int)in + i < left ? one(p + at + i) : 0.f;
         }
     }
 }
 template <bool FULL, typename E>
-__device__ __forceinline__ void store8(E* p, int lane, int left, const float (&v)[8]) {
+__device__ __forceinline__ void store8(E* p, uint32_t base, uint32_t lane, int left, const float (&v)[8]) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int at = 128 * h + 4 * lane;
-        if (FULL || at + 4 <= left) store4(p + at, v + 4 * h);
+    for (uint32_t h = 0; h < 2; ++h) {
+        const uint32_t in = 128 * h + 4 * lane, at = base + in;
+        if (FULL || (int)in + 4 <= left) store4(p + at, v + 4 * h);
         else
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (at + i < left) put_one(p + at + i, v[4 * h + i]);
+                if ((int)in + i < left) put_one(p + at + i, v[4 * h + i]);
     }
 }
 
@@ -166,14 +167,28 @@ struct AdamBlock {                                                   // what hol
     float f, keep, rate, root_inv2;
     uint32_t step_term;
 };
+// The tensors from the chunk's first element on.  (The same for the whole block; a thread adds 32 bits to them.)
+template <typename P, typename G, typename S>
+struct Chunk {
+    P* param;
+    float* master;
+    const G* grad;
+    S *m, *v;
+    float *m_scale, *v_scale;
+    uint32_t place;                                                  // of its first element in the tensor
+    __device__ __forceinline__ Chunk(const qlora_adamw_tensor& t, long long begin)
+        : param(static_cast<P*>(t.param) + begin), master(t.master != nullptr ? t.master + begin : nullptr), grad(static_cast<const G*>(t.grad) + begin),
+          m(static_cast<S*>(t.m) + begin), v(static_cast<S*>(t.v) + begin), m_scale(t.m_scale + begin / OP_BLOCK), v_scale(t.v_scale + begin / OP_BLOCK), place((uint32_t)begin) {}
+};
+
 template <typename P, typename G, bool FULL>
-__device__ __forceinline__ void adamw8_block(const qlora_adamw_tensor& t, const AdamScalars& sc, const AdamBlock& k, long long base, int left, int lane) {
+__device__ __forceinline__ void adamw8_block(const Chunk<P, G, uint8_t>& t, const AdamScalars& sc, const AdamBlock& k, uint32_t base, int left, uint32_t lane) {
     float g[8], w[8], mc[8], uc[8];
-    load8<FULL>(static_cast<const G*>(t.grad) + base, lane, left, g);
-    load8<FULL>(static_cast<const uint8_t*>(t.m) + base, lane, left, mc);
-    load8<FULL>(static_cast<const uint8_t*>(t.v) + base, lane, left, uc);
-    if (t.master != nullptr) load8<FULL>(t.master + base, lane, left, w);
-    else load8<FULL>(static_cast<const P*>(t.param) + base, lane, left, w);
+    load8<FULL>(t.grad, base, lane, left, g);
+    load8<FULL>(t.m, base, lane, left, mc);
+    load8<FULL>(t.v, base, lane, left, uc);
+    if (t.master != nullptr) load8<FULL>(t.master, base, lane, left, w);
+    else load8<FULL>(t.param, base, lane, left, w);
     const float ms = t.m_scale[base / OP_BLOCK], us = t.v_scale[base / OP_BLOCK];
     const f2 m_by = both(sc.beta1 * ms), one_minus1 = both(sc.one_minus_beta1), u_by = both(us), beta2 = both(sc.beta2), one_minus2 = both(sc.one_minus_beta2);
     f2 m[4], u[4];
@@ -193,13 +208,13 @@ __device__ __forceinline__ void adamw8_block(const qlora_adamw_tensor& t, const 
         fold_top(top_m, m[i]);
         fold_top(top_u, u[i]);
     }
-    if (t.master != nullptr) store8<FULL>(t.master + base, lane, left, w);
-    store8<FULL>(static_cast<P*>(t.param) + base, lane, left, w);
+    if (t.master != nullptr) store8<FULL>(t.master, base, lane, left, w);
+    store8<FULL>(t.param, base, lane, left, w);
     top_m = warp_top(top_m);
     top_u = warp_top(top_u);
     const bool held_m = !(top_m <= 0x1p-100f), held_u = !(top_u <= 0x1p-100f);
     const f2 inv_m = both(held_m ? 448.f * inverse_ftz(top_m) : 0.f), inv_u = both(held_u ? 448.f * inverse_ftz(top_u) : 0.f), down = both(0x1p-120f);
-    const uint32_t place = ((uint32_t)base + 4u * lane) * 0x9E3779B1u + k.step_term;
+    const uint32_t place = (t.place + base + 4u * lane) * 0x9E3779B1u + k.step_term;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {                                    // four consecutive elements
         uint32_t cm[4], cu[4], sign[4];
@@ -216,16 +231,15 @@ __device__ __forceinline__ void adamw8_block(const qlora_adamw_tensor& t, const 
         }
         const uint32_t codes_m = at_most_448(top_bytes(cm[0], cm[1], cm[2], cm[3]) & 0x7F7F7F7Fu) | (top_bytes(sign[0], sign[1], sign[2], sign[3]) & 0x80808080u);
         const uint32_t codes_u = at_most_448(top_bytes(cu[0], cu[1], cu[2], cu[3]));
-        const int at = 128 * q + 4 * lane;
-        uint8_t *pm = static_cast<uint8_t*>(t.m) + base + at, *pu = static_cast<uint8_t*>(t.v) + base + at;
-        if (FULL || at + 4 <= left) {
-            *reinterpret_cast<uint32_t*>(pm) = codes_m;
-            *reinterpret_cast<uint32_t*>(pu) = codes_u;
+        const uint32_t in = 128 * q + 4 * lane, at = base + in;
+        if (FULL || (int)in + 4 <= left) {
+            *reinterpret_cast<uint32_t*>(t.m + at) = codes_m;
+            *reinterpret_cast<uint32_t*>(t.v + at) = codes_u;
         } else {
             for (int e = 0; e < 4; ++e)
-                if (at + e < left) {
-                    pm[e] = (uint8_t)(codes_m >> (8 * e));
-                    pu[e] = (uint8_t)(codes_u >> (8 * e));
+                if ((int)in + e < left) {
+                    t.m[at + e] = (uint8_t)(codes_m >> (8 * e));
+                    t.v[at + e] = (uint8_t)(codes_u >> (8 * e));
                 }
         }
     }
@@ -236,13 +250,13 @@ __device__ __forceinline__ void adamw8_block(const qlora_adamw_tensor& t, const 
 }
 
 template <typename P, typename G, bool FULL>
-__device__ __forceinline__ void adamw32_block(const qlora_adamw_tensor& t, const AdamScalars& sc, const AdamBlock& k, long long base, int left, int lane) {
+__device__ __forceinline__ void adamw32_block(const Chunk<P, G, float>& t, const AdamScalars& sc, const AdamBlock& k, uint32_t base, int left, uint32_t lane) {
     float g[8], w[8], m[8], v[8];
-    load8<FULL>(static_cast<const G*>(t.grad) + base, lane, left, g);
-    if (t.master != nullptr) load8<FULL>(t.master + base, lane, left, w);
-    else load8<FULL>(static_cast<const P*>(t.param) + base, lane, left, w);
-    load8<FULL>(static_cast<const float*>(t.m) + base, lane, left, m);
-    load8<FULL>(static_cast<const float*>(t.v) + base, lane, left, v);
+    load8<FULL>(t.grad, base, lane, left, g);
+    if (t.master != nullptr) load8<FULL>(t.master, base, lane, left, w);
+    else load8<FULL>(t.param, base, lane, left, w);
+    load8<FULL>(t.m, base, lane, left, m);
+    load8<FULL>(t.v, base, lane, left, v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float gi = k.f * g[i];
@@ -250,22 +264,22 @@ __device__ __forceinline__ void adamw32_block(const qlora_adamw_tensor& t, const
         v[i] = fmaf(sc.beta2, v[i], sc.one_minus_beta2 * (gi * gi));
         w[i] = fmaf(w[i], k.keep, -__fdividef(k.rate * m[i], fmaf(fast_sqrt(v[i]), k.root_inv2, sc.eps)));
     }
-    if (t.master != nullptr) store8<FULL>(t.master + base, lane, left, w);
-    store8<FULL>(static_cast<P*>(t.param) + base, lane, left, w);
-    store8<FULL>(static_cast<float*>(t.m) + base, lane, left, m);
-    store8<FULL>(static_cast<float*>(t.v) + base, lane, left, v);
+    if (t.master != nullptr) store8<FULL>(t.master, base, lane, left, w);
+    store8<FULL>(t.param, base, lane, left, w);
+    store8<FULL>(t.m, base, lane, left, m);
+    store8<FULL>(t.v, base, lane, left, v);
 }
 
-// One warp per block of 256 elements (8 per lane).
+// A chunk to a block of threads, 256 elements to a warp (8 per lane).
 template <typename P, typename G, bool EIGHT, int CAP>
-__global__ void __launch_bounds__(OP_THREADS) adamw_kernel(const __grid_constant__ OptTable<CAP> tab, const __grid_constant__ AdamScalars sc) {
+__global__ void __launch_bounds__(OP_THREADS, 4) adamw_kernel(const __grid_constant__ OptTable<CAP> tab, const __grid_constant__ AdamScalars sc) {
     __shared__ float corr[2];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_launch_dependents();
     const int j = tensor_of_chunk(tab, blockIdx.x);
-    const qlora_adamw_tensor& t = tab.t[j];
-    const long long begin = (long long)(blockIdx.x - tab.first[j]) * tab.chunk;
-    const long long end = begin + tab.chunk < t.n ? begin + tab.chunk : t.n;
+    const long long begin = (long long)(blockIdx.x - tab.first[j]) * OP_CHUNK;
+    const Chunk<P, G, std::conditional_t<EIGHT, uint8_t, float>> t(tab.t[j], begin);
+    const int n = (int)min((long long)OP_CHUNK, tab.t[j].n - begin);
     pdl_wait();
     const float f = sc.norm != nullptr ? sc.norm[1] : 1.f;
     const float lr = sc.lr_dev != nullptr ? *sc.lr_dev : sc.lr;
@@ -283,15 +297,14 @@ __global__ void __launch_bounds__(OP_THREADS) adamw_kernel(const __grid_constant
     if (!(fabsf(f) < INFINITY)) return;
     const float keep = 1.f - lr * sc.weight_decay, rate = lr * inv1;
     const AdamBlock k{f, keep, rate, root_inv2, (uint32_t)step * 0x7F4A7C15u};
-    for (long long base = begin + warp * OP_BLOCK; base < end; base += OP_THREADS / 32 * OP_BLOCK) {
-        const int left = (int)(end - base < OP_BLOCK ? end - base : OP_BLOCK);
-        if constexpr (EIGHT) {
-            if (left == OP_BLOCK) adamw8_block<P, G, true>(t, sc, k, base, left, lane);
-            else adamw8_block<P, G, false>(t, sc, k, base, left, lane);
-        } else {
-            if (left == OP_BLOCK) adamw32_block<P, G, true>(t, sc, k, base, left, lane);
-            else adamw32_block<P, G, false>(t, sc, k, base, left, lane);
-        }
+    const uint32_t base = warp * OP_BLOCK;
+    const int left = min(n - (int)base, OP_BLOCK);
+    if constexpr (EIGHT) {
+        if (n == OP_CHUNK) adamw8_block<P, G, true>(t, sc, k, base, left, lane);
+        else if (left > 0) adamw8_block<P, G, false>(t, sc, k, base, left, lane);
+    } else {
+        if (n == OP_CHUNK) adamw32_block<P, G, true>(t, sc, k, base, left, lane);
+        else if (left > 0) adamw32_block<P, G, false>(t, sc, k, base, left, lane);
     }
 }
 
@@ -346,7 +359,7 @@ __global__ void __launch_bounds__(OP_THREADS) grad_square_kernel(const __grid_co
     for (; c < stop; ++j) {                                          // the stretch's part of one tensor after the other
         const qlora_adamw_tensor& t = tab.t[j];
         const uint32_t next = min(stop, tab.first[j + 1]);
-        const long long begin = (long long)(c - tab.first[j]) * tab.chunk, end = min((long long)(next - tab.first[j]) * tab.chunk, t.n);
+        const long long begin = (long long)(c - tab.first[j]) * OP_CHUNK, end = min((long long)(next - tab.first[j]) * OP_CHUNK, t.n);
         const G* grad = static_cast<const G*>(t.grad) + begin;
         const long long vectors = (end - begin) / PER;
         const uint4* body = reinterpret_cast<const uint4*>(grad);
@@ -384,13 +397,12 @@ __global__ void __launch_bounds__(OP_THREADS) grad_norm_kernel(int n, const doub
 
 // Fills the table with tensors from *at on; returns the number of chunks (0: nothing left).
 template <int CAP>
-static uint32_t fill_table(const qlora_adamw_desc& d, int* at, int chunk, OptTable<CAP>& tab) {
+static uint32_t fill_table(const qlora_adamw_desc& d, int* at, OptTable<CAP>& tab) {
     uint32_t chunks = 0;
     tab.n = 0;
-    tab.chunk = chunk;
     while (*at < d.n_tensors && tab.n < CAP) {
         const qlora_adamw_tensor& t = d.tensors[*at];
-        const uint32_t c = (uint32_t)((t.n + chunk - 1) / chunk);
+        const uint32_t c = (uint32_t)((t.n + OP_CHUNK - 1) / OP_CHUNK);
         if (chunks > 0 && chunks + c > 0x7FFFFFFFu) break;
         if (c > 0) {
             tab.t[tab.n] = t;
@@ -413,7 +425,6 @@ static uint32_t fill_table(const qlora_adamw_desc& d, int* at, int chunk, OptTab
 #ifndef NB
 #define NB 4
 #endif
-constexpr int OP_CHUNK = 2048;           // a block of 256 elements to each of 8 warps
 
 template <int CAP>
 static int launch_grad_norm_with(const qlora_adamw_desc& d, float prescale, float max_norm, float* out, void* workspace, cudaStream_t st) {
@@ -422,7 +433,7 @@ static int launch_grad_norm_with(const qlora_adamw_desc& d, float prescale, floa
     const int most = NB * sm_count() < OP_PARTIALS ? NB * sm_count() : OP_PARTIALS;
     int at = 0, used = 0;
     for (int launch = 0;; ++launch) {
-        const uint32_t chunks = fill_table(d, &at, OP_CHUNK, tab);
+        const uint32_t chunks = fill_table(d, &at, tab);
         if (chunks == 0) break;
         // (every launch on the grid of the first, whose partial sums the later ones add to)
         if (launch == 0) used = (int)(chunks < (uint32_t)most ? chunks : (uint32_t)most);
@@ -456,7 +467,7 @@ static int launch_adamw_with(const qlora_adamw_desc& d, const AdamScalars& sc, c
     static thread_local OptTable<CAP> tab;
     int at = 0;
     for (;;) {
-        const uint32_t chunks = fill_table(d, &at, OP_CHUNK, tab);
+        const uint32_t chunks = fill_table(d, &at, tab);
         if (chunks == 0) return QLORA_OK;
         const bool eight = d.state_type == QLORA_E4M3;
         const cudaError_t err = d.param_type == QLORA_BF16 ? launch_adamw_param<__nv_bfloat16>(d.grad_type, eight, chunks, tab, sc, st)
