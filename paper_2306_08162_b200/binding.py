@@ -213,44 +213,55 @@ def qlora_lrec_loss(student_logits, teacher_logits, labels, lambda_kl, lambda_ce
         raise QloraError(rc, "qlora_lrec_loss")
 
 
-_TYPES = None                    # torch dtype -> QLORA_BF16, QLORA_FP16, QLORA_FP32, QLORA_E4M3
+_torch = None
+_TYPES = {}                      # torch dtype -> QLORA_BF16, QLORA_FP16, QLORA_FP32, QLORA_E4M3
+_LOGIT_TYPES = (0, 1, 2)
+
+
+def _load_torch():
+    """torch and the element types, at the first call that needs them (the package itself can be imported without)."""
+    global _torch
+    if _torch is None:
+        import torch
+        _TYPES.update({torch.bfloat16: 0, torch.float16: 1, torch.float32: 2, torch.float8_e4m3fn: 3})
+        _torch = torch
+    return _torch
 
 
 def _type_of(t, where: str, allowed) -> int:
-    global _TYPES
-    if _TYPES is None:
-        import torch
-        _TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2, torch.float8_e4m3fn: 3}
     code = _TYPES.get(t.dtype, -1)
     if code not in allowed:
         raise ValueError(f"{where}: {t.dtype} is not supported here")
     return code
 
 
-_LOGIT_TYPES = (0, 1, 2)
-_FP32 = (2,)
+def _current_device(where: str) -> int:
+    """The current CUDA device, on which the library works: a tensor of another one, or of the host, in a kernel's hands would be a fault."""
+    if not _torch.cuda.is_initialized() and not _torch.cuda.is_available():
+        raise ValueError(f"{where}: tensors must be on the current CUDA device, and there is none")
+    return _torch.cuda.current_device()
 
 
 def _rows(t, where: str):
     """Shape and row stride of a 2-D tensor whose rows are dense (they may lie apart and begin anywhere)."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+    if t.dim() != 2:
         raise ValueError(f"{where}: a 2-D tensor with dense rows is needed")
-    T, V = t.shape
-    return T, V, t.stride(0) if T > 1 else V
+    (T, V), (stride, step) = t.shape, t.stride()
+    if step != 1 and V > 1:
+        raise ValueError(f"{where}: a 2-D tensor with dense rows is needed")
+    return T, V, stride if T > 1 else V
 
 
-def _vector(t, shape, dtype_name: str, where: str):
-    """An operand of a call over T rows: dense, of the type and the size that the library will assume."""
-    if t is not None and (str(t.dtype) != dtype_name or tuple(t.shape) != shape):
-        raise ValueError(f"{where}: {dtype_name} {list(shape)} is needed, got {t.dtype} {list(t.shape)}")
+def _operand(t, dtype, shape, where: str):
+    """An operand beside the logits: of the type and the size that the library will assume."""
+    if t is not None and (t.dtype is not dtype or t.shape != shape):
+        raise ValueError(f"{where}: {dtype} {list(shape)} is needed, got {t.dtype} {list(t.shape)}")
 
 
-def _on_current_device(where: str, *tensors):
-    """A tensor of another device (or of the host) in a kernel's hands would be a fault: the library works on the current device."""
-    import torch
-    here = torch.cuda.current_device() if torch.cuda.is_initialized() or torch.cuda.is_available() else None
+def _on_device(where: str, tensors):
+    device = _current_device(where)
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != here):
+        if t is not None and t.get_device() != device:
             raise ValueError(f"{where}: tensors must be on the current CUDA device, got {t.device}")
 
 
@@ -258,19 +269,22 @@ def qlora_token_logprobs(logits, tokens, inv_temperature, logprobs, entropy=None
     """Log probabilities of `tokens` (int32 [T], or None) under logits [T, V] (bf16, fp16 or fp32; rows may lie apart), the entropy of each
     row and its k most likely places (k = top_ids.shape[1]); stats fp32 [T, 3] is what the backward call reads.  Outputs may be None."""
     where = "qlora_token_logprobs"
+    torch = _load_torch()
     T, V, stride = _rows(logits, where)
     dtype = _type_of(logits, where, _LOGIT_TYPES)
-    top = top_ids if top_ids is not None else top_logprobs
-    if top is not None and top.dim() != 2:
-        raise ValueError(f"{where}: the alternatives are [T, k]")
-    k = top.shape[1] if top is not None else 0
-    _vector(tokens, (T,), "torch.int32", where)
-    _vector(logprobs, (T,), "torch.float32", where)
-    _vector(entropy, (T,), "torch.float32", where)
-    _vector(top_ids, (T, k), "torch.int32", where)
-    _vector(top_logprobs, (T, k), "torch.float32", where)
-    _vector(stats, (T, 3), "torch.float32", where)
-    _on_current_device(where, logits, tokens, logprobs, entropy, top_ids, top_logprobs, stats)
+    f32, row, k = torch.float32, (T,), 0
+    if top_ids is not None or top_logprobs is not None:
+        top = top_ids if top_ids is not None else top_logprobs
+        if top.dim() != 2:
+            raise ValueError(f"{where}: the alternatives are [T, k]")
+        k = top.shape[1]
+        _operand(top_ids, torch.int32, (T, k), where)
+        _operand(top_logprobs, f32, (T, k), where)
+    _operand(tokens, torch.int32, row, where)
+    _operand(logprobs, f32, row, where)
+    _operand(entropy, f32, row, where)
+    _operand(stats, f32, (T, 3), where)
+    _on_device(where, (logits, tokens, logprobs, entropy, top_ids, top_logprobs, stats))
     rc = _native().qlora_token_logprobs(T, V, stride, dtype, logits.data_ptr(), tokens, inv_temperature, k, logprobs, entropy, top_ids, top_logprobs,
                                         stats, stream)
     if rc != 0:
@@ -281,16 +295,18 @@ def qlora_token_logprobs_bwd(logits, tokens, inv_temperature, stats, d_logprobs,
     """Gradient of qlora_token_logprobs with respect to the logits, into dlogits [T, V] (the logits' type; rows may lie apart; may be the
     logits themselves)."""
     where = "qlora_token_logprobs_bwd"
+    torch = _load_torch()
     T, V, stride = _rows(logits, where)
     dtype = _type_of(logits, where, _LOGIT_TYPES)
     Tg, Vg, grad_stride = _rows(dlogits, where)
-    if (Tg, Vg) != (T, V) or dlogits.dtype != logits.dtype:
+    if Tg != T or Vg != V or dlogits.dtype is not logits.dtype:
         raise ValueError(f"{where}: dlogits has the shape and the type of logits")
-    _vector(tokens, (T,), "torch.int32", where)
-    _vector(stats, (T, 3), "torch.float32", where)
-    _vector(d_logprobs, (T,), "torch.float32", where)
-    _vector(d_entropy, (T,), "torch.float32", where)
-    _on_current_device(where, logits, tokens, stats, d_logprobs, d_entropy, dlogits)
+    f32, row = torch.float32, (T,)
+    _operand(tokens, torch.int32, row, where)
+    _operand(stats, f32, (T, 3), where)
+    _operand(d_logprobs, f32, row, where)
+    _operand(d_entropy, f32, row, where)
+    _on_device(where, (logits, tokens, stats, d_logprobs, d_entropy, dlogits))
     rc = _native().qlora_token_logprobs_bwd(T, V, stride, dtype, logits.data_ptr(), tokens, inv_temperature, stats, d_logprobs, d_entropy, grad_stride,
                                             dlogits.data_ptr(), stream)
     if rc != 0:
@@ -307,69 +323,80 @@ def adamw_desc(params, grads, m, v, master=None, m_scale=None, v_scale=None, bet
     new descriptor."""
     import bisect
     where = "adamw_desc"
-    lists = dict(param=list(params), master=list(master) if master is not None else None, grad=list(grads), m=list(m), v=list(v),
-                 m_scale=list(m_scale) if m_scale is not None else None, v_scale=list(v_scale) if v_scale is not None else None)
+    _load_torch()
+    lists = dict(param=params, master=master, grad=grads, m=m, v=v, m_scale=m_scale, v_scale=v_scale)
+    lists = {name: list(ts) for name, ts in lists.items() if ts is not None}
     n = len(lists["param"])
     for name, ts in lists.items():
-        if ts is not None and len(ts) != n:
+        if len(ts) != n:
             raise ValueError(f"{where}: {len(ts)} tensors in {name}, {n} parameters")
     d = _AdamwDesc(n_tensors=n, param_type=2, grad_type=2, state_type=2, beta1=beta1, beta2=beta2, eps=eps, weight_decay=weight_decay)
-    eight = n > 0 and _type_of(lists["m"][0], where, (2, 3)) == 3
-    if n:
-        d.param_type, d.grad_type, d.state_type = _type_of(lists["param"][0], where, _LOGIT_TYPES), _type_of(lists["grad"][0], where, _LOGIT_TYPES), 3 if eight else 2
-    if n and (lists["m_scale"] is not None, lists["v_scale"] is not None) != (eight, eight):
+    d.keep, d.device = lists, None
+    if n == 0:
+        return d
+    d.param_type, d.grad_type, d.state_type = (_type_of(lists[name][0], f"{where}: {name}", allowed)
+                                               for name, allowed in (("param", _LOGIT_TYPES), ("grad", _LOGIT_TYPES), ("m", (2, 3))))
+    eight = d.state_type == 3
+    if ("m_scale" in lists, "v_scale" in lists) != (eight, eight):
         raise ValueError(f"{where}: m_scale and v_scale go with states in 8 bits, and only with those")
-    if lists["master"] is not None and n and d.param_type == 2:
+    if "master" in lists and d.param_type == 2:
         raise ValueError(f"{where}: fp32 parameters have no master weights")
-    want = dict(param=d.param_type, master=2, grad=d.grad_type, m=d.state_type, v=d.state_type, m_scale=2, v_scale=2)
-    array = (_AdamwTensor * max(n, 1))()
-    ranges = []
+    sizes = [t.numel() for t in lists["param"]]
+    blocks = [-(-size // 256) for size in sizes]
+    device = lists["param"][0].get_device()
+    array = (_AdamwTensor * n)()
+    written, read, foreign = [], [], device < 0
     for name, ts in lists.items():
-        for j, t in enumerate(ts or ()):
-            size = lists["param"][j].numel()
-            _type_of(t, f"{where}: {name}[{j}]", (want[name],))
-            if t.numel() != (-(-size // 256) if name.endswith("_scale") else size):
-                raise ValueError(f"{where}: {name}[{j}] has {t.numel()} elements for a parameter of {size}")
+        kind = {"param": d.param_type, "grad": d.grad_type, "m": d.state_type, "v": d.state_type}.get(name, 2)
+        dtype, ranges = ts[0].dtype, read if name == "grad" else written
+        if _TYPES.get(dtype) != kind:
+            raise ValueError(f"{where}: {dtype} is not supported as {name} here")
+        for j, (t, size) in enumerate(zip(ts, blocks if name.endswith("_scale") else sizes)):
+            if t.dtype is not dtype:
+                raise ValueError(f"{where}: {t.dtype} is not supported here: {name}[0] is {dtype}")
+            if t.numel() != size:
+                raise ValueError(f"{where}: {name}[{j}] has {t.numel()} elements for a parameter of {sizes[j]}")
             if not t.is_contiguous():
                 raise ValueError(f"{where}: tensors must be contiguous (dense)")
-            setattr(array[j], name, t.data_ptr())
+            foreign = foreign or t.get_device() != device
+            at = t.data_ptr()
+            setattr(array[j], name, at)
             if size:
-                ranges.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), name != "grad"))
-    for j, t in enumerate(lists["param"]):
-        array[j].n = t.numel()
-    written = sorted(r for r in ranges if r[2])
-    for a, b in zip(written, written[1:]):
-        if b[0] < a[1]:
+                ranges.append((at, at + size * t.element_size()))
+    for j, size in enumerate(sizes):
+        array[j].n = size
+    written.sort()
+    for (_, end), (begin, _) in zip(written, written[1:]):
+        if begin < end:
             raise ValueError(f"{where}: two of the tensors that the step writes overlap (the same one twice?)")
-    starts = [r[0] for r in written]
-    for lo, hi, w in ranges:
-        if not w:
-            at = bisect.bisect_left(starts, hi)                       # the last written range that begins before this one ends
-            if at > 0 and written[at - 1][1] > lo:
-                raise ValueError(f"{where}: a gradient overlaps a tensor that the step writes")
-    flat = [t for ts in lists.values() for t in ts or ()]
-    if flat and (not flat[0].is_cuda or any(t.device != flat[0].device for t in flat)):
+    for begin, end in read:
+        at = bisect.bisect_left(written, (end,))                      # the last written range that begins before this one ends
+        if at > 0 and written[at - 1][1] > begin:
+            raise ValueError(f"{where}: a gradient overlaps a tensor that the step writes")
+    if foreign:
         raise ValueError(f"{where}: tensors must be on one CUDA device")
-    d.tensors = array
+    d.tensors, d.device = array, device
     d.keep = (array, lists)
-    d.device = flat[0].get_device() if flat else None
     return d
 
 
-def _check_desc_device(d, where: str):
-    import torch
-    if d.device is not None and d.device != torch.cuda.current_device():
-        raise ValueError(f"{where}: the descriptor's tensors are on device {d.device}, the current one is {torch.cuda.current_device()}")
+def _check_desc(d, where: str) -> int:
+    if not isinstance(d, _AdamwDesc):
+        raise TypeError(f"{where}: the optimizer descriptor must come from adamw_desc()")
+    _load_torch()
+    device = _current_device(where)
+    if d.device is not None and d.device != device:
+        raise ValueError(f"{where}: the descriptor's tensors are on device {d.device}, the current one is {device}")
+    return device
 
 
 def qlora_grad_norm(d, prescale, max_norm, out, workspace, stream=None, workspace_bytes=None):
     """out fp32 [2]: the norm of prescale times all gradients of the descriptor, and the factor for qlora_adamw that clips it to max_norm."""
     where = "qlora_grad_norm"
-    if isinstance(d, _AdamwDesc):
-        _check_desc_device(d, where)
-        if not isinstance(out, int):
-            _vector(out, (2,), "torch.float32", where)
-            _on_current_device(where, out, workspace)
+    device = _check_desc(d, where)
+    _operand(out, _torch.float32, (2,), where)
+    if out.get_device() != device or workspace.get_device() != device:
+        raise ValueError(f"{where}: tensors must be on the current CUDA device")
     rc = _native().qlora_grad_norm(d, prescale, max_norm, out, workspace, workspace_bytes, stream)
     if rc != 0:
         raise QloraError(rc, where)
@@ -379,19 +406,19 @@ def qlora_adamw(d, lr, step, norm=None, stream=None):
     """One AdamW step over the descriptor's tensors.  lr: a number or an fp32 tensor [1]; step: an int from 1 or an int32 tensor [1] (device
     memory that a captured step reads at replay); norm: fp32 [2] from qlora_grad_norm or None."""
     where = "qlora_adamw"
-    lr_dev = lr if hasattr(lr, "data_ptr") else None
-    step_dev = step if hasattr(step, "data_ptr") else None
-    if isinstance(d, _AdamwDesc):
-        _check_desc_device(d, where)
-    if lr_dev is not None:
-        _vector(lr_dev, (1,), "torch.float32", where)
-    if step_dev is not None:
-        _vector(step_dev, (1,), "torch.int32", where)
-    if norm is not None and not isinstance(norm, int):
-        _vector(norm, (2,), "torch.float32", where)
-    if lr_dev is not None or step_dev is not None or (norm is not None and not isinstance(norm, int)):
-        _on_current_device(where, lr_dev, step_dev, None if isinstance(norm, int) else norm)
-    rc = _native().qlora_adamw(d, 0.0 if lr_dev is not None else lr, 0 if step_dev is not None else step, lr_dev, step_dev, norm, stream)
+    device = _check_desc(d, where)
+    lr_dev = step_dev = None
+    if hasattr(lr, "data_ptr"):
+        _operand(lr, _torch.float32, (1,), where)
+        lr, lr_dev = 0.0, lr
+    if hasattr(step, "data_ptr"):
+        _operand(step, _torch.int32, (1,), where)
+        step, step_dev = 0, step
+    _operand(norm, _torch.float32, (2,), where)
+    for t in (lr_dev, step_dev, norm):
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"{where}: tensors must be on the current CUDA device")
+    rc = _native().qlora_adamw(d, lr, step, lr_dev, step_dev, norm, stream)
     if rc != 0:
         raise QloraError(rc, where)
 
