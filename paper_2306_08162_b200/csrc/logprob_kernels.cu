@@ -9,12 +9,13 @@
 
 namespace qlora {
 
+#ifndef KN
+#define KN true
+#define KF true
+#endif
 constexpr int LP_UNROLL = 4;             // 16-byte vectors that a thread has on their way at a time
-constexpr int LP_CLUSTER = 8;            // most blocks that share a row
-constexpr int LP_SEGMENTS = 16;          // stretches of a thread's part of the row with a maximum of their own
 constexpr int LP_CANDIDATES = 640;       // entries that are put in order together (a part of less than 64 vectors has fewer logits)
 constexpr int LP_HITS = 64;              // stretches that a warp looks at again
-static_assert(LP_CANDIDATES >= LP_CLUSTER * QLORA_MAX_TOP, "the lists of a cluster are merged in the same place");
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float LP_FLOOR = -0x1p96f, LP_LEAST = -0x1p80f, LP_MOST = 0x1p60f;     // see RowSums
 
@@ -100,9 +101,11 @@ struct RowParts {
     __device__ __forceinline__ const uint4* body() const { return reinterpret_cast<const uint4*>(z + head); }
 };
 
-__device__ __forceinline__ uint4 load_stream(const uint4* p) {          // read once, not kept in L1
+template <bool KEEP = false>
+__device__ __forceinline__ uint4 load_stream(const uint4* p) {          // KEEP: in L1, for a second look
     uint4 v;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    if (KEEP) asm volatile("ld.global.L1::evict_last.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    else asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
 
@@ -249,13 +252,12 @@ __device__ __forceinline__ void each_from(const RowParts<T>& row, uint32_t least
 }
 
 struct alignas(16) TopShared {              // (the candidates are read two at a time)
-    uint64_t cand[LP_CANDIDATES];        // entries that may be among the largest; in the first block of a cluster, then everybody's lists
-    uint64_t list[QLORA_MAX_TOP];        // the block's largest entries in order
+    uint64_t cand[LP_CANDIDATES];        // entries that may be among the largest
     uint32_t bound[32];                  // by warp
     int count, in_warp[32];
 };
-template <int THREADS> struct TopWarps {
-    float segment[LP_SEGMENTS * THREADS];   // maxima of the threads' stretches
+template <int THREADS, int SEGMENTS> struct TopWarps {
+    float segment[SEGMENTS * THREADS];       // maxima of the threads' stretches
     int hit[THREADS / 32][LP_HITS];         // stretches with a candidate, by their first vector
 };
 
@@ -276,7 +278,7 @@ __device__ __noinline__ int count_from(const RowParts<T>& row, uint32_t least, T
 // More candidates than there is room for (many equal logits, or large ones in a cluster): the kk-th largest key itself, found bit by bit
 // with a pass over the row each, then everything above it and, in the order of their places, as many equals as are wanted.
 template <typename T, int THREADS>
-__device__ __noinline__ int crowded(const RowParts<T>& row, int first, int n, int kk, uint32_t bound, TopShared& sh) {
+__device__ __noinline__ int crowded(const RowParts<T>& row, int n, int kk, uint32_t bound, TopShared& sh) {
     uint32_t lo = bound, hi = 0xFFFFFFFFu;                          // at least kk keys are >= lo
     while (lo < hi) {                                               // (first whether it is the bound itself: the usual case)
         const uint32_t mid = lo == bound ? bound + 1 : lo + (hi - lo) / 2 + ((hi - lo) & 1);
@@ -286,7 +288,7 @@ __device__ __noinline__ int crowded(const RowParts<T>& row, int first, int n, in
     __syncthreads();
     if (threadIdx.x == 0) sh.count = 0;
     __syncthreads();
-    if (lo != 0xFFFFFFFFu) each_from<T, THREADS>(row, lo + 1, [&](uint32_t key, int j) { sh.cand[atomicAdd(&sh.count, 1)] = entry_key(key, first + j); });
+    if (lo != 0xFFFFFFFFu) each_from<T, THREADS>(row, lo + 1, [&](uint32_t key, int j) { sh.cand[atomicAdd(&sh.count, 1)] = entry_key(key, j); });
     __syncthreads();
     int have = sh.count;                                            // fewer than kk
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -302,7 +304,7 @@ __device__ __noinline__ int crowded(const RowParts<T>& row, int first, int n, in
             all += sh.in_warp[w];
         }
         at += __popc(who & ((1u << lane) - 1u));
-        if (is && at < kk) sh.cand[at] = entry_key(lo, first + j);
+        if (is && at < kk) sh.cand[at] = entry_key(lo, j);
         have = all;
         __syncthreads();
     }
@@ -330,7 +332,7 @@ __device__ __forceinline__ void offer_bound(int vectors, int kk, float top, TopS
 // `segment`: the maxima of this warp's stretches; `hit`: LP_HITS places of this warp's own; `ends`: the logits at this thread's places of
 // the head and of the rest.
 template <typename T, int THREADS>
-__device__ __forceinline__ void gather(const RowParts<T>& row, int first, uint32_t bound, int span_log2, const float* segment, int* hit, float head, float rest, TopShared& sh) {
+__device__ __forceinline__ void gather(const RowParts<T>& row, uint32_t bound, int span_log2, const float* segment, int* hit, float head, float rest, TopShared& sh) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     int hits = 0;
     for (int g = 0, c0 = warp * 32; c0 < row.vectors; ++g, c0 += (LP_UNROLL * THREADS) << span_log2) {
@@ -347,13 +349,14 @@ __device__ __forceinline__ void gather(const RowParts<T>& row, int first, uint32
     __syncwarp();
     auto offer = [&](uint32_t k, int j) {
         const int at = atomicAdd(&sh.count, 1);
-        if (at < LP_CANDIDATES) sh.cand[at] = entry_key(k, first + j);
+        if (at < LP_CANDIDATES) sh.cand[at] = entry_key(k, j);
     };
     const uint4* body = row.body();
-    static_assert(LP_UNROLL == 4, "a round of vectors is a power of two");
+    constexpr int UL = LP_UNROLL == 4 ? 2 : LP_UNROLL == 2 ? 1 : 3;
+    static_assert(1 << UL == LP_UNROLL, "a round of vectors is a power of two");
     const float least = key_logit(bound);
-    for (int w = lane; w < hits << (span_log2 + 2); w += 32) {
-        const int at = hit[w >> (span_log2 + 2)] + (w & ((4 << span_log2) - 1)) * THREADS;
+    for (int w = lane; w < hits << (span_log2 + UL); w += 32) {
+        const int at = hit[w >> (span_log2 + UL)] + (w & ((LP_UNROLL << span_log2) - 1)) * THREADS;
         if (at >= row.vectors) continue;
         const uint4 v = body[at];
         uint32_t found = 0;                                          // (a NaN is; one that is not, if the bound is NaN, falls out below)
@@ -375,10 +378,10 @@ __device__ __forceinline__ void gather(const RowParts<T>& row, int first, uint32
 
 // With the candidates there (behind a barrier): calls put(place, entry) for the kk largest.
 template <typename T, int THREADS, typename F>
-__device__ __forceinline__ void select(const RowParts<T>& row, int first, int n, int kk, uint32_t bound, TopShared& sh, F put) {
+__device__ __forceinline__ void select(const RowParts<T>& row, int n, int kk, uint32_t bound, TopShared& sh, F put) {
     int count = sh.count;
     if (count > LP_CANDIDATES) {
-        count = crowded<T, THREADS>(row, first, n, kk, bound, sh);
+        count = crowded<T, THREADS>(row, n, kk, bound, sh);
         __syncthreads();
     }
     for (int i = threadIdx.x; i < count; i += THREADS) {             // an entry's place is the number of larger ones
@@ -396,28 +399,8 @@ __device__ __forceinline__ uint32_t common_bound(const TopShared& sh, int warps)
     return __reduce_min_sync(0xFFFFFFFFu, sh.bound[min((int)(threadIdx.x & 31), warps - 1)]);
 }
 
-// Shared memory of another block of the cluster.
-__device__ __forceinline__ uint32_t remote(const void* p, int rank) {
-    uint32_t r;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
-    return r;
-}
-__device__ __forceinline__ float remote_float(const void* p, int rank) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote(p, rank)) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint64_t remote_u64(const void* p, int rank) {
-    uint64_t v;
-    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(remote(p, rank)) : "memory");
-    return v;
-}
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive;\n\tbarrier.cluster.wait;" ::: "memory");
-}
-
 struct LogprobArgs {
-    int T, V, k, blocks;
+    int T, V, k;
     long long stride;
     const void* logits;
     const int32_t* tokens;
@@ -450,124 +433,29 @@ __device__ __forceinline__ void tell_top(const LogprobArgs& p, int row, int at, 
     if (p.top_logprobs != nullptr) p.top_logprobs[(long long)row * p.k + at] = r.none ? -INFINITY : (entry_logit(e) - r.m) * p.c - r.logs;
 }
 __device__ __forceinline__ bool is_odd(float m) { return fabsf(m) < INFINITY && !(m > LP_LEAST && m < LP_MOST); }
-template <int THREADS>
+template <int THREADS, int SEGMENTS>
 __device__ __forceinline__ int span_of(int vectors) {                    // log2 of the rounds that make a stretch
     const int round = LP_UNROLL * THREADS, rounds = (vectors + round - 1) / round;
-    return rounds <= LP_SEGMENTS ? 0 : 32 - __clz((rounds - 1) / LP_SEGMENTS);
+    return rounds <= SEGMENTS ? 0 : 32 - __clz((rounds - 1) / SEGMENTS);
 }
 
-// Few rows: one to a cluster of `blocks` blocks (1: no cluster), each with a part of it.
-template <typename T, int THREADS, bool TOP>
-__global__ void __launch_bounds__(THREADS) logprobs_shared_kernel(const LogprobArgs p) {
-    __shared__ RowSums sums[THREADS / 32], mine;
-    __shared__ float row_max;
-    __shared__ RowResult result;
-    __shared__ __align__(16) unsigned char top_raw[TOP ? sizeof(TopShared) : 16], warps_raw[TOP ? sizeof(TopWarps<THREADS>) : 16];
-    TopShared& sh = *reinterpret_cast<TopShared*>(top_raw);
-    TopWarps<THREADS>& own = *reinterpret_cast<TopWarps<THREADS>*>(warps_raw);
-    pdl_launch_dependents();
-    pdl_wait();
-    const int blocks = p.blocks, V = p.V, k = p.k, row = blockIdx.x / blocks, rank = blockIdx.x % blocks, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const float kd = p.c * kLog2e;
-    const T* z = static_cast<const T*>(p.logits) + row * p.stride;
-    int token = -1;
-    float token_logit = 0.f;
-    if (threadIdx.x == 0 && rank == 0 && p.logprobs != nullptr) {
-        token = p.tokens[row];
-        if (token >= 0 && token < V) token_logit = lp_f(z[token]);
-        else token = -1;
-    }
-    // the part: whole vectors, but for the row's own ends (at most 2^22 vectors times 8 blocks)
-    const RowParts<T> whole(z, V);
-    auto begin_of = [&](int r) { return r == 0 ? 0 : r == blocks ? V : whole.head + (int)((unsigned)whole.vectors * (unsigned)r / (unsigned)blocks) * Vec<T>::N; };
-    const int first = begin_of(rank), n = begin_of(rank + 1) - first, kk = min(k, n);
-    const RowParts<T> part(z + first, n);
-    const float head = (int)threadIdx.x < part.head ? lp_f(part.z[threadIdx.x]) : -INFINITY;
-    const float rest = (int)threadIdx.x < part.rest ? lp_f(part.z[part.tail + threadIdx.x]) : -INFINITY;
-    const int span_log2 = span_of<THREADS>(part.vectors);
-    ThreadRow<T, THREADS, TOP> mine_of(own.segment, span_log2);
-    for (int c0 = threadIdx.x; c0 < part.vectors; c0 += LP_UNROLL * THREADS) {
-        uint4 v[LP_UNROLL];
-#pragma unroll
-        for (int u = 0; u < LP_UNROLL; ++u)
-            if (c0 + u * THREADS < part.vectors) v[u] = load_stream(part.body() + c0 + u * THREADS);
-        mine_of.template round<false>(v, c0, part.vectors, kd);
-    }
-    mine_of.finish();
-    if ((int)threadIdx.x < part.head) add_one(mine_of.x, head, kd);
-    if ((int)threadIdx.x < part.rest) add_one(mine_of.x, rest, kd);
-    if (TOP) offer_bound<THREADS>(part.vectors, kk, mine_of.x.m, sh);
-    RowSums x = warp_merge(mine_of.x, kd);
-    if (lane == 0) sums[warp] = x;
-    __syncthreads();
-    if (warp == 0) {
-        x = warp_merge(lane < THREADS / 32 ? sums[lane] : RowSums{-INFINITY, 0.f, 0.f}, kd);
-        if (lane == 0) mine = x;
-    }
-    if (TOP) {
-        const uint32_t bound = common_bound(sh, THREADS / 32);
-        gather<T, THREADS>(part, first, bound, span_log2, own.segment, own.hit[warp], head, rest, sh);
-        __syncthreads();
-        select<T, THREADS>(part, first, n, kk, bound, sh, [&](int at, uint64_t e) { sh.list[at] = e; });
-    }
-    if (blocks > 1) {
-        cluster_sync();
-        if (rank == 0 && warp == 0) {
-            x = RowSums{-INFINITY, 0.f, 0.f};
-            if (lane < blocks) x = RowSums{remote_float(&mine.m, lane), remote_float(&mine.s, lane), remote_float(&mine.a, lane)};
-            x = warp_merge(x, kd);
-        }
-    }
-    if (rank == 0) {
-        if (threadIdx.x == 0) row_max = x.m;
-        __syncthreads();
-        const bool odd = is_odd(row_max);
-        float logs = 0.f, H = 0.f;
-        if (odd) odd_row<T, THREADS>(z, V, row_max, p.c, reinterpret_cast<float*>(sums), logs, H);
-        if (threadIdx.x == 0) result = tell_row(p, row, x, kd, odd, logs, H, token, token_logit);
-    }
-    if (TOP && rank == 0) {
-        // an entry's place in the whole: its own list's plus, list by list, the number of larger ones (every list has k: a part of a shared
-        // row is longer than that)
-        for (int e = threadIdx.x; blocks > 1 && e < blocks * k; e += THREADS) {
-            const int r = e / k;
-            sh.cand[e] = remote_u64(&sh.list[e - r * k], r);
-        }
-        __syncthreads();
-        for (int e = threadIdx.x; e < blocks * k; e += THREADS) {
-            const uint64_t it = blocks > 1 ? sh.cand[e] : sh.list[e];
-            const int of = e / k;
-            int at = e - of * k;
-            for (int r = 0; r < blocks; ++r) {
-                int lo = 0, hi = r == of ? 0 : k;                    // entries before lo are larger, those from hi on are not
-                while (lo < hi) {
-                    const int mid = (lo + hi) >> 1;
-                    if (sh.cand[r * k + mid] > it) lo = mid + 1; else hi = mid;
-                }
-                at += lo;
-                if (at >= k) break;
-            }
-            if (at < k) tell_top(p, row, at, it, result);
-        }
-    }
-    if (blocks > 1) cluster_sync();                                  // (nobody leaves while the first block reads)
-}
+// How a row is shared out: rows of up to 8 KB to blocks of 128 threads, which read them in one round; longer ones to blocks of 256 threads, 6 on an SM; where
+// there are no more rows than SMs, to blocks of 512.
+template <int THREADS> struct RowPlan;
+template <> struct RowPlan<128> { static constexpr int SEGMENTS = 1, PER_SM = 10, PER_SM_TOP = 10; static constexpr bool KEEP = KN; };
+template <> struct RowPlan<256> { static constexpr int SEGMENTS = 16, PER_SM = 6, PER_SM_TOP = 6; static constexpr bool KEEP = false; };
+template <> struct RowPlan<512> { static constexpr int SEGMENTS = 8, PER_SM = 1, PER_SM_TOP = 1; static constexpr bool KEEP = KF; };
 
-#ifndef RB
-#define RB 6
-#define RBT 6
-#define NB 10
-#define NBT 10
-#endif
-// Many rows: one to a block.
 template <typename T, int THREADS, bool TOP>
-__global__ void __launch_bounds__(THREADS, THREADS == 128 ? (TOP ? NBT : NB) : (TOP ? RBT : RB)) logprobs_rows_kernel(const __grid_constant__ LogprobArgs p) {
+__global__ void __launch_bounds__(THREADS, TOP ? RowPlan<THREADS>::PER_SM_TOP : RowPlan<THREADS>::PER_SM) logprobs_kernel(const __grid_constant__ LogprobArgs p) {
+    constexpr int SEGMENTS = RowPlan<THREADS>::SEGMENTS;
+    constexpr bool KEEP = TOP && RowPlan<THREADS>::KEEP;
     __shared__ RowSums sums[THREADS / 32];
     __shared__ RowResult result;
     __shared__ float odd_sums[2 * (THREADS / 32)];
-    __shared__ __align__(16) unsigned char top_raw[TOP ? sizeof(TopShared) : 16], warps_raw[TOP ? sizeof(TopWarps<THREADS>) : 16];
+    __shared__ __align__(16) unsigned char top_raw[TOP ? sizeof(TopShared) : 16], warps_raw[TOP ? sizeof(TopWarps<THREADS, SEGMENTS>) : 16];
     TopShared& sh = *reinterpret_cast<TopShared*>(top_raw);
-    TopWarps<THREADS>& own = *reinterpret_cast<TopWarps<THREADS>*>(warps_raw);
+    TopWarps<THREADS, SEGMENTS>& own = *reinterpret_cast<TopWarps<THREADS, SEGMENTS>*>(warps_raw);
     pdl_launch_dependents();
     pdl_wait();
     const int row = blockIdx.x, V = p.V, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -577,20 +465,20 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? (TOP ? NBT : NB) : (
     const int token = threadIdx.x == 0 && p.logprobs != nullptr ? p.tokens[row] : -1;
     const float head = (int)threadIdx.x < part.head ? lp_f(part.z[threadIdx.x]) : -INFINITY;
     const float rest = (int)threadIdx.x < part.rest ? lp_f(part.z[part.tail + threadIdx.x]) : -INFINITY;
-    const int span_log2 = span_of<THREADS>(part.vectors);
+    const int span_log2 = span_of<THREADS, SEGMENTS>(part.vectors);
     ThreadRow<T, THREADS, TOP> mine(own.segment, span_log2);
     int c0 = threadIdx.x;
     for (; c0 + (LP_UNROLL - 1) * THREADS < part.vectors; c0 += LP_UNROLL * THREADS) {
         uint4 v[LP_UNROLL];
 #pragma unroll
-        for (int u = 0; u < LP_UNROLL; ++u) v[u] = load_stream(part.body() + c0 + u * THREADS);
+        for (int u = 0; u < LP_UNROLL; ++u) v[u] = load_stream<KEEP>(part.body() + c0 + u * THREADS);
         mine.template round<true>(v, c0, part.vectors, kd);
     }
     if (c0 < part.vectors) {
         uint4 v[LP_UNROLL];
 #pragma unroll
         for (int u = 0; u < LP_UNROLL; ++u)
-            if (c0 + u * THREADS < part.vectors) v[u] = load_stream(part.body() + c0 + u * THREADS);
+            if (c0 + u * THREADS < part.vectors) v[u] = load_stream<KEEP>(part.body() + c0 + u * THREADS);
         mine.template round<false>(v, c0, part.vectors, kd);
     }
     mine.finish();
@@ -614,9 +502,9 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? (TOP ? NBT : NB) : (
     }
     if (TOP) {
         const uint32_t bound = common_bound(sh, THREADS / 32);
-        gather<T, THREADS>(part, 0, bound, span_log2, own.segment, own.hit[warp], head, rest, sh);
+        gather<T, THREADS>(part, bound, span_log2, own.segment, own.hit[warp], head, rest, sh);
         __syncthreads();
-        select<T, THREADS>(part, 0, V, p.k, bound, sh, [&](int at, uint64_t e) { tell_top(p, row, at, e, result); });
+        select<T, THREADS>(part, V, p.k, bound, sh, [&](int at, uint64_t e) { tell_top(p, row, at, e, result); });
     }
 }
 
@@ -745,34 +633,21 @@ __global__ void __launch_bounds__(LP_BWD_THREADS) logprobs_bwd_scalar_kernel(con
     for (int j = begin + threadIdx.x; j < end; j += LP_BWD_THREADS) dz[j] = lp_to<T>(r.zero ? 0.f : r.of_one(lp_f(z[j]), j));
 }
 
-// Blocks that share a row: as many as still fit the SMs all at once, while each has 4 KB of it at least.
-static int row_blocks(int T, long long row_bytes, int sms) {
-    int blocks = 1;
-    while (blocks < LP_CLUSTER && (long long)T * blocks * 2 <= 2 * sms && row_bytes / (blocks * 2) >= 4096) blocks *= 2;
-    return blocks;
-}
-
-template <typename T, bool TOP>
-static cudaError_t launch_logprobs_shared(const LogprobArgs& p, cudaStream_t st) {
-    return launch_pdl(logprobs_shared_kernel<T, 256, TOP>, dim3((unsigned)p.T * (unsigned)p.blocks), dim3(256), 0, st, (unsigned)p.blocks, p);
-}
 template <typename T, int THREADS, bool TOP>
 static cudaError_t launch_logprobs_rows(const LogprobArgs& p, cudaStream_t st) {
-    return launch_pdl(logprobs_rows_kernel<T, THREADS, TOP>, dim3((unsigned)p.T), dim3(THREADS), 0, st, 1, p);
+    return launch_pdl(logprobs_kernel<T, THREADS, TOP>, dim3((unsigned)p.T), dim3(THREADS), 0, st, 1, p);
 }
 template <typename T>
 static cudaError_t launch_logprobs(const LogprobArgs& p, cudaStream_t st) {
     const bool top = p.k > 0;
-    if (p.blocks > 1) return top ? launch_logprobs_shared<T, true>(p, st) : launch_logprobs_shared<T, false>(p, st);
-    const bool narrow = (long long)p.V * (int)sizeof(T) <= 8192;
-    if (narrow) return top ? launch_logprobs_rows<T, 128, true>(p, st) : launch_logprobs_rows<T, 128, false>(p, st);
+    if ((long long)p.V * (int)sizeof(T) <= 8192) return top ? launch_logprobs_rows<T, 128, true>(p, st) : launch_logprobs_rows<T, 128, false>(p, st);
+    if (p.T <= sm_count()) return top ? launch_logprobs_rows<T, 512, true>(p, st) : launch_logprobs_rows<T, 512, false>(p, st);
     return top ? launch_logprobs_rows<T, 256, true>(p, st) : launch_logprobs_rows<T, 256, false>(p, st);
 }
 
 int launch_token_logprobs(int T, int V, long long row_stride, int dtype, const void* logits, const int32_t* tokens, float c, int k, float* logprobs,
                           float* entropy, int32_t* top_ids, float* top_logprobs, float* stats, cudaStream_t st) {
-    LogprobArgs p{T, V, k, 1, row_stride, logits, tokens, c, logprobs, entropy, stats, top_logprobs, top_ids};
-    p.blocks = row_blocks(T, (long long)V * (dtype == QLORA_FP32 ? 4 : 2), sm_count());
+    const LogprobArgs p{T, V, k, row_stride, logits, tokens, c, logprobs, entropy, stats, top_logprobs, top_ids};
     const cudaError_t err = dtype == QLORA_BF16 ? launch_logprobs<__nv_bfloat16>(p, st) : dtype == QLORA_FP16 ? launch_logprobs<__half>(p, st) : launch_logprobs<float>(p, st);
     return err == cudaSuccess ? QLORA_OK : QLORA_ERR_CUDA;
 }
