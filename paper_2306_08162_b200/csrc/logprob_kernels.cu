@@ -9,10 +9,6 @@
 
 namespace qlora {
 
-#ifndef KN
-#define KN true
-#define KF true
-#endif
 constexpr int LP_UNROLL = 4;             // 16-byte vectors that a thread has on their way at a time
 constexpr int LP_CANDIDATES = 640;       // entries that are put in order together (a part of less than 64 vectors has fewer logits)
 constexpr int LP_HITS = 64;              // stretches that a warp looks at again
@@ -439,17 +435,16 @@ __device__ __forceinline__ int span_of(int vectors) {                    // log2
     return rounds <= SEGMENTS ? 0 : 32 - __clz((rounds - 1) / SEGMENTS);
 }
 
-// How a row is shared out: rows of up to 8 KB to blocks of 128 threads, which read them in one round; longer ones to blocks of 256 threads, 6 on an SM; where
-// there are no more rows than SMs, to blocks of 512.
-template <int THREADS> struct RowPlan;
-template <> struct RowPlan<128> { static constexpr int SEGMENTS = 1, PER_SM = 10, PER_SM_TOP = 10; static constexpr bool KEEP = KN; };
-template <> struct RowPlan<256> { static constexpr int SEGMENTS = 16, PER_SM = 6, PER_SM_TOP = 6; static constexpr bool KEEP = false; };
-template <> struct RowPlan<512> { static constexpr int SEGMENTS = 8, PER_SM = 1, PER_SM_TOP = 1; static constexpr bool KEEP = KF; };
+// How a row is shared out.  KEEP: the row stays in L1 for the second look at it.
+struct ShortRow { static constexpr int THREADS = 128, SEGMENTS = 1, PER_SM = 10; static constexpr bool KEEP = true; };      // up to 8 KB: one round
+struct MiddleRow { static constexpr int THREADS = 256, SEGMENTS = 4, PER_SM = 6; static constexpr bool KEEP = true; };      // up to 64 KB
+struct LongRow { static constexpr int THREADS = 256, SEGMENTS = 16, PER_SM = 6; static constexpr bool KEEP = false; };
+struct LoneRow { static constexpr int THREADS = 512, SEGMENTS = 8, PER_SM = 1; static constexpr bool KEEP = true; };        // no more rows than SMs
 
-template <typename T, int THREADS, bool TOP>
-__global__ void __launch_bounds__(THREADS, TOP ? RowPlan<THREADS>::PER_SM_TOP : RowPlan<THREADS>::PER_SM) logprobs_kernel(const __grid_constant__ LogprobArgs p) {
-    constexpr int SEGMENTS = RowPlan<THREADS>::SEGMENTS;
-    constexpr bool KEEP = TOP && RowPlan<THREADS>::KEEP;
+template <typename T, typename Plan, bool TOP>
+__global__ void __launch_bounds__(Plan::THREADS, Plan::PER_SM) logprobs_kernel(const __grid_constant__ LogprobArgs p) {
+    constexpr int THREADS = Plan::THREADS, SEGMENTS = Plan::SEGMENTS;
+    constexpr bool KEEP = TOP && Plan::KEEP;
     __shared__ RowSums sums[THREADS / 32];
     __shared__ RowResult result;
     __shared__ float odd_sums[2 * (THREADS / 32)];
@@ -633,16 +628,18 @@ __global__ void __launch_bounds__(LP_BWD_THREADS) logprobs_bwd_scalar_kernel(con
     for (int j = begin + threadIdx.x; j < end; j += LP_BWD_THREADS) dz[j] = lp_to<T>(r.zero ? 0.f : r.of_one(lp_f(z[j]), j));
 }
 
-template <typename T, int THREADS, bool TOP>
-static cudaError_t launch_logprobs_rows(const LogprobArgs& p, cudaStream_t st) {
-    return launch_pdl(logprobs_kernel<T, THREADS, TOP>, dim3((unsigned)p.T), dim3(THREADS), 0, st, 1, p);
+template <typename T, typename Plan>
+static cudaError_t launch_logprobs_as(const LogprobArgs& p, cudaStream_t st) {
+    const dim3 grid((unsigned)p.T), block(Plan::THREADS);
+    return p.k > 0 ? launch_pdl(logprobs_kernel<T, Plan, true>, grid, block, 0, st, 1, p) : launch_pdl(logprobs_kernel<T, Plan, false>, grid, block, 0, st, 1, p);
 }
 template <typename T>
 static cudaError_t launch_logprobs(const LogprobArgs& p, cudaStream_t st) {
-    const bool top = p.k > 0;
-    if ((long long)p.V * (int)sizeof(T) <= 8192) return top ? launch_logprobs_rows<T, 128, true>(p, st) : launch_logprobs_rows<T, 128, false>(p, st);
-    if (p.T <= sm_count()) return top ? launch_logprobs_rows<T, 512, true>(p, st) : launch_logprobs_rows<T, 512, false>(p, st);
-    return top ? launch_logprobs_rows<T, 256, true>(p, st) : launch_logprobs_rows<T, 256, false>(p, st);
+    const long long row_bytes = (long long)p.V * (int)sizeof(T);
+    if (row_bytes <= 8 << 10) return launch_logprobs_as<T, ShortRow>(p, st);
+    if (p.T <= sm_count()) return launch_logprobs_as<T, LoneRow>(p, st);
+    if (row_bytes <= 64 << 10) return launch_logprobs_as<T, MiddleRow>(p, st);
+    return launch_logprobs_as<T, LongRow>(p, st);
 }
 
 int launch_token_logprobs(int T, int V, long long row_stride, int dtype, const void* logits, const int32_t* tokens, float c, int k, float* logprobs,
