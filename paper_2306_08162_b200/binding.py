@@ -408,10 +408,10 @@ def qlora_adamw(d, lr, step, norm=None, stream=None):
     where = "qlora_adamw"
     device = _check_desc(d, where)
     lr_dev = step_dev = None
-    if hasattr(lr, "data_ptr"):
+    if not isinstance(lr, float) and hasattr(lr, "data_ptr"):
         _operand(lr, _torch.float32, (1,), where)
         lr, lr_dev = 0.0, lr
-    if hasattr(step, "data_ptr"):
+    if not isinstance(step, int) and hasattr(step, "data_ptr"):
         _operand(step, _torch.int32, (1,), where)
         step, step_dev = 0, step
     _operand(norm, _torch.float32, (2,), where)

@@ -15,13 +15,9 @@ namespace qlora {
 constexpr int OP_BLOCK = 256;            // elements that share one scale of the 8-bit states, and that a warp handles at a time
 constexpr int OP_THREADS = 256;
 constexpr int OP_CHUNK = 2048;           // elements of a chunk: a block of 256 to each of 8 warps
-constexpr int OP_TABLE = 448, OP_SMALL_TABLE = 16;   // tensors per launch: their table travels in the kernel's parameters (32764 bytes at most)
-#ifndef NU
-#define NU 4
-#endif
-#ifndef NB
-#define NB 4
-#endif
+// Tensors per launch: their table travels in the kernel's parameters (32764 bytes at most), and a launch costs the host more the larger it is.
+constexpr int OP_TABLE = 448, OP_MIDDLE_TABLE = 128, OP_SMALL_TABLE = 16;
+constexpr int OP_CLUSTER = 8, OP_CLUSTER_CHUNKS = 64;
 constexpr int OP_PARTIALS = QLORA_GRAD_NORM_WORKSPACE_BYTES / sizeof(double);
 
 // The tensors of one launch, cut into chunks of OP_CHUNK elements (the last one of a tensor may be shorter): chunk c belongs to the tensor
@@ -344,19 +340,12 @@ __device__ __forceinline__ void add_squares(double& acc, const uint4& v) {
     }
 }
 
-// Sums of squares in 64 bits (a square can leave fp32's range, and HBM leaves the time), one per block of the launch, each block with a
-// stretch of the chunks (the same number to within one); `add`: on top of the previous launch's (more tensors than one table holds).
+// The sum of squares of chunks c to stop - 1, this thread's part: in 64 bits, since a square can leave fp32's range and HBM leaves the time.
 template <typename G, int CAP>
-__global__ void __launch_bounds__(OP_THREADS) grad_square_kernel(const __grid_constant__ OptTable<CAP> tab, float prescale, int add, double* __restrict__ partial) {
-    constexpr int PER = 16 / sizeof(G), UNROLL = NU;
-    pdl_launch_dependents();
-    const uint64_t chunks = tab.first[tab.n];
-    uint32_t c = (uint32_t)(chunks * blockIdx.x / gridDim.x);
-    const uint32_t stop = (uint32_t)(chunks * (blockIdx.x + 1) / gridDim.x);
-    int j = c < stop ? tensor_of_chunk(tab, c) : 0;
-    pdl_wait();
+__device__ __forceinline__ double squares_of(const OptTable<CAP>& tab, int j, uint32_t c, uint32_t stop) {
+    constexpr int PER = 16 / sizeof(G), UNROLL = 4;
     double acc = 0.0;
-    for (; c < stop; ++j) {                                          // the stretch's part of one tensor after the other
+    for (; c < stop; ++j) {                                          // the stretch's part of one tensor after the other (c lies in tensor j)
         const qlora_adamw_tensor& t = tab.t[j];
         const uint32_t next = min(stop, tab.first[j + 1]);
         const long long begin = (long long)(c - tab.first[j]) * OP_CHUNK, end = min((long long)(next - tab.first[j]) * OP_CHUNK, t.n);
@@ -375,7 +364,27 @@ __global__ void __launch_bounds__(OP_THREADS) grad_square_kernel(const __grid_co
         for (long long e = vectors * PER + threadIdx.x; e < end - begin; e += OP_THREADS) acc = fma((double)one(grad + e), (double)one(grad + e), acc);
         c = next;
     }
-    acc = block_sum(acc) * (double)prescale * (double)prescale;
+    return acc;
+}
+__device__ __forceinline__ void tell_norm(double squares, float prescale, float max_norm, float* out) {
+    const float norm = (float)(sqrt(squares) * fabs((double)prescale));
+    float f = prescale;
+    if (max_norm > 0.f && norm > max_norm) f = prescale * (max_norm / norm);
+    if (!(norm < INFINITY)) f = __int_as_float(0x7FC00000);
+    out[0] = norm;
+    out[1] = f;
+}
+
+// One partial sum to each block of the launch, which has a stretch of the chunks (the same number to within one); `add`: on top of the
+// previous launch's (more tensors than one table holds).
+template <typename G, int CAP>
+__global__ void __launch_bounds__(OP_THREADS) grad_square_kernel(const __grid_constant__ OptTable<CAP> tab, int add, double* __restrict__ partial) {
+    pdl_launch_dependents();
+    const uint64_t chunks = tab.first[tab.n];
+    const uint32_t c = (uint32_t)(chunks * blockIdx.x / gridDim.x), stop = (uint32_t)(chunks * (blockIdx.x + 1) / gridDim.x);
+    const int j = c < stop ? tensor_of_chunk(tab, c) : 0;
+    pdl_wait();
+    const double acc = block_sum(squares_of<G>(tab, j, c, stop));
     if (threadIdx.x == 0) partial[blockIdx.x] = add ? partial[blockIdx.x] + acc : acc;
 }
 
@@ -385,13 +394,28 @@ __global__ void __launch_bounds__(OP_THREADS) grad_norm_kernel(int n, const doub
     double acc = 0.0;
     for (int i = threadIdx.x; i < n; i += OP_THREADS) acc += partial[i];
     acc = block_sum(acc);
+    if (threadIdx.x == 0) tell_norm(acc, prescale, max_norm, out);
+}
+
+// Few chunks: all of it in one launch, a cluster of OP_CLUSTER blocks whose sums meet in the shared memory of the first.
+template <typename G, int CAP>
+__global__ void __launch_bounds__(OP_THREADS) grad_norm_cluster_kernel(const __grid_constant__ OptTable<CAP> tab, float prescale, float max_norm, float* __restrict__ out) {
+    __shared__ double sums[OP_CLUSTER];
+    pdl_launch_dependents();
+    const uint32_t chunks = tab.first[tab.n], c = chunks * blockIdx.x / OP_CLUSTER, stop = chunks * (blockIdx.x + 1) / OP_CLUSTER;
+    const int j = c < stop ? tensor_of_chunk(tab, c) : 0;
+    pdl_wait();
+    double acc = block_sum(squares_of<G>(tab, j, c, stop));
     if (threadIdx.x == 0) {
-        const float norm = (float)sqrt(acc);
-        out[0] = norm;
-        float f = prescale;
-        if (max_norm > 0.f && norm > max_norm) f = prescale * (max_norm / norm);
-        if (!(norm < INFINITY)) f = __int_as_float(0x7FC00000);
-        out[1] = f;
+        uint32_t at;
+        asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(&sums[blockIdx.x])));
+        asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(at), "d"(acc) : "memory");
+    }
+    asm volatile("barrier.cluster.arrive;\n\tbarrier.cluster.wait;" ::: "memory");
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        acc = 0.0;
+        for (int b = 0; b < OP_CLUSTER; ++b) acc += sums[b];
+        tell_norm(acc, prescale, max_norm, out);
     }
 }
 
@@ -422,33 +446,34 @@ static uint32_t fill_table(const qlora_adamw_desc& d, int* at, OptTable<CAP>& ta
     return chunks;
 }
 
-#ifndef NB
-#define NB 4
-#endif
-
-template <int CAP>
-static int launch_grad_norm_with(const qlora_adamw_desc& d, float prescale, float max_norm, float* out, void* workspace, cudaStream_t st) {
+template <typename G, int CAP>
+static int launch_grad_norm_as(const qlora_adamw_desc& d, float prescale, float max_norm, float* out, void* workspace, cudaStream_t st) {
     static thread_local OptTable<CAP> tab;
     double* partial = static_cast<double*>(workspace);
-    const int most = NB * sm_count() < OP_PARTIALS ? NB * sm_count() : OP_PARTIALS;
+    const int most = 4 * sm_count() < OP_PARTIALS ? 4 * sm_count() : OP_PARTIALS;
     int at = 0, used = 0;
     for (int launch = 0;; ++launch) {
         const uint32_t chunks = fill_table(d, &at, tab);
         if (chunks == 0) break;
+        if (launch == 0 && at == d.n_tensors && chunks <= OP_CLUSTER_CHUNKS)
+            return launch_pdl(grad_norm_cluster_kernel<G, CAP>, dim3(OP_CLUSTER), dim3(OP_THREADS), 0, st, OP_CLUSTER, tab, prescale, max_norm, out) == cudaSuccess ? QLORA_OK : QLORA_ERR_CUDA;
         // (every launch on the grid of the first, whose partial sums the later ones add to)
         if (launch == 0) used = (int)(chunks < (uint32_t)most ? chunks : (uint32_t)most);
-        cudaError_t err;
-        if (d.grad_type == QLORA_FP32) err = launch_pdl(grad_square_kernel<float, CAP>, dim3(used), dim3(OP_THREADS), 0, st, 1, tab, prescale, launch, partial);
-        else if (d.grad_type == QLORA_BF16) err = launch_pdl(grad_square_kernel<__nv_bfloat16, CAP>, dim3(used), dim3(OP_THREADS), 0, st, 1, tab, prescale, launch, partial);
-        else err = launch_pdl(grad_square_kernel<__half, CAP>, dim3(used), dim3(OP_THREADS), 0, st, 1, tab, prescale, launch, partial);
-        if (err != cudaSuccess) return QLORA_ERR_CUDA;
+        if (launch_pdl(grad_square_kernel<G, CAP>, dim3(used), dim3(OP_THREADS), 0, st, 1, tab, launch, partial) != cudaSuccess) return QLORA_ERR_CUDA;
     }
     return launch_pdl(grad_norm_kernel, dim3(1), dim3(OP_THREADS), 0, st, 1, used, partial, prescale, max_norm, out) == cudaSuccess ? QLORA_OK : QLORA_ERR_CUDA;
 }
+template <int CAP>
+static int launch_grad_norm_with(const qlora_adamw_desc& d, float prescale, float max_norm, float* out, void* workspace, cudaStream_t st) {
+    if (d.grad_type == QLORA_FP32) return launch_grad_norm_as<float, CAP>(d, prescale, max_norm, out, workspace, st);
+    if (d.grad_type == QLORA_BF16) return launch_grad_norm_as<__nv_bfloat16, CAP>(d, prescale, max_norm, out, workspace, st);
+    return launch_grad_norm_as<__half, CAP>(d, prescale, max_norm, out, workspace, st);
+}
 
 int launch_grad_norm(const qlora_adamw_desc& d, float prescale, float max_norm, float* out, void* workspace, cudaStream_t st) {
-    return d.n_tensors <= OP_SMALL_TABLE ? launch_grad_norm_with<OP_SMALL_TABLE>(d, prescale, max_norm, out, workspace, st)
-                                         : launch_grad_norm_with<OP_TABLE>(d, prescale, max_norm, out, workspace, st);
+    if (d.n_tensors <= OP_SMALL_TABLE) return launch_grad_norm_with<OP_SMALL_TABLE>(d, prescale, max_norm, out, workspace, st);
+    if (d.n_tensors <= OP_MIDDLE_TABLE) return launch_grad_norm_with<OP_MIDDLE_TABLE>(d, prescale, max_norm, out, workspace, st);
+    return launch_grad_norm_with<OP_TABLE>(d, prescale, max_norm, out, workspace, st);
 }
 
 template <typename P, typename G, int CAP>
@@ -486,7 +511,9 @@ int launch_adamw(const qlora_adamw_desc& d, double lr, int step, const float* lr
     sc.lr = (float)lr;
     sc.inv_corr1 = (float)(-1.0 / expm1(step * log(d.beta1))); sc.root_inv_corr2 = (float)(1.0 / sqrt(-expm1(step * log(d.beta2))));
     sc.step = step; sc.lr_dev = lr_dev; sc.step_dev = step_dev; sc.norm = norm;
-    return d.n_tensors <= OP_SMALL_TABLE ? launch_adamw_with<OP_SMALL_TABLE>(d, sc, st) : launch_adamw_with<OP_TABLE>(d, sc, st);
+    if (d.n_tensors <= OP_SMALL_TABLE) return launch_adamw_with<OP_SMALL_TABLE>(d, sc, st);
+    if (d.n_tensors <= OP_MIDDLE_TABLE) return launch_adamw_with<OP_MIDDLE_TABLE>(d, sc, st);
+    return launch_adamw_with<OP_TABLE>(d, sc, st);
 }
 
 }  // namespace qlora
