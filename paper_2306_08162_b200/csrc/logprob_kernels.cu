@@ -435,11 +435,18 @@ __device__ __forceinline__ int span_of(int vectors) {                    // log2
     return rounds <= SEGMENTS ? 0 : 32 - __clz((rounds - 1) / SEGMENTS);
 }
 
-// How a row is shared out.  KEEP: the row stays in L1 for the second look at it.
-struct ShortRow { static constexpr int THREADS = 128, SEGMENTS = 1, PER_SM = 10; static constexpr bool KEEP = true; };      // up to 8 KB: one round
-struct MiddleRow { static constexpr int THREADS = 256, SEGMENTS = 4, PER_SM = 6; static constexpr bool KEEP = true; };      // up to 64 KB
+// How a row is shared out.  What a row costs beside its logits goes with the warps that share it, so they are as few as its length allows:
+//                                      64 threads    128 threads    256 threads
+//   8192 rows of 4000 bf16, k = 5         26 us         35 us           -
+//   4000 rows of 10000, k = 20             -            28 us          38 us
+//   2048 rows of 32000, k = 32             -            53 us          37 us       (fewer warps than hide the loads' latency)
+// and 512 where there is an SM for every row (one row of 32000, k = 20: 6.4 us, with 256 threads 6.6).  KEEP: the row stays in L1 for the second look at
+// it (2048 rows of 32000, k = 32: 36.9 us, without 39.3; rows of 200 KB: 48 us, without 45).
+struct TinyRow { static constexpr int THREADS = 64, SEGMENTS = 8, PER_SM = 20; static constexpr bool KEEP = true; };
+struct ShortRow { static constexpr int THREADS = 128, SEGMENTS = 4, PER_SM = 10; static constexpr bool KEEP = true; };
+struct MiddleRow { static constexpr int THREADS = 256, SEGMENTS = 4, PER_SM = 6; static constexpr bool KEEP = true; };
 struct LongRow { static constexpr int THREADS = 256, SEGMENTS = 16, PER_SM = 6; static constexpr bool KEEP = false; };
-struct LoneRow { static constexpr int THREADS = 512, SEGMENTS = 8, PER_SM = 1; static constexpr bool KEEP = true; };        // no more rows than SMs
+struct LoneRow { static constexpr int THREADS = 512, SEGMENTS = 8, PER_SM = 1; static constexpr bool KEEP = true; };
 
 template <typename T, typename Plan, bool TOP>
 __global__ void __launch_bounds__(Plan::THREADS, Plan::PER_SM) logprobs_kernel(const __grid_constant__ LogprobArgs p) {
@@ -636,8 +643,11 @@ static cudaError_t launch_logprobs_as(const LogprobArgs& p, cudaStream_t st) {
 template <typename T>
 static cudaError_t launch_logprobs(const LogprobArgs& p, cudaStream_t st) {
     const long long row_bytes = (long long)p.V * (int)sizeof(T);
-    if (row_bytes <= 8 << 10) return launch_logprobs_as<T, ShortRow>(p, st);
-    if (p.T <= sm_count()) return launch_logprobs_as<T, LoneRow>(p, st);
+    const int sms = sm_count();
+    // (64 threads: their 64 maxima bound up to 32 alternatives well, and it takes more rows than 20 blocks an SM to gain)
+    if (row_bytes <= 8 << 10 && p.k <= 32 && p.T > 20 * sms) return launch_logprobs_as<T, TinyRow>(p, st);
+    if (row_bytes <= 8 << 10 || (row_bytes <= 32 << 10 && p.T > sms)) return launch_logprobs_as<T, ShortRow>(p, st);
+    if (p.T <= sms) return launch_logprobs_as<T, LoneRow>(p, st);
     if (row_bytes <= 64 << 10) return launch_logprobs_as<T, MiddleRow>(p, st);
     return launch_logprobs_as<T, LongRow>(p, st);
 }

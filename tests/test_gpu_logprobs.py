@@ -73,7 +73,8 @@ def check_forward(z, tokens, c, k):
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
 @pytest.mark.parametrize("T,V,k", [(1, 1, 1), (1, 32000, 20), (3, 7, 7), (2, 8, 0), (5, 255, 64), (2, 256, 1), (1, 257, 5), (4, 1000, 32), (9, 4097, 20),
                                    (150, 2053, 3), (17, 32000, 5), (2, 50021, 64), (1, 128000, 20), (300, 515, 33), (40, 16001, 64),
-                                   (2500, 70, 7), (1900, 1031, 20), (1300, 8200, 64), (1000, 10007, 0)])
+                                   (2500, 70, 7), (1900, 1031, 20), (1300, 8200, 64), (1000, 10007, 0),
+                                   (3001, 331, 32), (6100, 70, 1), (160, 20011, 64), (1000, 16390, 31)])
 def test_rows_of_every_length(T, V, k, dtype):
     z, tokens = make(T, V, dtype, seed=T + V + k)
     if T > 2:
