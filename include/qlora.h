@@ -230,7 +230,7 @@ int qlora_token_logprobs(int T, int V, long long row_stride, int dtype, const vo
  * NULL (tokens too, where d_logprobs is).  A row whose token is outside [0, V) takes no d_logprobs.  A row without a
  * gradient (both zero) gets zeros, whatever its logits and stats hold.  dlogits: the type of logits, [T, V] with rows
  * grad_stride >= V elements apart (what lies between the rows is left as it was); may be the logits themselves
- * (same address and stride), must not overlap them otherwise. */
+ * (same address and stride); any other overlap of the two is refused. */
 int qlora_token_logprobs_bwd(int T, int V, long long row_stride, int dtype, const void* logits, const int32_t* tokens,
                              float inv_temperature, const float* stats, const float* d_logprobs, const float* d_entropy,
                              long long grad_stride, void* dlogits, void* cuda_stream);

@@ -48,6 +48,16 @@ int check_logits(int T, int V, long long row_stride, int dtype, float inv_temper
     return QLORA_OK;
 }
 
+// Whether two [T, V] tensors of rows that lie apart share memory.  (Different strides in the same stretch of memory: taken to.)
+bool rows_overlap(const void* a, long long stride_a, const void* b, long long stride_b, int T, int V, size_t bytes) {
+    const long long pa = (long long)reinterpret_cast<uintptr_t>(a), pb = (long long)reinterpret_cast<uintptr_t>(b), size = (long long)bytes;
+    const long long end_a = pa + ((T - 1) * stride_a + V) * size, end_b = pb + ((T - 1) * stride_b + V) * size;
+    if (end_a <= pb || end_b <= pa) return false;
+    if (T == 1 || stride_a != stride_b) return true;
+    const long long by = (pb > pa ? pb - pa : pa - pb) % (stride_a * size);   // (columns of one buffer may lie beside each other)
+    return by < V * size || stride_a * size - by < V * size;
+}
+
 // `step`: the whole step (else only the gradients are used).
 int check_adamw(const qlora_adamw_desc* d, bool step) {
     if (d == nullptr || d->n_tensors < 0 || (d->n_tensors > 0 && d->tensors == nullptr)) return QLORA_ERR_INVALID_ARG;
@@ -196,7 +206,8 @@ int qlora_token_logprobs_bwd(int T, int V, long long row_stride, int dtype, cons
     if (T > 1 && grad_stride < V) return QLORA_ERR_INVALID_ARG;
     if (T == 0) return QLORA_OK;
     if (!logits || !stats || !dlogits || (!d_logprobs && !d_entropy) || (d_logprobs && !tokens)) return QLORA_ERR_INVALID_ARG;
-    if (logits == dlogits && T > 1 && row_stride != grad_stride) return QLORA_ERR_INVALID_ARG;
+    const bool in_place = logits == dlogits && (T == 1 || row_stride == grad_stride);
+    if (!in_place && rows_overlap(logits, row_stride, dlogits, grad_stride, T, V, element_bytes(dtype))) return QLORA_ERR_INVALID_ARG;
     if (!element_aligned(logits, dtype) || !element_aligned(dlogits, dtype) || !aligned16(tokens) || !aligned16(stats) ||
         !aligned16(d_logprobs) || !aligned16(d_entropy))
         return QLORA_ERR_ALIGNMENT;

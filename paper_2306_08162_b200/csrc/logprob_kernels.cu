@@ -2,6 +2,13 @@
 // respect to the logits.  Per row, with c the inverse temperature, m = max z and d_j = c (z_j - m) <= 0:
 //     s = sum exp d_j,    log p_j = d_j - log s,    H = log s - (sum exp(d_j) d_j) / s
 // in one pass over the row: every thread keeps its own maximum and sums relative to it and corrects them when the maximum moves.
+// Bound by HBM in the long run (2 bytes a bf16 logit: 16000 rows of 32000 in 156 us, the time of a copy of as many bytes), by the beginning and end of the
+// launch where it is short (888 rows, all that run at a time: 13.7 us, each 888 more: 9.0; 2048 rows: 25.9 us, 5.1 TB/s) and by instructions where there are
+// alternatives (k = 32: 36.9 us; 4096 rows of 128000, k = 20: 184 us, 5.7 TB/s).  A logit takes 1 exponential of the special-function unit, whose 16 a
+// clock and SM are 57 % busy at 5.1 TB/s, and some 4.5 other instructions: maximum and clamp of two bf16 at once, a fused multiply-add, two sums in pairs.
+// The alternatives cost no sorting: see offer_bound.
+// Timed and taken out: blocks that stay, with a ring of copies ahead in shared memory (2048 x 32000: 27 - 35 us: fewer warps fit); clusters that share a
+// row (one token, k = 20: 8.6 us on 8 blocks, 6.1 on one); the next round's loads ahead of the sums (26.7 us); 512 or 1024 threads to a row (28, 52 us).
 #include "common.cuh"
 #include "device_state.h"
 #include "f32x2.cuh"
@@ -10,7 +17,7 @@
 namespace qlora {
 
 constexpr int LP_UNROLL = 4;             // 16-byte vectors that a thread has on their way at a time
-constexpr int LP_CANDIDATES = 640;       // entries that are put in order together (a part of less than 64 vectors has fewer logits)
+constexpr int LP_CANDIDATES = 640;       // entries that are put in order together (a row of less than 64 vectors has fewer logits)
 constexpr int LP_HITS = 64;              // stretches that a warp looks at again
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float LP_FLOOR = -0x1p96f, LP_LEAST = -0x1p80f, LP_MOST = 0x1p60f;     // see RowSums
@@ -97,6 +104,7 @@ struct RowParts {
     __device__ __forceinline__ const uint4* body() const { return reinterpret_cast<const uint4*>(z + head); }
 };
 
+// 16 bytes that are read once.  asm volatile: several loads stay ahead of their uses.
 template <bool KEEP = false>
 __device__ __forceinline__ uint4 load_stream(const uint4* p) {          // KEEP: in L1, for a second look
     uint4 v;
@@ -150,7 +158,7 @@ __device__ __forceinline__ RowSums warp_merge(RowSums x, float kd) {
 }
 
 // log s and the entropy of a row whose maximum m is finite but too large or too small for the sums above (a row masked by the type's lowest value
-// altogether, say): the differences to m themselves, by the whole block, in two passes.
+// altogether, say): from the differences to m themselves, by the whole block.
 template <typename T, int THREADS>
 __device__ __noinline__ void odd_row(const T* z, int V, float m, float c, float* sums, float& logs, float& H) {
     float s = 0.f, a = 0.f;
@@ -217,7 +225,7 @@ struct ThreadRow {
     }
 };
 
-// Calls f(key, place) for this thread's logits of the part of the row (the same ones as in thread_sums) whose key is at least `least`.
+// Calls f(key, place) for this thread's logits whose key is at least `least`.
 template <typename T, int THREADS, typename F>
 __device__ __forceinline__ void each_from(const RowParts<T>& row, uint32_t least, F f) {
     const uint4* body = row.body();
@@ -257,7 +265,7 @@ template <int THREADS, int SEGMENTS> struct TopWarps {
     int hit[THREADS / 32][LP_HITS];         // stretches with a candidate, by their first vector
 };
 
-// How many logits of the part have a key of at least `least` (the same in every thread).
+// How many logits of the row have a key of at least `least` (the same in every thread).
 template <typename T, int THREADS>
 __device__ __noinline__ int count_from(const RowParts<T>& row, uint32_t least, TopShared& sh) {
     int n = 0;
@@ -271,8 +279,8 @@ __device__ __noinline__ int count_from(const RowParts<T>& row, uint32_t least, T
     return sh.count;
 }
 
-// More candidates than there is room for (many equal logits, or large ones in a cluster): the kk-th largest key itself, found bit by bit
-// with a pass over the row each, then everything above it and, in the order of their places, as many equals as are wanted.
+// More candidates than there is room for (many equal logits, as where fewer than kk are unmasked, or large ones close together): the kk-th largest key
+// itself, halving what is left by a pass over the row each time, then everything above it and, in the order of their places, as many equals as are wanted.
 template <typename T, int THREADS>
 __device__ __noinline__ int crowded(const RowParts<T>& row, int n, int kk, uint32_t bound, TopShared& sh) {
     uint32_t lo = bound, hi = 0xFFFFFFFFu;                          // at least kk keys are >= lo
@@ -307,14 +315,14 @@ __device__ __noinline__ int crowded(const RowParts<T>& row, int n, int kk, uint3
     return kk;
 }
 
-// Before the block waits: this warp's share of the bound.  At least kk logits of the part are as large as the smallest of the warps' q-th
-// largest lane maxima, q = kk / warps, and not many more are (256 threads and kk = 20: some 50 in the mean).  `top`: the maximum of this thread's
-// logits.  Warps that lack logits stay out of it.
+// The alternatives.  At least kk logits of the row are as large as the smallest of the warps' q-th largest lane maxima, q = kk / warps rounded up, and not many
+// more are (256 threads and kk = 20: some 50 in the mean), so these are found again and put in order, and nothing else is done for the others.
+// Here, before the block waits: this warp's share of that bound.  `top`: the maximum of this thread's logits.  Warps that lack logits stay out of it.
 template <int THREADS>
 __device__ __forceinline__ void offer_bound(int vectors, int kk, float top, TopShared& sh) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = min(THREADS / 32, vectors / 32);
     uint32_t key = order_key(top), least = 0xFFFFFFFFu;
-    if (warps * 32 < kk) least = 0;                                  // (a short part: everything is a candidate)
+    if (warps * 32 < kk) least = 0;                                  // (a short row: everything is a candidate)
     else if (warp < warps)
         for (int q = 0; q < kk; q += warps) {
             least = __reduce_max_sync(0xFFFFFFFFu, key);
@@ -324,9 +332,8 @@ __device__ __forceinline__ void offer_bound(int vectors, int kk, float top, TopS
     if (threadIdx.x == 0) sh.count = 0;
 }
 
-// After it: the entries of the block's part of the row from the bound on.  Only warps whose logits reach it look at some of them again, which by now are in L2.
-// `segment`: the maxima of this warp's stretches; `hit`: LP_HITS places of this warp's own; `ends`: the logits at this thread's places of
-// the head and of the rest.
+// After it: the entries from the bound on.  Each warp looks again at the stretches of its own lanes that reach it; their logits are in L1 or L2 by now.
+// `segment`: the maxima of the stretches; `hit`: LP_HITS places of this warp's own; head, rest: the logits at this thread's places there.
 template <typename T, int THREADS>
 __device__ __forceinline__ void gather(const RowParts<T>& row, uint32_t bound, int span_log2, const float* segment, int* hit, float head, float rest, TopShared& sh) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -348,11 +355,10 @@ __device__ __forceinline__ void gather(const RowParts<T>& row, uint32_t bound, i
         if (at < LP_CANDIDATES) sh.cand[at] = entry_key(k, j);
     };
     const uint4* body = row.body();
-    constexpr int UL = LP_UNROLL == 4 ? 2 : LP_UNROLL == 2 ? 1 : 3;
-    static_assert(1 << UL == LP_UNROLL, "a round of vectors is a power of two");
+    static_assert(LP_UNROLL == 4, "the vectors of a stretch are a power of two");
     const float least = key_logit(bound);
-    for (int w = lane; w < hits << (span_log2 + UL); w += 32) {
-        const int at = hit[w >> (span_log2 + UL)] + (w & ((LP_UNROLL << span_log2) - 1)) * THREADS;
+    for (int w = lane; w < hits << (span_log2 + 2); w += 32) {
+        const int at = hit[w >> (span_log2 + 2)] + (w & ((LP_UNROLL << span_log2) - 1)) * THREADS;
         if (at >= row.vectors) continue;
         const uint4 v = body[at];
         uint32_t found = 0;                                          // (a NaN is; one that is not, if the bound is NaN, falls out below)
@@ -405,7 +411,7 @@ struct LogprobArgs {
     int32_t* top_ids;
 };
 
-// What is told about a row, by one thread that has its sums; `found` receives what the alternatives need.
+// What one thread that has a row's sums tells about it; the result is what the alternatives need.
 struct RowResult {
     float m, logs;
     int none;
@@ -414,7 +420,7 @@ __device__ __forceinline__ RowResult tell_row(const LogprobArgs& p, int row, Row
     const bool none = x.m == -INFINITY;
     if (!odd) {
         const float ln_s = logf(x.s);
-        logs = fmaf(fmaf(-x.m, kd, reference(x.m, kd)), kLn2, ln_s);
+        logs = fmaxf(fmaf(fmaf(-x.m, kd, reference(x.m, kd)), kLn2, ln_s), 0.f);   // (a sum relative to the maximum is at least 1)
         H = fmaxf(ln_s - kLn2 * (x.a / x.s), 0.f);
         if (none) { logs = -INFINITY; H = 0.f; }
         if (!(x.m < INFINITY)) x.m = logs = H = __int_as_float(0x7FC00000);

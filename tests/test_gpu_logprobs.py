@@ -242,6 +242,16 @@ def test_gradient_in_place_and_into_other_rows(dtype):
     assert torch.equal(z, kept)
 
 
+def test_gradient_beside_the_logits_in_one_buffer():
+    V = 777
+    buf = torch.full((50, 1600), 3.0, dtype=torch.bfloat16, device="cuda")
+    z, out = buf[:, 8:8 + V], buf[:, 808:808 + V]
+    z.copy_(torch.randn((50, V), device="cuda"))
+    kept = z.clone()
+    check_backward(z, torch.arange(50, dtype=torch.int32, device="cuda"), 1.0, torch.ones(50, device="cuda"), None, out=out)
+    assert torch.equal(z, kept) and (buf[:, :8] == 3).all() and (buf[:, 785:808] == 3).all() and (buf[:, 1585:] == 3).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
 def test_gradient_of_masked_and_broken_rows(dtype):
     """Masked entries have none; a row with nothing left, or without a gradient, is zeros whatever it holds; a broken one is NaN."""

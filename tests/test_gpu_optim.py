@@ -1,8 +1,9 @@
 """Parity of the gradients' norm and the AdamW step with the 64-bit oracle (needs a B200).
 
-Tolerances (u = 2^-24).  Moments: two products and a sum in fp32, at most 4u of the larger term's size; the update has at most 24u of its own size
-(two products, square root, division, reciprocal approximations of 2^-22), its weight decay 4u of the weight; the weight is then rounded
-once to its type (half a step).  8-bit states are compared by what they stand for: within one step of the unrounded moment, and equal to the
+Tolerances (u = 2^-24).  Moments: m = (beta1 s) code + (1 - beta1) (f g), every product rounded (at most three roundings a term, beta and scale included)
+and the sum once: at most 4u of |beta1 m| + |(1 - beta1) f g|, which can be far above |m| where the two cancel.  The update is m times
+lr / (1 - beta1^step) / (sqrt + eps): it carries that error along and adds at most 24u of its own size (two products, square root, division, reciprocal
+approximations of 2^-22), its weight decay 4u of the weight; the weight is then rounded once to its type (half a step).  8-bit states are compared by what they stand for: within one step of the unrounded moment, and equal to the
 oracle's codes but for a share of 2^-10 (a code can go the other way where the dither lies within the fp32 error of the value's share)."""
 import numpy as np
 import pytest
@@ -65,21 +66,26 @@ class Model:
         return m * np.repeat(to_f64(self.m_scale[j]), 256)[:n], (v * np.repeat(to_f64(self.v_scale[j]), 256)[:n]) ** 2
 
     def expected(self, step, lr, factor=1.0):
-        h = self.hyper
-        return [orc.adamw_step(to_f64((self.master or self.param)[j]), to_f64(self.grad[j]), *self.held(j), step, lr, h["beta1"], h["beta2"], h["eps"],
-                               h["weight_decay"], factor) for j in range(len(self.sizes))]
+        """(w, m, v) after the step, and what the terms of m alone would move w by (the size that rounding errors of m are relative to)."""
+        h, out = self.hyper, []
+        for j in range(len(self.sizes)):
+            g, (m, v) = to_f64(self.grad[j]), self.held(j)
+            stepped = orc.adamw_step(to_f64((self.master or self.param)[j]), g, m, v, step, lr, h["beta1"], h["beta2"], h["eps"], h["weight_decay"], factor)
+            terms = h["beta1"] * np.abs(m) + (1 - h["beta1"]) * np.abs(factor * g)
+            out.append((*stepped, lr * terms / (1 - h["beta1"] ** step) / (np.sqrt(stepped[2] / (1 - h["beta2"] ** step)) + h["eps"])))
+        return out
 
     def check(self, want, before, step, lr):
         torch.cuda.synchronize()
         for raw, shape, dtype in self.raw:
             assert canaries_intact(raw, shape, dtype), "write outside a tensor"
-        for j, (w, m, v) in enumerate(want):
+        for j, (w, m, v, terms) in enumerate(want):
             n = self.sizes[j]
             if n == 0:
                 continue
             old = before[j]
             update = np.abs(w - old * (1 - lr * self.hyper["weight_decay"]))
-            tol = 24 * U * update + 4 * U * np.abs(old) + 1e-30
+            tol = 24 * U * update + 4 * U * terms + 4 * U * np.abs(old) + 1e-30
             if self.master is not None:
                 got = to_f64(self.master[j])
                 assert (np.abs(got - w) <= tol).all()
@@ -89,8 +95,8 @@ class Model:
                 assert (np.abs(to_f64(self.param[j]) - w) <= tol + info.eps / 2 * (np.abs(w) + tol) + info.tiny * info.eps).all()
             gm, gv = self.held(j)
             if self.bits == 32:
-                g = np.abs(to_f64(self.grad[j]))
-                assert (np.abs(gm - m) <= 4 * U * (np.abs(m) + g)).all() and (np.abs(gv - v) <= 8 * U * v + 1e-44).all()
+                g = np.abs(to_f64(self.grad[j]))                     # (|beta1 m| + |(1 - beta1) g| is below |m| + 2 |g|)
+                assert (np.abs(gm - m) <= 4 * U * (np.abs(m) + 2 * g)).all() and (np.abs(gv - v) <= 8 * U * v + 1e-44).all()
                 continue
             place = np.arange(n)
             for got, scale, x, r, root in ((self.m[j], self.m_scale[j], m, 0, False), (self.v[j], self.v_scale[j], np.sqrt(v), 1, True)):

@@ -43,8 +43,14 @@ def test_token_logprobs_bwd_arguments(ql):
     assert status(V=0) == -2 and status(dtype=3) == -2
     assert status(logits=None) == -1 and status(stats=None) == -1 and status(out=None) == -1 and status(tokens=None) == -1
     assert status(gl=None) == -1                                            # no gradient at all
-    assert status(ld=128, out=OK) == -1                                     # in place, at another stride
-    assert status(out=OK + 1) == -3 and status(dtype=2, logits=OK + 2) == -3 and status(gl=OK + 4) == -3
+    # over the logits in part: at another stride, a row further, a few columns further, over the last row's end
+    big = 1 << 20
+    assert status(ld=128, out=OK) == -1 and status(logits=big, out=big + 200) == -1 and status(logits=big, out=big + 16) == -1
+    assert status(logits=big, ld=256, gld=256, out=big + 2 * (256 + 99)) == -1 and status(logits=big, ld=256, gld=256, out=big - 2 * 99) == -1
+    assert status(logits=big, ld=128, gld=300, out=big - 2 * (3 * 300 + 99)) == -1 and status(T=1, logits=big, out=big + 198) == -1
+    # beside them in one buffer, or right behind: nothing wrong with that (what is refused, later on, is an address)
+    assert status(logits=big, ld=256, gld=256, out=big + 2 * 128, gl=OK + 4) == -3 and status(logits=big, out=big + 2 * 400, gl=OK + 4) == -3
+    assert status(out=2 * OK + 1) == -3 and status(dtype=2, logits=OK + 2) == -3 and status(gl=OK + 4) == -3
     assert status(T=0, logits=None) == 0
 
 
