@@ -343,28 +343,23 @@ def adamw_desc(params, grads, m, v, master=None, m_scale=None, v_scale=None, bet
         raise ValueError(f"{where}: fp32 parameters have no master weights")
     sizes = [t.numel() for t in lists["param"]]
     blocks = [-(-size // 256) for size in sizes]
-    device = lists["param"][0].get_device()
-    array = (_AdamwTensor * n)()
-    written, read, foreign = [], [], device < 0
+    columns, written, read, devices = {}, [], [], set()
     for name, ts in lists.items():
         kind = {"param": d.param_type, "grad": d.grad_type, "m": d.state_type, "v": d.state_type}.get(name, 2)
-        dtype, ranges = ts[0].dtype, read if name == "grad" else written
-        if _TYPES.get(dtype) != kind:
-            raise ValueError(f"{where}: {dtype} is not supported as {name} here")
-        for j, (t, size) in enumerate(zip(ts, blocks if name.endswith("_scale") else sizes)):
-            if t.dtype is not dtype:
-                raise ValueError(f"{where}: {t.dtype} is not supported here: {name}[0] is {dtype}")
-            if t.numel() != size:
-                raise ValueError(f"{where}: {name}[{j}] has {t.numel()} elements for a parameter of {sizes[j]}")
-            if not t.is_contiguous():
-                raise ValueError(f"{where}: tensors must be contiguous (dense)")
-            foreign = foreign or t.get_device() != device
-            at = t.data_ptr()
-            setattr(array[j], name, at)
-            if size:
-                ranges.append((at, at + size * t.element_size()))
-    for j, size in enumerate(sizes):
-        array[j].n = size
+        wanted = blocks if name.endswith("_scale") else sizes
+        for dtype in {t.dtype for t in ts}:
+            if _TYPES.get(dtype) != kind:
+                raise ValueError(f"{where}: {dtype} is not supported as {name} here (one call, one type)")
+        found = [t.numel() for t in ts]
+        if found != wanted:
+            j = next(j for j in range(n) if found[j] != wanted[j])
+            raise ValueError(f"{where}: {name}[{j}] has {found[j]} elements for a parameter of {sizes[j]}")
+        if not all(t.is_contiguous() for t in ts):
+            raise ValueError(f"{where}: tensors must be contiguous (dense)")
+        columns[name] = at = [t.data_ptr() for t in ts]
+        bytes_each = ts[0].element_size()
+        (read if name == "grad" else written).extend((a, a + size * bytes_each) for a, size in zip(at, found) if size)
+        devices.update(t.get_device() for t in ts)
     written.sort()
     for (_, end), (begin, _) in zip(written, written[1:]):
         if begin < end:
@@ -373,9 +368,13 @@ def adamw_desc(params, grads, m, v, master=None, m_scale=None, v_scale=None, bet
         at = bisect.bisect_left(written, (end,))                      # the last written range that begins before this one ends
         if at > 0 and written[at - 1][1] > begin:
             raise ValueError(f"{where}: a gradient overlaps a tensor that the step writes")
-    if foreign:
+    if len(devices) != 1 or min(devices) < 0:
         raise ValueError(f"{where}: tensors must be on one CUDA device")
-    d.tensors, d.device = array, device
+    # the structures' fields in order, all of them 64 bits wide
+    none = [0] * n
+    fields = [columns.get(name, none) for name, _ in _AdamwTensor._fields_[:-1]] + [sizes]
+    array = (ctypes.c_longlong * (len(fields) * n))(*(value for tensor in zip(*fields) for value in tensor))
+    d.tensors, d.device = ctypes.cast(array, ctypes.POINTER(_AdamwTensor)), devices.pop()
     d.keep = (array, lists)
     return d
 
