@@ -46,6 +46,7 @@ template <> struct Vec<float> {
         return make_f2(fmaxf(lo_of(p), LP_FLOOR), fmaxf(hi_of(p), LP_FLOOR));
     }
     static __device__ __forceinline__ f2 pair(const uint4& v, int i) { return i == 0 ? make_f2(__uint_as_float(v.x), __uint_as_float(v.y)) : make_f2(__uint_as_float(v.z), __uint_as_float(v.w)); }
+    static __device__ __forceinline__ float element(const uint4& v, int i) { return __uint_as_float((i & 2) != 0 ? ((i & 1) != 0 ? v.w : v.z) : ((i & 1) != 0 ? v.y : v.x)); }
     typedef float Max;
     static __device__ __forceinline__ Max lowest() { return -INFINITY; }
     static __device__ __forceinline__ Max fold(Max m, const uint4& v) {
@@ -57,6 +58,10 @@ template <> struct Vec<__nv_bfloat16> {
     static constexpr int N = 8;
     static __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
     static __device__ __forceinline__ f2 pair(const uint4& v, int i) { return unpack_bf16(word(v, i)); }
+    static __device__ __forceinline__ float element(const uint4& v, int i) {
+        const uint32_t w = word(v, i >> 1);
+        return (i & 1) != 0 ? bf16_hi(w) : bf16_lo(w);
+    }
     typedef __nv_bfloat162 Max;
     static __device__ __forceinline__ f2 above_floor(const uint4& v, int i) {            // (both at once, as they lie in memory)
         const Max m = __hmax2(of(word(v, i)), __float2bfloat162_rn(LP_FLOOR));
@@ -77,6 +82,7 @@ template <> struct Vec<__half> {
         const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
         return make_f2(f.x, f.y);
     }
+    static __device__ __forceinline__ float element(const uint4& v, int i) { return __half2float(__ushort_as_half((unsigned short)(word(v, i >> 1) >> (16 * (i & 1))))); }
     static __device__ __forceinline__ f2 above_floor(const uint4& v, int i) {
         const f2 p = pair(v, i);
         return make_f2(fmaxf(lo_of(p), LP_FLOOR), fmaxf(hi_of(p), LP_FLOOR));
@@ -148,13 +154,18 @@ __device__ __forceinline__ void add_one(RowSums& x, float z, float kd) {
     x.s += e;
     x.a = fmaf(e, y, x.a);
 }
-// Sums of a warp's lanes, the same in all of them.
-__device__ __forceinline__ RowSums warp_merge(RowSums x, float kd) {
-    float m = x.m;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+// The largest of a warp's values, NaN if one of them is (one reduction of whole numbers instead of five exchanges).
+__device__ __forceinline__ float warp_max_nan(float m) { return key_logit(__reduce_max_sync(0xFFFFFFFFu, order_key(m))); }
+// Sums over LANES lanes of a warp that are next to each other, relative to their common maximum m, the same in all of them.
+template <int LANES>
+__device__ __forceinline__ RowSums merged(RowSums x, float m, float kd) {
     rebase(x, m, kd);
-    return RowSums{m, warp_sum(x.s), warp_sum(x.a)};
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) {
+        x.s += __shfl_xor_sync(0xFFFFFFFFu, x.s, o);
+        x.a += __shfl_xor_sync(0xFFFFFFFFu, x.a, o);
+    }
+    return x;
 }
 
 // log s and the entropy of a row whose maximum m is finite but too large or too small for the sums above (a row masked by the type's lowest value
@@ -177,8 +188,7 @@ __device__ __noinline__ void odd_row(const T* z, int V, float m, float c, float*
     H = fmaxf(logs - a / s, 0.f);
 }
 
-// This thread's part of a row, LP_UNROLL vectors (a round) at a time.  TOP: the maximum of each stretch of 2^span_log2 rounds goes to
-// segment[stretch * THREADS + thread].
+// This thread's part of a row, LP_UNROLL vectors (a round) at a time.  TOP: the maximum of each stretch of 2^span_log2 rounds goes to segment[stretch].
 template <typename T, int THREADS, bool TOP>
 struct ThreadRow {
     RowSums x;
@@ -197,8 +207,7 @@ struct ThreadRow {
         if (TOP) {
             stretch = max_nan(stretch, here);
             if (--left == 0) {
-                segment[threadIdx.x] = stretch;
-                segment += THREADS;
+                *segment++ = stretch;
                 stretch = -INFINITY;
                 left = span;
             }
@@ -221,7 +230,7 @@ struct ThreadRow {
         x.a = lo_of(a2) + hi_of(a2);
     }
     __device__ __forceinline__ void finish() {
-        if (TOP && left != span) segment[threadIdx.x] = stretch;
+        if (TOP && left != span) *segment = stretch;
     }
 };
 
@@ -257,11 +266,12 @@ __device__ __forceinline__ void each_from(const RowParts<T>& row, uint32_t least
 
 struct alignas(16) TopShared {              // (the candidates are read two at a time)
     uint64_t cand[LP_CANDIDATES];        // entries that may be among the largest
-    uint32_t bound[32];                  // by warp
+    uint32_t bound[32], next[32];        // by warp
     int count, in_warp[32];
 };
-template <int THREADS, int SEGMENTS> struct TopWarps {
-    float segment[SEGMENTS * THREADS];       // maxima of the threads' stretches
+template <int THREADS, int SEGMENTS> struct alignas(16) TopWarps {
+    static constexpr int STRIDE = SEGMENTS == 4 ? 4 : SEGMENTS + 4;          // (16 bytes at a time, and fewer in the same bank)
+    float segment[THREADS * STRIDE];         // maxima of the threads' stretches
     int hit[THREADS / 32][LP_HITS];         // stretches with a candidate, by their first vector
 };
 
@@ -315,90 +325,126 @@ __device__ __noinline__ int crowded(const RowParts<T>& row, int n, int kk, uint3
     return kk;
 }
 
-// The alternatives.  At least kk logits of the row are as large as the smallest of the warps' q-th largest lane maxima, q = kk / warps rounded up, and not many
-// more are (256 threads and kk = 20: some 50 in the mean), so these are found again and put in order, and nothing else is done for the others.
-// Here, before the block waits: this warp's share of that bound.  `top`: the maximum of this thread's logits.  Warps that lack logits stay out of it.
+// The alternatives.  kk = q warps + r: at least kk logits of the row are as large as both the smallest of the warps' q-th largest lane maxima and the r-th largest
+// of their next ones, and not many more are (256 threads and kk = 20: some 40 in the mean), so these are found again and put in order, and nothing else
+// is done for the others.
+// Here, before the block waits: what this warp gives to that bound.  `top`: the maximum of this thread's logits.  Warps that lack logits stay out of it.
 template <int THREADS>
 __device__ __forceinline__ void offer_bound(int vectors, int kk, float top, TopShared& sh) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = min(THREADS / 32, vectors / 32);
-    uint32_t key = order_key(top), least = 0xFFFFFFFFu;
+    uint32_t key = order_key(top), least = 0xFFFFFFFFu, next = 0;
     if (warps * 32 < kk) least = 0;                                  // (a short row: everything is a candidate)
-    else if (warp < warps)
-        for (int q = 0; q < kk; q += warps) {
-            least = __reduce_max_sync(0xFFFFFFFFu, key);
+    else if (warp < warps) {
+        for (int q = kk; q > 0; q -= warps) {
+            next = __reduce_max_sync(0xFFFFFFFFu, key);
+            if (q < warps) break;                                    // (r more from one warp or another)
+            least = next;
             if (lane == __ffs(__ballot_sync(0xFFFFFFFFu, key == least)) - 1) key = 0;
         }
-    if (lane == 0) sh.bound[warp] = least;
+    }
+    if (lane == 0) {
+        sh.bound[warp] = least;
+        sh.next[warp] = next;
+    }
     if (threadIdx.x == 0) sh.count = 0;
+}
+template <int THREADS>
+__device__ __forceinline__ uint32_t common_bound(int vectors, int kk, const TopShared& sh) {
+    const int lane = threadIdx.x & 31, warps = min(THREADS / 32, vectors / 32);
+    uint32_t bound = __reduce_min_sync(0xFFFFFFFFu, sh.bound[lane & (THREADS / 32 - 1)]);
+    if (warps * 32 < kk) return bound;
+    uint32_t next = lane < warps ? sh.next[lane] : 0, r_th = 0xFFFFFFFFu;
+    for (int r = kk % warps; r > 0; --r) {
+        r_th = __reduce_max_sync(0xFFFFFFFFu, next);
+        if (lane == __ffs(__ballot_sync(0xFFFFFFFFu, next == r_th)) - 1) next = 0;
+    }
+    return min(bound, r_th);
 }
 
 // After it: the entries from the bound on.  Each warp looks again at the stretches of its own lanes that reach it; their logits are in L1 or L2 by now.
-// `segment`: the maxima of the stretches; `hit`: LP_HITS places of this warp's own; head, rest: the logits at this thread's places there.
-template <typename T, int THREADS>
-__device__ __forceinline__ void gather(const RowParts<T>& row, uint32_t bound, int span_log2, const float* segment, int* hit, float head, float rest, TopShared& sh) {
+// `segment`: the maxima of this thread's stretches; `hit`: LP_HITS places of this warp's own; head, rest: the logits at this thread's places there.
+// meanwhile(): work of the warp that does not depend on the loads.
+template <typename T, int THREADS, int SEGMENTS, typename F>
+__device__ __forceinline__ void gather(const RowParts<T>& row, uint32_t bound, int span_log2, const float* segment, int* hit, float head, float rest, TopShared& sh, F meanwhile) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int hits = 0;
-    for (int g = 0, c0 = warp * 32; c0 < row.vectors; ++g, c0 += (LP_UNROLL * THREADS) << span_log2) {
-        const bool is = c0 + lane < row.vectors && order_key(segment[g * THREADS + threadIdx.x]) >= bound;
-        const uint32_t who = __ballot_sync(0xFFFFFFFFu, is);
-        const int at = hits + __popc(who & ((1u << lane) - 1u));
-        if (is && at < LP_HITS) hit[at] = c0 + lane;
-        hits += __popc(who);
+    const uint32_t below = (1u << lane) - 1u;
+    // the stretches of this lane that reach the bound, as bits
+    const float least = key_logit(bound);
+    const int stretches = row.vectors > (int)threadIdx.x ? (row.vectors - (int)threadIdx.x + ((LP_UNROLL * THREADS) << span_log2) - 1) / ((LP_UNROLL * THREADS) << span_log2) : 0;
+    uint32_t reach = 0;
+#pragma unroll
+    for (int g = 0; g < SEGMENTS; g += 4) {
+        if (g > 0 && g >= stretches) break;
+        const float4 four = *reinterpret_cast<const float4*>(segment + g);
+        if (!(four.x < least)) reach |= 1u << g;
+        if (!(four.y < least)) reach |= 2u << g;
+        if (!(four.z < least)) reach |= 4u << g;
+        if (!(four.w < least)) reach |= 8u << g;
     }
-    if (hits > LP_HITS) {                                            // (each has a candidate)
+    reach &= (1u << stretches) - 1u;
+    int hits = 0;
+    for (uint32_t who; (who = __ballot_sync(0xFFFFFFFFu, reach != 0)) != 0; hits += __popc(who)) {
+        if (reach == 0) continue;
+        const int at = hits + __popc(who & below), g = __ffs(reach) - 1;
+        if (at < LP_HITS) hit[at] = threadIdx.x + g * ((LP_UNROLL * THREADS) << span_log2);
+        reach &= reach - 1;
+    }
+    if (hits > LP_HITS || bound == 0xFFFFFFFFu) {                    // (each has a candidate; kk NaN)
         if (lane == 0) atomicAdd(&sh.count, LP_CANDIDATES + 1);
         hits = 0;
     }
     __syncwarp();
-    auto offer = [&](uint32_t k, int j) {
-        const int at = atomicAdd(&sh.count, 1);
-        if (at < LP_CANDIDATES) sh.cand[at] = entry_key(k, j);
+    auto put = [&](int at, uint32_t key, int j) {
+        if (at < LP_CANDIDATES) sh.cand[at] = entry_key(key, j);
     };
-    const uint4* body = row.body();
     static_assert(LP_UNROLL == 4, "the vectors of a stretch are a power of two");
-    const float least = key_logit(bound);
-    for (int w = lane; w < hits << (span_log2 + 2); w += 32) {
-        const int at = hit[w >> (span_log2 + 2)] + (w & ((LP_UNROLL << span_log2) - 1)) * THREADS;
-        if (at >= row.vectors) continue;
-        const uint4 v = body[at];
-        uint32_t found = 0;                                          // (a NaN is; one that is not, if the bound is NaN, falls out below)
+    const int work = hits << (span_log2 + 2);
+    if (work == 0) meanwhile();
+    for (int w0 = 0; w0 < work; w0 += 32) {
+        const int w = w0 + lane, at = w < work ? hit[w >> (span_log2 + 2)] + (w & ((LP_UNROLL << span_log2) - 1)) * THREADS : row.vectors;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (at < row.vectors) v = load_stream<true>(row.body() + at);
+        if (w0 == 0) meanwhile();
+        uint32_t found = 0;
 #pragma unroll
         for (int i = 0; i < Vec<T>::N; i += 2) {
             const f2 pr = Vec<T>::pair(v, i / 2);
-            if (!(lo_of(pr) < least)) found |= 1u << i;
+            if (!(lo_of(pr) < least)) found |= 1u << i;             // (a NaN is)
             if (!(hi_of(pr) < least)) found |= 2u << i;
         }
+        if (at >= row.vectors) found = 0;
         for (; found != 0; found &= found - 1) {
-            const int j = row.head + at * Vec<T>::N + __ffs(found) - 1;
-            const uint32_t key = order_key(lp_f(row.z[j]));
-            if (key >= bound) offer(key, j);
+            const int i = __ffs(found) - 1;
+            put(atomicAdd(&sh.count, 1), order_key(Vec<T>::element(v, i)), row.head + at * Vec<T>::N + i);
         }
     }
-    if ((int)threadIdx.x < row.head && order_key(head) >= bound) offer(order_key(head), (int)threadIdx.x);
-    if ((int)threadIdx.x < row.rest && order_key(rest) >= bound) offer(order_key(rest), row.tail + (int)threadIdx.x);
+    if ((int)threadIdx.x < row.head && order_key(head) >= bound) put(atomicAdd(&sh.count, 1), order_key(head), threadIdx.x);
+    if ((int)threadIdx.x < row.rest && order_key(rest) >= bound) put(atomicAdd(&sh.count, 1), order_key(rest), row.tail + threadIdx.x);
 }
 
 // With the candidates there (behind a barrier): calls put(place, entry) for the kk largest.
-template <typename T, int THREADS, typename F>
+template <typename T, int THREADS, int LANES, typename F>
 __device__ __forceinline__ void select(const RowParts<T>& row, int n, int kk, uint32_t bound, TopShared& sh, F put) {
     int count = sh.count;
     if (count > LP_CANDIDATES) {
         count = crowded<T, THREADS>(row, n, kk, bound, sh);
         __syncthreads();
     }
-    for (int i = threadIdx.x; i < count; i += THREADS) {             // an entry's place is the number of larger ones
-        const uint64_t mine = sh.cand[i];
+    // An entry's place is the number of larger ones, which LANES lanes count a part of each.
+    const int part = threadIdx.x % LANES, warp = threadIdx.x >> 5;
+    for (int i0 = warp * (32 / LANES); i0 < count; i0 += THREADS / LANES) {
+        const int i = i0 + (threadIdx.x & 31) / LANES;
+        const uint64_t mine = sh.cand[min(i, count - 1)];
         int above = 0;
-        for (int q = 0; q + 1 < count; q += 2) {
+        for (int q = 2 * part; q + 1 < count; q += 2 * LANES) {
             const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(&sh.cand[q]);
             above += (two.x > mine) + (two.y > mine);
         }
-        if (count & 1) above += sh.cand[count - 1] > mine;
-        if (above < kk) put(above, mine);
+        if ((count & 1) && part == 0) above += sh.cand[count - 1] > mine;
+#pragma unroll
+        for (int o = 1; o < LANES; o <<= 1) above += __shfl_xor_sync(0xFFFFFFFFu, above, o);
+        if (part == 0 && i < count && above < kk) put(above, mine);
     }
-}
-__device__ __forceinline__ uint32_t common_bound(const TopShared& sh, int warps) {
-    return __reduce_min_sync(0xFFFFFFFFu, sh.bound[min((int)(threadIdx.x & 31), warps - 1)]);
 }
 
 struct LogprobArgs {
@@ -421,7 +467,7 @@ __device__ __forceinline__ RowResult tell_row(const LogprobArgs& p, int row, Row
     if (!odd) {
         const float ln_s = logf(x.s);
         logs = fmaxf(fmaf(fmaf(-x.m, kd, reference(x.m, kd)), kLn2, ln_s), 0.f);   // (a sum relative to the maximum is at least 1)
-        H = fmaxf(ln_s - kLn2 * (x.a / x.s), 0.f);
+        H = fmaxf(ln_s - kLn2 * __fdividef(x.a, x.s), 0.f);
         if (none) { logs = -INFINITY; H = 0.f; }
         if (!(x.m < INFINITY)) x.m = logs = H = __int_as_float(0x7FC00000);
     }
@@ -448,11 +494,11 @@ __device__ __forceinline__ int span_of(int vectors) {                    // log2
 //   2048 rows of 32000, k = 32             -            53 us          37 us       (fewer warps than hide the loads' latency)
 // and 512 where there is an SM for every row (one row of 32000, k = 20: 6.4 us, with 256 threads 6.6).  KEEP: the row stays in L1 for the second look at
 // it (2048 rows of 32000, k = 32: 36.9 us, without 39.3; rows of 200 KB: 48 us, without 45).
-struct TinyRow { static constexpr int THREADS = 64, SEGMENTS = 8, PER_SM = 20; static constexpr bool KEEP = true; };
-struct ShortRow { static constexpr int THREADS = 128, SEGMENTS = 4, PER_SM = 10; static constexpr bool KEEP = true; };
-struct MiddleRow { static constexpr int THREADS = 256, SEGMENTS = 4, PER_SM = 6; static constexpr bool KEEP = true; };
-struct LongRow { static constexpr int THREADS = 256, SEGMENTS = 16, PER_SM = 6; static constexpr bool KEEP = false; };
-struct LoneRow { static constexpr int THREADS = 512, SEGMENTS = 8, PER_SM = 1; static constexpr bool KEEP = true; };
+struct TinyRow { static constexpr int THREADS = 64, SEGMENTS = 8, PER_SM = 20; static constexpr bool AHEAD = false, KEEP = true; };
+struct ShortRow { static constexpr int THREADS = 128, SEGMENTS = 4, PER_SM = 10; static constexpr bool AHEAD = false, KEEP = true; };
+struct MiddleRow { static constexpr int THREADS = 256, SEGMENTS = 4, PER_SM = 6; static constexpr bool AHEAD = false, KEEP = true; };
+struct LongRow { static constexpr int THREADS = 256, SEGMENTS = 16, PER_SM = 6; static constexpr bool AHEAD = false, KEEP = false; };
+struct LoneRow { static constexpr int THREADS = 512, SEGMENTS = 8, PER_SM = 1; static constexpr bool AHEAD = true, KEEP = true; };
 
 template <typename T, typename Plan, bool TOP>
 __global__ void __launch_bounds__(Plan::THREADS, Plan::PER_SM) logprobs_kernel(const __grid_constant__ LogprobArgs p) {
@@ -474,8 +520,23 @@ __global__ void __launch_bounds__(Plan::THREADS, Plan::PER_SM) logprobs_kernel(c
     const float head = (int)threadIdx.x < part.head ? lp_f(part.z[threadIdx.x]) : -INFINITY;
     const float rest = (int)threadIdx.x < part.rest ? lp_f(part.z[part.tail + threadIdx.x]) : -INFINITY;
     const int span_log2 = span_of<THREADS, SEGMENTS>(part.vectors);
-    ThreadRow<T, THREADS, TOP> mine(own.segment, span_log2);
+    ThreadRow<T, THREADS, TOP> mine(own.segment + own.STRIDE * threadIdx.x, span_log2);
     int c0 = threadIdx.x;
+    if (Plan::AHEAD) {                                                // the next round's vectors are on their way while one is summed
+        uint4 v[LP_UNROLL], w[LP_UNROLL];
+        auto load = [&](uint4 (&to)[LP_UNROLL], int c) {
+#pragma unroll
+            for (int u = 0; u < LP_UNROLL; ++u)
+                if (c + u * THREADS < part.vectors) to[u] = load_stream<KEEP>(part.body() + c + u * THREADS);
+        };
+        load(v, c0);
+        for (; c0 < part.vectors; c0 += LP_UNROLL * THREADS) {
+            load(w, c0 + LP_UNROLL * THREADS);
+            mine.template round<false>(v, c0, part.vectors, kd);
+#pragma unroll
+            for (int u = 0; u < LP_UNROLL; ++u) v[u] = w[u];
+        }
+    }
     for (; c0 + (LP_UNROLL - 1) * THREADS < part.vectors; c0 += LP_UNROLL * THREADS) {
         uint4 v[LP_UNROLL];
 #pragma unroll
@@ -494,25 +555,26 @@ __global__ void __launch_bounds__(Plan::THREADS, Plan::PER_SM) logprobs_kernel(c
     if ((int)threadIdx.x < part.head) add_one(mine.x, head, kd);
     if ((int)threadIdx.x < part.rest) add_one(mine.x, rest, kd);
     if (TOP) offer_bound<THREADS>(part.vectors, p.k, mine.x.m, sh);
-    RowSums x = warp_merge(mine.x, kd);
+    RowSums x = merged<32>(mine.x, warp_max_nan(mine.x.m), kd);
     if (lane == 0) sums[warp] = x;
     __syncthreads();
     x = sums[lane & (THREADS / 32 - 1)];
-    float m = x.m;
-#pragma unroll
-    for (int o = THREADS / 64; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    const float m = warp_max_nan(x.m);
     const bool odd = is_odd(m);
     float logs = 0.f, H = 0.f;
     if (odd) odd_row<T, THREADS>(z, V, m, p.c, odd_sums, logs, H);
-    if (warp == 0) {
-        x = warp_merge(lane < THREADS / 32 ? x : RowSums{-INFINITY, 0.f, 0.f}, kd);
+    auto tell = [&]() {
+        if (warp != 0) return;
+        x = merged<THREADS / 32>(x, m, kd);
         if (lane == 0) result = tell_row(p, row, x, kd, odd, logs, H, token >= 0 && token < V ? token : -1, token_logit);
-    }
+    };
     if (TOP) {
-        const uint32_t bound = common_bound(sh, THREADS / 32);
-        gather<T, THREADS>(part, bound, span_log2, own.segment, own.hit[warp], head, rest, sh);
+        const uint32_t bound = common_bound<THREADS>(part.vectors, p.k, sh);
+        gather<T, THREADS, SEGMENTS>(part, bound, span_log2, own.segment + own.STRIDE * threadIdx.x, own.hit[warp], head, rest, sh, tell);
         __syncthreads();
-        select<T, THREADS>(part, V, p.k, bound, sh, [&](int at, uint64_t e) { tell_top(p, row, at, e, result); });
+        select<T, THREADS, Plan::AHEAD ? 4 : 1>(part, V, p.k, bound, sh, [&](int at, uint64_t e) { tell_top(p, row, at, e, result); });
+    } else {
+        tell();
     }
 }
 
