@@ -237,7 +237,9 @@ def _type_of(t, where: str, allowed) -> int:
 
 def _current_device(where: str) -> int:
     """The current CUDA device, on which the library works: a tensor of another one, or of the host, in a kernel's hands would be a fault."""
-    if not _torch.cuda.is_initialized() and not _torch.cuda.is_available():
+    if _torch.cuda.is_initialized():
+        return _torch._C._cuda_getDevice()
+    if not _torch.cuda.is_available():
         raise ValueError(f"{where}: tensors must be on the current CUDA device, and there is none")
     return _torch.cuda.current_device()
 
@@ -252,16 +254,12 @@ def _rows(t, where: str):
     return T, V, stride if T > 1 else V
 
 
-def _operand(t, dtype, shape, where: str):
-    """An operand beside the logits: of the type and the size that the library will assume."""
-    if t is not None and (t.dtype is not dtype or t.shape != shape):
-        raise ValueError(f"{where}: {dtype} {list(shape)} is needed, got {t.dtype} {list(t.shape)}")
-
-
-def _on_device(where: str, tensors):
-    device = _current_device(where)
-    for t in tensors:
-        if t is not None and t.get_device() != device:
+def _operands(where: str, device: int, *wanted):
+    """The operands beside the logits: each None or of the type, the size and on the device that the library will assume."""
+    for t, dtype, shape in wanted:
+        if t is not None and (t.dtype is not dtype or t.shape != shape or t.get_device() != device):
+            if t.dtype is not dtype or t.shape != shape:
+                raise ValueError(f"{where}: {dtype} {list(shape)} is needed, got {t.dtype} {list(t.shape)}")
             raise ValueError(f"{where}: tensors must be on the current CUDA device, got {t.device}")
 
 
@@ -269,22 +267,19 @@ def qlora_token_logprobs(logits, tokens, inv_temperature, logprobs, entropy=None
     """Log probabilities of `tokens` (int32 [T], or None) under logits [T, V] (bf16, fp16 or fp32; rows may lie apart), the entropy of each
     row and its k most likely places (k = top_ids.shape[1]); stats fp32 [T, 3] is what the backward call reads.  Outputs may be None."""
     where = "qlora_token_logprobs"
-    torch = _load_torch()
+    torch = _torch or _load_torch()
     T, V, stride = _rows(logits, where)
     dtype = _type_of(logits, where, _LOGIT_TYPES)
-    f32, row, k = torch.float32, (T,), 0
+    f32, i32, row, k = torch.float32, torch.int32, (T,), 0
     if top_ids is not None or top_logprobs is not None:
         top = top_ids if top_ids is not None else top_logprobs
         if top.dim() != 2:
             raise ValueError(f"{where}: the alternatives are [T, k]")
         k = top.shape[1]
-        _operand(top_ids, torch.int32, (T, k), where)
-        _operand(top_logprobs, f32, (T, k), where)
-    _operand(tokens, torch.int32, row, where)
-    _operand(logprobs, f32, row, where)
-    _operand(entropy, f32, row, where)
-    _operand(stats, f32, (T, 3), where)
-    _on_device(where, (logits, tokens, logprobs, entropy, top_ids, top_logprobs, stats))
+    device = logits.get_device()
+    _operands(where, device, (tokens, i32, row), (logprobs, f32, row), (entropy, f32, row), (top_ids, i32, (T, k)), (top_logprobs, f32, (T, k)), (stats, f32, (T, 3)))
+    if device != _current_device(where):
+        raise ValueError(f"{where}: tensors must be on the current CUDA device, got {logits.device}")
     rc = _native().qlora_token_logprobs(T, V, stride, dtype, logits.data_ptr(), tokens, inv_temperature, k, logprobs, entropy, top_ids, top_logprobs,
                                         stats, stream)
     if rc != 0:
@@ -295,18 +290,16 @@ def qlora_token_logprobs_bwd(logits, tokens, inv_temperature, stats, d_logprobs,
     """Gradient of qlora_token_logprobs with respect to the logits, into dlogits [T, V] (the logits' type; rows may lie apart; may be the
     logits themselves)."""
     where = "qlora_token_logprobs_bwd"
-    torch = _load_torch()
+    torch = _torch or _load_torch()
     T, V, stride = _rows(logits, where)
     dtype = _type_of(logits, where, _LOGIT_TYPES)
     Tg, Vg, grad_stride = _rows(dlogits, where)
     if Tg != T or Vg != V or dlogits.dtype is not logits.dtype:
         raise ValueError(f"{where}: dlogits has the shape and the type of logits")
-    f32, row = torch.float32, (T,)
-    _operand(tokens, torch.int32, row, where)
-    _operand(stats, f32, (T, 3), where)
-    _operand(d_logprobs, f32, row, where)
-    _operand(d_entropy, f32, row, where)
-    _on_device(where, (logits, tokens, stats, d_logprobs, d_entropy, dlogits))
+    f32, row, device = torch.float32, (T,), logits.get_device()
+    _operands(where, device, (tokens, torch.int32, row), (stats, f32, (T, 3)), (d_logprobs, f32, row), (d_entropy, f32, row), (dlogits, logits.dtype, (T, V)))
+    if device != _current_device(where):
+        raise ValueError(f"{where}: tensors must be on the current CUDA device, got {logits.device}")
     rc = _native().qlora_token_logprobs_bwd(T, V, stride, dtype, logits.data_ptr(), tokens, inv_temperature, stats, d_logprobs, d_entropy, grad_stride,
                                             dlogits.data_ptr(), stream)
     if rc != 0:
@@ -379,10 +372,11 @@ def adamw_desc(params, grads, m, v, master=None, m_scale=None, v_scale=None, bet
     return d
 
 
-def _check_desc(d, where: str) -> int:
+def _desc_device(d, where: str) -> int:
     if not isinstance(d, _AdamwDesc):
         raise TypeError(f"{where}: the optimizer descriptor must come from adamw_desc()")
-    _load_torch()
+    if _torch is None:
+        _load_torch()
     device = _current_device(where)
     if d.device is not None and d.device != device:
         raise ValueError(f"{where}: the descriptor's tensors are on device {d.device}, the current one is {device}")
@@ -392,10 +386,10 @@ def _check_desc(d, where: str) -> int:
 def qlora_grad_norm(d, prescale, max_norm, out, workspace, stream=None, workspace_bytes=None):
     """out fp32 [2]: the norm of prescale times all gradients of the descriptor, and the factor for qlora_adamw that clips it to max_norm."""
     where = "qlora_grad_norm"
-    device = _check_desc(d, where)
-    _operand(out, _torch.float32, (2,), where)
-    if out.get_device() != device or workspace.get_device() != device:
-        raise ValueError(f"{where}: tensors must be on the current CUDA device")
+    device = _desc_device(d, where)
+    _operands(where, device, (out, _torch.float32, (2,)))
+    if workspace is not None and workspace.get_device() != device:
+        raise ValueError(f"{where}: tensors must be on the current CUDA device, got {workspace.device}")
     rc = _native().qlora_grad_norm(d, prescale, max_norm, out, workspace, workspace_bytes, stream)
     if rc != 0:
         raise QloraError(rc, where)
@@ -405,18 +399,13 @@ def qlora_adamw(d, lr, step, norm=None, stream=None):
     """One AdamW step over the descriptor's tensors.  lr: a number or an fp32 tensor [1]; step: an int from 1 or an int32 tensor [1] (device
     memory that a captured step reads at replay); norm: fp32 [2] from qlora_grad_norm or None."""
     where = "qlora_adamw"
-    device = _check_desc(d, where)
+    device = _desc_device(d, where)
     lr_dev = step_dev = None
     if not isinstance(lr, float) and hasattr(lr, "data_ptr"):
-        _operand(lr, _torch.float32, (1,), where)
         lr, lr_dev = 0.0, lr
     if not isinstance(step, int) and hasattr(step, "data_ptr"):
-        _operand(step, _torch.int32, (1,), where)
         step, step_dev = 0, step
-    _operand(norm, _torch.float32, (2,), where)
-    for t in (lr_dev, step_dev, norm):
-        if t is not None and t.get_device() != device:
-            raise ValueError(f"{where}: tensors must be on the current CUDA device")
+    _operands(where, device, (lr_dev, _torch.float32, (1,)), (step_dev, _torch.int32, (1,)), (norm, _torch.float32, (2,)))
     rc = _native().qlora_adamw(d, lr, step, lr_dev, step_dev, norm, stream)
     if rc != 0:
         raise QloraError(rc, where)
