@@ -244,8 +244,8 @@ typedef struct {
     const void* grad;  /* [n] */
     void* m;           /* [n] first moment, updated: fp32, or e4m3 with m_scale */
     void* v;           /* [n] second moment, updated: fp32, or the e4m3 root of it with v_scale */
-    float* m_scale;    /* fp32 [ceil(n / 256)]; NULL with 32-bit states */
-    float* v_scale;    /* fp32 [ceil(n / 256)]; NULL with 32-bit states */
+    float* m_scale;    /* fp32 [ceil(n / 256)], may begin at any float; NULL with 32-bit states */
+    float* v_scale;    /* fp32 [ceil(n / 256)], may begin at any float; NULL with 32-bit states */
     long long n;       /* elements; 0 is allowed */
 } qlora_adamw_tensor;
 

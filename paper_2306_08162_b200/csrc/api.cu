@@ -77,8 +77,8 @@ int check_adamw(const qlora_adamw_desc* d, bool step) {
         if (step) {
             if (!t.param || !t.m || !t.v || (t.m_scale != nullptr) != eight || (t.v_scale != nullptr) != eight) return QLORA_ERR_INVALID_ARG;
             if (t.master && d->param_type == QLORA_FP32) return QLORA_ERR_INVALID_ARG;
-            for (const void* p : {(const void*)t.param, (const void*)t.master, (const void*)t.m, (const void*)t.v, (const void*)t.m_scale, (const void*)t.v_scale})
-                all |= reinterpret_cast<uintptr_t>(p);
+            for (const void* p : {(const void*)t.param, (const void*)t.master, (const void*)t.m, (const void*)t.v}) all |= reinterpret_cast<uintptr_t>(p);
+            if ((reinterpret_cast<uintptr_t>(t.m_scale) | reinterpret_cast<uintptr_t>(t.v_scale)) & 3u) return QLORA_ERR_ALIGNMENT;
         }
         if (all & 15u) return QLORA_ERR_ALIGNMENT;
     }

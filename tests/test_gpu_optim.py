@@ -245,6 +245,32 @@ def test_8_bit_states_follow_the_moments():
     assert np.corrcoef(gm, em)[0, 1] > 0.98
 
 
+def test_tensors_and_scales_cut_from_flat_buffers():
+    """The tensors of a model in one buffer each, at multiples of 256 elements: the scales then begin at any float.  Each tensor like one alone."""
+    sizes = [300, 257, 1000]
+    alone = Model(sizes, bits=8, seed=37)
+    starts = [0, 512, 1024]
+    flat = dict(param=torch.zeros(2048, dtype=torch.bfloat16, device="cuda"), grad=torch.zeros(2048, device="cuda"), m=torch.zeros(2048, device="cuda").to(torch.float8_e4m3fn),
+                v=torch.zeros(2048, device="cuda").to(torch.float8_e4m3fn), m_scale=torch.full((9,), 7.0, device="cuda"), v_scale=torch.full((9,), 7.0, device="cuda"))
+    views = {}
+    for name, buf in flat.items():
+        scale = name.endswith("_scale")
+        views[name] = [buf[1 + a // 256:1 + a // 256 + -(-n // 256)] if scale else buf[a:a + n] for a, n in zip(starts, sizes)]
+        for view, t in zip(views[name], getattr(alone, name)):
+            view.copy_(t)
+    kept = {name: buf.clone() for name, buf in flat.items()}
+    desc = ql.adamw_desc(views["param"], views["grad"], views["m"], views["v"], m_scale=views["m_scale"], v_scale=views["v_scale"], **HYPER)
+    ql.qlora_adamw(desc, 1e-2, 5)
+    ql.qlora_adamw(alone.desc, 1e-2, 5)
+    for name, buf in flat.items():
+        for view, t in zip(views[name], getattr(alone, name)):
+            assert torch.equal(view.view(torch.uint8), t.view(torch.uint8)), name
+            view.view(torch.uint8).zero_()
+        for view in (kept[name][1 + a // 256:1 + a // 256 + -(-n // 256)] if name.endswith("_scale") else kept[name][a:a + n] for a, n in zip(starts, sizes)):
+            view.view(torch.uint8).zero_()
+        assert torch.equal(buf.view(torch.uint8), kept[name].view(torch.uint8)), name      # nothing between the tensors is touched
+
+
 def test_descriptor_refuses_what_would_race():
     m = Model([300, 300])
     with pytest.raises(ValueError, match="overlap"):

@@ -91,7 +91,7 @@ def test_adamw_arguments(ql):
     assert changed(param=OK + 2) == -3 and changed(grad=OK + 4) == -3 and changed(master=OK + 4) == -3
     d, array = adam(ql, state_type=3)
     assert status(d) == -1                                                  # 8-bit states without scales
-    array[0].m_scale, array[0].v_scale = OK, OK + 4
+    array[0].m_scale, array[0].v_scale = OK + 4, OK + 2                     # (scales may begin at any float)
     assert status(d) == -3
     d, array = adam(ql, param_type=2)
     array[0].master = OK
