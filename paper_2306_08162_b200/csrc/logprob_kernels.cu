@@ -4,7 +4,7 @@
 // in one pass over the row: every thread keeps its own maximum and sums relative to it and corrects them when the maximum moves.
 // Bound by HBM in the long run (2 bytes a bf16 logit: 16000 rows of 32000 in 156 us, the time of a copy of as many bytes), by the beginning and end of the
 // launch where it is short (888 rows, all that run at a time: 13.7 us, each 888 more: 9.0; 2048 rows: 25.9 us, 5.1 TB/s) and by instructions where there are
-// alternatives (k = 32: 36.9 us; 4096 rows of 128000, k = 20: 184 us, 5.7 TB/s).  A logit takes 1 exponential of the special-function unit, whose 16 a
+// alternatives (k = 32: 36.2 us; 4096 rows of 128000, k = 20: 179 us, 5.9 TB/s).  A logit takes 1 exponential of the special-function unit, whose 16 a
 // clock and SM are 57 % busy at 5.1 TB/s, and some 4.5 other instructions: maximum and clamp of two bf16 at once, a fused multiply-add, two sums in pairs.
 // The alternatives cost no sorting: see offer_bound.
 // Timed and taken out: blocks that stay, with a ring of copies ahead in shared memory (2048 x 32000: 27 - 35 us: fewer warps fit); clusters that share a
@@ -47,6 +47,11 @@ template <> struct Vec<float> {
     }
     static __device__ __forceinline__ f2 pair(const uint4& v, int i) { return i == 0 ? make_f2(__uint_as_float(v.x), __uint_as_float(v.y)) : make_f2(__uint_as_float(v.z), __uint_as_float(v.w)); }
     static __device__ __forceinline__ float element(const uint4& v, int i) { return __uint_as_float((i & 2) != 0 ? ((i & 1) != 0 ? v.w : v.z) : ((i & 1) != 0 ? v.y : v.x)); }
+    // Bits of the elements that are not below `least` (a NaN is not); element_of(bit) is the element's number.
+    static __device__ __forceinline__ uint32_t reaching(const uint4& v, float least) {
+        return (__uint_as_float(v.x) < least ? 0u : 1u) | (__uint_as_float(v.y) < least ? 0u : 2u) | (__uint_as_float(v.z) < least ? 0u : 4u) | (__uint_as_float(v.w) < least ? 0u : 8u);
+    }
+    static __device__ __forceinline__ int element_of(int bit) { return bit; }
     typedef float Max;
     static __device__ __forceinline__ Max lowest() { return -INFINITY; }
     static __device__ __forceinline__ Max fold(Max m, const uint4& v) {
@@ -69,6 +74,12 @@ template <> struct Vec<__nv_bfloat16> {
     }
     static __device__ __forceinline__ Max lowest() { return __float2bfloat162_rn(-INFINITY); }
     static __device__ __forceinline__ Max of(uint32_t w) { return *reinterpret_cast<const Max*>(&w); }
+    // (two elements at once; the upper ones of the pairs are 16 bits up)
+    static __device__ __forceinline__ uint32_t reaching(const uint4& v, float least) {
+        const Max b = __float2bfloat162_rn(least);
+        return (~__hlt2_mask(of(v.x), b) & 0x00020001u) | (~__hlt2_mask(of(v.y), b) & 0x00080004u) | (~__hlt2_mask(of(v.z), b) & 0x00200010u) | (~__hlt2_mask(of(v.w), b) & 0x00800040u);
+    }
+    static __device__ __forceinline__ int element_of(int bit) { return bit & 15; }
     static __device__ __forceinline__ Max fold(Max m, const uint4& v) {
         return __hmax2_nan(__hmax2_nan(m, __hmax2_nan(of(v.x), of(v.y))), __hmax2_nan(of(v.z), of(v.w)));
     }
@@ -90,6 +101,12 @@ template <> struct Vec<__half> {
     typedef __half2 Max;
     static __device__ __forceinline__ Max lowest() { return __float2half2_rn(-INFINITY); }
     static __device__ __forceinline__ Max of(uint32_t w) { return *reinterpret_cast<const Max*>(&w); }
+    // (two elements at once; the upper ones of the pairs are 16 bits up)
+    static __device__ __forceinline__ uint32_t reaching(const uint4& v, float least) {
+        const Max b = __float2half2_rn(least);
+        return (~__hlt2_mask(of(v.x), b) & 0x00020001u) | (~__hlt2_mask(of(v.y), b) & 0x00080004u) | (~__hlt2_mask(of(v.z), b) & 0x00200010u) | (~__hlt2_mask(of(v.w), b) & 0x00800040u);
+    }
+    static __device__ __forceinline__ int element_of(int bit) { return bit & 15; }
     static __device__ __forceinline__ Max fold(Max m, const uint4& v) {
         return __hmax2_nan(__hmax2_nan(m, __hmax2_nan(of(v.x), of(v.y))), __hmax2_nan(of(v.z), of(v.w)));
     }
@@ -189,7 +206,8 @@ __device__ __noinline__ void odd_row(const T* z, int V, float m, float c, float*
 }
 
 // This thread's part of a row, LP_UNROLL vectors (a round) at a time.  TOP: the maximum of each stretch of 2^span_log2 rounds goes to segment[stretch].
-template <typename T, int THREADS, bool TOP>
+// (SINGLE: every round is one.)
+template <typename T, int THREADS, bool TOP, bool SINGLE>
 struct ThreadRow {
     RowSums x;
     float stretch;
@@ -204,7 +222,8 @@ struct ThreadRow {
         for (int u = 0; u < LP_UNROLL; ++u)
             if (WHOLE || c0 + u * THREADS < vectors) top = Vec<T>::fold(top, v[u]);
         const float here = Vec<T>::value(top), m = max_nan(x.m, here);
-        if (TOP) {
+        if (TOP && SINGLE) *segment++ = here;
+        if (TOP && !SINGLE) {
             stretch = max_nan(stretch, here);
             if (--left == 0) {
                 *segment++ = stretch;
@@ -230,7 +249,7 @@ struct ThreadRow {
         x.a = lo_of(a2) + hi_of(a2);
     }
     __device__ __forceinline__ void finish() {
-        if (TOP && left != span) *segment = stretch;
+        if (TOP && !SINGLE && left != span) *segment = stretch;
     }
 };
 
@@ -370,7 +389,9 @@ __device__ __forceinline__ void gather(const RowParts<T>& row, uint32_t bound, i
     const uint32_t below = (1u << lane) - 1u;
     // the stretches of this lane that reach the bound, as bits
     const float least = key_logit(bound);
-    const int stretches = row.vectors > (int)threadIdx.x ? (row.vectors - (int)threadIdx.x + ((LP_UNROLL * THREADS) << span_log2) - 1) / ((LP_UNROLL * THREADS) << span_log2) : 0;
+    constexpr int ROUND_LOG2 = THREADS == 64 ? 8 : THREADS == 128 ? 9 : THREADS == 256 ? 10 : 11;
+    static_assert(1 << ROUND_LOG2 == LP_UNROLL * THREADS, "vectors of a round");
+    const int stretch_log2 = ROUND_LOG2 + span_log2, stretches = (max(row.vectors - (int)threadIdx.x, 0) + (1 << stretch_log2) - 1) >> stretch_log2;
     uint32_t reach = 0;
 #pragma unroll
     for (int g = 0; g < SEGMENTS; g += 4) {
@@ -386,7 +407,7 @@ __device__ __forceinline__ void gather(const RowParts<T>& row, uint32_t bound, i
     for (uint32_t who; (who = __ballot_sync(0xFFFFFFFFu, reach != 0)) != 0; hits += __popc(who)) {
         if (reach == 0) continue;
         const int at = hits + __popc(who & below), g = __ffs(reach) - 1;
-        if (at < LP_HITS) hit[at] = threadIdx.x + g * ((LP_UNROLL * THREADS) << span_log2);
+        if (at < LP_HITS) hit[at] = threadIdx.x + (g << stretch_log2);
         reach &= reach - 1;
     }
     if (hits > LP_HITS || bound == 0xFFFFFFFFu) {                    // (each has a candidate; kk NaN)
@@ -405,16 +426,9 @@ __device__ __forceinline__ void gather(const RowParts<T>& row, uint32_t bound, i
         uint4 v = make_uint4(0, 0, 0, 0);
         if (at < row.vectors) v = load_stream<true>(row.body() + at);
         if (w0 == 0) meanwhile();
-        uint32_t found = 0;
-#pragma unroll
-        for (int i = 0; i < Vec<T>::N; i += 2) {
-            const f2 pr = Vec<T>::pair(v, i / 2);
-            if (!(lo_of(pr) < least)) found |= 1u << i;             // (a NaN is)
-            if (!(hi_of(pr) < least)) found |= 2u << i;
-        }
-        if (at >= row.vectors) found = 0;
+        uint32_t found = at < row.vectors ? Vec<T>::reaching(v, least) : 0;
         for (; found != 0; found &= found - 1) {
-            const int i = __ffs(found) - 1;
+            const int i = Vec<T>::element_of(__ffs(found) - 1);
             put(atomicAdd(&sh.count, 1), order_key(Vec<T>::element(v, i)), row.head + at * Vec<T>::N + i);
         }
     }
@@ -492,13 +506,14 @@ __device__ __forceinline__ int span_of(int vectors) {                    // log2
 //   8192 rows of 4000 bf16, k = 5         26 us         35 us           -
 //   4000 rows of 10000, k = 20             -            28 us          38 us
 //   2048 rows of 32000, k = 32             -            53 us          37 us       (fewer warps than hide the loads' latency)
-// and 512 where there is an SM for every row (one row of 32000, k = 20: 6.4 us, with 256 threads 6.6).  KEEP: the row stays in L1 for the second look at
-// it (2048 rows of 32000, k = 32: 36.9 us, without 39.3; rows of 200 KB: 48 us, without 45).
-struct TinyRow { static constexpr int THREADS = 64, SEGMENTS = 8, PER_SM = 20; static constexpr bool AHEAD = false, KEEP = true; };
-struct ShortRow { static constexpr int THREADS = 128, SEGMENTS = 4, PER_SM = 10; static constexpr bool AHEAD = false, KEEP = true; };
-struct MiddleRow { static constexpr int THREADS = 256, SEGMENTS = 4, PER_SM = 6; static constexpr bool AHEAD = false, KEEP = true; };
-struct LongRow { static constexpr int THREADS = 256, SEGMENTS = 16, PER_SM = 6; static constexpr bool AHEAD = false, KEEP = false; };
-struct LoneRow { static constexpr int THREADS = 512, SEGMENTS = 8, PER_SM = 1; static constexpr bool AHEAD = true, KEEP = true; };
+// and 512 where there is an SM for every row (one row of 32000, k = 20: 6.4 us, with 256 threads 6.6; the next loads ahead: 6.1).  SINGLE: a row is few enough
+// rounds that each is a stretch.  KEEP: the row stays in L1 for the second look at it (2048 rows of 32000, k = 32: 36.9 us, without 39.3; rows of 200 KB:
+// 48 us, without 45).
+struct TinyRow { static constexpr int THREADS = 64, SEGMENTS = 4, PER_SM = 20; static constexpr bool SINGLE = true, AHEAD = false, KEEP = true; };
+struct ShortRow { static constexpr int THREADS = 128, SEGMENTS = 4, PER_SM = 10; static constexpr bool SINGLE = true, AHEAD = false, KEEP = true; };
+struct MiddleRow { static constexpr int THREADS = 256, SEGMENTS = 4, PER_SM = 6; static constexpr bool SINGLE = true, AHEAD = false, KEEP = true; };
+struct LongRow { static constexpr int THREADS = 256, SEGMENTS = 16, PER_SM = 6; static constexpr bool SINGLE = false, AHEAD = false, KEEP = false; };
+struct LoneRow { static constexpr int THREADS = 512, SEGMENTS = 8, PER_SM = 1; static constexpr bool SINGLE = false, AHEAD = true, KEEP = true; };
 
 template <typename T, typename Plan, bool TOP>
 __global__ void __launch_bounds__(Plan::THREADS, Plan::PER_SM) logprobs_kernel(const __grid_constant__ LogprobArgs p) {
@@ -519,8 +534,8 @@ __global__ void __launch_bounds__(Plan::THREADS, Plan::PER_SM) logprobs_kernel(c
     const int token = threadIdx.x == 0 && p.logprobs != nullptr ? p.tokens[row] : -1;
     const float head = (int)threadIdx.x < part.head ? lp_f(part.z[threadIdx.x]) : -INFINITY;
     const float rest = (int)threadIdx.x < part.rest ? lp_f(part.z[part.tail + threadIdx.x]) : -INFINITY;
-    const int span_log2 = span_of<THREADS, SEGMENTS>(part.vectors);
-    ThreadRow<T, THREADS, TOP> mine(own.segment + own.STRIDE * threadIdx.x, span_log2);
+    const int span_log2 = Plan::SINGLE ? 0 : span_of<THREADS, SEGMENTS>(part.vectors);
+    ThreadRow<T, THREADS, TOP, Plan::SINGLE> mine(own.segment + own.STRIDE * threadIdx.x, span_log2);
     int c0 = threadIdx.x;
     if (Plan::AHEAD) {                                                // the next round's vectors are on their way while one is summed
         uint4 v[LP_UNROLL], w[LP_UNROLL];
