@@ -146,6 +146,43 @@ def test_ties_and_orders(V, k, dtype):
     check_forward(z, tokens, 1.0, k)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,V,k", [(3100, 1000, 20), (3100, 1501, 32), (170, 7000, 20), (170, 12001, 64), (170, 30000, 20), (160, 60011, 33), (20, 40000, 64)])
+def test_odd_rows_among_many(T, V, k, dtype):
+    """The rows of the tests above among as many others as make every way of sharing rows out take them: each with the oracle, the others with
+    themselves in a batch where the odd rows are not."""
+    z, tokens = make(T, V, dtype, seed=T + V, ld=V + 3)
+    plain = forward(z, tokens, 1.0, k)                               # (the same memory: the order of a sum goes with where the row begins)
+    j = torch.arange(V, device="cuda")
+    odd = torch.arange(0, 14, device="cuda") * (T // 14)
+    low, inf = torch.finfo(z.dtype).min, float("inf")
+    z[odd[0]] = 1.5
+    z[odd[1]] = (j % 3).to(z.dtype)
+    z[odd[2]] = -inf
+    z[odd[3]] = low
+    z[odd[4], 5:] = -inf
+    z[odd[5], 7:] = low
+    z[odd[6], : V - 3] = -inf
+    z[odd[7], V // 2] = float("nan")
+    z[odd[8], V - 1] = inf
+    z[odd[9], V - 70:] = 20.0
+    z[odd[10], 300:600] = 20.0 + (j[:300] % 7).to(z.dtype)
+    z[odd[11]] = torch.where(j % 2 == 0, -0.0, 0.0).to(z.dtype)
+    z[odd[12], ::8] = 9.0
+    z[odd[13]] = ((j % 2048) < 8).to(z.dtype)
+    out = forward(z, tokens, 1.0, k)
+    check = {key: v[odd] for key, v in out.items()}
+    want = orc.token_logprobs(to_f64(z[odd]), tokens[odd].cpu().numpy(), 1.0, k)
+    close(check["logprobs"], want["logprobs"], chain(V))
+    close(check["entropy"], want["entropy"], 25 * chain(V))
+    assert np.array_equal(check["top_ids"].cpu().numpy(), want["top_ids"])
+    close(check["top_logprobs"], want["top_logprobs"], chain(V))
+    others = torch.ones(T, dtype=torch.bool, device="cuda")
+    others[odd] = False
+    for key in out:
+        assert torch.equal(out[key][others], plain[key][others]), key
+
+
 def test_large_logits_keep_their_differences():
     """Logits of several thousand: the statistics are relative to the row's maximum, so nothing is lost."""
     z, tokens = make(4, 9000, "fp32", seed=19)
