@@ -19,7 +19,8 @@ def allreduce_lora_grads(grads: Iterable[torch.Tensor], group=None, bucket_bytes
     """Sum the fp32 gradient tensors `grads` (dA / dB of any number of projections) over the process group, in place.
 
     Tensors are copied into flat buckets of at most `bucket_bytes`, each bucket is all-reduced (SUM) once, and the
-    result is copied back.  The order of `grads` must be the same on every rank.  A single-process run is a no-op."""
+    result is copied back.  The order of `grads` must be the same on every rank.  A single-process run is a no-op.
+    (qlora_grad_norm's prescale = 1 / world size makes the sum a mean for the step.)"""
     if not dist.is_available() or not dist.is_initialized() or dist.get_world_size(group) == 1:
         return
     pending: List[torch.Tensor] = []

@@ -327,6 +327,26 @@ def test_gradient_against_differences():
     assert np.abs(to_f64((grad * d).sum(1)) - want).max() <= 2 * h * h + 8 * chain(V) * 26 / (2 * h)
 
 
+def test_the_longest_row_and_very_many_short_ones():
+    """2^24 logits; 200000 rows of 5.  The reference is the formula in 64 bits on the GPU (the oracle goes row by row)."""
+    for T, V, k in ((1, 1 << 24, 5), (200000, 5, 3)):
+        z, tokens = make(T, V, "fp16", seed=53)
+        out = forward(z, tokens, 1.0, k)
+        lp = torch.log_softmax(z.double(), 1)
+        close(out["logprobs"], lp.gather(1, tokens.long()[:, None]).squeeze(1).cpu().numpy(), chain(V))
+        close(out["entropy"], -(lp.exp() * lp).sum(1).cpu().numpy(), 25 * chain(V))
+        order = torch.sort(z.float(), dim=1, descending=True, stable=True).indices[:, :k]
+        assert torch.equal(out["top_ids"].long(), order)
+        close(out["top_logprobs"], lp.gather(1, order).cpu().numpy(), chain(V))
+        grad = torch.empty_like(z)
+        ql.qlora_token_logprobs_bwd(z, tokens, 1.0, out["stats"], torch.ones(T, device="cuda"), None, grad)
+        want = -lp.exp()
+        want.scatter_add_(1, tokens.long()[:, None], torch.ones_like(want[:, :1]))
+        size = lp.exp().scatter_add(1, tokens.long()[:, None], torch.ones_like(want[:, :1]))
+        bound = 2.0 ** -11 * want.abs() + (chain(V) + 4 * U * (16 + lp.abs())) * size + 2.0 ** -24
+        assert ((grad.double() - want).abs() <= bound).all()
+
+
 def test_long_offsets():
     """A row that begins beyond 2^31 elements."""
     rows, ld = 3, (1 << 30) + 8
