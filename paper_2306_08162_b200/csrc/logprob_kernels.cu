@@ -285,8 +285,8 @@ __device__ __forceinline__ void each_from(const RowParts<T>& row, uint32_t least
 
 struct alignas(16) TopShared {              // (the candidates are read two at a time)
     uint64_t cand[LP_CANDIDATES];        // entries that may be among the largest
-    uint32_t bound[32], next[32];        // by warp
-    int count, in_warp[32];
+    uint32_t bound[32], next[32];        // by warp (of those that stay out: the largest key, and 0)
+    int count, more, in_warp[32];
 };
 template <int THREADS, int SEGMENTS> struct alignas(16) TopWarps {
     static constexpr int STRIDE = SEGMENTS == 4 ? 4 : SEGMENTS + 4;          // (16 bytes at a time, and fewer in the same bank)
@@ -352,11 +352,15 @@ template <int THREADS>
 __device__ __forceinline__ void offer_bound(int vectors, int kk, float top, TopShared& sh) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = min(THREADS / 32, vectors / 32);
     uint32_t key = order_key(top), least = 0xFFFFFFFFu, next = 0;
+    int more = 0;
     if (warps * 32 < kk) least = 0;                                  // (a short row: everything is a candidate)
     else if (warp < warps) {
         for (int q = kk; q > 0; q -= warps) {
             next = __reduce_max_sync(0xFFFFFFFFu, key);
-            if (q < warps) break;                                    // (r more from one warp or another)
+            if (q < warps) {                                         // (r more from one warp or another)
+                more = q;
+                break;
+            }
             least = next;
             if (lane == __ffs(__ballot_sync(0xFFFFFFFFu, key == least)) - 1) key = 0;
         }
@@ -365,19 +369,27 @@ __device__ __forceinline__ void offer_bound(int vectors, int kk, float top, TopS
         sh.bound[warp] = least;
         sh.next[warp] = next;
     }
-    if (threadIdx.x == 0) sh.count = 0;
+    if (threadIdx.x == 0) {
+        sh.count = 0;
+        sh.more = more;
+    }
 }
 template <int THREADS>
-__device__ __forceinline__ uint32_t common_bound(int vectors, int kk, const TopShared& sh) {
-    const int lane = threadIdx.x & 31, warps = min(THREADS / 32, vectors / 32);
-    uint32_t bound = __reduce_min_sync(0xFFFFFFFFu, sh.bound[lane & (THREADS / 32 - 1)]);
-    if (warps * 32 < kk) return bound;
-    uint32_t next = lane < warps ? sh.next[lane] : 0, r_th = 0xFFFFFFFFu;
-    for (int r = kk % warps; r > 0; --r) {
-        r_th = __reduce_max_sync(0xFFFFFFFFu, next);
-        if (lane == __ffs(__ballot_sync(0xFFFFFFFFu, next == r_th)) - 1) next = 0;
+__device__ __forceinline__ uint32_t common_bound(const TopShared& sh) {
+    constexpr int WARPS = THREADS / 32;
+    const int lane = threadIdx.x & 31, r = sh.more;
+    uint32_t bound = sh.bound[lane & (WARPS - 1)];
+    if (r > 0 && lane < WARPS) {                                     // (the r largest of the next ones: fewer than r are above)
+        const uint32_t mine = sh.next[lane];
+        int above = 0;
+#pragma unroll
+        for (int w = 0; w < WARPS; w += 2) {
+            const uint2 two = *reinterpret_cast<const uint2*>(&sh.next[w]);
+            above += (two.x > mine) + (two.y > mine);
+        }
+        if (above < r) bound = min(bound, mine);
     }
-    return min(bound, r_th);
+    return __reduce_min_sync(0xFFFFFFFFu, bound);
 }
 
 // After it: the entries from the bound on.  Each warp looks again at the stretches of its own lanes that reach it; their logits are in L1 or L2 by now.
@@ -573,23 +585,35 @@ __global__ void __launch_bounds__(Plan::THREADS, Plan::PER_SM) logprobs_kernel(c
     RowSums x = merged<32>(mine.x, warp_max_nan(mine.x.m), kd);
     if (lane == 0) sums[warp] = x;
     __syncthreads();
-    x = sums[lane & (THREADS / 32 - 1)];
-    const float m = warp_max_nan(x.m);
-    const bool odd = is_odd(m);
-    float logs = 0.f, H = 0.f;
-    if (odd) odd_row<T, THREADS>(z, V, m, p.c, odd_sums, logs, H);
-    auto tell = [&]() {
+    // One warp tells about the row; where its maximum is odd, all of them sum it again first.
+    auto tell = [&](bool odd, float logs, float H) {
         if (warp != 0) return;
-        x = merged<THREADS / 32>(x, m, kd);
+        if (!odd) {
+            x = sums[lane & (THREADS / 32 - 1)];
+            x = merged<THREADS / 32>(x, warp_max_nan(x.m), kd);
+        }
         if (lane == 0) result = tell_row(p, row, x, kd, odd, logs, H, token >= 0 && token < V ? token : -1, token_logit);
     };
+    auto tell_odd = [&]() {
+        float logs, H;
+        odd_row<T, THREADS>(z, V, result.m, p.c, odd_sums, logs, H);
+        tell(true, logs, H);
+    };
     if (TOP) {
-        const uint32_t bound = common_bound<THREADS>(part.vectors, p.k, sh);
-        gather<T, THREADS, SEGMENTS>(part, bound, span_log2, own.segment + own.STRIDE * threadIdx.x, own.hit[warp], head, rest, sh, tell);
+        const uint32_t bound = common_bound<THREADS>(sh);
+        gather<T, THREADS, SEGMENTS>(part, bound, span_log2, own.segment + own.STRIDE * threadIdx.x, own.hit[warp], head, rest, sh, [&]() { tell(false, 0.f, 0.f); });
         __syncthreads();
+        if (is_odd(result.m)) {
+            tell_odd();
+            __syncthreads();
+        }
         select<T, THREADS, Plan::AHEAD ? 4 : 1>(part, V, p.k, bound, sh, [&](int at, uint64_t e) { tell_top(p, row, at, e, result); });
     } else {
-        tell();
+        tell(false, 0.f, 0.f);
+        if (is_odd(warp_max_nan(sums[lane & (THREADS / 32 - 1)].m))) {
+            __syncthreads();
+            tell_odd();
+        }
     }
 }
 
