@@ -518,13 +518,15 @@ __device__ __forceinline__ int span_of(int vectors) {                    // log2
 //   8192 rows of 4000 bf16, k = 5         26 us         35 us           -
 //   4000 rows of 10000, k = 20             -            28 us          38 us
 //   2048 rows of 32000, k = 32             -            53 us          37 us       (fewer warps than hide the loads' latency)
-// and 512 where there is an SM for every row (one row of 32000, k = 20: 6.4 us, with 256 threads 6.6; the next loads ahead: 6.1).  SINGLE: a row is few enough
+// and 512 where all rows run at a time even so: three to an SM (300 rows of 128000, k = 20: 24.6 us, with 256 threads 29.6; 300 of 32000, k = 0: 6.6, with 256
+// 7.6; with alternatives rows of up to 64 KB gain nothing: 160 of 32000, k = 20: 10.3, with 256 8.5), or an SM for every row (one row of 32000, k = 20: 6.4 us, with 256 threads 6.6; the next loads ahead: 6.1).  SINGLE: a row is few enough
 // rounds that each is a stretch.  KEEP: the row stays in L1 for the second look at it (2048 rows of 32000, k = 32: 36.9 us, without 39.3; rows of 200 KB:
 // 48 us, without 45).
 struct TinyRow { static constexpr int THREADS = 64, SEGMENTS = 4, PER_SM = 20; static constexpr bool SINGLE = true, AHEAD = false, KEEP = true; };
 struct ShortRow { static constexpr int THREADS = 128, SEGMENTS = 4, PER_SM = 10; static constexpr bool SINGLE = true, AHEAD = false, KEEP = true; };
 struct MiddleRow { static constexpr int THREADS = 256, SEGMENTS = 4, PER_SM = 6; static constexpr bool SINGLE = true, AHEAD = false, KEEP = true; };
 struct LongRow { static constexpr int THREADS = 256, SEGMENTS = 16, PER_SM = 6; static constexpr bool SINGLE = false, AHEAD = false, KEEP = false; };
+struct FewRow { static constexpr int THREADS = 512, SEGMENTS = 8, PER_SM = 3; static constexpr bool SINGLE = false, AHEAD = false, KEEP = false; };
 struct LoneRow { static constexpr int THREADS = 512, SEGMENTS = 8, PER_SM = 1; static constexpr bool SINGLE = false, AHEAD = true, KEEP = true; };
 
 template <typename T, typename Plan, bool TOP>
@@ -755,6 +757,7 @@ static cudaError_t launch_logprobs(const LogprobArgs& p, cudaStream_t st) {
     if (row_bytes <= 8 << 10 && p.k <= 32 && p.T > 20 * sms) return launch_logprobs_as<T, TinyRow>(p, st);
     if (row_bytes <= 8 << 10 || (row_bytes <= 32 << 10 && p.T > sms)) return launch_logprobs_as<T, ShortRow>(p, st);
     if (p.T <= sms) return launch_logprobs_as<T, LoneRow>(p, st);
+    if (p.T <= FewRow::PER_SM * sms && (p.k == 0 || row_bytes > 64 << 10)) return launch_logprobs_as<T, FewRow>(p, st);
     if (row_bytes <= 64 << 10) return launch_logprobs_as<T, MiddleRow>(p, st);
     return launch_logprobs_as<T, LongRow>(p, st);
 }

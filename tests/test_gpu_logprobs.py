@@ -147,7 +147,7 @@ def test_ties_and_orders(V, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("T,V,k", [(3100, 1000, 20), (3100, 1501, 32), (170, 7000, 20), (170, 12001, 64), (170, 30000, 20), (160, 60011, 33), (20, 40000, 64)])
+@pytest.mark.parametrize("T,V,k", [(3100, 1000, 20), (3100, 1501, 32), (170, 7000, 20), (170, 12001, 64), (170, 30000, 20), (160, 60011, 33), (460, 40000, 33), (20, 40000, 64)])
 def test_odd_rows_among_many(T, V, k, dtype):
     """The rows of the tests above among as many others as make every way of sharing rows out take them: each with the oracle, the others with
     themselves in a batch where the odd rows are not."""
