@@ -3,12 +3,12 @@
 //     s = sum exp d_j,    log p_j = d_j - log s,    H = log s - (sum exp(d_j) d_j) / s
 // in one pass over the row: every thread keeps its own maximum and sums relative to it and corrects them when the maximum moves.
 // Bound by HBM in the long run (2 bytes a bf16 logit: 16000 rows of 32000 in 156 us, the time of a copy of as many bytes), by the beginning and end of the
-// launch where it is short (888 rows, all that run at a time: 13.7 us, each 888 more: 9.0; 2048 rows: 25.9 us, 5.1 TB/s) and by instructions where there are
-// alternatives (k = 32: 36.2 us; 4096 rows of 128000, k = 20: 179 us, 5.9 TB/s).  A logit takes 1 exponential of the special-function unit, whose 16 a
+// launch where it is short (888 rows, all that run at a time: 13.7 us, each 888 more: 9.0; 2048 rows: 25.6 us, 5.1 TB/s) and by instructions where there are
+// alternatives (k = 32: 36.3 us; 4096 rows of 128000, k = 20: 173 us, 6.1 TB/s).  A logit takes 1 exponential of the special-function unit, whose 16 a
 // clock and SM are 57 % busy at 5.1 TB/s, and some 4.5 other instructions: maximum and clamp of two bf16 at once, a fused multiply-add, two sums in pairs.
 // The alternatives cost no sorting: see offer_bound.
 // Timed and taken out: blocks that stay, with a ring of copies ahead in shared memory (2048 x 32000: 27 - 35 us: fewer warps fit); clusters that share a
-// row (one token, k = 20: 8.6 us on 8 blocks, 6.1 on one); the next round's loads ahead of the sums (26.7 us); 512 or 1024 threads to a row (28, 52 us).
+// row (one token, k = 20: 8.6 us on 8 blocks, 6.1 then on one); the next round's loads ahead of the sums (26.7 us); 512 or 1024 threads to a row (28, 52 us).
 #include "common.cuh"
 #include "device_state.h"
 #include "f32x2.cuh"
@@ -518,10 +518,11 @@ __device__ __forceinline__ int span_of(int vectors) {                    // log2
 //   8192 rows of 4000 bf16, k = 5         26 us         35 us           -
 //   4000 rows of 10000, k = 20             -            28 us          38 us
 //   2048 rows of 32000, k = 32             -            53 us          37 us       (fewer warps than hide the loads' latency)
-// and 512 where all rows run at a time even so: three to an SM (300 rows of 128000, k = 20: 24.6 us, with 256 threads 29.6; 300 of 32000, k = 0: 6.6, with 256
-// 7.6; with alternatives rows of up to 64 KB gain nothing: 160 of 32000, k = 20: 10.3, with 256 8.5), or an SM for every row (one row of 32000, k = 20: 6.4 us, with 256 threads 6.6; the next loads ahead: 6.1).  SINGLE: a row is few enough
-// rounds that each is a stretch.  KEEP: the row stays in L1 for the second look at it (2048 rows of 32000, k = 32: 36.9 us, without 39.3; rows of 200 KB:
-// 48 us, without 45).
+// and 512 where all rows run at a time even so, three to an SM (300 rows of 128000, k = 20: 24.6 us, with 256 threads 29.6; 300 of 32000, k = 0: 6.4, with 256
+// 7.6; with alternatives rows of up to 64 KB gain nothing: 160 of 32000, k = 20: 10.3, with 256 8.5), or an SM to every row, with the next round's loads
+// ahead (one row of 32000, k = 20: 5.6 us).
+// SINGLE: a row has so few rounds that each is a stretch.  KEEP: the row stays in L1 for the second look at it (2048 rows of 32000, k = 32: 36.9 us,
+// without 39.3; rows of 200 KB: 48 us, without 45).
 struct TinyRow { static constexpr int THREADS = 64, SEGMENTS = 4, PER_SM = 20; static constexpr bool SINGLE = true, AHEAD = false, KEEP = true; };
 struct ShortRow { static constexpr int THREADS = 128, SEGMENTS = 4, PER_SM = 10; static constexpr bool SINGLE = true, AHEAD = false, KEEP = true; };
 struct MiddleRow { static constexpr int THREADS = 256, SEGMENTS = 4, PER_SM = 6; static constexpr bool SINGLE = true, AHEAD = false, KEEP = true; };
