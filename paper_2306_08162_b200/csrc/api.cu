@@ -50,12 +50,12 @@ int check_logits(int T, int V, long long row_stride, int dtype, float inv_temper
 
 // Whether two [T, V] tensors of rows that lie apart share memory.  (Different strides in the same stretch of memory: taken to.)
 bool rows_overlap(const void* a, long long stride_a, const void* b, long long stride_b, int T, int V, size_t bytes) {
-    const long long pa = (long long)reinterpret_cast<uintptr_t>(a), pb = (long long)reinterpret_cast<uintptr_t>(b), size = (long long)bytes;
-    const long long end_a = pa + ((T - 1) * stride_a + V) * size, end_b = pb + ((T - 1) * stride_b + V) * size;
-    if (end_a <= pb || end_b <= pa) return false;
+    typedef __int128 wide;                                            // (any stride that fits a long long)
+    const wide pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b), size = bytes, length = V * size;
+    if (pa + (T - 1) * size * stride_a + length <= pb || pb + (T - 1) * size * stride_b + length <= pa) return false;
     if (T == 1 || stride_a != stride_b) return true;
-    const long long by = (pb > pa ? pb - pa : pa - pb) % (stride_a * size);   // (columns of one buffer may lie beside each other)
-    return by < V * size || stride_a * size - by < V * size;
+    const wide by = (pb > pa ? pb - pa : pa - pb) % (size * stride_a);   // (columns of one buffer may lie beside each other)
+    return by < length || size * stride_a - by < length;
 }
 
 // `step`: the whole step (else only the gradients are used).

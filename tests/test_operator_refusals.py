@@ -48,6 +48,7 @@ def test_token_logprobs_bwd_arguments(ql):
     assert status(ld=128, out=OK) == -1 and status(logits=big, out=big + 200) == -1 and status(logits=big, out=big + 16) == -1
     assert status(logits=big, ld=256, gld=256, out=big + 2 * (256 + 99)) == -1 and status(logits=big, ld=256, gld=256, out=big - 2 * 99) == -1
     assert status(logits=big, ld=128, gld=300, out=big - 2 * (3 * 300 + 99)) == -1 and status(T=1, logits=big, out=big + 198) == -1
+    assert status(logits=big, ld=1 << 60, gld=1 << 61, out=big + 1000) == -1 and status(logits=big, ld=1 << 62, gld=1 << 62, out=big + 198) == -1
     # beside them in one buffer, or right behind: nothing wrong with that (what is refused, later on, is an address)
     assert status(logits=big, ld=256, gld=256, out=big + 2 * 128, gl=OK + 4) == -3 and status(logits=big, out=big + 2 * 400, gl=OK + 4) == -3
     assert status(out=2 * OK + 1) == -3 and status(dtype=2, logits=OK + 2) == -3 and status(gl=OK + 4) == -3
