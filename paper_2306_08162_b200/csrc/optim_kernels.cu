@@ -408,10 +408,12 @@ template <typename G, int CAP>
 __global__ void __launch_bounds__(OP_THREADS) grad_norm_cluster_kernel(const __grid_constant__ OptTable<CAP> tab, float prescale, float max_norm, float* __restrict__ out) {
     __shared__ double sums[OP_CLUSTER];
     pdl_launch_dependents();
+    asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");    // this block has begun: the others may write to its shared memory
     const uint32_t chunks = tab.first[tab.n], c = chunks * blockIdx.x / OP_CLUSTER, stop = chunks * (blockIdx.x + 1) / OP_CLUSTER;
     const int j = c < stop ? tensor_of_chunk(tab, c) : 0;
     pdl_wait();
     double acc = block_sum(squares_of<G>(tab, j, c, stop));
+    asm volatile("barrier.cluster.wait;" ::: "memory");
     if (threadIdx.x == 0) {
         uint32_t at;
         asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(&sums[blockIdx.x])));
