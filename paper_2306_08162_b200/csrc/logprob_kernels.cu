@@ -20,7 +20,7 @@ constexpr int LP_UNROLL = 4;             // 16-byte vectors that a thread has on
 constexpr int LP_CANDIDATES = 640;       // entries that are put in order together (a row of less than 64 vectors has fewer logits)
 constexpr int LP_HITS = 64;              // stretches that a warp looks at again
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float LP_FLOOR = -0x1p96f, LP_LEAST = -0x1p80f, LP_MOST = 0x1p60f;     // see RowSums
+constexpr float LP_FLOOR = -0x1p96f, LP_LEAST = -0x1p80f, LP_ODD = 0x1p24f;       // see RowSums
 
 __device__ __forceinline__ float lp_f(float x) { return x; }
 __device__ __forceinline__ float lp_f(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -151,8 +151,10 @@ __device__ __forceinline__ float entry_logit(uint64_t e) { return key_logit((uin
 
 // A maximum m and sums relative to it in base 2: with kd = c log2(e) and r = m kd as it is rounded,
 //     s = sum 2^x_j,   a = sum 2^x_j x_j,   x_j = z_j kd - r   (one fused multiply-add: an error of half a place of x_j, not of z_j kd)
-// For that 2^-30 <= c <= 2^30, logits below LP_FLOOR count as that (-inf among them: 2^x is 0 and 2^x x is 0, not NaN), r is at least
-// LP_LEAST kd, and rows whose maximum is not between LP_LEAST and LP_MOST are summed again in another way (odd_row).
+// For that 2^-30 <= c <= 2^30, logits below LP_FLOOR count as that (-inf among them: 2^x is 0 and 2^x x is 0, not NaN), and r is at least
+// LP_LEAST kd.  The maximum's own x is the rounding error of r, half a place of m kd: below LP_ODD = 2^24 at most a half, but 128 and more from 2^31 on, where
+// 2^x leaves fp32's range.  Rows with |m| kd from LP_ODD on are summed again from the differences (odd_row).  A thread whose own maximum is that large
+// in a row that is not (masked logits) may hold infinite sums: its maximum lies far enough below the row's for rebase to drop them.
 struct RowSums {
     float m, s, a;
 };
@@ -185,8 +187,8 @@ __device__ __forceinline__ RowSums merged(RowSums x, float m, float kd) {
     return x;
 }
 
-// log s and the entropy of a row whose maximum m is finite but too large or too small for the sums above (a row masked by the type's lowest value
-// altogether, say): from the differences to m themselves, by the whole block.
+// log s and the entropy of a row whose maximum m is finite but too far from zero for the sums above (a row masked altogether by a large negative number,
+// a temperature near zero): from the differences to m themselves, by the whole block.
 template <typename T, int THREADS>
 __device__ __noinline__ void odd_row(const T* z, int V, float m, float c, float* sums, float& logs, float& H) {
     float s = 0.f, a = 0.f;
@@ -506,7 +508,7 @@ __device__ __forceinline__ void tell_top(const LogprobArgs& p, int row, int at, 
     if (p.top_ids != nullptr) p.top_ids[(long long)row * p.k + at] = entry_place(e);
     if (p.top_logprobs != nullptr) p.top_logprobs[(long long)row * p.k + at] = r.none ? -INFINITY : (entry_logit(e) - r.m) * p.c - r.logs;
 }
-__device__ __forceinline__ bool is_odd(float m) { return fabsf(m) < INFINITY && !(m > LP_LEAST && m < LP_MOST); }
+__device__ __forceinline__ bool is_odd(float m, float kd) { return fabsf(m) < INFINITY && !(fabsf(m) * kd < LP_ODD); }
 template <int THREADS, int SEGMENTS>
 __device__ __forceinline__ int span_of(int vectors) {                    // log2 of the rounds that make a stretch
     const int round = LP_UNROLL * THREADS, rounds = (vectors + round - 1) / round;
@@ -606,14 +608,14 @@ __global__ void __launch_bounds__(Plan::THREADS, Plan::PER_SM) logprobs_kernel(c
         const uint32_t bound = common_bound<THREADS>(sh);
         gather<T, THREADS, SEGMENTS>(part, bound, span_log2, own.segment + own.STRIDE * threadIdx.x, own.hit[warp], head, rest, sh, [&]() { tell(false, 0.f, 0.f); });
         __syncthreads();
-        if (is_odd(result.m)) {
+        if (is_odd(result.m, kd)) {
             tell_odd();
             __syncthreads();
         }
         select<T, THREADS, Plan::AHEAD ? 4 : 1>(part, V, p.k, bound, sh, [&](int at, uint64_t e) { tell_top(p, row, at, e, result); });
     } else {
         tell(false, 0.f, 0.f);
-        if (is_odd(warp_max_nan(sums[lane & (THREADS / 32 - 1)].m))) {
+        if (is_odd(warp_max_nan(sums[lane & (THREADS / 32 - 1)].m), kd)) {
             __syncthreads();
             tell_odd();
         }

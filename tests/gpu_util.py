@@ -76,3 +76,18 @@ class GpuLayer:
 
 def to_f64(t: torch.Tensor) -> np.ndarray:
     return t.detach().to(torch.float64).cpu().numpy()
+
+
+def agree(got, want, absolute, relative) -> None:
+    """Fails unless got is within absolute + relative |want| of want where both are finite, and the same infinity or NaN everywhere else (a
+    tolerance relative to an infinity would take any number for it)."""
+    got = to_f64(got) if isinstance(got, torch.Tensor) else np.asarray(got, np.float64)
+    want = to_f64(want) if isinstance(want, torch.Tensor) else np.asarray(want, np.float64)
+    assert got.shape == want.shape, (got.shape, want.shape)
+    finite = np.isfinite(got) & np.isfinite(want)
+    off = np.where(finite, np.abs(np.where(finite, got, 0.0) - np.where(finite, want, 0.0)), 0.0)
+    bound = np.where(finite, absolute + relative * np.abs(np.where(finite, want, 0.0)), 0.0)
+    fine = np.where(finite, off <= bound, (got == want) | (np.isnan(got) & np.isnan(want)))
+    if not fine.all():
+        at = np.unravel_index(np.argmin(fine), fine.shape) if fine.ndim else ()
+        raise AssertionError(f"{int((~fine).sum())} of {fine.size} differ, the first at {tuple(int(i) for i in at)}: {got[at]!r}, {want[at]!r} wanted, bound {bound[at]!r}")
