@@ -166,7 +166,7 @@ __device__ __forceinline__ float inverse_ftz(float x) {
 
 // The step of a block with 8-bit states.  It is bound by instructions, so arithmetic goes by pairs and one square root serves the update and the state.
 struct AdamBlock {                                                   // what holds for the whole call
-    float f, keep, rate, root_inv2;
+    float f, minus_decay, rate, root_inv2;                           // -lr weight_decay (1 - lr weight_decay, rounded, would be off by up to half of 2^-24 at every step)
     uint32_t step_term;
 };
 // The tensors from the chunk's first element on.  (The same for the whole block; a thread adds 32 bits to them.)
@@ -204,7 +204,7 @@ __device__ __forceinline__ void adamw8_block(const Chunk<P, G, uint8_t>& t, cons
         u[i] = make_f2(root_ftz(lo_of(v)), root_ftz(hi_of(v)));
         const f2 den = fma2(u[i], both(k.root_inv2), both(sc.eps));
         const f2 q = mul2(mul2(m[i], both(-k.rate)), make_f2(inverse_ftz(lo_of(den)), inverse_ftz(hi_of(den))));
-        const f2 wi = fma2(make_f2(w[2 * i], w[2 * i + 1]), both(k.keep), q);
+        const f2 old_w = make_f2(w[2 * i], w[2 * i + 1]), wi = add2(old_w, fma2(old_w, both(k.minus_decay), q));
         w[2 * i] = lo_of(wi);
         w[2 * i + 1] = hi_of(wi);
         fold_top(top_m, m[i]);
@@ -264,7 +264,7 @@ __device__ __forceinline__ void adamw32_block(const Chunk<P, G, float>& t, const
         const float gi = k.f * g[i];
         m[i] = fmaf(sc.beta1, m[i], sc.one_minus_beta1 * gi);
         v[i] = fmaf(sc.beta2, v[i], sc.one_minus_beta2 * (gi * gi));
-        w[i] = fmaf(w[i], k.keep, -__fdividef(k.rate * m[i], fmaf(fast_sqrt(v[i]), k.root_inv2, sc.eps)));
+        w[i] += fmaf(w[i], k.minus_decay, -__fdividef(k.rate * m[i], fmaf(fast_sqrt(v[i]), k.root_inv2, sc.eps)));
     }
     if (t.master != nullptr) store8<FULL>(t.master, base, lane, left, w);
     store8<FULL>(t.param, base, lane, left, w);
@@ -297,8 +297,7 @@ __global__ void __launch_bounds__(OP_THREADS, 4) adamw_kernel(const __grid_const
         root_inv2 = corr[1];
     }
     if (!(fabsf(f) < INFINITY)) return;
-    const float keep = 1.f - lr * sc.weight_decay, rate = lr * inv1;
-    const AdamBlock k{f, keep, rate, root_inv2, (uint32_t)step * 0x7F4A7C15u};
+    const AdamBlock k{f, -lr * sc.weight_decay, lr * inv1, root_inv2, (uint32_t)step * 0x7F4A7C15u};
     const uint32_t base = warp * OP_BLOCK;
     const int left = min(n - (int)base, OP_BLOCK);
     if constexpr (EIGHT) {
