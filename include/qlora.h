@@ -281,7 +281,8 @@ int qlora_grad_norm(const qlora_adamw_desc* desc, float prescale, float max_norm
  * as zeros).  A code is one of the two e4m3 neighbours of value / scale, the upper one (in size) with a chance that is the
  * value's share of the step, decided by a hash of the element's place in its tensor and the number of the step: nearest
  * rounding would hold v still, as it changes by a thousandth a step where codes lie a sixteenth apart.  A root above zero
- * stays above zero.  The weights are updated with the moments before they are rounded. */
+ * stays above zero.  The weights are updated with the moments before they are rounded.
+ * v itself is an fp32 number before its root is taken: squares (1 - beta2) g^2 below 2^-126 lose bits, below 2^-150 they are 0. */
 int qlora_adamw(const qlora_adamw_desc* desc, double lr, int step, const float* lr_dev, const int32_t* step_dev,
                 const float* norm, void* cuda_stream);
 
