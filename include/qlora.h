@@ -209,9 +209,9 @@ enum { QLORA_BF16 = 0, QLORA_FP16 = 1, QLORA_FP32 = 2, QLORA_E4M3 = 3 };
  *     top_ids[t, i], top_logprobs[t, i] = the i-th largest logit's place and its log p, i < k; equal logits (-0 and 0
  *                          among them) in the order of their places
  *     stats[t, 0 .. 2]   = max_j z_j,  log sum_j exp(c (z_j - max z)),  entropy    (what the backward call reads)
- * logits: dtype QLORA_BF16, QLORA_FP16 or QLORA_FP32, [T, V] with rows row_stride >= V elements apart; unlike the other
- * tensors they may begin at any element (a vocabulary of an odd size, a batch without its first token).  tokens: int32
- * [T], or NULL when logprobs is NULL.  logprobs, entropy: fp32 [T]; top_ids int32 [T, k], top_logprobs fp32 [T, k]; stats
+ * logits: dtype QLORA_BF16, QLORA_FP16 or QLORA_FP32, [T, V] with rows row_stride >= V elements apart.  tokens: int32
+ * [T], or NULL when logprobs is NULL.  Unlike the other tensors these two may begin at any element (a vocabulary of an odd
+ * size; a text without its last row of logits and its first token).  logprobs, entropy: fp32 [T]; top_ids int32 [T, k], top_logprobs fp32 [T, k]; stats
  * fp32 [T, 3]; each of them may be NULL, not all.  0 <= k <= QLORA_MAX_TOP and k <= V (k = 0: no alternatives; both
  * arrays NULL); 2^-30 <= inv_temperature <= 2^30; V <= 2^24.
  * Masked logits (-inf, or the type's lowest value) have probability 0 and add nothing to the sums; a row with nothing
@@ -226,7 +226,7 @@ int qlora_token_logprobs(int T, int V, long long row_stride, int dtype, const vo
 /* Gradient of qlora_token_logprobs with respect to the logits, for upstream gradients of the log probabilities and of the
  * entropies (the alternatives carry none):
  *     dlogits[t, j] = c * ( d_logprobs[t] ([j == tokens[t]] - p_j) - d_entropy[t] p_j (log p_j + entropy[t]) )
- * stats: the forward call's, for the same logits and inv_temperature.  d_logprobs, d_entropy: fp32 [T]; one of them may be
+ * stats: the forward call's, for the same logits and inv_temperature.  tokens as there.  d_logprobs, d_entropy: fp32 [T]; one of them may be
  * NULL (tokens too, where d_logprobs is).  A row whose token is outside [0, V) takes no d_logprobs.  A row without a
  * gradient (both zero) gets zeros, whatever its logits and stats hold.  dlogits: the type of logits, [T, V] with rows
  * grad_stride >= V elements apart (what lies between the rows is left as it was); may be the logits themselves

@@ -11,6 +11,7 @@ namespace {
 
 using namespace qlora;
 
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
@@ -191,7 +192,7 @@ int qlora_token_logprobs(int T, int V, long long row_stride, int dtype, const vo
     if (T == 0) return QLORA_OK;
     if (!logits || (!logprobs && !entropy && !top_ids && !top_logprobs && !stats)) return QLORA_ERR_INVALID_ARG;
     if ((logprobs && !tokens) || ((top_ids || top_logprobs) != (k > 0))) return QLORA_ERR_INVALID_ARG;
-    if (!element_aligned(logits, dtype) || !aligned16(tokens) || !aligned16(logprobs) || !aligned16(entropy) || !aligned16(top_ids) ||
+    if (!element_aligned(logits, dtype) || !aligned4(tokens) || !aligned16(logprobs) || !aligned16(entropy) || !aligned16(top_ids) ||
         !aligned16(top_logprobs) || !aligned16(stats))
         return QLORA_ERR_ALIGNMENT;
     return launch_token_logprobs(T, V, row_stride, dtype, logits, tokens, inv_temperature, k, logprobs, entropy, top_ids, top_logprobs, stats,
@@ -208,7 +209,7 @@ int qlora_token_logprobs_bwd(int T, int V, long long row_stride, int dtype, cons
     if (!logits || !stats || !dlogits || (!d_logprobs && !d_entropy) || (d_logprobs && !tokens)) return QLORA_ERR_INVALID_ARG;
     const bool in_place = logits == dlogits && (T == 1 || row_stride == grad_stride);
     if (!in_place && rows_overlap(logits, row_stride, dlogits, grad_stride, T, V, element_bytes(dtype))) return QLORA_ERR_INVALID_ARG;
-    if (!element_aligned(logits, dtype) || !element_aligned(dlogits, dtype) || !aligned16(tokens) || !aligned16(stats) ||
+    if (!element_aligned(logits, dtype) || !element_aligned(dlogits, dtype) || !aligned4(tokens) || !aligned16(stats) ||
         !aligned16(d_logprobs) || !aligned16(d_entropy))
         return QLORA_ERR_ALIGNMENT;
     return launch_token_logprobs_bwd(T, V, row_stride, dtype, logits, tokens, inv_temperature, stats, d_logprobs, d_entropy, grad_stride, dlogits,
