@@ -214,10 +214,13 @@ enum { QLORA_BF16 = 0, QLORA_FP16 = 1, QLORA_FP32 = 2, QLORA_E4M3 = 3 };
  * size; a text without its last row of logits and its first token).  logprobs, entropy: fp32 [T]; top_ids int32 [T, k], top_logprobs fp32 [T, k]; stats
  * fp32 [T, 3]; each of them may be NULL, not all.  0 <= k <= QLORA_MAX_TOP and k <= V (k = 0: no alternatives; both
  * arrays NULL); 2^-30 <= inv_temperature <= 2^30; V <= 2^24.
- * Masked logits (-inf, or the type's lowest value) have probability 0 and add nothing to the sums; a row with nothing
- * above -inf has log p = -inf everywhere and entropy 0; a row that holds a NaN or +inf has no distribution: its numbers
+ * Masked logits (-inf, or a number far below the row's largest) have probability 0 and add nothing to the sums; a row of
+ * nothing but one finite number is uniform, whatever the number; a row with nothing above -inf has log p = -inf everywhere
+ * and entropy 0; a row that holds a NaN or +inf has no distribution: its numbers
  * are NaN, its places are ordered all the same (a NaN counts as larger than anything).
- * fp32 arithmetic, fixed-order sums (bitwise reproducible).  The logits are read once. */
+ * fp32 arithmetic, fixed-order sums (bitwise reproducible).  A row is read once, but for a second look at the places where
+ * its alternatives may be; it is read again as a whole where more than some hundred logits may be among them (many equal
+ * ones), and where inv_temperature |max z| is 1.16e7 or more. */
 #define QLORA_MAX_TOP 64
 int qlora_token_logprobs(int T, int V, long long row_stride, int dtype, const void* logits, const int32_t* tokens,
                          float inv_temperature, int k, float* logprobs, float* entropy, int32_t* top_ids,

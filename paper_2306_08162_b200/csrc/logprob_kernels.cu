@@ -2,9 +2,10 @@
 // respect to the logits.  Per row, with c the inverse temperature, m = max z and d_j = c (z_j - m) <= 0:
 //     s = sum exp d_j,    log p_j = d_j - log s,    H = log s - (sum exp(d_j) d_j) / s
 // in one pass over the row: every thread keeps its own maximum and sums relative to it and corrects them when the maximum moves.
-// Bound by HBM in the long run (2 bytes a bf16 logit: 16000 rows of 32000 in 156 us, the time of a copy of as many bytes), by the beginning and end of the
-// launch where it is short (888 rows, all that run at a time: 13.7 us, each 888 more: 9.0; 2048 rows: 25.6 us, 5.1 TB/s) and by instructions where there are
-// alternatives (k = 32: 36.3 us; 4096 rows of 128000, k = 20: 173 us, 6.1 TB/s).  A logit takes 1 exponential of the special-function unit, whose 16 a
+// Bound by HBM in the long run (2 bytes a bf16 logit: 16000 rows of 32000 in 153 us, the time of a copy of as many bytes), by the beginning and end of the
+// launch where it is short (888 rows, all that run at a time: 12.6 us; 2048 rows: 26 us, 5.0 TB/s) and, where there are alternatives, by the end of each row, when
+// its block has no load on its way: at k = 20 some 9600 of a row's 24700 cycles go to merge, bound, second look and order, with issue 62 % and DRAM 45 % busy
+// (k = 32: 36.6 us; 4096 rows of 128000, k = 20: 173 us, 6.1 TB/s).  A logit takes 1 exponential of the special-function unit, whose 16 a
 // clock and SM are 57 % busy at 5.1 TB/s, and some 4.5 other instructions: maximum and clamp of two bf16 at once, a fused multiply-add, two sums in pairs.
 // The alternatives cost no sorting: see offer_bound.
 // Timed and taken out: blocks that stay, with a ring of copies ahead in shared memory (2048 x 32000: 27 - 35 us: fewer warps fit); clusters that share a
@@ -189,6 +190,7 @@ __device__ __forceinline__ RowSums merged(RowSums x, float m, float kd) {
 
 // log s and the entropy of a row whose maximum m is finite but too far from zero for the sums above (a row masked altogether by a large negative number,
 // a temperature near zero): from the differences to m themselves, by the whole block.
+// (Logit by logit: 2048 such rows of 32000 take 69 us.)
 template <typename T, int THREADS>
 __device__ __noinline__ void odd_row(const T* z, int V, float m, float c, float* sums, float& logs, float& H) {
     float s = 0.f, a = 0.f;
@@ -521,8 +523,8 @@ __device__ __forceinline__ int span_of(int vectors) {                    // log2
 //   4000 rows of 10000, k = 20             -            28 us          38 us
 //   2048 rows of 32000, k = 32             -            53 us          37 us       (fewer warps than hide the loads' latency)
 // and 512 where all rows run at a time even so, three to an SM (300 rows of 128000, k = 20: 24.6 us, with 256 threads 29.6; 300 of 32000, k = 0: 6.4, with 256
-// 7.6; with alternatives rows of up to 64 KB gain nothing: 160 of 32000, k = 20: 10.3, with 256 8.5), or an SM to every row, with the next round's loads
-// ahead (one row of 32000, k = 20: 5.6 us).
+// 7.6; with alternatives rows of up to 64 KB gain at some numbers and lose at others: 200 of 32000, k = 20: 11.2, with 256 12.7; 296: 12.4 and 9.9), or an SM to
+// every row, with the next round's loads ahead (one row of 32000, k = 20: 5.9 us).
 // SINGLE: a row has so few rounds that each is a stretch.  KEEP: the row stays in L1 for the second look at it (2048 rows of 32000, k = 32: 36.9 us,
 // without 39.3; rows of 200 KB: 48 us, without 45).
 struct TinyRow { static constexpr int THREADS = 64, SEGMENTS = 4, PER_SM = 20; static constexpr bool SINGLE = true, AHEAD = false, KEEP = true; };
@@ -734,7 +736,7 @@ __global__ void __launch_bounds__(LP_BWD_THREADS, 8) logprobs_bwd_kernel(const _
     }
 }
 
-// Rows that begin at different places: one logit at a time.
+// Rows that begin at different places: one logit at a time, 2 bytes a load (2048 x 32000 bf16: 138 us, where rows that begin alike take 44).
 template <typename T>
 __global__ void __launch_bounds__(LP_BWD_THREADS) logprobs_bwd_scalar_kernel(const __grid_constant__ BwdArgs p) {
     pdl_launch_dependents();

@@ -1,9 +1,10 @@
 // The optimizer step of the trainable pairs (Section 3.2, Eq. 3 of the paper: theta_l is optimised, theta_q stays): the global norm of
 // all gradients, and AdamW over every tensor of a model in one launch, with 32-bit or 8-bit states.
-// 32-bit states: bound by HBM.  Rank 32 on all projections of 32 layers (80 M elements in 448 tensors, bf16 weights, 24 bytes an element): 280 us, 6.9 TB/s;
-// rank 64 with fp32 master weights behind the norm: 796 us, where the step's bytes alone take 734 at the copy rate and the gradients' second reading 98.
-// 8-bit states: 12 bytes an element leave some 65 instructions an element at the copy rate; the step takes 55, two fifths of them on the integer pipe, whose
-// rate is half of fp32's: the same 80 M elements in 173 us, 5.6 TB/s, 231 us behind the norm.
+// 32-bit states: bound by HBM.  Rank 32 on all projections of 32 layers (80 M elements in 448 tensors, bf16 weights, 24 bytes an element): 277 us, 6.9 TB/s;
+// rank 64 with fp32 master weights behind the norm: 803 us, where the step's bytes alone take 734 at the copy rate and the gradients' second reading 98.
+// 8-bit states: the same 80 M elements in 177 us, 5.4 TB/s, 234 us behind the norm, where their bytes take 147.  No unit is full: 58 instructions an element are 130 us
+// of issue, which is 74 % busy, two fifths of them on the integer pipe (some 60 %), DRAM 57 %; 62 registers a thread leave 43 % of the warps to cover the latencies.
+// Rate and step number from device memory stand ahead of the loads: 192 us.
 // A block of threads has one chunk, 8 elements a thread, and ends: with more of them in a loop (2 to 8, with or without the next one's loads ahead) the
 // blocks of an SM load and compute in step with each other, 190 to 290 us.
 #include <cuda_fp8.h>
@@ -140,7 +141,7 @@ __device__ __forceinline__ void store8(E* p, uint32_t base, uint32_t lane, int l
 }
 
 // (The errors of this root and of the update's quotient are 2^-22 of an update that is a small part of its weight.  Not the form that takes numbers below
-// 2^-126 for zero: a second moment there has a root of up to 2^-63, far above the smallest eps.  In the 8-bit step that costs 1.2 %.)
+// 2^-126 for zero: a second moment there has a root of up to 2^-63, far above the smallest eps.  In the 8-bit step that costs 1.2 % of its time.)
 __device__ __forceinline__ float fast_sqrt(float x) {
     float r;
     asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -160,7 +161,7 @@ __device__ __forceinline__ float inverse_ftz(float x) {
     return r;
 }
 
-// The step of a block with 8-bit states.  It is bound by instructions, so arithmetic goes by pairs and one square root serves the update and the state.
+// The step of a block with 8-bit states.  Instructions are most of its time, so arithmetic goes by pairs and one square root serves the update and the state.
 struct AdamBlock {                                                   // what holds for the whole call
     float f, minus_decay, rate, root_inv2;                           // -lr weight_decay (1 - lr weight_decay, rounded, would be off by up to half of 2^-24 at every step)
     uint32_t step_term;
