@@ -185,6 +185,40 @@ int qlora_bwd_lora_static(const qlora_desc* desc, int M, const void* X, const vo
 int qlora_pack(int bits, int K, int N, const uint8_t* codes, int32_t* Q, void* cuda_stream);
 int qlora_unpack(int bits, int K, int N, const int32_t* Q, uint8_t* codes, void* cuda_stream);
 
+/* Adapters of many requests or tasks beside one frozen projection (Section 1: one quantized base, a small pair for every task):
+ * token t of the batch has adapter a = adapter_of[t], or none where that is outside [0, n_adapters).
+ *     H[t]  = X[t] A_a^T                      Y[t]  = Y_base[t]  + scales[a] H[t] B_a^T
+ *     G[t]  = dY[t] B_a                       dX[t] = dX_base[t] + scales[a] G[t] A_a
+ *     dA_a  = scales[a] sum G[t]^T X[t]       dB_a  = scales[a] sum dY[t]^T H[t]        (sums over the tokens of a)
+ * Y_base and dX_base are what the shared projection gives, e.g. qlora_fwd and qlora_bwd_input with r = 0. */
+typedef struct {
+    int K;          /* input features */
+    int N;          /* output features */
+    int r;          /* rank, 8 .. 64 in steps of 8; adapters of lower ranks are held with rows of A and columns of B that are zero */
+    int n_adapters; /* at most 65535 */
+} qlora_adapters_desc;
+
+/* Bytes of scratch for M tokens, for all three calls. */
+int qlora_adapters_workspace_bytes(const qlora_adapters_desc* desc, int M, size_t* out);
+
+/* X bf16 [M, K]; adapter_of int32 [M]; A bf16 [n_adapters, r, K]; B bf16 [n_adapters, N, r]; scales fp32 [n_adapters] (alpha / r of
+ * each).  Y_base, Y: bf16 [M, N]; Y may be Y_base, any other overlap of the two is refused.  H_out: fp32 [M, r] or NULL; rows of tokens without an adapter are 0.
+ * A token without an adapter has Y = Y_base bit for bit; what an adapter holds reaches its own tokens only.  Any order of tokens is right; with
+ * many tokens those of one adapter should lie together, as the rows of one request do, or its matrices are read for each of their places.
+ * adapter_of and scales may begin at any element.  Sums are fp32; s P enters the second product as two bf16 (16 bits), or in fp32 with up to 256 tokens. */
+int qlora_adapters_fwd(const qlora_adapters_desc* desc, int M, const void* X, const int32_t* adapter_of, const void* A, const void* B, const float* scales,
+                       const void* Y_base, void* Y, float* H_out, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* dY bf16 [M, N]; dX_base, dX bf16 [M, K]; G_out fp32 [M, r] or NULL.  Everything else as above. */
+int qlora_adapters_bwd_input(const qlora_adapters_desc* desc, int M, const void* dY, const int32_t* adapter_of, const void* A, const void* B,
+                             const float* scales, const void* dX_base, void* dX, float* G_out, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* dA fp32 [n_adapters, r, K], dB fp32 [n_adapters, N, r].  H, G: what the two calls above have left, or NULL to recompute them here (A, B are
+ * needed for that only).  accumulate = 0 overwrites dA and dB, with zeros for an adapter without tokens; 1 adds to them. */
+int qlora_adapters_bwd_lora(const qlora_adapters_desc* desc, int M, const void* X, const void* dY, const int32_t* adapter_of, const void* A, const void* B,
+                            const float* scales, const float* H, const float* G, float* dA, float* dB, int accumulate, void* workspace,
+                            size_t workspace_bytes, void* cuda_stream);
+
 /* Fused LREC training loss and its gradient (Section 3.2, Eq. 1-2): per token, with p = softmax(student logits) and
  * q = softmax(teacher logits) over the V vocabulary entries,
  *     loss_tokens[t] = lambda_kl * sum_i p_i log(p_i / q_i)  +  lambda_ce * ( -log p[labels[t]] )

@@ -381,6 +381,34 @@ def token_logprobs_backward(logits, tokens, c: float, d_logprobs, d_entropy):
 
 
 # ----------------------------------------------------------------------------------------------
+# Adapters of many requests beside one frozen projection: token t has adapter adapter_of[t], or none where that is no adapter's number.
+# ----------------------------------------------------------------------------------------------
+def adapters_forward(X, adapter_of, A, B, scales, base):
+    """(Y, H): Y[t] = base[t] + scales[a] (X[t] A_a^T) B_a^T.  A [L, r, K], B [L, N, r]; float64, a loop over the tokens."""
+    X, A, B, Y = (np.asarray(v, np.float64) for v in (X, A, B, base))
+    Y, H = Y.copy(), np.zeros((X.shape[0], A.shape[1]))
+    for t, a in enumerate(adapter_of):
+        if 0 <= int(a) < A.shape[0]:
+            H[t] = A[int(a)] @ X[t]
+            Y[t] += float(scales[int(a)]) * (B[int(a)] @ H[t])
+    return Y, H
+
+
+def adapters_backward(X, dY, adapter_of, A, B, scales, base):
+    """(dX, G, dA, dB): dX[t] = base[t] + scales[a] (dY[t] B_a) A_a, and the gradients of every adapter's pair."""
+    X, dY, A, B, dX = (np.asarray(v, np.float64) for v in (X, dY, A, B, base))
+    dX, G, dA, dB = dX.copy(), np.zeros((X.shape[0], A.shape[1])), np.zeros_like(A), np.zeros_like(B)
+    for t, a in enumerate(adapter_of):
+        if 0 <= int(a) < A.shape[0]:
+            a, s = int(a), float(scales[int(a)])
+            G[t] = dY[t] @ B[a]
+            dX[t] += s * (G[t] @ A[a])
+            dA[a] += s * np.outer(G[t], X[t])
+            dB[a] += s * np.outer(dY[t], A[a] @ X[t])
+    return dX, G, dA, dB
+
+
+# ----------------------------------------------------------------------------------------------
 # The optimizer step of the trainable pairs (Section 3.2, Eq. 3; the paper does not name the optimizer): AdamW, and the factor that
 # clips the gradients' global norm.
 # ----------------------------------------------------------------------------------------------

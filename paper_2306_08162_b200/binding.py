@@ -33,9 +33,18 @@ class _AdamwDesc(ctypes.Structure):
                 ("weight_decay", ctypes.c_double)]
 
 
+class _AdaptersDesc(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_int), ("N", ctypes.c_int), ("r", ctypes.c_int), ("n_adapters", ctypes.c_int)]
+
+
 def desc(bits: int, group_size: int, K: int, N: int, r: int, alpha: float) -> _Desc:
     """Layer descriptor (qlora_desc)."""
     return _Desc(int(bits), int(group_size), int(K), int(N), int(r), float(alpha))
+
+
+def adapters_desc(K: int, N: int, r: int, n_adapters: int) -> _AdaptersDesc:
+    """Descriptor (qlora_adapters_desc) of the adapters of one projection."""
+    return _AdaptersDesc(int(K), int(N), int(r), int(n_adapters))
 
 
 def library_path() -> str:
@@ -78,12 +87,18 @@ def library() -> ctypes.CDLL:
     lib.qlora_token_logprobs_bwd.argtypes = [i32, i32, i64, i32, vp, vp, f32, vp, vp, vp, i64, vp, vp]
     lib.qlora_grad_norm.argtypes = [ap, f32, f32, vp, vp, sz, vp]
     lib.qlora_adamw.argtypes = [ap, f64, i32, vp, vp, vp, vp]
+    dd = ctypes.POINTER(_AdaptersDesc)
+    lib.qlora_adapters_workspace_bytes.argtypes = [dd, i32, ctypes.POINTER(sz)]
+    lib.qlora_adapters_fwd.argtypes = [dd, i32] + [vp] * 9 + [sz, vp]
+    lib.qlora_adapters_bwd_input.argtypes = [dd, i32] + [vp] * 9 + [sz, vp]
+    lib.qlora_adapters_bwd_lora.argtypes = [dd, i32] + [vp] * 10 + [i32, vp, sz, vp]
     lib.qlora_device_status.argtypes = [ctypes.POINTER(ctypes.c_uint), i32]
     lib.qlora_selftest_bounded_wait.argtypes = [i32, vp]
     for name in ("qlora_workspace_bytes", "qlora_fwd", "qlora_bwd_input", "qlora_bwd_input_db", "qlora_bwd_lora", "qlora_bwd_lora_static", "qlora_fwd_dropout", "qlora_bwd_input_dropout",
                  "qlora_bwd_lora_dropout", "qlora_pack",
                  "qlora_unpack", "qlora_dequant", "qlora_quantize_rtn", "qlora_gather_columns", "qlora_lrec_loss", "qlora_device_status", "qlora_selftest_bounded_wait",
-                 "qlora_token_logprobs", "qlora_token_logprobs_bwd", "qlora_grad_norm", "qlora_adamw"):
+                 "qlora_token_logprobs", "qlora_token_logprobs_bwd", "qlora_grad_norm", "qlora_adamw",
+                 "qlora_adapters_workspace_bytes", "qlora_adapters_fwd", "qlora_adapters_bwd_input", "qlora_adapters_bwd_lora"):
         getattr(lib, name).restype = i32
     _lib = lib
     return lib
@@ -95,7 +110,7 @@ def _native():
     if _calls is None:
         library()
         from . import _pycall
-        _pycall.set_desc_types((_Desc, _AdamwDesc))
+        _pycall.set_desc_types((_Desc, _AdamwDesc, _AdaptersDesc))
         _calls = _pycall
     return _calls
 
@@ -407,6 +422,53 @@ def qlora_adamw(d, lr, step, norm=None, stream=None):
         step, step_dev = 0, step
     _operands(where, device, (lr_dev, _torch.float32, (1,)), (step_dev, _torch.int32, (1,)), (norm, _torch.float32, (2,)))
     rc = _native().qlora_adamw(d, lr, step, lr_dev, step_dev, norm, stream)
+    if rc != 0:
+        raise QloraError(rc, where)
+
+
+def qlora_adapters_workspace_bytes(d: _AdaptersDesc, M: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(library().qlora_adapters_workspace_bytes(ctypes.byref(d), int(M), ctypes.byref(out)), "qlora_adapters_workspace_bytes")
+    return int(out.value)
+
+
+def _adapters_operands(where, d, M, adapter_of, A, B, scales, workspace, *more):
+    if not isinstance(d, _AdaptersDesc):
+        raise TypeError(f"{where}: the adapters' descriptor must come from adapters_desc()")
+    torch = _torch or _load_torch()
+    device, bf16, L, r = _current_device(where), torch.bfloat16, d.n_adapters, d.r
+    _operands(where, device, (adapter_of, torch.int32, (M,)), (A, bf16, (L, r, d.K)), (B, bf16, (L, d.N, r)), (scales, torch.float32, (L,)),
+              *((t, torch.float32 if low else bf16, shape) for t, low, shape in more))
+    if workspace is not None and workspace.get_device() != device:
+        raise ValueError(f"{where}: tensors must be on the current CUDA device, got {workspace.device}")
+
+
+def qlora_adapters_fwd(d, M, X, adapter_of, A, B, scales, Y_base, Y, H_out, workspace, stream=None, workspace_bytes=None):
+    """Y[t] = Y_base[t] + scales[a] (X[t] A_a^T) B_a^T with a = adapter_of[t] (none outside [0, n_adapters)); Y may be Y_base, H_out may be None."""
+    where = "qlora_adapters_fwd"
+    _adapters_operands(where, d, M, adapter_of, A, B, scales, workspace, (X, False, (M, d.K)), (Y_base, False, (M, d.N)), (Y, False, (M, d.N)),
+                       (H_out, True, (M, d.r)))
+    rc = _native().qlora_adapters_fwd(d, M, X, adapter_of, A, B, scales, Y_base, Y, H_out, workspace, workspace_bytes, stream)
+    if rc != 0:
+        raise QloraError(rc, where)
+
+
+def qlora_adapters_bwd_input(d, M, dY, adapter_of, A, B, scales, dX_base, dX, G_out, workspace, stream=None, workspace_bytes=None):
+    """dX[t] = dX_base[t] + scales[a] (dY[t] B_a) A_a; dX may be dX_base, G_out may be None."""
+    where = "qlora_adapters_bwd_input"
+    _adapters_operands(where, d, M, adapter_of, A, B, scales, workspace, (dY, False, (M, d.N)), (dX_base, False, (M, d.K)), (dX, False, (M, d.K)),
+                       (G_out, True, (M, d.r)))
+    rc = _native().qlora_adapters_bwd_input(d, M, dY, adapter_of, A, B, scales, dX_base, dX, G_out, workspace, workspace_bytes, stream)
+    if rc != 0:
+        raise QloraError(rc, where)
+
+
+def qlora_adapters_bwd_lora(d, M, X, dY, adapter_of, A, B, scales, H, G, dA, dB, accumulate, workspace, stream=None, workspace_bytes=None):
+    """dA fp32 [n_adapters, r, K] and dB fp32 [n_adapters, N, r] of every adapter; H and G as the calls above left them, or None (recomputed)."""
+    where = "qlora_adapters_bwd_lora"
+    _adapters_operands(where, d, M, adapter_of, A, B, scales, workspace, (X, False, (M, d.K)), (dY, False, (M, d.N)), (H, True, (M, d.r)), (G, True, (M, d.r)),
+                       (dA, True, (d.n_adapters, d.r, d.K)), (dB, True, (d.n_adapters, d.N, d.r)))
+    rc = _native().qlora_adapters_bwd_lora(d, M, X, dY, adapter_of, A, B, scales, H, G, dA, dB, accumulate, workspace, workspace_bytes, stream)
     if rc != 0:
         raise QloraError(rc, where)
 

@@ -86,6 +86,13 @@ int check_adamw(const qlora_adamw_desc* d, bool step) {
     return QLORA_OK;
 }
 
+int check_adapters(const qlora_adapters_desc* d) {
+    if (d == nullptr || d->K < 0 || d->N < 0 || d->r < 0 || d->n_adapters < 0) return QLORA_ERR_INVALID_ARG;
+    if (d->K % 32 != 0 || d->N % 8 != 0 || d->r % 8 != 0 || d->r == 0 || d->r > 64 || d->n_adapters > 65535) return QLORA_ERR_UNSUPPORTED;
+    return QLORA_OK;
+}
+size_t adapters_low_bytes(const qlora_adapters_desc& d, int M) { return align_up((size_t)M * (size_t)d.r * sizeof(float), 256); }
+
 struct Workspace {
     size_t p0_off, p1_off, grad_off, sync_off, split_off, db_off;
     size_t required;   // what a call cannot do without
@@ -233,6 +240,78 @@ int qlora_adamw(const qlora_adamw_desc* desc, double lr, int step, const float* 
     if ((!lr_dev && !(lr - lr == 0.0)) || (!step_dev && step < 1)) return QLORA_ERR_INVALID_ARG;      // a finite rate, steps from 1
     if (!aligned16(lr_dev) || !aligned16(step_dev) || !aligned16(norm)) return QLORA_ERR_ALIGNMENT;
     return launch_adamw(*desc, lr, step, lr_dev, step_dev, norm, (cudaStream_t)cuda_stream);
+}
+
+int qlora_adapters_workspace_bytes(const qlora_adapters_desc* desc, int M, size_t* out) {
+    if (out == nullptr || M < 0) return QLORA_ERR_INVALID_ARG;
+    const int rc = check_adapters(desc);
+    if (rc != QLORA_OK) return rc;
+    *out = align_up(2 * adapters_low_bytes(*desc, M), 256) + 256;
+    return QLORA_OK;
+}
+
+// Forward: In = X [M, K], Base and Out [M, N].  Backward: In = dY [M, N], Base and Out [M, K].
+static int adapters_common(bool forward, const qlora_adapters_desc* desc, int M, const void* In, const int32_t* adapter_of, const void* A, const void* B,
+                           const float* scales, const void* Base, void* Out, float* low, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    int rc = check_adapters(desc);
+    if (rc != QLORA_OK) return rc;
+    if (M < 0) return QLORA_ERR_INVALID_ARG;
+    const qlora_adapters_desc& d = *desc;
+    const int T = forward ? d.K : d.N, C = forward ? d.N : d.K;
+    if (M == 0 || C == 0) return QLORA_OK;
+    if ((!In && T > 0) || !adapter_of || (d.n_adapters > 0 && (!A || !B || !scales)) || !Base || !Out) return QLORA_ERR_INVALID_ARG;
+    if (Base != Out && rows_overlap(Base, C, Out, C, M, C, 2)) return QLORA_ERR_INVALID_ARG;
+    if (!aligned16(In) || !aligned4(adapter_of) || !aligned16(A) || !aligned16(B) || !aligned4(scales) || !aligned16(Base) || !aligned16(Out) ||
+        !aligned16(low) || !aligned16(workspace))
+        return QLORA_ERR_ALIGNMENT;
+    if (workspace == nullptr || workspace_bytes < 2 * adapters_low_bytes(d, M)) return QLORA_ERR_WORKSPACE;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    const void *L1 = forward ? A : B, *L2 = forward ? B : A;
+    if (adapters_few(M)) return launch_adapters_few(M, T, C, d.r, d.n_adapters, forward, In, adapter_of, L1, L2, scales, Base, Out, low, st);
+    float* P = low ? low : static_cast<float*>(workspace);
+    rc = launch_adapters_down(M, T, d.r, d.n_adapters, forward, In, adapter_of, L1, P, st);
+    if (rc != QLORA_OK) return rc;
+    return launch_adapters_up(M, C, d.r, d.n_adapters, forward, P, adapter_of, L2, scales, Base, Out, st);
+}
+
+int qlora_adapters_fwd(const qlora_adapters_desc* desc, int M, const void* X, const int32_t* adapter_of, const void* A, const void* B, const float* scales,
+                       const void* Y_base, void* Y, float* H_out, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    return adapters_common(true, desc, M, X, adapter_of, A, B, scales, Y_base, Y, H_out, workspace, workspace_bytes, cuda_stream);
+}
+
+int qlora_adapters_bwd_input(const qlora_adapters_desc* desc, int M, const void* dY, const int32_t* adapter_of, const void* A, const void* B,
+                             const float* scales, const void* dX_base, void* dX, float* G_out, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    return adapters_common(false, desc, M, dY, adapter_of, A, B, scales, dX_base, dX, G_out, workspace, workspace_bytes, cuda_stream);
+}
+
+int qlora_adapters_bwd_lora(const qlora_adapters_desc* desc, int M, const void* X, const void* dY, const int32_t* adapter_of, const void* A, const void* B,
+                            const float* scales, const float* H, const float* G, float* dA, float* dB, int accumulate, void* workspace,
+                            size_t workspace_bytes, void* cuda_stream) {
+    int rc = check_adapters(desc);
+    if (rc != QLORA_OK) return rc;
+    if (M < 0 || (accumulate != 0 && accumulate != 1)) return QLORA_ERR_INVALID_ARG;
+    const qlora_adapters_desc& d = *desc;
+    if (d.n_adapters == 0 || (d.K == 0 && d.N == 0)) return QLORA_OK;
+    if ((!dA && d.K > 0) || (!dB && d.N > 0) || !scales) return QLORA_ERR_INVALID_ARG;
+    if (M > 0 && ((!X && d.K > 0) || (!dY && d.N > 0) || !adapter_of || (!H && !A) || (!G && !B))) return QLORA_ERR_INVALID_ARG;
+    if (!aligned16(X) || !aligned16(dY) || !aligned4(adapter_of) || !aligned16(A) || !aligned16(B) || !aligned4(scales) || !aligned16(H) || !aligned16(G) ||
+        !aligned16(dA) || !aligned16(dB) || !aligned16(workspace))
+        return QLORA_ERR_ALIGNMENT;
+    if (workspace == nullptr || workspace_bytes < 2 * adapters_low_bytes(d, M)) return QLORA_ERR_WORKSPACE;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (M > 0 && !H) {
+        float* Hs = static_cast<float*>(workspace);
+        rc = launch_adapters_down(M, d.K, d.r, d.n_adapters, true, X, adapter_of, A, Hs, st);
+        if (rc != QLORA_OK) return rc;
+        H = Hs;
+    }
+    if (M > 0 && !G) {
+        float* Gs = reinterpret_cast<float*>(static_cast<char*>(workspace) + adapters_low_bytes(d, M));
+        rc = launch_adapters_down(M, d.N, d.r, d.n_adapters, false, dY, adapter_of, B, Gs, st);
+        if (rc != QLORA_OK) return rc;
+        G = Gs;
+    }
+    return launch_adapters_grads(M, d.K, d.N, d.r, d.n_adapters, X, dY, adapter_of, scales, H, G, dA, dB, accumulate, st);
 }
 
 int qlora_gather_columns(int elem_bytes, int rows, int cols, const void* in, const int32_t* perm, void* out, void* cuda_stream) {

@@ -30,6 +30,19 @@ int launch_token_logprobs_bwd(int T, int V, long long row_stride, int dtype, con
 int launch_grad_norm(const qlora_adamw_desc& d, float prescale, float max_norm, float* out, void* workspace, cudaStream_t st);
 int launch_adamw(const qlora_adamw_desc& d, double lr, int step, const float* lr_dev, const int32_t* step_dev, const float* norm, cudaStream_t st);
 
+// adapter_kernels.cu -- adapters of many requests: L [n_adapters, ...], the adapter of each row of In in adapter_of (none outside [0, n_adapters))
+// P[m, :] = In[m, :] L_a (rows without an adapter: 0); l_is_A: L = A [., r, T], else B [., T, r]
+int launch_adapters_down(int M, int T, int r, int n_adapters, bool l_is_A, const void* In, const int32_t* adapter_of, const void* L, float* P, cudaStream_t st);
+// Out[m, :] = Base[m, :] + scales[a] P[m, :] L_a; from_B: L = B [., C, r], else A [., r, C]; Out may be Base
+int launch_adapters_up(int M, int C, int r, int n_adapters, bool from_B, const float* P, const int32_t* adapter_of, const void* L, const float* scales,
+                       const void* Base, void* Out, cudaStream_t st);
+// Both in one launch, for so few rows.  forward: L1 = A, L2 = B, else the reverse; P_out may be NULL.
+bool adapters_few(int M);
+int launch_adapters_few(int M, int T, int C, int r, int n_adapters, bool forward, const void* In, const int32_t* adapter_of, const void* L1, const void* L2,
+                        const float* scales, const void* Base, void* Out, float* P_out, cudaStream_t st);
+int launch_adapters_grads(int M, int K, int N, int r, int n_adapters, const void* X, const void* dY, const int32_t* adapter_of, const float* scales,
+                          const float* H, const float* G, float* dA, float* dB, int accumulate, cudaStream_t st);
+
 // simt_kernels.cu -- CUDA-core kernels, correct for every supported shape
 // In [M, T] bf16 times the dequantised weight, plus s * P L.  transposed = false: forward (T = K, C = N);
 // true: backward-input (T = N, C = K).  P fp32 [M, r] (H or G) may be NULL when r == 0.

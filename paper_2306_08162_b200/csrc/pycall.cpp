@@ -16,7 +16,8 @@
 namespace {
 
 PyObject* g_desc_type = nullptr;                     // the ctypes structure of qlora_desc
-PyObject* g_adamw_type = nullptr;                    // ... and of qlora_adamw_desc
+PyObject* g_adamw_type = nullptr;                    // ... of qlora_adamw_desc
+PyObject* g_adapters_type = nullptr;                 // ... and of qlora_adapters_desc
 PyObject *s_is_contiguous, *s_data_ptr, *s_cuda_stream, *s_numel, *s_element_size, *s_current_stream;
 PyObject *g_torch_cuda = nullptr, *g_get_device = nullptr, *g_raw_stream = nullptr;
 bool g_cuda_ready = false;                           // torch has initialised CUDA in this process
@@ -107,6 +108,8 @@ bool to_arg(PyObject* const* args, size_t i, size_t n, T* out) {
         return to_desc(a, g_desc_type, "the layer descriptor must come from desc()", out);
     } else if constexpr (std::is_same_v<T, const qlora_adamw_desc*>) {
         return to_desc(a, g_adamw_type, "the optimizer descriptor must come from adamw_desc()", out);
+    } else if constexpr (std::is_same_v<T, const qlora_adapters_desc*>) {
+        return to_desc(a, g_adapters_type, "the adapters' descriptor must come from adapters_desc()", out);
     } else if constexpr (std::is_pointer_v<T>) {
         void* p = nullptr;
         if (!(i + 1 == n ? to_stream(a, &p) : to_pointer(a, &p))) return false;
@@ -167,12 +170,14 @@ template <auto Fn>
 PyObject* py_call(PyObject*, PyObject* const* args, Py_ssize_t n) { return checked_call(Fn, args, n); }
 
 PyObject* py_set_desc_types(PyObject*, PyObject* types) {
-    PyObject *layer, *adamw;
-    if (!PyArg_ParseTuple(types, "OO", &layer, &adamw)) return nullptr;
+    PyObject *layer, *adamw, *adapters;
+    if (!PyArg_ParseTuple(types, "OOO", &layer, &adamw, &adapters)) return nullptr;
     Py_INCREF(layer);
     Py_XSETREF(g_desc_type, layer);
     Py_INCREF(adamw);
     Py_XSETREF(g_adamw_type, adamw);
+    Py_INCREF(adapters);
+    Py_XSETREF(g_adapters_type, adapters);
     Py_RETURN_NONE;
 }
 
@@ -182,6 +187,7 @@ PyMethodDef methods[] = {
     QLORA_PY(qlora_fwd_dropout), QLORA_PY(qlora_bwd_input_dropout), QLORA_PY(qlora_bwd_lora_dropout),
     QLORA_PY(qlora_gather_columns), QLORA_PY(qlora_lrec_loss), QLORA_PY(qlora_quantize_rtn),
     QLORA_PY(qlora_token_logprobs), QLORA_PY(qlora_token_logprobs_bwd), QLORA_PY(qlora_grad_norm), QLORA_PY(qlora_adamw),
+    QLORA_PY(qlora_adapters_fwd), QLORA_PY(qlora_adapters_bwd_input), QLORA_PY(qlora_adapters_bwd_lora),
     {"set_desc_types", py_set_desc_types, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
