@@ -232,6 +232,22 @@ int qlora_adapters_bwd_lora(const qlora_adapters_desc* desc, int M, const void* 
 int qlora_lrec_loss(int T, int V, const void* student_logits, const void* teacher_logits, const int32_t* labels, float lambda_kl,
                     float lambda_ce, float grad_scale, float* loss_tokens, void* dlogits, void* cuda_stream);
 
+/* Cross entropy of the model's head straight from the hidden states, and its gradient with respect to them; the [T, V] logits are never in memory:
+ *     z[t] = hidden[t] head^T,   loss_tokens[t] = log sum_v exp z[t, v] - z[t, labels[t]]
+ *     d_hidden[t] = d_loss[t] (sum_v p[t, v] head[v] - head[labels[t]]),   p = softmax(z[t])
+ * The head is frozen, as every weight of the base (Section 3.1): it has no gradient.
+ * hidden bf16 [T, D]; head bf16 [V, D]; labels int32 [T]: a token whose label is outside [0, V) has loss 0 and gradient 0 and costs nothing (padding, the
+ * tokens of a prompt); d_loss fp32 [T]: the upstream gradient of every token's loss (1 / n for the mean of n), with d_hidden bf16 [T, D]; both NULL: the loss
+ * alone.  labels, d_loss and loss_tokens may begin at any element.  d_hidden may be hidden itself; any other overlap of the two is refused.  D: a multiple of 8, 64 at least;
+ * V up to 2^24.  workspace: qlora_head_loss_workspace_bytes(T, V, D, gradient), of which the part that grows with V is 64 MB at most or three pieces of
+ * the vocabulary for 2048 tokens, and 8 bytes for every token and 256 entries.
+ * Sums, maxima and losses are fp32 (a token that is almost certain keeps its small loss and gradient); probabilities are rounded to bf16 where they
+ * enter the gradient's product.  The logits may be of any size; a block of 256 tokens is computed twice where one of them has a logit more than 83 above
+ * the largest of its first 256.  A token with a NaN or infinity among its logits has loss and gradient NaN. */
+int qlora_head_loss_workspace_bytes(int T, int V, int D, int gradient, size_t* out);
+int qlora_head_loss(int T, int V, int D, const void* hidden, const void* head, const int32_t* labels, const float* d_loss, float* loss_tokens,
+                    void* d_hidden, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 /* Element types of the tensors that the calls below take in more than one. */
 enum { QLORA_BF16 = 0, QLORA_FP16 = 1, QLORA_FP32 = 2, QLORA_E4M3 = 3 };
 

@@ -92,13 +92,16 @@ def library() -> ctypes.CDLL:
     lib.qlora_adapters_fwd.argtypes = [dd, i32] + [vp] * 9 + [sz, vp]
     lib.qlora_adapters_bwd_input.argtypes = [dd, i32] + [vp] * 9 + [sz, vp]
     lib.qlora_adapters_bwd_lora.argtypes = [dd, i32] + [vp] * 10 + [i32, vp, sz, vp]
+    lib.qlora_head_loss_workspace_bytes.argtypes = [i32, i32, i32, i32, ctypes.POINTER(sz)]
+    lib.qlora_head_loss.argtypes = [i32, i32, i32] + [vp] * 7 + [sz, vp]
     lib.qlora_device_status.argtypes = [ctypes.POINTER(ctypes.c_uint), i32]
     lib.qlora_selftest_bounded_wait.argtypes = [i32, vp]
     for name in ("qlora_workspace_bytes", "qlora_fwd", "qlora_bwd_input", "qlora_bwd_input_db", "qlora_bwd_lora", "qlora_bwd_lora_static", "qlora_fwd_dropout", "qlora_bwd_input_dropout",
                  "qlora_bwd_lora_dropout", "qlora_pack",
                  "qlora_unpack", "qlora_dequant", "qlora_quantize_rtn", "qlora_gather_columns", "qlora_lrec_loss", "qlora_device_status", "qlora_selftest_bounded_wait",
                  "qlora_token_logprobs", "qlora_token_logprobs_bwd", "qlora_grad_norm", "qlora_adamw",
-                 "qlora_adapters_workspace_bytes", "qlora_adapters_fwd", "qlora_adapters_bwd_input", "qlora_adapters_bwd_lora"):
+                 "qlora_adapters_workspace_bytes", "qlora_adapters_fwd", "qlora_adapters_bwd_input", "qlora_adapters_bwd_lora",
+                 "qlora_head_loss_workspace_bytes", "qlora_head_loss"):
         getattr(lib, name).restype = i32
     _lib = lib
     return lib
@@ -469,6 +472,30 @@ def qlora_adapters_bwd_lora(d, M, X, dY, adapter_of, A, B, scales, H, G, dA, dB,
     _adapters_operands(where, d, M, adapter_of, A, B, scales, workspace, (X, False, (M, d.K)), (dY, False, (M, d.N)), (H, True, (M, d.r)), (G, True, (M, d.r)),
                        (dA, True, (d.n_adapters, d.r, d.K)), (dB, True, (d.n_adapters, d.N, d.r)))
     rc = _native().qlora_adapters_bwd_lora(d, M, X, dY, adapter_of, A, B, scales, H, G, dA, dB, accumulate, workspace, workspace_bytes, stream)
+    if rc != 0:
+        raise QloraError(rc, where)
+
+
+def qlora_head_loss_workspace_bytes(T: int, V: int, D: int, gradient: bool) -> int:
+    out = ctypes.c_size_t(0)
+    _check(library().qlora_head_loss_workspace_bytes(int(T), int(V), int(D), 1 if gradient else 0, ctypes.byref(out)), "qlora_head_loss_workspace_bytes")
+    return int(out.value)
+
+
+def qlora_head_loss(hidden, head, labels, loss_tokens, workspace, d_loss=None, d_hidden=None, stream=None, workspace_bytes=None):
+    """Cross entropy of labels (int32 [T]; outside [0, V): none) under softmax(hidden head^T), hidden bf16 [T, D], head bf16 [V, D], into loss_tokens fp32 [T];
+    with d_loss (fp32 [T]) and d_hidden (bf16 [T, D], may be hidden itself) also its gradient with respect to hidden."""
+    where = "qlora_head_loss"
+    torch = _torch or _load_torch()
+    if hidden.dim() != 2 or head.dim() != 2:
+        raise ValueError(f"{where}: hidden is [T, D] and head [V, D]")
+    (T, D), V = hidden.shape, head.shape[0]
+    device, bf16, f32 = _current_device(where), torch.bfloat16, torch.float32
+    _operands(where, device, (hidden, bf16, (T, D)), (head, bf16, (V, D)), (labels, torch.int32, (T,)), (loss_tokens, f32, (T,)), (d_loss, f32, (T,)),
+              (d_hidden, bf16, (T, D)))
+    if workspace is not None and workspace.get_device() != device:
+        raise ValueError(f"{where}: tensors must be on the current CUDA device, got {workspace.device}")
+    rc = _native().qlora_head_loss(T, V, D, hidden, head, labels, d_loss, loss_tokens, d_hidden, workspace, workspace_bytes, stream)
     if rc != 0:
         raise QloraError(rc, where)
 

@@ -139,8 +139,11 @@ const char* qlora_status_string(int status) {
 int qlora_device_status(unsigned int* status_out, int clear) {
     if (status_out == nullptr) return QLORA_ERR_INVALID_ARG;
     if (cudaDeviceSynchronize() != cudaSuccess) return QLORA_ERR_CUDA;
-    const int rc = read_device_status(status_out, clear);
+    unsigned int head = 0;
+    int rc = read_device_status(status_out, clear);
+    if (rc == QLORA_OK) rc = read_head_status(&head, clear);
     if (rc != QLORA_OK) return rc;
+    *status_out |= head;
     return *status_out == 0 ? QLORA_OK : QLORA_ERR_TIMEOUT;
 }
 
@@ -312,6 +315,34 @@ int qlora_adapters_bwd_lora(const qlora_adapters_desc* desc, int M, const void* 
         G = Gs;
     }
     return launch_adapters_grads(M, d.K, d.N, d.r, d.n_adapters, X, dY, adapter_of, scales, H, G, dA, dB, accumulate, st);
+}
+
+static int check_head(int T, int V, int D) {
+    if (T < 0 || V < 0 || D < 0) return QLORA_ERR_INVALID_ARG;
+    if (V == 0 || V > (1 << 24) || D < 64 || D % 8 != 0 || D > (1 << 20)) return QLORA_ERR_UNSUPPORTED;
+    if (((long long)T / 256 + 1) * ((long long)V / 256 + 1 + D / 256 + 1) > (1 << 28)) return QLORA_ERR_UNSUPPORTED;   // (items of work are counted in 32 bits)
+    return QLORA_OK;
+}
+
+int qlora_head_loss_workspace_bytes(int T, int V, int D, int gradient, size_t* out) {
+    if (out == nullptr || (gradient != 0 && gradient != 1)) return QLORA_ERR_INVALID_ARG;
+    const int rc = check_head(T, V, D);
+    if (rc != QLORA_OK) return rc;
+    *out = head_loss_workspace_bytes(T > 0 ? T : 1, V, D, gradient != 0);
+    return QLORA_OK;
+}
+
+int qlora_head_loss(int T, int V, int D, const void* hidden, const void* head, const int32_t* labels, const float* d_loss, float* loss_tokens,
+                    void* d_hidden, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    const int rc = check_head(T, V, D);
+    if (rc != QLORA_OK) return rc;
+    if (T == 0) return QLORA_OK;
+    if (!hidden || !head || !labels || !loss_tokens || (d_hidden != nullptr) != (d_loss != nullptr)) return QLORA_ERR_INVALID_ARG;
+    if (d_hidden != nullptr && d_hidden != hidden && rows_overlap(hidden, D, d_hidden, D, T, D, 2)) return QLORA_ERR_INVALID_ARG;
+    if (!aligned16(hidden) || !aligned16(head) || !aligned4(labels) || !aligned4(d_loss) || !aligned4(loss_tokens) || !aligned16(d_hidden) || !aligned16(workspace))
+        return QLORA_ERR_ALIGNMENT;
+    if (workspace == nullptr || workspace_bytes < head_loss_workspace_bytes(T, V, D, d_hidden != nullptr)) return QLORA_ERR_WORKSPACE;
+    return launch_head_loss(T, V, D, hidden, head, labels, d_loss, loss_tokens, d_hidden, workspace, (cudaStream_t)cuda_stream);
 }
 
 int qlora_gather_columns(int elem_bytes, int rows, int cols, const void* in, const int32_t* perm, void* out, void* cuda_stream) {

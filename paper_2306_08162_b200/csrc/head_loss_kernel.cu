@@ -1,0 +1,659 @@
+// Cross entropy of the model's head from the hidden states, and its gradient with respect to them, without the logits in memory.
+//   z = h W^T,   loss = log sum_v exp z_v - z_label,   dh = d_loss (sum_v p_v W_v - W_label),   p = softmax(z)
+//
+// Two products, 2 T V D operations each, and nothing is computed twice: the probabilities of a piece of the vocabulary (4096 entries) go to the second
+// product as P = exp(z - ref), bf16, through a small ring that stays in L2, with one reference per token for the whole vocabulary, which is known
+// before the row's true maximum is: the largest of its first 256 logits and 40 ln 2 more.  The sums over the pieces then need no rescaling -- they are
+// divided by the row's sum of P at the end -- and bf16 has the range of fp32: nothing is lost while the row's maximum lies up to 120 ln 2 = 83 above
+// those first logits, and what flushes to zero is below 2^-86 of the largest.  A token whose largest logit lies further above is found at the end, and its block of 256 tokens is computed
+// again from its true maximum (by a second launch of the same kernel, which ends at once where there is none).
+//
+// The label's own term is kept out of P: p_label - 1 = -(sum of the others) / sum has no cancellation, and where a token is almost
+// certain the gradient would otherwise be the rounding error of P.
+//
+// Rounding: P to bf16 (a relative error of 2^-9 on average over many terms of either sign), dh to bf16; everything else is fp32.
+//
+// One persistent kernel: a pair of CTAs (two SMs) claims items of both products from one counter (head_plan.h), so there is no wave to wait for
+// between the products or the pieces.  An item is a tile of 256 x 256 (tcgen05.mma.cta_group::2, M = 256, N = 256; 128 rows and half of the other
+// operand per CTA), operands staged by TMA in six stages of 64 contraction elements, accumulators in tensor memory twice, so that the epilogue of an item
+// runs beside the products of the next.  What an item needs from others (probabilities of its rows, the previous piece's sums, a free slot
+// of the ring, the reference) it waits for through counters in the workspace; those items were claimed earlier, so the wait ends
+// whichever CTAs share the GPU.  Every wait is bounded.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "common.cuh"
+#include "device_state.h"
+#include "f32x2.cuh"
+#include "head_plan.h"
+#include "launch.h"
+#include "tcgen05.cuh"
+
+namespace qlora {
+
+__device__ unsigned int g_head_status = 0;   // sticky; bit 0: a wait gave up
+
+namespace {
+
+typedef __nv_bfloat16 bf16;
+
+constexpr int HL_THREADS = 256, HL_STAGES = 6, HL_EPI_WARP0 = 4, HL_EPI_WARPS = 4, HL_CLAIMS = 4;
+constexpr uint32_t HL_HALF = 128 * 64 * 2, HL_STAGE = 2 * HL_HALF;     // one CTA's part of an operand; of both
+constexpr uint32_t HL_SLICE = 4096;                                   // staging of an epilogue warp
+constexpr uint32_t HL_OFF_SLICES = HL_STAGES * HL_STAGE, HL_OFF_BARS = HL_OFF_SLICES + HL_EPI_WARPS * HL_SLICE;
+constexpr size_t HL_SMEM = HL_OFF_BARS + 256 + 1024;
+constexpr int HL_WAIT_US = 250000;
+constexpr uint32_t HL_SPINS = 1u << 26;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f, MOST = 3.402823466e38f;
+constexpr float REF_ABOVE = 40.f * LN2;      // the reference over the largest of the first logits
+constexpr float REF_REACH = 80.f * LN2;      // how far a logit may lie above it: sums of 2^24 terms times weights below 2^20 stay finite
+
+struct HeadParams {
+    HeadPlan plan;
+    int again;                               // the second launch: only blocks that are to be done again
+    int wait_limit_us;
+    size_t padded;                           // rows of the buffers
+    unsigned* counters;
+    const int* label;
+    float *ref, *label_logit, *tile_max, *tile_sum;
+    bf16* probs;
+    float* sums;
+};
+
+// Where the counters lie.
+__device__ __forceinline__ unsigned* ref_known(const HeadParams& p) { return p.counters + 4; }
+__device__ __forceinline__ unsigned* to_do_again(const HeadParams& p) { return p.counters + 4 + p.plan.blocks_max; }
+__device__ __forceinline__ unsigned* logits_done(const HeadParams& p) {
+    const size_t set = (size_t)head_div_up(p.plan.blocks_max, kHeadChunk) * p.plan.pieces * kHeadChunk;
+    return p.counters + 4 + 2 * p.plan.blocks_max + (p.again ? 2 * set : 0);
+}
+__device__ __forceinline__ unsigned* grads_done(const HeadParams& p) {
+    return logits_done(p) + (size_t)head_div_up(p.plan.blocks_max, kHeadChunk) * p.plan.pieces * kHeadChunk;
+}
+
+__device__ __forceinline__ bool gave_up(volatile int* abort_flag) {
+    *abort_flag = 1;
+    atomicOr(&g_head_status, 1u);
+    return false;
+}
+// Waits of a whole warp: on a barrier (all lanes see the completed phase), and on a counter in global memory (lane 0 reads, the warp's
+// barrier hands it on).  They give up after abort_flag[1] microseconds.
+__device__ __forceinline__ bool poll(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+    uint64_t t0 = 0;
+    for (uint32_t i = 0; i < HL_SPINS; ++i) {
+        if (__all_sync(0xFFFFFFFFu, mbar_try_wait_cluster(bar, parity) != 0u)) return true;
+        if ((i & 63u) == 63u) {
+            if (__any_sync(0xFFFFFFFFu, *abort_flag != 0)) return false;
+            const uint64_t now = __shfl_sync(0xFFFFFFFFu, global_ns(), 0);
+            if (t0 == 0) t0 = now;
+            else if (now - t0 > (uint64_t)abort_flag[1] * 1000ull) break;
+        }
+    }
+    return gave_up(abort_flag);
+}
+__device__ __forceinline__ bool poll_counter(const unsigned* counter, unsigned target, volatile int* abort_flag) {
+    uint64_t t0 = 0;
+    const int lane = threadIdx.x & 31;
+    for (uint32_t i = 0; i < HL_SPINS; ++i) {
+        unsigned v = 0;
+        if (lane == 0) asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(counter) : "memory");
+        if (__shfl_sync(0xFFFFFFFFu, v, 0) >= target) { __syncwarp(); return true; }
+        __nanosleep(100);
+        if ((i & 63u) == 63u) {
+            if (__any_sync(0xFFFFFFFFu, *abort_flag != 0)) return false;
+            const uint64_t now = __shfl_sync(0xFFFFFFFFu, global_ns(), 0);
+            if (t0 == 0) t0 = now;
+            else if (now - t0 > (uint64_t)abort_flag[1] * 1000ull) break;
+        }
+    }
+    return gave_up(abort_flag);
+}
+__device__ __forceinline__ void arrive_release_cluster(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+__device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
+// An epilogue warp's writes to global memory, counted in where other SMs read them (also through TMA).  Every warp counts for itself, so that none
+// waits for one that has given up: a tile is COUNTS_PER_TILE.
+constexpr unsigned COUNTS_PER_TILE = 2 * HL_EPI_WARPS;
+__device__ __forceinline__ void publish(unsigned* counter) {
+    fence_proxy_async_all();
+    __threadfence();
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(counter) : "memory");
+}
+
+template <bool GRAD>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HL_THREADS, 1)
+head_loss_kernel(const __grid_constant__ CUtensorMap tm_rows, const __grid_constant__ CUtensorMap tm_head, const __grid_constant__ CUtensorMap tm_head_t,
+                 const __grid_constant__ CUtensorMap tm_probs, const HeadParams p) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint32_t tmem_base_slot;
+    __shared__ int abort_flag_s[2];
+    __shared__ int claimed_s[HL_CLAIMS];
+    volatile int* abort_flag = abort_flag_s;
+    volatile int* claimed = claimed_s;
+    pdl_launch_dependents();
+    if (p.again) {
+        pdl_wait();
+        if (__ldcg(p.counters + 3) == 0u) return;                      // nothing to do again (the same for both CTAs of a pair)
+    }
+    const uint32_t smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* smem_gen = smem_raw + (smem0 - smem_u32(smem_raw));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t cta = cluster_ctarank();                            // 0 = leader: issues the products, claims the items
+
+    const uint32_t bar_full = smem0 + HL_OFF_BARS;                     // [stages] leader's: both CTAs' operands landed
+    const uint32_t bar_empty = bar_full + 8 * HL_STAGES;               // [stages] both: read by the products (multicast commit)
+    const uint32_t bar_acc_full = bar_empty + 8 * HL_STAGES;           // [2] both: accumulators complete (multicast commit)
+    const uint32_t bar_acc_empty = bar_acc_full + 16;                  // [2] leader's: drained by both epilogues
+    const uint32_t bar_claim_full = bar_acc_empty + 16;                // [claims] both: an item's number is there
+    const uint32_t bar_claim_empty = bar_claim_full + 8 * HL_CLAIMS;   // [claims] leader's: read by every role of both CTAs
+
+    if (threadIdx.x == 0) {
+        abort_flag_s[0] = 0;
+        abort_flag_s[1] = p.wait_limit_us;
+        for (int i = 0; i < HL_STAGES; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(bar_acc_full + 8 * i, 1); mbar_init(bar_acc_empty + 8 * i, 2 * HL_EPI_WARPS); }
+        for (int i = 0; i < HL_CLAIMS; ++i) { mbar_init(bar_claim_full + 8 * i, 1); mbar_init(bar_claim_empty + 8 * i, 2 + 1 + 2 * HL_EPI_WARPS); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_slot)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();                                                // the peer's barriers are initialised before anything arrives on them
+    tc_fence_after();
+    const uint32_t tmem_base = tmem_base_slot;
+    pdl_wait();
+
+    const HeadPlan& plan = p.plan;
+    const int n_rows = (int)__ldcg(p.counters);
+    const HeadRows rows = head_rows(plan, n_rows);
+    const int steps_d = head_div_up(plan.D, kHeadStep);
+    const uint32_t leader_claim_empty = map_to_cta(bar_claim_empty, 0);
+    auto active = [&](int block) { return block < rows.blocks && (!p.again || __ldcg(to_do_again(p) + block) != 0u); };
+    auto steps_of = [&](const HeadItem& it) { return it.of_grad ? head_div_up(head_piece_entries(plan, it.piece), kHeadStep) : steps_d; };
+
+    // What every role does for its next item: the number that the leader claimed, -1 at the end.  (leave() gives the place back.)
+    Ring claim;
+    auto next = [&](int* index) -> bool {
+        if (!poll(bar_claim_full + 8 * claim.slot, claim.phase, abort_flag)) return false;
+        *index = claimed[claim.slot];
+        __syncwarp();
+        if (lane == 0) arrive_release_cluster(leader_claim_empty + 8 * claim.slot);
+        claim.advance(HL_CLAIMS);
+        return *index >= 0;
+    };
+
+    if (warp == 2) {
+        // ------------------------------------------------------------------ claims items for the pair
+        if (cta == 0) {
+            unsigned* counter = p.counters + (p.again ? 2 : 1);
+            const uint32_t mine = smem_u32(claimed_s), peer = map_to_cta(mine, 1), peer_full = map_to_cta(bar_claim_full, 1);
+            for (bool more = true; more;) {
+                if (!poll(bar_claim_empty + 8 * claim.slot, claim.phase ^ 1u, abort_flag)) break;
+                int index = -1;
+                if (lane == 0) {
+                    for (;;) {
+                        const unsigned i = atomicAdd(counter, 1u);
+                        if ((long long)i >= rows.total) break;
+                        const HeadItem it = head_item(plan, rows, i);
+                        if (!active(it.block) || (!it.of_grad && it.tile * kHeadTile >= head_piece_entries(plan, it.piece))) continue;   // (the last piece and chunk are shorter)
+                        index = (int)i;
+                        break;
+                    }
+                    claimed[claim.slot] = index;
+                    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer + 4 * claim.slot), "r"(index) : "memory");
+                    mbar_arrive(bar_claim_full + 8 * claim.slot);
+                    arrive_release_cluster(peer_full + 8 * claim.slot);
+                }
+                more = __shfl_sync(0xFFFFFFFFu, index, 0) >= 0;
+                claim.advance(HL_CLAIMS);
+            }
+        }
+    } else if (warp == 0) {
+        // ------------------------------------------------------------------ TMA: both operands of this CTA
+        Ring ring;
+        const uint32_t leader_full = map_to_cta(bar_full, 0);
+        int index;
+        while (next(&index)) {
+            const HeadItem it = head_item(plan, rows, index);
+            const int steps = steps_of(it);
+            if (GRAD && it.of_grad) {
+                const unsigned tiles = (unsigned)head_div_up(head_piece_entries(plan, it.piece), kHeadTile);
+                if (!poll_counter(logits_done(p) + (size_t)it.q * kHeadChunk + it.block_in_chunk, COUNTS_PER_TILE * tiles, abort_flag)) goto done;
+                fence_proxy_async_all();                               // (written by other SMs' ordinary stores)
+            }
+            const int row0 = it.of_grad ? ((it.q % plan.ring) * plan.chunk_max + it.block_in_chunk) * kHeadTile + (int)cta * 128 : it.block * kHeadTile + (int)cta * 128;
+            const int other0 = it.of_grad ? it.tile * kHeadTile + (int)cta * 128 : it.piece * plan.piece + it.tile * kHeadTile + (int)cta * 128;
+            for (int step = 0; step < steps; ++step) {
+                if (!poll(bar_empty + 8 * ring.slot, ring.phase ^ 1u, abort_flag)) goto done;
+                if (elect_one()) {
+                    if (cta == 0) mbar_expect_tx(bar_full + 8 * ring.slot, 2 * HL_STAGE);
+                    const uint32_t dst = smem0 + ring.slot * HL_STAGE, bar = leader_full + 8 * ring.slot;
+                    if (GRAD && it.of_grad) {
+                        const int v = it.piece * plan.piece + step * kHeadStep;
+                        tma_load_2d_pair(dst, &tm_probs, bar, step * kHeadStep, row0);
+                        tma_load_2d_pair(dst + HL_HALF, &tm_head_t, bar, other0, v);
+                        tma_load_2d_pair(dst + HL_HALF + HL_HALF / 2, &tm_head_t, bar, other0 + 64, v);
+                    } else {
+                        tma_load_2d_pair(dst, &tm_rows, bar, step * kHeadStep, row0);
+                        tma_load_2d_pair(dst + HL_HALF, &tm_head, bar, step * kHeadStep, other0);
+                    }
+                }
+                __syncwarp();
+                ring.advance(HL_STAGES);
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ products (leader)
+        if (cta == 0) {
+            // rows: contraction-contiguous, 128-byte swizzle, 8-row groups 1024 B apart; the head likewise for the logits, and for the gradient with
+            // 64 features contiguous: 64-feature atoms 8192 B apart, groups of 8 entries 1024 B apart
+            const uint64_t a_desc0 = smem_desc(smem0, 16, 1024, 2);
+            const uint64_t b_logits = smem_desc(smem0 + HL_HALF, 16, 1024, 2), b_grad = smem_desc(smem0 + HL_HALF, 8192, 1024, 2);
+            Ring ring;
+            uint32_t n = 0;
+            int index;
+            while (next(&index)) {
+                const HeadItem it = head_item(plan, rows, index);
+                const int steps = steps_of(it);
+                const bool of_grad = GRAD && it.of_grad;
+                const uint32_t idesc = instr_desc_pair(256u, 0u, of_grad ? 1u : 0u), b_k16 = of_grad ? 2048u >> 4 : 32u >> 4;
+                const uint64_t b_desc0 = of_grad ? b_grad : b_logits;
+                const uint32_t buffer = n & 1u, acc = tmem_base + buffer * 256u;
+                if (!poll(bar_acc_empty + 8 * buffer, ((n >> 1) & 1u) ^ 1u, abort_flag)) goto done;
+                tc_fence_after();
+                for (int step = 0; step < steps; ++step) {
+                    if (!poll(bar_full + 8 * ring.slot, ring.phase, abort_flag)) goto done;
+                    tc_fence_after();
+                    const uint32_t at = ring.slot * (HL_STAGE >> 4);
+                    if (elect_one()) {
+#pragma unroll
+                        for (uint32_t k = 0; k < kHeadStep / 16; ++k)
+                            tc_mma_pair(acc, a_desc0 + at + k * 2, b_desc0 + at + k * b_k16, idesc, (uint32_t)(step > 0 || k > 0));
+                        tc_commit_pair(bar_empty + 8 * ring.slot);
+                        if (step + 1 == steps) tc_commit_pair(bar_acc_full + 8 * buffer);
+                    }
+                    __syncwarp();
+                    ring.advance(HL_STAGES);
+                }
+                ++n;
+            }
+        }
+    } else if (warp >= HL_EPI_WARP0) {
+        // ------------------------------------------------------------------ epilogue: a thread has one row
+        const int quarter = warp & 3;
+        const uint32_t leader_acc_empty = map_to_cta(bar_acc_empty, 0);
+        uint8_t* slice = smem_gen + HL_OFF_SLICES + quarter * HL_SLICE;
+        uint32_t n = 0;
+        int index;
+        for (; next(&index); ++n) {
+            const HeadItem it = head_item(plan, rows, index);
+            const uint32_t buffer = n & 1u, taddr = tmem_base + buffer * 256u + ((uint32_t)(quarter * 32) << 16);
+            const int row_w = it.block * kHeadTile + (int)cta * 128 + quarter * 32, row = row_w + lane;   // (of the buffers: row < p.padded)
+            if (GRAD && it.of_grad) {
+                // ---- a tile of the gradient's sums
+                const int set = it.piece % plan.sums;
+                const bool add = it.piece >= plan.sums;
+                if (add && !poll_counter(grads_done(p) + (size_t)(it.q - plan.sums) * kHeadChunk + it.block_in_chunk, COUNTS_PER_TILE * plan.feature_tiles, abort_flag)) break;
+                if (!poll(bar_acc_full + 8 * buffer, (n >> 1) & 1u, abort_flag)) break;
+                tc_fence_after();
+                float* out = p.sums + ((size_t)set * p.padded + row_w) * plan.D;
+                const int rows_here = n_rows - row_w;
+#pragma unroll 1
+                for (int idx = 0; idx < 8; ++idx) {
+                    const int c = it.tile * kHeadTile + 32 * idx + 4 * (lane & 7);
+                    float4 old[8];
+                    if (add) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int R = 4 * i + (lane >> 3);
+                            old[i] = R < rows_here && c < plan.D ? __ldcg(reinterpret_cast<const float4*>(out + (size_t)R * plan.D + c)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                        }
+                    }
+                    uint32_t v[32];
+                    tc_ld32(taddr + 32 * idx, v);
+                    tc_wait_ld();
+                    __syncwarp();                                      // the previous chunk has been read back
+#pragma unroll
+                    for (int c4 = 0; c4 < 8; ++c4)
+                        *reinterpret_cast<uint4*>(slice + lane * 128 + ((c4 ^ (lane & 7)) << 4)) = make_uint4(v[4 * c4], v[4 * c4 + 1], v[4 * c4 + 2], v[4 * c4 + 3]);
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int R = 4 * i + (lane >> 3);
+                        float4 x = *reinterpret_cast<const float4*>(slice + R * 128 + (((lane & 7) ^ (R & 7)) << 4));
+                        if (add) { x.x += old[i].x; x.y += old[i].y; x.z += old[i].z; x.w += old[i].w; }
+                        if (R < rows_here && c < plan.D) __stcg(reinterpret_cast<float4*>(out + (size_t)R * plan.D + c), x);
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(leader_acc_empty + 8 * buffer);
+                publish(grads_done(p) + (size_t)it.q * kHeadChunk + it.block_in_chunk);
+                continue;
+            }
+            // ---- a tile of logits
+            const int v0 = it.piece * plan.piece + it.tile * kHeadTile, valid = min(plan.V - v0, kHeadTile);
+            const int label = row < n_rows ? __ldcg(p.label + row) - v0 : -1;
+            const bool first = it.piece == 0 && it.tile == 0 && !p.again;
+            float ref = 0.f;
+            if (GRAD) {
+                if (it.q >= plan.ring) {                               // the slot's previous probabilities have been read
+                    const int before = it.q - plan.ring, block = before / plan.pieces * rows.chunk + it.block_in_chunk;
+                    if (active(block) && !poll_counter(grads_done(p) + (size_t)before * kHeadChunk + it.block_in_chunk, COUNTS_PER_TILE * plan.feature_tiles, abort_flag)) break;
+                }
+                if (!first) {
+                    if (!p.again && !poll_counter(ref_known(p) + it.block, COUNTS_PER_TILE, abort_flag)) break;
+                    ref = __ldcg(p.ref + row);
+                }
+            }
+            if (!poll(bar_acc_full + 8 * buffer, (n >> 1) & 1u, abort_flag)) break;
+            tc_fence_after();
+            if (GRAD && first) {
+                float m = -INFINITY;
+#pragma unroll 1
+                for (int idx = 0; idx < 8; ++idx) {
+                    uint32_t v[32];
+                    tc_ld32(taddr + 32 * idx, v);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (32 * idx + j < valid) m = fmaxf(m, __uint_as_float(v[j]));
+                }
+                ref = m == -INFINITY ? 0.f : fminf(m + REF_ABOVE, MOST);
+                __stcg(p.ref + row, ref);
+                publish(ref_known(p) + it.block);
+            }
+            float m = -INFINITY, s = 0.f;                              // the largest logit; the sum over the reference, or over m
+            bf16* out = nullptr;
+            if constexpr (GRAD)
+                out = p.probs + ((size_t)((it.q % plan.ring) * plan.chunk_max + it.block_in_chunk) * kHeadTile + (int)cta * 128 + quarter * 32) * plan.piece + it.tile * kHeadTile;
+            // 32 logits of the row; SPECIAL: the label or the vocabulary's end is among some row's
+            auto chunk = [&](uint32_t (&v)[32], int idx, auto special) {
+                constexpr bool SPECIAL = decltype(special)::value;
+                float sum[2] = {0.f, 0.f};
+                if constexpr (SPECIAL) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        if (32 * idx + j == label) __stcg(p.label_logit + row, __uint_as_float(v[j]));
+                        if (32 * idx + j >= valid) v[j] = 0xFF800000u;           // -inf
+                    }
+                }
+                float top = __uint_as_float(v[0]);
+#pragma unroll
+                for (int j = 1; j < 32; ++j) top = fmaxf(top, __uint_as_float(v[j]));
+                const float to = fmaxf(m, top), base = GRAD ? ref : to == -INFINITY ? 0.f : to;
+                if constexpr (!GRAD) s *= fast_exp2((m - base) * LOG2E);
+                m = to;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    float e = fast_exp2((__uint_as_float(v[j]) - base) * LOG2E);
+                    if (SPECIAL && 32 * idx + j == label) e = 0.f;
+                    sum[j & 1] += e;
+                    v[j] = __float_as_uint(e);
+                }
+                s += sum[0] + sum[1];
+                if constexpr (GRAD) {
+                    // by rows into the warp's slice, out of it so that four lanes have 64 bytes of a row
+                    __syncwarp();
+#pragma unroll
+                    for (int c8 = 0; c8 < 4; ++c8) {
+                        uint32_t o[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const __nv_bfloat162 pr = __floats2bfloat162_rn(__uint_as_float(v[c8 * 8 + 2 * j]), __uint_as_float(v[c8 * 8 + 2 * j + 1]));
+                            o[j] = *reinterpret_cast<const uint32_t*>(&pr);
+                        }
+                        *reinterpret_cast<uint4*>(slice + lane * 64 + ((c8 ^ ((lane >> 1) & 3)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int R = 8 * i + (lane >> 2);
+                        const uint4 val = *reinterpret_cast<const uint4*>(slice + R * 64 + (((lane & 3) ^ ((R >> 1) & 3)) << 4));
+                        __stcg(reinterpret_cast<uint4*>(out + (size_t)R * plan.piece + 32 * idx + 8 * (lane & 3)), val);
+                    }
+                }
+            };
+#pragma unroll 1
+            for (int idx = 0; idx < 8; ++idx) {
+                uint32_t v[32];
+                tc_ld32(taddr + 32 * idx, v);
+                tc_wait_ld();
+                const bool special = 32 * idx + 32 > valid || (label >= 32 * idx && label < 32 * idx + 32);
+                if (__any_sync(0xFFFFFFFFu, special)) chunk(v, idx, std::true_type{});
+                else chunk(v, idx, std::false_type{});
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(leader_acc_empty + 8 * buffer);
+            const size_t at = (size_t)(v0 / kHeadTile) * p.padded + row;
+            __stcg(p.tile_max + at, m);
+            __stcg(p.tile_sum + at, s);
+            if constexpr (GRAD) publish(logits_done(p) + (size_t)it.q * kHeadChunk + it.block_in_chunk);
+        }
+    }
+
+done:
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag) {   // copies that may still be in flight land before the CTA's memory is released
+        for (int i = 0; i < 200; ++i) __nanosleep(1000);
+        __syncthreads();
+    }
+    cluster_sync_all();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+    }
+}
+
+// Tokens that have a label become rows, in their order: place[t] (-1 without), the rows' labels, and the hidden states side by side.  A block takes
+// 32 tokens and counts the labels before them itself.  The counters are set to zero.
+constexpr int PREP_THREADS = 256, PREP_TOKENS = 32;
+__global__ void __launch_bounds__(PREP_THREADS)
+head_prepare_kernel(int T, int V, int D, const int32_t* __restrict__ labels, const bf16* __restrict__ hidden, int* __restrict__ place, int* __restrict__ row_label,
+                    bf16* __restrict__ rows, unsigned* __restrict__ counters, size_t counter_words) {
+    __shared__ int parts[PREP_THREADS / 32];
+    __shared__ int place_s[PREP_TOKENS];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t0 = blockIdx.x * PREP_TOKENS;
+    for (size_t i = 1 + blockIdx.x * PREP_THREADS + threadIdx.x; i < counter_words; i += (size_t)gridDim.x * PREP_THREADS) counters[i] = 0u;
+    int n = 0;
+    for (int t = threadIdx.x; t < t0; t += PREP_THREADS) n += (unsigned)__ldg(labels + t) < (unsigned)V;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xFFFFFFFFu, n, o);
+    if (lane == 0) parts[warp] = n;
+    __syncthreads();
+    if (warp == 0) {
+        int before = 0;
+#pragma unroll
+        for (int w = 0; w < PREP_THREADS / 32; ++w) before += parts[w];
+        const int t = t0 + lane, label = t < T ? __ldg(labels + t) : -1;
+        const bool has = (unsigned)label < (unsigned)V;
+        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, has);
+        const int at = has ? before + __popc(mask & ((1u << lane) - 1u)) : -1;
+        place_s[lane] = at;
+        if (t < T) place[t] = at;
+        if (has) row_label[at] = label;
+        if (lane == 0 && blockIdx.x == gridDim.x - 1) counters[0] = (unsigned)(before + __popc(mask));
+    }
+    __syncthreads();
+    const int chunks = D / 8;
+    for (int i = warp; i < PREP_TOKENS; i += PREP_THREADS / 32) {
+        if (place_s[i] < 0) continue;
+        const uint4* src = reinterpret_cast<const uint4*>(hidden + (size_t)(t0 + i) * D);
+        uint4* dst = reinterpret_cast<uint4*>(rows + (size_t)place_s[i] * D);
+#pragma unroll 4
+        for (int c = lane; c < chunks; c += 32) dst[c] = __ldg(src + c);
+    }
+}
+
+// One block per token: its loss from the tiles' sums, and its row of the gradient from the pieces' sums.
+constexpr int FIN_THREADS = 256;
+__device__ __forceinline__ float block_sum(float v, float* parts) {
+    v = warp_sum(v);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) parts[threadIdx.x >> 5] = v;
+    __syncthreads();
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < FIN_THREADS / 32; ++w) s += parts[w];
+    return s;
+}
+__device__ __forceinline__ float block_max(float v, float* parts) {
+    v = warp_max(v);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) parts[threadIdx.x >> 5] = v;
+    __syncthreads();
+    float m = parts[0];
+#pragma unroll
+    for (int w = 1; w < FIN_THREADS / 32; ++w) m = fmaxf(m, parts[w]);
+    return m;
+}
+
+template <bool GRAD>
+__global__ void __launch_bounds__(FIN_THREADS)
+head_finish_kernel(HeadParams p, const int* __restrict__ place, const bf16* __restrict__ head, const float* __restrict__ d_loss, float* __restrict__ loss,
+                   bf16* __restrict__ d_hidden) {
+    __shared__ float parts[FIN_THREADS / 32];
+    pdl_launch_dependents();
+    pdl_wait();
+    if (p.again && __ldcg(p.counters + 3) == 0u) return;
+    const int t = blockIdx.x, row = place[t], D = p.plan.D;
+    uint4* out = GRAD ? reinterpret_cast<uint4*>(d_hidden + (size_t)t * D) : nullptr;
+    if (row < 0) {
+        if (p.again) return;
+        if (threadIdx.x == 0) loss[t] = 0.f;
+        if (GRAD)
+            for (int c = threadIdx.x; c < D / 8; c += FIN_THREADS) out[c] = make_uint4(0, 0, 0, 0);
+        return;
+    }
+    if (p.again && __ldcg(to_do_again(p) + row / kHeadTile) == 0u) return;
+    const int tiles = head_div_up(p.plan.V, kHeadTile);
+    float m = -INFINITY;
+    for (int i = threadIdx.x; i < tiles; i += FIN_THREADS) m = fmaxf(m, __ldcg(p.tile_max + (size_t)i * p.padded + row));
+    m = block_max(m, parts);
+    float s = 0.f;
+    for (int i = threadIdx.x; i < tiles; i += FIN_THREADS) {
+        const float x = __ldcg(p.tile_sum + (size_t)i * p.padded + row);
+        if constexpr (GRAD) s += x;
+        else s += x * fast_exp2((__ldcg(p.tile_max + (size_t)i * p.padded + row) - m) * LOG2E);
+    }
+    const float others = block_sum(s, parts);
+    const float ref = GRAD ? __ldcg(p.ref + row) : m;
+    const float at_label = (__ldcg(p.label_logit + row) - ref) * LOG2E, mine = fast_exp2(at_label), total = others + mine;
+    if (threadIdx.x == 0) {
+        // (a label that has most of the probability: the small loss from the small sum)
+        float l = others <= mine ? log1pf(others / mine) : LN2 * (log2f(total) - at_label);
+        if (!(total < INFINITY)) l = NAN;
+        loss[t] = l;
+        if (GRAD && !p.again && m - ref > REF_REACH) {
+            p.counters[3] = 1u;
+            to_do_again(p)[row / kHeadTile] = 1u;
+            p.ref[row] = fminf(m, MOST);
+        }
+    }
+    if constexpr (GRAD) {
+        const float f = d_loss[t], share = f / total, back = -share * others;
+        const int label = __ldcg(p.label + row);
+        const uint4* w = reinterpret_cast<const uint4*>(head + (size_t)label * D);
+        const float* sums = p.sums + (size_t)row * D;
+        const bool none = f == 0.f;
+        for (int c = threadIdx.x; c < D / 8; c += FIN_THREADS) {
+            float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+            for (int k = 0; k < p.plan.sums; ++k) {
+                const float4* from = reinterpret_cast<const float4*>(sums + (size_t)k * p.padded * D) + 2 * c;
+                const float4 x = __ldcg(from), y = __ldcg(from + 1);
+                a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
+                b.x += y.x; b.y += y.y; b.z += y.z; b.w += y.w;
+            }
+            const uint4 l = __ldg(w + c);
+            const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            const uint32_t lw[4] = {l.x, l.y, l.z, l.w};
+            uint32_t o[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const __nv_bfloat162 pr = __floats2bfloat162_rn(fmaf(share, v[2 * j], back * bf16_lo(lw[j])), fmaf(share, v[2 * j + 1], back * bf16_hi(lw[j])));
+                o[j] = none ? 0u : *reinterpret_cast<const uint32_t*>(&pr);
+            }
+            out[c] = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+    }
+}
+
+}  // namespace
+
+size_t head_loss_workspace_bytes(int T, int V, int D, bool grad) { return head_layout(head_plan(T, V, D, grad ? 1 : 0), T).total; }
+
+template <bool GRAD>
+static int head_loss_impl(int T, int V, int D, const void* hidden, const void* head, const int32_t* labels, const float* d_loss, float* loss, void* d_hidden,
+                          void* workspace, cudaStream_t st) {
+    HeadParams p{};
+    p.plan = head_plan(T, V, D, GRAD ? 1 : 0);
+    const HeadLayout l = head_layout(p.plan, T);
+    char* ws = static_cast<char*>(workspace);
+    p.wait_limit_us = HL_WAIT_US;
+    p.padded = (size_t)p.plan.blocks_max * kHeadTile;
+    p.counters = reinterpret_cast<unsigned*>(ws + l.counters);
+    p.label = reinterpret_cast<int*>(ws + l.label);
+    p.ref = reinterpret_cast<float*>(ws + l.ref);
+    p.label_logit = reinterpret_cast<float*>(ws + l.label_logit);
+    p.tile_max = reinterpret_cast<float*>(ws + l.tile_max);
+    p.tile_sum = reinterpret_cast<float*>(ws + l.tile_sum);
+    p.probs = reinterpret_cast<bf16*>(ws + l.probs);
+    p.sums = reinterpret_cast<float*>(ws + l.sums);
+    int* place = reinterpret_cast<int*>(ws + l.place);
+    bf16* rows = reinterpret_cast<bf16*>(ws + l.rows);
+
+    CUtensorMap tr, th, tt{}, tp{};
+    const CUtensorMapDataType type = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    if (!make_map_2d(&tr, type, 2, rows, (uint64_t)D, p.padded, 64, 128, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !make_map_2d(&th, type, 2, head, (uint64_t)D, (uint64_t)V, 64, 128, CU_TENSOR_MAP_SWIZZLE_128B))
+        return QLORA_ERR_CUDA;
+    if (GRAD && (!make_map_2d(&tt, type, 2, head, (uint64_t)D, (uint64_t)V, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B) ||
+                 !make_map_2d(&tp, type, 2, p.probs, (uint64_t)p.plan.piece, (uint64_t)p.plan.ring * p.plan.chunk_max * kHeadTile, 64, 128, CU_TENSOR_MAP_SWIZZLE_128B)))
+        return QLORA_ERR_CUDA;
+    static SmemLimit limit;
+    auto kern = head_loss_kernel<GRAD>;
+    if (!limit.raise(kern, HL_SMEM)) return QLORA_ERR_CUDA;
+    if (launch_pdl(head_prepare_kernel, dim3((T + PREP_TOKENS - 1) / PREP_TOKENS), dim3(PREP_THREADS), 0, st, 1, T, V, D, labels, (const bf16*)hidden, place,
+                   const_cast<int*>(p.label), rows, p.counters, l.counter_words) != cudaSuccess)
+        return QLORA_ERR_CUDA;
+    const long long items = head_rows(p.plan, T).total;
+    const int pairs = (int)(items < sm_count() / 2 ? items : sm_count() / 2);
+    for (p.again = 0; p.again < (GRAD ? 2 : 1); ++p.again) {
+        if (launch_pdl(kern, dim3(2 * pairs), dim3(HL_THREADS), HL_SMEM, st, 1, tr, th, tt, tp, p) != cudaSuccess) return QLORA_ERR_CUDA;
+        if (launch_pdl(head_finish_kernel<GRAD>, dim3(T), dim3(FIN_THREADS), 0, st, 1, p, place, (const bf16*)head, d_loss, loss, (bf16*)d_hidden) != cudaSuccess)
+            return QLORA_ERR_CUDA;
+    }
+    return QLORA_OK;
+}
+
+int launch_head_loss(int T, int V, int D, const void* hidden, const void* head, const int32_t* labels, const float* d_loss, float* loss, void* d_hidden,
+                     void* workspace, cudaStream_t st) {
+    return d_hidden != nullptr ? head_loss_impl<true>(T, V, D, hidden, head, labels, d_loss, loss, d_hidden, workspace, st)
+                               : head_loss_impl<false>(T, V, D, hidden, head, labels, nullptr, loss, nullptr, workspace, st);
+}
+
+int read_head_status(unsigned int* out, int clear) {
+    unsigned int v = 0;
+    if (cudaMemcpyFromSymbol(&v, g_head_status, sizeof(v)) != cudaSuccess) return QLORA_ERR_CUDA;
+    if (clear && v != 0) {
+        const unsigned int zero = 0;
+        if (cudaMemcpyToSymbol(g_head_status, &zero, sizeof(zero)) != cudaSuccess) return QLORA_ERR_CUDA;
+    }
+    *out = v;
+    return QLORA_OK;
+}
+
+}  // namespace qlora

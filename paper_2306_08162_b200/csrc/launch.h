@@ -43,6 +43,12 @@ int launch_adapters_few(int M, int T, int C, int r, int n_adapters, bool forward
 int launch_adapters_grads(int M, int K, int N, int r, int n_adapters, const void* X, const void* dY, const int32_t* adapter_of, const float* scales,
                           const float* H, const float* G, float* dA, float* dB, int accumulate, cudaStream_t st);
 
+// head_loss_kernel.cu -- cross entropy of the head from the hidden states; d_hidden NULL: the loss alone
+size_t head_loss_workspace_bytes(int T, int V, int D, bool grad);
+int launch_head_loss(int T, int V, int D, const void* hidden, const void* head, const int32_t* labels, const float* d_loss, float* loss, void* d_hidden,
+                     void* workspace, cudaStream_t st);
+int read_head_status(unsigned int* out, int clear);
+
 // simt_kernels.cu -- CUDA-core kernels, correct for every supported shape
 // In [M, T] bf16 times the dequantised weight, plus s * P L.  transposed = false: forward (T = K, C = N);
 // true: backward-input (T = N, C = K).  P fp32 [M, r] (H or G) may be NULL when r == 0.

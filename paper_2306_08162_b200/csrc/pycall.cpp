@@ -187,7 +187,7 @@ PyMethodDef methods[] = {
     QLORA_PY(qlora_fwd_dropout), QLORA_PY(qlora_bwd_input_dropout), QLORA_PY(qlora_bwd_lora_dropout),
     QLORA_PY(qlora_gather_columns), QLORA_PY(qlora_lrec_loss), QLORA_PY(qlora_quantize_rtn),
     QLORA_PY(qlora_token_logprobs), QLORA_PY(qlora_token_logprobs_bwd), QLORA_PY(qlora_grad_norm), QLORA_PY(qlora_adamw),
-    QLORA_PY(qlora_adapters_fwd), QLORA_PY(qlora_adapters_bwd_input), QLORA_PY(qlora_adapters_bwd_lora),
+    QLORA_PY(qlora_adapters_fwd), QLORA_PY(qlora_adapters_bwd_input), QLORA_PY(qlora_adapters_bwd_lora), QLORA_PY(qlora_head_loss),
     {"set_desc_types", py_set_desc_types, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
