@@ -59,12 +59,14 @@ constexpr float REF_REACH = 80.f * LN2;      // how far a logit may lie above it
 struct HeadParams {
     HeadPlan plan;
     int again;                               // the second launch: only blocks that are to be done again
+    int tokens, copies;                      // copies: the hidden states are copied even where every token has a label
     int wait_limit_us;
     float scale;                             // log2 e, and what the products' sums lose (CUT_OFF)
     size_t padded;                           // rows of the buffers
     unsigned* counters;
     const int* label;
-    float *ref, *label_logit, *tile_max, *tile_sum;
+    float *ref, *label_logit;
+    float2* tile_stats;                      // [rows][tiles]: the largest logit, the sum
     bf16* probs;
     float* sums;
 };
@@ -133,7 +135,7 @@ __device__ __forceinline__ void publish(unsigned* counter) {
 
 template <bool GRAD>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HL_THREADS, 1)
-head_loss_kernel(const __grid_constant__ CUtensorMap tm_rows, const __grid_constant__ CUtensorMap tm_head, const __grid_constant__ CUtensorMap tm_head_t,
+head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_constant__ CUtensorMap tm_rows, const __grid_constant__ CUtensorMap tm_head, const __grid_constant__ CUtensorMap tm_head_t,
                  const __grid_constant__ CUtensorMap tm_probs, const HeadParams p) {
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint32_t tmem_base_slot;
@@ -226,6 +228,7 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_rows, const __grid_const
         // ------------------------------------------------------------------ TMA: both operands of this CTA
         Ring ring;
         const uint32_t leader_full = map_to_cta(bar_full, 0);
+        const CUtensorMap* of_rows = n_rows == p.tokens && !p.copies ? &tm_hidden : &tm_rows;
         int index;
         while (next(&index)) {
             const HeadItem it = head_item(plan, rows, index);
@@ -248,7 +251,7 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_rows, const __grid_const
                         tma_load_2d_pair(dst + HL_HALF, &tm_head_t, bar, other0, v);
                         tma_load_2d_pair(dst + HL_HALF + HL_HALF / 2, &tm_head_t, bar, other0 + 64, v);
                     } else {
-                        tma_load_2d_pair(dst, &tm_rows, bar, step * kHeadStep, row0);
+                        tma_load_2d_pair(dst, of_rows, bar, step * kHeadStep, row0);
                         tma_load_2d_pair(dst + HL_HALF, &tm_head, bar, step * kHeadStep, other0);
                     }
                 }
@@ -440,9 +443,7 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_rows, const __grid_const
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(leader_acc_empty + 8 * buffer);
-            const size_t at = (size_t)(v0 / kHeadTile) * p.padded + row;
-            __stcg(p.tile_max + at, m);
-            __stcg(p.tile_sum + at, s);
+            __stcg(p.tile_stats + (size_t)row * head_div_up(plan.V, kHeadTile) + v0 / kHeadTile, make_float2(m, s));
             if constexpr (GRAD) publish(logits_done(p) + (size_t)it.q * kHeadChunk + it.block_in_chunk);
         }
     }
@@ -461,138 +462,154 @@ done:
     }
 }
 
-// Tokens that have a label become rows, in their order: place[t] (-1 without), the rows' labels, and the hidden states side by side.  A block takes
-// 32 tokens and counts the labels before them itself.  The counters are set to zero.
-constexpr int PREP_THREADS = 256, PREP_TOKENS = 32;
+// Tokens that have a label become rows, in their order: place[t] (-1 without), the rows' labels, and, unless every token has one, the hidden states side
+// by side.  A block takes 8 tokens, a warp each, and counts the labels itself: those before its tokens and all of them.  The counters are set to zero.
+constexpr int PREP_TOKENS = 8, PREP_THREADS = 32 * PREP_TOKENS;
 __global__ void __launch_bounds__(PREP_THREADS)
-head_prepare_kernel(int T, int V, int D, const int32_t* __restrict__ labels, const bf16* __restrict__ hidden, int* __restrict__ place, int* __restrict__ row_label,
-                    bf16* __restrict__ rows, unsigned* __restrict__ counters, size_t counter_words) {
-    __shared__ int parts[PREP_THREADS / 32];
-    __shared__ int place_s[PREP_TOKENS];
+head_prepare_kernel(int T, int V, int D, int copies, const int32_t* __restrict__ labels, const bf16* __restrict__ hidden, int* __restrict__ place,
+                    int* __restrict__ row_label, bf16* __restrict__ rows, unsigned* __restrict__ counters, size_t counter_words) {
+    __shared__ int parts[2][PREP_TOKENS];
     pdl_launch_dependents();
     pdl_wait();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t0 = blockIdx.x * PREP_TOKENS;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t0 = blockIdx.x * PREP_TOKENS, t = t0 + warp;
     for (size_t i = 1 + blockIdx.x * PREP_THREADS + threadIdx.x; i < counter_words; i += (size_t)gridDim.x * PREP_THREADS) counters[i] = 0u;
-    int n = 0;
-    for (int t = threadIdx.x; t < t0; t += PREP_THREADS) n += (unsigned)__ldg(labels + t) < (unsigned)V;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xFFFFFFFFu, n, o);
-    if (lane == 0) parts[warp] = n;
-    __syncthreads();
-    if (warp == 0) {
-        int before = 0;
-#pragma unroll
-        for (int w = 0; w < PREP_THREADS / 32; ++w) before += parts[w];
-        const int t = t0 + lane, label = t < T ? __ldg(labels + t) : -1;
-        const bool has = (unsigned)label < (unsigned)V;
-        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, has);
-        const int at = has ? before + __popc(mask & ((1u << lane) - 1u)) : -1;
-        place_s[lane] = at;
-        if (t < T) place[t] = at;
-        if (has) row_label[at] = label;
-        if (lane == 0 && blockIdx.x == gridDim.x - 1) counters[0] = (unsigned)(before + __popc(mask));
+    int before = 0, after = 0;                                         // labels of tokens before this warp's, and of the others
+    for (int i = threadIdx.x; i < T; i += PREP_THREADS) {
+        const int has = (unsigned)__ldg(labels + i) < (unsigned)V;
+        before += i < t0 ? has : 0;
+        after += i < t0 ? 0 : has;
     }
-    __syncthreads();
-    const int chunks = D / 8;
-    for (int i = warp; i < PREP_TOKENS; i += PREP_THREADS / 32) {
-        if (place_s[i] < 0) continue;
-        const uint4* src = reinterpret_cast<const uint4*>(hidden + (size_t)(t0 + i) * D);
-        uint4* dst = reinterpret_cast<uint4*>(rows + (size_t)place_s[i] * D);
-#pragma unroll 4
-        for (int c = lane; c < chunks; c += 32) dst[c] = __ldg(src + c);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        before += __shfl_xor_sync(0xFFFFFFFFu, before, o);
+        after += __shfl_xor_sync(0xFFFFFFFFu, after, o);
     }
+    if (lane == 0) { parts[0][warp] = before; parts[1][warp] = after; }
+    const int label = lane < PREP_TOKENS && t0 + lane < T ? __ldg(labels + t0 + lane) : -1;
+    const uint32_t mask = __ballot_sync(0xFFFFFFFFu, (unsigned)label < (unsigned)V);
+    __syncthreads();
+    before = after = 0;
+#pragma unroll
+    for (int w = 0; w < PREP_TOKENS; ++w) { before += parts[0][w]; after += parts[1][w]; }
+    const int all = before + after, at = (mask >> warp) & 1u ? before + __popc(mask & ((1u << warp) - 1u)) : -1;
+    if (lane == 0 && t < T) {
+        place[t] = at;
+        if (at >= 0) row_label[at] = __ldg(labels + t);
+        if (t == 0) counters[0] = (unsigned)all;
+    }
+    if (at < 0 || (all == T && !copies)) return;
+    const uint4* src = reinterpret_cast<const uint4*>(hidden + (size_t)t * D);
+    uint4* dst = reinterpret_cast<uint4*>(rows + (size_t)at * D);
+#pragma unroll 8
+    for (int c = lane; c < D / 8; c += 32) dst[c] = __ldg(src + c);
 }
 
-// One block per token: its loss from the tiles' sums, and its row of the gradient from the pieces' sums.
-constexpr int FIN_THREADS = 256;
-__device__ __forceinline__ float block_sum(float v, float* parts) {
-    v = warp_sum(v);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) parts[threadIdx.x >> 5] = v;
-    __syncthreads();
-    float s = 0.f;
+// One block per token: its loss from the tiles' sums, and its row of the gradient from the pieces' sums, which are asked for first.
+constexpr int FIN_THREADS = 256, FIN_AHEAD = 2;
+struct MaxSum { float m, s; };
+// Each thread's maximum and sum -> the block's (in a fixed order).
+template <bool RESCALE>
+__device__ __forceinline__ MaxSum block_max_sum(MaxSum v, float scale, float (*parts)[2]) {
+    auto join = [&](MaxSum a, MaxSum b) {
+        MaxSum r{fmaxf(a.m, b.m), a.s + b.s};
+        if constexpr (RESCALE)                                         // (a sum over its own maximum; one without a term has none)
+            r.s = (a.s == 0.f ? 0.f : a.s * fast_exp2((a.m - r.m) * scale)) + (b.s == 0.f ? 0.f : b.s * fast_exp2((b.m - r.m) * scale));
+        return r;
+    };
 #pragma unroll
-    for (int w = 0; w < FIN_THREADS / 32; ++w) s += parts[w];
-    return s;
-}
-__device__ __forceinline__ float block_max(float v, float* parts) {
-    v = warp_max(v);
+    for (int o = 16; o > 0; o >>= 1) v = join(v, MaxSum{__shfl_xor_sync(0xFFFFFFFFu, v.m, o), __shfl_xor_sync(0xFFFFFFFFu, v.s, o)});
+    if ((threadIdx.x & 31) == 0) { parts[threadIdx.x >> 5][0] = v.m; parts[threadIdx.x >> 5][1] = v.s; }
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) parts[threadIdx.x >> 5] = v;
-    __syncthreads();
-    float m = parts[0];
+    v = MaxSum{parts[0][0], parts[0][1]};
 #pragma unroll
-    for (int w = 1; w < FIN_THREADS / 32; ++w) m = fmaxf(m, parts[w]);
-    return m;
+    for (int w = 1; w < FIN_THREADS / 32; ++w) v = join(v, MaxSum{parts[w][0], parts[w][1]});
+    return v;
 }
 
 template <bool GRAD>
 __global__ void __launch_bounds__(FIN_THREADS)
 head_finish_kernel(HeadParams p, const int* __restrict__ place, const bf16* __restrict__ head, const float* __restrict__ d_loss, float* __restrict__ loss,
                    bf16* __restrict__ d_hidden) {
-    __shared__ float parts[FIN_THREADS / 32];
+    __shared__ float parts[FIN_THREADS / 32][2];
     pdl_launch_dependents();
     pdl_wait();
     if (p.again && __ldcg(p.counters + 3) == 0u) return;
-    const int t = blockIdx.x, row = place[t], D = p.plan.D;
-    uint4* out = GRAD ? reinterpret_cast<uint4*>(d_hidden + (size_t)t * D) : nullptr;
-    if (row < 0) {
-        if (p.again) return;
-        if (threadIdx.x == 0) loss[t] = 0.f;
-        if (GRAD)
-            for (int c = threadIdx.x; c < D / 8; c += FIN_THREADS) out[c] = make_uint4(0, 0, 0, 0);
-        return;
-    }
-    if (p.again && __ldcg(to_do_again(p) + row / kHeadTile) == 0u) return;
-    const int tiles = head_div_up(p.plan.V, kHeadTile);
-    float m = -INFINITY;
-    for (int i = threadIdx.x; i < tiles; i += FIN_THREADS) m = fmaxf(m, __ldcg(p.tile_max + (size_t)i * p.padded + row));
-    m = block_max(m, parts);
-    float s = 0.f;
-    for (int i = threadIdx.x; i < tiles; i += FIN_THREADS) {
-        const float x = __ldcg(p.tile_sum + (size_t)i * p.padded + row);
-        if constexpr (GRAD) s += x;
-        else s += x * fast_exp2((__ldcg(p.tile_max + (size_t)i * p.padded + row) - m) * p.scale);
-    }
-    const float others = block_sum(s, parts);
-    const float ref = GRAD ? __ldcg(p.ref + row) : m;
-    const float at_label = (__ldcg(p.label_logit + row) - ref) * p.scale, mine = fast_exp2(at_label), total = others + mine;
-    if (threadIdx.x == 0) {
-        // (a label that has most of the probability: the small loss from the small sum)
-        float l = others <= mine ? log1pf(others / mine) : LN2 * (log2f(total) - at_label);
-        if (!(total < INFINITY)) l = NAN;
-        loss[t] = l;
-        if (GRAD && !p.again && m - ref > REF_REACH) {
-            p.counters[3] = 1u;
-            to_do_again(p)[row / kHeadTile] = 1u;
-            p.ref[row] = fminf(m, MOST);
+    for (int t = blockIdx.x; t < p.tokens; t += gridDim.x) {
+        const int row = __ldcg(place + t), D = p.plan.D, chunks = D / 8;
+        uint4* out = GRAD ? reinterpret_cast<uint4*>(d_hidden + (size_t)t * D) : nullptr;
+        if (row < 0) {
+            if (p.again) continue;
+            if (threadIdx.x == 0) loss[t] = 0.f;
+            if (GRAD)
+                for (int c = threadIdx.x; c < chunks; c += FIN_THREADS) out[c] = make_uint4(0, 0, 0, 0);
+            continue;
         }
-    }
-    if constexpr (GRAD) {
-        const float f = d_loss[t], share = f / total, back = -share * others;
-        const int label = __ldcg(p.label + row);
-        const uint4* w = reinterpret_cast<const uint4*>(head + (size_t)label * D);
-        const float* sums = p.sums + (size_t)row * D;
-        const bool none = f == 0.f;
-        for (int c = threadIdx.x; c < D / 8; c += FIN_THREADS) {
-            float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+        if (p.again && __ldcg(to_do_again(p) + row / kHeadTile) == 0u) continue;
+        // eight features of the row: the pieces' sums and the label's row of the head
+        struct Chunk { float v[8]; uint4 w; };
+        const uint4* w = GRAD ? reinterpret_cast<const uint4*>(head + (size_t)__ldcg(p.label + row) * D) : nullptr;
+        const float* sums = GRAD ? p.sums + (size_t)row * D : nullptr;
+        auto load = [&](int c) {
+            Chunk x{};
             for (int k = 0; k < p.plan.sums; ++k) {
                 const float4* from = reinterpret_cast<const float4*>(sums + (size_t)k * p.padded * D) + 2 * c;
-                const float4 x = __ldcg(from), y = __ldcg(from + 1);
-                a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
-                b.x += y.x; b.y += y.y; b.z += y.z; b.w += y.w;
+                const float4 a = __ldcg(from), b = __ldcg(from + 1);
+                x.v[0] += a.x; x.v[1] += a.y; x.v[2] += a.z; x.v[3] += a.w;
+                x.v[4] += b.x; x.v[5] += b.y; x.v[6] += b.z; x.v[7] += b.w;
             }
-            const uint4 l = __ldg(w + c);
-            const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-            const uint32_t lw[4] = {l.x, l.y, l.z, l.w};
-            uint32_t o[4];
+            x.w = __ldg(w + c);
+            return x;
+        };
+        Chunk ahead[FIN_AHEAD];
+        if constexpr (GRAD) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const __nv_bfloat162 pr = __floats2bfloat162_rn(fmaf(share, v[2 * j], back * bf16_lo(lw[j])), fmaf(share, v[2 * j + 1], back * bf16_hi(lw[j])));
-                o[j] = none ? 0u : *reinterpret_cast<const uint32_t*>(&pr);
-            }
-            out[c] = make_uint4(o[0], o[1], o[2], o[3]);
+            for (int i = 0; i < FIN_AHEAD; ++i)
+                if (threadIdx.x + i * FIN_THREADS < chunks) ahead[i] = load(threadIdx.x + i * FIN_THREADS);
         }
+        const int tiles = head_div_up(p.plan.V, kHeadTile);
+        MaxSum v{-INFINITY, 0.f};
+        for (int i = threadIdx.x; i < tiles; i += FIN_THREADS) {
+            const float2 stats = __ldcg(p.tile_stats + (size_t)row * tiles + i);
+            const float m = stats.x, s = stats.y;
+            if constexpr (GRAD) v = MaxSum{fmaxf(v.m, m), v.s + s};
+            else {
+                const float to = fmaxf(v.m, m);
+                v.s = (v.s == 0.f ? 0.f : v.s * fast_exp2((v.m - to) * p.scale)) + (s == 0.f ? 0.f : s * fast_exp2((m - to) * p.scale));
+                v.m = to;
+            }
+        }
+        v = block_max_sum<!GRAD>(v, p.scale, parts);
+        const float ref = GRAD ? __ldcg(p.ref + row) : v.m, others = v.s;
+        const float at_label = (__ldcg(p.label_logit + row) - ref) * p.scale, mine = fast_exp2(at_label), total = others + mine;
+        if (threadIdx.x == 0) {
+            // (a label that has most of the probability: the small loss from the small sum)
+            float l = others <= mine ? log1pf(others / mine) : LN2 * (log2f(total) - at_label);
+            if (!(total < INFINITY)) l = NAN;
+            loss[t] = l;
+            if (GRAD && !p.again && v.m - ref > REF_REACH) {
+                p.counters[3] = 1u;
+                to_do_again(p)[row / kHeadTile] = 1u;
+                p.ref[row] = fminf(v.m, MOST);
+            }
+        }
+        if constexpr (GRAD) {
+            const float f = d_loss[t], share = f / total, back = -share * others;
+            auto store = [&](int c, const Chunk& x) {
+                const uint32_t lw[4] = {x.w.x, x.w.y, x.w.z, x.w.w};
+                uint32_t o[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const __nv_bfloat162 pr = __floats2bfloat162_rn(fmaf(share, x.v[2 * j], back * bf16_lo(lw[j])), fmaf(share, x.v[2 * j + 1], back * bf16_hi(lw[j])));
+                    o[j] = f == 0.f ? 0u : *reinterpret_cast<const uint32_t*>(&pr);
+                }
+                out[c] = make_uint4(o[0], o[1], o[2], o[3]);
+            };
+#pragma unroll
+            for (int i = 0; i < FIN_AHEAD; ++i)
+                if (threadIdx.x + i * FIN_THREADS < chunks) store(threadIdx.x + i * FIN_THREADS, ahead[i]);
+            for (int c = threadIdx.x + FIN_AHEAD * FIN_THREADS; c < chunks; c += FIN_THREADS) store(c, load(c));
+        }
+        __syncthreads();                                               // `parts` is written again
     }
 }
 
@@ -614,16 +631,18 @@ static int head_loss_impl(int T, int V, int D, const void* hidden, const void* h
     p.label = reinterpret_cast<int*>(ws + l.label);
     p.ref = reinterpret_cast<float*>(ws + l.ref);
     p.label_logit = reinterpret_cast<float*>(ws + l.label_logit);
-    p.tile_max = reinterpret_cast<float*>(ws + l.tile_max);
-    p.tile_sum = reinterpret_cast<float*>(ws + l.tile_sum);
+    p.tile_stats = reinterpret_cast<float2*>(ws + l.tile_stats);
     p.probs = reinterpret_cast<bf16*>(ws + l.probs);
     p.sums = reinterpret_cast<float*>(ws + l.sums);
     int* place = reinterpret_cast<int*>(ws + l.place);
     bf16* rows = reinterpret_cast<bf16*>(ws + l.rows);
 
-    CUtensorMap tr, th, tt{}, tp{};
+    p.tokens = T;
+    p.copies = hidden == d_hidden;                                     // (the second launch still reads them)
+    CUtensorMap tx, tr, th, tt{}, tp{};
     const CUtensorMapDataType type = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-    if (!make_map_2d(&tr, type, 2, rows, (uint64_t)D, p.padded, 64, 128, CU_TENSOR_MAP_SWIZZLE_128B) ||
+    if (!make_map_2d(&tx, type, 2, hidden, (uint64_t)D, (uint64_t)T, 64, 128, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !make_map_2d(&tr, type, 2, rows, (uint64_t)D, p.padded, 64, 128, CU_TENSOR_MAP_SWIZZLE_128B) ||
         !make_map_2d(&th, type, 2, head, (uint64_t)D, (uint64_t)V, 64, 128, CU_TENSOR_MAP_SWIZZLE_128B))
         return QLORA_ERR_CUDA;
     if (GRAD && (!make_map_2d(&tt, type, 2, head, (uint64_t)D, (uint64_t)V, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B) ||
@@ -632,14 +651,14 @@ static int head_loss_impl(int T, int V, int D, const void* hidden, const void* h
     static SmemLimit limit;
     auto kern = head_loss_kernel<GRAD>;
     if (!limit.raise(kern, HL_SMEM)) return QLORA_ERR_CUDA;
-    if (launch_pdl(head_prepare_kernel, dim3((T + PREP_TOKENS - 1) / PREP_TOKENS), dim3(PREP_THREADS), 0, st, 1, T, V, D, labels, (const bf16*)hidden, place,
+    if (launch_pdl(head_prepare_kernel, dim3((T + PREP_TOKENS - 1) / PREP_TOKENS), dim3(PREP_THREADS), 0, st, 1, T, V, D, p.copies, labels, (const bf16*)hidden, place,
                    const_cast<int*>(p.label), rows, p.counters, l.counter_words) != cudaSuccess)
         return QLORA_ERR_CUDA;
     const long long items = head_rows(p.plan, T).total;
     const int pairs = (int)(items < sm_count() / 2 ? items : sm_count() / 2);
     for (p.again = 0; p.again < (GRAD ? 2 : 1); ++p.again) {
-        if (launch_pdl(kern, dim3(2 * pairs), dim3(HL_THREADS), HL_SMEM, st, 1, tr, th, tt, tp, p) != cudaSuccess) return QLORA_ERR_CUDA;
-        if (launch_pdl(head_finish_kernel<GRAD>, dim3(T), dim3(FIN_THREADS), 0, st, 1, p, place, (const bf16*)head, d_loss, loss, (bf16*)d_hidden) != cudaSuccess)
+        if (launch_pdl(kern, dim3(2 * pairs), dim3(HL_THREADS), HL_SMEM, st, 1, tx, tr, th, tt, tp, p) != cudaSuccess) return QLORA_ERR_CUDA;
+        if (launch_pdl(head_finish_kernel<GRAD>, dim3(p.again && T > 4 * sm_count() ? 4 * sm_count() : T), dim3(FIN_THREADS), 0, st, 1, p, place, (const bf16*)head, d_loss, loss, (bf16*)d_hidden) != cudaSuccess)
             return QLORA_ERR_CUDA;
     }
     return QLORA_OK;

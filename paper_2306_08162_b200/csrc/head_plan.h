@@ -105,14 +105,14 @@ QLORA_HD int head_piece_entries(const HeadPlan& p, int piece) { return p.V - pie
 
 // The workspace, in bytes from its beginning.
 struct HeadLayout {
-    size_t place, label, ref, label_logit, tile_max, tile_sum, rows, probs, sums, counters;
+    size_t place, label, ref, label_logit, tile_stats, rows, probs, sums, counters;
     size_t counter_words, total;
 };
 
 QLORA_HD HeadLayout head_layout(const HeadPlan& p, int T) {
     HeadLayout l;
     size_t at = 0;
-    const size_t padded = (size_t)p.blocks_max * kHeadTile, tiles = (size_t)p.pieces * (p.piece / kHeadTile);
+    const size_t padded = (size_t)p.blocks_max * kHeadTile, tiles = (size_t)head_div_up(p.V, kHeadTile);
     const int chunks = head_div_up(p.blocks_max, kHeadChunk);
 #define QLORA_TAKE(name, bytes) l.name = at; at += ((size_t)(bytes) + 1023) / 1024 * 1024
     // [0] rows, [1] claimed, [2] claimed again, [3] anything to do again; per block: reference known, to do again; twice per piece and block: logits, gradient
@@ -122,8 +122,7 @@ QLORA_HD HeadLayout head_layout(const HeadPlan& p, int T) {
     QLORA_TAKE(label, padded * 4);
     QLORA_TAKE(ref, padded * 4);
     QLORA_TAKE(label_logit, padded * 4);
-    QLORA_TAKE(tile_max, tiles * padded * 4);
-    QLORA_TAKE(tile_sum, tiles * padded * 4);
+    QLORA_TAKE(tile_stats, tiles * padded * 8);
     QLORA_TAKE(rows, padded * p.D * 2);
     QLORA_TAKE(probs, p.grad ? (size_t)p.ring * p.chunk_max * kHeadTile * p.piece * 2 : 0);
     QLORA_TAKE(sums, p.grad ? (size_t)p.sums * padded * p.D * 4 : 0);
