@@ -54,276 +54,83 @@ __device__ __forceinline__ uint32_t finite_pair(uint32_t w) {
     return w;
 }
 
-// ---------------------------------------------------------------------------------------------------------------- down
-constexpr int DN_ROWS = 16, DN_SHARE = 4;
-
-// One block per 16 tokens and DN_SHARE-th of their entries.  The warps stride over the contraction; fragments as in lora_down.cuh.
-template <int NT> constexpr int DN_WARPS = NT <= 4 ? 16 : 8;             // (what 48 KB of shared memory hold of their sums)
-
-template <bool L_IS_A, int NT>
-__global__ void __launch_bounds__(32 * DN_WARPS<NT>)
-adapters_down_kernel(int M, int T, int r, int n_adapters, const bf16* __restrict__ In, const int32_t* __restrict__ adapter_of,
-                     const bf16* __restrict__ L, float* __restrict__ P) {
-    constexpr int UNROLL = NT <= 2 ? 4 : NT <= 4 ? 2 : 1, WARPS = DN_WARPS<NT>;
-    __shared__ float red[WARPS * NT * 128];
-    __shared__ uint32_t entry_mask[DN_ROWS];
-    __shared__ int entry_adapter[DN_ROWS], n_entries_s;
-    __shared__ uint32_t bare_s;
-    pdl_launch_dependents();
-    pdl_wait();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-    const int m0 = blockIdx.x * DN_ROWS;
-    if (warp == 0) {
-        const bool in = lane < DN_ROWS && m0 + lane < M;
-        int a = in ? adapter_of[m0 + lane] : -1;
-        if (a < 0 || a >= n_adapters) a = -1;
-        const uint32_t mask = entry_of_lane(a);
-        const uint32_t firsts = __ballot_sync(0xFFFFFFFFu, mask != 0), bare = __ballot_sync(0xFFFFFFFFu, in && a < 0);
-        if (mask != 0) {
-            const int e = __popc(firsts & ((1u << lane) - 1u));
-            entry_mask[e] = mask;
-            entry_adapter[e] = a;
-        }
-        if (lane == 0) { n_entries_s = __popc(firsts); bare_s = bare; }
-    }
-    __syncthreads();
-    if (blockIdx.y == 0) {
-        for (int i = threadIdx.x; i < DN_ROWS * r; i += 32 * WARPS)
-            if ((bare_s >> (i / r)) & 1u) P[(size_t)m0 * r + i] = 0.f;
-    }
-    const int n_entries = n_entries_s;
-    const uint4 zero4 = make_uint4(0, 0, 0, 0);
-    for (int e = blockIdx.y; e < n_entries; e += DN_SHARE) {
-        const uint32_t mask = entry_mask[e];
-        const bf16* La = L + (size_t)entry_adapter[e] * r * T;
-        const bool on0 = (mask >> g) & 1u, on1 = (mask >> (g + 8)) & 1u;
-        const bf16 *x0 = In + (size_t)(m0 + g) * T, *x1 = x0 + (size_t)8 * T;
-        float acc[NT][4];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.f;
-#pragma unroll 1
-        for (int kk = warp * 32; kk < T; kk += WARPS * 32 * UNROLL) {
-            uint4 xlo[UNROLL], xhi[UNROLL], l[UNROLL][NT];
-#pragma unroll
-            for (int u = 0; u < UNROLL; ++u) {
-                const int k0 = kk + u * WARPS * 32, k = k0 + q * 8;
-                xlo[u] = on0 && k < T ? ldg16(x0 + k) : zero4;
-                xhi[u] = on1 && k < T ? ldg16(x1 + k) : zero4;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    uint4 lv = zero4;
-                    if (L_IS_A) {
-                        const int j = nt * 8 + g;
-                        if (k < T && j < r) lv = ldg16(La + (size_t)j * T + k);
-                    } else if (nt * 8 < r) {
-                        const int n = k0 + 8 * (g >> 1) + (g & 1);
-                        const uint32_t* src = reinterpret_cast<const uint32_t*>(La + (size_t)n * r + nt * 8 + 2 * q);
-                        if (n < T) lv = make_uint4(__ldg(src), __ldg(src + r), __ldg(src + 2 * r), __ldg(src + 3 * r));
-                    }
-                    l[u][nt] = lv;
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < UNROLL; ++u) {
-                if (kk + u * WARPS * 32 >= T) break;
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    uint4 lv = l[u][nt];
-                    if (!L_IS_A) lv = make_uint4(movmatrix_trans(lv.x), movmatrix_trans(lv.y), movmatrix_trans(lv.z), movmatrix_trans(lv.w));
-                    mma_bf16_16816(acc[nt], xlo[u].x, xhi[u].x, xlo[u].y, xhi[u].y, lv.x, lv.y);
-                    mma_bf16_16816(acc[nt], xlo[u].z, xhi[u].z, xlo[u].w, xhi[u].w, lv.z, lv.w);
-                }
-            }
-        }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) red[((warp * NT + nt) * 4 + c) * 32 + lane] = acc[nt][c];
-        __syncthreads();
-        for (int idx = threadIdx.x; idx < NT * 128; idx += 32 * WARPS) {
-            float v = 0.f;
-#pragma unroll
-            for (int w = 0; w < WARPS; ++w) v += red[w * NT * 128 + idx];
-            const int nt = idx >> 7, c = (idx >> 5) & 3, ln = idx & 31;
-            const int row = (ln >> 2) + ((c & 2) ? 8 : 0), col = nt * 8 + (ln & 3) * 2 + (c & 1);
-            if (((mask >> row) & 1u) && col < r) P[(size_t)(m0 + row) * r + col] = v;
-        }
-        __syncthreads();
-    }
+// 16 bytes to shared memory, zeros where `in` is false; groups of such copies; 8 x 8 matrices out of it, as they lie or transposed.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool in) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
 }
-
-// ------------------------------------------------------------------------------------------------------------------ up
-constexpr int UP_ROWS = 16, UP_WARPS = 8, UP_BLOCKS = 2;               // a warp: 16 tokens x 2 blocks of 32 columns
-
-// The adapter's part for 32 columns (c0 ..) and ranks 16 ks .. 16 ks + 15 as four column tiles of an MMA.  Column c of tile t is
-// c0 + 8 (c / 2) + 2 t + c % 2, so a thread's sums are eight neighbouring columns.  FROM_B: L2 = B [C, r]; else A [r, C].  The ranks are in the order
-// (4 q, 4 q + 1; 4 q + 2, 4 q + 3) for B, which is read along them, and (2 q, 2 q + 1; 8 + 2 q, 9 + 2 q) for A.
-template <bool FROM_B>
-__device__ __forceinline__ void up_fragments(const bf16* __restrict__ L2, int C, int r, int c0, int ks, int g, int q, uint32_t (&b)[4][2]) {
-    if constexpr (FROM_B) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int n = c0 + 8 * (g >> 1) + 2 * t + (g & 1), j = 16 * ks + 4 * q;
-            uint2 v = make_uint2(0, 0);
-            if (n < C && j < r) v = __ldg(reinterpret_cast<const uint2*>(L2 + (size_t)n * r + j));
-            b[t][0] = v.x;
-            b[t][1] = v.y;
-        }
-    } else {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int j = 16 * ks + 8 * h + g, n = c0 + 8 * q;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (n < C && j < r) v = ldg16(L2 + (size_t)j * C + n);
-            b[0][h] = movmatrix_trans(v.x);
-            b[1][h] = movmatrix_trans(v.y);
-            b[2][h] = movmatrix_trans(v.z);
-            b[3][h] = movmatrix_trans(v.w);
-        }
-    }
-}
-
-template <bool FROM_B>
-__global__ void __launch_bounds__(32 * UP_WARPS)
-adapters_up_kernel(int M, int C, int r, int n_adapters, const float* __restrict__ P, const int32_t* __restrict__ adapter_of,
-                   const bf16* __restrict__ L, const float* __restrict__ scales, const bf16* Base, bf16* Out) {
-    pdl_launch_dependents();
-    pdl_wait();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-    const int m0 = blockIdx.x * UP_ROWS, c_warp = (blockIdx.y * UP_WARPS + warp) * 32 * UP_BLOCKS;
-    if (c_warp >= C) return;
-    int a = lane < UP_ROWS && m0 + lane < M ? adapter_of[m0 + lane] : -1;
-    if (a < 0 || a >= n_adapters) a = -1;
-    const uint32_t mask_here = entry_of_lane(a);
-    uint32_t firsts = __ballot_sync(0xFFFFFFFFu, mask_here != 0);
-    const int row0 = m0 + g, row1 = row0 + 8;
-    uint4 base[UP_BLOCKS][2];
-#pragma unroll
-    for (int i = 0; i < UP_BLOCKS; ++i) {
-        const int c = c_warp + 32 * i + 8 * q;
-        const uint4 zero4 = make_uint4(0, 0, 0, 0);
-        base[i][0] = row0 < M && c < C ? *reinterpret_cast<const uint4*>(Base + (size_t)row0 * C + c) : zero4;
-        base[i][1] = row1 < M && c < C ? *reinterpret_cast<const uint4*>(Base + (size_t)row1 * C + c) : zero4;
-    }
-    float sum[UP_BLOCKS][4][4] = {};
-    while (firsts != 0) {
-        const int first = __ffs(firsts) - 1;
-        firsts &= firsts - 1;
-        const uint32_t mask = __shfl_sync(0xFFFFFFFFu, mask_here, first);
-        const int adapter = __shfl_sync(0xFFFFFFFFu, a, first);
-        const bool on0 = (mask >> g) & 1u, on1 = (mask >> (g + 8)) & 1u;
-        const float s = scales[adapter];
-        const bf16* L2 = L + (size_t)adapter * r * C;
-        float part[UP_BLOCKS][4][4] = {};
-        for (int ks = 0; 16 * ks < r; ++ks) {
-            // the tokens' part: s P of ranks in the adapter's order, as two bf16 each
-            float2 p[2][2];                                            // [row][half]
-            const int j0 = FROM_B ? 16 * ks + 4 * q : 16 * ks + 2 * q, j1 = FROM_B ? j0 + 2 : j0 + 8;
-            const float2 none = make_float2(0.f, 0.f);
-            p[0][0] = on0 && j0 < r ? __ldcg(reinterpret_cast<const float2*>(P + (size_t)row0 * r + j0)) : none;
-            p[1][0] = on1 && j0 < r ? __ldcg(reinterpret_cast<const float2*>(P + (size_t)row1 * r + j0)) : none;
-            p[0][1] = on0 && j1 < r ? __ldcg(reinterpret_cast<const float2*>(P + (size_t)row0 * r + j1)) : none;
-            p[1][1] = on1 && j1 < r ? __ldcg(reinterpret_cast<const float2*>(P + (size_t)row1 * r + j1)) : none;
-            Split x[2][2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) x[i][h] = split_bf16(s * p[i][h].x, s * p[i][h].y);
-#pragma unroll
-            for (int i = 0; i < UP_BLOCKS; ++i) {
-                uint32_t b[4][2];
-                up_fragments<FROM_B>(L2, C, r, c_warp + 32 * i, ks, g, q, b);
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    mma_bf16_16816(part[i][t], x[0][0].hi, x[1][0].hi, x[0][1].hi, x[1][1].hi, b[t][0], b[t][1]);
-                    mma_bf16_16816(part[i][t], x[0][0].lo, x[1][0].lo, x[0][1].lo, x[1][1].lo, finite_pair(b[t][0]), finite_pair(b[t][1]));
-                }
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < UP_BLOCKS; ++i)
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                if (on0) { sum[i][t][0] = part[i][t][0]; sum[i][t][1] = part[i][t][1]; }
-                if (on1) { sum[i][t][2] = part[i][t][2]; sum[i][t][3] = part[i][t][3]; }
-            }
-    }
-    const bool any0 = __shfl_sync(0xFFFFFFFFu, a, g) >= 0, any1 = __shfl_sync(0xFFFFFFFFu, a, g + 8) >= 0;
-#pragma unroll
-    for (int i = 0; i < UP_BLOCKS; ++i) {
-        const int c = c_warp + 32 * i + 8 * q;
-        if (c >= C) continue;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int row = h ? row1 : row0;
-            if (row >= M) continue;
-            uint4 v = base[i][h];
-            if (h ? any1 : any0) {                                     // (a token without an adapter keeps its bits, whatever they are)
-                uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                for (int t = 0; t < 4; ++t) w[t] = bf16x2(bf16_lo(w[t]) + sum[i][t][2 * h], bf16_hi(w[t]) + sum[i][t][2 * h + 1]);
-                v = make_uint4(w[0], w[1], w[2], w[3]);
-            }
-            *reinterpret_cast<uint4*>(Out + (size_t)row * C + c) = v;
-        }
-    }
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+template <bool TRANS>
+__device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t& a, uint32_t& b, uint32_t& c, uint32_t& d) {
+    if constexpr (TRANS) asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(addr));
+    else asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(addr));
 }
 
 // ----------------------------------------------------------------------------------------------------------- few tokens
-constexpr int FEW_ROWS = 4, FEW_CTAS = 8, FEW_WARPS = 8;
+// Both products of ROWS tokens by a cluster (or one block).  Its CTAs share the contraction out; each stores its sums into the shared memory of all, and one cluster
+// barrier later they share the columns out.  The adapters' second matrices are asked into L2 before the first product begins.  The second product
+// is fp32 throughout: a few tokens leave the CUDA cores enough time.
+constexpr int FEW_CTAS = 8, FEW_WARPS = 8, FEW_TOKENS = 256;
 
-// Both products of FEW_ROWS tokens in one launch, by a cluster.  Its CTAs share the contraction out; each stores its sums into the shared memory
-// of all, and one cluster barrier later they share the columns out.  The adapters' second matrices are asked into L2 before the first product
-// begins.  The second product is fp32 throughout: a few tokens leave the CUDA cores enough time.
-template <bool FORWARD, int NT>
-__global__ void __cluster_dims__(FEW_CTAS, 1, 1) __launch_bounds__(32 * FEW_WARPS)
-adapters_few_kernel(int M, int T, int C, int r, int n_adapters, const bf16* __restrict__ In, const int32_t* __restrict__ adapter_of,
-                    const bf16* __restrict__ L1, const bf16* __restrict__ L2, const float* __restrict__ scales, const bf16* Base, bf16* Out,
-                    float* __restrict__ P_out) {
+template <int NT, int ROWS, int CTAS>
+struct FewShared {
+    float parts[CTAS][ROWS][NT * 8];                               // [CTA that summed]
+    float red[FEW_WARPS][ROWS][NT * 8];
+    float low[ROWS][NT * 8];                                           // s P
+    uint32_t entry_mask[ROWS];
+    int entry_adapter[ROWS], entry_of[ROWS], n_entries;
+};
+
+struct Products {                            // the operands of both products
+    int M, T, C, r, n_adapters;
+    const bf16* In;                          // [M, T]
+    const int32_t* adapter_of;
+    const bf16 *L1, *L2;                     // forward: A, B; else B, A
+    const float* scales;
+    const bf16* Base;                        // [M, C]; no second product where Out is NULL
+    bf16* Out;
+    float* P;                                // [M, r] or NULL
+    uint2* split;                            // [M, r / 2]: pairs of s P as two bf16 pairs, for the second product of many tokens; or NULL
+};
+
+// Called by all threads of all CTAs of the cluster, with the same m0, after the cluster's CTAs have begun.
+template <bool FORWARD, int NT, int ROWS, int CTAS>
+__device__ __forceinline__ void few_tokens(const Products& p, int m0, FewShared<NT, ROWS, CTAS>& sh) {
     constexpr int UNROLL = NT <= 2 ? 4 : NT <= 4 ? 2 : 1, THREADS = 32 * FEW_WARPS;
-    __shared__ float red[FEW_WARPS][FEW_ROWS][NT * 8];
-    __shared__ __align__(16) float parts[FEW_CTAS][FEW_ROWS][NT * 8];  // [CTA that summed]
-    __shared__ __align__(16) float low[FEW_ROWS][NT * 8];              // s P
-    __shared__ uint32_t entry_mask[FEW_ROWS];
-    __shared__ int entry_adapter[FEW_ROWS], entry_of[FEW_ROWS], n_entries_s;
-    pdl_launch_dependents();
-    cluster_arrive();                                                  // (a CTA's shared memory is written to once it has begun)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-    const int cta = (int)cluster_ctarank(), m0 = (int)(blockIdx.x / FEW_CTAS) * FEW_ROWS, rows = min(FEW_ROWS, M - m0);
-    pdl_wait();
+    const int cta = CTAS > 1 ? (int)cluster_ctarank() : 0, rows = min(ROWS, p.M - m0), r = p.r, T = p.T, C = p.C;
     if (warp == 0) {
-        int a = lane < rows ? adapter_of[m0 + lane] : -1;
-        if (a < 0 || a >= n_adapters) a = -1;
+        int a = lane < rows ? p.adapter_of[m0 + lane] : -1;
+        if (a < 0 || a >= p.n_adapters) a = -1;
         const uint32_t mask = entry_of_lane(a), firsts = __ballot_sync(0xFFFFFFFFu, mask != 0);
         const int first = __ffs(__match_any_sync(0xFFFFFFFFu, a)) - 1, e = __popc(firsts & ((1u << (a >= 0 ? first : 0)) - 1u));
-        if (lane < FEW_ROWS) entry_of[lane] = a >= 0 ? e : -1;
-        if (mask != 0) { entry_mask[e] = mask; entry_adapter[e] = a; }
-        if (lane == 0) n_entries_s = __popc(firsts);
+        if (lane < ROWS) sh.entry_of[lane] = a >= 0 ? e : -1;
+        if (mask != 0) { sh.entry_mask[e] = mask; sh.entry_adapter[e] = a; }
+        if (lane == 0) sh.n_entries = __popc(firsts);
     }
     __syncthreads();
-    const int n_entries = n_entries_s, pairs = C / 2;
-    const int p_lo = (int)((long long)pairs * cta / FEW_CTAS), p_hi = (int)((long long)pairs * (cta + 1) / FEW_CTAS);
+    const int n_entries = sh.n_entries, pairs = p.Out != nullptr ? C / 2 : 0;
+    const int p_lo = (int)((long long)pairs * cta / CTAS), p_hi = (int)((long long)pairs * (cta + 1) / CTAS);
     for (int e = 0; e < n_entries; ++e) {
-        const bf16* La = L2 + (size_t)entry_adapter[e] * r * C;
+        const bf16* La = p.L2 + (size_t)sh.entry_adapter[e] * r * C;
         if constexpr (FORWARD) {                                       // B: the columns' rows lie together
-            for (int i = p_lo * 2 * r + 64 * threadIdx.x; i < p_hi * 2 * r; i += 64 * THREADS) asm volatile("prefetch.global.L2 [%0];" ::"l"(La + i));
+            for (int i = p_lo * 2 * r + 64 * threadIdx.x; i < p_hi * 2 * r; i += 64 * THREADS) prefetch_l2(La + i);
         } else {
             const int lines = (p_hi - p_lo + 31) / 32;
-            for (int i = threadIdx.x; i < lines * r; i += THREADS)
-                asm volatile("prefetch.global.L2 [%0];" ::"l"(La + (size_t)(i / lines) * C + 2 * p_lo + 64 * (i % lines)));
+            for (int i = threadIdx.x; i < lines * r; i += THREADS) prefetch_l2(La + (size_t)(i / lines) * C + 2 * p_lo + 64 * (i % lines));
         }
     }
-    // ---- the first product: warps share the entries and their parts of the contraction
+    // ---- the first product: warps share the entries and their parts of the contraction.  (A row of the result depends on its own row of In alone, so
+    // rows of other entries need no mask: they are not taken.)
     const int per_entry = n_entries <= 1 ? 8 : n_entries == 2 ? 4 : 2, my_entry = warp / per_entry, sub = warp % per_entry;
     if (my_entry < n_entries) {
-        const int steps = (T + 31) / 32, s_lo = steps * cta / FEW_CTAS, s_hi = steps * (cta + 1) / FEW_CTAS;
-        const bf16* La = L1 + (size_t)entry_adapter[my_entry] * r * T;
-        const bool on = g < FEW_ROWS && ((entry_mask[my_entry] >> g) & 1u);
-        const bf16* x0 = In + (size_t)(m0 + g) * T;
+        const int steps = (T + 31) / 32, s_lo = steps * cta / CTAS, s_hi = steps * (cta + 1) / CTAS;
+        const bf16* La = p.L1 + (size_t)sh.entry_adapter[my_entry] * r * T;
+        const bool on = g < rows;
+        const bf16* x0 = p.In + (size_t)(m0 + g) * T;
         const uint4 zero4 = make_uint4(0, 0, 0, 0);
-        float acc[NT][4];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.f;
+        float acc[NT][4] = {};
 #pragma unroll 1
         for (int step = s_lo + sub; step < s_hi; step += per_entry * UNROLL) {
             uint4 x[UNROLL], l[UNROLL][NT];
@@ -356,280 +163,865 @@ adapters_few_kernel(int M, int T, int C, int r, int n_adapters, const bf16* __re
                     mma_bf16_16816(acc[nt], x[u].z, 0u, x[u].w, 0u, lv.z, lv.w);
                 }
         }
-        if (g < FEW_ROWS)
+        if (g < ROWS)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                red[warp][g][nt * 8 + 2 * q] = acc[nt][0];
-                red[warp][g][nt * 8 + 2 * q + 1] = acc[nt][1];
-            }
+            for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<float2*>(&sh.red[warp][g][nt * 8 + 2 * q]) = make_float2(acc[nt][0], acc[nt][1]);
     }
     __syncthreads();
-    cluster_wait();                                                    // every CTA of the cluster has begun
-    if (threadIdx.x < FEW_ROWS * NT * 8) {
-        const int row = threadIdx.x / (NT * 8), j = threadIdx.x % (NT * 8), e = row < rows ? entry_of[row] : -1;
+    constexpr int VALUES = ROWS * NT * 8;
+    if (threadIdx.x < VALUES) {
+        const int row = threadIdx.x / (NT * 8), j = threadIdx.x % (NT * 8), e = row < rows ? sh.entry_of[row] : -1;
         float v = 0.f;
         if (e >= 0)
-            for (int w = 0; w < per_entry; ++w) v += red[e * per_entry + w][row][j];
-        const uint32_t here = (uint32_t)__cvta_generic_to_shared(&parts[cta][row][j]);
+            for (int w = 0; w < per_entry; ++w) v += sh.red[e * per_entry + w][row][j];
+        if constexpr (CTAS > 1) {
+            const uint32_t here = smem_u32(&sh.parts[cta][row][j]);
 #pragma unroll
-        for (int i = 0; i < FEW_CTAS; ++i) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(map_to_cta(here, i)), "f"(v) : "memory");
+            for (int i = 0; i < CTAS; ++i) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(map_to_cta(here, i)), "f"(v) : "memory");
+        } else {
+            sh.parts[0][row][j] = v;                                   // (read by the thread that wrote it)
+        }
     }
-    __syncwarp();
-    cluster_arrive();
-    cluster_wait();
-    if (threadIdx.x < FEW_ROWS * NT * 8) {
-        const int row = threadIdx.x / (NT * 8), j = threadIdx.x % (NT * 8), e = row < rows ? entry_of[row] : -1;
+    if constexpr (CTAS > 1) {
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();
+    }
+    if (threadIdx.x < VALUES) {
+        const int row = threadIdx.x / (NT * 8), j = threadIdx.x % (NT * 8), e = row < rows ? sh.entry_of[row] : -1;
         float v = 0.f;
 #pragma unroll
-        for (int i = 0; i < FEW_CTAS; ++i) v += parts[i][row][j];
-        if (P_out != nullptr && cta == 0 && row < rows && j < r) P_out[(size_t)(m0 + row) * r + j] = v;
-        low[row][j] = e >= 0 ? scales[entry_adapter[e]] * v : 0.f;
+        for (int i = 0; i < CTAS; ++i) v += sh.parts[i][row][j];
+        if (p.P != nullptr && cta == 0 && row < rows && j < r) p.P[(size_t)(m0 + row) * r + j] = v;
+        sh.low[row][j] = e >= 0 && p.Out != nullptr ? p.scales[sh.entry_adapter[e]] * v : 0.f;
     }
     __syncthreads();
-    // ---- the second product: a thread has two neighbouring columns of one entry
-    const int n_pairs = p_hi - p_lo;
-    for (int unit = threadIdx.x; unit < n_entries * n_pairs; unit += THREADS) {
-        const int e = unit / n_pairs, c = 2 * (p_lo + unit - e * n_pairs);
-        const bf16* La = L2 + (size_t)entry_adapter[e] * r * C;
-        const uint32_t mask = entry_mask[e];
-        float sum[FEW_ROWS][2] = {};
-        uint32_t base[FEW_ROWS];
+    if (p.Out == nullptr) return;
+    // ---- the second product: a thread has two neighbouring columns of one entry, BATCH such units at a time
+    constexpr int BATCH = NT <= 2 ? 4 : NT <= 4 ? 2 : 1;
+    const int n_pairs = p_hi - p_lo, units = n_entries * n_pairs;
+    for (int unit0 = threadIdx.x; unit0 < units; unit0 += THREADS * BATCH) {
+        uint32_t w[BATCH][NT * 8], base[BATCH][ROWS], masks[BATCH];    // w: FORWARD: eight ranks of a column, then of the other; else a rank of both
+        int column[BATCH];
 #pragma unroll
-        for (int i = 0; i < FEW_ROWS; ++i)
-            base[i] = (mask >> i) & 1u ? *reinterpret_cast<const uint32_t*>(Base + (size_t)(m0 + i) * C + c) : 0u;
+        for (int u = 0; u < BATCH; ++u) {
+            const int unit = unit0 + u * THREADS, e = ROWS > 1 && unit < units ? unit / n_pairs : 0, c = 2 * (p_lo + (unit < units ? unit - e * n_pairs : 0));
+            column[u] = c;
+            masks[u] = unit < units ? sh.entry_mask[e] : 0u;
+            const bf16* La = p.L2 + (size_t)sh.entry_adapter[e] * r * C;
 #pragma unroll
-        for (int j = 0; j < NT * 8; j += 8) {
-            if (j >= r) break;
-            float w[8][2];                                             // eight ranks of both columns
-            if constexpr (FORWARD) {
-                const uint4 a = ldg16(La + (size_t)c * r + j), b = ldg16(La + (size_t)(c + 1) * r + j);
-                const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {b.x, b.y, b.z, b.w};
+            for (int j = 0; j < NT; ++j) {
+                if (8 * j >= r) break;
+                if constexpr (FORWARD) {
+                    const uint4 a = ldg16(La + (size_t)c * r + 8 * j), b = ldg16(La + (size_t)(c + 1) * r + 8 * j);
+                    w[u][8 * j] = a.x; w[u][8 * j + 1] = a.y; w[u][8 * j + 2] = a.z; w[u][8 * j + 3] = a.w;
+                    w[u][8 * j + 4] = b.x; w[u][8 * j + 5] = b.y; w[u][8 * j + 6] = b.z; w[u][8 * j + 7] = b.w;
+                } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    w[i][0] = i & 1 ? bf16_hi(wa[i / 2]) : bf16_lo(wa[i / 2]);
-                    w[i][1] = i & 1 ? bf16_hi(wb[i / 2]) : bf16_lo(wb[i / 2]);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t a = __ldg(reinterpret_cast<const uint32_t*>(La + (size_t)(j + i) * C + c));
-                    w[i][0] = bf16_lo(a);
-                    w[i][1] = bf16_hi(a);
+                    for (int i = 0; i < 8; ++i) w[u][8 * j + i] = __ldg(reinterpret_cast<const uint32_t*>(La + (size_t)(8 * j + i) * C + c));
                 }
             }
 #pragma unroll
-            for (int i = 0; i < FEW_ROWS; ++i)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const float p = low[i][j + k];
-                    sum[i][0] = fmaf(p, w[k][0], sum[i][0]);
-                    sum[i][1] = fmaf(p, w[k][1], sum[i][1]);
-                }
+            for (int i = 0; i < ROWS; ++i)
+                base[u][i] = (masks[u] >> i) & 1u ? *reinterpret_cast<const uint32_t*>(p.Base + (size_t)(m0 + i) * C + c) : 0u;
         }
 #pragma unroll
-        for (int i = 0; i < FEW_ROWS; ++i)
-            if ((mask >> i) & 1u)
-                *reinterpret_cast<uint32_t*>(Out + (size_t)(m0 + i) * C + c) = bf16x2(bf16_lo(base[i]) + sum[i][0], bf16_hi(base[i]) + sum[i][1]);
+        for (int u = 0; u < BATCH; ++u)
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) {
+                if (!((masks[u] >> i) & 1u)) continue;
+                float a = 0.f, b = 0.f;
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    if (8 * j >= r) break;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const float v = sh.low[i][8 * j + k];
+                        if constexpr (FORWARD) {
+                            const uint32_t wa = w[u][8 * j + k / 2], wb = w[u][8 * j + 4 + k / 2];
+                            a = fmaf(v, k & 1 ? bf16_hi(wa) : bf16_lo(wa), a);
+                            b = fmaf(v, k & 1 ? bf16_hi(wb) : bf16_lo(wb), b);
+                        } else {
+                            a = fmaf(v, bf16_lo(w[u][8 * j + k]), a);
+                            b = fmaf(v, bf16_hi(w[u][8 * j + k]), b);
+                        }
+                    }
+                }
+                *reinterpret_cast<uint32_t*>(p.Out + (size_t)(m0 + i) * C + column[u]) = bf16x2(bf16_lo(base[u][i]) + a, bf16_hi(base[u][i]) + b);
+            }
     }
-    if (Out != Base)                                                   // tokens without an adapter
+    if (p.Out != p.Base)                                               // tokens without an adapter
         for (int i = 0; i < rows; ++i)
-            if (entry_of[i] < 0)
-                for (int p = p_lo + threadIdx.x; p < p_hi; p += THREADS)
-                    *reinterpret_cast<uint32_t*>(Out + (size_t)(m0 + i) * C + 2 * p) = *reinterpret_cast<const uint32_t*>(Base + (size_t)(m0 + i) * C + 2 * p);
+            if (sh.entry_of[i] < 0)
+                for (int c = p_lo + threadIdx.x; c < p_hi; c += THREADS)
+                    *reinterpret_cast<uint32_t*>(p.Out + (size_t)(m0 + i) * C + 2 * c) = *reinterpret_cast<const uint32_t*>(p.Base + (size_t)(m0 + i) * C + 2 * c);
 }
 
-// --------------------------------------------------------------------------------------------------------------- grads
-constexpr int GR_WARPS = 8, GR_WINDOW = 2048;
+template <bool FORWARD, int NT, int ROWS>
+__global__ void __cluster_dims__(FEW_CTAS, 1, 1) __launch_bounds__(32 * FEW_WARPS)
+adapters_few_kernel(const Products p) {
+    __shared__ __align__(16) FewShared<NT, ROWS, FEW_CTAS> sh;
+    pdl_launch_dependents();
+    cluster_arrive();                                                  // (a CTA's shared memory is written to once it has begun)
+    pdl_wait();
+    cluster_wait();
+    few_tokens<FORWARD, NT, ROWS, FEW_CTAS>(p, (int)(blockIdx.x / FEW_CTAS) * ROWS, sh);
+}
 
-// One block per adapter and slice of 32 NB columns of X (then of dY): the block finds its adapter's tokens, window by window, in the order
-// of their places; its warps take sixteen of them at a time, and their sums are added in the order of the warps.  MT tiles of 16 ranks.
-template <int MT, int NB>
-__global__ void __launch_bounds__(32 * GR_WARPS)
-adapters_grad_kernel(int M, int K, int N, int r, int n_adapters, const bf16* __restrict__ X, const bf16* __restrict__ dY,
-                     const int32_t* __restrict__ adapter_of, const float* __restrict__ scales, const float* __restrict__ H, const float* __restrict__ G,
-                     float* __restrict__ dA, float* __restrict__ dB, int accumulate) {
-    extern __shared__ float red[];                                     // [warps][MT * 16][32 NB]
-    __shared__ int list[GR_WINDOW];
-    __shared__ int counts[GR_WARPS];
+// ---------------------------------------------------------------------------------------------------------------- down
+// Many tokens, the first product.  A block has 16 NB tokens and reads their rows of In once where they have one adapter; its warps stride over the
+// contraction (fragments as in lora_down.cuh) and add their sums in order.  The second product gets s P as two bf16 each from here, so that it
+// need not take every value apart again for each of its columns.
+//
+// Tiles of 16 tokens with more than two adapters (single tokens in generation beside the prompts of others) would be sixteen blocks' work for one block, in
+// both products: blocks of their own, the last of the grid, look for such tiles and take their tokens in turn, both products of one at a time.
+constexpr int DN_WARPS = 8, DN_ENTRIES = 2, DN_WINDOW = 16384;
+
+// Lane i holds the adapter of token i of one (16 lanes) or two tiles: whether its tile is one of more than DN_ENTRIES adapters.
+__device__ __forceinline__ bool of_scattered_tile(int adapter) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t half = lane < 16 ? 0x0000FFFFu : 0xFFFF0000u, same = __match_any_sync(0xFFFFFFFFu, adapter) & half;
+    const uint32_t firsts = __ballot_sync(0xFFFFFFFFu, adapter >= 0 && (same & ((1u << lane) - 1u)) == 0) & half;
+    return __popc(firsts) > DN_ENTRIES;
+}
+
+// Every warp has a ring of its own in shared memory, a stage of which holds 64 contraction elements of the tile's rows and of the adapter; copies
+// run ahead without holding registers.  16-byte pieces are XORed by row, so that the matrix loads have no bank conflicts.
+template <bool L_IS_A, int NT, int NB>
+struct DownTile {
+    static constexpr int ROWS = 16 * NB, CHUNK = 64;
+    static constexpr int IN_BYTES = ROWS * 128, L_BYTES = NT * 8 * 128, STAGE = IN_BYTES + L_BYTES;
+    static constexpr int STAGES = NT == 1 ? 4 : NT == 8 ? 2 : 3;
+    static constexpr size_t RING = (size_t)STAGES * STAGE * DN_WARPS, SUMS = sizeof(float) * DN_WARPS * NB * NT * 128, FEW = sizeof(FewShared<NT, 1, 1>);
+    static constexpr size_t SMEM = RING > SUMS ? (RING > FEW ? RING : FEW) : (SUMS > FEW ? SUMS : FEW);
+};
+
+template <bool L_IS_A, int NT, int NB>
+__global__ void __launch_bounds__(32 * DN_WARPS, NT <= 2 ? 2 : 1)
+adapters_down_kernel(const Products p, int n_tiles) {
+    using Tile = DownTile<L_IS_A, NT, NB>;
+    constexpr int ROWS = Tile::ROWS, CHUNK = Tile::CHUNK, STAGES = Tile::STAGES;
+    union Shared {
+        float red[DN_WARPS][NB][NT][4][32];
+        FewShared<NT, 1, 1> few;
+    };
+    extern __shared__ __align__(128) uint8_t smem[];
+    Shared& sh = *reinterpret_cast<Shared*>(smem);
+    __shared__ uint32_t scattered[DN_WINDOW / 512];                    // a bit for every tile of 16
+    pdl_launch_dependents();
+    pdl_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int M = p.M, T = p.T, r = p.r;
+    if ((int)blockIdx.x >= n_tiles) {
+        const int me = (int)blockIdx.x - n_tiles, blocks = (int)gridDim.x - n_tiles;
+        int n = 0;                                                     // tokens of such tiles so far
+        for (int w0 = 0; w0 < M; w0 += DN_WINDOW) {
+            const int chunks = min(DN_WINDOW, M - w0 + 31) / 32;       // of 32 tokens
+            __syncthreads();
+            for (int i = threadIdx.x; i < DN_WINDOW / 512; i += 32 * DN_WARPS) scattered[i] = 0u;
+            __syncthreads();
+            for (int i0 = warp; i0 < chunks; i0 += 8 * DN_WARPS) {
+                int a[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int t = w0 + (i0 + k * DN_WARPS) * 32 + lane;
+                    a[k] = i0 + k * DN_WARPS < chunks && t < M ? __ldg(p.adapter_of + t) : -1;
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const uint32_t found = __ballot_sync(0xFFFFFFFFu, of_scattered_tile(a[k] >= p.n_adapters ? -1 : a[k]));
+                    const int i = i0 + k * DN_WARPS;
+                    if (lane == 0 && found != 0) atomicOr(&scattered[i / 16], ((found & 1u) | ((found >> 15) & 2u)) << (2 * (i % 16)));
+                }
+            }
+            __syncthreads();
+            for (int i = 0; i < DN_WINDOW / 512; ++i)
+                for (uint32_t bits = scattered[i]; bits != 0; bits &= bits - 1) {
+                    const int m0 = w0 + (32 * i + __ffs(bits) - 1) * 16;
+                    for (int k = 0; k < 16 && m0 + k < M; ++k)
+                        if (n++ % blocks == me) {
+                            few_tokens<L_IS_A, NT, 1, 1>(p, m0 + k, sh.few);
+                            __syncthreads();
+                        }
+                }
+        }
+        return;
+    }
+    const int m0 = (int)blockIdx.x * ROWS;
+    const uint32_t ring = smem_u32(smem) + warp * STAGES * Tile::STAGE;
+    const int chunks = (T + CHUNK - 1) / CHUNK, mine = warp < chunks ? (chunks - warp + DN_WARPS - 1) / DN_WARPS : 0;
+    // what a lane copies: a 16-byte piece of every fourth row of the tile, and of the adapter
+    const int piece = lane & 7, row0 = lane >> 3;
+    const bf16* in0 = p.In + (size_t)(m0 + row0) * T + warp * CHUNK + 8 * piece;
+    uint32_t rows_in = 0;
+#pragma unroll
+    for (int n = 0; n < ROWS / 4; ++n) rows_in |= (uint32_t)(m0 + row0 + 4 * n < M) << n;
+    const uint32_t swizzled[2] = {(uint32_t)(row0 * 128 + ((piece ^ row0) << 4)), (uint32_t)(row0 * 128 + ((piece ^ (row0 + 4)) << 4))};   // rows 4 n: n even, odd
+    auto load_in = [&](int i) {                                        // chunk i of this warp's
+        const int from = i * (DN_WARPS * CHUNK);
+        const bool k_in = warp * CHUNK + 8 * piece + from < T;
+        const bf16* src = in0 + from;
+        const uint32_t to = ring + (i % STAGES) * Tile::STAGE;
+#pragma unroll
+        for (int n = 0; n < ROWS / 4; ++n) {
+            const bool in = k_in && ((rows_in >> n) & 1u);
+            copy16(to + 512 * n + swizzled[n & 1], in ? src : p.In, in);
+            src += (size_t)4 * T;
+        }
+    };
+    auto load_adapter = [&](int i, const bf16* La) {
+        const int from = i * (DN_WARPS * CHUNK), k0 = warp * CHUNK + from;
+        const uint32_t to = ring + (i % STAGES) * Tile::STAGE + Tile::IN_BYTES;
+        if constexpr (L_IS_A) {                                        // rows of ranks, 64 elements each
+            const bool k_in = k0 + 8 * piece < T;
+            const bf16* src = La + (size_t)row0 * T + k0 + 8 * piece;
+#pragma unroll
+            for (int n = 0; n < 2 * NT; ++n) {
+                const bool in = k_in && 4 * n + row0 < r;
+                copy16(to + 512 * n + swizzled[n & 1], in ? src : La, in);
+                src += (size_t)4 * T;
+            }
+        } else {                                                       // rows of contraction elements, 8 NT ranks each
+#pragma unroll
+            for (int n = 0; n < 2 * NT; ++n) {
+                const int at = 32 * n + lane, k = at / NT, j = at % NT;
+                const bool in = k0 + k < T && 8 * j < r;
+                copy16(to + k * (16 * NT) + ((j ^ ((k * NT / 8) % NT)) << 4), La + (in ? (size_t)(k0 + k) * r + 8 * j : 0), in);
+            }
+        }
+    };
+    const bool in = lane < ROWS && m0 + lane < M;
+    int a = in ? __ldg(p.adapter_of + m0 + lane) : -1;
+    for (int i = 0; i < STAGES - 1 && i < mine; ++i) load_in(i);       // on their way while the tile's adapters are looked at
+    if (a < 0 || a >= p.n_adapters) a = -1;
+    const bool elsewhere = of_scattered_tile(a);
+    if (warp == 0 && p.P != nullptr && in && a < 0 && !elsewhere)
+        for (int j = 0; j < r; j += 4) *reinterpret_cast<float4*>(p.P + (size_t)(m0 + lane) * r + j) = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (elsewhere) a = -1;
+    const uint32_t mask_here = entry_of_lane(a);
+    uint32_t firsts = __ballot_sync(0xFFFFFFFFu, mask_here != 0);
+    bool begun = true;
+    for (; firsts != 0; firsts &= firsts - 1) {
+        const int first = __ffs(firsts) - 1, adapter = __shfl_sync(0xFFFFFFFFu, a, first);
+        const uint32_t mask = __shfl_sync(0xFFFFFFFFu, mask_here, first);
+        const bf16* La = p.L1 + (size_t)adapter * r * T;
+        const float s = p.scales != nullptr ? __ldg(p.scales + adapter) : 0.f;
+        float acc[NB][NT][4] = {};
+#pragma unroll
+        for (int i = 0; i < STAGES - 1; ++i) {
+            if (i < mine) {
+                if (!begun) load_in(i);
+                load_adapter(i, La);
+            }
+            copy_commit();
+        }
+        begun = false;
+#pragma unroll 1
+        for (int i = 0; i < mine; ++i) {
+            copy_wait<STAGES - 2>();
+            __syncwarp();                                              // chunk i is there, chunk i - 1 has been read by every lane
+            if (i + STAGES - 1 < mine) {
+                load_in(i + STAGES - 1);
+                load_adapter(i + STAGES - 1, La);
+            }
+            copy_commit();
+            const uint32_t x = ring + (i % STAGES) * Tile::STAGE, l = x + Tile::IN_BYTES;
+            const int row8 = lane & 7, quarter = lane >> 3;            // matrix `quarter` of four, its row `row8`
+#pragma unroll
+            for (int k = 0; k < CHUNK / 16; ++k) {
+                uint32_t xa[NB][4];
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {                         // rows 0 - 7, 8 - 15 of elements 0 - 7; then of 8 - 15
+                    const int row = 16 * b + row8 + 8 * (quarter & 1), piece = 2 * k + (quarter >> 1);
+                    ldmatrix4<false>(x + row * 128 + ((piece ^ (row & 7)) << 4), xa[b][0], xa[b][1], xa[b][2], xa[b][3]);
+                }
+                uint32_t lb[NT][2];
+                if constexpr (NT == 1) {                               // (two steps' worth is not worth the registers: the second half of the four is not used)
+                    uint32_t u0, u1;
+                    if constexpr (L_IS_A) ldmatrix4<false>(l + row8 * 128 + (((2 * k + (quarter & 1)) ^ row8) << 4), lb[0][0], lb[0][1], u0, u1);
+                    else ldmatrix4<true>(l + (16 * k + row8 + 8 * (quarter & 1)) * 16, lb[0][0], lb[0][1], u0, u1);
+                } else {
+#pragma unroll
+                    for (int nt = 0; nt < NT; nt += 2) {
+                        if constexpr (L_IS_A) {
+                            const int j = 8 * (nt + (quarter >> 1)) + row8, piece = 2 * k + (quarter & 1);
+                            ldmatrix4<false>(l + j * 128 + ((piece ^ row8) << 4), lb[nt][0], lb[nt][1], lb[nt + 1][0], lb[nt + 1][1]);
+                        } else {
+                            const int e = 16 * k + row8 + 8 * (quarter & 1), j = nt + (quarter >> 1);
+                            ldmatrix4<true>(l + e * (16 * NT) + ((j ^ ((e * NT / 8) % NT)) << 4), lb[nt][0], lb[nt][1], lb[nt + 1][0], lb[nt + 1][1]);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma_bf16_16816(acc[b][nt], xa[b][0], xa[b][1], xa[b][2], xa[b][3], lb[nt][0], lb[nt][1]);
+            }
+        }
+        copy_wait<0>();
+        __syncthreads();                                               // the sums lie where the rings are
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) sh.red[warp][b][nt][c][lane] = acc[b][nt][c];
+        __syncthreads();
+        // two neighbouring ranks of a row
+        for (int idx = threadIdx.x; idx < NB * NT * 64; idx += 32 * DN_WARPS) {
+            const int b = idx / (NT * 64), nt = (idx >> 6) % NT, h = (idx >> 5) & 1, ln = idx & 31;
+            float v0 = 0.f, v1 = 0.f;
+#pragma unroll
+            for (int w = 0; w < DN_WARPS; ++w) { v0 += sh.red[w][b][nt][2 * h][ln]; v1 += sh.red[w][b][nt][2 * h + 1][ln]; }
+            const int row = 16 * b + (ln >> 2) + 8 * h, col = nt * 8 + (ln & 3) * 2;
+            if (((mask >> row) & 1u) && col < r) {
+                const size_t at = ((size_t)(m0 + row) * r + col) / 2;
+                if (p.P != nullptr) reinterpret_cast<float2*>(p.P)[at] = make_float2(v0, v1);
+                if (p.split != nullptr) {
+                    const Split v = split_bf16(s * v0, s * v1);
+                    p.split[at] = make_uint2(v.hi, v.lo);
+                }
+            }
+        }
+        __syncthreads();
+    }
+    copy_commit();
+    copy_wait<0>();                                                    // (a tile without an entry leaves with its copies done)
+}
+
+// ------------------------------------------------------------------------------------------------------------------ up
+// Many tokens, the second product.  A warp has 32 UB columns and goes down the rows, sixteen at a time.  It keeps its columns of the adapter in registers
+// for as long as the adapter stays the same, so long requests read Base and write Out and little else; the next rows are asked for a tile ahead.
+constexpr int UP_ROWS = 16, UP_WARPS = 8;
+
+// Ranks 16 ks .. 16 ks + 15 of 32 columns (c0 ..) as four column tiles of an MMA.  Column c of tile t is c0 + 8 (c / 2) + 2 t + c % 2, so that a
+// thread's sums are eight neighbouring columns.  FROM_B: L2 = B [C, r]; else A [r, C].  The ranks are in the order (4 q, 4 q + 1; 4 q + 2, 4 q + 3) for B,
+// which is read along them, and (2 q, 2 q + 1; 8 + 2 q, 9 + 2 q) for A.
+template <bool FROM_B>
+__device__ __forceinline__ void up_fragments(const bf16* __restrict__ L2, int C, int r, int c0, int ks, int g, int q, uint32_t (&b)[4][2]) {
+    if constexpr (FROM_B) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int n = c0 + 8 * (g >> 1) + 2 * t + (g & 1), j = 16 * ks + 4 * q;
+            uint2 v = make_uint2(0, 0);
+            if (n < C && j < r) v = __ldg(reinterpret_cast<const uint2*>(L2 + (size_t)n * r + j));
+            b[t][0] = v.x;
+            b[t][1] = v.y;
+        }
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int j = 16 * ks + 8 * h + g, n = c0 + 8 * q;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (n < C && j < r) v = ldg16(L2 + (size_t)j * C + n);
+            b[0][h] = movmatrix_trans(v.x);
+            b[1][h] = movmatrix_trans(v.y);
+            b[2][h] = movmatrix_trans(v.z);
+            b[3][h] = movmatrix_trans(v.w);
+        }
+    }
+}
+
+// KS steps of 16 ranks.
+template <bool FROM_B, int KS, int UB>
+__global__ void __launch_bounds__(32 * UP_WARPS, 2)
+adapters_up_kernel(const Products p, int tiles_each) {
     pdl_launch_dependents();
     pdl_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-    const int adapter = blockIdx.y, slices_x = (K + 32 * NB - 1) / (32 * NB);
-    const bool of_x = (int)blockIdx.x < slices_x;
-    const int C = of_x ? K : N, c0 = (of_x ? blockIdx.x : blockIdx.x - slices_x) * 32 * NB;
-    const bf16* V = of_x ? X : dY;
-    const float* P = of_x ? G : H;
-    float acc[MT][NB][4][4] = {};
-    bool any = false;
-    for (int w0 = 0; w0 < M; w0 += GR_WINDOW) {
-        // this warp's share of the window: GR_WINDOW / GR_WARPS places in a row
-        constexpr int SHARE = GR_WINDOW / GR_WARPS;
-        const int from = w0 + warp * SHARE;
-        uint32_t found[SHARE / 32];
-        int n = 0;
+    const int c_warp = (blockIdx.y * UP_WARPS + warp) * 32 * UB, M = p.M, C = p.C, r = p.r;
+    if (c_warp >= C) return;
+    const int tiles = (M + UP_ROWS - 1) / UP_ROWS, tile_end = min(tiles, ((int)blockIdx.x + 1) * tiles_each);
+    struct Tile {
+        uint4 base[UB][2];
+        int adapter;                                                   // of row `lane`, modulo sixteen
+    };
+    struct Low { uint4 v[KS][2]; };                                    // [step][row]: both halves of the step's ranks, each (high, low)
+    int tile = blockIdx.x * tiles_each;
+    const size_t at0 = (size_t)(tile * UP_ROWS + g) * C + c_warp + 8 * q;      // this lane's first element
+    bool c_in[UB];
 #pragma unroll
-        for (int i = 0; i < SHARE / 32; ++i) {
-            const int t = from + 32 * i + lane;
-            found[i] = __ballot_sync(0xFFFFFFFFu, t < M && __ldg(adapter_of + t) == adapter);
-            n += __popc(found[i]);
-        }
-        if (lane == 0) counts[warp] = n;
-        __syncthreads();
-        int at = 0, total = 0;
+    for (int i = 0; i < UB; ++i) c_in[i] = c_warp + 32 * i + 8 * q < C;
+    // (`ahead`: how many tiles this one lies behind the block's first; `whole`: all its rows exist)
+    auto load = [&](int ahead, bool whole, Tile& x) {
+        const int m0 = (tile + ahead) * UP_ROWS, row = m0 + (lane & 15);
+        x.adapter = whole || row < M ? __ldg(p.adapter_of + row) : -1;
+        const bf16* from = p.Base + at0 + (size_t)(m0 - (int)blockIdx.x * tiles_each * UP_ROWS) * C;
 #pragma unroll
-        for (int w = 0; w < GR_WARPS; ++w) {
-            if (w == warp) at = total;
-            total += counts[w];
-        }
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int i = 0; i < SHARE / 32; ++i) {
-            if ((found[i] >> lane) & 1u) list[at + __popc(found[i] & ((1u << lane) - 1u))] = from + 32 * i + lane;
-            at += __popc(found[i]);
-        }
-        __syncthreads();
-        any |= total > 0;
-        for (int i0 = warp * 16; i0 < total; i0 += GR_WARPS * 16) {
-            // tokens i0 + g and i0 + 8 + g in rows of 32 columns; after the transposition a thread has tokens 2 q, 2 q + 1 (+ 8) of one column
-            uint32_t b[NB][4][2];
+            for (int i = 0; i < UB; ++i)
+                x.base[i][h] = c_in[i] && (whole || m0 + g + 8 * h < M) ? *reinterpret_cast<const uint4*>(from + (size_t)(8 * h) * C + 32 * i) : make_uint4(0, 0, 0, 0);
+    };
+    auto load_low = [&](int ahead, bool whole, Low& x) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int i = i0 + 8 * h + g;
-                const bf16* row = i < total ? V + (size_t)list[i] * C : nullptr;
+        for (int h = 0; h < 2; ++h) {
+            const int row = (tile + ahead) * UP_ROWS + g + 8 * h;
+            const uint2* from = p.split + (size_t)row * (r / 2);
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                    const int c = c0 + 32 * nb + 8 * q;
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (row != nullptr && c < C) v = ldg16(row + c);
-                    b[nb][0][h] = v.x; b[nb][1][h] = v.y; b[nb][2][h] = v.z; b[nb][3][h] = v.w;
+            for (int ks = 0; ks < KS; ++ks) {
+                x.v[ks][h] = make_uint4(0, 0, 0, 0);
+                if (!whole && row >= M) continue;
+                if constexpr (FROM_B) {
+                    if (16 * ks + 4 * q < r) x.v[ks][h] = *reinterpret_cast<const uint4*>(from + 8 * ks + 2 * q);
+                } else {
+                    const uint2 none = make_uint2(0, 0), u = 16 * ks + 2 * q < r ? from[8 * ks + q] : none, v = 16 * ks + 8 + 2 * q < r ? from[8 * ks + 4 + q] : none;
+                    x.v[ks][h] = make_uint4(u.x, u.y, v.x, v.y);
                 }
             }
+        }
+    };
+    uint32_t held[KS][UB][4][2];
+    int held_adapter = -1;
+    bool held_finite = true;
+    Tile x;
+    Low low;
+    auto whole = [&](int i) { return (i + 1) * UP_ROWS <= M; };
+    if (tile < tile_end) {
+        load(0, whole(tile), x);
+        load_low(0, whole(tile), low);
+    }
+#pragma unroll 1
+    for (; tile < tile_end; ++tile) {
+        Tile following;
+        Low following_low;                                             // (of more ranks the registers hold one tile's)
+        if (tile + 1 < tile_end) {
+            load(1, whole(tile + 1), following);
+            if (KS == 1) load_low(1, whole(tile + 1), following_low);
+        }
+        const int m0 = tile * UP_ROWS;
+        const int a = x.adapter >= 0 && x.adapter < p.n_adapters ? x.adapter : -1;
+        uint32_t mask_here = 0xFFFFu, firsts = 1u;
+        bool elsewhere = false;
+        const bool one = held_adapter >= 0 && __all_sync(0xFFFFFFFFu, a == held_adapter);   // the adapter before, in every row
+        if (!one) {
+            mask_here = entry_of_lane(lane < UP_ROWS ? a : -1);
+            firsts = __ballot_sync(0xFFFFFFFFu, mask_here != 0);
+            elsewhere = __popc(firsts) > DN_ENTRIES;                   // (of_scattered_tile)
+            if (elsewhere) firsts = 0;
+        }
+        while (firsts != 0) {
+            const int first = __ffs(firsts) - 1;
+            firsts &= firsts - 1;
+            const uint32_t mask = one ? 0xFFFFu : __shfl_sync(0xFFFFFFFFu, mask_here, first);
+            const int adapter = one ? held_adapter : __shfl_sync(0xFFFFFFFFu, a, first);
+            if (adapter != held_adapter) {                             // (the same for the whole warp)
+                const bf16* L2 = p.L2 + (size_t)adapter * r * C;
+                uint32_t odd = 0;                                      // bits 15 and 31: an exponent of all ones
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
+                for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    b[nb][t][0] = movmatrix_trans(b[nb][t][0]);
-                    b[nb][t][1] = movmatrix_trans(b[nb][t][1]);
-                }
-            const float* pt[4];                                        // rows of P of tokens 2 q, 2 q + 1, 8 + 2 q, 9 + 2 q
+                    for (int i = 0; i < UB; ++i) {
+                        up_fragments<FROM_B>(L2, C, r, c_warp + 32 * i, ks, g, q, held[ks][i]);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int i = i0 + 2 * q + (k & 1) + 8 * (k >> 1);
-                pt[k] = i < total ? P + (size_t)list[i] * r : nullptr;
+                        for (int t = 0; t < 4; ++t) odd |= ((held[ks][i][t][0] & 0x7F807F80u) + 0x00800080u) | ((held[ks][i][t][1] & 0x7F807F80u) + 0x00800080u);
+                    }
+                held_finite = !__any_sync(0xFFFFFFFFu, (odd & 0x80008000u) != 0);
+                held_adapter = adapter;
             }
+            // the rows of Base and on top of them the products with both parts of s P.  (A row of the result depends on its own row of P alone: rows of other
+            // entries are computed and not stored.)
+            float sum[UB][4][4];
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                Split p[2][2];                                         // [rank half][token half]
+            for (int i = 0; i < UB; ++i)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int j = 16 * mt + 8 * i + g;
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t w[4] = {x.base[i][h].x, x.base[i][h].y, x.base[i][h].z, x.base[i][h].w};
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
-                        p[i][h] = split_bf16(pt[2 * h] && j < r ? __ldg(pt[2 * h] + j) : 0.f, pt[2 * h + 1] && j < r ? __ldg(pt[2 * h + 1] + j) : 0.f);
+                    for (int t = 0; t < 4; ++t) { sum[i][t][2 * h] = bf16_lo(w[t]); sum[i][t][2 * h + 1] = bf16_hi(w[t]); }
                 }
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb)
+            for (int ks = 0; ks < KS; ++ks) {
+                const uint4 v0 = low.v[ks][0], v1 = low.v[ks][1];
+#pragma unroll
+                for (int i = 0; i < UB; ++i)
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
-                        mma_bf16_16816(acc[mt][nb][t], p[0][0].hi, p[1][0].hi, p[0][1].hi, p[1][1].hi, b[nb][t][0], b[nb][t][1]);
-                        mma_bf16_16816(acc[mt][nb][t], p[0][0].lo, p[1][0].lo, p[0][1].lo, p[1][1].lo, finite_pair(b[nb][t][0]), finite_pair(b[nb][t][1]));
+                        const uint32_t b0 = held[ks][i][t][0], b1 = held[ks][i][t][1];
+                        mma_bf16_16816(sum[i][t], v0.x, v1.x, v0.z, v1.z, b0, b1);
+                        if (held_finite) mma_bf16_16816(sum[i][t], v0.y, v1.y, v0.w, v1.w, b0, b1);
+                        else mma_bf16_16816(sum[i][t], v0.y, v1.y, v0.w, v1.w, finite_pair(b0), finite_pair(b1));
                     }
             }
+            bf16* to = p.Out + (size_t)(m0 + g) * C + c_warp + 8 * q;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (!((mask >> (g + 8 * h)) & 1u)) continue;
+#pragma unroll
+                for (int i = 0; i < UB; ++i)
+                    if (c_in[i])
+                        *reinterpret_cast<uint4*>(to + (size_t)(8 * h) * C + 32 * i) =
+                            make_uint4(bf16x2(sum[i][0][2 * h], sum[i][0][2 * h + 1]), bf16x2(sum[i][1][2 * h], sum[i][1][2 * h + 1]),
+                                       bf16x2(sum[i][2][2 * h], sum[i][2][2 * h + 1]), bf16x2(sum[i][3][2 * h], sum[i][3][2 * h + 1]));
+            }
         }
-        __syncthreads();                                               // the list is written again
+        if (!one && !elsewhere && p.Out != p.Base) {                   // tokens without an adapter keep their bits, whatever they are
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int row = m0 + g + 8 * h;
+                if (__shfl_sync(0xFFFFFFFFu, a, g + 8 * h) >= 0 || row >= M) continue;
+#pragma unroll
+                for (int i = 0; i < UB; ++i)
+                    if (c_in[i]) *reinterpret_cast<uint4*>(p.Out + (size_t)row * C + c_warp + 32 * i + 8 * q) = x.base[i][h];
+            }
+        }
+        x = following;
+        if (KS == 1) low = following_low;
+        else if (tile + 1 < tile_end) load_low(1, whole(tile + 1), low);
     }
-    if (!any && accumulate) return;                                    // (the same for the whole block)
-    // acc[mt][nb][t][c]: rank 16 mt + g (+ 8 where c >= 2), column 32 nb + 8 q + 2 t + c % 2
-    constexpr int COLS = 32 * NB;
+}
+
+// --------------------------------------------------------------------------------------------------------------- grads
+// A task is one adapter, a slice of columns of X or of dY (128 up to 16 ranks, else 64) and 16 MT ranks, or -- where there are few of those -- one part of
+// `parts`: every parts-th tile of the adapter.  Adapters differ in their tokens, so blocks claim tasks one by one.  A block finds the tiles of sixteen
+// tokens that hold any of its adapter's, window by window; its warps take them in turn, each through a ring of its own in shared memory, rows of other
+// adapters as zeros, and their sums are added in the order of the warps.  The block that finishes a slice's last part adds the parts in their order.
+//
+// Both operands are transposed on the way out of shared memory.  G and H are taken as two bf16 each (made once, not by every slice), one product after the
+// other into the same sums.  Where a sum is not finite the low parts have nothing to say, but may have made a NaN of an infinity: the task is
+// then done again without them.
+constexpr int GR_WARPS = 4, GR_WINDOW = GR_WARPS * 512, GR_STAGES = 3, GR_BLOCKS = 3;
+
+struct Grads {
+    int M, K, N, r, n_adapters;
+    const bf16 *X, *dY;                      // [M, K], [M, N]
+    const int32_t* adapter_of;
+    const float* scales;
+    const bf16 *G, *H;                       // [2][M, r]: high parts, low parts
+    float *dA, *dB;
+    int accumulate;
+    int slices_x, slices, rank_blocks, parts;
+    unsigned* counters;                      // [0] claimed; with parts: [1 + task / parts] parts done
+    float* partial;                          // [task][16 MT][columns]
+};
+
+// G and H in two parts, and the counters set to zero.
+__global__ void __launch_bounds__(256)
+adapters_split_kernel(long long n, const float* __restrict__ G, const float* __restrict__ H, uint32_t* __restrict__ g, uint32_t* __restrict__ h, unsigned* counters,
+                      int n_counters) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (blockIdx.x == 0)
+        for (int i = threadIdx.x; i < n_counters; i += 256) counters[i] = 0u;
+    if (2 * at >= n) return;
+    const float2 vg = __ldcg(reinterpret_cast<const float2*>(G) + at), vh = __ldcg(reinterpret_cast<const float2*>(H) + at);
+    const Split sg = split_bf16(vg.x, vg.y), sh = split_bf16(vh.x, vh.y);
+    g[at] = sg.hi;
+    g[n / 2 + at] = sg.lo;
+    h[at] = sh.hi;
+    h[n / 2 + at] = sh.lo;
+}
+
+template <int MT>
+struct GradTile {
+    static constexpr int COLS = MT == 1 ? 128 : 64, RANKS = 16 * MT, PITCH = COLS + 4;    // PITCH: of the sums in shared memory
+    static constexpr int V_BYTES = 16 * COLS * 2, P_BYTES = 16 * RANKS * 2, STAGE = V_BYTES + 2 * P_BYTES;
+    static constexpr size_t RING = (size_t)GR_WARPS * GR_STAGES * STAGE, SUMS = sizeof(float) * GR_WARPS * RANKS * PITCH, LIST = sizeof(uint32_t) * GR_WINDOW / 16;
+    static constexpr size_t SMEM = (RING > SUMS ? RING : SUMS) + LIST;
+};
+
+template <int MT>
+__device__ __forceinline__ void grad_task(const Grads& p, int task, uint8_t* smem, int* counts, int* is_last) {
+    using Tile = GradTile<MT>;
+    constexpr int COLS = Tile::COLS, RANKS = Tile::RANKS, PITCH = Tile::PITCH, CT = COLS / 8;
+    float* red = reinterpret_cast<float*>(smem);                       // [warps][RANKS][PITCH], where the rings were
+    uint32_t* list = reinterpret_cast<uint32_t*>(smem + Tile::SMEM - Tile::LIST);       // tile of the window << 16 | mask of its tokens
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3, row8 = lane & 7, quarter = lane >> 3;
+    // (adapters change fastest: the tasks of one with many tokens are spread over the blocks)
+    const int adapter = task % p.n_adapters, part = task / p.n_adapters % p.parts, block = task / p.n_adapters / p.parts;
+    const int slice = block / p.rank_blocks, j0 = block % p.rank_blocks * RANKS;
+    const bool of_x = slice < p.slices_x;
+    const int C = of_x ? p.K : p.N, c0 = (of_x ? slice : slice - p.slices_x) * COLS, M = p.M, r = p.r;
+    const bf16 *V = of_x ? p.X : p.dY, *P = of_x ? p.G : p.H;
+    const uint32_t ring = smem_u32(smem) + warp * GR_STAGES * Tile::STAGE;
+    // what a lane copies: a 16-byte piece of every PER-th row of V, and pieces of both parts of P.  Pieces are XORed by row.
+    constexpr int PIECES = COLS / 8, PER = 32 / PIECES, P_PIECES = RANKS / 8;
+    const int v_row = lane / PIECES, v_piece = lane % PIECES;
+    const bool v_in = c0 + 8 * v_piece < C;
+    const int p_row = lane / P_PIECES % 16, p_piece = lane % P_PIECES;
+    const bool p_in = j0 + 8 * p_piece < r;
+    float acc[MT][CT][4];
+    bool any = false;
+    for (int low_parts = 1; low_parts >= 0; --low_parts) {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int t = 0; t < CT; ++t) acc[mt][t][0] = acc[mt][t][1] = acc[mt][t][2] = acc[mt][t][3] = 0.f;
+        for (int w0 = 0; w0 < M; w0 += GR_WINDOW) {
+            // this warp looks at 512 places: lane i has tile i
+            const int from = w0 + warp * 512;
+            uint32_t mask = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int t = from + 32 * i + lane;
+                const uint32_t found = __ballot_sync(0xFFFFFFFFu, t < M && __ldg(p.adapter_of + t) == adapter);
+                if (lane >> 1 == i) mask = lane & 1 ? found >> 16 : found & 0xFFFFu;
+            }
+            const uint32_t tiles = __ballot_sync(0xFFFFFFFFu, mask != 0);
+            if (lane == 0) counts[warp] = __popc(tiles);
+            __syncthreads();
+            int at = 0, total = 0;
+#pragma unroll
+            for (int w = 0; w < GR_WARPS; ++w) {
+                if (w == warp) at = total;
+                total += counts[w];
+            }
+            if (mask != 0) list[at + __popc(tiles & ((1u << lane) - 1u))] = (uint32_t)(warp * 32 + lane) << 16 | mask;
+            __syncthreads();
+            any |= total > 0;
+            const int first = warp * p.parts + part, step = GR_WARPS * p.parts, mine = first < total ? (total - first + step - 1) / step : 0;
+            auto load = [&](int i) {
+                const uint32_t to = ring + (i % GR_STAGES) * Tile::STAGE, entry = list[first + i * step];
+                const int t0 = w0 + (int)(entry >> 16) * 16;
+                const bf16* v = V + (size_t)(t0 + v_row) * C + (v_in ? c0 + 8 * v_piece : 0);
+#pragma unroll
+                for (int n = 0; n < 16 / PER; ++n) {
+                    const int row = n * PER + v_row;
+                    const bool in = v_in && ((entry >> row) & 1u);
+                    copy16(to + row * (COLS * 2) + ((v_piece ^ (row & 7)) << 4), in ? v : V, in);      // (128 or 256 bytes to a row)
+                    v += (size_t)PER * C;
+                }
+                const bf16* low = P + (size_t)(t0 + p_row) * r + (p_in ? j0 + 8 * p_piece : 0);
+                const bool in = p_in && ((entry >> p_row) & 1u);
+                const uint32_t p_to = to + Tile::V_BYTES + p_row * (RANKS * 2) + ((p_piece ^ (p_row * P_PIECES / 8 % P_PIECES)) << 4);
+                if constexpr (P_PIECES == 2) {                         // 32 pieces in each part
+                    copy16(p_to, in ? low : P, in);
+                    copy16(p_to + Tile::P_BYTES, in ? low + (size_t)M * r : P, in);
+                } else {                                               // 64: eight rows further on as well
+                    const bool in8 = p_in && ((entry >> (p_row + 8)) & 1u);
+                    const uint32_t p_to8 = p_to + 8 * (RANKS * 2);     // (the same XOR: 8 rows of 64 bytes on)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        copy16(p_to + half * Tile::P_BYTES, in ? low + (size_t)half * M * r : P, in);
+                        copy16(p_to8 + half * Tile::P_BYTES, in8 ? low + ((size_t)half * M + 8) * r : P, in8);
+                    }
+                }
+            };
+#pragma unroll
+            for (int i = 0; i < GR_STAGES - 1; ++i) {
+                if (i < mine) load(i);
+                copy_commit();
+            }
+            const uint32_t v_off = (row8 + 8 * (quarter & 1)) * (COLS * 2), v_xor = (uint32_t)((quarter >> 1) ^ row8) << 4;
+            const int a_row = row8 + 8 * (quarter >> 1);
+#pragma unroll 1
+            for (int i = 0; i < mine; ++i) {
+                copy_wait<GR_STAGES - 2>();
+                __syncwarp();                                          // tile i is there, tile i - 1 has been read by every lane
+                if (i + GR_STAGES - 1 < mine) load(i + GR_STAGES - 1);
+                copy_commit();
+                const uint32_t v = ring + (i % GR_STAGES) * Tile::STAGE, pp = v + Tile::V_BYTES;
+                uint32_t a[2][MT][4];
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {                  // ranks 0 - 7, 8 - 15 of tokens 0 - 7; then of 8 - 15
+                        const int piece = 2 * mt + (quarter & 1);
+                        ldmatrix4<true>(pp + half * Tile::P_BYTES + a_row * (RANKS * 2) + ((piece ^ (a_row * P_PIECES / 8 % P_PIECES)) << 4), a[half][mt][0],
+                                        a[half][mt][1], a[half][mt][2], a[half][mt][3]);
+                    }
+#pragma unroll
+                for (int t = 0; t < CT; t += 2) {                      // tokens 0 - 7, 8 - 15 of columns 8 t ..; then of the next eight
+                    uint32_t b[4];
+                    ldmatrix4<true>(v + v_off + (v_xor ^ (t << 4)), b[0], b[1], b[2], b[3]);
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        mma_bf16_16816(acc[mt][t], a[0][mt][0], a[0][mt][1], a[0][mt][2], a[0][mt][3], b[0], b[1]);
+                        mma_bf16_16816(acc[mt][t + 1], a[0][mt][0], a[0][mt][1], a[0][mt][2], a[0][mt][3], b[2], b[3]);
+                        if (low_parts) {
+                            mma_bf16_16816(acc[mt][t], a[1][mt][0], a[1][mt][1], a[1][mt][2], a[1][mt][3], b[0], b[1]);
+                            mma_bf16_16816(acc[mt][t + 1], a[1][mt][0], a[1][mt][1], a[1][mt][2], a[1][mt][3], b[2], b[3]);
+                        }
+                    }
+                }
+            }
+            copy_wait<0>();
+            __syncthreads();                                           // the list is written again, the sums where the rings are
+        }
+        float worst = 0.f;                                             // (x - x is 0, or a NaN)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int t = 0; t < CT; ++t)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) worst += acc[mt][t][k] - acc[mt][t][k];
+        if (!__syncthreads_or(worst != 0.f)) break;
+    }
+    if (!any && p.accumulate) return;                                  // (the same for the whole block, and for all parts)
+    // [mt][t][c]: rank 16 mt + g (+ 8 where c >= 2), column 8 t + 2 q + c % 2
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
+        for (int t = 0; t < CT; ++t)
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    *reinterpret_cast<float2*>(red + ((size_t)warp * MT * 16 + 16 * mt + 8 * h + g) * COLS + 32 * nb + 8 * q + 2 * t) =
-                        make_float2(acc[mt][nb][t][2 * h], acc[mt][nb][t][2 * h + 1]);
+            for (int h = 0; h < 2; ++h)
+                *reinterpret_cast<float2*>(red + ((size_t)warp * RANKS + 16 * mt + 8 * h + g) * PITCH + 8 * t + 2 * q) =
+                    make_float2(acc[mt][t][2 * h], acc[mt][t][2 * h + 1]);
     __syncthreads();
-    const float s = scales[adapter];
-    for (int idx = threadIdx.x; idx < r * COLS; idx += 32 * GR_WARPS) {
-        // in the order of the output: A's gradient along the columns, B's along the ranks
-        const int j = of_x ? idx / COLS : idx % r, c = of_x ? idx % COLS : idx / r;
-        if (c0 + c >= C) continue;
+    const bool split = p.parts > 1 && any;
+    const size_t whole = (size_t)block * p.n_adapters + adapter;
+    float* partial = p.partial + whole * p.parts * (RANKS * COLS);
+    auto sum = [&](int j, int c) {
         float v = 0.f;
 #pragma unroll
-        for (int w = 0; w < GR_WARPS; ++w) v += red[((size_t)w * MT * 16 + j) * COLS + c];
-        float* dst = of_x ? dA + ((size_t)adapter * r + j) * K + c0 + c : dB + ((size_t)adapter * N + c0 + c) * r + j;
+        for (int w = 0; w < GR_WARPS; ++w) v += red[(w * RANKS + j) * PITCH + c];
+        return v;
+    };
+    if (split) {
+        for (int idx = threadIdx.x; idx < RANKS * COLS; idx += 32 * GR_WARPS) __stcg(partial + (size_t)part * RANKS * COLS + idx, sum(idx / COLS, idx % COLS));
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            *is_last = atomicAdd(p.counters + 1 + whole, 1u) == (unsigned)p.parts - 1u;
+            __threadfence();
+        }
+        __syncthreads();
+        if (!*is_last) return;
+    } else if (part > 0) {
+        return;                                                        // an adapter without tokens: its zeros are written once
+    }
+    const float s = p.scales[adapter];
+    const int ranks = min(RANKS, r - j0);
+#pragma unroll 4
+    for (int idx = threadIdx.x; idx < RANKS * COLS; idx += 32 * GR_WARPS) {
+        // in the order of the output: A's gradient along the columns, B's along the ranks
+        const int j = of_x ? idx / COLS : idx % RANKS, c = of_x ? idx % COLS : idx / RANKS;
+        if (j >= ranks || c0 + c >= C) continue;
+        float v = 0.f;
+        if (split) {
+            for (int k = 0; k < p.parts; ++k) v += __ldcg(partial + ((size_t)k * RANKS + j) * COLS + c);
+        } else {
+            v = sum(j, c);
+        }
+        float* dst = of_x ? p.dA + ((size_t)adapter * r + j0 + j) * p.K + c0 + c : p.dB + ((size_t)adapter * p.N + c0 + c) * r + j0 + j;
         v = any ? s * v : 0.f;
-        *dst = accumulate ? *dst + v : v;
+        *dst = p.accumulate ? *dst + v : v;
     }
 }
 
-template <bool L_IS_A, int NT>
-int down_impl(int M, int T, int r, int n_adapters, const void* In, const int32_t* adapter_of, const void* L, float* P, cudaStream_t st) {
-    return launch_pdl(adapters_down_kernel<L_IS_A, NT>, dim3((M + DN_ROWS - 1) / DN_ROWS, DN_SHARE), dim3(32 * DN_WARPS<NT>), 0, st, 1, M, T, r, n_adapters,
-                      (const bf16*)In, adapter_of, (const bf16*)L, P) == cudaSuccess ? QLORA_OK : QLORA_ERR_CUDA;
+template <int MT>
+__global__ void __launch_bounds__(32 * GR_WARPS, GR_BLOCKS)
+adapters_grad_kernel(const Grads p) {
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ int counts[GR_WARPS], claimed, is_last;
+    pdl_launch_dependents();
+    pdl_wait();
+    const int n_tasks = p.slices * p.rank_blocks * p.n_adapters * p.parts;
+    for (;;) {
+        __syncthreads();                                               // shared memory is written again
+        if (threadIdx.x == 0) claimed = (int)atomicAdd(p.counters, 1u);
+        __syncthreads();
+        const int task = claimed;
+        if (task >= n_tasks) break;
+        grad_task<MT>(p, task, smem, counts, &is_last);
+    }
 }
 
-template <bool FORWARD, int NT>
-int few_impl(int M, int T, int C, int r, int L, const void* In, const int32_t* adapter_of, const void* L1, const void* L2, const float* scales,
-             const void* Base, void* Out, float* P_out, cudaStream_t st) {
-    return launch_pdl(adapters_few_kernel<FORWARD, NT>, dim3((M + FEW_ROWS - 1) / FEW_ROWS * FEW_CTAS), dim3(32 * FEW_WARPS), 0, st, 1, M, T, C, r, L,
-                      (const bf16*)In, adapter_of, (const bf16*)L1, (const bf16*)L2, scales, (const bf16*)Base, (bf16*)Out, P_out) == cudaSuccess
+template <bool L_IS_A, int NT, int NB>
+int down_impl(const Products& p, cudaStream_t st) {
+    constexpr size_t smem = DownTile<L_IS_A, NT, NB>::SMEM;
+    static SmemLimit limit;
+    auto kern = adapters_down_kernel<L_IS_A, NT, NB>;
+    if (!limit.raise(kern, smem)) return QLORA_ERR_CUDA;
+    const int tiles = (p.M + 16 * NB - 1) / (16 * NB);
+    return launch_pdl(kern, dim3(tiles + sm_count()), dim3(32 * DN_WARPS), smem, st, 1, p, tiles) == cudaSuccess ? QLORA_OK : QLORA_ERR_CUDA;
+}
+
+template <bool FROM_B, int KS, int UB>
+int up_impl(const Products& p, cudaStream_t st) {
+    const int columns = (p.C + 32 * UB * UP_WARPS - 1) / (32 * UB * UP_WARPS), tiles = (p.M + UP_ROWS - 1) / UP_ROWS;
+    // as many tiles to a block as leave every SM its two blocks twice
+    int each = (int)((long long)tiles * columns / (4 * sm_count()));
+    each = each < 1 ? 1 : each > 16 ? 16 : each;
+    return launch_pdl(adapters_up_kernel<FROM_B, KS, UB>, dim3((tiles + each - 1) / each, columns), dim3(32 * UP_WARPS), 0, st, 1, p, each) == cudaSuccess
+               ? QLORA_OK : QLORA_ERR_CUDA;
+}
+
+template <bool FORWARD, int NT, int ROWS>
+int few_impl(const Products& p, cudaStream_t st) {
+    return launch_pdl(adapters_few_kernel<FORWARD, NT, ROWS>, dim3((p.M + ROWS - 1) / ROWS * FEW_CTAS), dim3(32 * FEW_WARPS), 0, st, 1, p) == cudaSuccess
                ? QLORA_OK : QLORA_ERR_CUDA;   // (the cluster's width is an attribute of the kernel)
 }
 
-template <int MT, int NB>
-int grad_impl(int M, int K, int N, int r, int L, const void* X, const void* dY, const int32_t* adapter_of, const float* scales, const float* H,
-              const float* G, float* dA, float* dB, int accumulate, cudaStream_t st) {
-    constexpr size_t smem = sizeof(float) * GR_WARPS * MT * 16 * 32 * NB;
+template <bool FORWARD, int NT, int NB, int KS, int UB>
+int products(const Products& p, cudaStream_t st) {
+    if (p.Out != nullptr && p.M <= FEW_TOKENS) return p.M <= 64 ? few_impl<FORWARD, NT, 1>(p, st) : few_impl<FORWARD, NT, 4>(p, st);
+    const int rc = down_impl<FORWARD, NT, NB>(p, st);
+    return rc != QLORA_OK || p.Out == nullptr ? rc : up_impl<FORWARD, KS, UB>(p, st);
+}
+
+// How the gradients are cut into tasks: into parts where the slices are too few for every SM to have all its blocks.
+void cut_grads(Grads& p) {
+    const int columns = p.r <= 16 ? GradTile<1>::COLS : GradTile<2>::COLS, ranks = p.r <= 16 ? GradTile<1>::RANKS : GradTile<2>::RANKS;
+    p.slices_x = (p.K + columns - 1) / columns;
+    p.slices = p.slices_x + (p.N + columns - 1) / columns;
+    p.rank_blocks = (p.r + ranks - 1) / ranks;
+    const long long whole = (long long)p.slices * p.rank_blocks * p.n_adapters, wanted = GR_BLOCKS * sm_count();
+    p.parts = whole >= wanted || whole == 0 ? 1 : (int)(wanted / whole < 8 ? (wanted + whole - 1) / whole : 8);
+}
+
+struct GradScratch { size_t g, h, counters, partial, total; };
+GradScratch grad_scratch(const Grads& p) {
+    auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    const size_t whole = (size_t)p.slices * p.rank_blocks * p.n_adapters, ranks = p.r <= 16 ? GradTile<1>::RANKS : GradTile<2>::RANKS,
+                 columns = p.r <= 16 ? GradTile<1>::COLS : GradTile<2>::COLS;
+    GradScratch s;
+    s.g = 0;
+    s.h = up((size_t)p.M * p.r * 4);
+    s.counters = s.h + up((size_t)p.M * p.r * 4);
+    s.partial = s.counters + up(4 * (p.parts > 1 ? 1 + whole : 1));
+    s.total = s.partial + (p.parts > 1 ? whole * p.parts * ranks * columns * sizeof(float) : 0);
+    return s;
+}
+
+template <int MT>
+int grad_impl(const Grads& p, cudaStream_t st) {
     static SmemLimit limit;
-    auto kern = adapters_grad_kernel<MT, NB>;
-    if (!limit.raise(kern, smem)) return QLORA_ERR_CUDA;
-    const int slices = (K + 32 * NB - 1) / (32 * NB) + (N + 32 * NB - 1) / (32 * NB);
-    return launch_pdl(kern, dim3(slices, L), dim3(32 * GR_WARPS), smem, st, 1, M, K, N, r, L, (const bf16*)X, (const bf16*)dY, adapter_of, scales, H, G,
-                      dA, dB, accumulate) == cudaSuccess ? QLORA_OK : QLORA_ERR_CUDA;
+    auto kern = adapters_grad_kernel<MT>;
+    if (!limit.raise(kern, GradTile<MT>::SMEM)) return QLORA_ERR_CUDA;
+    const long long tasks = (long long)p.slices * p.rank_blocks * p.n_adapters * p.parts, blocks = (long long)GR_BLOCKS * sm_count();
+    return launch_pdl(kern, dim3((unsigned)(tasks < blocks ? tasks : blocks)), dim3(32 * GR_WARPS), GradTile<MT>::SMEM, st, 1, p) == cudaSuccess ? QLORA_OK
+                                                                                                                                                    : QLORA_ERR_CUDA;
 }
 
 }  // namespace
 
-int launch_adapters_down(int M, int T, int r, int n_adapters, bool l_is_A, const void* In, const int32_t* adapter_of, const void* L, float* P, cudaStream_t st) {
-#define QLORA_DOWN(NT) return l_is_A ? down_impl<true, NT>(M, T, r, n_adapters, In, adapter_of, L, P, st) : down_impl<false, NT>(M, T, r, n_adapters, In, adapter_of, L, P, st)
-    if (r <= 8) QLORA_DOWN(1);
-    if (r <= 16) QLORA_DOWN(2);
-    if (r <= 32) QLORA_DOWN(4);
-    QLORA_DOWN(8);
-#undef QLORA_DOWN
+int launch_adapters(bool forward, int M, int T, int C, int r, int n_adapters, const void* In, const int32_t* adapter_of, const void* L1, const void* L2,
+                    const float* scales, const void* Base, void* Out, float* P, void* split, cudaStream_t st) {
+    const Products p{M, T, C, r, n_adapters, (const bf16*)In, adapter_of, (const bf16*)L1, (const bf16*)L2, scales, (const bf16*)Base, (bf16*)Out, P, (uint2*)split};
+#define QLORA_PRODUCTS(NT, NB, KS, UB) return forward ? products<true, NT, NB, KS, UB>(p, st) : products<false, NT, NB, KS, UB>(p, st)
+    if (r <= 8) QLORA_PRODUCTS(1, 1, 1, 2);
+    if (r <= 16) QLORA_PRODUCTS(2, 1, 1, 2);
+    if (r <= 32) QLORA_PRODUCTS(4, 2, 2, 1);
+    QLORA_PRODUCTS(8, 2, 4, 1);
+#undef QLORA_PRODUCTS
 }
 
-int launch_adapters_up(int M, int C, int r, int n_adapters, bool from_B, const float* P, const int32_t* adapter_of, const void* L, const float* scales,
-                       const void* Base, void* Out, cudaStream_t st) {
-    const dim3 grid((M + UP_ROWS - 1) / UP_ROWS, (C + 32 * UP_BLOCKS * UP_WARPS - 1) / (32 * UP_BLOCKS * UP_WARPS));
-    return launch_pdl(from_B ? adapters_up_kernel<true> : adapters_up_kernel<false>, grid, dim3(32 * UP_WARPS), 0, st, 1, M, C, r, n_adapters, P, adapter_of,
-                      (const bf16*)L, scales, (const bf16*)Base, (bf16*)Out) == cudaSuccess ? QLORA_OK : QLORA_ERR_CUDA;
-}
-
-bool adapters_few(int M) { return M <= 256; }
-
-int launch_adapters_few(int M, int T, int C, int r, int n_adapters, bool forward, const void* In, const int32_t* adapter_of, const void* L1, const void* L2,
-                        const float* scales, const void* Base, void* Out, float* P_out, cudaStream_t st) {
-#define QLORA_FEW(NT)                                                                                                               \
-    return forward ? few_impl<true, NT>(M, T, C, r, n_adapters, In, adapter_of, L1, L2, scales, Base, Out, P_out, st)              \
-                   : few_impl<false, NT>(M, T, C, r, n_adapters, In, adapter_of, L1, L2, scales, Base, Out, P_out, st)
-    if (r <= 8) QLORA_FEW(1);
-    if (r <= 16) QLORA_FEW(2);
-    if (r <= 32) QLORA_FEW(4);
-    QLORA_FEW(8);
-#undef QLORA_FEW
+size_t adapters_grad_scratch_bytes(int M, int K, int N, int r, int n_adapters) {
+    Grads p{};
+    p.M = M; p.K = K; p.N = N; p.r = r; p.n_adapters = n_adapters;
+    cut_grads(p);
+    return grad_scratch(p).total;
 }
 
 int launch_adapters_grads(int M, int K, int N, int r, int n_adapters, const void* X, const void* dY, const int32_t* adapter_of, const float* scales,
-                          const float* H, const float* G, float* dA, float* dB, int accumulate, cudaStream_t st) {
-#define QLORA_GRAD(MT, NB) return grad_impl<MT, NB>(M, K, N, r, n_adapters, X, dY, adapter_of, scales, H, G, dA, dB, accumulate, st)
-    if (r <= 16) QLORA_GRAD(1, 2);
-    if (r <= 32) QLORA_GRAD(2, 1);
-    QLORA_GRAD(4, 1);
-#undef QLORA_GRAD
+                          const float* H, const float* G, float* dA, float* dB, int accumulate, void* scratch, cudaStream_t st) {
+    Grads p{};
+    p.M = M; p.K = K; p.N = N; p.r = r; p.n_adapters = n_adapters;
+    p.X = (const bf16*)X; p.dY = (const bf16*)dY; p.adapter_of = adapter_of; p.scales = scales; p.dA = dA; p.dB = dB; p.accumulate = accumulate;
+    cut_grads(p);
+    const GradScratch s = grad_scratch(p);
+    char* at = static_cast<char*>(scratch);
+    p.G = reinterpret_cast<bf16*>(at + s.g);
+    p.H = reinterpret_cast<bf16*>(at + s.h);
+    p.counters = reinterpret_cast<unsigned*>(at + s.counters);
+    p.partial = reinterpret_cast<float*>(at + s.partial);
+    const long long n = (long long)M * r;
+    if (launch_pdl(adapters_split_kernel, dim3((unsigned)(n == 0 ? 1 : (n / 2 + 255) / 256)), dim3(256), 0, st, 1, n, G, H, reinterpret_cast<uint32_t*>(at + s.g),
+                   reinterpret_cast<uint32_t*>(at + s.h), p.counters, (int)((s.partial - s.counters) / 4)) != cudaSuccess)
+        return QLORA_ERR_CUDA;
+    return r <= 16 ? grad_impl<1>(p, st) : grad_impl<2>(p, st);
 }
 
 }  // namespace qlora

@@ -91,7 +91,9 @@ int check_adapters(const qlora_adapters_desc* d) {
     if (d->K % 32 != 0 || d->N % 8 != 0 || d->r % 8 != 0 || d->r == 0 || d->r > 64 || d->n_adapters > 65535) return QLORA_ERR_UNSUPPORTED;
     return QLORA_OK;
 }
+// Workspace of the calls on adapters: two [M, r] products, then the scratch of the gradients.
 size_t adapters_low_bytes(const qlora_adapters_desc& d, int M) { return align_up((size_t)M * (size_t)d.r * sizeof(float), 256); }
+size_t adapters_bytes(const qlora_adapters_desc& d, int M) { return 2 * adapters_low_bytes(d, M) + adapters_grad_scratch_bytes(M, d.K, d.N, d.r, d.n_adapters); }
 
 struct Workspace {
     size_t p0_off, p1_off, grad_off, sync_off, split_off, db_off;
@@ -249,14 +251,14 @@ int qlora_adapters_workspace_bytes(const qlora_adapters_desc* desc, int M, size_
     if (out == nullptr || M < 0) return QLORA_ERR_INVALID_ARG;
     const int rc = check_adapters(desc);
     if (rc != QLORA_OK) return rc;
-    *out = align_up(2 * adapters_low_bytes(*desc, M), 256) + 256;
+    *out = adapters_bytes(*desc, M);
     return QLORA_OK;
 }
 
 // Forward: In = X [M, K], Base and Out [M, N].  Backward: In = dY [M, N], Base and Out [M, K].
 static int adapters_common(bool forward, const qlora_adapters_desc* desc, int M, const void* In, const int32_t* adapter_of, const void* A, const void* B,
                            const float* scales, const void* Base, void* Out, float* low, void* workspace, size_t workspace_bytes, void* cuda_stream) {
-    int rc = check_adapters(desc);
+    const int rc = check_adapters(desc);
     if (rc != QLORA_OK) return rc;
     if (M < 0) return QLORA_ERR_INVALID_ARG;
     const qlora_adapters_desc& d = *desc;
@@ -267,14 +269,9 @@ static int adapters_common(bool forward, const qlora_adapters_desc* desc, int M,
     if (!aligned16(In) || !aligned4(adapter_of) || !aligned16(A) || !aligned16(B) || !aligned4(scales) || !aligned16(Base) || !aligned16(Out) ||
         !aligned16(low) || !aligned16(workspace))
         return QLORA_ERR_ALIGNMENT;
-    if (workspace == nullptr || workspace_bytes < 2 * adapters_low_bytes(d, M)) return QLORA_ERR_WORKSPACE;
-    cudaStream_t st = (cudaStream_t)cuda_stream;
-    const void *L1 = forward ? A : B, *L2 = forward ? B : A;
-    if (adapters_few(M)) return launch_adapters_few(M, T, C, d.r, d.n_adapters, forward, In, adapter_of, L1, L2, scales, Base, Out, low, st);
-    float* P = low ? low : static_cast<float*>(workspace);
-    rc = launch_adapters_down(M, T, d.r, d.n_adapters, forward, In, adapter_of, L1, P, st);
-    if (rc != QLORA_OK) return rc;
-    return launch_adapters_up(M, C, d.r, d.n_adapters, forward, P, adapter_of, L2, scales, Base, Out, st);
+    if (workspace == nullptr || workspace_bytes < adapters_bytes(d, M)) return QLORA_ERR_WORKSPACE;
+    return launch_adapters(forward, M, T, C, d.r, d.n_adapters, In, adapter_of, forward ? A : B, forward ? B : A, scales, Base, Out, low, workspace,
+                           (cudaStream_t)cuda_stream);
 }
 
 int qlora_adapters_fwd(const qlora_adapters_desc* desc, int M, const void* X, const int32_t* adapter_of, const void* A, const void* B, const float* scales,
@@ -300,21 +297,22 @@ int qlora_adapters_bwd_lora(const qlora_adapters_desc* desc, int M, const void* 
     if (!aligned16(X) || !aligned16(dY) || !aligned4(adapter_of) || !aligned16(A) || !aligned16(B) || !aligned4(scales) || !aligned16(H) || !aligned16(G) ||
         !aligned16(dA) || !aligned16(dB) || !aligned16(workspace))
         return QLORA_ERR_ALIGNMENT;
-    if (workspace == nullptr || workspace_bytes < 2 * adapters_low_bytes(d, M)) return QLORA_ERR_WORKSPACE;
+    if (workspace == nullptr || workspace_bytes < adapters_bytes(d, M)) return QLORA_ERR_WORKSPACE;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (M > 0 && !H) {
         float* Hs = static_cast<float*>(workspace);
-        rc = launch_adapters_down(M, d.K, d.r, d.n_adapters, true, X, adapter_of, A, Hs, st);
+        rc = launch_adapters(true, M, d.K, 0, d.r, d.n_adapters, X, adapter_of, A, nullptr, scales, nullptr, nullptr, Hs, nullptr, st);
         if (rc != QLORA_OK) return rc;
         H = Hs;
     }
     if (M > 0 && !G) {
         float* Gs = reinterpret_cast<float*>(static_cast<char*>(workspace) + adapters_low_bytes(d, M));
-        rc = launch_adapters_down(M, d.N, d.r, d.n_adapters, false, dY, adapter_of, B, Gs, st);
+        rc = launch_adapters(false, M, d.N, 0, d.r, d.n_adapters, dY, adapter_of, B, nullptr, scales, nullptr, nullptr, Gs, nullptr, st);
         if (rc != QLORA_OK) return rc;
         G = Gs;
     }
-    return launch_adapters_grads(M, d.K, d.N, d.r, d.n_adapters, X, dY, adapter_of, scales, H, G, dA, dB, accumulate, st);
+    return launch_adapters_grads(M, d.K, d.N, d.r, d.n_adapters, X, dY, adapter_of, scales, H, G, dA, dB, accumulate,
+                                 static_cast<char*>(workspace) + 2 * adapters_low_bytes(d, M), st);
 }
 
 static int check_head(int T, int V, int D) {

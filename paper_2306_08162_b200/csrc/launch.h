@@ -30,18 +30,15 @@ int launch_token_logprobs_bwd(int T, int V, long long row_stride, int dtype, con
 int launch_grad_norm(const qlora_adamw_desc& d, float prescale, float max_norm, float* out, void* workspace, cudaStream_t st);
 int launch_adamw(const qlora_adamw_desc& d, double lr, int step, const float* lr_dev, const int32_t* step_dev, const float* norm, cudaStream_t st);
 
-// adapter_kernels.cu -- adapters of many requests: L [n_adapters, ...], the adapter of each row of In in adapter_of (none outside [0, n_adapters))
-// P[m, :] = In[m, :] L_a (rows without an adapter: 0); l_is_A: L = A [., r, T], else B [., T, r]
-int launch_adapters_down(int M, int T, int r, int n_adapters, bool l_is_A, const void* In, const int32_t* adapter_of, const void* L, float* P, cudaStream_t st);
-// Out[m, :] = Base[m, :] + scales[a] P[m, :] L_a; from_B: L = B [., C, r], else A [., r, C]; Out may be Base
-int launch_adapters_up(int M, int C, int r, int n_adapters, bool from_B, const float* P, const int32_t* adapter_of, const void* L, const float* scales,
-                       const void* Base, void* Out, cudaStream_t st);
-// Both in one launch, for so few rows.  forward: L1 = A, L2 = B, else the reverse; P_out may be NULL.
-bool adapters_few(int M);
-int launch_adapters_few(int M, int T, int C, int r, int n_adapters, bool forward, const void* In, const int32_t* adapter_of, const void* L1, const void* L2,
-                        const float* scales, const void* Base, void* Out, float* P_out, cudaStream_t st);
+// adapter_kernels.cu -- adapters of many requests, the adapter of each row of In in adapter_of (none outside [0, n_adapters)):
+//   P[m, :] = In[m, :] L1_a (rows without an adapter: 0),   Out[m, :] = Base[m, :] + scales[a] P[m, :] L2_a
+// forward: L1 = A [., r, T], L2 = B [., C, r]; else L1 = B [., T, r], L2 = A [., r, C].  Out may be Base, or NULL: P alone (then L2, scales and Base may be NULL
+// too); P may be NULL otherwise.  split: scratch of M r / 2 x 8 bytes (with Out).
+int launch_adapters(bool forward, int M, int T, int C, int r, int n_adapters, const void* In, const int32_t* adapter_of, const void* L1, const void* L2,
+                    const float* scales, const void* Base, void* Out, float* P, void* split, cudaStream_t st);
 int launch_adapters_grads(int M, int K, int N, int r, int n_adapters, const void* X, const void* dY, const int32_t* adapter_of, const float* scales,
-                          const float* H, const float* G, float* dA, float* dB, int accumulate, cudaStream_t st);
+                          const float* H, const float* G, float* dA, float* dB, int accumulate, void* scratch, cudaStream_t st);
+size_t adapters_grad_scratch_bytes(int M, int K, int N, int r, int n_adapters);
 
 // head_loss_kernel.cu -- cross entropy of the head from the hidden states; d_hidden NULL: the loss alone
 size_t head_loss_workspace_bytes(int T, int V, int D, bool grad);
