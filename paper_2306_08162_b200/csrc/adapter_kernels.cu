@@ -71,7 +71,7 @@ __device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t& a, uint32_t& 
 // Both products of ROWS tokens by a cluster (or one block).  Its CTAs share the contraction out; each stores its sums into the shared memory of all, and one cluster
 // barrier later they share the columns out.  The adapters' second matrices are asked into L2 before the first product begins.  The second product
 // is fp32 throughout: a few tokens leave the CUDA cores enough time.
-constexpr int FEW_CTAS = 8, FEW_WARPS = 8, FEW_TOKENS = 256;
+constexpr int FEW_WARPS = 8, FEW_TOKENS = 256;
 
 template <int NT, int ROWS, int CTAS>
 struct FewShared {
@@ -257,15 +257,15 @@ __device__ __forceinline__ void few_tokens(const Products& p, int m0, FewShared<
                     *reinterpret_cast<uint32_t*>(p.Out + (size_t)(m0 + i) * C + 2 * c) = *reinterpret_cast<const uint32_t*>(p.Base + (size_t)(m0 + i) * C + 2 * c);
 }
 
-template <bool FORWARD, int NT, int ROWS>
-__global__ void __cluster_dims__(FEW_CTAS, 1, 1) __launch_bounds__(32 * FEW_WARPS)
+template <bool FORWARD, int NT, int ROWS, int CTAS>
+__global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(32 * FEW_WARPS, 2)
 adapters_few_kernel(const Products p) {
-    __shared__ __align__(16) FewShared<NT, ROWS, FEW_CTAS> sh;
+    __shared__ __align__(16) FewShared<NT, ROWS, CTAS> sh;
     pdl_launch_dependents();
     cluster_arrive();                                                  // (a CTA's shared memory is written to once it has begun)
     pdl_wait();
     cluster_wait();
-    few_tokens<FORWARD, NT, ROWS, FEW_CTAS>(p, (int)(blockIdx.x / FEW_CTAS) * ROWS, sh);
+    few_tokens<FORWARD, NT, ROWS, CTAS>(p, (int)(blockIdx.x / CTAS) * ROWS, sh);
 }
 
 // ---------------------------------------------------------------------------------------------------------------- down
@@ -286,20 +286,22 @@ __device__ __forceinline__ bool of_scattered_tile(int adapter) {
 }
 
 // Every warp has a ring of its own in shared memory, a stage of which holds 64 contraction elements of the tile's rows and of the adapter; copies
-// run ahead without holding registers.  16-byte pieces are XORed by row, so that the matrix loads have no bank conflicts.
-template <bool L_IS_A, int NT, int NB>
+// run ahead without holding registers.  16-byte pieces are XORed by row, so that the matrix loads have no bank conflicts.  Where there are few tiles a
+// cluster of CTAS blocks shares the contraction out, and its first one adds their sums in order.
+template <bool L_IS_A, int NT, int NB, int CTAS>
 struct DownTile {
     static constexpr int ROWS = 16 * NB, CHUNK = 64;
     static constexpr int IN_BYTES = ROWS * 128, L_BYTES = NT * 8 * 128, STAGE = IN_BYTES + L_BYTES;
     static constexpr int STAGES = NT == 1 ? 4 : NT == 8 ? 2 : 3;
     static constexpr size_t RING = (size_t)STAGES * STAGE * DN_WARPS, SUMS = sizeof(float) * DN_WARPS * NB * NT * 128, FEW = sizeof(FewShared<NT, 1, 1>);
-    static constexpr size_t SMEM = RING > SUMS ? (RING > FEW ? RING : FEW) : (SUMS > FEW ? SUMS : FEW);
+    static constexpr size_t OWN = RING > SUMS ? (RING > FEW ? RING : FEW) : (SUMS > FEW ? SUMS : FEW), PARTS = CTAS > 1 ? CTAS * NB * NT * 64 * sizeof(float2) : 0;
+    static constexpr size_t SMEM = OWN + PARTS;
 };
 
-template <bool L_IS_A, int NT, int NB>
+template <bool L_IS_A, int NT, int NB, int CTAS>
 __global__ void __launch_bounds__(32 * DN_WARPS, NT <= 2 ? 2 : 1)
 adapters_down_kernel(const Products p, int n_tiles) {
-    using Tile = DownTile<L_IS_A, NT, NB>;
+    using Tile = DownTile<L_IS_A, NT, NB, CTAS>;
     constexpr int ROWS = Tile::ROWS, CHUNK = Tile::CHUNK, STAGES = Tile::STAGES;
     union Shared {
         float red[DN_WARPS][NB][NT][4][32];
@@ -309,11 +311,13 @@ adapters_down_kernel(const Products p, int n_tiles) {
     Shared& sh = *reinterpret_cast<Shared*>(smem);
     __shared__ uint32_t scattered[DN_WINDOW / 512];                    // a bit for every tile of 16
     pdl_launch_dependents();
+    if (CTAS > 1) cluster_arrive();                                    // (a block's shared memory is written to once it has begun)
     pdl_wait();
+    if (CTAS > 1) cluster_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int M = p.M, T = p.T, r = p.r;
-    if ((int)blockIdx.x >= n_tiles) {
-        const int me = (int)blockIdx.x - n_tiles, blocks = (int)gridDim.x - n_tiles;
+    if ((int)blockIdx.x >= n_tiles * CTAS) {
+        const int me = (int)blockIdx.x - n_tiles * CTAS, blocks = (int)gridDim.x - n_tiles * CTAS;
         int n = 0;                                                     // tokens of such tiles so far
         for (int w0 = 0; w0 < M; w0 += DN_WINDOW) {
             const int chunks = min(DN_WINDOW, M - w0 + 31) / 32;       // of 32 tokens
@@ -347,19 +351,21 @@ adapters_down_kernel(const Products p, int n_tiles) {
         }
         return;
     }
-    const int m0 = (int)blockIdx.x * ROWS;
+    const int m0 = (int)blockIdx.x / CTAS * ROWS, cta = CTAS > 1 ? (int)cluster_ctarank() : 0;
+    constexpr int ALL = DN_WARPS * CTAS;                               // warps of the tile
+    const int me = cta * DN_WARPS + warp;
     const uint32_t ring = smem_u32(smem) + warp * STAGES * Tile::STAGE;
-    const int chunks = (T + CHUNK - 1) / CHUNK, mine = warp < chunks ? (chunks - warp + DN_WARPS - 1) / DN_WARPS : 0;
+    const int chunks = (T + CHUNK - 1) / CHUNK, mine = me < chunks ? (chunks - me + ALL - 1) / ALL : 0;
     // what a lane copies: a 16-byte piece of every fourth row of the tile, and of the adapter
     const int piece = lane & 7, row0 = lane >> 3;
-    const bf16* in0 = p.In + (size_t)(m0 + row0) * T + warp * CHUNK + 8 * piece;
+    const bf16* in0 = p.In + (size_t)(m0 + row0) * T + me * CHUNK + 8 * piece;
     uint32_t rows_in = 0;
 #pragma unroll
     for (int n = 0; n < ROWS / 4; ++n) rows_in |= (uint32_t)(m0 + row0 + 4 * n < M) << n;
     const uint32_t swizzled[2] = {(uint32_t)(row0 * 128 + ((piece ^ row0) << 4)), (uint32_t)(row0 * 128 + ((piece ^ (row0 + 4)) << 4))};   // rows 4 n: n even, odd
     auto load_in = [&](int i) {                                        // chunk i of this warp's
-        const int from = i * (DN_WARPS * CHUNK);
-        const bool k_in = warp * CHUNK + 8 * piece + from < T;
+        const int from = i * (ALL * CHUNK);
+        const bool k_in = me * CHUNK + 8 * piece + from < T;
         const bf16* src = in0 + from;
         const uint32_t to = ring + (i % STAGES) * Tile::STAGE;
 #pragma unroll
@@ -370,7 +376,7 @@ adapters_down_kernel(const Products p, int n_tiles) {
         }
     };
     auto load_adapter = [&](int i, const bf16* La) {
-        const int from = i * (DN_WARPS * CHUNK), k0 = warp * CHUNK + from;
+        const int from = i * (ALL * CHUNK), k0 = me * CHUNK + from;
         const uint32_t to = ring + (i % STAGES) * Tile::STAGE + Tile::IN_BYTES;
         if constexpr (L_IS_A) {                                        // rows of ranks, 64 elements each
             const bool k_in = k0 + 8 * piece < T;
@@ -395,11 +401,24 @@ adapters_down_kernel(const Products p, int n_tiles) {
     for (int i = 0; i < STAGES - 1 && i < mine; ++i) load_in(i);       // on their way while the tile's adapters are looked at
     if (a < 0 || a >= p.n_adapters) a = -1;
     const bool elsewhere = of_scattered_tile(a);
-    if (warp == 0 && p.P != nullptr && in && a < 0 && !elsewhere)
+    if (me == 0 && p.P != nullptr && in && a < 0 && !elsewhere)
         for (int j = 0; j < r; j += 4) *reinterpret_cast<float4*>(p.P + (size_t)(m0 + lane) * r + j) = make_float4(0.f, 0.f, 0.f, 0.f);
     if (elsewhere) a = -1;
     const uint32_t mask_here = entry_of_lane(a);
     uint32_t firsts = __ballot_sync(0xFFFFFFFFu, mask_here != 0);
+    const uint32_t parts = smem_u32(smem) + (uint32_t)Tile::OWN;
+    // two neighbouring ranks of a row
+    auto take = [&](int idx, uint32_t mask, float s, float v0, float v1) {
+        const int b = idx / (NT * 64), nt = (idx >> 6) % NT, h = (idx >> 5) & 1, ln = idx & 31;
+        const int row = 16 * b + (ln >> 2) + 8 * h, col = nt * 8 + (ln & 3) * 2;
+        if (!((mask >> row) & 1u) || col >= r) return;
+        const size_t at = ((size_t)(m0 + row) * r + col) / 2;
+        if (p.P != nullptr) reinterpret_cast<float2*>(p.P)[at] = make_float2(v0, v1);
+        if (p.split != nullptr) {
+            const Split v = split_bf16(s * v0, s * v1);
+            p.split[at] = make_uint2(v.hi, v.lo);
+        }
+    };
     bool begun = true;
     for (; firsts != 0; firsts &= firsts - 1) {
         const int first = __ffs(firsts) - 1, adapter = __shfl_sync(0xFFFFFFFFu, a, first);
@@ -467,21 +486,33 @@ adapters_down_kernel(const Products p, int n_tiles) {
 #pragma unroll
                 for (int c = 0; c < 4; ++c) sh.red[warp][b][nt][c][lane] = acc[b][nt][c];
         __syncthreads();
-        // two neighbouring ranks of a row
         for (int idx = threadIdx.x; idx < NB * NT * 64; idx += 32 * DN_WARPS) {
             const int b = idx / (NT * 64), nt = (idx >> 6) % NT, h = (idx >> 5) & 1, ln = idx & 31;
             float v0 = 0.f, v1 = 0.f;
 #pragma unroll
             for (int w = 0; w < DN_WARPS; ++w) { v0 += sh.red[w][b][nt][2 * h][ln]; v1 += sh.red[w][b][nt][2 * h + 1][ln]; }
-            const int row = 16 * b + (ln >> 2) + 8 * h, col = nt * 8 + (ln & 3) * 2;
-            if (((mask >> row) & 1u) && col < r) {
-                const size_t at = ((size_t)(m0 + row) * r + col) / 2;
-                if (p.P != nullptr) reinterpret_cast<float2*>(p.P)[at] = make_float2(v0, v1);
-                if (p.split != nullptr) {
-                    const Split v = split_bf16(s * v0, s * v1);
-                    p.split[at] = make_uint2(v.hi, v.lo);
-                }
+            if constexpr (CTAS > 1) {
+                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(map_to_cta(parts + 8 * (cta * NB * NT * 64 + idx), 0)), "f"(v0), "f"(v1) : "memory");
+                continue;
             }
+            take(idx, mask, s, v0, v1);
+        }
+        if constexpr (CTAS > 1) {
+            __syncwarp();
+            cluster_sync_all();
+            if (cta == 0)
+                for (int idx = threadIdx.x; idx < NB * NT * 64; idx += 32 * DN_WARPS) {
+                    float2 v = make_float2(0.f, 0.f);
+#pragma unroll
+                    for (int i = 0; i < CTAS; ++i) {
+                        const float2 x = *reinterpret_cast<const float2*>(smem + Tile::OWN + 8 * (i * NB * NT * 64 + idx));
+                        v.x += x.x;
+                        v.y += x.y;
+                    }
+                    take(idx, mask, s, v.x, v.y);
+                }
+            __syncwarp();
+            cluster_sync_all();                                        // (the next entry's sums go where these were)
         }
         __syncthreads();
     }
@@ -672,15 +703,17 @@ adapters_up_kernel(const Products p, int tiles_each) {
 }
 
 // --------------------------------------------------------------------------------------------------------------- grads
-// A task is one adapter, a slice of columns of X or of dY (128 up to 16 ranks, else 64) and 16 MT ranks, or -- where there are few of those -- one part of
-// `parts`: every parts-th tile of the adapter.  Adapters differ in their tokens, so blocks claim tasks one by one.  A block finds the tiles of sixteen
-// tokens that hold any of its adapter's, window by window; its warps take them in turn, each through a ring of its own in shared memory, rows of other
-// adapters as zeros, and their sums are added in the order of the warps.  The block that finishes a slice's last part adds the parts in their order.
+// First the tiles of sixteen tokens are listed with the adapters in them (an entry: adapter, tile, mask of its tokens), in the order of the tokens, and every
+// adapter's entries are cut into chunks of equal length: adapters differ in their tokens, and the one with the most would be what all wait for.  A task is
+// a chunk, a slice of columns of X or of dY (128 up to 16 ranks, else 64) and 16 MT ranks; blocks claim tasks one by one, slices first, so that those under
+// way at a time read whole rows.  A block picks its chunk's entries out of the list; its warps take them in turn, each through a ring of its own in shared
+// memory, rows of other adapters as zeros, and their sums are added in the order of the warps.  The block that finishes an adapter's last chunk of a
+// slice adds the chunks in their order.
 //
 // Both operands are transposed on the way out of shared memory.  G and H are taken as two bf16 each (made once, not by every slice), one product after the
 // other into the same sums.  Where a sum is not finite the low parts have nothing to say, but may have made a NaN of an infinity: the task is
 // then done again without them.
-constexpr int GR_WARPS = 4, GR_WINDOW = GR_WARPS * 512, GR_STAGES = 3, GR_BLOCKS = 3;
+constexpr int GR_WARPS = 4, GR_STAGES = 3, GR_BLOCKS = 3, GR_MIN_TILES = 32;
 
 struct Grads {
     int M, K, N, r, n_adapters;
@@ -690,47 +723,128 @@ struct Grads {
     const bf16 *G, *H;                       // [2][M, r]: high parts, low parts
     float *dA, *dB;
     int accumulate;
-    int slices_x, slices, rank_blocks, parts;
-    unsigned* counters;                      // [0] claimed; with parts: [1 + task / parts] parts done
-    float* partial;                          // [task][16 MT][columns]
+    int slices_x, slices, rank_blocks;
+    int most_chunks;                         // chunks of adapters that have more than one: at most twice as many
+    unsigned* counters;                      // [0] claimed, [1] entries, [2] tiles of a chunk, [3] chunks; [4 ..] chunks done, by first chunk of an adapter of several and slice
+    uint2* entries;                          // [M]: adapter, tile << 16 | mask (tile < 65536: up to 2^20 tokens)
+    int* counts;                             // [n_adapters]: entries
+    int4* chunks;                            // [n_adapters + 2 most_chunks]: adapter, part, parts, place of the adapter's first part among those of several
+    float* partial;                          // [2 most_chunks][slices * rank_blocks][16 MT][columns]
 };
 
-// G and H in two parts, and the counters set to zero.
-__global__ void __launch_bounds__(256)
-adapters_split_kernel(long long n, const float* __restrict__ G, const float* __restrict__ H, uint32_t* __restrict__ g, uint32_t* __restrict__ h, unsigned* counters,
-                      int n_counters) {
+// Block 0: entries and chunks, and the counters set to zero.  The others: G and H in two parts.
+constexpr int GP_THREADS = 1024, GP_ROUNDS = 8;
+__global__ void __launch_bounds__(GP_THREADS)
+adapters_grad_plan_kernel(const Grads p, const float* __restrict__ G, const float* __restrict__ H, uint32_t* __restrict__ g, uint32_t* __restrict__ h, int n_counters) {
+    __shared__ int counts[GP_ROUNDS * 32], parts_s[32], several_s[32], total_s;
     pdl_launch_dependents();
     pdl_wait();
-    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (blockIdx.x == 0)
-        for (int i = threadIdx.x; i < n_counters; i += 256) counters[i] = 0u;
-    if (2 * at >= n) return;
-    const float2 vg = __ldcg(reinterpret_cast<const float2*>(G) + at), vh = __ldcg(reinterpret_cast<const float2*>(H) + at);
-    const Split sg = split_bf16(vg.x, vg.y), sh = split_bf16(vh.x, vh.y);
-    g[at] = sg.hi;
-    g[n / 2 + at] = sg.lo;
-    h[at] = sh.hi;
-    h[n / 2 + at] = sh.lo;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (blockIdx.x > 0) {
+        const long long n = (long long)p.M * p.r, at = (long long)(blockIdx.x - 1) * GP_THREADS + threadIdx.x;
+        if (2 * at >= n) return;
+        const float2 vg = __ldcg(reinterpret_cast<const float2*>(G) + at), vh = __ldcg(reinterpret_cast<const float2*>(H) + at);
+        const Split sg = split_bf16(vg.x, vg.y), sh = split_bf16(vh.x, vh.y);
+        g[at] = sg.hi;
+        g[n / 2 + at] = sg.lo;
+        h[at] = sh.hi;
+        h[n / 2 + at] = sh.lo;
+        return;
+    }
+    for (int i = threadIdx.x; i < n_counters; i += GP_THREADS) p.counters[i] = 0u;
+    for (int i = threadIdx.x; i < p.n_adapters; i += GP_THREADS) p.counts[i] = 0;
+    __threadfence_block();
+    __syncthreads();
+    int n_entries = 0;
+    for (int w0 = 0; w0 < p.M; w0 += GP_ROUNDS * GP_THREADS) {
+        int a[GP_ROUNDS];
+        uint32_t mask[GP_ROUNDS];
+#pragma unroll
+        for (int k = 0; k < GP_ROUNDS; ++k) {
+            const int t = w0 + k * GP_THREADS + threadIdx.x;
+            a[k] = t < p.M ? __ldg(p.adapter_of + t) : -1;
+        }
+#pragma unroll
+        for (int k = 0; k < GP_ROUNDS; ++k) {
+            if (a[k] >= p.n_adapters) a[k] = -1;
+            const uint32_t same = __match_any_sync(0xFFFFFFFFu, a[k]) & (lane < 16 ? 0x0000FFFFu : 0xFFFF0000u);
+            mask[k] = a[k] >= 0 && (same & ((1u << lane) - 1u)) == 0 ? same : 0u;      // the first token of an entry
+            const int n = __popc(__ballot_sync(0xFFFFFFFFu, mask[k] != 0));
+            if (lane == 0) counts[k * 32 + warp] = n;
+        }
+        __syncthreads();
+        if (warp == 0) {                                               // counts -> places
+            int mine[GP_ROUNDS], sum = 0;
+#pragma unroll
+            for (int k = 0; k < GP_ROUNDS; ++k) { mine[k] = sum; sum += counts[lane * GP_ROUNDS + k]; }
+            int before = sum;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int x = __shfl_up_sync(0xFFFFFFFFu, before, o);
+                if (lane >= o) before += x;
+            }
+            if (lane == 31) total_s = before;
+#pragma unroll
+            for (int k = 0; k < GP_ROUNDS; ++k) counts[lane * GP_ROUNDS + k] = before - sum + mine[k];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < GP_ROUNDS; ++k) {
+            const uint32_t firsts = __ballot_sync(0xFFFFFFFFu, mask[k] != 0);
+            if (mask[k] != 0) {
+                const int t = w0 + k * GP_THREADS + warp * 32 + lane;
+                p.entries[n_entries + counts[k * 32 + warp] + __popc(firsts & ((1u << lane) - 1u))] =
+                    make_uint2((unsigned)a[k], (uint32_t)(t / 16) << 16 | (lane < 16 ? mask[k] : mask[k] >> 16));
+                atomicAdd(p.counts + a[k], 1);
+            }
+        }
+        n_entries += total_s;
+        __syncthreads();
+    }
+    const int tiles = max(GR_MIN_TILES, (n_entries + p.most_chunks - 1) / p.most_chunks);
+    int n_chunks = 0, n_several = 0;
+    for (int a0 = 0; a0 < p.n_adapters; a0 += GP_THREADS) {
+        const int a = a0 + threadIdx.x;
+        const int n = a < p.n_adapters ? max(1, (*(volatile int*)(p.counts + a) + tiles - 1) / tiles) : 0, several = n > 1 ? n : 0;   // (one without tokens has a chunk that writes its zeros)
+        int before = n, before_several = several;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xFFFFFFFFu, before, o), y = __shfl_up_sync(0xFFFFFFFFu, before_several, o);
+            if (lane >= o) { before += x; before_several += y; }
+        }
+        if (lane == 31) { parts_s[warp] = before; several_s[warp] = before_several; }
+        __syncthreads();
+        int at = n_chunks + before - n, at_several = n_several + before_several - several;
+        for (int w = 0; w < 32; ++w) {
+            if (w < warp) { at += parts_s[w]; at_several += several_s[w]; }
+            n_chunks += parts_s[w];
+            n_several += several_s[w];
+        }
+        for (int i = 0; i < n; ++i) p.chunks[at + i] = make_int4(a, i, n, at_several);
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) { p.counters[1] = (unsigned)n_entries; p.counters[2] = (unsigned)tiles; p.counters[3] = (unsigned)n_chunks; }
 }
 
 template <int MT>
 struct GradTile {
     static constexpr int COLS = MT == 1 ? 128 : 64, RANKS = 16 * MT, PITCH = COLS + 4;    // PITCH: of the sums in shared memory
     static constexpr int V_BYTES = 16 * COLS * 2, P_BYTES = 16 * RANKS * 2, STAGE = V_BYTES + 2 * P_BYTES;
-    static constexpr size_t RING = (size_t)GR_WARPS * GR_STAGES * STAGE, SUMS = sizeof(float) * GR_WARPS * RANKS * PITCH, LIST = sizeof(uint32_t) * GR_WINDOW / 16;
-    static constexpr size_t SMEM = (RING > SUMS ? RING : SUMS) + LIST;
+    static constexpr size_t RING = (size_t)GR_WARPS * GR_STAGES * STAGE, SUMS = sizeof(float) * GR_WARPS * RANKS * PITCH;
+    static constexpr size_t SMEM = RING > SUMS ? RING : SUMS;
 };
 
+constexpr int GR_LIST = 512, GR_READ = 2;                                  // entries of a chunk that are worked on at a time; entries that a thread reads at a time
+
 template <int MT>
-__device__ __forceinline__ void grad_task(const Grads& p, int task, uint8_t* smem, int* counts, int* is_last) {
+__device__ __forceinline__ void grad_task(const Grads& p, int task, int n_entries, int chunk_tiles, uint8_t* smem, uint32_t* list, int* counts, int* is_last) {
     using Tile = GradTile<MT>;
     constexpr int COLS = Tile::COLS, RANKS = Tile::RANKS, PITCH = Tile::PITCH, CT = COLS / 8;
     float* red = reinterpret_cast<float*>(smem);                       // [warps][RANKS][PITCH], where the rings were
-    uint32_t* list = reinterpret_cast<uint32_t*>(smem + Tile::SMEM - Tile::LIST);       // tile of the window << 16 | mask of its tokens
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3, row8 = lane & 7, quarter = lane >> 3;
-    // (adapters change fastest: the tasks of one with many tokens are spread over the blocks)
-    const int adapter = task % p.n_adapters, part = task / p.n_adapters % p.parts, block = task / p.n_adapters / p.parts;
-    const int slice = block / p.rank_blocks, j0 = block % p.rank_blocks * RANKS;
+    const int blocks = p.slices * p.rank_blocks, block = task % blocks, slice = block / p.rank_blocks, j0 = block % p.rank_blocks * RANKS;
+    const int4 chunk = __ldcg(p.chunks + task / blocks);
+    const int adapter = chunk.x, part = chunk.y, parts = chunk.z;
     const bool of_x = slice < p.slices_x;
     const int C = of_x ? p.K : p.N, c0 = (of_x ? slice : slice - p.slices_x) * COLS, M = p.M, r = p.r;
     const bf16 *V = of_x ? p.X : p.dY, *P = of_x ? p.G : p.H;
@@ -741,6 +855,7 @@ __device__ __forceinline__ void grad_task(const Grads& p, int task, uint8_t* sme
     const bool v_in = c0 + 8 * v_piece < C;
     const int p_row = lane / P_PIECES % 16, p_piece = lane % P_PIECES;
     const bool p_in = j0 + 8 * p_piece < r;
+    const int lo = part * chunk_tiles, hi = lo + chunk_tiles;          // of the adapter's entries
     float acc[MT][CT][4];
     bool any = false;
     for (int low_parts = 1; low_parts >= 0; --low_parts) {
@@ -748,32 +863,43 @@ __device__ __forceinline__ void grad_task(const Grads& p, int task, uint8_t* sme
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
             for (int t = 0; t < CT; ++t) acc[mt][t][0] = acc[mt][t][1] = acc[mt][t][2] = acc[mt][t][3] = 0.f;
-        for (int w0 = 0; w0 < M; w0 += GR_WINDOW) {
-            // this warp looks at 512 places: lane i has tile i
-            const int from = w0 + warp * 512;
-            uint32_t mask = 0;
+        int seen = 0;                                                  // of the adapter's entries
+        for (int e0 = 0; e0 < n_entries && seen < hi;) {
+            // the chunk's entries from e0 on, until the list is full
+            int total = 0;
+            for (; e0 < n_entries && seen < hi && total <= GR_LIST - GR_READ * 32 * GR_WARPS;) {
+                uint2 e[GR_READ];
+                uint32_t votes[GR_READ];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int t = from + 32 * i + lane;
-                const uint32_t found = __ballot_sync(0xFFFFFFFFu, t < M && __ldg(p.adapter_of + t) == adapter);
-                if (lane >> 1 == i) mask = lane & 1 ? found >> 16 : found & 0xFFFFu;
-            }
-            const uint32_t tiles = __ballot_sync(0xFFFFFFFFu, mask != 0);
-            if (lane == 0) counts[warp] = __popc(tiles);
-            __syncthreads();
-            int at = 0, total = 0;
+                for (int k = 0; k < GR_READ; ++k) {
+                    const int i = e0 + (k * GR_WARPS + warp) * 32 + lane;
+                    e[k] = i < n_entries ? __ldcg(p.entries + i) : make_uint2(0xFFFFFFFFu, 0u);
+                }
 #pragma unroll
-            for (int w = 0; w < GR_WARPS; ++w) {
-                if (w == warp) at = total;
-                total += counts[w];
+                for (int k = 0; k < GR_READ; ++k) {
+                    votes[k] = __ballot_sync(0xFFFFFFFFu, e[k].x == (unsigned)adapter);
+                    if (lane == 0) counts[k * GR_WARPS + warp] = __popc(votes[k]);
+                }
+                __syncthreads();
+                int all = 0;
+#pragma unroll
+                for (int k = 0; k < GR_READ; ++k)
+#pragma unroll
+                    for (int w = 0; w < GR_WARPS; ++w) {
+                        const int ordinal = seen + all + __popc(votes[k] & ((1u << lane) - 1u));
+                        if (w == warp && ((votes[k] >> lane) & 1u) && ordinal >= lo && ordinal < hi) list[total + ordinal - max(lo, seen)] = e[k].y;
+                        all += counts[k * GR_WARPS + w];
+                    }
+                total += max(0, min(hi, seen + all) - max(lo, seen));
+                seen += all;
+                e0 += GR_READ * GR_WARPS * 32;
+                __syncthreads();
             }
-            if (mask != 0) list[at + __popc(tiles & ((1u << lane) - 1u))] = (uint32_t)(warp * 32 + lane) << 16 | mask;
-            __syncthreads();
             any |= total > 0;
-            const int first = warp * p.parts + part, step = GR_WARPS * p.parts, mine = first < total ? (total - first + step - 1) / step : 0;
+            const int mine = warp < total ? (total - warp + GR_WARPS - 1) / GR_WARPS : 0;
             auto load = [&](int i) {
-                const uint32_t to = ring + (i % GR_STAGES) * Tile::STAGE, entry = list[first + i * step];
-                const int t0 = w0 + (int)(entry >> 16) * 16;
+                const uint32_t to = ring + (i % GR_STAGES) * Tile::STAGE, entry = list[warp + i * GR_WARPS];
+                const int t0 = (int)(entry >> 16) * 16;
                 const bf16* v = V + (size_t)(t0 + v_row) * C + (v_in ? c0 + 8 * v_piece : 0);
 #pragma unroll
                 for (int n = 0; n < 16 / PER; ++n) {
@@ -848,7 +974,7 @@ __device__ __forceinline__ void grad_task(const Grads& p, int task, uint8_t* sme
                 for (int k = 0; k < 4; ++k) worst += acc[mt][t][k] - acc[mt][t][k];
         if (!__syncthreads_or(worst != 0.f)) break;
     }
-    if (!any && p.accumulate) return;                                  // (the same for the whole block, and for all parts)
+    if (!any && p.accumulate) return;                                  // (the same for the whole block; an adapter without tokens has one chunk)
     // [mt][t][c]: rank 16 mt + g (+ 8 where c >= 2), column 8 t + 2 q + c % 2
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
@@ -859,44 +985,70 @@ __device__ __forceinline__ void grad_task(const Grads& p, int task, uint8_t* sme
                 *reinterpret_cast<float2*>(red + ((size_t)warp * RANKS + 16 * mt + 8 * h + g) * PITCH + 8 * t + 2 * q) =
                     make_float2(acc[mt][t][2 * h], acc[mt][t][2 * h + 1]);
     __syncthreads();
-    const bool split = p.parts > 1 && any;
-    const size_t whole = (size_t)block * p.n_adapters + adapter;
-    float* partial = p.partial + whole * p.parts * (RANKS * COLS);
-    auto sum = [&](int j, int c) {
-        float v = 0.f;
+    // From here on four values at a time, in the order of the output: A's gradient along the columns, B's along the ranks.
+    constexpr int QUADS = RANKS * COLS / 4;
+    auto place = [&](int quad, int& j, int& c) {
+        if (of_x) { j = quad / (COLS / 4); c = 4 * (quad % (COLS / 4)); }
+        else { c = quad / (RANKS / 4); j = 4 * (quad % (RANKS / 4)); }
+    };
+    auto sum = [&](int quad) {
+        int j, c;
+        place(quad, j, c);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int w = 0; w < GR_WARPS; ++w) v += red[(w * RANKS + j) * PITCH + c];
+        for (int w = 0; w < GR_WARPS; ++w) {
+            const float* from = red + (w * RANKS + j) * PITCH + c;
+            if (of_x) {
+                const float4 x = *reinterpret_cast<const float4*>(from);
+                v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+            } else {
+                v.x += from[0]; v.y += from[PITCH]; v.z += from[2 * PITCH]; v.w += from[3 * PITCH];
+            }
+        }
         return v;
     };
+    const bool split = parts > 1;
+    const size_t apart = (size_t)blocks * QUADS;                       // from one chunk's sums to the next one's
+    float4* partial = reinterpret_cast<float4*>(p.partial) + (size_t)chunk.w * apart + (size_t)block * QUADS;
     if (split) {
-        for (int idx = threadIdx.x; idx < RANKS * COLS; idx += 32 * GR_WARPS) __stcg(partial + (size_t)part * RANKS * COLS + idx, sum(idx / COLS, idx % COLS));
+        for (int quad = threadIdx.x; quad < QUADS; quad += 32 * GR_WARPS) __stcg(partial + part * apart + quad, sum(quad));
         __threadfence();
         __syncthreads();
         if (threadIdx.x == 0) {
-            *is_last = atomicAdd(p.counters + 1 + whole, 1u) == (unsigned)p.parts - 1u;
+            *is_last = atomicAdd(p.counters + 4 + (size_t)chunk.w * blocks + block, 1u) == (unsigned)parts - 1u;
             __threadfence();
         }
         __syncthreads();
         if (!*is_last) return;
-    } else if (part > 0) {
-        return;                                                        // an adapter without tokens: its zeros are written once
     }
     const float s = p.scales[adapter];
-    const int ranks = min(RANKS, r - j0);
+    constexpr int EACH = QUADS / (32 * GR_WARPS);
+    float4 v[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int quad = threadIdx.x + i * 32 * GR_WARPS;
+        v[i] = split ? __ldcg(partial + quad) : sum(quad);
+    }
+    if (split)
 #pragma unroll 4
-    for (int idx = threadIdx.x; idx < RANKS * COLS; idx += 32 * GR_WARPS) {
-        // in the order of the output: A's gradient along the columns, B's along the ranks
-        const int j = of_x ? idx / COLS : idx % RANKS, c = of_x ? idx % COLS : idx / RANKS;
-        if (j >= ranks || c0 + c >= C) continue;
-        float v = 0.f;
-        if (split) {
-            for (int k = 0; k < p.parts; ++k) v += __ldcg(partial + ((size_t)k * RANKS + j) * COLS + c);
-        } else {
-            v = sum(j, c);
+        for (int k = 1; k < parts; ++k)
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                const float4 x = __ldcg(partial + k * apart + threadIdx.x + i * 32 * GR_WARPS);
+                v[i].x += x.x; v[i].y += x.y; v[i].z += x.z; v[i].w += x.w;
+            }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        int j, c;
+        place(threadIdx.x + i * 32 * GR_WARPS, j, c);
+        if (j0 + j >= r || c0 + c >= C) continue;                      // (four are inside or outside together)
+        float4* dst = reinterpret_cast<float4*>(of_x ? p.dA + ((size_t)adapter * r + j0 + j) * p.K + c0 + c : p.dB + ((size_t)adapter * p.N + c0 + c) * r + j0 + j);
+        float4 x = any ? make_float4(s * v[i].x, s * v[i].y, s * v[i].z, s * v[i].w) : make_float4(0.f, 0.f, 0.f, 0.f);
+        if (p.accumulate) {
+            const float4 old = *dst;
+            x.x += old.x; x.y += old.y; x.z += old.z; x.w += old.w;
         }
-        float* dst = of_x ? p.dA + ((size_t)adapter * r + j0 + j) * p.K + c0 + c : p.dB + ((size_t)adapter * p.N + c0 + c) * r + j0 + j;
-        v = any ? s * v : 0.f;
-        *dst = p.accumulate ? *dst + v : v;
+        *dst = x;
     }
 }
 
@@ -904,74 +1056,94 @@ template <int MT>
 __global__ void __launch_bounds__(32 * GR_WARPS, GR_BLOCKS)
 adapters_grad_kernel(const Grads p) {
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ int counts[GR_WARPS], claimed, is_last;
+    __shared__ uint32_t list[GR_LIST];
+    __shared__ int counts[GR_READ * GR_WARPS], claimed, is_last;
     pdl_launch_dependents();
     pdl_wait();
-    const int n_tasks = p.slices * p.rank_blocks * p.n_adapters * p.parts;
-    for (;;) {
-        __syncthreads();                                               // shared memory is written again
-        if (threadIdx.x == 0) claimed = (int)atomicAdd(p.counters, 1u);
+    const int n_entries = (int)__ldcg(p.counters + 1), chunk_tiles = (int)__ldcg(p.counters + 2);
+    const int n_tasks = p.slices * p.rank_blocks * (int)__ldcg(p.counters + 3);
+    // the first task is the block's own number; the next is claimed while one is worked on
+    for (int task = blockIdx.x; task < n_tasks;) {
+        if (threadIdx.x == 0) claimed = (int)(gridDim.x + atomicAdd(p.counters, 1u));
+        grad_task<MT>(p, task, n_entries, chunk_tiles, smem, list, counts, &is_last);
         __syncthreads();
-        const int task = claimed;
-        if (task >= n_tasks) break;
-        grad_task<MT>(p, task, smem, counts, &is_last);
+        task = claimed;
+        __syncthreads();                                               // shared memory is written again
     }
 }
 
-template <bool L_IS_A, int NT, int NB>
+template <bool L_IS_A, int NT, int NB, int CTAS>
 int down_impl(const Products& p, cudaStream_t st) {
-    constexpr size_t smem = DownTile<L_IS_A, NT, NB>::SMEM;
+    constexpr size_t smem = DownTile<L_IS_A, NT, NB, CTAS>::SMEM;
     static SmemLimit limit;
-    auto kern = adapters_down_kernel<L_IS_A, NT, NB>;
+    auto kern = adapters_down_kernel<L_IS_A, NT, NB, CTAS>;
     if (!limit.raise(kern, smem)) return QLORA_ERR_CUDA;
     const int tiles = (p.M + 16 * NB - 1) / (16 * NB);
-    return launch_pdl(kern, dim3(tiles + sm_count()), dim3(32 * DN_WARPS), smem, st, 1, p, tiles) == cudaSuccess ? QLORA_OK : QLORA_ERR_CUDA;
+    return launch_pdl(kern, dim3((tiles + sm_count() / CTAS) * CTAS), dim3(32 * DN_WARPS), smem, st, CTAS, p, tiles) == cudaSuccess ? QLORA_OK : QLORA_ERR_CUDA;
 }
 
 template <bool FROM_B, int KS, int UB>
 int up_impl(const Products& p, cudaStream_t st) {
     const int columns = (p.C + 32 * UB * UP_WARPS - 1) / (32 * UB * UP_WARPS), tiles = (p.M + UP_ROWS - 1) / UP_ROWS;
-    // as many tiles to a block as leave every SM its two blocks twice
-    int each = (int)((long long)tiles * columns / (4 * sm_count()));
-    each = each < 1 ? 1 : each > 16 ? 16 : each;
+    // Tiles to a block: two blocks run on an SM, so it is waves of blocks times the tiles of one, and about two tiles' time for a block to begin.
+    const long long room = 2 * sm_count();
+    int each = 1;
+    for (long long i = 1, best = 1ll << 60; i <= 64; ++i) {
+        const long long blocks = (tiles + i - 1) / i * columns, cost = (blocks + room - 1) / room * (i + 2);
+        if (cost < best) { best = cost; each = (int)i; }
+    }
     return launch_pdl(adapters_up_kernel<FROM_B, KS, UB>, dim3((tiles + each - 1) / each, columns), dim3(32 * UP_WARPS), 0, st, 1, p, each) == cudaSuccess
                ? QLORA_OK : QLORA_ERR_CUDA;
 }
 
-template <bool FORWARD, int NT, int ROWS>
+template <bool FORWARD, int NT, int ROWS, int CTAS>
 int few_impl(const Products& p, cudaStream_t st) {
-    return launch_pdl(adapters_few_kernel<FORWARD, NT, ROWS>, dim3((p.M + ROWS - 1) / ROWS * FEW_CTAS), dim3(32 * FEW_WARPS), 0, st, 1, p) == cudaSuccess
+    return launch_pdl(adapters_few_kernel<FORWARD, NT, ROWS, CTAS>, dim3((p.M + ROWS - 1) / ROWS * CTAS), dim3(32 * FEW_WARPS), 0, st, 1, p) == cudaSuccess
                ? QLORA_OK : QLORA_ERR_CUDA;   // (the cluster's width is an attribute of the kernel)
 }
 
 template <bool FORWARD, int NT, int NB, int KS, int UB>
 int products(const Products& p, cudaStream_t st) {
-    if (p.Out != nullptr && p.M <= FEW_TOKENS) return p.M <= 64 ? few_impl<FORWARD, NT, 1>(p, st) : few_impl<FORWARD, NT, 4>(p, st);
-    const int rc = down_impl<FORWARD, NT, NB>(p, st);
+    if (p.Out != nullptr && p.M <= FEW_TOKENS) {
+        // a cluster for every token, as wide as lets all of them run at a time (two blocks to an SM), then for every four
+        const int room = 2 * sm_count();
+        if (8 * p.M <= room) return few_impl<FORWARD, NT, 1, 8>(p, st);
+        if (4 * p.M <= room) return few_impl<FORWARD, NT, 1, 4>(p, st);
+        if (2 * p.M <= room) return few_impl<FORWARD, NT, 1, 2>(p, st);
+        return few_impl<FORWARD, NT, 4, 4>(p, st);
+    }
+    // blocks to a tile: while all of them run at a time
+    const int tiles = (p.M + 16 * NB - 1) / (16 * NB), room = (NT <= 2 ? 2 : 1) * sm_count();
+    const int rc = 4 * tiles <= room ? down_impl<FORWARD, NT, NB, 4>(p, st) : 2 * tiles <= room ? down_impl<FORWARD, NT, NB, 2>(p, st) : down_impl<FORWARD, NT, NB, 1>(p, st);
     return rc != QLORA_OK || p.Out == nullptr ? rc : up_impl<FORWARD, KS, UB>(p, st);
 }
 
-// How the gradients are cut into tasks: into parts where the slices are too few for every SM to have all its blocks.
+// Slices and chunks of the gradients: as many chunks as give every SM all its blocks twice, sixteen at least.
 void cut_grads(Grads& p) {
     const int columns = p.r <= 16 ? GradTile<1>::COLS : GradTile<2>::COLS, ranks = p.r <= 16 ? GradTile<1>::RANKS : GradTile<2>::RANKS;
     p.slices_x = (p.K + columns - 1) / columns;
     p.slices = p.slices_x + (p.N + columns - 1) / columns;
     p.rank_blocks = (p.r + ranks - 1) / ranks;
-    const long long whole = (long long)p.slices * p.rank_blocks * p.n_adapters, wanted = GR_BLOCKS * sm_count();
-    p.parts = whole >= wanted || whole == 0 ? 1 : (int)(wanted / whole < 8 ? (wanted + whole - 1) / whole : 8);
+    const int blocks = p.slices * p.rank_blocks, wanted = 2 * GR_BLOCKS * sm_count();
+    p.most_chunks = blocks == 0 ? 16 : (wanted + blocks - 1) / blocks;
+    p.most_chunks = p.most_chunks < 16 ? 16 : p.most_chunks > 128 ? 128 : p.most_chunks;
 }
 
-struct GradScratch { size_t g, h, counters, partial, total; };
+struct GradScratch { size_t g, h, counters, entries, counts, chunks, partial, total; };
 GradScratch grad_scratch(const Grads& p) {
-    auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-    const size_t whole = (size_t)p.slices * p.rank_blocks * p.n_adapters, ranks = p.r <= 16 ? GradTile<1>::RANKS : GradTile<2>::RANKS,
-                 columns = p.r <= 16 ? GradTile<1>::COLS : GradTile<2>::COLS;
+    const size_t blocks = (size_t)p.slices * p.rank_blocks, several = 2 * (size_t)p.most_chunks;
+    const size_t tile = p.r <= 16 ? GradTile<1>::RANKS * GradTile<1>::COLS : GradTile<2>::RANKS * GradTile<2>::COLS;
     GradScratch s;
-    s.g = 0;
-    s.h = up((size_t)p.M * p.r * 4);
-    s.counters = s.h + up((size_t)p.M * p.r * 4);
-    s.partial = s.counters + up(4 * (p.parts > 1 ? 1 + whole : 1));
-    s.total = s.partial + (p.parts > 1 ? whole * p.parts * ranks * columns * sizeof(float) : 0);
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
+    s.g = take((size_t)p.M * p.r * 4);
+    s.h = take((size_t)p.M * p.r * 4);
+    s.counters = take(4 * (4 + several * blocks));
+    s.entries = take((size_t)p.M * sizeof(uint2));
+    s.counts = take((size_t)p.n_adapters * 4);
+    s.chunks = take(((size_t)p.n_adapters + several) * sizeof(int4));
+    s.partial = take(several * blocks * tile * sizeof(float));
+    s.total = at;
     return s;
 }
 
@@ -980,9 +1152,7 @@ int grad_impl(const Grads& p, cudaStream_t st) {
     static SmemLimit limit;
     auto kern = adapters_grad_kernel<MT>;
     if (!limit.raise(kern, GradTile<MT>::SMEM)) return QLORA_ERR_CUDA;
-    const long long tasks = (long long)p.slices * p.rank_blocks * p.n_adapters * p.parts, blocks = (long long)GR_BLOCKS * sm_count();
-    return launch_pdl(kern, dim3((unsigned)(tasks < blocks ? tasks : blocks)), dim3(32 * GR_WARPS), GradTile<MT>::SMEM, st, 1, p) == cudaSuccess ? QLORA_OK
-                                                                                                                                                    : QLORA_ERR_CUDA;
+    return launch_pdl(kern, dim3(GR_BLOCKS * sm_count()), dim3(32 * GR_WARPS), GradTile<MT>::SMEM, st, 1, p) == cudaSuccess ? QLORA_OK : QLORA_ERR_CUDA;
 }
 
 }  // namespace
@@ -1016,10 +1186,13 @@ int launch_adapters_grads(int M, int K, int N, int r, int n_adapters, const void
     p.G = reinterpret_cast<bf16*>(at + s.g);
     p.H = reinterpret_cast<bf16*>(at + s.h);
     p.counters = reinterpret_cast<unsigned*>(at + s.counters);
+    p.entries = reinterpret_cast<uint2*>(at + s.entries);
+    p.counts = reinterpret_cast<int*>(at + s.counts);
+    p.chunks = reinterpret_cast<int4*>(at + s.chunks);
     p.partial = reinterpret_cast<float*>(at + s.partial);
-    const long long n = (long long)M * r;
-    if (launch_pdl(adapters_split_kernel, dim3((unsigned)(n == 0 ? 1 : (n / 2 + 255) / 256)), dim3(256), 0, st, 1, n, G, H, reinterpret_cast<uint32_t*>(at + s.g),
-                   reinterpret_cast<uint32_t*>(at + s.h), p.counters, (int)((s.partial - s.counters) / 4)) != cudaSuccess)
+    const long long pairs = (long long)M * r / 2;
+    if (launch_pdl(adapters_grad_plan_kernel, dim3((unsigned)(1 + (pairs + GP_THREADS - 1) / GP_THREADS)), dim3(GP_THREADS), 0, st, 1, p, G, H,
+                   reinterpret_cast<uint32_t*>(at + s.g), reinterpret_cast<uint32_t*>(at + s.h), (int)((s.entries - s.counters) / 4)) != cudaSuccess)
         return QLORA_ERR_CUDA;
     return r <= 16 ? grad_impl<1>(p, st) : grad_impl<2>(p, st);
 }

@@ -86,10 +86,11 @@ int check_adamw(const qlora_adamw_desc* d, bool step) {
     return QLORA_OK;
 }
 
-int check_adapters(const qlora_adapters_desc* d) {
+int check_adapters(const qlora_adapters_desc* d, int M) {
     if (d == nullptr || d->K < 0 || d->N < 0 || d->r < 0 || d->n_adapters < 0) return QLORA_ERR_INVALID_ARG;
     if (d->K % 32 != 0 || d->N % 8 != 0 || d->r % 8 != 0 || d->r == 0 || d->r > 64 || d->n_adapters > 65535) return QLORA_ERR_UNSUPPORTED;
-    return QLORA_OK;
+    if (M < 0) return QLORA_ERR_INVALID_ARG;
+    return M > (1 << 20) ? QLORA_ERR_UNSUPPORTED : QLORA_OK;
 }
 // Workspace of the calls on adapters: two [M, r] products, then the scratch of the gradients.
 size_t adapters_low_bytes(const qlora_adapters_desc& d, int M) { return align_up((size_t)M * (size_t)d.r * sizeof(float), 256); }
@@ -248,8 +249,8 @@ int qlora_adamw(const qlora_adamw_desc* desc, double lr, int step, const float* 
 }
 
 int qlora_adapters_workspace_bytes(const qlora_adapters_desc* desc, int M, size_t* out) {
-    if (out == nullptr || M < 0) return QLORA_ERR_INVALID_ARG;
-    const int rc = check_adapters(desc);
+    if (out == nullptr) return QLORA_ERR_INVALID_ARG;
+    const int rc = check_adapters(desc, M);
     if (rc != QLORA_OK) return rc;
     *out = adapters_bytes(*desc, M);
     return QLORA_OK;
@@ -258,9 +259,8 @@ int qlora_adapters_workspace_bytes(const qlora_adapters_desc* desc, int M, size_
 // Forward: In = X [M, K], Base and Out [M, N].  Backward: In = dY [M, N], Base and Out [M, K].
 static int adapters_common(bool forward, const qlora_adapters_desc* desc, int M, const void* In, const int32_t* adapter_of, const void* A, const void* B,
                            const float* scales, const void* Base, void* Out, float* low, void* workspace, size_t workspace_bytes, void* cuda_stream) {
-    const int rc = check_adapters(desc);
+    const int rc = check_adapters(desc, M);
     if (rc != QLORA_OK) return rc;
-    if (M < 0) return QLORA_ERR_INVALID_ARG;
     const qlora_adapters_desc& d = *desc;
     const int T = forward ? d.K : d.N, C = forward ? d.N : d.K;
     if (M == 0 || C == 0) return QLORA_OK;
@@ -269,7 +269,7 @@ static int adapters_common(bool forward, const qlora_adapters_desc* desc, int M,
     if (!aligned16(In) || !aligned4(adapter_of) || !aligned16(A) || !aligned16(B) || !aligned4(scales) || !aligned16(Base) || !aligned16(Out) ||
         !aligned16(low) || !aligned16(workspace))
         return QLORA_ERR_ALIGNMENT;
-    if (workspace == nullptr || workspace_bytes < adapters_bytes(d, M)) return QLORA_ERR_WORKSPACE;
+    if (workspace == nullptr || workspace_bytes < adapters_low_bytes(d, M)) return QLORA_ERR_WORKSPACE;
     return launch_adapters(forward, M, T, C, d.r, d.n_adapters, In, adapter_of, forward ? A : B, forward ? B : A, scales, Base, Out, low, workspace,
                            (cudaStream_t)cuda_stream);
 }
@@ -287,9 +287,9 @@ int qlora_adapters_bwd_input(const qlora_adapters_desc* desc, int M, const void*
 int qlora_adapters_bwd_lora(const qlora_adapters_desc* desc, int M, const void* X, const void* dY, const int32_t* adapter_of, const void* A, const void* B,
                             const float* scales, const float* H, const float* G, float* dA, float* dB, int accumulate, void* workspace,
                             size_t workspace_bytes, void* cuda_stream) {
-    int rc = check_adapters(desc);
+    int rc = check_adapters(desc, M);
     if (rc != QLORA_OK) return rc;
-    if (M < 0 || (accumulate != 0 && accumulate != 1)) return QLORA_ERR_INVALID_ARG;
+    if (accumulate != 0 && accumulate != 1) return QLORA_ERR_INVALID_ARG;
     const qlora_adapters_desc& d = *desc;
     if (d.n_adapters == 0 || (d.K == 0 && d.N == 0)) return QLORA_OK;
     if ((!dA && d.K > 0) || (!dB && d.N > 0) || !scales) return QLORA_ERR_INVALID_ARG;
