@@ -198,8 +198,8 @@ typedef struct {
     int n_adapters; /* at most 65535 */
 } qlora_adapters_desc;
 
-/* Bytes of scratch for M tokens (2^20 at most), for all three calls.  The first two need 4 M r of them, rounded up to 256; the gradients up to 32 sums of
- * every 2048 elements of an adapter's gradients. */
+/* Bytes of scratch for M tokens (2^20 at most), for all three calls.  The first two need 4 M r + M / 4 + 8 of them; the gradients
+ * take most: up to 32 sums of every 2048 elements of an adapter's gradients. */
 int qlora_adapters_workspace_bytes(const qlora_adapters_desc* desc, int M, size_t* out);
 
 /* X bf16 [M, K]; adapter_of int32 [M]; A bf16 [n_adapters, r, K]; B bf16 [n_adapters, N, r]; scales fp32 [n_adapters] (alpha / r of

@@ -92,10 +92,11 @@ struct Products {                            // the operands of both products
     bf16* Out;
     float* P;                                // [M, r] or NULL
     uint2* split;                            // [M, r / 2]: pairs of s P as two bf16 pairs, for the second product of many tokens; or NULL
+    int* left;                               // with split: [0] how many tiles of 16 tokens hold more than DN_ENTRIES adapters, [1 ..] which
 };
 
-// Called by all threads of all CTAs of the cluster, with the same m0, after the cluster's CTAs have begun.
-template <bool FORWARD, int NT, int ROWS, int CTAS>
+// Called by all threads of all CTAs of the cluster, with the same m0, after the cluster's CTAs have begun.  Without BOTH: the first product alone.
+template <bool FORWARD, int NT, int ROWS, int CTAS, bool BOTH>
 __device__ __forceinline__ void few_tokens(const Products& p, int m0, FewShared<NT, ROWS, CTAS>& sh) {
     constexpr int UNROLL = NT <= 2 ? 4 : NT <= 4 ? 2 : 1, THREADS = 32 * FEW_WARPS;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
@@ -110,17 +111,18 @@ __device__ __forceinline__ void few_tokens(const Products& p, int m0, FewShared<
         if (lane == 0) sh.n_entries = __popc(firsts);
     }
     __syncthreads();
-    const int n_entries = sh.n_entries, pairs = p.Out != nullptr ? C / 2 : 0;
+    const int n_entries = sh.n_entries, pairs = BOTH ? C / 2 : 0;
     const int p_lo = (int)((long long)pairs * cta / CTAS), p_hi = (int)((long long)pairs * (cta + 1) / CTAS);
-    for (int e = 0; e < n_entries; ++e) {
-        const bf16* La = p.L2 + (size_t)sh.entry_adapter[e] * r * C;
-        if constexpr (FORWARD) {                                       // B: the columns' rows lie together
-            for (int i = p_lo * 2 * r + 64 * threadIdx.x; i < p_hi * 2 * r; i += 64 * THREADS) prefetch_l2(La + i);
-        } else {
-            const int lines = (p_hi - p_lo + 31) / 32;
-            for (int i = threadIdx.x; i < lines * r; i += THREADS) prefetch_l2(La + (size_t)(i / lines) * C + 2 * p_lo + 64 * (i % lines));
+    if constexpr (BOTH)
+        for (int e = 0; e < n_entries; ++e) {
+            const bf16* La = p.L2 + (size_t)sh.entry_adapter[e] * r * C;
+            if constexpr (FORWARD) {                                   // B: the columns' rows lie together
+                for (int i = p_lo * 2 * r + 64 * threadIdx.x; i < p_hi * 2 * r; i += 64 * THREADS) prefetch_l2(La + i);
+            } else {
+                const int lines = (p_hi - p_lo + 31) / 32;
+                for (int i = threadIdx.x; i < lines * r; i += THREADS) prefetch_l2(La + (size_t)(i / lines) * C + 2 * p_lo + 64 * (i % lines));
+            }
         }
-    }
     // ---- the first product: warps share the entries and their parts of the contraction.  (A row of the result depends on its own row of In alone, so
     // rows of other entries need no mask: they are not taken.)
     const int per_entry = n_entries <= 1 ? 8 : n_entries == 2 ? 4 : 2, my_entry = warp / per_entry, sub = warp % per_entry;
@@ -193,62 +195,98 @@ __device__ __forceinline__ void few_tokens(const Products& p, int m0, FewShared<
 #pragma unroll
         for (int i = 0; i < CTAS; ++i) v += sh.parts[i][row][j];
         if (p.P != nullptr && cta == 0 && row < rows && j < r) p.P[(size_t)(m0 + row) * r + j] = v;
-        sh.low[row][j] = e >= 0 && p.Out != nullptr ? p.scales[sh.entry_adapter[e]] * v : 0.f;
+        sh.low[row][j] = e >= 0 && p.scales != nullptr ? p.scales[sh.entry_adapter[e]] * v : 0.f;
     }
     __syncthreads();
-    if (p.Out == nullptr) return;
-    // ---- the second product: a thread has two neighbouring columns of one entry, BATCH such units at a time
-    constexpr int BATCH = NT <= 2 ? 4 : NT <= 4 ? 2 : 1;
-    const int n_pairs = p_hi - p_lo, units = n_entries * n_pairs;
-    for (int unit0 = threadIdx.x; unit0 < units; unit0 += THREADS * BATCH) {
-        uint32_t w[BATCH][NT * 8], base[BATCH][ROWS], masks[BATCH];    // w: FORWARD: eight ranks of a column, then of the other; else a rank of both
-        int column[BATCH];
+    if constexpr (!BOTH) {
+        if (p.split != nullptr && threadIdx.x < ROWS * (r / 2)) {
+            const int row = threadIdx.x / (r / 2), j = 2 * (threadIdx.x % (r / 2));
+            const Split v = split_bf16(sh.low[row][j], sh.low[row][j + 1]);
+            if (row < rows) p.split[((size_t)(m0 + row) * r + j) / 2] = make_uint2(v.hi, v.lo);
+        }
+        return;
+    }
+    if constexpr (FORWARD) {
+        // ---- the second product with B [C, r]: NT threads share a column, eight ranks each, so that a warp reads in one stretch
+        constexpr int BATCH = 8;
+        const int j = lane % NT, c_lo = 2 * p_lo, total = 2 * (p_hi - p_lo) * NT;
+        float low[ROWS][8];
 #pragma unroll
-        for (int u = 0; u < BATCH; ++u) {
-            const int unit = unit0 + u * THREADS, e = ROWS > 1 && unit < units ? unit / n_pairs : 0, c = 2 * (p_lo + (unit < units ? unit - e * n_pairs : 0));
-            column[u] = c;
-            masks[u] = unit < units ? sh.entry_mask[e] : 0u;
-            const bf16* La = p.L2 + (size_t)sh.entry_adapter[e] * r * C;
+        for (int i = 0; i < ROWS; ++i)
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                if (8 * j >= r) break;
-                if constexpr (FORWARD) {
-                    const uint4 a = ldg16(La + (size_t)c * r + 8 * j), b = ldg16(La + (size_t)(c + 1) * r + 8 * j);
-                    w[u][8 * j] = a.x; w[u][8 * j + 1] = a.y; w[u][8 * j + 2] = a.z; w[u][8 * j + 3] = a.w;
-                    w[u][8 * j + 4] = b.x; w[u][8 * j + 5] = b.y; w[u][8 * j + 6] = b.z; w[u][8 * j + 7] = b.w;
-                } else {
+            for (int k = 0; k < 8; ++k) low[i][k] = sh.low[i][8 * j + k];
+        for (int e = 0; e < n_entries; ++e) {
+            const bf16* La = p.L2 + (size_t)sh.entry_adapter[e] * r * C + 8 * j;
+            const uint32_t mask = sh.entry_mask[e];
+            for (int at = warp * 32; at < total; at += THREADS * BATCH) {
+                uint4 w[BATCH];
+                uint32_t base[BATCH][ROWS];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) w[u][8 * j + i] = __ldg(reinterpret_cast<const uint32_t*>(La + (size_t)(8 * j + i) * C + c));
+                for (int u = 0; u < BATCH; ++u) {
+                    const int i = at + u * THREADS + lane, c = c_lo + i / NT;
+                    w[u] = i < total && 8 * j < r ? ldg16(La + (size_t)c * r) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                    for (int k = 0; k < ROWS; ++k)
+                        base[u][k] = j == 0 && i < total && ((mask >> k) & 1u) ? *reinterpret_cast<const uint16_t*>(p.Base + (size_t)(m0 + k) * C + c) : 0u;
+                }
+#pragma unroll
+                for (int u = 0; u < BATCH; ++u) {
+                    const int i = at + u * THREADS + lane, c = c_lo + i / NT;
+                    const uint32_t v[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
+#pragma unroll
+                    for (int k = 0; k < ROWS; ++k) {
+                        float s = 0.f;
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) s = fmaf(low[k][2 * h], bf16_lo(v[h]), fmaf(low[k][2 * h + 1], bf16_hi(v[h]), s));
+#pragma unroll
+                        for (int o = 1; o < NT; o <<= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+                        if (j == 0 && i < total && ((mask >> k) & 1u)) p.Out[(size_t)(m0 + k) * C + c] = __float2bfloat16_rn(bf16_lo(base[u][k]) + s);
+                    }
                 }
             }
-#pragma unroll
-            for (int i = 0; i < ROWS; ++i)
-                base[u][i] = (masks[u] >> i) & 1u ? *reinterpret_cast<const uint32_t*>(p.Base + (size_t)(m0 + i) * C + c) : 0u;
         }
+    } else {
+        // ---- the second product with A [r, C]: a thread has two neighbouring columns of one entry, BATCH such units at a time
+        constexpr int BATCH = NT <= 2 ? 4 : NT <= 4 ? 2 : 1;
+        const int n_pairs = p_hi - p_lo, units = n_entries * n_pairs;
+        for (int unit0 = threadIdx.x; unit0 < units; unit0 += THREADS * BATCH) {
+            uint32_t w[BATCH][NT * 8], base[BATCH][ROWS], masks[BATCH];
+            int column[BATCH];
 #pragma unroll
-        for (int u = 0; u < BATCH; ++u)
-#pragma unroll
-            for (int i = 0; i < ROWS; ++i) {
-                if (!((masks[u] >> i) & 1u)) continue;
-                float a = 0.f, b = 0.f;
+            for (int u = 0; u < BATCH; ++u) {
+                const int unit = unit0 + u * THREADS, e = ROWS > 1 && unit < units ? unit / n_pairs : 0, c = 2 * (p_lo + (unit < units ? unit - e * n_pairs : 0));
+                column[u] = c;
+                masks[u] = unit < units ? sh.entry_mask[e] : 0u;
+                const bf16* La = p.L2 + (size_t)sh.entry_adapter[e] * r * C;
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
                     if (8 * j >= r) break;
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const float v = sh.low[i][8 * j + k];
-                        if constexpr (FORWARD) {
-                            const uint32_t wa = w[u][8 * j + k / 2], wb = w[u][8 * j + 4 + k / 2];
-                            a = fmaf(v, k & 1 ? bf16_hi(wa) : bf16_lo(wa), a);
-                            b = fmaf(v, k & 1 ? bf16_hi(wb) : bf16_lo(wb), b);
-                        } else {
+                    for (int i = 0; i < 8; ++i) w[u][8 * j + i] = __ldg(reinterpret_cast<const uint32_t*>(La + (size_t)(8 * j + i) * C + c));
+                }
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i)
+                    base[u][i] = (masks[u] >> i) & 1u ? *reinterpret_cast<const uint32_t*>(p.Base + (size_t)(m0 + i) * C + c) : 0u;
+            }
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u)
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i) {
+                    if (!((masks[u] >> i) & 1u)) continue;
+                    float a = 0.f, b = 0.f;
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) {
+                        if (8 * j >= r) break;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const float v = sh.low[i][8 * j + k];
                             a = fmaf(v, bf16_lo(w[u][8 * j + k]), a);
                             b = fmaf(v, bf16_hi(w[u][8 * j + k]), b);
                         }
                     }
+                    *reinterpret_cast<uint32_t*>(p.Out + (size_t)(m0 + i) * C + column[u]) = bf16x2(bf16_lo(base[u][i]) + a, bf16_hi(base[u][i]) + b);
                 }
-                *reinterpret_cast<uint32_t*>(p.Out + (size_t)(m0 + i) * C + column[u]) = bf16x2(bf16_lo(base[u][i]) + a, bf16_hi(base[u][i]) + b);
-            }
+        }
     }
     if (p.Out != p.Base)                                               // tokens without an adapter
         for (int i = 0; i < rows; ++i)
@@ -265,7 +303,7 @@ adapters_few_kernel(const Products p) {
     cluster_arrive();                                                  // (a CTA's shared memory is written to once it has begun)
     pdl_wait();
     cluster_wait();
-    few_tokens<FORWARD, NT, ROWS, CTAS>(p, (int)(blockIdx.x / CTAS) * ROWS, sh);
+    few_tokens<FORWARD, NT, ROWS, CTAS, true>(p, (int)(blockIdx.x / CTAS) * ROWS, sh);
 }
 
 // ---------------------------------------------------------------------------------------------------------------- down
@@ -273,9 +311,10 @@ adapters_few_kernel(const Products p) {
 // contraction (fragments as in lora_down.cuh) and add their sums in order.  The second product gets s P as two bf16 each from here, so that it
 // need not take every value apart again for each of its columns.
 //
-// Tiles of 16 tokens with more than two adapters (single tokens in generation beside the prompts of others) would be sixteen blocks' work for one block, in
-// both products: blocks of their own, the last of the grid, look for such tiles and take their tokens in turn, both products of one at a time.
-constexpr int DN_WARPS = 8, DN_ENTRIES = 2, DN_WINDOW = 16384;
+// Tiles of 16 tokens with more than two adapters (single tokens in generation beside the prompts of others) would be sixteen blocks' work for one block:
+// helpers, the first blocks of the grid, look for such tiles and take their tokens in turn; the first of them lists the tiles, for the second product, whose blocks
+// share them out when they are through with their own.
+constexpr int DN_WARPS = 8, DN_ENTRIES = 2, DN_WINDOW = 16384, DN_HELPERS = 32;
 
 // Lane i holds the adapter of token i of one (16 lanes) or two tiles: whether its tile is one of more than DN_ENTRIES adapters.
 __device__ __forceinline__ bool of_scattered_tile(int adapter) {
@@ -292,15 +331,15 @@ template <bool L_IS_A, int NT, int NB, int CTAS>
 struct DownTile {
     static constexpr int ROWS = 16 * NB, CHUNK = 64;
     static constexpr int IN_BYTES = ROWS * 128, L_BYTES = NT * 8 * 128, STAGE = IN_BYTES + L_BYTES;
-    static constexpr int STAGES = NT == 1 ? 4 : NT == 8 ? 2 : 3;
+    static constexpr int STAGES = NT == 1 ? 4 : NT == 2 ? 3 : 2;
     static constexpr size_t RING = (size_t)STAGES * STAGE * DN_WARPS, SUMS = sizeof(float) * DN_WARPS * NB * NT * 128, FEW = sizeof(FewShared<NT, 1, 1>);
     static constexpr size_t OWN = RING > SUMS ? (RING > FEW ? RING : FEW) : (SUMS > FEW ? SUMS : FEW), PARTS = CTAS > 1 ? CTAS * NB * NT * 64 * sizeof(float2) : 0;
     static constexpr size_t SMEM = OWN + PARTS;
 };
 
 template <bool L_IS_A, int NT, int NB, int CTAS>
-__global__ void __launch_bounds__(32 * DN_WARPS, NT <= 2 ? 2 : 1)
-adapters_down_kernel(const Products p, int n_tiles) {
+__global__ void __launch_bounds__(32 * DN_WARPS, NT <= 4 ? 2 : 1)
+adapters_down_kernel(const Products p, int n_helpers) {
     using Tile = DownTile<L_IS_A, NT, NB, CTAS>;
     constexpr int ROWS = Tile::ROWS, CHUNK = Tile::CHUNK, STAGES = Tile::STAGES;
     union Shared {
@@ -316,14 +355,15 @@ adapters_down_kernel(const Products p, int n_tiles) {
     if (CTAS > 1) cluster_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int M = p.M, T = p.T, r = p.r;
-    if ((int)blockIdx.x >= n_tiles * CTAS) {
-        const int me = (int)blockIdx.x - n_tiles * CTAS, blocks = (int)gridDim.x - n_tiles * CTAS;
-        int n = 0;                                                     // tokens of such tiles so far
+    if ((int)blockIdx.x < n_helpers) {
+        const int me = (int)blockIdx.x, blocks = n_helpers;
+        int n = 0, n_tiles = 0;                                        // tokens of such tiles so far
         for (int w0 = 0; w0 < M; w0 += DN_WINDOW) {
             const int chunks = min(DN_WINDOW, M - w0 + 31) / 32;       // of 32 tokens
             __syncthreads();
             for (int i = threadIdx.x; i < DN_WINDOW / 512; i += 32 * DN_WARPS) scattered[i] = 0u;
             __syncthreads();
+            bool any = false;
             for (int i0 = warp; i0 < chunks; i0 += 8 * DN_WARPS) {
                 int a[8];
 #pragma unroll
@@ -335,23 +375,27 @@ adapters_down_kernel(const Products p, int n_tiles) {
                 for (int k = 0; k < 8; ++k) {
                     const uint32_t found = __ballot_sync(0xFFFFFFFFu, of_scattered_tile(a[k] >= p.n_adapters ? -1 : a[k]));
                     const int i = i0 + k * DN_WARPS;
+                    any |= found != 0;
                     if (lane == 0 && found != 0) atomicOr(&scattered[i / 16], ((found & 1u) | ((found >> 15) & 2u)) << (2 * (i % 16)));
                 }
             }
-            __syncthreads();
+            if (!__syncthreads_or(any)) continue;
             for (int i = 0; i < DN_WINDOW / 512; ++i)
                 for (uint32_t bits = scattered[i]; bits != 0; bits &= bits - 1) {
                     const int m0 = w0 + (32 * i + __ffs(bits) - 1) * 16;
+                    if (me == 0 && threadIdx.x == 0 && p.left != nullptr) p.left[1 + n_tiles] = m0 / 16;
+                    ++n_tiles;
                     for (int k = 0; k < 16 && m0 + k < M; ++k)
                         if (n++ % blocks == me) {
-                            few_tokens<L_IS_A, NT, 1, 1>(p, m0 + k, sh.few);
+                            few_tokens<L_IS_A, NT, 1, 1, false>(p, m0 + k, sh.few);
                             __syncthreads();
                         }
                 }
         }
+        if (me == 0 && threadIdx.x == 0 && p.left != nullptr) p.left[0] = n_tiles;
         return;
     }
-    const int m0 = (int)blockIdx.x / CTAS * ROWS, cta = CTAS > 1 ? (int)cluster_ctarank() : 0;
+    const int m0 = ((int)blockIdx.x - n_helpers) / CTAS * ROWS, cta = CTAS > 1 ? (int)cluster_ctarank() : 0;
     constexpr int ALL = DN_WARPS * CTAS;                               // warps of the tile
     const int me = cta * DN_WARPS + warp;
     const uint32_t ring = smem_u32(smem) + warp * STAGES * Tile::STAGE;
@@ -553,6 +597,98 @@ __device__ __forceinline__ void up_fragments(const bf16* __restrict__ L2, int C,
     }
 }
 
+// Four tokens (m0 ..) of a tile of more than DN_ENTRIES adapters, a warp's columns of them, on the CUDA cores.
+template <bool FROM_B, int KS, int UB>
+__device__ __forceinline__ void up_scattered(const Products& p, int m0, int c_warp) {
+    const int lane = threadIdx.x & 31, C = p.C, r = p.r;
+    if (c_warp >= C) return;
+    int adapter[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        adapter[k] = m0 + k < p.M ? __ldg(p.adapter_of + m0 + k) : -1;
+        if (adapter[k] < 0 || adapter[k] >= p.n_adapters) adapter[k] = -1;
+    }
+    if constexpr (FROM_B) {
+        // NL lanes share a column, eight ranks each
+        constexpr int NL = 2 * KS, ITEMS = UB * NL, AHEAD = ITEMS <= 4 ? 4 : 2;
+        const int j = lane % NL;
+#pragma unroll
+        for (int k0 = 0; k0 < 4; k0 += AHEAD) {
+            uint4 w[AHEAD][ITEMS], low[AHEAD][2];
+            uint32_t base[AHEAD][ITEMS];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int a = adapter[k0 + k], m = m0 + k0 + k;
+                const bool on = a >= 0 && 8 * j < r;
+                const bf16* La = p.L2 + (size_t)max(a, 0) * r * C + 8 * j;
+                const uint4* from = reinterpret_cast<const uint4*>(p.split + (size_t)m * (r / 2) + 4 * j);
+                low[k][0] = on ? from[0] : make_uint4(0, 0, 0, 0);
+                low[k][1] = on ? from[1] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < ITEMS; ++i) {
+                    const int c = c_warp + (32 / NL) * i + lane / NL;
+                    w[k][i] = on && c < C ? ldg16(La + (size_t)c * r) : make_uint4(0, 0, 0, 0);
+                    base[k][i] = j == 0 && m < p.M && c < C ? *reinterpret_cast<const uint16_t*>(p.Base + (size_t)m * C + c) : 0u;
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int m = m0 + k0 + k;
+                const uint32_t lw[8] = {low[k][0].x, low[k][0].y, low[k][0].z, low[k][0].w, low[k][1].x, low[k][1].y, low[k][1].z, low[k][1].w};   // (high, low) pairs
+#pragma unroll
+                for (int i = 0; i < ITEMS; ++i) {
+                    const uint32_t v[4] = {w[k][i].x, w[k][i].y, w[k][i].z, w[k][i].w};
+                    float s = 0.f;
+#pragma unroll
+                    for (int h = 0; h < 4; ++h)
+                        s = fmaf(bf16_lo(lw[2 * h]) + bf16_lo(lw[2 * h + 1]), bf16_lo(v[h]), fmaf(bf16_hi(lw[2 * h]) + bf16_hi(lw[2 * h + 1]), bf16_hi(v[h]), s));
+#pragma unroll
+                    for (int o = 1; o < NL; o <<= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+                    const int c = c_warp + (32 / NL) * i + lane / NL;
+                    if (j == 0 && m < p.M && c < C)
+                        *reinterpret_cast<uint16_t*>(p.Out + (size_t)m * C + c) =
+                            adapter[k0 + k] >= 0 ? __bfloat16_as_ushort(__float2bfloat16_rn(bf16_lo(base[k][i]) + s)) : (uint16_t)base[k][i];
+                }
+            }
+        }
+    } else {
+        // two neighbouring columns to a lane, eight ranks of all four tokens at a time
+#pragma unroll
+        for (int i = 0; i < UB; ++i) {
+            const int c = c_warp + 64 * i + 2 * lane;
+            if (2 * lane + 64 * i >= 32 * UB || c >= C) continue;
+            uint32_t base[4];
+            float x[4], y[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                base[k] = m0 + k < p.M ? *reinterpret_cast<const uint32_t*>(p.Base + (size_t)(m0 + k) * C + c) : 0u;
+                x[k] = y[k] = 0.f;
+            }
+            for (int j = 0; j < r; j += 8) {
+                uint32_t w[4][8];
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int h = 0; h < 8; ++h)
+                        w[k][h] = adapter[k] >= 0 ? __ldg(reinterpret_cast<const uint32_t*>(p.L2 + ((size_t)adapter[k] * r + j + h) * C + c)) : 0u;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int h = 0; h < 8; h += 2) {
+                        const uint2 l = adapter[k] >= 0 ? p.split[((size_t)(m0 + k) * r + j + h) / 2] : make_uint2(0, 0);
+                        const float v0 = bf16_lo(l.x) + bf16_lo(l.y), v1 = bf16_hi(l.x) + bf16_hi(l.y);
+                        x[k] = fmaf(v0, bf16_lo(w[k][h]), fmaf(v1, bf16_lo(w[k][h + 1]), x[k]));
+                        y[k] = fmaf(v0, bf16_hi(w[k][h]), fmaf(v1, bf16_hi(w[k][h + 1]), y[k]));
+                    }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (m0 + k < p.M)
+                    *reinterpret_cast<uint32_t*>(p.Out + (size_t)(m0 + k) * C + c) = adapter[k] >= 0 ? bf16x2(bf16_lo(base[k]) + x[k], bf16_hi(base[k]) + y[k]) : base[k];
+        }
+    }
+}
+
 // KS steps of 16 ranks.
 template <bool FROM_B, int KS, int UB>
 __global__ void __launch_bounds__(32 * UP_WARPS, 2)
@@ -561,8 +697,8 @@ adapters_up_kernel(const Products p, int tiles_each) {
     pdl_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
     const int c_warp = (blockIdx.y * UP_WARPS + warp) * 32 * UB, M = p.M, C = p.C, r = p.r;
-    if (c_warp >= C) return;
-    const int tiles = (M + UP_ROWS - 1) / UP_ROWS, tile_end = min(tiles, ((int)blockIdx.x + 1) * tiles_each);
+    const int n_left = __ldcg(p.left);
+    const int tiles = (M + UP_ROWS - 1) / UP_ROWS, tile_end = c_warp < C ? min(tiles, ((int)blockIdx.x + 1) * tiles_each) : 0;
     struct Tile {
         uint4 base[UB][2];
         int adapter;                                                   // of row `lane`, modulo sixteen
@@ -623,12 +759,12 @@ adapters_up_kernel(const Products p, int tiles_each) {
         const int m0 = tile * UP_ROWS;
         const int a = x.adapter >= 0 && x.adapter < p.n_adapters ? x.adapter : -1;
         uint32_t mask_here = 0xFFFFu, firsts = 1u;
-        bool elsewhere = false;
+        bool elsewhere = false;                                        // one of the tiles that are left for the end
         const bool one = held_adapter >= 0 && __all_sync(0xFFFFFFFFu, a == held_adapter);   // the adapter before, in every row
         if (!one) {
             mask_here = entry_of_lane(lane < UP_ROWS ? a : -1);
             firsts = __ballot_sync(0xFFFFFFFFu, mask_here != 0);
-            elsewhere = __popc(firsts) > DN_ENTRIES;                   // (of_scattered_tile)
+            elsewhere = __popc(firsts) > DN_ENTRIES;
             if (elsewhere) firsts = 0;
         }
         while (firsts != 0) {
@@ -700,6 +836,11 @@ adapters_up_kernel(const Products p, int tiles_each) {
         if (KS == 1) low = following_low;
         else if (tile + 1 < tile_end) load_low(1, whole(tile + 1), low);
     }
+    // what was left: four tokens and a block's columns at a time, all blocks in turn
+    const int groups = gridDim.y;
+#pragma unroll 1
+    for (int i = blockIdx.y * gridDim.x + blockIdx.x; i < n_left * 4 * groups; i += gridDim.x * groups)
+        up_scattered<FROM_B, KS, UB>(p, __ldcg(p.left + 1 + i / (4 * groups)) * UP_ROWS + i / groups % 4 * 4, (i % groups * UP_WARPS + warp) * 32 * UB);
 }
 
 // --------------------------------------------------------------------------------------------------------------- grads
@@ -1078,8 +1219,10 @@ int down_impl(const Products& p, cudaStream_t st) {
     static SmemLimit limit;
     auto kern = adapters_down_kernel<L_IS_A, NT, NB, CTAS>;
     if (!limit.raise(kern, smem)) return QLORA_ERR_CUDA;
-    const int tiles = (p.M + 16 * NB - 1) / (16 * NB);
-    return launch_pdl(kern, dim3((tiles + sm_count() / CTAS) * CTAS), dim3(32 * DN_WARPS), smem, st, CTAS, p, tiles) == cudaSuccess ? QLORA_OK : QLORA_ERR_CUDA;
+    // helpers: on what the tiles leave free, or a few that are soon through with looking
+    const int tiles = (p.M + 16 * NB - 1) / (16 * NB) * CTAS, room = (NT <= 4 ? 2 : 1) * sm_count() - tiles;
+    const int helpers = (room < DN_HELPERS / 2 ? DN_HELPERS : room > sm_count() ? sm_count() : room) / CTAS * CTAS;
+    return launch_pdl(kern, dim3(helpers + tiles), dim3(32 * DN_WARPS), smem, st, CTAS, p, helpers) == cudaSuccess ? QLORA_OK : QLORA_ERR_CUDA;
 }
 
 template <bool FROM_B, int KS, int UB>
@@ -1113,7 +1256,7 @@ int products(const Products& p, cudaStream_t st) {
         return few_impl<FORWARD, NT, 4, 4>(p, st);
     }
     // blocks to a tile: while all of them run at a time
-    const int tiles = (p.M + 16 * NB - 1) / (16 * NB), room = (NT <= 2 ? 2 : 1) * sm_count();
+    const int tiles = (p.M + 16 * NB - 1) / (16 * NB), room = (NT <= 4 ? 2 : 1) * sm_count();
     const int rc = 4 * tiles <= room ? down_impl<FORWARD, NT, NB, 4>(p, st) : 2 * tiles <= room ? down_impl<FORWARD, NT, NB, 2>(p, st) : down_impl<FORWARD, NT, NB, 1>(p, st);
     return rc != QLORA_OK || p.Out == nullptr ? rc : up_impl<FORWARD, KS, UB>(p, st);
 }
@@ -1157,13 +1300,16 @@ int grad_impl(const Grads& p, cudaStream_t st) {
 
 }  // namespace
 
+size_t adapters_scratch_bytes(int M, int r) { return (size_t)M * r * 4 + 4 * (1 + ((size_t)M + 15) / 16); }
+
 int launch_adapters(bool forward, int M, int T, int C, int r, int n_adapters, const void* In, const int32_t* adapter_of, const void* L1, const void* L2,
-                    const float* scales, const void* Base, void* Out, float* P, void* split, cudaStream_t st) {
-    const Products p{M, T, C, r, n_adapters, (const bf16*)In, adapter_of, (const bf16*)L1, (const bf16*)L2, scales, (const bf16*)Base, (bf16*)Out, P, (uint2*)split};
+                    const float* scales, const void* Base, void* Out, float* P, void* scratch, cudaStream_t st) {
+    const Products p{M, T, C, r, n_adapters, (const bf16*)In, adapter_of, (const bf16*)L1, (const bf16*)L2, scales, (const bf16*)Base, (bf16*)Out, P, (uint2*)scratch,
+                     scratch != nullptr ? reinterpret_cast<int*>(static_cast<char*>(scratch) + (size_t)M * r * 4) : nullptr};
 #define QLORA_PRODUCTS(NT, NB, KS, UB) return forward ? products<true, NT, NB, KS, UB>(p, st) : products<false, NT, NB, KS, UB>(p, st)
     if (r <= 8) QLORA_PRODUCTS(1, 1, 1, 2);
     if (r <= 16) QLORA_PRODUCTS(2, 1, 1, 2);
-    if (r <= 32) QLORA_PRODUCTS(4, 2, 2, 1);
+    if (r <= 32) QLORA_PRODUCTS(4, 1, 2, 1);
     QLORA_PRODUCTS(8, 2, 4, 1);
 #undef QLORA_PRODUCTS
 }

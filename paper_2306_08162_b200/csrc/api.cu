@@ -94,7 +94,10 @@ int check_adapters(const qlora_adapters_desc* d, int M) {
 }
 // Workspace of the calls on adapters: two [M, r] products, then the scratch of the gradients.
 size_t adapters_low_bytes(const qlora_adapters_desc& d, int M) { return align_up((size_t)M * (size_t)d.r * sizeof(float), 256); }
-size_t adapters_bytes(const qlora_adapters_desc& d, int M) { return 2 * adapters_low_bytes(d, M) + adapters_grad_scratch_bytes(M, d.K, d.N, d.r, d.n_adapters); }
+size_t adapters_bytes(const qlora_adapters_desc& d, int M) {
+    const size_t grads = 2 * adapters_low_bytes(d, M) + adapters_grad_scratch_bytes(M, d.K, d.N, d.r, d.n_adapters), products = adapters_scratch_bytes(M, d.r);
+    return grads > products ? grads : products;
+}
 
 struct Workspace {
     size_t p0_off, p1_off, grad_off, sync_off, split_off, db_off;
@@ -269,7 +272,7 @@ static int adapters_common(bool forward, const qlora_adapters_desc* desc, int M,
     if (!aligned16(In) || !aligned4(adapter_of) || !aligned16(A) || !aligned16(B) || !aligned4(scales) || !aligned16(Base) || !aligned16(Out) ||
         !aligned16(low) || !aligned16(workspace))
         return QLORA_ERR_ALIGNMENT;
-    if (workspace == nullptr || workspace_bytes < adapters_low_bytes(d, M)) return QLORA_ERR_WORKSPACE;
+    if (workspace == nullptr || workspace_bytes < adapters_scratch_bytes(M, d.r)) return QLORA_ERR_WORKSPACE;
     return launch_adapters(forward, M, T, C, d.r, d.n_adapters, In, adapter_of, forward ? A : B, forward ? B : A, scales, Base, Out, low, workspace,
                            (cudaStream_t)cuda_stream);
 }
