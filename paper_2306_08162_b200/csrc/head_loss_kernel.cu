@@ -15,7 +15,7 @@
 //
 // One persistent kernel: a pair of CTAs (two SMs) claims items of both products from one counter (head_plan.h), so there is no wave to wait for
 // between the products or the pieces.  An item is a tile of 256 x 256 (tcgen05.mma.cta_group::2, M = 256, N = 256; 128 rows and half of the other
-// operand per CTA), operands staged by TMA in six stages of 64 contraction elements, accumulators in tensor memory twice, so that the epilogue of an item
+// operand per CTA), operands staged by TMA in six stages (more for few rows) of 64 contraction elements, accumulators in tensor memory twice, so that the epilogue of an item
 // runs beside the products of the next.  What an item needs from others (probabilities of its rows, the previous piece's sums, a free slot
 // of the ring, the reference) it waits for through counters in the workspace; those items were claimed earlier, so the wait ends
 // whichever CTAs share the GPU.  Every wait is bounded.
@@ -41,11 +41,11 @@ namespace {
 
 typedef __nv_bfloat16 bf16;
 
-constexpr int HL_THREADS = 256, HL_STAGES = 6, HL_EPI_WARP0 = 4, HL_EPI_WARPS = 4, HL_CLAIMS = 4;
-constexpr uint32_t HL_HALF = 128 * 64 * 2, HL_STAGE = 2 * HL_HALF;     // one CTA's part of an operand; of both
+constexpr int HL_THREADS = 256, HL_MAX_STAGES = 12, HL_EPI_WARP0 = 4, HL_EPI_WARPS = 4, HL_CLAIMS = 4;
+constexpr uint32_t HL_HALF = 128 * 64 * 2;                            // one CTA's part of an operand
 constexpr uint32_t HL_SLICE = 4096;                                   // staging of an epilogue warp
-constexpr uint32_t HL_OFF_SLICES = HL_STAGES * HL_STAGE, HL_OFF_BARS = HL_OFF_SLICES + HL_EPI_WARPS * HL_SLICE;
-constexpr size_t HL_SMEM = HL_OFF_BARS + 256 + 1024;
+constexpr uint32_t HL_RING = 6 * 2 * HL_HALF, HL_OFF_SLICES = HL_RING, HL_OFF_BARS = HL_OFF_SLICES + HL_EPI_WARPS * HL_SLICE;
+constexpr size_t HL_SMEM = HL_OFF_BARS + 512 + 1024;
 constexpr int HL_WAIT_US = 250000;
 constexpr uint32_t HL_SPINS = 1u << 26;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f, MOST = 3.402823466e38f;
@@ -61,6 +61,9 @@ struct HeadParams {
     int again;                               // the second launch: only blocks that are to be done again
     int tokens, copies;                      // copies: the hidden states are copied even where every token has a label
     int wait_limit_us;
+    // A stage: the rows' operand (row_bytes) and the head's.  Up to 128 tokens it has room for those rows alone, so that more stages are under way, which is what
+    // reading the head takes: the products read on into whatever lies behind, for rows of the result that nobody takes.
+    uint32_t stages, stage, row_bytes;
     float scale;                             // log2 e, and what the products' sums lose (CUT_OFF)
     size_t padded;                           // rows of the buffers
     unsigned* counters;
@@ -140,9 +143,8 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint32_t tmem_base_slot;
     __shared__ int abort_flag_s[2];
-    __shared__ int claimed_s[HL_CLAIMS];
+    __shared__ int4 claimed_s[HL_CLAIMS][2];                           // kind (-1 at the end), q, piece, block in its chunk; block, tile, steps
     volatile int* abort_flag = abort_flag_s;
-    volatile int* claimed = claimed_s;
     pdl_launch_dependents();
     if (p.again) {
         pdl_wait();
@@ -154,8 +156,8 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
     const uint32_t cta = cluster_ctarank();                            // 0 = leader: issues the products, claims the items
 
     const uint32_t bar_full = smem0 + HL_OFF_BARS;                     // [stages] leader's: both CTAs' operands landed
-    const uint32_t bar_empty = bar_full + 8 * HL_STAGES;               // [stages] both: read by the products (multicast commit)
-    const uint32_t bar_acc_full = bar_empty + 8 * HL_STAGES;           // [2] both: accumulators complete (multicast commit)
+    const uint32_t bar_empty = bar_full + 8 * HL_MAX_STAGES;           // [stages] both: read by the products (multicast commit)
+    const uint32_t bar_acc_full = bar_empty + 8 * HL_MAX_STAGES;           // [2] both: accumulators complete (multicast commit)
     const uint32_t bar_acc_empty = bar_acc_full + 16;                  // [2] leader's: drained by both epilogues
     const uint32_t bar_claim_full = bar_acc_empty + 16;                // [claims] both: an item's number is there
     const uint32_t bar_claim_empty = bar_claim_full + 8 * HL_CLAIMS;   // [claims] leader's: read by every role of both CTAs
@@ -163,7 +165,7 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
     if (threadIdx.x == 0) {
         abort_flag_s[0] = 0;
         abort_flag_s[1] = p.wait_limit_us;
-        for (int i = 0; i < HL_STAGES; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
+        for (uint32_t i = 0; i < p.stages; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(bar_acc_full + 8 * i, 1); mbar_init(bar_acc_empty + 8 * i, 2 * HL_EPI_WARPS); }
         for (int i = 0; i < HL_CLAIMS; ++i) { mbar_init(bar_claim_full + 8 * i, 1); mbar_init(bar_claim_empty + 8 * i, 2 + 1 + 2 * HL_EPI_WARPS); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -187,15 +189,19 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
     auto active = [&](int block) { return block < rows.blocks && (!p.again || __ldcg(to_do_again(p) + block) != 0u); };
     auto steps_of = [&](const HeadItem& it) { return it.of_grad ? head_div_up(head_piece_entries(plan, it.piece), kHeadStep) : steps_d; };
 
-    // What every role does for its next item: the number that the leader claimed, -1 at the end.  (leave() gives the place back.)
+    // What every role does for its next item, which the leader has claimed, looked up and waited for: decoding a number costs some hundred cycles of
+    // divisions, in which a role that issues copies or products would fall behind.
+    struct Item : HeadItem { int steps; };
     Ring claim;
-    auto next = [&](int* index) -> bool {
+    auto next = [&](Item* it) -> bool {
         if (!poll(bar_claim_full + 8 * claim.slot, claim.phase, abort_flag)) return false;
-        *index = claimed[claim.slot];
+        const int4 a = claimed_s[claim.slot][0], b = claimed_s[claim.slot][1];
         __syncwarp();
         if (lane == 0) arrive_release_cluster(leader_claim_empty + 8 * claim.slot);
         claim.advance(HL_CLAIMS);
-        return *index >= 0;
+        it->of_grad = a.x; it->q = a.y; it->piece = a.z; it->block_in_chunk = a.w;
+        it->block = b.x; it->tile = b.y; it->steps = b.z;
+        return a.x >= 0;
     };
 
     if (warp == 2) {
@@ -211,16 +217,30 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
                         const unsigned i = atomicAdd(counter, 1u);
                         if ((long long)i >= rows.total) break;
                         const HeadItem it = head_item(plan, rows, i);
-                        if (!active(it.block) || (!it.of_grad && it.tile * kHeadTile >= head_piece_entries(plan, it.piece))) continue;   // (the last piece and chunk are shorter)
+                        if (!active(it.block) || (!it.of_grad && it.tile * plan.tile >= head_piece_entries(plan, it.piece))) continue;   // (the last piece and chunk are shorter)
                         index = (int)i;
                         break;
                     }
-                    claimed[claim.slot] = index;
-                    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer + 4 * claim.slot), "r"(index) : "memory");
+                }
+                index = __shfl_sync(0xFFFFFFFFu, index, 0);
+                more = index >= 0;
+                HeadItem it{};
+                it.of_grad = -1;
+                if (more) it = head_item(plan, rows, index);
+                if (GRAD && it.of_grad > 0) {                          // its probabilities
+                    const unsigned tiles = (unsigned)head_div_up(head_piece_entries(plan, it.piece), plan.tile);
+                    if (!poll_counter(logits_done(p) + (size_t)it.q * kHeadChunk + it.block_in_chunk, COUNTS_PER_TILE * tiles, abort_flag)) break;
+                }
+                if (lane == 0) {
+                    const int steps = more ? steps_of(it) : 0;
+                    claimed_s[claim.slot][0] = make_int4(it.of_grad, it.q, it.piece, it.block_in_chunk);
+                    claimed_s[claim.slot][1] = make_int4(it.block, it.tile, steps, 0);
+                    st_cluster_16(peer + 32 * claim.slot, (uint32_t)it.of_grad, (uint32_t)it.q, (uint32_t)it.piece, (uint32_t)it.block_in_chunk);
+                    st_cluster_16(peer + 32 * claim.slot + 16, (uint32_t)it.block, (uint32_t)it.tile, (uint32_t)steps, 0u);
                     mbar_arrive(bar_claim_full + 8 * claim.slot);
                     arrive_release_cluster(peer_full + 8 * claim.slot);
                 }
-                more = __shfl_sync(0xFFFFFFFFu, index, 0) >= 0;
+                __syncwarp();
                 claim.advance(HL_CLAIMS);
             }
         }
@@ -229,34 +249,32 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
         Ring ring;
         const uint32_t leader_full = map_to_cta(bar_full, 0);
         const CUtensorMap* of_rows = n_rows == p.tokens && !p.copies ? &tm_hidden : &tm_rows;
-        int index;
-        while (next(&index)) {
-            const HeadItem it = head_item(plan, rows, index);
-            const int steps = steps_of(it);
-            if (GRAD && it.of_grad) {
-                const unsigned tiles = (unsigned)head_div_up(head_piece_entries(plan, it.piece), kHeadTile);
-                if (!poll_counter(logits_done(p) + (size_t)it.q * kHeadChunk + it.block_in_chunk, COUNTS_PER_TILE * tiles, abort_flag)) goto done;
-                fence_proxy_async_all();                               // (written by other SMs' ordinary stores)
-            }
+        Item it;
+        while (next(&it)) {
+            const int steps = it.steps;
+            if (GRAD && it.of_grad) fence_proxy_async_all();           // (what it reads was written by other SMs' ordinary stores)
             const int row0 = it.of_grad ? ((it.q % plan.ring) * plan.chunk_max + it.block_in_chunk) * kHeadTile + (int)cta * 128 : it.block * kHeadTile + (int)cta * 128;
-            const int other0 = it.of_grad ? it.tile * kHeadTile + (int)cta * 128 : it.piece * plan.piece + it.tile * kHeadTile + (int)cta * 128;
+            const int other0 = it.of_grad ? it.tile * kHeadTile + (int)cta * 128 : it.piece * plan.piece + it.tile * plan.tile + (int)cta * (plan.tile / 2);
+            // (a CTA none of whose rows are there leaves its part of the operand as it is: its rows of the result are not used)
+            const bool here = it.block * kHeadTile + (int)cta * 128 < n_rows, there = it.block * kHeadTile + 128 < n_rows;
+            const uint32_t bytes = (there ? 2 : 1) * p.row_bytes + (it.of_grad ? 2 * HL_HALF : (uint32_t)plan.tile * 128u);      // of both CTAs
             for (int step = 0; step < steps; ++step) {
                 if (!poll(bar_empty + 8 * ring.slot, ring.phase ^ 1u, abort_flag)) goto done;
                 if (elect_one()) {
-                    if (cta == 0) mbar_expect_tx(bar_full + 8 * ring.slot, 2 * HL_STAGE);
-                    const uint32_t dst = smem0 + ring.slot * HL_STAGE, bar = leader_full + 8 * ring.slot;
+                    if (cta == 0) mbar_expect_tx(bar_full + 8 * ring.slot, bytes);
+                    const uint32_t dst = smem0 + ring.slot * p.stage, other = dst + p.row_bytes, bar = leader_full + 8 * ring.slot;
                     if (GRAD && it.of_grad) {
                         const int v = it.piece * plan.piece + step * kHeadStep;
-                        tma_load_2d_pair(dst, &tm_probs, bar, step * kHeadStep, row0);
-                        tma_load_2d_pair(dst + HL_HALF, &tm_head_t, bar, other0, v);
-                        tma_load_2d_pair(dst + HL_HALF + HL_HALF / 2, &tm_head_t, bar, other0 + 64, v);
+                        if (here) tma_load_2d_pair(dst, &tm_probs, bar, step * kHeadStep, row0);
+                        tma_load_2d_pair(other, &tm_head_t, bar, other0, v);
+                        tma_load_2d_pair(other + HL_HALF / 2, &tm_head_t, bar, other0 + 64, v);
                     } else {
-                        tma_load_2d_pair(dst, of_rows, bar, step * kHeadStep, row0);
-                        tma_load_2d_pair(dst + HL_HALF, &tm_head, bar, step * kHeadStep, other0);
+                        if (here) tma_load_2d_pair(dst, of_rows, bar, step * kHeadStep, row0);
+                        tma_load_2d_pair(other, &tm_head, bar, step * kHeadStep, other0);
                     }
                 }
                 __syncwarp();
-                ring.advance(HL_STAGES);
+                ring.advance(p.stages);
             }
         }
     } else if (warp == 1) {
@@ -265,15 +283,14 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
             // rows: contraction-contiguous, 128-byte swizzle, 8-row groups 1024 B apart; the head likewise for the logits, and for the gradient with
             // 64 features contiguous: 64-feature atoms 8192 B apart, groups of 8 entries 1024 B apart
             const uint64_t a_desc0 = smem_desc(smem0, 16, 1024, 2);
-            const uint64_t b_logits = smem_desc(smem0 + HL_HALF, 16, 1024, 2), b_grad = smem_desc(smem0 + HL_HALF, 8192, 1024, 2);
+            const uint64_t b_logits = smem_desc(smem0 + p.row_bytes, 16, 1024, 2), b_grad = smem_desc(smem0 + p.row_bytes, 8192, 1024, 2);
             Ring ring;
             uint32_t n = 0;
-            int index;
-            while (next(&index)) {
-                const HeadItem it = head_item(plan, rows, index);
-                const int steps = steps_of(it);
+            Item it;
+            while (next(&it)) {
+                const int steps = it.steps;
                 const bool of_grad = GRAD && it.of_grad;
-                const uint32_t idesc = instr_desc_pair(256u, 0u, of_grad ? 1u : 0u), b_k16 = of_grad ? 2048u >> 4 : 32u >> 4;
+                const uint32_t idesc = instr_desc_pair(of_grad ? 256u : (uint32_t)plan.tile, 0u, of_grad ? 1u : 0u), b_k16 = of_grad ? 2048u >> 4 : 32u >> 4;
                 const uint64_t b_desc0 = of_grad ? b_grad : b_logits;
                 const uint32_t buffer = n & 1u, acc = tmem_base + buffer * 256u;
                 if (!poll(bar_acc_empty + 8 * buffer, ((n >> 1) & 1u) ^ 1u, abort_flag)) goto done;
@@ -281,7 +298,7 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
                 for (int step = 0; step < steps; ++step) {
                     if (!poll(bar_full + 8 * ring.slot, ring.phase, abort_flag)) goto done;
                     tc_fence_after();
-                    const uint32_t at = ring.slot * (HL_STAGE >> 4);
+                    const uint32_t at = ring.slot * (p.stage >> 4);
                     if (elect_one()) {
 #pragma unroll
                         for (uint32_t k = 0; k < kHeadStep / 16; ++k)
@@ -290,7 +307,7 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
                         if (step + 1 == steps) tc_commit_pair(bar_acc_full + 8 * buffer);
                     }
                     __syncwarp();
-                    ring.advance(HL_STAGES);
+                    ring.advance(p.stages);
                 }
                 ++n;
             }
@@ -301,9 +318,8 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
         const uint32_t leader_acc_empty = map_to_cta(bar_acc_empty, 0);
         uint8_t* slice = smem_gen + HL_OFF_SLICES + quarter * HL_SLICE;
         uint32_t n = 0;
-        int index;
-        for (; next(&index); ++n) {
-            const HeadItem it = head_item(plan, rows, index);
+        Item it;
+        for (; next(&it); ++n) {
             const uint32_t buffer = n & 1u, taddr = tmem_base + buffer * 256u + ((uint32_t)(quarter * 32) << 16);
             const int row_w = it.block * kHeadTile + (int)cta * 128 + quarter * 32, row = row_w + lane;   // (of the buffers: row < p.padded)
             if (GRAD && it.of_grad) {
@@ -316,7 +332,7 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
                 float* out = p.sums + ((size_t)set * p.padded + row_w) * plan.D;
                 const int rows_here = n_rows - row_w;
 #pragma unroll 1
-                for (int idx = 0; idx < 8; ++idx) {
+                for (int idx = 0; idx < (row_w < n_rows ? 8 : 0); ++idx) {
                     const int c = it.tile * kHeadTile + 32 * idx + 4 * (lane & 7);
                     float4 old[8];
                     if (add) {
@@ -349,7 +365,7 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
                 continue;
             }
             // ---- a tile of logits
-            const int v0 = it.piece * plan.piece + it.tile * kHeadTile, valid = min(plan.V - v0, kHeadTile);
+            const int v0 = it.piece * plan.piece + it.tile * plan.tile, valid = min(plan.V - v0, plan.tile), chunks = row_w < n_rows ? plan.tile / 32 : 0;
             const int label = row < n_rows ? __ldcg(p.label + row) - v0 : -1;
             const bool first = it.piece == 0 && it.tile == 0 && !p.again;
             float ref = 0.f;
@@ -368,7 +384,7 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
             if (GRAD && first) {
                 float m = -INFINITY;
 #pragma unroll 1
-                for (int idx = 0; idx < 8; ++idx) {
+                for (int idx = 0; idx < chunks; ++idx) {
                     uint32_t v[32];
                     tc_ld32(taddr + 32 * idx, v);
                     tc_wait_ld();
@@ -383,7 +399,7 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
             float m = -INFINITY, s = 0.f;                              // the largest logit; the sum over the reference, or over m
             bf16* out = nullptr;
             if constexpr (GRAD)
-                out = p.probs + ((size_t)((it.q % plan.ring) * plan.chunk_max + it.block_in_chunk) * kHeadTile + (int)cta * 128 + quarter * 32) * plan.piece + it.tile * kHeadTile;
+                out = p.probs + ((size_t)((it.q % plan.ring) * plan.chunk_max + it.block_in_chunk) * kHeadTile + (int)cta * 128 + quarter * 32) * plan.piece + it.tile * plan.tile;
             // 32 logits of the row; SPECIAL: the label or the vocabulary's end is among some row's
             auto chunk = [&](uint32_t (&v)[32], int idx, auto special) {
                 constexpr bool SPECIAL = decltype(special)::value;
@@ -432,7 +448,7 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
                 }
             };
 #pragma unroll 1
-            for (int idx = 0; idx < 8; ++idx) {
+            for (int idx = 0; idx < chunks; ++idx) {
                 uint32_t v[32];
                 tc_ld32(taddr + 32 * idx, v);
                 tc_wait_ld();
@@ -443,7 +459,7 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(leader_acc_empty + 8 * buffer);
-            __stcg(p.tile_stats + (size_t)row * head_div_up(plan.V, kHeadTile) + v0 / kHeadTile, make_float2(m, s));
+            __stcg(p.tile_stats + (size_t)row * head_div_up(plan.V, plan.tile) + v0 / plan.tile, make_float2(m, s));
             if constexpr (GRAD) publish(logits_done(p) + (size_t)it.q * kHeadChunk + it.block_in_chunk);
         }
     }
@@ -566,7 +582,8 @@ head_finish_kernel(HeadParams p, const int* __restrict__ place, const bf16* __re
             for (int i = 0; i < FIN_AHEAD; ++i)
                 if (threadIdx.x + i * FIN_THREADS < chunks) ahead[i] = load(threadIdx.x + i * FIN_THREADS);
         }
-        const int tiles = head_div_up(p.plan.V, kHeadTile);
+        const int tiles = head_div_up(p.plan.V, p.plan.tile);
+        const float label_logit = __ldcg(p.label_logit + row), known_ref = GRAD ? __ldcg(p.ref + row) : 0.f;
         MaxSum v{-INFINITY, 0.f};
         for (int i = threadIdx.x; i < tiles; i += FIN_THREADS) {
             const float2 stats = __ldcg(p.tile_stats + (size_t)row * tiles + i);
@@ -579,8 +596,8 @@ head_finish_kernel(HeadParams p, const int* __restrict__ place, const bf16* __re
             }
         }
         v = block_max_sum<!GRAD>(v, p.scale, parts);
-        const float ref = GRAD ? __ldcg(p.ref + row) : v.m, others = v.s;
-        const float at_label = (__ldcg(p.label_logit + row) - ref) * p.scale, mine = fast_exp2(at_label), total = others + mine;
+        const float ref = GRAD ? known_ref : v.m, others = v.s;
+        const float at_label = (label_logit - ref) * p.scale, mine = fast_exp2(at_label), total = others + mine;
         if (threadIdx.x == 0) {
             // (a label that has most of the probability: the small loss from the small sum)
             float l = others <= mine ? log1pf(others / mine) : LN2 * (log2f(total) - at_label);
@@ -641,12 +658,16 @@ static int head_loss_impl(int T, int V, int D, const void* hidden, const void* h
     p.copies = hidden == d_hidden;                                     // (the second launch still reads them)
     CUtensorMap tx, tr, th, tt{}, tp{};
     const CUtensorMapDataType type = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-    if (!make_map_2d(&tx, type, 2, hidden, (uint64_t)D, (uint64_t)T, 64, 128, CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !make_map_2d(&tr, type, 2, rows, (uint64_t)D, p.padded, 64, 128, CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !make_map_2d(&th, type, 2, head, (uint64_t)D, (uint64_t)V, 64, 128, CU_TENSOR_MAP_SWIZZLE_128B))
+    const uint32_t rows_box = T < 128 ? (uint32_t)(T + 7) / 8 * 8 : 128;
+    p.row_bytes = rows_box * 128;
+    p.stage = p.row_bytes + HL_HALF;
+    p.stages = HL_RING / p.stage < HL_MAX_STAGES ? HL_RING / p.stage : HL_MAX_STAGES;
+    if (!make_map_2d(&tx, type, 2, hidden, (uint64_t)D, (uint64_t)T, 64, rows_box, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !make_map_2d(&tr, type, 2, rows, (uint64_t)D, p.padded, 64, rows_box, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !make_map_2d(&th, type, 2, head, (uint64_t)D, (uint64_t)V, 64, (uint32_t)p.plan.tile / 2, CU_TENSOR_MAP_SWIZZLE_128B))
         return QLORA_ERR_CUDA;
     if (GRAD && (!make_map_2d(&tt, type, 2, head, (uint64_t)D, (uint64_t)V, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B) ||
-                 !make_map_2d(&tp, type, 2, p.probs, (uint64_t)p.plan.piece, (uint64_t)p.plan.ring * p.plan.chunk_max * kHeadTile, 64, 128, CU_TENSOR_MAP_SWIZZLE_128B)))
+                 !make_map_2d(&tp, type, 2, p.probs, (uint64_t)p.plan.piece, (uint64_t)p.plan.ring * p.plan.chunk_max * kHeadTile, 64, rows_box, CU_TENSOR_MAP_SWIZZLE_128B)))
         return QLORA_ERR_CUDA;
     static SmemLimit limit;
     auto kern = head_loss_kernel<GRAD>;

@@ -9,11 +9,11 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 SOURCE = r"""
 #include "head_plan.h"
 using namespace qlora;
-struct Out { int blocks_max, chunk_max, piece, pieces, features, ring, sums, blocks, chunk, chunks, all_pieces, lead; long long total; };
+struct Out { int blocks_max, chunk_max, tile, piece, pieces, features, ring, sums, blocks, chunk, chunks, all_pieces, lead; long long total; };
 extern "C" void plan(int T, int V, int D, int grad, int rows, Out* o) {
     const HeadPlan p = head_plan(T, V, D, grad);
     const HeadRows r = head_rows(p, rows);
-    *o = Out{p.blocks_max, p.chunk_max, p.piece, p.pieces, p.feature_tiles, p.ring, p.sums, r.blocks, r.chunk, r.chunks, r.all_pieces, r.lead, r.total};
+    *o = Out{p.blocks_max, p.chunk_max, p.tile, p.piece, p.pieces, p.feature_tiles, p.ring, p.sums, r.blocks, r.chunk, r.chunks, r.all_pieces, r.lead, r.total};
 }
 extern "C" void items(int T, int V, int D, int grad, int rows, long long n, int* out) {
     const HeadPlan p = head_plan(T, V, D, grad);
@@ -41,7 +41,7 @@ def lib(tmp_path_factory):
 
 
 class Out(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_int) for n in "blocks_max chunk_max piece pieces features ring sums blocks chunk chunks all_pieces lead".split()] + [("total", ctypes.c_longlong)]
+    _fields_ = [(n, ctypes.c_int) for n in "blocks_max chunk_max tile piece pieces features ring sums blocks chunk chunks all_pieces lead".split()] + [("total", ctypes.c_longlong)]
 
 
 SHAPES = [(T, V, D, rows) for T, rows in ((1, 1), (16, 9), (256, 256), (257, 257), (600, 600), (2048, 2048), (2049, 2049), (2305, 2048), (2305, 17), (8192, 8192), (5000, 4100), (9000, 0))
@@ -58,9 +58,9 @@ def test_every_tile_once_and_in_an_order_without_circles(lib, T, V, D, rows, gra
     lib.items(T, V, D, grad, rows, ctypes.c_longlong(o.total), flat)
     items = [tuple(flat[6 * i:6 * i + 6]) for i in range(o.total)]
     entries = lambda piece: min(o.piece, V - piece * o.piece)  # noqa: E731
-    real = [it for it in items if it[4] < o.blocks and (it[0] or it[5] * 256 < entries(it[2]))]
+    real = [it for it in items if it[4] < o.blocks and (it[0] or it[5] * o.tile < entries(it[2]))]
     logits, grads = [it for it in real if not it[0]], [it for it in real if it[0]]
-    assert sorted((it[4], it[2] * (o.piece // 256) + it[5]) for it in logits) == [(b, t) for b in range(o.blocks) for t in range(-(-V // 256))]
+    assert sorted((it[4], it[2] * (o.piece // o.tile) + it[5]) for it in logits) == [(b, t) for b in range(o.blocks) for t in range(-(-V // o.tile))]
     if not grad:
         assert not grads
         return
