@@ -203,7 +203,7 @@ typedef struct {
 int qlora_adapters_workspace_bytes(const qlora_adapters_desc* desc, int M, size_t* out);
 
 /* X bf16 [M, K]; adapter_of int32 [M]; A bf16 [n_adapters, r, K]; B bf16 [n_adapters, N, r]; scales fp32 [n_adapters] (alpha / r of
- * each).  Y_base, Y: bf16 [M, N]; Y may be Y_base, any other overlap of the two is refused.  H_out: fp32 [M, r] or NULL; rows of tokens without an adapter are 0.
+ * each).  Y_base, Y: bf16 [M, N]; Y may be Y_base; any other overlap of the two is refused, and so is one of Y with X.  H_out: fp32 [M, r] or NULL; rows of tokens without an adapter are 0.
  * A token without an adapter has Y = Y_base bit for bit; what an adapter holds reaches its own tokens only.  Any order of tokens is right; with
  * many tokens those of one adapter should lie together, as the rows of one request do, or its matrices are read for each of their places.
  * adapter_of and scales may begin at any element.  Sums are fp32; s P enters the second product as two bf16 (16 bits), or in fp32 with up to 256 tokens. */
@@ -240,8 +240,8 @@ int qlora_lrec_loss(int T, int V, const void* student_logits, const void* teache
  * hidden bf16 [T, D]; head bf16 [V, D]; labels int32 [T]: a token whose label is outside [0, V) has loss 0 and gradient 0 and costs nothing (padding, the
  * tokens of a prompt); d_loss fp32 [T]: the upstream gradient of every token's loss (1 / n for the mean of n), with d_hidden bf16 [T, D]; both NULL: the loss
  * alone.  labels, d_loss and loss_tokens may begin at any element.  d_hidden may be hidden itself; any other overlap of the two is refused.  D: a multiple of 8, 64 at least;
- * V up to 2^24.  workspace: qlora_head_loss_workspace_bytes(T, V, D, gradient), of which the part that grows with V is 64 MB at most or three pieces of
- * the vocabulary for 2048 tokens, and 8 bytes for every token and 256 entries.
+ * V up to 2^24.  workspace: qlora_head_loss_workspace_bytes(T, V, D, gradient), of which the part that grows with V is 50 MB at most
+ * and 8 bytes for every token and 256 entries.
  * Sums, maxima and losses are fp32 (a token that is almost certain keeps its small loss and gradient); probabilities are rounded to bf16 where they
  * enter the gradient's product.  The logits may be of any size; a block of 256 tokens is computed twice where one of them has a logit more than 83 above
  * the largest of its first 256.  A token with a NaN or infinity among its logits has loss and gradient NaN. */

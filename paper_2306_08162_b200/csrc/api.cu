@@ -49,6 +49,11 @@ int check_logits(int T, int V, long long row_stride, int dtype, float inv_temper
     return QLORA_OK;
 }
 
+bool overlap(const void* a, size_t bytes_a, const void* b, size_t bytes_b) {
+    const uintptr_t pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
+    return pa < pb + bytes_b && pb < pa + bytes_a;
+}
+
 // Whether two [T, V] tensors of rows that lie apart share memory.  (Different strides in the same stretch of memory: taken to.)
 bool rows_overlap(const void* a, long long stride_a, const void* b, long long stride_b, int T, int V, size_t bytes) {
     typedef __int128 wide;                                            // (any stride that fits a long long)
@@ -269,6 +274,7 @@ static int adapters_common(bool forward, const qlora_adapters_desc* desc, int M,
     if (M == 0 || C == 0) return QLORA_OK;
     if ((!In && T > 0) || !adapter_of || (d.n_adapters > 0 && (!A || !B || !scales)) || !Base || !Out) return QLORA_ERR_INVALID_ARG;
     if (Base != Out && rows_overlap(Base, C, Out, C, M, C, 2)) return QLORA_ERR_INVALID_ARG;
+    if (In != nullptr && overlap(In, (size_t)M * T * 2, Out, (size_t)M * C * 2)) return QLORA_ERR_INVALID_ARG;
     if (!aligned16(In) || !aligned4(adapter_of) || !aligned16(A) || !aligned16(B) || !aligned4(scales) || !aligned16(Base) || !aligned16(Out) ||
         !aligned16(low) || !aligned16(workspace))
         return QLORA_ERR_ALIGNMENT;

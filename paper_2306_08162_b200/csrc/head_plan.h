@@ -57,13 +57,13 @@ inline HeadPlan head_plan(int T, int V, int D, int grad) {
         }
     }
     cut(best);
-    // 64 MB of probabilities (what stays in L2), three pieces at least: one being read, one written, one between
+    // 48 MB of probabilities (what stays in L2), three pieces at least: one being read, one written, one between
     const long long slot = 2ll * p.chunk_max * kHeadTile * p.piece;
-    const long long fit = (64ll << 20) / slot;
+    const long long fit = (48ll << 20) / slot;
     const int most = p.pieces * head_div_up(p.blocks_max, kHeadChunk);
     p.ring = fit < 3 ? 3 : fit < most ? (int)fit : most;
     // as many sets of sums as there are pieces under way at a time where there are few tiles
-    p.sums = tiles >= 2 * kHeadPairs ? 1 : head_div_up(2 * kHeadPairs, tiles);
+    p.sums = tiles >= 128 ? 1 : head_div_up(128, tiles);
     if (p.sums > p.pieces) p.sums = p.pieces;
     return p;
 }

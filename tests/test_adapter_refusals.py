@@ -55,6 +55,7 @@ def test_products_arguments(ql, name):
         assert status(**{off: OK + 8}) == -3
     assert status(out=16 * OK + 8) == -3 and status(ids=OK + 2) == -3 and status(s=OK + 1) == -3
     assert status(out=OK + 16) == -1 and status(base=OK + 16, out=OK) == -1        # they overlap
+    assert status(X=32 * OK, base=32 * OK + 64, out=32 * OK + 64) == -1             # the input is overwritten
     assert status(ws=None) == -4 and status(size=100) == -4
     assert status(M=0, X=None) == 0                                                # nothing to do
 
