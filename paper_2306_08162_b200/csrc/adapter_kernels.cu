@@ -851,17 +851,17 @@ adapters_up_kernel(const Products p, int tiles_each) {
 // memory, rows of other adapters as zeros, and their sums are added in the order of the warps.  The block that finishes an adapter's last chunk of a
 // slice adds the chunks in their order.
 //
-// Both operands are transposed on the way out of shared memory.  G and H are taken as two bf16 each (made once, not by every slice), one product after the
-// other into the same sums.  Where a sum is not finite the low parts have nothing to say, but may have made a NaN of an infinity: the task is
-// then done again without them.
-constexpr int GR_WARPS = 4, GR_STAGES = 3, GR_BLOCKS = 3, GR_MIN_TILES = 32;
+// Both operands are transposed on the way out of shared memory.  G and H are taken as three bf16 each, which hold all of an fp32 value (made once, not by every
+// slice; with two the gradients were 2.5e-6 off, with three 5e-7), one product after the other into the same sums.  Where a sum is not finite the lower parts
+// have nothing to say, but may have made a NaN of an infinity: the task is then done again without them.
+constexpr int GR_PARTS = 3, GR_WARPS = 4, GR_STAGES = 3, GR_BLOCKS = 3, GR_MIN_TILES = 32;
 
 struct Grads {
     int M, K, N, r, n_adapters;
     const bf16 *X, *dY;                      // [M, K], [M, N]
     const int32_t* adapter_of;
     const float* scales;
-    const bf16 *G, *H;                       // [2][M, r]: high parts, low parts
+    const bf16 *G, *H;                       // [GR_PARTS][M, r]: from the highest parts down
     float *dA, *dB;
     int accumulate;
     int slices_x, slices, rank_blocks;
@@ -873,7 +873,7 @@ struct Grads {
     float* partial;                          // [2 most_chunks][slices * rank_blocks][16 MT][columns]
 };
 
-// Block 0: entries and chunks, and the counters set to zero.  The others: G and H in two parts.
+// Block 0: entries and chunks, and the counters set to zero.  The others: G and H in parts.
 constexpr int GP_THREADS = 1024, GP_ROUNDS = 8;
 __global__ void __launch_bounds__(GP_THREADS)
 adapters_grad_plan_kernel(const Grads p, const float* __restrict__ G, const float* __restrict__ H, uint32_t* __restrict__ g, uint32_t* __restrict__ h, int n_counters) {
@@ -884,12 +884,21 @@ adapters_grad_plan_kernel(const Grads p, const float* __restrict__ G, const floa
     if (blockIdx.x > 0) {
         const long long n = (long long)p.M * p.r, at = (long long)(blockIdx.x - 1) * GP_THREADS + threadIdx.x;
         if (2 * at >= n) return;
-        const float2 vg = __ldcg(reinterpret_cast<const float2*>(G) + at), vh = __ldcg(reinterpret_cast<const float2*>(H) + at);
-        const Split sg = split_bf16(vg.x, vg.y), sh = split_bf16(vh.x, vh.y);
-        g[at] = sg.hi;
-        g[n / 2 + at] = sg.lo;
-        h[at] = sh.hi;
-        h[n / 2 + at] = sh.lo;
+        const float2 v[2] = {__ldcg(reinterpret_cast<const float2*>(G) + at), __ldcg(reinterpret_cast<const float2*>(H) + at)};
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            uint32_t* to = k ? h : g;
+            float x = v[k].x, y = v[k].y;
+#pragma unroll
+            for (int i = 0; i < GR_PARTS; ++i) {
+                const uint32_t w = bf16x2(x, y);
+                to[i * (n / 2) + at] = w;
+                x -= bf16_lo(w);                                       // (nothing is left of what is not finite)
+                y -= bf16_hi(w);
+                x = fabsf(x) < INFINITY ? x : 0.f;
+                y = fabsf(y) < INFINITY ? y : 0.f;
+            }
+        }
         return;
     }
     for (int i = threadIdx.x; i < n_counters; i += GP_THREADS) p.counters[i] = 0u;
@@ -970,7 +979,7 @@ adapters_grad_plan_kernel(const Grads p, const float* __restrict__ G, const floa
 template <int MT>
 struct GradTile {
     static constexpr int COLS = MT == 1 ? 128 : 64, RANKS = 16 * MT, PITCH = COLS + 4;    // PITCH: of the sums in shared memory
-    static constexpr int V_BYTES = 16 * COLS * 2, P_BYTES = 16 * RANKS * 2, STAGE = V_BYTES + 2 * P_BYTES;
+    static constexpr int V_BYTES = 16 * COLS * 2, P_BYTES = 16 * RANKS * 2, STAGE = V_BYTES + GR_PARTS * P_BYTES;
     static constexpr size_t RING = (size_t)GR_WARPS * GR_STAGES * STAGE, SUMS = sizeof(float) * GR_WARPS * RANKS * PITCH;
     static constexpr size_t SMEM = RING > SUMS ? RING : SUMS;
 };
@@ -990,7 +999,7 @@ __device__ __forceinline__ void grad_task(const Grads& p, int task, int n_entrie
     const int C = of_x ? p.K : p.N, c0 = (of_x ? slice : slice - p.slices_x) * COLS, M = p.M, r = p.r;
     const bf16 *V = of_x ? p.X : p.dY, *P = of_x ? p.G : p.H;
     const uint32_t ring = smem_u32(smem) + warp * GR_STAGES * Tile::STAGE;
-    // what a lane copies: a 16-byte piece of every PER-th row of V, and pieces of both parts of P.  Pieces are XORed by row.
+    // what a lane copies: a 16-byte piece of every PER-th row of V, and pieces of all parts of P.  Pieces are XORed by row.
     constexpr int PIECES = COLS / 8, PER = 32 / PIECES, P_PIECES = RANKS / 8;
     const int v_row = lane / PIECES, v_piece = lane % PIECES;
     const bool v_in = c0 + 8 * v_piece < C;
@@ -1052,17 +1061,12 @@ __device__ __forceinline__ void grad_task(const Grads& p, int task, int n_entrie
                 const bf16* low = P + (size_t)(t0 + p_row) * r + (p_in ? j0 + 8 * p_piece : 0);
                 const bool in = p_in && ((entry >> p_row) & 1u);
                 const uint32_t p_to = to + Tile::V_BYTES + p_row * (RANKS * 2) + ((p_piece ^ (p_row * P_PIECES / 8 % P_PIECES)) << 4);
-                if constexpr (P_PIECES == 2) {                         // 32 pieces in each part
-                    copy16(p_to, in ? low : P, in);
-                    copy16(p_to + Tile::P_BYTES, in ? low + (size_t)M * r : P, in);
-                } else {                                               // 64: eight rows further on as well
-                    const bool in8 = p_in && ((entry >> (p_row + 8)) & 1u);
-                    const uint32_t p_to8 = p_to + 8 * (RANKS * 2);     // (the same XOR: 8 rows of 64 bytes on)
+                // (a part is 32 pieces, or 64: then eight rows further on as well, with the same XOR)
+                const bool in8 = p_in && ((entry >> ((p_row + 8) & 31)) & 1u);
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        copy16(p_to + half * Tile::P_BYTES, in ? low + (size_t)half * M * r : P, in);
-                        copy16(p_to8 + half * Tile::P_BYTES, in8 ? low + ((size_t)half * M + 8) * r : P, in8);
-                    }
+                for (int k = 0; k < GR_PARTS; ++k) {
+                    copy16(p_to + k * Tile::P_BYTES, in ? low + (size_t)k * M * r : P, in);
+                    if constexpr (P_PIECES == 4) copy16(p_to + k * Tile::P_BYTES + 8 * (RANKS * 2), in8 ? low + ((size_t)k * M + 8) * r : P, in8);
                 }
             };
 #pragma unroll
@@ -1079,9 +1083,9 @@ __device__ __forceinline__ void grad_task(const Grads& p, int task, int n_entrie
                 if (i + GR_STAGES - 1 < mine) load(i + GR_STAGES - 1);
                 copy_commit();
                 const uint32_t v = ring + (i % GR_STAGES) * Tile::STAGE, pp = v + Tile::V_BYTES;
-                uint32_t a[2][MT][4];
+                uint32_t a[GR_PARTS][MT][4];
 #pragma unroll
-                for (int half = 0; half < 2; ++half)
+                for (int half = 0; half < GR_PARTS; ++half)
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt) {                  // ranks 0 - 7, 8 - 15 of tokens 0 - 7; then of 8 - 15
                         const int piece = 2 * mt + (quarter & 1);
@@ -1097,8 +1101,11 @@ __device__ __forceinline__ void grad_task(const Grads& p, int task, int n_entrie
                         mma_bf16_16816(acc[mt][t], a[0][mt][0], a[0][mt][1], a[0][mt][2], a[0][mt][3], b[0], b[1]);
                         mma_bf16_16816(acc[mt][t + 1], a[0][mt][0], a[0][mt][1], a[0][mt][2], a[0][mt][3], b[2], b[3]);
                         if (low_parts) {
-                            mma_bf16_16816(acc[mt][t], a[1][mt][0], a[1][mt][1], a[1][mt][2], a[1][mt][3], b[0], b[1]);
-                            mma_bf16_16816(acc[mt][t + 1], a[1][mt][0], a[1][mt][1], a[1][mt][2], a[1][mt][3], b[2], b[3]);
+#pragma unroll
+                            for (int k = 1; k < GR_PARTS; ++k) {
+                                mma_bf16_16816(acc[mt][t], a[k][mt][0], a[k][mt][1], a[k][mt][2], a[k][mt][3], b[0], b[1]);
+                                mma_bf16_16816(acc[mt][t + 1], a[k][mt][0], a[k][mt][1], a[k][mt][2], a[k][mt][3], b[2], b[3]);
+                            }
                         }
                     }
                 }
@@ -1279,8 +1286,8 @@ GradScratch grad_scratch(const Grads& p) {
     GradScratch s;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
-    s.g = take((size_t)p.M * p.r * 4);
-    s.h = take((size_t)p.M * p.r * 4);
+    s.g = take((size_t)GR_PARTS * p.M * p.r * 2);
+    s.h = take((size_t)GR_PARTS * p.M * p.r * 2);
     s.counters = take(4 * (4 + several * blocks));
     s.entries = take((size_t)p.M * sizeof(uint2));
     s.counts = take((size_t)p.n_adapters * 4);
