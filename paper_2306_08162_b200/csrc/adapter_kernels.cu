@@ -869,7 +869,7 @@ struct Grads {
     unsigned* counters;                      // [0] claimed, [1] entries, [2] tiles of a chunk, [3] chunks; [4 ..] chunks done, by first chunk of an adapter of several and slice
     uint2* entries;                          // [M]: adapter, tile << 16 | mask (tile < 65536: up to 2^20 tokens)
     int* counts;                             // [n_adapters]: entries
-    int4* chunks;                            // [n_adapters + 2 most_chunks]: adapter, part, parts, place of the adapter's first part among those of several
+    int4* chunks;                            // [n_adapters + 2 most_chunks]: adapter, part, parts (0: no token), place of the adapter's first part among those of several
     float* partial;                          // [2 most_chunks][slices * rank_blocks][16 MT][columns]
 };
 
@@ -955,7 +955,8 @@ adapters_grad_plan_kernel(const Grads p, const float* __restrict__ G, const floa
     int n_chunks = 0, n_several = 0;
     for (int a0 = 0; a0 < p.n_adapters; a0 += GP_THREADS) {
         const int a = a0 + threadIdx.x;
-        const int n = a < p.n_adapters ? max(1, (*(volatile int*)(p.counts + a) + tiles - 1) / tiles) : 0, several = n > 1 ? n : 0;   // (one without tokens has a chunk that writes its zeros)
+        const int count = a < p.n_adapters ? *(volatile int*)(p.counts + a) : 0;
+        const int n = a < p.n_adapters ? max(1, (count + tiles - 1) / tiles) : 0, several = n > 1 ? n : 0;   // (one without tokens has a chunk that writes its zeros)
         int before = n, before_several = several;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -970,7 +971,7 @@ adapters_grad_plan_kernel(const Grads p, const float* __restrict__ G, const floa
             n_chunks += parts_s[w];
             n_several += several_s[w];
         }
-        for (int i = 0; i < n; ++i) p.chunks[at + i] = make_int4(a, i, n, at_several);
+        for (int i = 0; i < n; ++i) p.chunks[at + i] = make_int4(a, i, count > 0 ? n : 0, at_several);
         __syncthreads();
     }
     if (threadIdx.x == 0) { p.counters[1] = (unsigned)n_entries; p.counters[2] = (unsigned)tiles; p.counters[3] = (unsigned)n_chunks; }
@@ -1005,9 +1006,18 @@ __device__ __forceinline__ void grad_task(const Grads& p, int task, int n_entrie
     const bool v_in = c0 + 8 * v_piece < C;
     const int p_row = lane / P_PIECES % 16, p_piece = lane % P_PIECES;
     const bool p_in = j0 + 8 * p_piece < r;
+    if (parts == 0) {                                                  // an adapter without tokens
+        if (p.accumulate) return;
+        for (int quad = threadIdx.x; quad < RANKS * COLS / 4; quad += 32 * GR_WARPS) {
+            const int j = of_x ? quad / (COLS / 4) : 4 * (quad % (RANKS / 4)), c = of_x ? 4 * (quad % (COLS / 4)) : quad / (RANKS / 4);
+            if (j0 + j < r && c0 + c < C)
+                *reinterpret_cast<float4*>(of_x ? p.dA + ((size_t)adapter * r + j0 + j) * p.K + c0 + c : p.dB + ((size_t)adapter * p.N + c0 + c) * r + j0 + j) =
+                    make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        return;
+    }
     const int lo = part * chunk_tiles, hi = lo + chunk_tiles;          // of the adapter's entries
     float acc[MT][CT][4];
-    bool any = false;
     for (int low_parts = 1; low_parts >= 0; --low_parts) {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
@@ -1045,7 +1055,6 @@ __device__ __forceinline__ void grad_task(const Grads& p, int task, int n_entrie
                 e0 += GR_READ * GR_WARPS * 32;
                 __syncthreads();
             }
-            any |= total > 0;
             const int mine = warp < total ? (total - warp + GR_WARPS - 1) / GR_WARPS : 0;
             auto load = [&](int i) {
                 const uint32_t to = ring + (i % GR_STAGES) * Tile::STAGE, entry = list[warp + i * GR_WARPS];
@@ -1122,7 +1131,6 @@ __device__ __forceinline__ void grad_task(const Grads& p, int task, int n_entrie
                 for (int k = 0; k < 4; ++k) worst += acc[mt][t][k] - acc[mt][t][k];
         if (!__syncthreads_or(worst != 0.f)) break;
     }
-    if (!any && p.accumulate) return;                                  // (the same for the whole block; an adapter without tokens has one chunk)
     // [mt][t][c]: rank 16 mt + g (+ 8 where c >= 2), column 8 t + 2 q + c % 2
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
@@ -1191,7 +1199,7 @@ __device__ __forceinline__ void grad_task(const Grads& p, int task, int n_entrie
         place(threadIdx.x + i * 32 * GR_WARPS, j, c);
         if (j0 + j >= r || c0 + c >= C) continue;                      // (four are inside or outside together)
         float4* dst = reinterpret_cast<float4*>(of_x ? p.dA + ((size_t)adapter * r + j0 + j) * p.K + c0 + c : p.dB + ((size_t)adapter * p.N + c0 + c) * r + j0 + j);
-        float4 x = any ? make_float4(s * v[i].x, s * v[i].y, s * v[i].z, s * v[i].w) : make_float4(0.f, 0.f, 0.f, 0.f);
+        float4 x = make_float4(s * v[i].x, s * v[i].y, s * v[i].z, s * v[i].w);
         if (p.accumulate) {
             const float4 old = *dst;
             x.x += old.x; x.y += old.y; x.z += old.z; x.w += old.w;
