@@ -192,8 +192,8 @@ int qlora_unpack(int bits, int K, int N, const int32_t* Q, uint8_t* codes, void*
  *     dA_a  = scales[a] sum G[t]^T X[t]       dB_a  = scales[a] sum dY[t]^T H[t]        (sums over the tokens of a)
  * Y_base and dX_base are what the shared projection gives, e.g. qlora_fwd and qlora_bwd_input with r = 0. */
 typedef struct {
-    int K;          /* input features */
-    int N;          /* output features */
+    int K;          /* input features, a multiple of 32 */
+    int N;          /* output features, a multiple of 8 */
     int r;          /* rank, 8 .. 64 in steps of 8; adapters of lower ranks are held with rows of A and columns of B that are zero */
     int n_adapters; /* at most 65535 */
 } qlora_adapters_desc;
@@ -203,10 +203,12 @@ typedef struct {
 int qlora_adapters_workspace_bytes(const qlora_adapters_desc* desc, int M, size_t* out);
 
 /* X bf16 [M, K]; adapter_of int32 [M]; A bf16 [n_adapters, r, K]; B bf16 [n_adapters, N, r]; scales fp32 [n_adapters] (alpha / r of
- * each).  Y_base, Y: bf16 [M, N]; Y may be Y_base; any other overlap of the two is refused, and so is one of Y with X.  H_out: fp32 [M, r] or NULL; rows of tokens without an adapter are 0.
+ * each).  Y_base, Y: bf16 [M, N]; Y may be Y_base; any other overlap of the two is refused, and so is one of Y with X.  H_out: fp32 [M, r] or NULL;
+ * rows of tokens without an adapter are 0.
  * A token without an adapter has Y = Y_base bit for bit; what an adapter holds reaches its own tokens only.  Any order of tokens is right; with
  * many tokens those of one adapter should lie together, as the rows of one request do, or its matrices are read for each of their places.
- * adapter_of and scales may begin at any element.  Sums are fp32; s P enters the second product as two bf16 (16 bits), or in fp32 with up to 256 tokens. */
+ * adapter_of and scales may begin at any element.  Sums are fp32; s H enters the second product as two bf16 (16 bits), or in fp32 with up to 256 tokens and
+ * where the tokens of three or more adapters lie mixed. */
 int qlora_adapters_fwd(const qlora_adapters_desc* desc, int M, const void* X, const int32_t* adapter_of, const void* A, const void* B, const float* scales,
                        const void* Y_base, void* Y, float* H_out, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
@@ -215,7 +217,8 @@ int qlora_adapters_bwd_input(const qlora_adapters_desc* desc, int M, const void*
                              const float* scales, const void* dX_base, void* dX, float* G_out, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /* dA fp32 [n_adapters, r, K], dB fp32 [n_adapters, N, r].  H, G: what the two calls above have left, or NULL to recompute them here (A, B are
- * needed for that only).  accumulate = 0 overwrites dA and dB, with zeros for an adapter without tokens; 1 adds to them. */
+ * needed for that only); as three bf16 each they enter the products, which is all of an fp32 value.  accumulate = 0 overwrites dA and dB, with zeros
+ * for an adapter without tokens; 1 adds to them. */
 int qlora_adapters_bwd_lora(const qlora_adapters_desc* desc, int M, const void* X, const void* dY, const int32_t* adapter_of, const void* A, const void* B,
                             const float* scales, const float* H, const float* G, float* dA, float* dB, int accumulate, void* workspace,
                             size_t workspace_bytes, void* cuda_stream);
@@ -239,9 +242,9 @@ int qlora_lrec_loss(int T, int V, const void* student_logits, const void* teache
  * The head is frozen, as every weight of the base (Section 3.1): it has no gradient.
  * hidden bf16 [T, D]; head bf16 [V, D]; labels int32 [T]: a token whose label is outside [0, V) has loss 0 and gradient 0 and costs nothing (padding, the
  * tokens of a prompt); d_loss fp32 [T]: the upstream gradient of every token's loss (1 / n for the mean of n), with d_hidden bf16 [T, D]; both NULL: the loss
- * alone.  labels, d_loss and loss_tokens may begin at any element.  d_hidden may be hidden itself; any other overlap of the two is refused.  D: a multiple of 8, 64 at least;
- * V up to 2^24.  workspace: qlora_head_loss_workspace_bytes(T, V, D, gradient), of which the part that grows with V is 50 MB at most
- * and 8 bytes for every token and 256 entries.
+ * alone.  labels, d_loss and loss_tokens may begin at any element; the latter two may not overlap.  d_hidden may be hidden itself; any other overlap of the
+ * two is refused.  D: a multiple of 8, 64 to 2^20; T and V up to 2^24, T (V + D) up to about 2^43.
+ * workspace: qlora_head_loss_workspace_bytes(T, V, D, gradient), of which the part that grows with V is 50 MB at most and 8 bytes for every token and 256 entries.
  * Sums, maxima and losses are fp32 (a token that is almost certain keeps its small loss and gradient); probabilities are rounded to bf16 where they
  * enter the gradient's product.  The logits may be of any size; a block of 256 tokens is computed twice where one of them has a logit more than 83 above
  * the largest of its first 256.  A token with a NaN or infinity among its logits has loss and gradient NaN. */

@@ -93,7 +93,7 @@ int check_adamw(const qlora_adamw_desc* d, bool step) {
 
 int check_adapters(const qlora_adapters_desc* d, int M) {
     if (d == nullptr || d->K < 0 || d->N < 0 || d->r < 0 || d->n_adapters < 0) return QLORA_ERR_INVALID_ARG;
-    if (d->K % 32 != 0 || d->N % 8 != 0 || d->r % 8 != 0 || d->r == 0 || d->r > 64 || d->n_adapters > 65535) return QLORA_ERR_UNSUPPORTED;
+    if (d->K == 0 || d->K % 32 != 0 || d->N == 0 || d->N % 8 != 0 || d->r % 8 != 0 || d->r == 0 || d->r > 64 || d->n_adapters > 65535) return QLORA_ERR_UNSUPPORTED;
     if (M < 0) return QLORA_ERR_INVALID_ARG;
     return M > (1 << 20) ? QLORA_ERR_UNSUPPORTED : QLORA_OK;
 }
@@ -271,10 +271,10 @@ static int adapters_common(bool forward, const qlora_adapters_desc* desc, int M,
     if (rc != QLORA_OK) return rc;
     const qlora_adapters_desc& d = *desc;
     const int T = forward ? d.K : d.N, C = forward ? d.N : d.K;
-    if (M == 0 || C == 0) return QLORA_OK;
-    if ((!In && T > 0) || !adapter_of || (d.n_adapters > 0 && (!A || !B || !scales)) || !Base || !Out) return QLORA_ERR_INVALID_ARG;
+    if (M == 0) return QLORA_OK;
+    if (!In || !adapter_of || (d.n_adapters > 0 && (!A || !B || !scales)) || !Base || !Out) return QLORA_ERR_INVALID_ARG;
     if (Base != Out && rows_overlap(Base, C, Out, C, M, C, 2)) return QLORA_ERR_INVALID_ARG;
-    if (In != nullptr && overlap(In, (size_t)M * T * 2, Out, (size_t)M * C * 2)) return QLORA_ERR_INVALID_ARG;
+    if (overlap(In, (size_t)M * T * 2, Out, (size_t)M * C * 2)) return QLORA_ERR_INVALID_ARG;
     if (!aligned16(In) || !aligned4(adapter_of) || !aligned16(A) || !aligned16(B) || !aligned4(scales) || !aligned16(Base) || !aligned16(Out) ||
         !aligned16(low) || !aligned16(workspace))
         return QLORA_ERR_ALIGNMENT;
@@ -300,9 +300,9 @@ int qlora_adapters_bwd_lora(const qlora_adapters_desc* desc, int M, const void* 
     if (rc != QLORA_OK) return rc;
     if (accumulate != 0 && accumulate != 1) return QLORA_ERR_INVALID_ARG;
     const qlora_adapters_desc& d = *desc;
-    if (d.n_adapters == 0 || (d.K == 0 && d.N == 0)) return QLORA_OK;
-    if ((!dA && d.K > 0) || (!dB && d.N > 0) || !scales) return QLORA_ERR_INVALID_ARG;
-    if (M > 0 && ((!X && d.K > 0) || (!dY && d.N > 0) || !adapter_of || (!H && !A) || (!G && !B))) return QLORA_ERR_INVALID_ARG;
+    if (d.n_adapters == 0) return QLORA_OK;
+    if (!dA || !dB || !scales) return QLORA_ERR_INVALID_ARG;
+    if (M > 0 && (!X || !dY || !adapter_of || (!H && !A) || (!G && !B))) return QLORA_ERR_INVALID_ARG;
     if (!aligned16(X) || !aligned16(dY) || !aligned4(adapter_of) || !aligned16(A) || !aligned16(B) || !aligned4(scales) || !aligned16(H) || !aligned16(G) ||
         !aligned16(dA) || !aligned16(dB) || !aligned16(workspace))
         return QLORA_ERR_ALIGNMENT;
@@ -326,7 +326,7 @@ int qlora_adapters_bwd_lora(const qlora_adapters_desc* desc, int M, const void* 
 
 static int check_head(int T, int V, int D) {
     if (T < 0 || V < 0 || D < 0) return QLORA_ERR_INVALID_ARG;
-    if (V == 0 || V > (1 << 24) || D < 64 || D % 8 != 0 || D > (1 << 20)) return QLORA_ERR_UNSUPPORTED;
+    if (T > (1 << 24) || V == 0 || V > (1 << 24) || D < 64 || D % 8 != 0 || D > (1 << 20)) return QLORA_ERR_UNSUPPORTED;
     if (((long long)T / 256 + 1) * ((long long)V / 256 + 1 + D / 256 + 1) > (1 << 28)) return QLORA_ERR_UNSUPPORTED;   // (items of work are counted in 32 bits)
     return QLORA_OK;
 }
@@ -348,6 +348,7 @@ int qlora_head_loss(int T, int V, int D, const void* hidden, const void* head, c
     if (d_hidden != nullptr && d_hidden != hidden && rows_overlap(hidden, D, d_hidden, D, T, D, 2)) return QLORA_ERR_INVALID_ARG;
     if (!aligned16(hidden) || !aligned16(head) || !aligned4(labels) || !aligned4(d_loss) || !aligned4(loss_tokens) || !aligned16(d_hidden) || !aligned16(workspace))
         return QLORA_ERR_ALIGNMENT;
+    if (d_loss != nullptr && overlap(d_loss, (size_t)T * 4, loss_tokens, (size_t)T * 4)) return QLORA_ERR_INVALID_ARG;
     if (workspace == nullptr || workspace_bytes < head_loss_workspace_bytes(T, V, D, d_hidden != nullptr)) return QLORA_ERR_WORKSPACE;
     return launch_head_loss(T, V, D, hidden, head, labels, d_loss, loss_tokens, d_hidden, workspace, (cudaStream_t)cuda_stream);
 }

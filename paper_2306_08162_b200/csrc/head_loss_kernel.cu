@@ -479,15 +479,16 @@ done:
 }
 
 // Tokens that have a label become rows, in their order: place[t] (-1 without), the rows' labels, and, unless every token has one, the hidden states side
-// by side.  A block takes 8 tokens, a warp each, and counts the labels itself: those before its tokens and all of them.  The counters are set to zero.
-constexpr int PREP_TOKENS = 8, PREP_THREADS = 32 * PREP_TOKENS;
+// by side.  A block takes 8 tokens at a time, a warp each, and counts the labels itself: those before its tokens and all of them.  The counters are set to zero.
+// Every block reads all the labels; with more than 16384 tokens it takes 8 several times, so that this does not grow as the square of the tokens.
+constexpr int PREP_TOKENS = 8, PREP_THREADS = 32 * PREP_TOKENS, PREP_BLOCKS = 2048;
 __global__ void __launch_bounds__(PREP_THREADS)
-head_prepare_kernel(int T, int V, int D, int copies, const int32_t* __restrict__ labels, const bf16* __restrict__ hidden, int* __restrict__ place,
+head_prepare_kernel(int T, int V, int D, int copies, int turns, const int32_t* __restrict__ labels, const bf16* __restrict__ hidden, int* __restrict__ place,
                     int* __restrict__ row_label, bf16* __restrict__ rows, unsigned* __restrict__ counters, size_t counter_words) {
     __shared__ int parts[2][PREP_TOKENS];
     pdl_launch_dependents();
     pdl_wait();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t0 = blockIdx.x * PREP_TOKENS, t = t0 + warp;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t0 = blockIdx.x * turns * PREP_TOKENS;
     for (size_t i = 1 + blockIdx.x * PREP_THREADS + threadIdx.x; i < counter_words; i += (size_t)gridDim.x * PREP_THREADS) counters[i] = 0u;
     int before = 0, after = 0;                                         // labels of tokens before this warp's, and of the others
     for (int i = threadIdx.x; i < T; i += PREP_THREADS) {
@@ -501,23 +502,28 @@ head_prepare_kernel(int T, int V, int D, int copies, const int32_t* __restrict__
         after += __shfl_xor_sync(0xFFFFFFFFu, after, o);
     }
     if (lane == 0) { parts[0][warp] = before; parts[1][warp] = after; }
-    const int label = lane < PREP_TOKENS && t0 + lane < T ? __ldg(labels + t0 + lane) : -1;
-    const uint32_t mask = __ballot_sync(0xFFFFFFFFu, (unsigned)label < (unsigned)V);
     __syncthreads();
     before = after = 0;
 #pragma unroll
     for (int w = 0; w < PREP_TOKENS; ++w) { before += parts[0][w]; after += parts[1][w]; }
-    const int all = before + after, at = (mask >> warp) & 1u ? before + __popc(mask & ((1u << warp) - 1u)) : -1;
-    if (lane == 0 && t < T) {
-        place[t] = at;
-        if (at >= 0) row_label[at] = __ldg(labels + t);
-        if (t == 0) counters[0] = (unsigned)all;
-    }
-    if (at < 0 || (all == T && !copies)) return;
-    const uint4* src = reinterpret_cast<const uint4*>(hidden + (size_t)t * D);
-    uint4* dst = reinterpret_cast<uint4*>(rows + (size_t)at * D);
+    const int all = before + after;
+    if (t0 == 0 && threadIdx.x == 0) counters[0] = (unsigned)all;
+    for (int turn = 0; turn < turns; ++turn) {
+        const int first = t0 + turn * PREP_TOKENS, t = first + warp;
+        const int label = lane < PREP_TOKENS && first + lane < T ? __ldg(labels + first + lane) : -1;
+        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, (unsigned)label < (unsigned)V);
+        const int at = (mask >> warp) & 1u ? before + __popc(mask & ((1u << warp) - 1u)) : -1, mine = __shfl_sync(0xFFFFFFFFu, label, warp);
+        before += __popc(mask);
+        if (lane == 0 && t < T) {
+            place[t] = at;
+            if (at >= 0) row_label[at] = mine;
+        }
+        if (at < 0 || (all == T && !copies)) continue;
+        const uint4* src = reinterpret_cast<const uint4*>(hidden + (size_t)t * D);
+        uint4* dst = reinterpret_cast<uint4*>(rows + (size_t)at * D);
 #pragma unroll 8
-    for (int c = lane; c < D / 8; c += 32) dst[c] = __ldg(src + c);
+        for (int c = lane; c < D / 8; c += 32) dst[c] = __ldg(src + c);
+    }
 }
 
 // One block per token: its loss from the tiles' sums, and its row of the gradient from the pieces' sums, which are asked for first.
@@ -672,7 +678,8 @@ static int head_loss_impl(int T, int V, int D, const void* hidden, const void* h
     static SmemLimit limit;
     auto kern = head_loss_kernel<GRAD>;
     if (!limit.raise(kern, HL_SMEM)) return QLORA_ERR_CUDA;
-    if (launch_pdl(head_prepare_kernel, dim3((T + PREP_TOKENS - 1) / PREP_TOKENS), dim3(PREP_THREADS), 0, st, 1, T, V, D, p.copies, labels, (const bf16*)hidden, place,
+    const int turns = (T + PREP_TOKENS * PREP_BLOCKS - 1) / (PREP_TOKENS * PREP_BLOCKS);
+    if (launch_pdl(head_prepare_kernel, dim3((T + turns * PREP_TOKENS - 1) / (turns * PREP_TOKENS)), dim3(PREP_THREADS), 0, st, 1, T, V, D, p.copies, turns, labels, (const bf16*)hidden, place,
                    const_cast<int*>(p.label), rows, p.counters, l.counter_words) != cudaSuccess)
         return QLORA_ERR_CUDA;
     const long long items = head_rows(p.plan, T).total;

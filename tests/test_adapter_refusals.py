@@ -17,7 +17,7 @@ def ql():
     return mod
 
 
-BAD = [(dict(K=33), -2), (dict(N=12), -2), (dict(r=0), -2), (dict(r=12), -2), (dict(r=72), -2), (dict(n_adapters=65536), -2),
+BAD = [(dict(K=33), -2), (dict(K=0), -2), (dict(N=0), -2), (dict(N=12), -2), (dict(r=0), -2), (dict(r=12), -2), (dict(r=72), -2), (dict(n_adapters=65536), -2),
        (dict(K=-32), -1), (dict(N=-8), -1), (dict(r=-8), -1), (dict(n_adapters=-1), -1)]
 
 

@@ -256,3 +256,34 @@ def test_a_long_pool_of_adapters():
         Y = torch.empty_like(base)
         ql.qlora_adapters_fwd(d, M, X, ids, A, B, scales, base, Y, None, ws)
         assert (Y[0] == 64.0).all() and (Y[1] == 0).all() and (Y[2:] == 64.0).all()    # 64 x 64 / 64
+
+
+def test_as_many_tokens_as_there_may_be():
+    """2^20 tokens, whose hidden states begin beyond 2^32 elements: the last ones are right, and what the gradients sum up comes from all."""
+    M, K, N, r, L = 1 << 20, 4128, 8, 8, 3
+    d = ql.adapters_desc(K, N, r, L)
+    X, dY = torch.zeros((M, K), dtype=torch.bfloat16, device="cuda"), torch.zeros((M, N), dtype=torch.bfloat16, device="cuda")
+    X[:, 0], X[-40:] = 1.0, 0.5
+    dY[:, 1], dY[-40:] = 0.5, 1.0
+    A, B = (torch.full(s, 2.0 ** -9, dtype=torch.bfloat16, device="cuda") for s in ((L, r, K), (L, N, r)))
+    scales = torch.full((L,), 2.0, device="cuda")
+    ids = (torch.arange(M, device="cuda") // 1000 % L).int()
+    ids[-5:] = 1
+    ws = torch.empty(ql.qlora_adapters_workspace_bytes(d, M), dtype=torch.uint8, device="cuda")
+    Y, H, G = torch.zeros((M, N), dtype=torch.bfloat16, device="cuda"), torch.empty((M, r), device="cuda"), torch.empty((M, r), device="cuda")
+    ql.qlora_adapters_fwd(d, M, X, ids, A, B, scales, Y, Y, H, ws)
+    assert (H[:-40] == 2.0 ** -9).all() and (H[-40:] == K * 2.0 ** -10).all()
+    assert (Y[:-40] == 2.0 ** -14).all() and (Y[-40:] == torch.tensor(K * 2.0 ** -15).bfloat16().item()).all()
+    dX = torch.zeros((M, K), dtype=torch.bfloat16, device="cuda")
+    ql.qlora_adapters_bwd_input(d, M, dY, ids, A, B, scales, dX, dX, G, ws)
+    assert (G[:-40] == 2.0 ** -10).all() and (G[-40:] == 2.0 ** -6).all()
+    assert (dX[-40:] == 2.0 ** -11).all() and (dX[-1000:-40] == 2.0 ** -15).all() and (dX[::1001] >= 2.0 ** -15).all()
+    dA, dB = torch.empty((L, r, K), device="cuda"), torch.empty((L, N, r), device="cuda")
+    ql.qlora_adapters_bwd_lora(d, M, X, dY, ids, A, B, scales, H, G, dA, dB, 0, ws)
+    n, last = torch.bincount(ids, minlength=L).double(), torch.bincount(ids[-40:], minlength=L).double()
+    # every addition is off by 2^-23 of the sum at most (cut off rather than rounded), and there are M / 16 in a chain at most
+    near = lambda got, want: torch.testing.assert_close(got.double(), want.expand_as(got), rtol=2.0 ** -23 * M / 16, atol=0.0)  # noqa: E731
+    near(dA[:, :, 0], (2.0 * ((n - last) * 2.0 ** -10 + last * 2.0 ** -7))[:, None])
+    near(dA[:, :, 1:], (2.0 * last * 2.0 ** -7)[:, None, None])
+    near(dB[:, 1], (2.0 * ((n - last) * 2.0 ** -10 + last * K * 2.0 ** -10))[:, None])
+    near(dB[:, 2:], (2.0 * last * K * 2.0 ** -10)[:, None, None])

@@ -63,7 +63,8 @@ def check(hidden, head, labels, d_loss, loss, grad=None, rows=slice(None)):
 
 
 SIZES = [(1, 1, 64, 0.0), (1, 300, 64, 0.0), (3, 257, 72, 0.0), (16, 5000, 512, 0.2), (129, 4096, 200, 0.0), (256, 4097, 136, 0.0), (257, 9001, 256, 0.5),
-         (300, 12345, 328, 1.0), (700, 50021, 128, 0.33), (1500, 255, 1000, 0.1), (2049, 4100, 72, 0.0), (2500, 300, 64, 0.0), (5000, 9000, 64, 0.1), (2304, 12300, 264, 0.0)]
+         (300, 12345, 328, 1.0), (700, 50021, 128, 0.33), (1500, 255, 1000, 0.1), (2049, 4100, 72, 0.0), (2500, 300, 64, 0.0), (5000, 9000, 64, 0.1), (2304, 12300, 264, 0.0),
+         (70, 600, 8200, 0.0), (20000, 300, 72, 0.2)]
 
 
 @pytest.mark.parametrize("T,V,D,missing", SIZES)
@@ -249,3 +250,20 @@ def test_the_gradient_is_that_of_differences():
     middle = ((up.double() + down.double()) / 2 - hidden.double()).abs() @ head.double().abs().amax(0)
     rounding = 2 * HALF_BF16 * (grad.double().abs() * moved.abs()).sum(1) + 2 * HALF_BF16 * moved.abs().sum(1) * head.double().abs().amax()
     assert ((change - want).abs() <= reach ** 3 + 4 * reach * middle + rounding + 1e-5).all()
+
+
+@pytest.mark.parametrize("missing", [0.0, 0.4])
+def test_hidden_states_beyond_2_31_elements(missing):
+    T, V, D = 530000, 300, 4104
+    head = problem(1, V, D)[1]
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    hidden = torch.empty((T, D), dtype=torch.bfloat16, device="cuda")
+    for part in hidden.split(50000):
+        part.copy_(torch.randn(part.shape, device="cuda", generator=gen))
+    labels = torch.randint(0, V, (T,), device="cuda", generator=gen)
+    labels[torch.rand(T, device="cuda", generator=gen) < missing] = -1
+    labels, d_loss = labels.int(), torch.rand(T, device="cuda", generator=gen)
+    loss, grad = run(hidden, head, labels, d_loss)
+    assert ql.qlora_device_status() == 0
+    for rows in (slice(0, 40), slice(265000, 265040), slice(T - 400, T)):
+        check(hidden, head, labels, d_loss, loss, grad, rows)

@@ -18,7 +18,7 @@ def ql():
 
 
 BAD_SIZES = [(dict(T=-1), -1), (dict(V=-1), -1), (dict(D=-8), -1), (dict(V=0), -2), (dict(V=(1 << 24) + 1), -2), (dict(D=56), -2), (dict(D=100), -2),
-             (dict(D=(1 << 20) + 8), -2), (dict(T=1 << 30, V=1 << 24), -2)]
+             (dict(D=(1 << 20) + 8), -2), (dict(T=1 << 30, V=1 << 24), -2), (dict(T=(1 << 24) + 1), -2), (dict(T=2 ** 31 - 1, V=1), -2)]
 
 
 @pytest.mark.parametrize("change,status", BAD_SIZES)
@@ -46,6 +46,7 @@ def test_arguments(ql):
         assert status(**{missing: None}) == -1
     assert status(d_loss=OK) == -1 and status(d_hidden=64 * OK) == -1                # the gradient takes both
     assert status(d_loss=OK, d_hidden=OK + 16) == -1                                 # overlaps the hidden states
+    assert status(d_loss=OK + 8, d_hidden=64 * OK) == -1                             # overlaps the losses
     for off in ("hidden", "head", "ws"):
         assert status(**{off: OK + 8}) == -3
     assert status(d_loss=OK, d_hidden=64 * OK + 8) == -3
