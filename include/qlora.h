@@ -198,7 +198,7 @@ typedef struct {
     int n_adapters; /* at most 65535 */
 } qlora_adapters_desc;
 
-/* Bytes of scratch for M tokens (2^20 at most), for all three calls.  The first two need 4 M r + M / 4 + 8 of them; the gradients
+/* Bytes of scratch for M tokens (2^20 at most), for all three calls.  The first two need 4 M r + 12 M + 8 of them; the gradients
  * take most: up to 32 sums of every 2048 elements of an adapter's gradients. */
 int qlora_adapters_workspace_bytes(const qlora_adapters_desc* desc, int M, size_t* out);
 
@@ -206,9 +206,8 @@ int qlora_adapters_workspace_bytes(const qlora_adapters_desc* desc, int M, size_
  * each).  Y_base, Y: bf16 [M, N]; Y may be Y_base; any other overlap of the two is refused, and so is one of Y with X.  H_out: fp32 [M, r] or NULL;
  * rows of tokens without an adapter are 0.
  * A token without an adapter has Y = Y_base bit for bit; what an adapter holds reaches its own tokens only.  Any order of tokens is right; with
- * many tokens those of one adapter should lie together, as the rows of one request do, or its matrices are read for each of their places.
- * adapter_of and scales may begin at any element.  Sums are fp32; s H enters the second product as two bf16 (16 bits), or in fp32 with up to 256 tokens and
- * where the tokens of three or more adapters lie mixed. */
+ * many tokens those of one adapter should lie together, as the rows of one request do: where three or more adapters share 16 tokens these are sorted first.
+ * adapter_of and scales may begin at any element.  Sums are fp32; s H enters the second product with 16 bits (as two bf16), or with all 24 where there are few tokens. */
 int qlora_adapters_fwd(const qlora_adapters_desc* desc, int M, const void* X, const int32_t* adapter_of, const void* A, const void* B, const float* scales,
                        const void* Y_base, void* Y, float* H_out, void* workspace, size_t workspace_bytes, void* cuda_stream);
 

@@ -308,20 +308,20 @@ int qlora_adapters_bwd_lora(const qlora_adapters_desc* desc, int M, const void* 
         return QLORA_ERR_ALIGNMENT;
     if (workspace == nullptr || workspace_bytes < adapters_bytes(d, M)) return QLORA_ERR_WORKSPACE;
     cudaStream_t st = (cudaStream_t)cuda_stream;
+    void* scratch = static_cast<char*>(workspace) + 2 * adapters_low_bytes(d, M);   // (the gradients' is the larger)
     if (M > 0 && !H) {
         float* Hs = static_cast<float*>(workspace);
-        rc = launch_adapters(true, M, d.K, 0, d.r, d.n_adapters, X, adapter_of, A, nullptr, scales, nullptr, nullptr, Hs, nullptr, st);
+        rc = launch_adapters(true, M, d.K, 0, d.r, d.n_adapters, X, adapter_of, A, nullptr, scales, nullptr, nullptr, Hs, scratch, st);
         if (rc != QLORA_OK) return rc;
         H = Hs;
     }
     if (M > 0 && !G) {
         float* Gs = reinterpret_cast<float*>(static_cast<char*>(workspace) + adapters_low_bytes(d, M));
-        rc = launch_adapters(false, M, d.N, 0, d.r, d.n_adapters, dY, adapter_of, B, nullptr, scales, nullptr, nullptr, Gs, nullptr, st);
+        rc = launch_adapters(false, M, d.N, 0, d.r, d.n_adapters, dY, adapter_of, B, nullptr, scales, nullptr, nullptr, Gs, scratch, st);
         if (rc != QLORA_OK) return rc;
         G = Gs;
     }
-    return launch_adapters_grads(M, d.K, d.N, d.r, d.n_adapters, X, dY, adapter_of, scales, H, G, dA, dB, accumulate,
-                                 static_cast<char*>(workspace) + 2 * adapters_low_bytes(d, M), st);
+    return launch_adapters_grads(M, d.K, d.N, d.r, d.n_adapters, X, dY, adapter_of, scales, H, G, dA, dB, accumulate, scratch, st);
 }
 
 static int check_head(int T, int V, int D) {

@@ -33,7 +33,7 @@ int launch_adamw(const qlora_adamw_desc& d, double lr, int step, const float* lr
 // adapter_kernels.cu -- adapters of many requests, the adapter of each row of In in adapter_of (none outside [0, n_adapters)):
 //   P[m, :] = In[m, :] L1_a (rows without an adapter: 0),   Out[m, :] = Base[m, :] + scales[a] P[m, :] L2_a
 // forward: L1 = A [., r, T], L2 = B [., C, r]; else L1 = B [., T, r], L2 = A [., r, C].  Out may be Base, or NULL: P alone (then L2, scales and Base may be NULL
-// too); P may be NULL otherwise.  scratch: adapters_scratch_bytes() (with Out).
+// too); P may be NULL otherwise.  scratch: adapters_scratch_bytes().
 int launch_adapters(bool forward, int M, int T, int C, int r, int n_adapters, const void* In, const int32_t* adapter_of, const void* L1, const void* L2,
                     const float* scales, const void* Base, void* Out, float* P, void* scratch, cudaStream_t st);
 size_t adapters_scratch_bytes(int M, int r);

@@ -86,6 +86,8 @@ SIZES = [
     (1, 32, 8, 8, 1, "one"), (1, 4096, 4096, 16, 8, "each"), (3, 96, 40, 24, 2, "scattered"), (4, 512, 1000, 64, 4, "each"), (5, 160, 72, 8, 9, "none"),
     (17, 1024, 520, 40, 3, "scattered"), (64, 2080, 1376, 16, 64, "each"), (256, 512, 264, 32, 7, "rows"),
     (257, 32, 8, 8, 2, "scattered"), (260, 96, 1000, 64, 5, "rows"), (300, 1056, 552, 16, 300, "each"), (301, 800, 104, 24, 4, "none"),
+    (149, 544, 520, 64, 40, "scattered"), (200, 1024, 264, 24, 4, "none"), (256, 96, 1000, 56, 256, "each"),
+    (4100, 96, 72, 8, 40, "scattered"), (9000, 64, 40, 24, 3, "each"), (4096, 32, 264, 16, 4096, "each"),
     (513, 4096, 776, 48, 3, "rows"), (1000, 544, 2056, 8, 6, "one"), (2100, 256, 264, 56, 31, "scattered"),
 ]
 
