@@ -5,8 +5,8 @@
 // product as P = exp(z - ref), bf16, through a small ring that stays in L2, with one reference per token for the whole vocabulary, which is known
 // before the row's true maximum is: the largest of its first 256 logits and 40 ln 2 more.  The sums over the pieces then need no rescaling -- they are
 // divided by the row's sum of P at the end -- and bf16 has the range of fp32: nothing is lost while the row's maximum lies up to 120 ln 2 = 83 above
-// those first logits, and what flushes to zero is below 2^-86 of the largest.  A token whose largest logit lies further above is found at the end, and its block of 256 tokens is computed
-// again from its true maximum (by a second launch of the same kernel, which ends at once where there is none).
+// those first logits, and what flushes to zero is below 2^-86 of the largest.  A token whose largest logit lies further above is found at the end, and its
+// block of 256 tokens is computed again from its true maximum (by a second launch of the same kernel, which ends at once where there is none).
 //
 // The label's own term is kept out of P: p_label - 1 = -(sum of the others) / sum has no cancellation, and where a token is almost
 // certain the gradient would otherwise be the rounding error of P.
@@ -15,10 +15,15 @@
 //
 // One persistent kernel: a pair of CTAs (two SMs) claims items of both products from one counter (head_plan.h), so there is no wave to wait for
 // between the products or the pieces.  An item is a tile of 256 x 256 (tcgen05.mma.cta_group::2, M = 256, N = 256; 128 rows and half of the other
-// operand per CTA), operands staged by TMA in six stages (more for few rows) of 64 contraction elements, accumulators in tensor memory twice, so that the epilogue of an item
-// runs beside the products of the next.  What an item needs from others (probabilities of its rows, the previous piece's sums, a free slot
+// operand per CTA), operands staged by TMA in six stages (more for few rows) of 64 contraction elements, accumulators in tensor memory twice, so that the
+// epilogue of an item runs beside the products of the next.  What an item needs from others (probabilities of its rows, the previous piece's sums, a free slot
 // of the ring, the reference) it waits for through counters in the workspace; those items were claimed earlier, so the wait ends
 // whichever CTAs share the GPU.  Every wait is bounded.
+//
+// Bound by the tensor cores.  2048 tokens, 32000 entries, 4096 features, a launch by itself: the loss 338 us (1589 TFLOP/s, the pipe 87 % active), with the gradient
+// 698 us (1539), of which writing the probabilities is some 30 and adding to the sums 5; calls in a loop, under the power limit, 409 and 896 us in all.  Pieces of 2048 and 8192 entries:
+// 761 and 750 us; four stages 738.  The kernel that finishes takes 25 us beside that, the second launches 7.  Few tokens are bound by reading the head: 12 us and 6.0
+// TB/s (16 tokens 70 us for 262 MB).  Blocks of rows are whole: 520 tokens are 2.03 of them and cost 3.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -138,8 +143,8 @@ __device__ __forceinline__ void publish(unsigned* counter) {
 
 template <bool GRAD>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(HL_THREADS, 1)
-head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_constant__ CUtensorMap tm_rows, const __grid_constant__ CUtensorMap tm_head, const __grid_constant__ CUtensorMap tm_head_t,
-                 const __grid_constant__ CUtensorMap tm_probs, const HeadParams p) {
+head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_constant__ CUtensorMap tm_rows, const __grid_constant__ CUtensorMap tm_head,
+                 const __grid_constant__ CUtensorMap tm_head_t, const __grid_constant__ CUtensorMap tm_probs, const HeadParams p) {
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint32_t tmem_base_slot;
     __shared__ int abort_flag_s[2];
@@ -217,7 +222,8 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
                         const unsigned i = atomicAdd(counter, 1u);
                         if ((long long)i >= rows.total) break;
                         const HeadItem it = head_item(plan, rows, i);
-                        if (!active(it.block) || (!it.of_grad && it.tile * plan.tile >= head_piece_entries(plan, it.piece))) continue;   // (the last piece and chunk are shorter)
+                        if (!active(it.block)) continue;               // (the last chunk is shorter, and so is the last piece)
+                        if (!it.of_grad && it.tile * plan.tile >= head_piece_entries(plan, it.piece)) continue;
                         index = (int)i;
                         break;
                     }
@@ -326,7 +332,8 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
                 // ---- a tile of the gradient's sums
                 const int set = it.piece % plan.sums;
                 const bool add = it.piece >= plan.sums;
-                if (add && !poll_counter(grads_done(p) + (size_t)(it.q - plan.sums) * kHeadChunk + it.block_in_chunk, COUNTS_PER_TILE * plan.feature_tiles, abort_flag)) break;
+                const unsigned* before = grads_done(p) + (size_t)(add ? it.q - plan.sums : it.q) * kHeadChunk + it.block_in_chunk;
+                if (add && !poll_counter(before, COUNTS_PER_TILE * plan.feature_tiles, abort_flag)) break;
                 if (!poll(bar_acc_full + 8 * buffer, (n >> 1) & 1u, abort_flag)) break;
                 tc_fence_after();
                 float* out = p.sums + ((size_t)set * p.padded + row_w) * plan.D;
@@ -372,7 +379,8 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
             if (GRAD) {
                 if (it.q >= plan.ring) {                               // the slot's previous probabilities have been read
                     const int before = it.q - plan.ring, block = before / plan.pieces * rows.chunk + it.block_in_chunk;
-                    if (active(block) && !poll_counter(grads_done(p) + (size_t)before * kHeadChunk + it.block_in_chunk, COUNTS_PER_TILE * plan.feature_tiles, abort_flag)) break;
+                    const unsigned* read = grads_done(p) + (size_t)before * kHeadChunk + it.block_in_chunk;
+                    if (active(block) && !poll_counter(read, COUNTS_PER_TILE * plan.feature_tiles, abort_flag)) break;
                 }
                 if (!first) {
                     if (!p.again && !poll_counter(ref_known(p) + it.block, COUNTS_PER_TILE, abort_flag)) break;
@@ -399,7 +407,8 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
             float m = -INFINITY, s = 0.f;                              // the largest logit; the sum over the reference, or over m
             bf16* out = nullptr;
             if constexpr (GRAD)
-                out = p.probs + ((size_t)((it.q % plan.ring) * plan.chunk_max + it.block_in_chunk) * kHeadTile + (int)cta * 128 + quarter * 32) * plan.piece + it.tile * plan.tile;
+                out = p.probs + it.tile * plan.tile +
+                      ((size_t)((it.q % plan.ring) * plan.chunk_max + it.block_in_chunk) * kHeadTile + (int)cta * 128 + quarter * 32) * plan.piece;
             // 32 logits of the row; SPECIAL: the label or the vocabulary's end is among some row's
             auto chunk = [&](uint32_t (&v)[32], int idx, auto special) {
                 constexpr bool SPECIAL = decltype(special)::value;
@@ -686,7 +695,8 @@ static int head_loss_impl(int T, int V, int D, const void* hidden, const void* h
     const int pairs = (int)(items < sm_count() / 2 ? items : sm_count() / 2);
     for (p.again = 0; p.again < (GRAD ? 2 : 1); ++p.again) {
         if (launch_pdl(kern, dim3(2 * pairs), dim3(HL_THREADS), HL_SMEM, st, 1, tx, tr, th, tt, tp, p) != cudaSuccess) return QLORA_ERR_CUDA;
-        if (launch_pdl(head_finish_kernel<GRAD>, dim3(p.again && T > 4 * sm_count() ? 4 * sm_count() : T), dim3(FIN_THREADS), 0, st, 1, p, place, (const bf16*)head, d_loss, loss, (bf16*)d_hidden) != cudaSuccess)
+        const int blocks = p.again && T > 4 * sm_count() ? 4 * sm_count() : T;
+        if (launch_pdl(head_finish_kernel<GRAD>, dim3(blocks), dim3(FIN_THREADS), 0, st, 1, p, place, (const bf16*)head, d_loss, loss, (bf16*)d_hidden) != cudaSuccess)
             return QLORA_ERR_CUDA;
     }
     return QLORA_OK;

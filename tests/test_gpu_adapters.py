@@ -228,6 +228,31 @@ def test_captured_replayed_for_another_batch_on_another_stream(M):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("M", [6, 300, 900])
+def test_everything_rewritten_in_stream_right_before_the_calls(M):
+    """What a call reads is written by the kernels just before it, over and over, and so is the workspace by the calls themselves."""
+    p, other = Problem(M, 512, 264, 16, 5, "rows"), Problem(M, 512, 264, 16, 5, "scattered", seed=7)
+    names = ("X", "dY", "A", "B", "scales", "Yb", "dXb", "adapter_of")
+
+    def results(q):
+        H, G = q.empty(M, 16), q.empty(M, 16)
+        Y, dX = q.forward(H=H), q.back(G=G)
+        return [Y, H, dX, G, *q.grads(H, G), *q.grads(None, None)]
+    want = []
+    for q in (p, other):
+        torch.cuda.synchronize()
+        want.append(results(q))
+        torch.cuda.synchronize()
+    sources = [{n: getattr(q, n).clone() for n in names} for q in (p, other)]
+    got = []
+    for i in range(12):
+        for n in names:
+            getattr(p, n).copy_(sources[i % 2][n])
+        got.append(results(p))
+    for i, result in enumerate(got):
+        assert all(torch.equal(a, b) for a, b in zip(result, want[i % 2])), i
+
+
 def test_two_streams_at_once():
     problems = [Problem(M, 1024, 520, 16, 4, "rows", seed) for seed, M in enumerate((5, 400, 64, 2000))]
     want = [p.forward().clone() for p in problems]
