@@ -198,7 +198,7 @@ typedef struct {
     int n_adapters; /* at most 65535 */
 } qlora_adapters_desc;
 
-/* Bytes of scratch for M tokens (2^20 at most), for all three calls.  The first two need 4 M r + 12 M + 8 of them; the gradients
+/* Bytes of scratch for M tokens (2^20 at most), for all three calls.  The first two need 4 M r (r in steps of 16) + 12 M + 8 of them; the gradients
  * take most: up to 32 sums of every 2048 elements of an adapter's gradients. */
 int qlora_adapters_workspace_bytes(const qlora_adapters_desc* desc, int M, size_t* out);
 

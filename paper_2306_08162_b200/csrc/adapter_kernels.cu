@@ -93,6 +93,9 @@ struct Groups {
     int* tokens;                             // [M]
 };
 
+// A row of s P in parts: sixteen ranks at a time, in the order in which the second product's lanes take them, 16 bytes each (`up_low`).
+constexpr __host__ __device__ int split_pairs(int r) { return (r + 15) / 16 * 8; }
+
 struct Products {                            // the operands of both products
     int M, T, C, r, n_adapters;
     const bf16* In;                          // [M, T]
@@ -102,7 +105,7 @@ struct Products {                            // the operands of both products
     const bf16* Base;                        // [M, C]; no second product where Out is NULL
     bf16* Out;
     float* P;                                // [M, r] or NULL
-    uint2* split;                            // [M, r / 2]: pairs of s P as two bf16 pairs, for the second product of many tokens; or NULL
+    uint2* split;                            // [M, split_pairs(r)]: pairs of s P as two bf16 pairs, for the second product of many tokens; or NULL
     Groups groups;                           // of many tokens
 };
 
@@ -524,11 +527,13 @@ adapters_down_kernel(const Products p, int n_tiles) {
             const int b = idx / (NT * 64), nt = (idx >> 6) % NT, h = (idx >> 5) & 1, ln = idx & 31;
             const int row = 16 * b + (ln >> 2) + 8 * h, col = nt * 8 + (ln & 3) * 2;
             if (!((mask >> row) & 1u) || col >= r) return;
-            const size_t at = ((size_t)(gathered.value ? tokens[row] : m0 + row) * r + col) / 2;
-            if (p.P != nullptr) reinterpret_cast<float2*>(p.P)[at] = make_float2(v0, v1);
+            const size_t token = gathered.value ? tokens[row] : m0 + row;
+            if (p.P != nullptr) *reinterpret_cast<float2*>(p.P + token * r + col) = make_float2(v0, v1);
             if (p.split != nullptr) {
                 const Split v = split_bf16(s * v0, s * v1);
-                p.split[at] = make_uint2(v.hi, v.lo);
+                uint2* to = p.split + token * split_pairs(r) + (L_IS_A ? col / 2 : col / 16 * 8 + col % 8 + col / 8 % 2);
+                to[0] = make_uint2(v.hi, v.lo);
+                if (!L_IS_A && r % 16 == 8 && col >= r - 8) to[1] = make_uint2(0u, 0u);      // the ranks that there are not
             }
         };
         float acc[NB][NT][4] = {};
@@ -698,12 +703,11 @@ __device__ __forceinline__ void up_fragments(const bf16* __restrict__ L2, int C,
     }
 }
 
-// The ranks 16 ks .. 16 ks + 15 of a row of s P in that order, each pair (high, low).
+// What lane q takes of the ranks 16 ks .. 16 ks + 15 of token t's s P, in that order, each pair (high, low).  (With eight ranks left the others' places hold zeros.)
 template <bool FROM_B>
-__device__ __forceinline__ uint4 up_low(const uint2* row, int r, int ks, int q) {
-    if constexpr (FROM_B) return 16 * ks + 4 * q < r ? *reinterpret_cast<const uint4*>(row + 8 * ks + 2 * q) : make_uint4(0, 0, 0, 0);
-    const uint2 none = make_uint2(0, 0), u = 16 * ks + 2 * q < r ? row[8 * ks + q] : none, v = 16 * ks + 8 + 2 * q < r ? row[8 * ks + 4 + q] : none;
-    return make_uint4(u.x, u.y, v.x, v.y);
+__device__ __forceinline__ uint4 up_low(const Products& p, int t, int ks, int q) {
+    const bool in = FROM_B ? 16 * ks + 4 * q < p.r : 16 * ks < p.r;
+    return in ? *reinterpret_cast<const uint4*>(p.split + (size_t)t * split_pairs(p.r) + 8 * ks + 2 * q) : make_uint4(0, 0, 0, 0);
 }
 
 // A group of tokens, a warp's columns of them.
@@ -740,7 +744,7 @@ __device__ __forceinline__ void up_group(const Products& p, int group, int c_war
         for (int ks = 0; ks < KS; ++ks) {
             uint4 low[2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) low[h] = token[h] >= 0 ? up_low<FROM_B>(p.split + (size_t)token[h] * (r / 2), r, ks, q) : make_uint4(0, 0, 0, 0);
+            for (int h = 0; h < 2; ++h) low[h] = token[h] >= 0 ? up_low<FROM_B>(p, token[h], ks, q) : make_uint4(0, 0, 0, 0);
 #pragma unroll
             for (int i = 0; i < UB; ++i) {
                 uint32_t b[4][2];
@@ -768,9 +772,11 @@ __device__ __forceinline__ void up_group(const Products& p, int group, int c_war
         }
 }
 
-// KS steps of 16 ranks.
+// KS steps of 16 ranks.  A warp has 64 columns, so that a row of s P is loaded for every 64; above one step that takes the registers of one block an SM (8192 tokens, 4096
+// x 4096, both products, forward and backward: rank 32 68 -> 65 and 84 -> 66 us against 32 columns and two blocks, rank 64 93 -> 88 and 115 -> 91).
+constexpr int up_blocks(int steps) { return steps > 1 ? 1 : 2; }
 template <bool FROM_B, int KS, int UB>
-__global__ void __launch_bounds__(32 * UP_WARPS, 2)
+__global__ void __launch_bounds__(32 * UP_WARPS, up_blocks(KS))
 adapters_up_kernel(const Products p, int tiles_each) {
     pdl_launch_dependents();
     pdl_wait();
@@ -805,7 +811,7 @@ adapters_up_kernel(const Products p, int tiles_each) {
             const int row = (tile + ahead) * UP_ROWS + g + 8 * h;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
-                x.v[ks][h] = whole || row < M ? up_low<FROM_B>(p.split + (size_t)row * (r / 2), r, ks, q) : make_uint4(0, 0, 0, 0);
+                x.v[ks][h] = whole || row < M ? up_low<FROM_B>(p, row, ks, q) : make_uint4(0, 0, 0, 0);
         }
     };
     uint32_t held[KS][UB][4][2];
@@ -821,10 +827,10 @@ adapters_up_kernel(const Products p, int tiles_each) {
 #pragma unroll 1
     for (; tile < tile_end; ++tile) {
         Tile following;
-        Low following_low;                                             // (of more ranks the registers hold one tile's)
+        Low following_low;
         if (tile + 1 < tile_end) {
             load(1, whole(tile + 1), following);
-            if (KS == 1) load_low(1, whole(tile + 1), following_low);
+            load_low(1, whole(tile + 1), following_low);
         }
         const int m0 = tile * UP_ROWS;
         const int a = x.adapter >= 0 && x.adapter < p.n_adapters ? x.adapter : -1;
@@ -903,8 +909,7 @@ adapters_up_kernel(const Products p, int tiles_each) {
             }
         }
         x = following;
-        if (KS == 1) low = following_low;
-        else if (tile + 1 < tile_end) load_low(1, whole(tile + 1), low);
+        low = following_low;
     }
     // the groups, a block's columns at a time, all blocks in turn
     const int slabs = gridDim.y;
@@ -1318,8 +1323,8 @@ int down_impl(const Products& p, cudaStream_t st) {
 template <bool FROM_B, int KS, int UB>
 int up_impl(const Products& p, cudaStream_t st) {
     const int columns = (p.C + 32 * UB * UP_WARPS - 1) / (32 * UB * UP_WARPS), tiles = (p.M + UP_ROWS - 1) / UP_ROWS;
-    // Tiles to a block: two blocks run on an SM, so it is waves of blocks times the tiles of one, and about two tiles' time for a block to begin.
-    const long long room = 2 * sm_count();
+    // Tiles to a block: up_blocks(KS) run on an SM, so it is waves of blocks times the tiles of one, and about two tiles' time for a block to begin.
+    const long long room = up_blocks(KS) * sm_count();
     int each = 1;
     for (long long i = 1, best = 1ll << 60; i <= 64; ++i) {
         const long long blocks = (tiles + i - 1) / i * columns, cost = (blocks + room - 1) / room * (i + 2);
@@ -1392,18 +1397,18 @@ int grad_impl(const Grads& p, cudaStream_t st) {
 
 }  // namespace
 
-size_t adapters_scratch_bytes(int M, int r) { return (size_t)M * r * 4 + 8 + (size_t)M * (sizeof(int2) + sizeof(int)); }
+size_t adapters_scratch_bytes(int M, int r) { return (size_t)M * split_pairs(r) * sizeof(uint2) + 8 + (size_t)M * (sizeof(int2) + sizeof(int)); }
 
 int launch_adapters(bool forward, int M, int T, int C, int r, int n_adapters, const void* In, const int32_t* adapter_of, const void* L1, const void* L2,
                     const float* scales, const void* Base, void* Out, float* P, void* scratch, cudaStream_t st) {
-    char* groups = static_cast<char*>(scratch) + (size_t)M * r * 4;
+    char* groups = static_cast<char*>(scratch) + (size_t)M * split_pairs(r) * sizeof(uint2);
     const Products p{M, T, C, r, n_adapters, (const bf16*)In, adapter_of, (const bf16*)L1, (const bf16*)L2, scales, (const bf16*)Base, (bf16*)Out, P,
                      Out != nullptr ? (uint2*)scratch : nullptr, Groups{(int*)groups, (int2*)(groups + 8), (int*)(groups + 8 + (size_t)M * sizeof(int2))}};
 #define QLORA_PRODUCTS(NT, NB, KS, UB) return forward ? products<true, NT, NB, KS, UB>(p, st) : products<false, NT, NB, KS, UB>(p, st)
     if (r <= 8) QLORA_PRODUCTS(1, 1, 1, 2);
     if (r <= 16) QLORA_PRODUCTS(2, 1, 1, 2);
-    if (r <= 32) QLORA_PRODUCTS(4, 1, 2, 1);
-    QLORA_PRODUCTS(8, 2, 4, 1);
+    if (r <= 32) QLORA_PRODUCTS(4, 1, 2, 2);
+    QLORA_PRODUCTS(8, 2, 4, 2);
 #undef QLORA_PRODUCTS
 }
 
