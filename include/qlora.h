@@ -199,7 +199,7 @@ typedef struct {
 } qlora_adapters_desc;
 
 /* Bytes of scratch for M tokens (2^20 at most), for all three calls.  The first two need 4 M r (r in steps of 16) + 12 M + 8 of them; the gradients
- * take most: up to 32 sums of every 2048 elements of an adapter's gradients. */
+ * take most: 20 M r, and sums of some 15 MB and four times an adapter's gradients. */
 int qlora_adapters_workspace_bytes(const qlora_adapters_desc* desc, int M, size_t* out);
 
 /* X bf16 [M, K]; adapter_of int32 [M]; A bf16 [n_adapters, r, K]; B bf16 [n_adapters, N, r]; scales fp32 [n_adapters] (alpha / r of

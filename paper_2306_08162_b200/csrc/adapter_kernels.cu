@@ -926,9 +926,9 @@ adapters_up_kernel(const Products p, int tiles_each) {
 // memory, rows of other adapters as zeros, and their sums are added in the order of the warps.  The block that finishes an adapter's last chunk of a
 // slice adds the chunks in their order.
 //
-// Bound by the tasks' own ends (the first loads, the sums of four warps, the chunks' sums), not by the bytes: 68 MB in 32 us after 10 us of listing (4096 tokens,
-// 4096 x 4096, rank 16, three blocks an SM).  Chunks of 48, 64 and 96 tiles at least: 44, 49 and 47 us in all instead of 40; 8 warps 42 instead of 38; two
-// blocks with four stages as three with three, but 161 instead of 129 for 22 adapters at rank 64.
+// Bound by the tasks' own ends (the first loads, the sums of four warps, the chunks' sums) and the chain of a warp's instructions, not by the bytes: 68 MB in 31 us after
+// 10 us of listing (4096 tokens, 4096 x 4096, rank 16, three blocks an SM: 12 warps, an instruction every 8.6 cycles each).  In all 37.7 us; chunks of 40 tiles at least 40.0, but 39
+// instead of 41 for 1531 tokens of 13 sequences; 8 warps, or two blocks with four stages, were slower or no faster, and so were 128 columns above rank 16 (231 -> 249).
 //
 // Both operands are transposed on the way out of shared memory.  G and H are taken as three bf16 each, which hold all of an fp32 value (made once, not by every
 // slice; with two the gradients were 2.5e-6 off, with three 5e-7), one product after the other into the same sums.  Where a sum is not finite the lower parts
@@ -1135,8 +1135,10 @@ __device__ __forceinline__ void grad_task(const Grads& p, int task, int n_entrie
                 __syncthreads();
             }
             const int mine = warp < total ? (total - warp + GR_WARPS - 1) / GR_WARPS : 0;
+            uint32_t to = ring, from = ring;                           // the stages that are filled and read next
+            auto after = [&](uint32_t stage) { return stage + Tile::STAGE == ring + GR_STAGES * Tile::STAGE ? ring : stage + Tile::STAGE; };
             auto load = [&](int i) {
-                const uint32_t to = ring + (i % GR_STAGES) * Tile::STAGE, entry = list[warp + i * GR_WARPS];
+                const uint32_t entry = list[warp + i * GR_WARPS];
                 const int t0 = (int)(entry >> 16) * 16;
                 const bf16* v = V + (size_t)(t0 + v_row) * C + (v_in ? c0 + 8 * v_piece : 0);
 #pragma unroll
@@ -1156,6 +1158,7 @@ __device__ __forceinline__ void grad_task(const Grads& p, int task, int n_entrie
                     copy16(p_to + k * Tile::P_BYTES, in ? low + (size_t)k * M * r : P, in);
                     if constexpr (P_PIECES == 4) copy16(p_to + k * Tile::P_BYTES + 8 * (RANKS * 2), in8 ? low + ((size_t)k * M + 8) * r : P, in8);
                 }
+                to = after(to);
             };
 #pragma unroll
             for (int i = 0; i < GR_STAGES - 1; ++i) {
@@ -1170,7 +1173,8 @@ __device__ __forceinline__ void grad_task(const Grads& p, int task, int n_entrie
                 __syncwarp();                                          // tile i is there, tile i - 1 has been read by every lane
                 if (i + GR_STAGES - 1 < mine) load(i + GR_STAGES - 1);
                 copy_commit();
-                const uint32_t v = ring + (i % GR_STAGES) * Tile::STAGE, pp = v + Tile::V_BYTES;
+                const uint32_t v = from, pp = v + Tile::V_BYTES;
+                from = after(from);
                 uint32_t a[GR_PARTS][MT][4];
 #pragma unroll
                 for (int half = 0; half < GR_PARTS; ++half)
@@ -1180,22 +1184,17 @@ __device__ __forceinline__ void grad_task(const Grads& p, int task, int n_entrie
                         ldmatrix4<true>(pp + half * Tile::P_BYTES + a_row * (RANKS * 2) + ((piece ^ (a_row * P_PIECES / 8 % P_PIECES)) << 4), a[half][mt][0],
                                         a[half][mt][1], a[half][mt][2], a[half][mt][3]);
                     }
+                uint32_t b[CT / 2][4];                                 // tokens 0 - 7, 8 - 15 of columns 16 t ..; then of the next eight
 #pragma unroll
-                for (int t = 0; t < CT; t += 2) {                      // tokens 0 - 7, 8 - 15 of columns 8 t ..; then of the next eight
-                    uint32_t b[4];
-                    ldmatrix4<true>(v + v_off + (v_xor ^ (t << 4)), b[0], b[1], b[2], b[3]);
+                for (int t = 0; t < CT / 2; ++t) ldmatrix4<true>(v + v_off + (v_xor ^ (t << 5)), b[t][0], b[t][1], b[t][2], b[t][3]);
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
-                        mma_bf16_16816(acc[mt][t], a[0][mt][0], a[0][mt][1], a[0][mt][2], a[0][mt][3], b[0], b[1]);
-                        mma_bf16_16816(acc[mt][t + 1], a[0][mt][0], a[0][mt][1], a[0][mt][2], a[0][mt][3], b[2], b[3]);
-                        if (low_parts) {
+                for (int k = 0; k < GR_PARTS; ++k) {                   // (part by part: a sum's products are far apart)
+                    if (k > 0 && !low_parts) break;
 #pragma unroll
-                            for (int k = 1; k < GR_PARTS; ++k) {
-                                mma_bf16_16816(acc[mt][t], a[k][mt][0], a[k][mt][1], a[k][mt][2], a[k][mt][3], b[0], b[1]);
-                                mma_bf16_16816(acc[mt][t + 1], a[k][mt][0], a[k][mt][1], a[k][mt][2], a[k][mt][3], b[2], b[3]);
-                            }
-                        }
-                    }
+                    for (int t = 0; t < CT; ++t)
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt)
+                            mma_bf16_16816(acc[mt][t], a[k][mt][0], a[k][mt][1], a[k][mt][2], a[k][mt][3], b[t / 2][2 * (t % 2)], b[t / 2][2 * (t % 2) + 1]);
                 }
             }
             copy_wait<0>();
@@ -1358,15 +1357,16 @@ int products(const Products& p, cudaStream_t st) {
     return rc != QLORA_OK || p.Out == nullptr ? rc : up_impl<FORWARD, KS, UB>(p, st);
 }
 
-// Slices and chunks of the gradients: as many chunks as give every SM all its blocks twice, sixteen at least.
+// Slices and chunks of the gradients: as many chunks as give every SM all its blocks twice, two at least.  (A task's own cost is that of a dozen tiles: with sixteen chunks at
+// least, 8192 tokens at rank 64, 4096 x 11008, took 220 us instead of 165, 22 prompts 124 instead of 96; with tasks for four or eight turns of blocks 159 and 181, 107 and 124.)
 void cut_grads(Grads& p) {
     const int columns = p.r <= 16 ? GradTile<1>::COLS : GradTile<2>::COLS, ranks = p.r <= 16 ? GradTile<1>::RANKS : GradTile<2>::RANKS;
     p.slices_x = (p.K + columns - 1) / columns;
     p.slices = p.slices_x + (p.N + columns - 1) / columns;
     p.rank_blocks = (p.r + ranks - 1) / ranks;
     const int blocks = p.slices * p.rank_blocks, wanted = 2 * GR_BLOCKS * sm_count();
-    p.most_chunks = blocks == 0 ? 16 : (wanted + blocks - 1) / blocks;
-    p.most_chunks = p.most_chunks < 16 ? 16 : p.most_chunks > 128 ? 128 : p.most_chunks;
+    p.most_chunks = blocks == 0 ? 2 : (wanted + blocks - 1) / blocks;
+    p.most_chunks = p.most_chunks < 2 ? 2 : p.most_chunks > 128 ? 128 : p.most_chunks;
 }
 
 struct GradScratch { size_t g, h, counters, entries, counts, chunks, partial, total; };
