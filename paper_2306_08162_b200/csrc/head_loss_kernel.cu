@@ -377,10 +377,10 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
             const bool first = it.piece == 0 && it.tile == 0 && !p.again;
             float ref = 0.f;
             if (GRAD) {
-                if (it.q >= plan.ring) {                               // the slot's previous probabilities have been read
-                    const int before = it.q - plan.ring, block = before / plan.pieces * rows.chunk + it.block_in_chunk;
+                const int before = head_slot_before(plan, rows, it.q, it.block_in_chunk, active);
+                if (before >= 0) {                                     // the slot's previous probabilities have been read
                     const unsigned* read = grads_done(p) + (size_t)before * kHeadChunk + it.block_in_chunk;
-                    if (active(block) && !poll_counter(read, COUNTS_PER_TILE * plan.feature_tiles, abort_flag)) break;
+                    if (!poll_counter(read, COUNTS_PER_TILE * plan.feature_tiles, abort_flag)) break;
                 }
                 if (!first) {
                     if (!p.again && !poll_counter(ref_known(p) + it.block, COUNTS_PER_TILE, abort_flag)) break;

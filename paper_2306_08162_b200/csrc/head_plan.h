@@ -118,6 +118,16 @@ QLORA_HD HeadItem head_item(const HeadPlan& p, const HeadRows& r, long long inde
     return it;
 }
 
+// The last piece before q whose probabilities lay where those of (q, block_in_chunk) go, or -1: its gradient has to be through before they are written.  Blocks
+// of rows that take no part (the last chunk's missing ones; in the second launch those that are not done again) wrote and read nothing, so the one
+// before them is who is waited for; it waited for the one before itself.
+template <typename Active>
+QLORA_HD int head_slot_before(const HeadPlan& p, const HeadRows& r, int q, int block_in_chunk, const Active& active) {
+    for (int before = q - p.ring; before >= 0; before -= p.ring)
+        if (active(before / p.pieces * r.chunk + block_in_chunk)) return before;
+    return -1;
+}
+
 QLORA_HD int head_piece_entries(const HeadPlan& p, int piece) { return p.V - piece * p.piece < p.piece ? p.V - piece * p.piece : p.piece; }
 
 // The workspace, in bytes from its beginning.
