@@ -243,9 +243,11 @@ int qlora_lrec_loss(int T, int V, const void* student_logits, const void* teache
  * tokens of a prompt); d_loss fp32 [T]: the upstream gradient of every token's loss (1 / n for the mean of n), with d_hidden bf16 [T, D]; both NULL: the loss
  * alone.  labels, d_loss and loss_tokens may begin at any element; the latter two may not overlap.  d_hidden may be hidden itself; any other overlap of the
  * two is refused.  D: a multiple of 8, 64 to 2^20; T and V up to 2^24, T (V + D) up to about 2^43.
- * workspace: qlora_head_loss_workspace_bytes(T, V, D, gradient), of which the part that grows with V is 50 MB at most and 8 bytes for every token and 256 entries.
+ * workspace: qlora_head_loss_workspace_bytes(T, V, D, gradient), of which the part that grows with V is 50 MB at most and 8 bytes (12 with
+ * the gradient) for every token and 256 entries.
  * Sums, maxima and losses are fp32 (a token that is almost certain keeps its small loss and gradient); probabilities are rounded to bf16 where they
- * enter the gradient's product.  The logits may be of any size; a block of 256 tokens is computed twice where one of them has a logit more than 83 above
+ * enter the gradient's product, and weighed so that those of all rows of the head, less the label's, still add up to 0: what all rows share does not
+ * reach the gradient.  The logits may be of any size; a block of 256 tokens is computed twice where one of them has a logit more than 83 above
  * the largest of its first 256.  A token with a NaN or infinity among its logits has loss and gradient NaN. */
 int qlora_head_loss_workspace_bytes(int T, int V, int D, int gradient, size_t* out);
 int qlora_head_loss(int T, int V, int D, const void* hidden, const void* head, const int32_t* labels, const float* d_loss, float* loss_tokens,

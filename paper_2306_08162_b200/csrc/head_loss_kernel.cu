@@ -9,7 +9,9 @@
 // block of 256 tokens is computed again from its true maximum (by a second launch of the same kernel, which ends at once where there is none).
 //
 // The label's own term is kept out of P: p_label - 1 = -(sum of the others) / sum has no cancellation, and where a token is almost
-// certain the gradient would otherwise be the rounding error of P.
+// certain the gradient would otherwise be the rounding error of P.  And the others' rows are weighed with sum P / sum of the rounded P, so that the weights of all
+// rows add up to nothing: a vector that all rows of the head share would otherwise come out times the rounding error (20 standard deviations of the rows'
+// own parts, logits that spread by 4: 5e-2 of a token's gradient, now 2e-3, which is the result's own rounding).
 //
 // Rounding: P to bf16 (a relative error of 2^-9 on average over many terms of either sign), dh to bf16; everything else is fp32.
 //
@@ -75,6 +77,7 @@ struct HeadParams {
     const int* label;
     float *ref, *label_logit;
     float2* tile_stats;                      // [rows][tiles]: the largest logit, the sum
+    float* tile_rounded;                     // [rows][tiles], with the gradient: the sum of what enters its product
     bf16* probs;
     float* sums;
 };
@@ -405,6 +408,7 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
                 publish(ref_known(p) + it.block);
             }
             float m = -INFINITY, s = 0.f;                              // the largest logit; the sum over the reference, or over m
+            f2 rounded = make_f2(0.f, 0.f);                            // the sum of the probabilities as they are stored
             bf16* out = nullptr;
             if constexpr (GRAD)
                 out = p.probs + it.tile * plan.tile +
@@ -444,6 +448,7 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
                         for (int j = 0; j < 4; ++j) {
                             const __nv_bfloat162 pr = __floats2bfloat162_rn(__uint_as_float(v[c8 * 8 + 2 * j]), __uint_as_float(v[c8 * 8 + 2 * j + 1]));
                             o[j] = *reinterpret_cast<const uint32_t*>(&pr);
+                            rounded = add2(rounded, unpack_bf16(o[j]));
                         }
                         *reinterpret_cast<uint4*>(slice + lane * 64 + ((c8 ^ ((lane >> 1) & 3)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
                     }
@@ -468,7 +473,9 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(leader_acc_empty + 8 * buffer);
-            __stcg(p.tile_stats + (size_t)row * head_div_up(plan.V, plan.tile) + v0 / plan.tile, make_float2(m, s));
+            const size_t stats = (size_t)row * head_div_up(plan.V, plan.tile) + v0 / plan.tile;
+            __stcg(p.tile_stats + stats, make_float2(m, s));
+            if constexpr (GRAD) __stcg(p.tile_rounded + stats, lo_of(rounded) + hi_of(rounded));
             if constexpr (GRAD) publish(logits_done(p) + (size_t)it.q * kHeadChunk + it.block_in_chunk);
         }
     }
@@ -537,23 +544,23 @@ head_prepare_kernel(int T, int V, int D, int copies, int turns, const int32_t* _
 
 // One block per token: its loss from the tiles' sums, and its row of the gradient from the pieces' sums, which are asked for first.
 constexpr int FIN_THREADS = 256, FIN_AHEAD = 2;
-struct MaxSum { float m, s; };
+struct MaxSum { float m, s, r; };             // r: the sum of the rounded terms, with the gradient
 // Each thread's maximum and sum -> the block's (in a fixed order).
 template <bool RESCALE>
-__device__ __forceinline__ MaxSum block_max_sum(MaxSum v, float scale, float (*parts)[2]) {
+__device__ __forceinline__ MaxSum block_max_sum(MaxSum v, float scale, float (*parts)[3]) {
     auto join = [&](MaxSum a, MaxSum b) {
-        MaxSum r{fmaxf(a.m, b.m), a.s + b.s};
+        MaxSum r{fmaxf(a.m, b.m), a.s + b.s, a.r + b.r};
         if constexpr (RESCALE)                                         // (a sum over its own maximum; one without a term has none)
             r.s = (a.s == 0.f ? 0.f : a.s * fast_exp2((a.m - r.m) * scale)) + (b.s == 0.f ? 0.f : b.s * fast_exp2((b.m - r.m) * scale));
         return r;
     };
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = join(v, MaxSum{__shfl_xor_sync(0xFFFFFFFFu, v.m, o), __shfl_xor_sync(0xFFFFFFFFu, v.s, o)});
-    if ((threadIdx.x & 31) == 0) { parts[threadIdx.x >> 5][0] = v.m; parts[threadIdx.x >> 5][1] = v.s; }
+    for (int o = 16; o > 0; o >>= 1) v = join(v, MaxSum{__shfl_xor_sync(0xFFFFFFFFu, v.m, o), __shfl_xor_sync(0xFFFFFFFFu, v.s, o), RESCALE ? 0.f : __shfl_xor_sync(0xFFFFFFFFu, v.r, o)});
+    if ((threadIdx.x & 31) == 0) { parts[threadIdx.x >> 5][0] = v.m; parts[threadIdx.x >> 5][1] = v.s; parts[threadIdx.x >> 5][2] = v.r; }
     __syncthreads();
-    v = MaxSum{parts[0][0], parts[0][1]};
+    v = MaxSum{parts[0][0], parts[0][1], parts[0][2]};
 #pragma unroll
-    for (int w = 1; w < FIN_THREADS / 32; ++w) v = join(v, MaxSum{parts[w][0], parts[w][1]});
+    for (int w = 1; w < FIN_THREADS / 32; ++w) v = join(v, MaxSum{parts[w][0], parts[w][1], parts[w][2]});
     return v;
 }
 
@@ -561,7 +568,7 @@ template <bool GRAD>
 __global__ void __launch_bounds__(FIN_THREADS)
 head_finish_kernel(HeadParams p, const int* __restrict__ place, const bf16* __restrict__ head, const float* __restrict__ d_loss, float* __restrict__ loss,
                    bf16* __restrict__ d_hidden) {
-    __shared__ float parts[FIN_THREADS / 32][2];
+    __shared__ float parts[FIN_THREADS / 32][3];
     pdl_launch_dependents();
     pdl_wait();
     if (p.again && __ldcg(p.counters + 3) == 0u) return;
@@ -599,11 +606,11 @@ head_finish_kernel(HeadParams p, const int* __restrict__ place, const bf16* __re
         }
         const int tiles = head_div_up(p.plan.V, p.plan.tile);
         const float label_logit = __ldcg(p.label_logit + row), known_ref = GRAD ? __ldcg(p.ref + row) : 0.f;
-        MaxSum v{-INFINITY, 0.f};
+        MaxSum v{-INFINITY, 0.f, 0.f};
         for (int i = threadIdx.x; i < tiles; i += FIN_THREADS) {
             const float2 stats = __ldcg(p.tile_stats + (size_t)row * tiles + i);
             const float m = stats.x, s = stats.y;
-            if constexpr (GRAD) v = MaxSum{fmaxf(v.m, m), v.s + s};
+            if constexpr (GRAD) v = MaxSum{fmaxf(v.m, m), v.s + s, v.r + __ldcg(p.tile_rounded + (size_t)row * tiles + i)};
             else {
                 const float to = fmaxf(v.m, m);
                 v.s = (v.s == 0.f ? 0.f : v.s * fast_exp2((v.m - to) * p.scale)) + (s == 0.f ? 0.f : s * fast_exp2((m - to) * p.scale));
@@ -625,7 +632,9 @@ head_finish_kernel(HeadParams p, const int* __restrict__ place, const bf16* __re
             }
         }
         if constexpr (GRAD) {
-            const float f = d_loss[t], share = f / total, back = -share * others;
+            // The pieces' sums hold rounded probabilities.  They are given the weight that the unrounded ones have, which is what the label's row is subtracted
+            // with: what all rows of the head have in common cancels to fp32's rounding.
+            const float f = d_loss[t], unit = f / total, back = -unit * others, share = v.r > 0.f ? unit * (others / v.r) : unit;
             auto store = [&](int c, const Chunk& x) {
                 const uint32_t lw[4] = {x.w.x, x.w.y, x.w.z, x.w.w};
                 uint32_t o[4];
@@ -664,6 +673,7 @@ static int head_loss_impl(int T, int V, int D, const void* hidden, const void* h
     p.ref = reinterpret_cast<float*>(ws + l.ref);
     p.label_logit = reinterpret_cast<float*>(ws + l.label_logit);
     p.tile_stats = reinterpret_cast<float2*>(ws + l.tile_stats);
+    p.tile_rounded = reinterpret_cast<float*>(ws + l.tile_rounded);
     p.probs = reinterpret_cast<bf16*>(ws + l.probs);
     p.sums = reinterpret_cast<float*>(ws + l.sums);
     int* place = reinterpret_cast<int*>(ws + l.place);

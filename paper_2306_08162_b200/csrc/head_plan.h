@@ -132,7 +132,7 @@ QLORA_HD int head_piece_entries(const HeadPlan& p, int piece) { return p.V - pie
 
 // The workspace, in bytes from its beginning.
 struct HeadLayout {
-    size_t place, label, ref, label_logit, tile_stats, rows, probs, sums, counters;
+    size_t place, label, ref, label_logit, tile_stats, tile_rounded, rows, probs, sums, counters;
     size_t counter_words, total;
 };
 
@@ -150,6 +150,7 @@ inline HeadLayout head_layout(const HeadPlan& p, int T) {
     QLORA_TAKE(ref, padded * 4);
     QLORA_TAKE(label_logit, padded * 4);
     QLORA_TAKE(tile_stats, tiles * padded * 8);
+    QLORA_TAKE(tile_rounded, p.grad ? tiles * padded * 4 : 0);
     QLORA_TAKE(rows, padded * p.D * 2);
     QLORA_TAKE(probs, p.grad ? (size_t)p.ring * p.chunk_max * kHeadTile * p.piece * 2 : 0);
     QLORA_TAKE(sums, p.grad ? (size_t)p.sums * padded * p.D * 4 : 0);
