@@ -932,7 +932,7 @@ adapters_up_kernel(const Products p, int tiles_each) {
 //
 // Both operands are transposed on the way out of shared memory.  G and H are taken as three bf16 each, which hold all of an fp32 value (made once, not by every
 // slice; with two the gradients were 2.5e-6 off, with three 5e-7), one product after the other into the same sums.  Where a sum is not finite the lower parts
-// have nothing to say, but may have made a NaN of an infinity: the task is then done again without them.
+// may have made a NaN of an infinity in X or dY: the task is then done again with zeros for them there, and finite sums come out as before.
 constexpr int GR_PARTS = 3, GR_WARPS = 4, GR_STAGES = 3, GR_BLOCKS = 3, GR_MIN_TILES = 32;
 
 struct Grads {
@@ -1097,7 +1097,7 @@ __device__ __forceinline__ void grad_task(const Grads& p, int task, int n_entrie
     }
     const int lo = part * chunk_tiles, hi = lo + chunk_tiles;          // of the adapter's entries
     float acc[MT][CT][4];
-    for (int low_parts = 1; low_parts >= 0; --low_parts) {
+    auto pass = [&](auto again) {                                      // whether a sum is not finite
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -1189,7 +1189,12 @@ __device__ __forceinline__ void grad_task(const Grads& p, int task, int n_entrie
                 for (int t = 0; t < CT / 2; ++t) ldmatrix4<true>(v + v_off + (v_xor ^ (t << 5)), b[t][0], b[t][1], b[t][2], b[t][3]);
 #pragma unroll
                 for (int k = 0; k < GR_PARTS; ++k) {                   // (part by part: a sum's products are far apart)
-                    if (k > 0 && !low_parts) break;
+                    if constexpr (decltype(again)::value)
+                        if (k == 1)
+#pragma unroll
+                            for (int t = 0; t < CT / 2; ++t)
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) b[t][i] = finite_pair(b[t][i]);
 #pragma unroll
                     for (int t = 0; t < CT; ++t)
 #pragma unroll
@@ -1207,8 +1212,9 @@ __device__ __forceinline__ void grad_task(const Grads& p, int task, int n_entrie
             for (int t = 0; t < CT; ++t)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) worst += acc[mt][t][k] - acc[mt][t][k];
-        if (!__syncthreads_or(worst != 0.f)) break;
-    }
+        return __syncthreads_or(worst != 0.f) != 0;
+    };
+    if (pass(std::false_type{})) pass(std::true_type{});
     // [mt][t][c]: rank 16 mt + g (+ 8 where c >= 2), column 8 t + 2 q + c % 2
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
