@@ -245,7 +245,9 @@ int qlora_lrec_loss(int T, int V, const void* student_logits, const void* teache
  * two is refused.  D: a multiple of 8, 64 to 2^20; T and V up to 2^24, T (V + D) up to about 2^43.
  * workspace: qlora_head_loss_workspace_bytes(T, V, D, gradient), of which the part that grows with V is 50 MB at most and 8 bytes (12 with
  * the gradient) for every token and 256 entries.
- * Sums, maxima and losses are fp32 (a token that is almost certain keeps its small loss and gradient); probabilities are rounded to bf16 where they
+ * The logits' sums are the tensor cores', fp32 cut off towards zero.  What random terms lose by it is taken back on average, 1e-9 of a logit for every feature up
+ * to 16384 of them, so a sum that loses nothing (few features that are not zero, whole numbers) comes out larger by that, 4e-6 of itself at D = 4096.
+ * Other sums, maxima and losses are fp32 (a token that is almost certain keeps its small loss and gradient); probabilities are rounded to bf16 where they
  * enter the gradient's product, and weighed so that those of all rows of the head, less the label's, still add up to 0: what all rows share does not
  * reach the gradient.  The logits may be of any size; a block of 256 tokens is computed twice where one of them has a logit more than 83 above
  * the largest of its first 256.  A token with a NaN or infinity among its logits has loss and gradient NaN. */

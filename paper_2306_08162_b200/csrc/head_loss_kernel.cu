@@ -57,9 +57,12 @@ constexpr int HL_WAIT_US = 250000;
 constexpr uint32_t HL_SPINS = 1u << 26;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f, MOST = 3.402823466e38f;
 // The tensor cores cut their fp32 sums off towards zero at every step, which is an expected loss, not a random one: logits of random terms came out smaller by
-// 1.0e-9 of their size per contraction element (measured at 64, 256, 1024 and 4096 elements against 64-bit sums, sums that grow steadily and sums that
-// wander alike).  The exponentials' scale takes the expected part back: 4096 elements, relative error of the losses 2.2e-6 -> 3e-7.
+// 1.0e-9 of their size per contraction element (measured against 64-bit sums at 1024, within 12 %, and from 4096 to 262144, within 2 %;
+// below it drowns in fp32's own rounding).  The exponentials' scale takes the expected part back: mean error of a logit at 4096 elements 4e-6 -> 1e-8, at 16384 1.6e-5 -> 1.2e-7.
+// It is the wrong thing for other sums: exact ones (few features that are not zero, whole numbers) lose nothing and come out larger by it, and those whose terms
+// have one sign lose more (in all 3e-9 per element at 4096, 4.5e-9 at 16384).  So it grows with the length up to 16384 only, 1.6e-5 of a logit.
 constexpr float CUT_OFF = 1.0e-9f;
+constexpr int CUT_OFF_LENGTH = 16384;
 constexpr float REF_ABOVE = 40.f * LN2;      // the reference over the largest of the first logits
 constexpr float REF_REACH = 80.f * LN2;      // how far a logit may lie above it: sums of 2^24 terms times weights below 2^20 stay finite
 
@@ -666,7 +669,7 @@ static int head_loss_impl(int T, int V, int D, const void* hidden, const void* h
     const HeadLayout l = head_layout(p.plan, T);
     char* ws = static_cast<char*>(workspace);
     p.wait_limit_us = HL_WAIT_US;
-    p.scale = LOG2E * (1.0f + CUT_OFF * (float)D);
+    p.scale = LOG2E * (1.0f + CUT_OFF * (float)(D < CUT_OFF_LENGTH ? D : CUT_OFF_LENGTH));
     p.padded = (size_t)p.plan.blocks_max * kHeadTile;
     p.counters = reinterpret_cast<unsigned*>(ws + l.counters);
     p.label = reinterpret_cast<int*>(ws + l.label);
