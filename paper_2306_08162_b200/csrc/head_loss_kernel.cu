@@ -637,7 +637,8 @@ head_finish_kernel(HeadParams p, const int* __restrict__ place, const bf16* __re
         if constexpr (GRAD) {
             // The pieces' sums hold rounded probabilities.  They are given the weight that the unrounded ones have, which is what the label's row is subtracted
             // with: what all rows of the head have in common cancels to fp32's rounding.
-            const float f = d_loss[t], unit = f / total, back = -unit * others, share = v.r > 0.f ? unit * (others / v.r) : unit;
+            // (A label whose logit is +infinity: a probability of infinity / infinity.)
+            const float f = d_loss[t], unit = total < INFINITY ? f / total : NAN, back = -unit * others, share = v.r > 0.f ? unit * (others / v.r) : unit;
             auto store = [&](int c, const Chunk& x) {
                 const uint32_t lw[4] = {x.w.x, x.w.y, x.w.z, x.w.w};
                 uint32_t o[4];
