@@ -378,15 +378,16 @@ int qlora_quantize_rtn(const qlora_desc* desc, const float* W, int32_t* Q, void*
 
 /* Health check of the kernels enqueued so far on the current device.  Every wait inside the tensor-core kernels (on a
  * TMA transfer, on another warp, on the tensor cores) is bounded; if one ever runs out, the kernel stops early, leaves
- * its outputs incomplete and sets a sticky per-device status word instead of hanging the GPU.  This call SYNCHRONISES
+ * its outputs incomplete and sets a sticky per-device status word (bit 0; the head's cross entropy bit 1) instead of hanging the GPU.  This call SYNCHRONISES
  * the device, copies the word to *status_out (host pointer; 0 = healthy), clears it when `clear` is non-zero, and
  * returns QLORA_OK or QLORA_ERR_TIMEOUT.  The paper has no counterpart; it exists so that a synchronisation fault cannot hang a device. */
 int qlora_device_status(unsigned int* status_out, int clear);
 
 /* Self-test of the give-up path behind qlora_device_status (the paper has no counterpart).  Enqueues a one-CTA kernel in
  * which one thread waits, with the same bounded wait the tensor-core kernels use, on a shared-memory barrier that nobody
- * arrives at.  After limit_us microseconds (1 .. 1000000) the wait gives up, the sticky status word is set and the kernel
- * ends normally; the next qlora_device_status call reports QLORA_ERR_TIMEOUT (and clears the word if asked to).  No real
+ * arrives at, and another in which two warps wait as the head's cross entropy does, on such a barrier and on a counter in
+ * global memory that nothing adds to.  After limit_us microseconds (1 .. 1000000) each wait gives up, both bits of the sticky
+ * status word are set and the kernels end normally; the next qlora_device_status call reports QLORA_ERR_TIMEOUT (and clears the word if asked to).  No real
  * kernel is stalled and nothing else on the device is touched. */
 int qlora_selftest_bounded_wait(int limit_us, void* cuda_stream);
 

@@ -154,13 +154,14 @@ int qlora_device_status(unsigned int* status_out, int clear) {
     int rc = read_device_status(status_out, clear);
     if (rc == QLORA_OK) rc = read_head_status(&head, clear);
     if (rc != QLORA_OK) return rc;
-    *status_out |= head;
+    *status_out |= head << 1;
     return *status_out == 0 ? QLORA_OK : QLORA_ERR_TIMEOUT;
 }
 
 int qlora_selftest_bounded_wait(int limit_us, void* cuda_stream) {
     if (limit_us < 1 || limit_us > 1000000) return QLORA_ERR_INVALID_ARG;
-    return launch_wait_probe(limit_us, (cudaStream_t)cuda_stream);
+    const int rc = launch_wait_probe(limit_us, (cudaStream_t)cuda_stream);
+    return rc != QLORA_OK ? rc : launch_head_wait_probe(limit_us, (cudaStream_t)cuda_stream);
 }
 
 int qlora_workspace_bytes(const qlora_desc* desc, int M, size_t* out) {

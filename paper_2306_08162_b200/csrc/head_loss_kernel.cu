@@ -658,7 +658,30 @@ head_finish_kernel(HeadParams p, const int* __restrict__ place, const bf16* __re
     }
 }
 
+// The waits' way out: a barrier that nobody arrives at, and a counter that nothing adds to, a warp each.
+__device__ unsigned g_head_never = 0;
+__global__ void __launch_bounds__(64)
+head_wait_probe_kernel(int limit_us) {
+    __shared__ uint64_t bar;
+    __shared__ int flags[2][2];                                        // (one for each wait: neither ends because the other has)
+    const int warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) {
+        flags[0][0] = flags[1][0] = 0;
+        flags[0][1] = flags[1][1] = limit_us;
+        mbar_init(smem_u32(&bar), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    if (warp == 0) (void)poll(smem_u32(&bar), 0u, flags[0]);
+    else (void)poll_counter(&g_head_never, 1u, flags[1]);
+}
+
 }  // namespace
+
+int launch_head_wait_probe(int limit_us, cudaStream_t st) {
+    head_wait_probe_kernel<<<1, 64, 0, st>>>(limit_us);
+    return cudaGetLastError() == cudaSuccess ? QLORA_OK : QLORA_ERR_CUDA;
+}
 
 size_t head_loss_workspace_bytes(int T, int V, int D, bool grad) { return head_layout(head_plan(T, V, D, grad ? 1 : 0), T).total; }
 

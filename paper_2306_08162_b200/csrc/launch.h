@@ -46,6 +46,7 @@ size_t head_loss_workspace_bytes(int T, int V, int D, bool grad);
 int launch_head_loss(int T, int V, int D, const void* hidden, const void* head, const int32_t* labels, const float* d_loss, float* loss, void* d_hidden,
                      void* workspace, cudaStream_t st);
 int read_head_status(unsigned int* out, int clear);
+int launch_head_wait_probe(int limit_us, cudaStream_t st);
 
 // simt_kernels.cu -- CUDA-core kernels, correct for every supported shape
 // In [M, T] bf16 times the dequantised weight, plus s * P L.  transposed = false: forward (T = K, C = N);
