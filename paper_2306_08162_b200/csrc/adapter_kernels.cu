@@ -1351,11 +1351,11 @@ int products(const Products& p, cudaStream_t st) {
     // take 14 us both ways, those of 32 adapters in turn 30 us instead of 25, and of 256 adapters 35 instead of 67; at rank 64 it is 40 instead of 15, 109
     // instead of 30 and 146 instead of 124 (4096 x 4096).
     const int room = 2 * sm_count();
-    if (p.Out != nullptr && (2 * p.M <= room || (p.r <= 16 && p.M <= FEW_TOKENS))) {
+    if (p.Out != nullptr && (2 * p.M <= room || (NT <= 2 && p.M <= FEW_TOKENS))) {
         if (8 * p.M <= room) return few_impl<FORWARD, NT, 1, 8>(p, st);
         if (4 * p.M <= room) return few_impl<FORWARD, NT, 1, 4>(p, st);
         if (2 * p.M <= room) return few_impl<FORWARD, NT, 1, 2>(p, st);
-        return few_impl<FORWARD, NT, 4, 4>(p, st);
+        if constexpr (NT <= 2) return few_impl<FORWARD, NT, 4, 4>(p, st);
     }
     // blocks to a tile: while all of them run at a time
     const int tiles = (p.M + 16 * NB - 1) / (16 * NB), at_a_time = (NT <= 4 ? 2 : 1) * sm_count();
