@@ -192,8 +192,8 @@ int qlora_unpack(int bits, int K, int N, const int32_t* Q, uint8_t* codes, void*
  *     dA_a  = scales[a] sum G[t]^T X[t]       dB_a  = scales[a] sum dY[t]^T H[t]        (sums over the tokens of a)
  * Y_base and dX_base are what the shared projection gives, e.g. qlora_fwd and qlora_bwd_input with r = 0. */
 typedef struct {
-    int K;          /* input features, a multiple of 32 */
-    int N;          /* output features, a multiple of 8 */
+    int K;          /* input features, a multiple of 32, at most 2^24 */
+    int N;          /* output features, a multiple of 8, at most 2^24 */
     int r;          /* rank, 8 .. 64 in steps of 8; adapters of lower ranks are held with rows of A and columns of B that are zero */
     int n_adapters; /* at most 65535 */
 } qlora_adapters_desc;

@@ -94,6 +94,7 @@ int check_adamw(const qlora_adamw_desc* d, bool step) {
 int check_adapters(const qlora_adapters_desc* d, int M) {
     if (d == nullptr || d->K < 0 || d->N < 0 || d->r < 0 || d->n_adapters < 0) return QLORA_ERR_INVALID_ARG;
     if (d->K == 0 || d->K % 32 != 0 || d->N == 0 || d->N % 8 != 0 || d->r % 8 != 0 || d->r == 0 || d->r > 64 || d->n_adapters > 65535) return QLORA_ERR_UNSUPPORTED;
+    if (d->K > (1 << 24) || d->N > (1 << 24)) return QLORA_ERR_UNSUPPORTED;   // (elements of an adapter's matrix are counted in 32 bits)
     if (M < 0) return QLORA_ERR_INVALID_ARG;
     return M > (1 << 20) ? QLORA_ERR_UNSUPPORTED : QLORA_OK;
 }
