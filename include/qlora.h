@@ -250,7 +250,7 @@ int qlora_lrec_loss(int T, int V, const void* student_logits, const void* teache
  * Other sums, maxima and losses are fp32 (a token that is almost certain keeps its small loss and gradient); probabilities are rounded to bf16 where they
  * enter the gradient's product, and weighed so that those of all rows of the head, less the label's, still add up to 0: what all rows share does not
  * reach the gradient.  The logits may be of any size; a block of 256 tokens is computed twice where one of them has a logit more than 83 above
- * the largest of its first 256.  A token with a NaN or +infinity among its logits has loss and gradient NaN; -infinity is a
+ * the largest of its first 256 (the label's apart).  A token with a NaN or +infinity among its logits has loss and gradient NaN; -infinity is a
  * probability of 0 (the label's: a loss of +infinity), and the gradient NaN at the features where the head's row is infinite.  Where d_loss is 0 the gradient is 0
  * whatever the token holds. */
 int qlora_head_loss_workspace_bytes(int T, int V, int D, int gradient, size_t* out);

@@ -3,7 +3,7 @@
 //
 // Two products, 2 T V D operations each, and nothing is computed twice: the probabilities of a piece of the vocabulary (4096 entries) go to the second
 // product as P = exp(z - ref), bf16, through a small ring that stays in L2, with one reference per token for the whole vocabulary, which is known
-// before the row's true maximum is: the largest of its first 256 logits and 40 ln 2 more.  The sums over the pieces then need no rescaling -- they are
+// before the row's true maximum is: the largest of its first 256 logits (the label's apart) and 40 ln 2 more.  The sums over the pieces then need no rescaling -- they are
 // divided by the row's sum of P at the end -- and bf16 has the range of fp32: nothing is lost while the row's maximum lies up to 120 ln 2 = 83 above
 // those first logits, and what flushes to zero is below 2^-86 of the largest.  A token whose largest logit lies further above is found at the end, and its
 // block of 256 tokens is computed again from its true maximum (by a second launch of the same kernel, which ends at once where there is none).
@@ -396,16 +396,21 @@ head_loss_kernel(const __grid_constant__ CUtensorMap tm_hidden, const __grid_con
             if (!poll(bar_acc_full + 8 * buffer, (n >> 1) & 1u, abort_flag)) break;
             tc_fence_after();
             if (GRAD && first) {
-                float m = -INFINITY;
+                // the others' alone: a label that is far above them would take the reference out of their reach
+                float m = -INFINITY, mine = -INFINITY;
 #pragma unroll 1
                 for (int idx = 0; idx < chunks; ++idx) {
                     uint32_t v[32];
                     tc_ld32(taddr + 32 * idx, v);
                     tc_wait_ld();
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (32 * idx + j < valid) m = fmaxf(m, __uint_as_float(v[j]));
+                    for (int j = 0; j < 32; ++j) {
+                        const float x = __uint_as_float(v[j]);
+                        if (32 * idx + j == label) mine = x;
+                        else if (32 * idx + j < valid) m = fmaxf(m, x);
+                    }
                 }
+                if (m == -INFINITY) m = mine;
                 ref = m == -INFINITY ? 0.f : fminf(m + REF_ABOVE, MOST);
                 __stcg(p.ref + row, ref);
                 publish(ref_known(p) + it.block);
