@@ -460,7 +460,9 @@ adapters_down_kernel(const Products p, int n_tiles) {
     extern __shared__ __align__(128) uint8_t smem[];
     auto& red = *reinterpret_cast<float (*)[DN_WARPS][NB][NT][4][32]>(smem);
     __shared__ int claimed, tokens[ROWS];                              // of a group: the number of a row's token, -1 for none
-    pdl_launch_dependents();                                           // (no wait: the sorting kernel lets this one in after its own)
+    // No wait ahead of the tiles: the sorting kernel lets this one begin after its own wait, when all kernels before it have completed and their writes lie in L2, which is
+    // where the tiles read everything from (asynchronous copies and loads past L1).  What the sorting kernel itself writes is waited for below.
+    pdl_launch_dependents();
     if (CTAS > 1) cluster_sync_all();                                  // (a block's shared memory is written to once it has begun)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int M = p.M, T = p.T, r = p.r;
@@ -521,7 +523,7 @@ adapters_down_kernel(const Products p, int n_tiles) {
     // The sums of one adapter's rows (mask) of the tile, or of a group.  begun: the first chunks of In are on their way.
     auto entry = [&](auto gathered, int adapter, uint32_t mask, bool begun) {
         const bf16* La = p.L1 + (size_t)adapter * r * T;
-        const float s = p.scales != nullptr ? __ldg(p.scales + adapter) : 0.f;
+        const float s = p.scales != nullptr ? __ldcg(p.scales + adapter) : 0.f;
         // two neighbouring ranks of a row
         auto take = [&](int idx, float v0, float v1) {
             const int b = idx / (NT * 64), nt = (idx >> 6) % NT, h = (idx >> 5) & 1, ln = idx & 31;
@@ -628,7 +630,7 @@ adapters_down_kernel(const Products p, int n_tiles) {
     };
     if ((int)blockIdx.x < n_tiles) {
         const bool in = lane < ROWS && m0 + lane < M;
-        int a = in ? __ldg(p.adapter_of + m0 + lane) : -1;
+        int a = in ? __ldcg(p.adapter_of + m0 + lane) : -1;
         for (int i = 0; i < STAGES - 1 && i < mine; ++i) load_in(i, of_tile);      // on their way while the tile's adapters are looked at
         if (a < 0 || a >= p.n_adapters) a = -1;
         const bool elsewhere = of_scattered_tile(a);
