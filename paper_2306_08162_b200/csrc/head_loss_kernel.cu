@@ -22,10 +22,11 @@
 // of the ring, the reference) it waits for through counters in the workspace; those items were claimed earlier, so the wait ends
 // whichever CTAs share the GPU.  Every wait is bounded.
 //
-// Bound by the tensor cores.  2048 tokens, 32000 entries, 4096 features, a launch by itself: the loss 338 us (1589 TFLOP/s, the pipe 87 % active), with the gradient
-// 698 us (1539), of which writing the probabilities is some 30 and adding to the sums 5; calls in a loop, under the power limit, 409 and 896 us in all.  Pieces of 2048 and 8192 entries:
-// 761 and 750 us; four stages 738.  The kernel that finishes takes 25 us beside that, the second launches 7.  Few tokens are bound by reading the head: 12 us and 6.0
-// TB/s (16 tokens 70 us for 262 MB).  Blocks of rows are whole: 520 tokens are 2.03 of them and cost 3.
+// Bound by the tensor cores.  2048 tokens, 32000 entries, 4096 features, a launch by itself: the loss 336 - 338 us (1590 TFLOP/s, the pipe 87 % active), with the gradient
+// 698 - 727 us (1477 - 1539), of which writing the probabilities is some 30 and adding to the sums 5; calls in a loop, under the power limit, 409 - 422 and 896 - 940 us in all,
+// by the GPU.  Pieces of 2048 and 8192 entries: 761 and 750 us where these take 698; four stages 738.  The kernel that finishes takes 23 - 25 us beside that, the second
+// launches 7.  Few tokens are bound by reading the head in whole tiles: 16 tokens 60 us for 262 MB (4.4 TB/s), 125 tiles in two rounds of 74 pairs, the second with
+// 51 of them reading, and 11 us of launches, preparing and finishing.  Blocks of rows are whole: 520 tokens are 2.03 of them and cost 3.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -58,7 +59,8 @@ constexpr uint32_t HL_SPINS = 1u << 26;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f, MOST = 3.402823466e38f;
 // The tensor cores cut their fp32 sums off towards zero at every step, which is an expected loss, not a random one: logits of random terms came out smaller by
 // 1.0e-9 of their size per contraction element (measured against 64-bit sums at 1024, within 12 %, and from 4096 to 262144, within 2 %;
-// below it drowns in fp32's own rounding).  The exponentials' scale takes the expected part back: mean error of a logit at 4096 elements 4e-6 -> 1e-8, at 16384 1.6e-5 -> 1.2e-7.
+// below it drowns in fp32's own rounding).  The exponentials' scale takes the expected part back: mean error of a logit at 4096 elements 4e-6 -> 2e-9, at 16384 1.6e-5 -> 1.2e-7;
+// of the losses at 4096, root of the mean square, 2.2e-6 -> 8e-7.
 // It is the wrong thing for other sums: exact ones (few features that are not zero, whole numbers) lose nothing and come out larger by it, and those whose terms
 // have one sign lose more (in all 3e-9 per element at 4096, 4.5e-9 at 16384).  So it grows with the length up to 16384 only, 1.6e-5 of a logit.
 constexpr float CUT_OFF = 1.0e-9f;
